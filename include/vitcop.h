@@ -54,6 +54,7 @@ extern "C" {
 #define VITCOP_OP_MERGE       7   /* vitcop_merge_clusters: Nv = Nv_cap, N = Mcap */
 #define VITCOP_OP_COLLAB_STEP 8   /* vitcop_collaborative_step */
 #define VITCOP_OP_KPROJ       9   /* vitcop_kproj_knorm: B, H, N, d */
+#define VITCOP_OP_CACHE_ATTENTION 10  /* vitcop_cache_attention: B, H = stored heads, N = Ncap, d, Nv = Tq, D = Hq */
 
 /* Human-readable name of a status code (static storage, never NULL). */
 const char* vitcop_status_string(int status);
@@ -318,6 +319,74 @@ int vitcop_kproj_knorm(const void* hidden, const void* W_k, int B, int N, int Dh
                        const float* rope_cos, const float* rope_sin, const int32_t* position_ids, int n_pos,
                        void* K_out, int vis_start, int Nv, float* score,
                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------- K/V cache in 4 bits
+ * The paper has no counterpart: it ends where the shortened sequence goes on through the model.  These three calls hold that
+ * sequence's K and V for the steps behind it, in 5 bits an element instead of 16: vitcop_cache_write quantises rows as it
+ * stores them (the rows that a pruning step keeps, a whole prompt, the token of a step), vitcop_cache_attention answers
+ * queries from the cache as it is, vitcop_cache_read gives rows back in bf16.
+ *
+ * A group is 32 elements of one row (one token of one head).  With lo, hi its smallest and largest element
+ *     s = bf16((hi - lo) / 15)      m = bf16(lo + 8 s)      code = clamp(round((x - m) / s) + 8, 0, 15)
+ * (round: to the nearest, ties to even) and the group stands for m + (code - 8) s.  s < 2^-100 counts as 0 (codes 8).  A group
+ * that holds a NaN or an infinity, or whose hi - lo passes the fp32 range, gets s = NaN and m = 0: all of it reads as NaN.
+ *
+ * cache: uint8 [B, H, Ncap / 32, 40 d], 16-byte aligned; Ncap a multiple of 32; d 64, 128 or 256.  A block holds 32 tokens r of
+ * a head, with G = d / 32, in little-endian words:
+ *     at  0    K codes   [r][t][g][4 bytes]   element 8 t + e of group g in nibble e (0 .. 7) of the word
+ *     at 16 d  K scales  bf16 s [r][g]
+ *     at 18 d  K centres bf16 m [r][g]
+ *     at 20 d  V codes   [r][u][g][2 bytes]   element 4 u + e of group g in nibble e (0 .. 3) of the half-word
+ *     at 36 d  V scales  bf16 s [r][g]
+ *     at 38 d  V centres bf16 m [g][r]
+ * Tokens share no byte: rows that a call does not write keep theirs, whether they were ever written or not.
+ * Sequence lengths live on the device (int32 [B]) where the calls before left them; negative ones count as 0, those above
+ * Ncap as Ncap.
+ *
+ * vitcop_cache_write stores rows of K and V at rows cache_len[b], cache_len[b] + 1, .. of the cache:
+ *   without keep_idx  the rows 0 .. seq_len[b] - 1 of K and V (vis_start, vis_len, vis_len_uniform, keep_stride, n_keep are not used)
+ *   with keep_idx     the rows that vitcop_compact_kv keeps, in its order: those in front of the visual span, the kept ones, those
+ *                     behind it (same arguments, same reading of them; keep_stride > 0)
+ *   K, V        bf16 [B, H, N, d], element (b,h,t,e) at K + b*k_stride_b + h*k_stride_h + t*k_stride_n + e (strides in elements,
+ *               multiples of 8, not negative); either may be NULL: its half of the cache is left as it is
+ *   seq_len     int32 [B] or NULL (= N for every sample)
+ *   cache_len   int32 [B] or NULL (= 0): rows that are in the cache already
+ *   new_len     int32 [B] out: cache_len[b] + rows of the sample, also where they did not all fit: rows from Ncap on are not
+ *               written.  Must not overlap cache_len or another input.
+ * Errors: INVALID_ARG (NULL cache/new_len, K and V both NULL, negative sizes or strides, span outside the sequence, overlap),
+ * UNSUPPORTED (d, Ncap % 32, alignment, more than 2^31 - 1 rows), CUDA. */
+int vitcop_cache_write(const void* K, const void* V, int B, int H, int N, int d,
+                       int64_t k_stride_b, int64_t k_stride_h, int64_t k_stride_n,
+                       int64_t v_stride_b, int64_t v_stride_h, int64_t v_stride_n,
+                       const int32_t* seq_len, int vis_start, const int32_t* vis_len, int vis_len_uniform,
+                       const int32_t* keep_idx, int keep_stride, const int32_t* n_keep,
+                       const int32_t* cache_len, void* cache, int Ncap, int32_t* new_len, void* stream);
+
+/* Row i of the outputs is row row_begin[b] + i of the cache, rounded to bf16, as far as that is below cache_len[b]; output rows
+ * behind that are left as they were.
+ *   cache_len  int32 [B] or NULL (= Ncap for every sample)
+ *   row_begin  int32 [B] (negative: 0) or NULL (= row_begin_uniform >= 0 for every sample)
+ *   K_out, V_out  bf16 [B, H, N_out, d]; either may be NULL; must not overlap the cache
+ * Errors: INVALID_ARG, UNSUPPORTED (as vitcop_cache_write), CUDA. */
+int vitcop_cache_read(const void* cache, int B, int H, int Ncap, int d, const int32_t* cache_len,
+                      const int32_t* row_begin, int row_begin_uniform, void* K_out, void* V_out, int N_out, void* stream);
+
+/* out = softmax(scale * q K^T) V over the rows of the cache that a query sees; logits, maximum, sum and output are held in fp32.
+ * Query head hq reads stored head hq / (Hq / H).  The Tq queries of a sample are the last Tq of its cache_len[b] tokens
+ * (their own K and V are in the cache already): with causal != 0 query t sees the first cache_len[b] - Tq + t + 1 rows, without it
+ * all cache_len[b].  A query that sees no row (an empty sample, more queries than rows) gets out = 0 and lse = -inf.
+ *   q, out  bf16 [B, Hq, Tq, d], element (b,h,t,e) at q + b*q_stride_b + h*q_stride_h + t*q_stride_t + e (strides in elements,
+ *           multiples of 8, not negative); out must not overlap q or the cache
+ *   cache_len  int32 [B] or NULL (= Ncap for every sample)
+ *   lse     fp32 [B, Hq, Tq] out, optional: log of the sum of exp(scale * q k) over the rows seen
+ *   workspace  vitcop_workspace_bytes(VITCOP_OP_CACHE_ATTENTION, B, H, Ncap, d, Tq, Hq, 0) bytes
+ * Errors: INVALID_ARG (NULL q/cache/out, negative sizes or strides, Hq no multiple of H, overlap), UNSUPPORTED (d, Ncap % 32,
+ * alignment, more than 2^31 - 1 query rows), WORKSPACE, CUDA. */
+int vitcop_cache_attention(const void* q, const void* cache, int B, int Hq, int H, int Tq, int d, int Ncap,
+                           int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_t,
+                           const int32_t* cache_len, float scale, int causal,
+                           void* out, int64_t out_stride_b, int64_t out_stride_h, int64_t out_stride_t, float* lse,
+                           void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------- schedule and cost model (host arithmetic)
  * Algorithm 1 prunes to floor(m * pi) tokens per stage (pi relative to the ORIGINAL m visual tokens); Appendix E

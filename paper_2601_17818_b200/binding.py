@@ -25,7 +25,7 @@ LIB_PATH = os.path.join(_PKG, "libvitcop.so")
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_BUDGET, ERR_CUDA, ERR_TIMEOUT = range(7)
 (OP_FILTER, OP_KNORM, OP_SELECT, OP_COMPACT, OP_PRUNE_STEP, OP_SIMILARITY, OP_SALIENCY, OP_MERGE, OP_COLLAB_STEP,
- OP_KPROJ) = range(10)
+ OP_KPROJ, OP_CACHE_ATTENTION) = range(11)
 MAX_VISUAL_TOKENS = 16384
 
 EXPORTS = [
@@ -35,13 +35,14 @@ EXPORTS = [
     "vitcop_prune_step_static", "vitcop_merge_clusters", "vitcop_cls_saliency", "vitcop_stage_count",
     "vitcop_flops_layer", "vitcop_visual_tokens_at_layer", "vitcop_flops_total", "vitcop_cr_int",
     "vitcop_collaborative_step", "vitcop_set_wait_limit", "vitcop_kproj_knorm",
+    "vitcop_cache_write", "vitcop_cache_read", "vitcop_cache_attention",
 ]
 
-# the calls of a pruning step, which go through the extension
+# the calls of a pruning step and of the cache behind it, which go through the extension
 NATIVE = [
     "vitcop_redundancy_filter", "vitcop_similarity_rows", "vitcop_knorm_score", "vitcop_select", "vitcop_compact_kv",
     "vitcop_prune_step", "vitcop_prune_step_static", "vitcop_merge_clusters", "vitcop_cls_saliency",
-    "vitcop_collaborative_step", "vitcop_kproj_knorm",
+    "vitcop_collaborative_step", "vitcop_kproj_knorm", "vitcop_cache_write", "vitcop_cache_read", "vitcop_cache_attention",
 ]
 
 
@@ -134,6 +135,11 @@ def lib() -> C.CDLL:
                                                 vp, vp, sz, vp]
         L.vitcop_set_wait_limit.argtypes = [C.c_ulonglong, i32]
         L.vitcop_kproj_knorm.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, i32, vp, i32, i32, vp, vp, sz, vp]
+        L.vitcop_cache_write.argtypes = [vp, vp, i32, i32, i32, i32, i64, i64, i64, i64, i64, i64, vp, i32, vp, i32, vp, i32, vp, vp, vp,
+                                         i32, vp, vp]
+        L.vitcop_cache_read.argtypes = [vp, i32, i32, i32, i32, vp, vp, i32, vp, vp, i32, vp]
+        L.vitcop_cache_attention.argtypes = [vp, vp, i32, i32, i32, i32, i32, i32, i64, i64, i64, vp, C.c_float, i32, vp, i64, i64, i64,
+                                             vp, vp, sz, vp]
         L.vitcop_kernel_timing_begin.argtypes = []
         L.vitcop_kernel_timing_end.argtypes = [C.POINTER(KernelTime), i32, C.POINTER(C.c_int)]
         for name in EXPORTS:
@@ -320,6 +326,97 @@ def vitcop_kproj_knorm(hidden, W_k, H: int, d: int, K_out, workspace, vis_start:
     _call("vitcop_kproj_knorm", hidden, W_k, B, N, Dh, H, d, rope_cos, rope_sin, position_ids, n_pos, K_out, int(vis_start), Nv,
           score, workspace, workspace.numel())
     return K_out
+
+
+def alloc_cache(B: int, H: int, Ncap: int, d: int, device="cuda") -> torch.Tensor:
+    """An uninitialised cache for ``Ncap`` rows (a multiple of 32) of H heads of d elements: uint8 [B, H, Ncap / 32, 40 d]."""
+    if Ncap % 32 or d not in (64, 128, 256):
+        raise ValueError("a cache holds a multiple of 32 rows of 64, 128 or 256 elements")
+    return torch.empty((B, H, Ncap // 32, 40 * d), dtype=torch.uint8, device=device)
+
+
+def _rows(t, what: str, shape=None):
+    """Data pointer and strides of bf16 rows [B, H, N, d] on the current device, elements of a row side by side; dimensions of
+    extent 1 have no stride."""
+    if t is None:
+        return 0, 0, 0, 0
+    if not t.is_cuda or t.get_device() != _device():
+        raise ValueError(f"{what}: expected a tensor on the current CUDA device")
+    if t.dtype != torch.bfloat16 or t.dim() != 4 or (t.stride(3) != 1 and t.numel() > 0) or (shape is not None and tuple(t.shape) != shape):
+        raise ValueError(f"{what}: expected bf16 [B, H, N, d]{'' if shape is None else ' = ' + str(shape)}, elements of a row side by side")
+    (b, h, n, _), (sb, sh, sn, _) = t.shape, t.stride()
+    return t.data_ptr(), sb if b > 1 else 0, sh if h > 1 else 0, sn if n > 1 else 0
+
+
+def _dense(t, what: str, dtype, shape):
+    """Checks an optional dense tensor on the current device; a dimension of -1 may have any extent."""
+    if t is None:
+        return
+    if not t.is_cuda or t.get_device() != _device():
+        raise ValueError(f"{what}: expected a tensor on the current CUDA device")
+    if t.dtype != dtype or t.dim() != len(shape) or any(n not in (-1, m) for n, m in zip(shape, t.shape)) or not t.is_contiguous():
+        raise ValueError(f"{what}: expected contiguous {dtype} {list(shape)}")
+
+
+def _cache_dims(cache):
+    _dense(cache, "cache", torch.uint8, (-1, -1, -1, -1))
+    B, H, blocks, width = cache.shape
+    if width % 40:
+        raise ValueError("cache: expected uint8 [B, H, Ncap / 32, 40 d]")
+    return B, H, blocks * 32, width // 40
+
+
+def vitcop_cache_write(K, V, cache, new_len, cache_len=None, seq_len=None, vis_start: int = 0, vis_len=0, keep_idx=None, n_keep=None):
+    """Rows of K and V (bf16 [B,H,N,d], any leading strides) to ``cache`` in 4 bits, from row ``cache_len`` on: all of them, or with
+    ``keep_idx`` those that ``vitcop_compact_kv`` keeps.  Returns ``new_len``, the rows that are in the cache then."""
+    B, H, Ncap, d = _cache_dims(cache)
+    ref = K if K is not None else V
+    if ref is None or ref.dim() != 4:
+        raise ValueError("K or V: expected bf16 [B, H, N, d]")
+    N = ref.shape[2]
+    k, kb, kh, kn = _rows(K, "K", (B, H, N, d))
+    v, vb_, vh, vn = _rows(V, "V", (B, H, N, d))
+    for t, what in ((new_len, "new_len"), (cache_len, "cache_len"), (seq_len, "seq_len"), (n_keep, "n_keep")):
+        _dense(t, what, torch.int32, (B,))
+    _dense(keep_idx, "keep_idx", torch.int32, (B, -1))
+    vp, vu = _vis(vis_len)
+    _dense(vp, "vis_len", torch.int32, (B,))
+    _call("vitcop_cache_write", k, v, B, H, N, d, kb, kh, kn, vb_, vh, vn, seq_len, int(vis_start), vp, vu, keep_idx,
+          0 if keep_idx is None else keep_idx.shape[1], n_keep, cache_len, cache, Ncap, new_len)
+    return new_len
+
+
+def vitcop_cache_read(cache, cache_len, K_out=None, V_out=None, row_begin=0):
+    """Rows of ``cache`` from ``row_begin`` (an int, or int32 [B]) on, up to ``cache_len`` (None: all), to bf16 [B,H,N_out,d]."""
+    B, H, Ncap, d = _cache_dims(cache)
+    ref = K_out if K_out is not None else V_out
+    if ref is None or ref.dim() != 4:
+        raise ValueError("K_out or V_out: expected bf16 [B, H, N_out, d]")
+    N_out = ref.shape[2]
+    for t, what in ((K_out, "K_out"), (V_out, "V_out")):
+        _dense(t, what, torch.bfloat16, (B, H, N_out, d))
+    _dense(cache_len, "cache_len", torch.int32, (B,))
+    bp, bu = _vis(row_begin)
+    _dense(bp, "row_begin", torch.int32, (B,))
+    _call("vitcop_cache_read", cache, B, H, Ncap, d, cache_len, bp, bu, K_out, V_out, N_out)
+    return K_out, V_out
+
+
+def vitcop_cache_attention(q, cache, cache_len, out, workspace, scale: float, causal: bool = True, lse=None):
+    """softmax(scale q K^T) V over ``cache``: q, out bf16 [B,Hq,Tq,d] (any leading strides), the last Tq of ``cache_len`` tokens."""
+    B, H, Ncap, d = _cache_dims(cache)
+    if q.dim() != 4:
+        raise ValueError("q: expected bf16 [B, Hq, Tq, d]")
+    Hq, Tq = q.shape[1], q.shape[2]
+    shape = (B, Hq, Tq, d)
+    qp, qb, qh, qt = _rows(q, "q", shape)
+    op, ob, oh, ot = _rows(out, "out", shape)
+    _dense(cache_len, "cache_len", torch.int32, (B,))
+    _dense(lse, "lse", torch.float32, (B, Hq, Tq))
+    _dense(workspace, "workspace", torch.uint8, (-1,))
+    _call("vitcop_cache_attention", qp, cache, B, Hq, H, Tq, d, Ncap, qb, qh, qt, cache_len, int(causal), op, ob, oh, ot, lse, workspace,
+          workspace.numel(), scale=scale)
+    return out
 
 
 def vitcop_stage_count(m: int, pi: float) -> int:

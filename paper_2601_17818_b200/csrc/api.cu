@@ -8,6 +8,7 @@
 
 #include "gram.cuh"
 #include "internal.cuh"
+#include "kv_cache.cuh"
 
 namespace vitcop {
 
@@ -210,6 +211,10 @@ int vitcop_workspace_bytes(int op, int B, int H, int N, int d, int Nv, int D, in
         case VITCOP_OP_SALIENCY:
             if (H < 0 || N < 0) return VITCOP_ERR_INVALID_ARG;
             *bytes = saliency_workspace_bytes(B, H, N);
+            return VITCOP_OK;
+        case VITCOP_OP_CACHE_ATTENTION:
+            if (H < 0 || N < 0 || d < 0) return VITCOP_ERR_INVALID_ARG;
+            *bytes = cache_attention_workspace_bytes(B, H, N, d, Nv, D);
             return VITCOP_OK;
         default: return VITCOP_ERR_INVALID_ARG;
     }
@@ -448,6 +453,104 @@ int vitcop_kproj_knorm(const void* hidden, const void* W_k, int B, int N, int Dh
     if (B == 0 || N == 0 || H == 0 || d == 0 || Dh == 0) return reset_status(workspace, s);
     return launch_kproj_knorm(hidden, W_k, B, N, Dh, H, d, rope_cos, rope_sin, position_ids, n_pos, K_out, vis_start,
                               score ? Nv : 0, score, workspace, s);
+}
+
+// Bytes that a tensor [B, H, N, d] of 2-byte elements with these strides (elements, not negative) reaches over.
+static size_t extent(int B, int H, int N, int d, int64_t sb, int64_t sh, int64_t sn) {
+    if (B <= 0 || H <= 0 || N <= 0 || d <= 0) return 0;
+    return ((size_t)(B - 1) * (size_t)sb + (size_t)(H - 1) * (size_t)sh + (size_t)(N - 1) * (size_t)sn + (size_t)d) * 2;
+}
+
+static int check_cache(int Ncap, int d, const void* cache) {
+    if ((d != 64 && d != 128 && d != 256) || Ncap % kCacheBlock || !aligned16(cache)) return VITCOP_ERR_UNSUPPORTED;
+    return VITCOP_OK;
+}
+
+int vitcop_cache_write(const void* K, const void* V, int B, int H, int N, int d, int64_t k_stride_b, int64_t k_stride_h,
+                       int64_t k_stride_n, int64_t v_stride_b, int64_t v_stride_h, int64_t v_stride_n, const int32_t* seq_len,
+                       int vis_start, const int32_t* vis_len, int vis_len_uniform, const int32_t* keep_idx, int keep_stride,
+                       const int32_t* n_keep, const int32_t* cache_len, void* cache, int Ncap, int32_t* new_len, void* stream) {
+    if ((!K && !V && N > 0) || !cache || !new_len || B < 0 || H < 0 || N < 0 || d < 0 || Ncap < 0) return VITCOP_ERR_INVALID_ARG;
+    const int64_t strides[6] = {k_stride_b, k_stride_h, k_stride_n, v_stride_b, v_stride_h, v_stride_n};
+    for (int i = 0; i < 6; ++i)
+        if (strides[i] < 0) return VITCOP_ERR_INVALID_ARG;
+    if (keep_idx) {
+        if (!n_keep || keep_stride <= 0) return VITCOP_ERR_INVALID_ARG;
+        const int rc = check_span(N, vis_start, vis_len, vis_len_uniform, -1);
+        if (rc != VITCOP_OK) return rc;
+    }
+    const int rc = check_cache(Ncap, d, cache);
+    if (rc != VITCOP_OK) return rc;
+    for (int i = 0; i < 6; ++i)
+        if (strides[i] % 8 && (i < 3 ? K : V)) return VITCOP_ERR_UNSUPPORTED;
+    if (!aligned16(K) || !aligned16(V) || B > 65535) return VITCOP_ERR_UNSUPPORTED;
+    const size_t kbytes = K ? extent(B, H, N, d, k_stride_b, k_stride_h, k_stride_n) : 0;
+    const size_t vbytes = V ? extent(B, H, N, d, v_stride_b, v_stride_h, v_stride_n) : 0;
+    const size_t cbytes = cache_bytes(B, H, Ncap, d), lens = (size_t)B * sizeof(int32_t);
+    const size_t list = keep_idx ? (size_t)B * keep_stride * sizeof(int32_t) : 0;
+    if (overlaps(K, kbytes, cache, cbytes) || overlaps(V, vbytes, cache, cbytes)) return VITCOP_ERR_INVALID_ARG;
+    const void* ins[] = {K, V, cache_len, seq_len, keep_idx ? vis_len : nullptr, keep_idx, keep_idx ? n_keep : nullptr, cache};
+    const size_t insz[] = {kbytes, vbytes, lens, lens, lens, list, lens, cbytes};
+    for (int i = 0; i < 8; ++i)
+        if (overlaps(ins[i], insz[i], new_len, lens)) return VITCOP_ERR_INVALID_ARG;
+    for (int i = 2; i < 7; ++i)
+        if (overlaps(ins[i], insz[i], cache, cbytes)) return VITCOP_ERR_INVALID_ARG;
+    const auto bf16 = [](const void* p) { return static_cast<const __nv_bfloat16*>(p); };
+    const CacheSource src = {bf16(K), bf16(V), k_stride_b, k_stride_h, k_stride_n, v_stride_b, v_stride_h, v_stride_n};
+    const CacheRows rows = {seq_len, vis_start, vis_len, vis_len_uniform, keep_idx, keep_stride, n_keep};
+    return launch_cache_write(src, rows, B, H, N, d, cache_len, cache, Ncap, new_len, static_cast<cudaStream_t>(stream));
+}
+
+int vitcop_cache_read(const void* cache, int B, int H, int Ncap, int d, const int32_t* cache_len, const int32_t* row_begin,
+                      int row_begin_uniform, void* K_out, void* V_out, int N_out, void* stream) {
+    if (!cache || (!K_out && !V_out && N_out > 0) || B < 0 || H < 0 || Ncap < 0 || d < 0 || N_out < 0) return VITCOP_ERR_INVALID_ARG;
+    if (!row_begin && row_begin_uniform < 0) return VITCOP_ERR_INVALID_ARG;
+    const int rc = check_cache(Ncap, d, cache);
+    if (rc != VITCOP_OK) return rc;
+    if (!aligned16(K_out) || !aligned16(V_out) || B > 65535) return VITCOP_ERR_UNSUPPORTED;
+    const size_t cbytes = cache_bytes(B, H, Ncap, d), obytes = (size_t)B * H * N_out * d * 2, lens = (size_t)B * sizeof(int32_t);
+    void* outs[] = {K_out, V_out};
+    for (void* out : outs)
+        if (overlaps(cache, cbytes, out, obytes) || overlaps(cache_len, lens, out, obytes) || overlaps(row_begin, lens, out, obytes))
+            return VITCOP_ERR_INVALID_ARG;
+    if (overlaps(K_out, obytes, V_out, obytes)) return VITCOP_ERR_INVALID_ARG;
+    return launch_cache_read(cache, B, H, Ncap, d, cache_len, row_begin, row_begin_uniform, K_out, V_out, N_out,
+                             static_cast<cudaStream_t>(stream));
+}
+
+int vitcop_cache_attention(const void* q, const void* cache, int B, int Hq, int H, int Tq, int d, int Ncap, int64_t q_stride_b,
+                           int64_t q_stride_h, int64_t q_stride_t, const int32_t* cache_len, float scale, int causal, void* out,
+                           int64_t out_stride_b, int64_t out_stride_h, int64_t out_stride_t, float* lse, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+    if (!q || !cache || !out || B < 0 || Hq < 0 || H < 0 || Tq < 0 || d < 0 || Ncap < 0) return VITCOP_ERR_INVALID_ARG;
+    if (H > 0 ? Hq % H != 0 : Hq != 0) return VITCOP_ERR_INVALID_ARG;
+    const int64_t strides[6] = {q_stride_b, q_stride_h, q_stride_t, out_stride_b, out_stride_h, out_stride_t};
+    for (int i = 0; i < 6; ++i)
+        if (strides[i] < 0) return VITCOP_ERR_INVALID_ARG;
+    const int rc = check_cache(Ncap, d, cache);
+    if (rc != VITCOP_OK) return rc;
+    for (int i = 0; i < 6; ++i)
+        if (strides[i] % 8) return VITCOP_ERR_UNSUPPORTED;
+    if (!aligned16(q) || !aligned16(out) || B > 65535) return VITCOP_ERR_UNSUPPORTED;
+    // (rows of the output that share elements have no value)
+    if ((B > 1 && out_stride_b < d) || (Hq > 1 && out_stride_h < d) || (Tq > 1 && out_stride_t < d)) return VITCOP_ERR_INVALID_ARG;
+    if ((int64_t)B * Hq * Tq > 0x7fffffff) return VITCOP_ERR_UNSUPPORTED;
+    const size_t need = cache_attention_workspace_bytes(B, H, Ncap, d, Tq, Hq);
+    const size_t obytes = extent(B, Hq, Tq, d, out_stride_b, out_stride_h, out_stride_t);
+    const size_t rows = (size_t)B * Hq * Tq * sizeof(float), lens = (size_t)B * sizeof(int32_t);
+    const void* ins[] = {q, cache, cache_len};
+    const size_t insz[] = {extent(B, Hq, Tq, d, q_stride_b, q_stride_h, q_stride_t), cache_bytes(B, H, Ncap, d), lens};
+    for (int i = 0; i < 3; ++i)
+        if (overlaps(ins[i], insz[i], out, obytes) || overlaps(ins[i], insz[i], lse, rows) || overlaps(ins[i], insz[i], workspace, need))
+            return VITCOP_ERR_INVALID_ARG;
+    if (overlaps(out, obytes, lse, rows) || overlaps(out, obytes, workspace, need) || overlaps(lse, rows, workspace, need))
+        return VITCOP_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < need || !aligned256(workspace)) return VITCOP_ERR_WORKSPACE;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (B == 0 || Hq == 0 || Tq == 0) return reset_status(workspace, s);
+    const CacheQueries io = {static_cast<const __nv_bfloat16*>(q), static_cast<__nv_bfloat16*>(out), q_stride_b, q_stride_h, q_stride_t,
+                             out_stride_b, out_stride_h, out_stride_t};
+    return launch_cache_attention(io, cache, B, Hq, H, Tq, d, Ncap, cache_len, scale, causal != 0, lse, workspace, s);
 }
 
 int vitcop_prune_step_static(const void* hidden, const void* K, const void* V, int B, int H, int N, int d, int Dh,

@@ -66,7 +66,8 @@ struct Entry {
 Entry entries[] = {
     ENTRY(vitcop_knorm_score), ENTRY(vitcop_select), ENTRY(vitcop_compact_kv), ENTRY(vitcop_prune_step),
     ENTRY(vitcop_prune_step_static), ENTRY(vitcop_collaborative_step), ENTRY(vitcop_merge_clusters),
-    ENTRY(vitcop_cls_saliency), ENTRY(vitcop_kproj_knorm), ENTRY(vitcop_redundancy_filter), ENTRY(vitcop_similarity_rows)};
+    ENTRY(vitcop_cls_saliency), ENTRY(vitcop_kproj_knorm), ENTRY(vitcop_redundancy_filter), ENTRY(vitcop_similarity_rows),
+    ENTRY(vitcop_cache_write), ENTRY(vitcop_cache_read), ENTRY(vitcop_cache_attention)};
 constexpr int kEntries = sizeof(entries) / sizeof(entries[0]);
 
 bool to_word(PyObject* o, int64_t& v) {
