@@ -1,99 +1,665 @@
 // Attention of query rows over the K/V cache in 4 bits: out = softmax(scale q K^T) V over the rows that a query sees.
 //
-// A CTA takes one query row; its warps share out the tokens, keep their own maximum, sum and output of the softmax, and join them.
+// The query rows of a stored head (Hq / H heads times Tq queries, a tile of 8 NT of them at a time) are the narrow side of every
+// matrix product (m16n8k16, bf16 in, fp32 out), tokens and then elements the wide one; codes become operands in registers:
+//   logits   a code c is the bf16 128 + c (its nibble under the exponent of 128), exactly.  Per group the product starts from
+//            -136 sum(q), so that it ends as sum((c - 8) q), which the group's scale multiplies in fp32; the centres are one
+//            more product, with sum(q) split into three bf16
+//   output   (128 + c) - 136 = c - 8 is exact too; the weight enters as bf16(p s) for each group, and bf16(p) with the centres
+// A warp takes every fourth block of 32 tokens of its CTA's piece, with blocks ahead in shared memory (cp.async), and keeps maximum, sum
+// and output of its own; the CTA joins its warps, a second kernel joins the CTAs that shared a head.
+#include <cuda_bf16.h>
+
+#include "async_copy.cuh"
 #include "f32x2.cuh"
 #include "kv_cache.cuh"
 
 namespace vitcop {
 namespace {
 
-constexpr int kAttWarps = 4;
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kWarps = 4;
+constexpr int kStages = 2;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+#define MINUS_INF (-__builtin_huge_valf())
 
-__device__ __forceinline__ float ld_bf16(const uint8_t* p) { return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(p) << 16); }
+// Resident CTAs an SM, which the registers of the accumulators and the ring's memory leave room for.
+constexpr int ctas_per_sm(int D, int NT) { return D == 256 || NT == 4 ? 2 : D * NT <= 128 ? 4 : 3; }
 
-template <int D>
-__global__ void __launch_bounds__(kAttWarps * 32)
-cache_attention_kernel(CacheQueries io, const uint8_t* cache, int Hq, int H, int Tq, int Ncap, const int32_t* cache_len,
-                       float scale, int causal, float* lse, int* status) {
-    using L = CacheBlock<D>;
-    constexpr int G = L::G;
-    grid_dependency_wait();
-    if (blockIdx.x == 0 && threadIdx.x == 0) *status = VITCOP_OK;
-    const int tq = blockIdx.x % Tq, bq = blockIdx.x / Tq, hq = bq % Hq, b = bq / Hq, h = hq / (Hq / H);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int len = cache_len ? max(0, min(cache_len[b], Ncap)) : Ncap;
-    const int limit = causal ? max(0, len - Tq + tq + 1) : len;
-    const uint8_t* const head = cache + ((int64_t)b * H + h) * (Ncap / kCacheBlock) * L::kBytes;
-    float q[G], o[G] = {}, mx = -__builtin_huge_valf(), sum = 0.f;
+struct AttArgs {
+    CacheQueries io;
+    const uint8_t* cache;
+    const int32_t* cache_len;
+    float* lse;
+    int* status;
+    int32_t* before;                                       // shares: blocks in front of each sample, [B + 1]
+    float* part;                                           // shares: two pieces a CTA, each [8 NT][D + 2]
+    int B, Hq, H, R, Tq, Ncap, RT, causal;
+    float scale_log2;
+};
+
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {   // an 8 x 8 matrix of 16-bit values, two of a row in a lane
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t code_pair(uint32_t w) { return (w & 0x000F000Fu) | 0x43004300u; }   // 128 + c, twice
+__device__ __forceinline__ uint32_t centred(uint32_t pair) {                                              // c - 8, twice
+    uint32_t r;
+    asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(pair), "r"(0xC308C308u));
+    return r;
+}
+template <int BYTES>
+__device__ __forceinline__ void lds(uint32_t* w, const uint8_t* p) {
+    if constexpr (BYTES >= 16) {
 #pragma unroll
-    for (int g = 0; g < G; ++g) q[g] = __bfloat162float(io.q[b * io.qb + hq * io.qh + tq * io.qt + g * 32 + lane]) * scale;
-    for (int j = warp; j < limit; j += kAttWarps) {
-        const uint8_t* const block = head + (int64_t)(j / kCacheBlock) * L::kBytes;
-        const int row = j % kCacheBlock;
-        float s = 0.f;
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-            const int byte = block[L::kKCodes + row * (D / 2) + lane / 8 * 4 * G + g * 4 + lane % 8 / 2];
-            const float c = (float)((byte >> (lane % 2 * 4) & 15) - 8);
-            s = fmaf(q[g], fmaf(c, ld_bf16(block + L::kKScale + (row * G + g) * 2), ld_bf16(block + L::kKCentre + (row * G + g) * 2)), s);
+        for (int i = 0; i < BYTES / 16; ++i) {
+            const uint4 v = *reinterpret_cast<const uint4*>(p + 16 * i);
+            w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
         }
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-        const float top = fmaxf(mx, s), keep = mx == top ? 1.f : exp2f((mx - top) * kLog2e), p = exp2f((s - top) * kLog2e);
-        mx = top;
-        sum = fmaf(sum, keep, p);
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-            const int byte = block[L::kVCodes + row * (D / 2) + lane / 4 * 2 * G + g * 2 + lane % 4 / 2];
-            const float c = (float)((byte >> (lane % 2 * 4) & 15) - 8);
-            const float v = fmaf(c, ld_bf16(block + L::kVScale + (row * G + g) * 2), ld_bf16(block + L::kVCentre + (g * 32 + row) * 2));
-            o[g] = fmaf(o[g], keep, p * v);
-        }
+    } else if constexpr (BYTES == 8) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        w[0] = v.x; w[1] = v.y;
+    } else {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
     }
-    __shared__ float wmax[kAttWarps], wsum[kAttWarps], wout[kAttWarps][D];
-    if (lane == 0) {
-        wmax[warp] = mx;
-        wsum[warp] = sum;
-    }
-#pragma unroll
-    for (int g = 0; g < G; ++g) wout[warp][g * 32 + lane] = o[g];
-    __syncthreads();
-    float top = -__builtin_huge_valf(), total = 0.f;
-    for (int w = 0; w < kAttWarps; ++w) top = fmaxf(top, wmax[w]);
-    float f[kAttWarps];
-    for (int w = 0; w < kAttWarps; ++w) {
-        f[w] = wmax[w] == top ? 1.f : exp2f((wmax[w] - top) * kLog2e);
-        total += wsum[w] * f[w];
-    }
-    for (int e = threadIdx.x; e < D; e += kAttWarps * 32) {
-        float v = 0.f;
-        for (int w = 0; w < kAttWarps; ++w) v = fmaf(wout[w][e], f[w], v);
-        io.out[b * io.ob + hq * io.oh + tq * io.ot + e] = __float2bfloat16_rn(limit > 0 ? v / total : 0.f);
-    }
-    if (lse && threadIdx.x == 0) lse[((int64_t)b * Hq + hq) * Tq + tq] = limit > 0 ? top + logf(total) : -__builtin_huge_valf();
 }
 
-}  // namespace
+// Eight query rows as the narrow operand, one lane's part: its eight elements of each group of row g, -136 times the groups' sums of
+// rows 2 t and 2 t + 1, and the sums of row g in three bf16 each (part p of group i is element p G + i of the product with the centres).
+template <int G>
+struct __align__(16) QueryOperand {
+    uint32_t q[G][4];
+    float start[G][2];
+    uint32_t sums[4];
+};
+template <int G>
+__device__ __forceinline__ void load_queries(QueryOperand<G>& to, const __nv_bfloat16* src, bool there, int t) {
+    float total[G];
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+        const uint4 v = there ? __ldg(reinterpret_cast<const uint4*>(src + t * 8 + i * 32)) : make_uint4(0, 0, 0, 0);
+        to.q[i][0] = __byte_perm(v.x, v.z, 0x5410);        // elements 0 and 4, 1 and 5, 2 and 6, 3 and 7, as the codes lie
+        to.q[i][1] = __byte_perm(v.x, v.z, 0x7632);
+        to.q[i][2] = __byte_perm(v.y, v.w, 0x5410);
+        to.q[i][3] = __byte_perm(v.y, v.w, 0x7632);
+        float x = ((bf16lo(v.x) + bf16hi(v.x)) + (bf16lo(v.y) + bf16hi(v.y))) + ((bf16lo(v.z) + bf16hi(v.z)) + (bf16lo(v.w) + bf16hi(v.w)));
+        x += __shfl_xor_sync(0xffffffffu, x, 1);
+        x += __shfl_xor_sync(0xffffffffu, x, 2);
+        total[i] = x;
+        to.start[i][0] = -136.f * __shfl_sync(0xffffffffu, x, 8 * t);
+        to.start[i][1] = -136.f * __shfl_sync(0xffffffffu, x, 8 * t + 4);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float v[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int k = 2 * t + 8 * i + e, p = k / G;
+            float x = 0.f;
+#pragma unroll
+            for (int j = 0; j < G; ++j)
+                if (k % G == j) x = total[j];
+            const float first = __bfloat162float(__float2bfloat16_rn(x)), second = __bfloat162float(__float2bfloat16_rn(x - first));
+            v[e] = p == 0 ? first : p == 1 ? second : p == 2 ? (x - first) - second : 0.f;
+        }
+        to.sums[i] = bf16x2(v[0], v[1]);
+    }
+}
 
-size_t cache_attention_workspace_bytes(int, int, int, int, int, int) { return kStatusBytes; }
+// Where a CTA is in its share of the work: block `tile` of segment `seg` (head and tile of rows) of sample b, `left` blocks to go.
+struct Walk {
+    int b, seg, tile, blocks, left;
+};
+__device__ __forceinline__ int blocks_of(const AttArgs& a, int b) {
+    const int len = a.cache_len ? max(0, min(__ldg(a.cache_len + b), a.Ncap)) : a.Ncap;
+    return (len + kCacheBlock - 1) / kCacheBlock;
+}
+// CTAs that `total` blocks are shared out to: each has a block for every warp, or there is one CTA.
+__device__ __forceinline__ int sharers(int64_t total, int ctas) {
+    return (int)max((int64_t)1, min((int64_t)ctas, total / kWarps));
+}
+__device__ __forceinline__ int piece(const Walk& w) { return min(w.blocks - w.tile, w.left); }
 
-int launch_cache_attention(const CacheQueries& io, const void* cache, int B, int Hq, int H, int Tq, int d, int Ncap,
-                           const int32_t* cache_len, float scale, bool causal, float* lse, void* workspace, cudaStream_t stream) {
-    if ((int64_t)B * Hq * Tq > 0x7fffffff) return VITCOP_ERR_UNSUPPORTED;
+template <int D, int NT, bool SHARES>
+__global__ void __launch_bounds__(kWarps * 32, ctas_per_sm(D, NT))
+cache_attention_kernel(AttArgs a) {
+    using L = CacheBlock<D>;
+    constexpr int G = L::G, NR = 8 * NT;
+    constexpr int kChunks = L::kBytes / 16;
+    extern __shared__ __align__(128) uint8_t smem[];
+    float* const join = reinterpret_cast<float*>(smem + kWarps * kStages * L::kBytes);      // [warp][2 groups][8][lane]
+    float* const join_max = join + kWarps * 512;                                            // [warp][NR]
+    float* const join_sum = join_max + kWarps * NR;
+    QueryOperand<G>* const operand = reinterpret_cast<QueryOperand<G>*>(join_sum + kWarps * NR);      // [NT][lane] where NT > 1
+    int32_t* const before = reinterpret_cast<int32_t*>(operand + (NT > 1 ? NT * 32 : 0));             // [B + 1]
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const int segs = a.H * a.RT;
+    grid_dependency_wait();
+    if constexpr (SHARES) grid_dependency_launch_dependents();     // (the join's CTAs, which wait for this grid to end)
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = VITCOP_OK;
+
+    Walk now;
+    if constexpr (SHARES) {
+        // blocks in front of each sample
+        if (warp == 0) {
+            int sum = 0;
+            for (int b0 = 0; b0 < a.B; b0 += 32) {
+                int v = b0 + lane < a.B ? blocks_of(a, b0 + lane) : 0;
+                const int mine = v;
+#pragma unroll
+                for (int off = 1; off < 32; off <<= 1) {
+                    const int u = __shfl_up_sync(0xffffffffu, v, off);
+                    if (lane >= off) v += u;
+                }
+                if (b0 + lane < a.B) before[b0 + lane] = sum + v - mine;
+                sum += __shfl_sync(0xffffffffu, v, 31);
+            }
+            if (lane == 0) before[a.B] = sum;
+        }
+        __syncthreads();
+        if (blockIdx.x == 0)
+            for (int i = threadIdx.x; i <= a.B; i += kWarps * 32) a.before[i] = before[i];
+        const int64_t total = (int64_t)before[a.B] * segs;
+        const int ctas = sharers(total, gridDim.x);
+        if (total == 0 || (int)blockIdx.x >= ctas) return;
+        const int64_t from = total * blockIdx.x / ctas, to = total * (blockIdx.x + 1) / ctas;
+        int lo = 0, hi = a.B;                              // the last sample that starts at or before `from` and has blocks
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if ((int64_t)before[mid] * segs <= from) lo = mid; else hi = mid;
+        }
+        now.b = lo;
+        now.blocks = before[lo + 1] - before[lo];
+        const int64_t in = from - (int64_t)before[lo] * segs;
+        now.seg = (int)(in / now.blocks);
+        now.tile = (int)(in - (int64_t)now.seg * now.blocks);
+        now.left = (int)(to - from);
+    } else {
+        now.b = blockIdx.x / segs;
+        now.seg = blockIdx.x - now.b * segs;
+        now.tile = 0;
+        now.blocks = blocks_of(a, now.b);
+        now.left = now.blocks;
+    }
+    const auto next = [&](Walk& w) {                       // to the piece behind
+        w.left -= piece(w);
+        w.tile = 0;
+        if (++w.seg == segs) {
+            w.seg = 0;
+            if constexpr (SHARES)
+                if (w.left > 0) do { ++w.b; w.blocks = before[w.b + 1] - before[w.b]; } while (w.blocks == 0);
+        }
+    };
+    // the sequence's blocks ahead of their use: this warp's share of every piece
+    Walk ahead = now;
+    int ahead_at = warp;
+    uint8_t* const ring = smem + warp * kStages * L::kBytes;
+    int fill = 0;
+    const auto fetch = [&]() {
+        while (ahead.left > 0 && ahead_at >= piece(ahead)) {
+            next(ahead);
+            ahead_at = warp;
+        }
+        if (ahead.left > 0) {
+            const uint8_t* const src = a.cache + (((int64_t)ahead.b * a.H + ahead.seg / a.RT) * (a.Ncap / kCacheBlock) + ahead.tile + ahead_at) * L::kBytes;
+            const uint32_t dst = smem_u32(ring + fill * L::kBytes);
+#pragma unroll
+            for (int i = 0; i < kChunks / 32; ++i)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (i * 32 + lane) * 16), "l"(src + (i * 32 + lane) * 16) : "memory");
+            ahead_at += kWarps;
+            fill = fill + 1 == kStages ? 0 : fill + 1;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int i = 0; i < kStages; ++i) fetch();
+    int use = 0;
+
+    for (bool first = true; first || now.left > 0; first = false) {
+        const int b = now.b, h = now.seg / a.RT, row0 = (now.seg - h * a.RT) * NR, rows = a.R * a.Tq;
+        const int count = piece(now);
+        const int len = a.cache_len ? max(0, min(__ldg(a.cache_len + b), a.Ncap)) : a.Ncap;
+        QueryOperand<G> own;
+        if constexpr (NT == 1) {
+            const int r = row0 + g, tq = r / a.R, hq = h * a.R + (r - tq * a.R);
+            load_queries<G>(own, a.io.q + b * a.io.qb + hq * a.io.qh + tq * a.io.qt, r < rows, t);
+        } else {
+            if (warp < NT) {
+                const int r = row0 + warp * 8 + g, tq = r / a.R, hq = h * a.R + (r - tq * a.R);
+                load_queries<G>(own, a.io.q + b * a.io.qb + hq * a.io.qh + tq * a.io.qt, r < rows, t);
+                operand[warp * 32 + lane] = own;
+            }
+            __syncthreads();
+        }
+        float o[NT][G][2][4], oc[NT][4], top[NT][2], sum[NT][2];
+        int limit[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int rc = row0 + n * 8 + 2 * t + e;
+                limit[n][e] = rc < rows ? (a.causal ? max(0, len - a.Tq + rc / a.R + 1) : len) : 0;
+                top[n][e] = MINUS_INF;
+                sum[n][e] = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < G; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[n][i][j][e] = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) oc[n][e] = 0.f;
+        }
+        // (rows are ordered by query: the first sees least, the last most)
+        const int last = min(row0 + NR, rows) - 1;
+        const int least = a.causal ? max(0, len - a.Tq + row0 / a.R + 1) : len;
+        const int most = a.causal ? max(0, len - a.Tq + last / a.R + 1) : len;
+
+        for (int at = warp; at < count; at += kWarps) {
+            const uint8_t* const block = ring + use * L::kBytes;
+            const int token0 = (now.tile + at) * kCacheBlock;
+            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+            __syncwarp();
+            if (token0 < most) {
+                const bool edge = token0 + kCacheBlock > least || token0 + kCacheBlock > len;
+                float z[NT][2][4];
+                {
+                    uint32_t k[2][2][G], ks[2][2][(G + 1) / 2];
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        uint32_t c[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int r = m * 16 + e * 8 + g;
+                            lds<4 * G>(k[m][e], block + L::kKCodes + r * (D / 2) + t * 4 * G);
+                            lds<2 * G>(ks[m][e], block + L::kKScale + r * 2 * G);
+                            c[e] = *reinterpret_cast<const uint32_t*>(block + L::kKCentre + r * 2 * G + 2 * ((2 * t) % G));
+                        }
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            const QueryOperand<G>& w = NT == 1 ? own : operand[n * 32 + lane];
+                            z[n][m][0] = z[n][m][1] = z[n][m][2] = z[n][m][3] = 0.f;
+                            mma(z[n][m], c[0], c[1], c[0], c[1], w.sums[0], w.sums[1]);
+                            if constexpr (G == 8) mma(z[n][m], c[0], c[1], c[0], c[1], w.sums[2], w.sums[3]);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < G; ++i) {
+                        uint32_t x[2][2][4];
+                        float f[2][2];
+#pragma unroll
+                        for (int m = 0; m < 2; ++m)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                f[m][e] = i & 1 ? bf16hi(ks[m][e][i / 2]) : bf16lo(ks[m][e][i / 2]);
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) x[m][e][j] = code_pair(k[m][e][i] >> (4 * j));
+                            }
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            const QueryOperand<G>& w = NT == 1 ? own : operand[n * 32 + lane];
+                            const uint4 q = *reinterpret_cast<const uint4*>(w.q[i]);
+                            const float2 s = *reinterpret_cast<const float2*>(w.start[i]);
+#pragma unroll
+                            for (int m = 0; m < 2; ++m) {
+                                float acc[4] = {s.x, s.y, s.x, s.y};
+                                mma(acc, x[m][0][0], x[m][1][0], x[m][0][1], x[m][1][1], q.x, q.y);
+                                mma(acc, x[m][0][2], x[m][1][2], x[m][0][3], x[m][1][3], q.z, q.w);
+                                z[n][m][0] = fmaf(f[m][0], acc[0], z[n][m][0]);
+                                z[n][m][1] = fmaf(f[m][0], acc[1], z[n][m][1]);
+                                z[n][m][2] = fmaf(f[m][1], acc[2], z[n][m][2]);
+                                z[n][m][3] = fmaf(f[m][1], acc[3], z[n][m][3]);
+                            }
+                        }
+                    }
+                }
+                // softmax: element (m, e) of n is token m 16 + g + 8 (e / 2) and row n 8 + 2 t + e % 2
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    float high[2] = {MINUS_INF, MINUS_INF};
+#pragma unroll
+                    for (int m = 0; m < 2; ++m)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            z[n][m][e] *= a.scale_log2;
+                            if (edge && token0 + m * 16 + g + 8 * (e / 2) >= limit[n][e & 1]) z[n][m][e] = MINUS_INF;
+                            high[e & 1] = fmaxf(high[e & 1], z[n][m][e]);
+                        }
+                    bool moved = false;
+                    float keep[2], base[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                        for (int off = 4; off < 32; off <<= 1) high[e] = fmaxf(high[e], __shfl_xor_sync(0xffffffffu, high[e], off));
+                        high[e] = fmaxf(high[e], top[n][e]);
+                        base[e] = high[e] == MINUS_INF ? 0.f : high[e];
+                        keep[e] = ex2_approx(top[n][e] - base[e]);
+                        moved |= high[e] != top[n][e];
+                        top[n][e] = high[e];
+                    }
+                    if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            sum[n][e] *= keep[e];
+                            oc[n][e] *= keep[e];
+#pragma unroll
+                            for (int i = 0; i < G; ++i)
+#pragma unroll
+                                for (int j = 0; j < 2; ++j) {
+                                    o[n][i][j][e] *= keep[e];
+                                    o[n][i][j][2 + e] *= keep[e];
+                                }
+                        }
+                    }
+#pragma unroll
+                    for (int m = 0; m < 2; ++m)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            z[n][m][e] = ex2_approx(z[n][m][e] - base[e & 1]);
+                            sum[n][e & 1] += z[n][m][e];
+                        }
+                }
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    const int r = m * 16 + g, v = m * 16 + 2 * t;
+                    uint32_t w[4][(G + 1) / 2], s0[(G + 1) / 2], s1[(G + 1) / 2];
+                    lds<2 * G>(s0, block + L::kVScale + r * 2 * G);
+                    lds<2 * G>(s1, block + L::kVScale + (r + 8) * 2 * G);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) lds<2 * G>(w[e], block + L::kVCodes + (v + (e & 1) + 8 * (e / 2)) * (D / 2) + g * 2 * G);
+                    uint32_t c0 = *reinterpret_cast<const uint32_t*>(block + L::kVCentre + ((g % G) * 32 + v) * 2);
+                    uint32_t c1 = *reinterpret_cast<const uint32_t*>(block + L::kVCentre + ((g % G) * 32 + v + 8) * 2);
+                    if (g >= G) c0 = c1 = 0u;
+                    if (edge) {                            // (what nobody wrote may be no number; what was written is one)
+                        const int there = len - token0 - v;
+                        c0 &= (there > 0 ? 0x0000FFFFu : 0u) | (there > 1 ? 0xFFFF0000u : 0u);
+                        c1 &= (there > 8 ? 0x0000FFFFu : 0u) | (there > 9 ? 0xFFFF0000u : 0u);
+                    }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+                        mma(oc[n], c0, 0u, c1, 0u, transposed(bf16x2(z[n][m][0], z[n][m][1])), transposed(bf16x2(z[n][m][2], z[n][m][3])));
+#pragma unroll
+                    for (int i = 0; i < G; ++i) {
+                        const uint32_t pick = i & 1 ? 0x7632u : 0x5410u;
+                        const uint32_t lo = __byte_perm(w[0][i / 2], w[1][i / 2], pick), hi = __byte_perm(w[2][i / 2], w[3][i / 2], pick);
+                        const float f0 = i & 1 ? bf16hi(s0[i / 2]) : bf16lo(s0[i / 2]), f1 = i & 1 ? bf16hi(s1[i / 2]) : bf16lo(s1[i / 2]);
+                        uint32_t x[8];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            x[e] = centred(code_pair(lo >> (4 * e)));
+                            x[4 + e] = centred(code_pair(hi >> (4 * e)));
+                        }
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            float p[4] = {z[n][m][0] * f0, z[n][m][1] * f0, z[n][m][2] * f1, z[n][m][3] * f1};
+                            if (edge) {                    // (the scale of a row that this query does not see may be no number)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    if (token0 + r + 8 * (e / 2) >= limit[n][e & 1]) p[e] = 0.f;
+                            }
+                            const uint32_t b0 = transposed(bf16x2(p[0], p[1])), b1 = transposed(bf16x2(p[2], p[3]));
+                            mma(o[n][i][0], x[0], x[1], x[4], x[5], b0, b1);
+                            mma(o[n][i][1], x[2], x[3], x[6], x[7], b0, b1);
+                        }
+                    }
+                }
+            }
+            __syncwarp();
+            fetch();
+            use = use + 1 == kStages ? 0 : use + 1;
+        }
+
+        // the CTA's warps joined, two groups at a time.  o[n][i][j][e]: element i 32 + 4 g + 2 j + e / 2 of row n 8 + 2 t + e % 2
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                for (int off = 4; off < 32; off <<= 1) sum[n][e] += __shfl_xor_sync(0xffffffffu, sum[n][e], off);
+                if (g == 0) {
+                    join_max[warp * NR + n * 8 + 2 * t + e] = top[n][e];
+                    join_sum[warp * NR + n * 8 + 2 * t + e] = sum[n][e];
+                }
+            }
+        const bool whole = now.tile == 0 && count == now.blocks;
+        float* const part = SHARES && !whole ? a.part + (size_t)(2 * blockIdx.x + (now.tile == 0 ? 1 : 0)) * NR * (D + 2) : nullptr;
+        const int je = warp & 1, ji = warp >> 1;           // this warp's share: group i0 + ji, rows n 8 + 2 t + je
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int rl = n * 8 + 2 * t + je, r = row0 + rl;
+            float f[kWarps], high = MINUS_INF, total = 0.f;
+#pragma unroll
+            for (int i0 = 0; i0 < G; i0 += 2) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float c = __shfl_sync(0xffffffffu, oc[n][e], 4 * (i0 + i) + t);
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            join[((warp * 2 + i) * 8 + 4 * e + 2 * j) * 32 + lane] = o[n][i0 + i][j][e] + c;
+                            join[((warp * 2 + i) * 8 + 4 * e + 2 * j + 1) * 32 + lane] = o[n][i0 + i][j][2 + e] + c;
+                        }
+                    }
+                __syncthreads();
+                if (i0 == 0) {
+#pragma unroll
+                    for (int w = 0; w < kWarps; ++w) high = fmaxf(high, join_max[w * NR + rl]);
+#pragma unroll
+                    for (int w = 0; w < kWarps; ++w) {
+                        f[w] = ex2_approx(join_max[w * NR + rl] - (high == MINUS_INF ? 0.f : high));
+                        total = fmaf(join_sum[w * NR + rl], f[w], total);
+                    }
+                }
+                float v[4] = {};
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = fmaf(join[((w * 2 + ji) * 8 + 4 * je + k) * 32 + lane], f[w], v[k]);
+                const bool none = high == MINUS_INF && total == 0.f;
+                const int tq = r / a.R, hq = h * a.R + (r - tq * a.R);
+                if (r < rows) {
+                    if (part) {
+                        *reinterpret_cast<float4*>(part + rl * D + (i0 + ji) * 32 + 4 * g) = make_float4(v[0], v[1], v[2], v[3]);
+                        if (i0 == 0 && ji == 0 && g == 0) {
+                            part[NR * D + rl] = high;
+                            part[NR * D + NR + rl] = total;
+                        }
+                    } else {
+                        const float inv = none ? 0.f : 1.f / total;
+                        *reinterpret_cast<uint2*>(a.io.out + b * a.io.ob + hq * a.io.oh + tq * a.io.ot + (i0 + ji) * 32 + 4 * g) =
+                            make_uint2(bf16x2(v[0] * inv, v[1] * inv), bf16x2(v[2] * inv, v[3] * inv));
+                        if (i0 == 0 && ji == 0 && g == 0 && a.lse)
+                            a.lse[((int64_t)b * a.Hq + hq) * a.Tq + tq] = none ? MINUS_INF : (high + __log2f(total)) * kLn2;
+                    }
+                }
+                __syncthreads();
+            }
+        }
+        next(now);
+    }
+}
+
+// The pieces of a head and tile of rows that several CTAs shared, in their order, one row a CTA.
+constexpr int kJoinThreads = 128;
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads)
+cache_attention_join_kernel(AttArgs a, int NR, int most) {
+    constexpr int kQuads = D / 4;                          // threads that share a row's elements; kBy of them by piece
+    constexpr int kBy = kJoinThreads / kQuads;
+    __shared__ float red[kBy][D];
+    __shared__ float weight[kJoinThreads];
+    const int segs = a.H * a.RT;
+    const int s = blockIdx.x / NR, rl = blockIdx.x - s * NR, b = s / segs, seg = s - b * segs;
+    const int h = seg / a.RT, r = (seg - h * a.RT) * NR + rl;
+    grid_dependency_wait();
+    if (r >= a.R * a.Tq) return;
+    const int first = a.before[b], blocks = a.before[b + 1] - first;
+    const int64_t total = (int64_t)a.before[a.B] * segs, from = (int64_t)first * segs + (int64_t)seg * blocks;
+    const int tq = r / a.R, hq = h * a.R + (r - tq * a.R);
+    __nv_bfloat16* const out = a.io.out + b * a.io.ob + hq * a.io.oh + tq * a.io.ot;
+    float* const lse = a.lse ? a.lse + ((int64_t)b * a.Hq + hq) * a.Tq + tq : nullptr;
+    if (blocks == 0) {
+        for (int e = threadIdx.x; e < D; e += kJoinThreads) out[e] = __float2bfloat16_rn(0.f);
+        if (lse && threadIdx.x == 0) *lse = MINUS_INF;
+        return;
+    }
+    const int ctas = sharers(total, most);
+    // CTA c has the blocks from total c / ctas on: the last one that starts at or before a block has it
+    const int c0 = (int)(((from + 1) * ctas - 1) / total), c1 = (int)(((from + blocks) * ctas - 1) / total);
+    if (c0 == c1) return;                                  // one CTA had it all, and wrote the result
+    const int n = c1 - c0 + 1;
+    const size_t size = (size_t)NR * (D + 2);
+    const auto slot = [&](int c) { return a.part + (size_t)(2 * (c0 + c) + (c == 0 ? 1 : 0)) * size; };
+    float high = MINUS_INF;
+    for (int c = threadIdx.x; c < n; c += kJoinThreads) high = fmaxf(high, slot(c)[NR * D + rl]);
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, off));
+    if ((threadIdx.x & 31) == 0) weight[threadIdx.x >> 5] = high;
+    __syncthreads();
+    high = fmaxf(fmaxf(weight[0], weight[1]), fmaxf(weight[2], weight[3]));
+    const float base = high == MINUS_INF ? 0.f : high;
+    __syncthreads();
+    const int col = threadIdx.x % kQuads, by = threadIdx.x / kQuads;
+    float v[4] = {}, sum = 0.f;
+    for (int c0_ = 0; c0_ < n; c0_ += kJoinThreads) {
+        const int m = min(n - c0_, kJoinThreads);
+        if ((int)threadIdx.x < m) {
+            const float* const p = slot(c0_ + threadIdx.x) + NR * D + rl;
+            const float f = ex2_approx(p[0] - base);
+            weight[threadIdx.x] = f;
+            sum = fmaf(p[NR], f, sum);
+        }
+        __syncthreads();
+#pragma unroll 8
+        for (int c = by; c < m; c += kBy) {
+            const float4 x = *reinterpret_cast<const float4*>(slot(c0_ + c) + rl * D + 4 * col);
+            const float f = weight[c];
+            v[0] = fmaf(x.x, f, v[0]);
+            v[1] = fmaf(x.y, f, v[1]);
+            v[2] = fmaf(x.z, f, v[2]);
+            v[3] = fmaf(x.w, f, v[3]);
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+    if ((threadIdx.x & 31) == 0) weight[threadIdx.x >> 5] = sum;
+    *reinterpret_cast<float4*>(&red[by][4 * col]) = make_float4(v[0], v[1], v[2], v[3]);
+    __syncthreads();
+    sum = (weight[0] + weight[1]) + (weight[2] + weight[3]);
+    __syncthreads();
+    const bool none = high == MINUS_INF && sum == 0.f;
+    const float inv = none ? 0.f : 1.f / sum;
+    for (int e = threadIdx.x; e < D; e += kJoinThreads) {
+        float x = red[0][e];
+#pragma unroll
+        for (int k = 1; k < kBy; ++k) x += red[k][e];
+        out[e] = __float2bfloat16_rn(x * inv);
+    }
+    if (lse && threadIdx.x == 0) *lse = none ? MINUS_INF : (base + __log2f(sum)) * kLn2;
+}
+
+int sm_count() {
+    static std::atomic<int> known[kMaxDevices];
+    std::atomic<int>& k = known[current_device()];
+    int v = k.load(std::memory_order_relaxed);
+    if (v == 0) {
+        if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, current_device()) != cudaSuccess || v <= 0) v = 148;
+        k.store(v, std::memory_order_relaxed);
+    }
+    return v;
+}
+
+struct Plan {
+    int NT, RT, ctas;                                      // ctas: of the shares; 0: a CTA a head and tile of rows
+};
+
+Plan plan_of(int B, int H, int Ncap, int d, int Tq, int Hq, int sms) {
+    Plan p;
+    const int64_t rows = (int64_t)(Hq / H) * Tq;
+    p.NT = rows <= 8 ? 1 : rows <= 16 || d == 256 ? 2 : 4;
+    p.RT = (int)((rows + 8 * p.NT - 1) / (8 * p.NT));
+    const int slots = sms * ctas_per_sm(d, p.NT);
+    const int64_t segs = (int64_t)B * H * p.RT, blocks = Ncap / kCacheBlock;
+    p.ctas = 0;
+    if (segs < 4 * slots && blocks > 2 * kWarps) {
+        const int64_t most = segs * blocks / kWarps;       // no fewer than a block a warp
+        p.ctas = (int)(most < slots ? most : slots);
+        if (p.ctas <= segs) p.ctas = segs < slots ? 0 : slots;
+    }
+    return p;
+}
+
+size_t part_bytes(const Plan& p, int d) { return align_up((size_t)2 * p.ctas * 8 * p.NT * (d + 2) * sizeof(float), 256); }
+
+template <int D, int NT>
+int launch(AttArgs a, const Plan& p, cudaStream_t stream) {
+    constexpr size_t kSmem = (size_t)kWarps * kStages * CacheBlock<D>::kBytes + kWarps * 2048 + 2 * kWarps * 8 * NT * 4 +
+                             (NT > 1 ? NT * 32 * sizeof(QueryOperand<D / 32>) : 0);
+    static DoneOnDevice done[2];
+    const bool shares = p.ctas > 0;
+    const size_t smem = kSmem + (shares ? align_up((size_t)(a.B + 1) * 4, 16) : 0);
+    const auto kern = shares ? cache_attention_kernel<D, NT, true> : cache_attention_kernel<D, NT, false>;
+    int rc = allow_dynamic_smem(kern, kSmem + 16384, done[shares]);
+    if (rc != VITCOP_OK) return rc;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(B * Hq * Tq));
-    cfg.blockDim = dim3(kAttWarps * 32);
+    cfg.gridDim = dim3((unsigned)(shares ? p.ctas : a.B * a.H * a.RT));
+    cfg.blockDim = dim3(kWarps * 32);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = pdl_allowed(true) ? 1 : 0;
-    KernelTimeScope timed("cache_attention_kernel", stream);
-    auto kern = d == 64 ? cache_attention_kernel<64> : d == 128 ? cache_attention_kernel<128> : cache_attention_kernel<256>;
-    return record_cuda(cudaLaunchKernelEx(&cfg, kern, io, static_cast<const uint8_t*>(cache), Hq, H, Tq, Ncap, cache_len, scale,
-                                          causal ? 1 : 0, lse, static_cast<int*>(workspace)));
+    {
+        KernelTimeScope timed("cache_attention_kernel", stream);
+        rc = record_cuda(cudaLaunchKernelEx(&cfg, kern, a));
+        if (rc != VITCOP_OK || !shares) return rc;
+    }
+    cfg.gridDim = dim3((unsigned)(a.B * a.H * a.RT * 8 * NT));
+    cfg.blockDim = dim3(kJoinThreads);
+    cfg.dynamicSmemBytes = 0;
+    KernelTimeScope timed("cache_attention_join_kernel", stream);
+    return record_cuda(cudaLaunchKernelEx(&cfg, cache_attention_join_kernel<D>, a, 8 * NT, p.ctas));
+}
+
+}  // namespace
+
+size_t cache_attention_workspace_bytes(int B, int H, int Ncap, int d, int Tq, int Hq) {
+    if (B < 1 || H < 1 || Hq < 1 || Tq < 1) return kStatusBytes;
+    const Plan p = plan_of(B, H, Ncap, d, Tq, Hq, sm_count());
+    return kStatusBytes + (p.ctas ? align_up((size_t)(B + 1) * 4, 256) + part_bytes(p, d) : 0);
+}
+
+int launch_cache_attention(const CacheQueries& io, const void* cache, int B, int Hq, int H, int Tq, int d, int Ncap,
+                           const int32_t* cache_len, float scale, bool causal, float* lse, void* workspace, cudaStream_t stream) {
+    const Plan p = plan_of(B, H, Ncap, d, Tq, Hq, sm_count());
+    if ((int64_t)B * H * p.RT > 0x7fffffff || (int64_t)Hq / H * Tq > 0x7fffffff - 64) return VITCOP_ERR_UNSUPPORTED;
+    AttArgs a;
+    a.io = io;
+    a.cache = static_cast<const uint8_t*>(cache);
+    a.cache_len = cache_len;
+    a.lse = lse;
+    a.status = static_cast<int*>(workspace);
+    a.before = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + kStatusBytes);
+    a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kStatusBytes + align_up((size_t)(B + 1) * 4, 256));
+    a.B = B; a.Hq = Hq; a.H = H; a.R = Hq / H; a.Tq = Tq; a.Ncap = Ncap; a.RT = p.RT; a.causal = causal ? 1 : 0;
+    a.scale_log2 = scale * kLog2e;
+    if (d == 64) return p.NT == 1 ? launch<64, 1>(a, p, stream) : p.NT == 2 ? launch<64, 2>(a, p, stream) : launch<64, 4>(a, p, stream);
+    if (d == 128) return p.NT == 1 ? launch<128, 1>(a, p, stream) : p.NT == 2 ? launch<128, 2>(a, p, stream) : launch<128, 4>(a, p, stream);
+    return p.NT == 1 ? launch<256, 1>(a, p, stream) : launch<256, 2>(a, p, stream);
 }
 
 }  // namespace vitcop

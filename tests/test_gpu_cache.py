@@ -259,7 +259,8 @@ def _attend(q, cache, lens, scale, causal=True, lse=True, strided=True, ws=None)
 def _check(q, cache, K, V, lens, scale, causal, out, lse):
     w, wl, tol, ltol = _bounds(_f64(q), K, V, lens, scale, causal)
     got = _f64(out)
-    assert np.all(np.abs(got - w) <= tol), (np.abs(got - w) / tol).max()
+    worst = (np.abs(got - w) / tol).max()
+    assert worst <= 1, worst
     if lse is not None:
         g = _f64(lse)
         empty = np.isneginf(wl)
