@@ -1,14 +1,16 @@
 // Attention of query rows over the K/V cache in 4 bits: out = softmax(scale q K^T) V over the rows that a query sees.
 //
-// The query rows of a stored head (Hq / H heads times Tq queries, a tile of 8 NT of them at a time) are the narrow side of every
-// matrix product (m16n8k16, bf16 in, fp32 out), tokens and then elements the wide one; codes become operands in registers:
-//   logits   a code c is the bf16 128 + c (its nibble under the exponent of 128), exactly.  Per group the product starts from
-//            -136 sum(q), so that it ends as sum((c - 8) q), which the group's scale multiplies in fp32; the centres are one
-//            more product, with sum(q) split into three bf16
-//   output   (128 + c) - 136 = c - 8 is exact too; the weight enters as bf16(p s) for each group, and bf16(p) with the centres
+// Every product is one of matrix instructions (m16n8k16, bf16 in, fp32 out), and codes become operands in registers:
+//   logits   query rows (Hq / H heads times Tq queries, a tile of 8 NT of them at a time) times tokens.  A code c is the bf16
+//            128 + c (its nibble under the exponent of 128), exactly; per group the token's scale multiplies the product in fp32.
+//            The centres, and the scales times -136, are one more product each, with the groups' sums of q split into three bf16
+//   output   elements times query rows: (128 + c) - 136 = c - 8 is exact too.  The weights of two neighbouring tokens lie in a lane as
+//            the logits left it there, and that is what this product takes: bf16(p) with the centres, bf16(bf16(p) s) with a group's codes
 // A warp takes every fourth block of 32 tokens of its CTA's piece, with blocks ahead in shared memory (cp.async), and keeps maximum, sum
 // and output of its own; the CTA joins its warps, a second kernel joins the CTAs that shared a head.
 #include <cuda_bf16.h>
+
+#include <type_traits>
 
 #include "async_copy.cuh"
 #include "f32x2.cuh"
@@ -25,6 +27,18 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // Resident CTAs an SM, which the registers of the accumulators and the ring's memory leave room for.
 constexpr int ctas_per_sm(int D, int NT) { return D == 256 || NT == 4 ? 2 : D * NT <= 128 ? 4 : 3; }
 
+// n / d for 0 <= n < 2^31 by a multiplication: with l = ceil(log2 d), mul = floor(2^(31 + l) / d) + 1 is off by less than 2^l / d parts of
+// 2^(31 + l), which n < 2^31 of them do not add up to a quotient.
+struct Divisor {
+    uint32_t d, mul, shift;
+};
+Divisor divisor(int d) {
+    int l = 0;
+    while ((1ll << l) < d) ++l;
+    return {(uint32_t)d, d == 1 ? 0u : (uint32_t)((1ull << (31 + l)) / (uint32_t)d + 1), (uint32_t)(l > 0 ? l - 1 : 0)};
+}
+__device__ __forceinline__ int quotient(int n, const Divisor& by) { return by.d == 1 ? n : (int)(__umulhi((uint32_t)n, by.mul) >> by.shift); }
+
 struct AttArgs {
     CacheQueries io;
     const uint8_t* cache;
@@ -33,8 +47,11 @@ struct AttArgs {
     int* status;
     int32_t* before;                                       // shares: blocks in front of each sample, [B + 1]
     float* part;                                           // shares: two pieces a CTA, each [8 NT][D + 2]
-    int B, Hq, H, R, Tq, Ncap, RT, causal;
-    float scale_log2;
+    int B, Hq, H, Tq, Ncap, causal;
+    Divisor R, RT;                                         // query heads of a stored one, tiles of rows
+    float scale_log2;                                      // above 0: the sign is the queries'
+    uint32_t sign;                                         // 0x80008000 turns it; scale 0: `zero`
+    bool zero;
 };
 
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -42,19 +59,30 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t transposed(uint32_t x) {   // an 8 x 8 matrix of 16-bit values, two of a row in a lane
-    uint32_t y;
-    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-    return y;
+// d = a b
+__device__ __forceinline__ void mma_zero(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
-__device__ __forceinline__ uint32_t code_pair(uint32_t w) { return (w & 0x000F000Fu) | 0x43004300u; }   // 128 + c, twice
+__device__ __forceinline__ uint32_t code_pair(uint32_t w) {    // 128 + c, twice
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(0x000F000Fu), "r"(0x43004300u));
+    return r;
+}
 __device__ __forceinline__ uint32_t centred(uint32_t pair) {                                              // c - 8, twice
     uint32_t r;
     asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(pair), "r"(0xC308C308u));
+    return r;
+}
+__device__ __forceinline__ uint32_t times(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
 template <int BYTES>
@@ -73,33 +101,30 @@ __device__ __forceinline__ void lds(uint32_t* w, const uint8_t* p) {
     }
 }
 
-// Eight query rows as the narrow operand, one lane's part: its eight elements of each group of row g, -136 times the groups' sums of
-// rows 2 t and 2 t + 1, and the sums of row g in three bf16 each (part p of group i is element p G + i of the product with the centres).
+// Eight query rows as operand, one lane's part: its eight elements of each group of row g, and the groups' sums in three bf16 each
+// (part p of group i is element p G + i of the products with centres and scales).
 template <int G>
 struct __align__(16) QueryOperand {
-    uint32_t q[G][4];
-    float start[G][2];
-    uint32_t sums[4];
+    uint4 q[G];
+    uint4 sums;                                            // (the second half: eight groups)
 };
 template <int G>
-__device__ __forceinline__ void load_queries(QueryOperand<G>& to, const __nv_bfloat16* src, bool there, int t) {
+__device__ __forceinline__ void load_queries(QueryOperand<G>* to, const __nv_bfloat16* src, bool there, uint32_t sign, int t) {
     float total[G];
 #pragma unroll
     for (int i = 0; i < G; ++i) {
-        const uint4 v = there ? __ldg(reinterpret_cast<const uint4*>(src + t * 8 + i * 32)) : make_uint4(0, 0, 0, 0);
-        to.q[i][0] = __byte_perm(v.x, v.z, 0x5410);        // elements 0 and 4, 1 and 5, 2 and 6, 3 and 7, as the codes lie
-        to.q[i][1] = __byte_perm(v.x, v.z, 0x7632);
-        to.q[i][2] = __byte_perm(v.y, v.w, 0x5410);
-        to.q[i][3] = __byte_perm(v.y, v.w, 0x7632);
+        uint4 v = there ? __ldg(reinterpret_cast<const uint4*>(src + t * 8 + i * 32)) : make_uint4(0, 0, 0, 0);
+        v = make_uint4(v.x ^ sign, v.y ^ sign, v.z ^ sign, v.w ^ sign);
+        // elements 0 and 4, 1 and 5, 2 and 6, 3 and 7, as the codes lie
+        to->q[i] = make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
         float x = ((bf16lo(v.x) + bf16hi(v.x)) + (bf16lo(v.y) + bf16hi(v.y))) + ((bf16lo(v.z) + bf16hi(v.z)) + (bf16lo(v.w) + bf16hi(v.w)));
         x += __shfl_xor_sync(0xffffffffu, x, 1);
         x += __shfl_xor_sync(0xffffffffu, x, 2);
         total[i] = x;
-        to.start[i][0] = -136.f * __shfl_sync(0xffffffffu, x, 8 * t);
-        to.start[i][1] = -136.f * __shfl_sync(0xffffffffu, x, 8 * t + 4);
     }
+    uint32_t sums[4] = {};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < (G == 8 ? 4 : 2); ++i) {
         float v[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -111,8 +136,9 @@ __device__ __forceinline__ void load_queries(QueryOperand<G>& to, const __nv_bfl
             const float first = __bfloat162float(__float2bfloat16_rn(x)), second = __bfloat162float(__float2bfloat16_rn(x - first));
             v[e] = p == 0 ? first : p == 1 ? second : p == 2 ? (x - first) - second : 0.f;
         }
-        to.sums[i] = bf16x2(v[0], v[1]);
+        sums[i] = bf16x2(v[0], v[1]);
     }
+    to->sums = make_uint4(sums[0], sums[1], sums[2], sums[3]);
 }
 
 // Where a CTA is in its share of the work: block `tile` of segment `seg` (head and tile of rows) of sample b, `left` blocks to go.
@@ -139,14 +165,18 @@ cache_attention_kernel(AttArgs a) {
     float* const join = reinterpret_cast<float*>(smem + kWarps * kStages * L::kBytes);      // [warp][2 groups][8][lane]
     float* const join_max = join + kWarps * 512;                                            // [warp][NR]
     float* const join_sum = join_max + kWarps * NR;
-    QueryOperand<G>* const operand = reinterpret_cast<QueryOperand<G>*>(join_sum + kWarps * NR);      // [NT][lane] where NT > 1
-    int32_t* const before = reinterpret_cast<int32_t*>(operand + (NT > 1 ? NT * 32 : 0));             // [B + 1]
+    QueryOperand<G>* const operand = reinterpret_cast<QueryOperand<G>*>(join_sum + kWarps * NR);      // [NT][lane]
+    Walk* const walks = reinterpret_cast<Walk*>(operand + NT * 32);                                   // [warp][2]
+    int32_t* const before = reinterpret_cast<int32_t*>(walks + kWarps * 2);                           // [B + 1]
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const int segs = a.H * a.RT;
+    const int segs = a.H * a.RT.d;
     grid_dependency_wait();
     if constexpr (SHARES) grid_dependency_launch_dependents();     // (the join's CTAs, which wait for this grid to end)
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = VITCOP_OK;
 
+    // (kept in shared memory, one copy a warp: registers are what the blocks' work is short of)
+    Walk* const at_work = walks + warp * 2;
+    Walk* const at_fetch = walks + warp * 2 + 1;
     Walk now;
     if constexpr (SHARES) {
         // blocks in front of each sample
@@ -199,23 +229,40 @@ cache_attention_kernel(AttArgs a) {
                 if (w.left > 0) do { ++w.b; w.blocks = before[w.b + 1] - before[w.b]; } while (w.blocks == 0);
         }
     };
+    // (a walk is copied, and written back by one lane, between barriers of the warp)
+    const auto put = [&](Walk* to, const Walk& w) {
+        __syncwarp();
+        if (lane == 0) *to = w;
+        __syncwarp();
+    };
     // the sequence's blocks ahead of their use: this warp's share of every piece
-    Walk ahead = now;
-    int ahead_at = warp;
+    const auto first_block = [&](const Walk& w) {
+        return a.cache + (((int64_t)w.b * a.H + quotient(w.seg, a.RT)) * (a.Ncap / kCacheBlock) + w.tile + warp) * L::kBytes + lane * 16;
+    };
+    put(at_work, now);
+    put(at_fetch, now);
+    int ahead_left = piece(now) - warp;                    // blocks of the piece from this warp's next on
+    const uint8_t* ahead_src = first_block(now);
     uint8_t* const ring = smem + warp * kStages * L::kBytes;
+    const uint32_t ring_at = smem_u32(ring) + lane * 16;
     int fill = 0;
     const auto fetch = [&]() {
-        while (ahead.left > 0 && ahead_at >= piece(ahead)) {
-            next(ahead);
-            ahead_at = warp;
+        if (SHARES && ahead_left <= 0) {
+            Walk w = *at_fetch;
+            while (ahead_left <= 0 && w.left > piece(w)) {
+                next(w);
+                ahead_left = piece(w) - warp;
+                ahead_src = first_block(w);
+            }
+            put(at_fetch, w);
         }
-        if (ahead.left > 0) {
-            const uint8_t* const src = a.cache + (((int64_t)ahead.b * a.H + ahead.seg / a.RT) * (a.Ncap / kCacheBlock) + ahead.tile + ahead_at) * L::kBytes;
-            const uint32_t dst = smem_u32(ring + fill * L::kBytes);
+        if (ahead_left > 0) {
+            const uint32_t dst = ring_at + fill * L::kBytes;
 #pragma unroll
             for (int i = 0; i < kChunks / 32; ++i)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (i * 32 + lane) * 16), "l"(src + (i * 32 + lane) * 16) : "memory");
-            ahead_at += kWarps;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + i * 512), "l"(ahead_src + i * 512) : "memory");
+            ahead_left -= kWarps;
+            ahead_src += kWarps * L::kBytes;
             fill = fill + 1 == kStages ? 0 : fill + 1;
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -224,195 +271,186 @@ cache_attention_kernel(AttArgs a) {
     for (int i = 0; i < kStages; ++i) fetch();
     int use = 0;
 
-    for (bool first = true; first || now.left > 0; first = false) {
-        const int b = now.b, h = now.seg / a.RT, row0 = (now.seg - h * a.RT) * NR, rows = a.R * a.Tq;
+    do {
+        now = *at_work;
+        const int b = now.b, h = quotient(now.seg, a.RT), row0 = (now.seg - h * (int)a.RT.d) * NR, rows = (int)a.R.d * a.Tq;
         const int count = piece(now);
         const int len = a.cache_len ? max(0, min(__ldg(a.cache_len + b), a.Ncap)) : a.Ncap;
-        QueryOperand<G> own;
-        if constexpr (NT == 1) {
-            const int r = row0 + g, tq = r / a.R, hq = h * a.R + (r - tq * a.R);
-            load_queries<G>(own, a.io.q + b * a.io.qb + hq * a.io.qh + tq * a.io.qt, r < rows, t);
-        } else {
-            if (warp < NT) {
-                const int r = row0 + warp * 8 + g, tq = r / a.R, hq = h * a.R + (r - tq * a.R);
-                load_queries<G>(own, a.io.q + b * a.io.qb + hq * a.io.qh + tq * a.io.qt, r < rows, t);
-                operand[warp * 32 + lane] = own;
-            }
-            __syncthreads();
+        if (warp < NT) {
+            const int r = row0 + warp * 8 + g, tq = quotient(r, a.R), hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
+            load_queries<G>(operand + warp * 32 + lane, a.io.q + b * a.io.qb + hq * a.io.qh + tq * a.io.qt, r < rows && !a.zero, a.sign, t);
         }
-        float o[NT][G][2][4], oc[NT][4], top[NT][2], sum[NT][2];
-        int limit[NT][2];
+        float o[NT][G][2][4], oc[NT][4], top[NT], sum[NT];
+        int limit[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
+            const int r = row0 + n * 8 + g;
+            limit[n] = r < rows ? (a.causal ? max(0, len - a.Tq + quotient(r, a.R) + 1) : len) : 0;
+            top[n] = MINUS_INF;
+            sum[n] = 0.f;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int rc = row0 + n * 8 + 2 * t + e;
-                limit[n][e] = rc < rows ? (a.causal ? max(0, len - a.Tq + rc / a.R + 1) : len) : 0;
-                top[n][e] = MINUS_INF;
-                sum[n][e] = 0.f;
+            for (int e = 0; e < 4; ++e) {
+                oc[n][e] = 0.f;
+#pragma unroll
+                for (int i = 0; i < G; ++i) o[n][i][0][e] = o[n][i][1][e] = 0.f;
             }
-#pragma unroll
-            for (int i = 0; i < G; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[n][i][j][e] = 0.f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) oc[n][e] = 0.f;
         }
         // (rows are ordered by query: the first sees least, the last most)
         const int last = min(row0 + NR, rows) - 1;
-        const int least = a.causal ? max(0, len - a.Tq + row0 / a.R + 1) : len;
-        const int most = a.causal ? max(0, len - a.Tq + last / a.R + 1) : len;
+        const int least = a.causal ? max(0, len - a.Tq + quotient(row0, a.R) + 1) : len;
+        const int most = a.causal ? max(0, len - a.Tq + quotient(last, a.R) + 1) : len;
 
-        for (int at = warp; at < count; at += kWarps) {
+        // Half m of a block: 16 tokens.  z[n][j][e]: row n 8 + g, token 8 j + 2 t + e.  EDGE: some row does not see some of them.
+        const auto half_block = [&](const uint8_t* block, int m, int token0, auto edge_) {
+            constexpr bool EDGE = decltype(edge_)::value;
+            constexpr int kHalves = NT > 1 ? 2 : 1;        // rows g, and g + 8 where there are any, of an operand
+            float z[NT][2][2];
+            {
+                uint32_t k[2][G], s[2][G];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int r = 16 * m + 8 * j;
+                    lds<4 * G>(k[j], block + L::kKCodes + (r + g) * (D / 2) + t * 4 * G);
+                    lds<4 * G>(s[j], block + L::kKScale + (r + 2 * t) * 2 * G);        // of two tokens
+                    const uint32_t kc = *reinterpret_cast<const uint32_t*>(block + L::kKCentre + (r + g) * 2 * G + 2 * ((2 * t) % G));
+                    const uint32_t ks = *reinterpret_cast<const uint32_t*>(block + L::kKScale + (r + g) * 2 * G + 2 * ((2 * t) % G));
+#pragma unroll
+                    for (int n = 0; n < NT; n += 2) {
+                        const uint4 u = operand[n * 32 + lane].sums;
+                        const uint4 v = NT > 1 ? operand[(n + 1) * 32 + lane].sums : make_uint4(0, 0, 0, 0);
+                        float c[4], f[4];
+                        mma_zero(c, u.x, v.x, u.y, v.y, kc, kc);
+                        mma_zero(f, u.x, v.x, u.y, v.y, ks, ks);
+                        if constexpr (G == 8) {
+                            mma(c, u.z, v.z, u.w, v.w, kc, kc);
+                            mma(f, u.z, v.z, u.w, v.w, ks, ks);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 2 * kHalves; ++e) z[n + e / 2][j][e & 1] = fmaf(-136.f, f[e], c[e]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < G; ++i) {
+                    uint32_t x[2][4];
+                    f32x2 f[2];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[j][e] = code_pair(k[j][i] >> (4 * e));
+                        f[j] = i & 1 ? pack2(bf16hi(s[j][i / 2]), bf16hi(s[j][(G + i) / 2])) : pack2(bf16lo(s[j][i / 2]), bf16lo(s[j][(G + i) / 2]));
+                    }
+#pragma unroll
+                    for (int n = 0; n < NT; n += 2) {
+                        const uint4 u = operand[n * 32 + lane].q[i];
+                        const uint4 v = NT > 1 ? operand[(n + 1) * 32 + lane].q[i] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            float acc[4];
+                            mma_zero(acc, u.x, v.x, u.y, v.y, x[j][0], x[j][1]);
+                            mma(acc, u.z, v.z, u.w, v.w, x[j][2], x[j][3]);
+#pragma unroll
+                            for (int e = 0; e < kHalves; ++e) {
+                                const float2 y = unpack2(fma2(f[j], pack2(acc[2 * e], acc[2 * e + 1]), pack2(z[n + e][j][0], z[n + e][j][1])));
+                                z[n + e][j][0] = y.x;
+                                z[n + e][j][1] = y.y;
+                            }
+                        }
+                    }
+                }
+            }
+            uint32_t p[NT][2], seen[NT][2];                // weights of two tokens; which of them the row sees
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float high = top[n];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    if constexpr (EDGE) {
+                        const int there = limit[n] - token0 - 8 * j - 2 * t;
+                        if (there < 1) z[n][j][0] = MINUS_INF;
+                        if (there < 2) z[n][j][1] = MINUS_INF;
+                        seen[n][j] = (there > 0 ? 0x0000FFFFu : 0u) | (there > 1 ? 0xFFFF0000u : 0u);
+                    }
+                    high = fmaxf(high, fmaxf(z[n][j][0], z[n][j][1]));
+                }
+                high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, 1));
+                high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, 2));
+                // (the sums stay relative to an older maximum until one of the warp's rows has passed its own 2^8 times)
+                if (__any_sync(0xffffffffu, (high - top[n]) * a.scale_log2 > 8.f)) {
+                    const float keep = high == MINUS_INF ? 1.f : ex2_approx((top[n] - high) * a.scale_log2);
+                    const float k0 = __shfl_sync(0xffffffffu, keep, 8 * t), k1 = __shfl_sync(0xffffffffu, keep, 8 * t + 4);
+                    top[n] = high;
+                    sum[n] *= keep;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        oc[n][e] *= e & 1 ? k1 : k0;
+#pragma unroll
+                        for (int i = 0; i < G; ++i) {
+                            o[n][i][0][e] *= e & 1 ? k1 : k0;
+                            o[n][i][1][e] *= e & 1 ? k1 : k0;
+                        }
+                    }
+                }
+                const float base = top[n] == MINUS_INF ? 0.f : top[n] * a.scale_log2;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const float p0 = ex2_approx(fmaf(z[n][j][0], a.scale_log2, -base)), p1 = ex2_approx(fmaf(z[n][j][1], a.scale_log2, -base));
+                    sum[n] += p0 + p1;
+                    p[n][j] = bf16x2(p0, p1);
+                }
+            }
+            {
+                const int v = m * 16 + 2 * t;              // tokens v, v + 1, v + 8, v + 9
+                uint32_t w[4][(G + 1) / 2], s0[G], s1[G];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) lds<2 * G>(w[e], block + L::kVCodes + (v + (e & 1) + 8 * (e / 2)) * (D / 2) + g * 2 * G);
+                lds<4 * G>(s0, block + L::kVScale + v * 2 * G);
+                lds<4 * G>(s1, block + L::kVScale + (v + 8) * 2 * G);
+                uint32_t c0 = *reinterpret_cast<const uint32_t*>(block + L::kVCentre + ((g % G) * 32 + v) * 2);
+                uint32_t c1 = *reinterpret_cast<const uint32_t*>(block + L::kVCentre + ((g % G) * 32 + v + 8) * 2);
+                if (g >= G) c0 = c1 = 0u;
+                if constexpr (EDGE) {                      // (what nobody wrote may be no number; what was written is one)
+                    const int there = len - token0 - 2 * t;
+                    c0 &= (there > 0 ? 0x0000FFFFu : 0u) | (there > 1 ? 0xFFFF0000u : 0u);
+                    c1 &= (there > 8 ? 0x0000FFFFu : 0u) | (there > 9 ? 0xFFFF0000u : 0u);
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n) mma(oc[n], c0, 0u, c1, 0u, p[n][0], p[n][1]);
+#pragma unroll
+                for (int i = 0; i < G; ++i) {
+                    const uint32_t pick = i & 1 ? 0x7632u : 0x5410u;
+                    const uint32_t lo = __byte_perm(w[0][i / 2], w[1][i / 2], pick), hi = __byte_perm(w[2][i / 2], w[3][i / 2], pick);
+                    const uint32_t f0 = __byte_perm(s0[i / 2], s0[(G + i) / 2], pick), f1 = __byte_perm(s1[i / 2], s1[(G + i) / 2], pick);
+                    uint32_t x[8];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        x[e] = centred(code_pair(lo >> (4 * e)));
+                        x[4 + e] = centred(code_pair(hi >> (4 * e)));
+                    }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        uint32_t b0 = times(p[n][0], f0), b1 = times(p[n][1], f1);
+                        if constexpr (EDGE) {              // (the scale of a row that this query does not see may be no number)
+                            b0 &= seen[n][0];
+                            b1 &= seen[n][1];
+                        }
+                        mma(o[n][i][0], x[0], x[1], x[4], x[5], b0, b1);
+                        mma(o[n][i][1], x[2], x[3], x[6], x[7], b0, b1);
+                    }
+                }
+            }
+        };
+
+        __syncthreads();                                   // (the queries)
+        int token0 = (now.tile + warp) * kCacheBlock;
+        for (const int end = (now.tile + count) * kCacheBlock; token0 < end; token0 += kWarps * kCacheBlock) {
             const uint8_t* const block = ring + use * L::kBytes;
-            const int token0 = (now.tile + at) * kCacheBlock;
             asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
             __syncwarp();
-            if (token0 < most) {
-                const bool edge = token0 + kCacheBlock > least || token0 + kCacheBlock > len;
-                float z[NT][2][4];
-                {
-                    uint32_t k[2][2][G], ks[2][2][(G + 1) / 2];
-#pragma unroll
-                    for (int m = 0; m < 2; ++m) {
-                        uint32_t c[2];
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const int r = m * 16 + e * 8 + g;
-                            lds<4 * G>(k[m][e], block + L::kKCodes + r * (D / 2) + t * 4 * G);
-                            lds<2 * G>(ks[m][e], block + L::kKScale + r * 2 * G);
-                            c[e] = *reinterpret_cast<const uint32_t*>(block + L::kKCentre + r * 2 * G + 2 * ((2 * t) % G));
-                        }
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            const QueryOperand<G>& w = NT == 1 ? own : operand[n * 32 + lane];
-                            z[n][m][0] = z[n][m][1] = z[n][m][2] = z[n][m][3] = 0.f;
-                            mma(z[n][m], c[0], c[1], c[0], c[1], w.sums[0], w.sums[1]);
-                            if constexpr (G == 8) mma(z[n][m], c[0], c[1], c[0], c[1], w.sums[2], w.sums[3]);
-                        }
-                    }
-#pragma unroll
-                    for (int i = 0; i < G; ++i) {
-                        uint32_t x[2][2][4];
-                        float f[2][2];
-#pragma unroll
-                        for (int m = 0; m < 2; ++m)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                f[m][e] = i & 1 ? bf16hi(ks[m][e][i / 2]) : bf16lo(ks[m][e][i / 2]);
-#pragma unroll
-                                for (int j = 0; j < 4; ++j) x[m][e][j] = code_pair(k[m][e][i] >> (4 * j));
-                            }
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            const QueryOperand<G>& w = NT == 1 ? own : operand[n * 32 + lane];
-                            const uint4 q = *reinterpret_cast<const uint4*>(w.q[i]);
-                            const float2 s = *reinterpret_cast<const float2*>(w.start[i]);
-#pragma unroll
-                            for (int m = 0; m < 2; ++m) {
-                                float acc[4] = {s.x, s.y, s.x, s.y};
-                                mma(acc, x[m][0][0], x[m][1][0], x[m][0][1], x[m][1][1], q.x, q.y);
-                                mma(acc, x[m][0][2], x[m][1][2], x[m][0][3], x[m][1][3], q.z, q.w);
-                                z[n][m][0] = fmaf(f[m][0], acc[0], z[n][m][0]);
-                                z[n][m][1] = fmaf(f[m][0], acc[1], z[n][m][1]);
-                                z[n][m][2] = fmaf(f[m][1], acc[2], z[n][m][2]);
-                                z[n][m][3] = fmaf(f[m][1], acc[3], z[n][m][3]);
-                            }
-                        }
-                    }
-                }
-                // softmax: element (m, e) of n is token m 16 + g + 8 (e / 2) and row n 8 + 2 t + e % 2
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    float high[2] = {MINUS_INF, MINUS_INF};
-#pragma unroll
-                    for (int m = 0; m < 2; ++m)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            z[n][m][e] *= a.scale_log2;
-                            if (edge && token0 + m * 16 + g + 8 * (e / 2) >= limit[n][e & 1]) z[n][m][e] = MINUS_INF;
-                            high[e & 1] = fmaxf(high[e & 1], z[n][m][e]);
-                        }
-                    bool moved = false;
-                    float keep[2], base[2];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                        for (int off = 4; off < 32; off <<= 1) high[e] = fmaxf(high[e], __shfl_xor_sync(0xffffffffu, high[e], off));
-                        high[e] = fmaxf(high[e], top[n][e]);
-                        base[e] = high[e] == MINUS_INF ? 0.f : high[e];
-                        keep[e] = ex2_approx(top[n][e] - base[e]);
-                        moved |= high[e] != top[n][e];
-                        top[n][e] = high[e];
-                    }
-                    if (__any_sync(0xffffffffu, moved)) {
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            sum[n][e] *= keep[e];
-                            oc[n][e] *= keep[e];
-#pragma unroll
-                            for (int i = 0; i < G; ++i)
-#pragma unroll
-                                for (int j = 0; j < 2; ++j) {
-                                    o[n][i][j][e] *= keep[e];
-                                    o[n][i][j][2 + e] *= keep[e];
-                                }
-                        }
-                    }
-#pragma unroll
-                    for (int m = 0; m < 2; ++m)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            z[n][m][e] = ex2_approx(z[n][m][e] - base[e & 1]);
-                            sum[n][e & 1] += z[n][m][e];
-                        }
-                }
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    const int r = m * 16 + g, v = m * 16 + 2 * t;
-                    uint32_t w[4][(G + 1) / 2], s0[(G + 1) / 2], s1[(G + 1) / 2];
-                    lds<2 * G>(s0, block + L::kVScale + r * 2 * G);
-                    lds<2 * G>(s1, block + L::kVScale + (r + 8) * 2 * G);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) lds<2 * G>(w[e], block + L::kVCodes + (v + (e & 1) + 8 * (e / 2)) * (D / 2) + g * 2 * G);
-                    uint32_t c0 = *reinterpret_cast<const uint32_t*>(block + L::kVCentre + ((g % G) * 32 + v) * 2);
-                    uint32_t c1 = *reinterpret_cast<const uint32_t*>(block + L::kVCentre + ((g % G) * 32 + v + 8) * 2);
-                    if (g >= G) c0 = c1 = 0u;
-                    if (edge) {                            // (what nobody wrote may be no number; what was written is one)
-                        const int there = len - token0 - v;
-                        c0 &= (there > 0 ? 0x0000FFFFu : 0u) | (there > 1 ? 0xFFFF0000u : 0u);
-                        c1 &= (there > 8 ? 0x0000FFFFu : 0u) | (there > 9 ? 0xFFFF0000u : 0u);
-                    }
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-                        mma(oc[n], c0, 0u, c1, 0u, transposed(bf16x2(z[n][m][0], z[n][m][1])), transposed(bf16x2(z[n][m][2], z[n][m][3])));
-#pragma unroll
-                    for (int i = 0; i < G; ++i) {
-                        const uint32_t pick = i & 1 ? 0x7632u : 0x5410u;
-                        const uint32_t lo = __byte_perm(w[0][i / 2], w[1][i / 2], pick), hi = __byte_perm(w[2][i / 2], w[3][i / 2], pick);
-                        const float f0 = i & 1 ? bf16hi(s0[i / 2]) : bf16lo(s0[i / 2]), f1 = i & 1 ? bf16hi(s1[i / 2]) : bf16lo(s1[i / 2]);
-                        uint32_t x[8];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            x[e] = centred(code_pair(lo >> (4 * e)));
-                            x[4 + e] = centred(code_pair(hi >> (4 * e)));
-                        }
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            float p[4] = {z[n][m][0] * f0, z[n][m][1] * f0, z[n][m][2] * f1, z[n][m][3] * f1};
-                            if (edge) {                    // (the scale of a row that this query does not see may be no number)
-#pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    if (token0 + r + 8 * (e / 2) >= limit[n][e & 1]) p[e] = 0.f;
-                            }
-                            const uint32_t b0 = transposed(bf16x2(p[0], p[1])), b1 = transposed(bf16x2(p[2], p[3]));
-                            mma(o[n][i][0], x[0], x[1], x[4], x[5], b0, b1);
-                            mma(o[n][i][1], x[2], x[3], x[6], x[7], b0, b1);
-                        }
-                    }
-                }
+#pragma unroll 1
+            for (int m = 0; m < 2; ++m) {
+                const int token = token0 + 16 * m;
+                if (token + 16 <= least) half_block(block, m, token, std::false_type{});
+                else if (token < most) half_block(block, m, token, std::true_type{});
             }
             __syncwarp();
             fetch();
@@ -421,16 +459,15 @@ cache_attention_kernel(AttArgs a) {
 
         // the CTA's warps joined, two groups at a time.  o[n][i][j][e]: element i 32 + 4 g + 2 j + e / 2 of row n 8 + 2 t + e % 2
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                for (int off = 4; off < 32; off <<= 1) sum[n][e] += __shfl_xor_sync(0xffffffffu, sum[n][e], off);
-                if (g == 0) {
-                    join_max[warp * NR + n * 8 + 2 * t + e] = top[n][e];
-                    join_sum[warp * NR + n * 8 + 2 * t + e] = sum[n][e];
-                }
+        for (int n = 0; n < NT; ++n) {
+            sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 1);
+            sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 2);
+            if (t == 0) {
+                join_max[warp * NR + n * 8 + g] = top[n] * a.scale_log2;
+                join_sum[warp * NR + n * 8 + g] = sum[n];
             }
+        }
+        now = *at_work;
         const bool whole = now.tile == 0 && count == now.blocks;
         float* const part = SHARES && !whole ? a.part + (size_t)(2 * blockIdx.x + (now.tile == 0 ? 1 : 0)) * NR * (D + 2) : nullptr;
         const int je = warp & 1, ji = warp >> 1;           // this warp's share: group i0 + ji, rows n 8 + 2 t + je
@@ -467,7 +504,7 @@ cache_attention_kernel(AttArgs a) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k) v[k] = fmaf(join[((w * 2 + ji) * 8 + 4 * je + k) * 32 + lane], f[w], v[k]);
                 const bool none = high == MINUS_INF && total == 0.f;
-                const int tq = r / a.R, hq = h * a.R + (r - tq * a.R);
+                const int tq = quotient(r, a.R), hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
                 if (r < rows) {
                     if (part) {
                         *reinterpret_cast<float4*>(part + rl * D + (i0 + ji) * 32 + 4 * g) = make_float4(v[0], v[1], v[2], v[3]);
@@ -487,26 +524,27 @@ cache_attention_kernel(AttArgs a) {
             }
         }
         next(now);
-    }
+        put(at_work, now);
+    } while (now.left > 0);
 }
 
 // The pieces of a head and tile of rows that several CTAs shared, in their order, one row a CTA.
 constexpr int kJoinThreads = 128;
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads)
-cache_attention_join_kernel(AttArgs a, int NR, int most) {
+cache_attention_join_kernel(AttArgs a, int NR, int rows, int most) {
     constexpr int kQuads = D / 4;                          // threads that share a row's elements; kBy of them by piece
     constexpr int kBy = kJoinThreads / kQuads;
     __shared__ float red[kBy][D];
     __shared__ float weight[kJoinThreads];
-    const int segs = a.H * a.RT;
-    const int s = blockIdx.x / NR, rl = blockIdx.x - s * NR, b = s / segs, seg = s - b * segs;
-    const int h = seg / a.RT, r = (seg - h * a.RT) * NR + rl;
+    const int segs = a.H * a.RT.d;
+    const int s = blockIdx.x / rows, rl = blockIdx.x - s * rows, b = s / segs, seg = s - b * segs;
+    const int h = quotient(seg, a.RT), r = (seg - h * (int)a.RT.d) * NR + rl;
     grid_dependency_wait();
-    if (r >= a.R * a.Tq) return;
+    if (r >= (int)a.R.d * a.Tq) return;
     const int first = a.before[b], blocks = a.before[b + 1] - first;
     const int64_t total = (int64_t)a.before[a.B] * segs, from = (int64_t)first * segs + (int64_t)seg * blocks;
-    const int tq = r / a.R, hq = h * a.R + (r - tq * a.R);
+    const int tq = quotient(r, a.R), hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
     __nv_bfloat16* const out = a.io.out + b * a.io.ob + hq * a.io.oh + tq * a.io.ot;
     float* const lse = a.lse ? a.lse + ((int64_t)b * a.Hq + hq) * a.Tq + tq : nullptr;
     if (blocks == 0) {
@@ -606,7 +644,7 @@ size_t part_bytes(const Plan& p, int d) { return align_up((size_t)2 * p.ctas * 8
 template <int D, int NT>
 int launch(AttArgs a, const Plan& p, cudaStream_t stream) {
     constexpr size_t kSmem = (size_t)kWarps * kStages * CacheBlock<D>::kBytes + kWarps * 2048 + 2 * kWarps * 8 * NT * 4 +
-                             (NT > 1 ? NT * 32 * sizeof(QueryOperand<D / 32>) : 0);
+                             NT * 32 * sizeof(QueryOperand<D / 32>) + kWarps * 2 * sizeof(Walk);
     static DoneOnDevice done[2];
     const bool shares = p.ctas > 0;
     const size_t smem = kSmem + (shares ? align_up((size_t)(a.B + 1) * 4, 16) : 0);
@@ -617,7 +655,7 @@ int launch(AttArgs a, const Plan& p, cudaStream_t stream) {
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(shares ? p.ctas : a.B * a.H * a.RT));
+    cfg.gridDim = dim3((unsigned)(shares ? p.ctas : a.B * a.H * p.RT));
     cfg.blockDim = dim3(kWarps * 32);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
@@ -628,11 +666,12 @@ int launch(AttArgs a, const Plan& p, cudaStream_t stream) {
         rc = record_cuda(cudaLaunchKernelEx(&cfg, kern, a));
         if (rc != VITCOP_OK || !shares) return rc;
     }
-    cfg.gridDim = dim3((unsigned)(a.B * a.H * a.RT * 8 * NT));
+    const int rows = (int)a.R.d * a.Tq < 8 * NT ? (int)a.R.d * a.Tq : 8 * NT;      // that a tile has at most
+    cfg.gridDim = dim3((unsigned)(a.B * a.H * (int)a.RT.d * rows));
     cfg.blockDim = dim3(kJoinThreads);
     cfg.dynamicSmemBytes = 0;
     KernelTimeScope timed("cache_attention_join_kernel", stream);
-    return record_cuda(cudaLaunchKernelEx(&cfg, cache_attention_join_kernel<D>, a, 8 * NT, p.ctas));
+    return record_cuda(cudaLaunchKernelEx(&cfg, cache_attention_join_kernel<D>, a, 8 * NT, rows, p.ctas));
 }
 
 }  // namespace
@@ -655,8 +694,11 @@ int launch_cache_attention(const CacheQueries& io, const void* cache, int B, int
     a.status = static_cast<int*>(workspace);
     a.before = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + kStatusBytes);
     a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kStatusBytes + align_up((size_t)(B + 1) * 4, 256));
-    a.B = B; a.Hq = Hq; a.H = H; a.R = Hq / H; a.Tq = Tq; a.Ncap = Ncap; a.RT = p.RT; a.causal = causal ? 1 : 0;
-    a.scale_log2 = scale * kLog2e;
+    a.B = B; a.Hq = Hq; a.H = H; a.R = divisor(Hq / H); a.Tq = Tq; a.Ncap = Ncap; a.RT = divisor(p.RT); a.causal = causal ? 1 : 0;
+    // (a scale of 0 is queries of 0)
+    a.zero = scale == 0.f;
+    a.sign = scale < 0.f ? 0x80008000u : 0u;
+    a.scale_log2 = a.zero ? 1.f : (scale < 0.f ? -scale : scale) * kLog2e;
     if (d == 64) return p.NT == 1 ? launch<64, 1>(a, p, stream) : p.NT == 2 ? launch<64, 2>(a, p, stream) : launch<64, 4>(a, p, stream);
     if (d == 128) return p.NT == 1 ? launch<128, 1>(a, p, stream) : p.NT == 2 ? launch<128, 2>(a, p, stream) : launch<128, 4>(a, p, stream);
     return p.NT == 1 ? launch<256, 1>(a, p, stream) : launch<256, 2>(a, p, stream);
