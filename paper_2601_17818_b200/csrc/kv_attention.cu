@@ -1,11 +1,11 @@
 // Attention of query rows over the K/V cache in 4 bits: out = softmax(scale q K^T) V over the rows that a query sees.
 //
 // Every product is one of matrix instructions (m16n8k16, bf16 in, fp32 out), and codes become operands in registers:
-//   logits   query rows (Hq / H heads times Tq queries, a tile of 8 NT of them at a time) times tokens.  A code c is the bf16
+//   logits   tokens times query rows (Hq / H heads times Tq queries, a tile of 8 NT of them at a time).  A code c is the bf16
 //            128 + c (its nibble under the exponent of 128), exactly; per group the token's scale multiplies the product in fp32.
 //            The centres, and the scales times -136, are one more product each, with the groups' sums of q split into three bf16
-//   output   elements times query rows: (128 + c) - 136 = c - 8 is exact too.  The weights of two neighbouring tokens lie in a lane as
-//            the logits left it there, and that is what this product takes: bf16(p) with the centres, bf16(bf16(p) s) with a group's codes
+//   output   elements times query rows: (128 + c) - 136 = c - 8 is exact too.  The weights enter, transposed, as bf16(p) with the
+//            centres and as bf16(bf16(p) s) with a group's codes
 // A warp takes every fourth block of 32 tokens of its CTA's piece, with blocks ahead in shared memory (cp.async), and keeps maximum, sum
 // and output of its own; the CTA joins its warps, a second kernel joins the CTAs that shared a head.
 #include <cuda_bf16.h>
@@ -23,6 +23,7 @@ constexpr int kWarps = 4;
 constexpr int kStages = 2;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 #define MINUS_INF (-__builtin_huge_valf())
+constexpr float kNoLogit = -3.4e38f;                       // below every logit that is a number: nothing seen yet
 
 // Resident CTAs an SM, which the registers of the accumulators and the ring's memory leave room for.
 constexpr int ctas_per_sm(int D, int NT) { return D == 256 || NT == 4 ? 2 : D * NT <= 128 ? 4 : 3; }
@@ -65,6 +66,11 @@ __device__ __forceinline__ void mma_zero(float (&d)[4], uint32_t a0, uint32_t a1
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {   // an 8 x 8 matrix of 16-bit values, two of a row in a lane
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
 __device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
@@ -280,14 +286,18 @@ cache_attention_kernel(AttArgs a) {
             const int r = row0 + warp * 8 + g, tq = quotient(r, a.R), hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
             load_queries<G>(operand + warp * 32 + lane, a.io.q + b * a.io.qb + hq * a.io.qh + tq * a.io.qt, r < rows && !a.zero, a.sign, t);
         }
-        float o[NT][G][2][4], oc[NT][4], top[NT], sum[NT];
-        int limit[NT];
+        // o[n][i][j][e]: element i 32 + 4 g + 2 j + e / 2 of row n 8 + 2 t + e % 2; base, sum: rows n 8 + 2 t + e, in powers of two
+        float o[NT][G][2][4], oc[NT][4], base[NT][2], sum[NT][2];
+        int limit[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int r = row0 + n * 8 + g;
-            limit[n] = r < rows ? (a.causal ? max(0, len - a.Tq + quotient(r, a.R) + 1) : len) : 0;
-            top[n] = MINUS_INF;
-            sum[n] = 0.f;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = row0 + n * 8 + 2 * t + e;
+                limit[n][e] = r < rows ? (a.causal ? max(0, len - a.Tq + quotient(r, a.R) + 1) : len) : 0;
+                base[n][e] = kNoLogit;
+                sum[n][e] = 0.f;
+            }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 oc[n][e] = 0.f;
@@ -300,103 +310,98 @@ cache_attention_kernel(AttArgs a) {
         const int least = a.causal ? max(0, len - a.Tq + quotient(row0, a.R) + 1) : len;
         const int most = a.causal ? max(0, len - a.Tq + quotient(last, a.R) + 1) : len;
 
-        // Half m of a block: 16 tokens.  z[n][j][e]: row n 8 + g, token 8 j + 2 t + e.  EDGE: some row does not see some of them.
+        // Half m of a block: 16 tokens from token0 on.  z[n][e]: token g + 8 (e / 2), row n 8 + 2 t + e % 2.  EDGE: some row does not
+        // see some of them.
         const auto half_block = [&](const uint8_t* block, int m, int token0, auto edge_) {
             constexpr bool EDGE = decltype(edge_)::value;
-            constexpr int kHalves = NT > 1 ? 2 : 1;        // rows g, and g + 8 where there are any, of an operand
-            float z[NT][2][2];
+            float z[NT][4];
             {
-                uint32_t k[2][G], s[2][G];
+                const int r = 16 * m + g;
+                uint32_t k0[G], k1[G], s0[(G + 1) / 2], s1[(G + 1) / 2];
+                lds<4 * G>(k0, block + L::kKCodes + r * (D / 2) + t * 4 * G);
+                lds<4 * G>(k1, block + L::kKCodes + (r + 8) * (D / 2) + t * 4 * G);
+                lds<2 * G>(s0, block + L::kKScale + r * 2 * G);
+                lds<2 * G>(s1, block + L::kKScale + (r + 8) * 2 * G);
+                const int pair = 2 * ((2 * t) % G);
+                const uint32_t c0 = *reinterpret_cast<const uint32_t*>(block + L::kKCentre + r * 2 * G + pair);
+                const uint32_t c1 = *reinterpret_cast<const uint32_t*>(block + L::kKCentre + (r + 8) * 2 * G + pair);
+                const uint32_t f0 = *reinterpret_cast<const uint32_t*>(block + L::kKScale + r * 2 * G + pair);
+                const uint32_t f1 = *reinterpret_cast<const uint32_t*>(block + L::kKScale + (r + 8) * 2 * G + pair);
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int r = 16 * m + 8 * j;
-                    lds<4 * G>(k[j], block + L::kKCodes + (r + g) * (D / 2) + t * 4 * G);
-                    lds<4 * G>(s[j], block + L::kKScale + (r + 2 * t) * 2 * G);        // of two tokens
-                    const uint32_t kc = *reinterpret_cast<const uint32_t*>(block + L::kKCentre + (r + g) * 2 * G + 2 * ((2 * t) % G));
-                    const uint32_t ks = *reinterpret_cast<const uint32_t*>(block + L::kKScale + (r + g) * 2 * G + 2 * ((2 * t) % G));
-#pragma unroll
-                    for (int n = 0; n < NT; n += 2) {
-                        const uint4 u = operand[n * 32 + lane].sums;
-                        const uint4 v = NT > 1 ? operand[(n + 1) * 32 + lane].sums : make_uint4(0, 0, 0, 0);
-                        float c[4], f[4];
-                        mma_zero(c, u.x, v.x, u.y, v.y, kc, kc);
-                        mma_zero(f, u.x, v.x, u.y, v.y, ks, ks);
-                        if constexpr (G == 8) {
-                            mma(c, u.z, v.z, u.w, v.w, kc, kc);
-                            mma(f, u.z, v.z, u.w, v.w, ks, ks);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 2 * kHalves; ++e) z[n + e / 2][j][e & 1] = fmaf(-136.f, f[e], c[e]);
+                for (int n = 0; n < NT; ++n) {
+                    const uint4 u = operand[n * 32 + lane].sums;
+                    float f[4];
+                    mma_zero(z[n], c0, c1, c0, c1, u.x, u.y);
+                    mma_zero(f, f0, f1, f0, f1, u.x, u.y);
+                    if constexpr (G == 8) {
+                        mma(z[n], c0, c1, c0, c1, u.z, u.w);
+                        mma(f, f0, f1, f0, f1, u.z, u.w);
                     }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) z[n][e] = fmaf(-136.f, f[e], z[n][e]);
                 }
 #pragma unroll
                 for (int i = 0; i < G; ++i) {
-                    uint32_t x[2][4];
-                    f32x2 f[2];
+                    uint32_t x0[4], x1[4];
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) x[j][e] = code_pair(k[j][i] >> (4 * e));
-                        f[j] = i & 1 ? pack2(bf16hi(s[j][i / 2]), bf16hi(s[j][(G + i) / 2])) : pack2(bf16lo(s[j][i / 2]), bf16lo(s[j][(G + i) / 2]));
+                    for (int e = 0; e < 4; ++e) {
+                        x0[e] = code_pair(k0[i] >> (4 * e));
+                        x1[e] = code_pair(k1[i] >> (4 * e));
                     }
+                    const float h0 = i & 1 ? bf16hi(s0[i / 2]) : bf16lo(s0[i / 2]), h1 = i & 1 ? bf16hi(s1[i / 2]) : bf16lo(s1[i / 2]);
 #pragma unroll
-                    for (int n = 0; n < NT; n += 2) {
+                    for (int n = 0; n < NT; ++n) {
                         const uint4 u = operand[n * 32 + lane].q[i];
-                        const uint4 v = NT > 1 ? operand[(n + 1) * 32 + lane].q[i] : make_uint4(0, 0, 0, 0);
+                        float acc[4];
+                        mma_zero(acc, x0[0], x1[0], x0[1], x1[1], u.x, u.y);
+                        mma(acc, x0[2], x1[2], x0[3], x1[3], u.z, u.w);
+                        z[n][0] = fmaf(h0, acc[0], z[n][0]);
+                        z[n][1] = fmaf(h0, acc[1], z[n][1]);
+                        z[n][2] = fmaf(h1, acc[2], z[n][2]);
+                        z[n][3] = fmaf(h1, acc[3], z[n][3]);
+                    }
+                }
+            }
+            uint32_t p[NT][2], seen[NT][2];                // weights of tokens 2 t, 2 t + 1 and 8 behind, row n 8 + g; which of them it sees
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            float acc[4];
-                            mma_zero(acc, u.x, v.x, u.y, v.y, x[j][0], x[j][1]);
-                            mma(acc, u.z, v.z, u.w, v.w, x[j][2], x[j][3]);
+            for (int n = 0; n < NT; ++n) {
+                if constexpr (EDGE) {
 #pragma unroll
-                            for (int e = 0; e < kHalves; ++e) {
-                                const float2 y = unpack2(fma2(f[j], pack2(acc[2 * e], acc[2 * e + 1]), pack2(z[n + e][j][0], z[n + e][j][1])));
-                                z[n + e][j][0] = y.x;
-                                z[n + e][j][1] = y.y;
+                    for (int e = 0; e < 4; ++e)
+                        if (token0 + g + 8 * (e / 2) >= limit[n][e & 1]) z[n][e] = MINUS_INF;
+                    const int even = __shfl_sync(0xffffffffu, limit[n][0], g >> 1), odd = __shfl_sync(0xffffffffu, limit[n][1], g >> 1);
+                    const int there = (g & 1 ? odd : even) - token0 - 2 * t;
+                    seen[n][0] = (there > 0 ? 0x0000FFFFu : 0u) | (there > 1 ? 0xFFFF0000u : 0u);
+                    seen[n][1] = (there > 8 ? 0x0000FFFFu : 0u) | (there > 9 ? 0xFFFF0000u : 0u);
+                }
+                // (the sums stay relative to an older maximum until a logit has passed it by 2^8)
+                float high[2] = {fmaxf(z[n][0], z[n][2]), fmaxf(z[n][1], z[n][3])};
+                if (__any_sync(0xffffffffu, fmaf(high[0], a.scale_log2, -base[n][0]) > 8.f || fmaf(high[1], a.scale_log2, -base[n][1]) > 8.f)) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                        for (int off = 4; off < 32; off <<= 1) high[e] = fmaxf(high[e], __shfl_xor_sync(0xffffffffu, high[e], off));
+                        const float top = fmaxf(base[n][e], high[e] * a.scale_log2), keep = ex2_approx(base[n][e] - top);
+                        base[n][e] = top;
+                        sum[n][e] *= keep;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            oc[n][2 * h + e] *= keep;
+#pragma unroll
+                            for (int i = 0; i < G; ++i) {
+                                o[n][i][0][2 * h + e] *= keep;
+                                o[n][i][1][2 * h + e] *= keep;
                             }
                         }
                     }
                 }
-            }
-            uint32_t p[NT][2], seen[NT][2];                // weights of two tokens; which of them the row sees
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float high = top[n];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    if constexpr (EDGE) {
-                        const int there = limit[n] - token0 - 8 * j - 2 * t;
-                        if (there < 1) z[n][j][0] = MINUS_INF;
-                        if (there < 2) z[n][j][1] = MINUS_INF;
-                        seen[n][j] = (there > 0 ? 0x0000FFFFu : 0u) | (there > 1 ? 0xFFFF0000u : 0u);
-                    }
-                    high = fmaxf(high, fmaxf(z[n][j][0], z[n][j][1]));
+                for (int e = 0; e < 4; ++e) {
+                    z[n][e] = ex2_approx(fmaf(z[n][e], a.scale_log2, -base[n][e & 1]));
+                    sum[n][e & 1] += z[n][e];
                 }
-                high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, 1));
-                high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, 2));
-                // (the sums stay relative to an older maximum until one of the warp's rows has passed its own 2^8 times)
-                if (__any_sync(0xffffffffu, (high - top[n]) * a.scale_log2 > 8.f)) {
-                    const float keep = high == MINUS_INF ? 1.f : ex2_approx((top[n] - high) * a.scale_log2);
-                    const float k0 = __shfl_sync(0xffffffffu, keep, 8 * t), k1 = __shfl_sync(0xffffffffu, keep, 8 * t + 4);
-                    top[n] = high;
-                    sum[n] *= keep;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        oc[n][e] *= e & 1 ? k1 : k0;
-#pragma unroll
-                        for (int i = 0; i < G; ++i) {
-                            o[n][i][0][e] *= e & 1 ? k1 : k0;
-                            o[n][i][1][e] *= e & 1 ? k1 : k0;
-                        }
-                    }
-                }
-                const float base = top[n] == MINUS_INF ? 0.f : top[n] * a.scale_log2;
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const float p0 = ex2_approx(fmaf(z[n][j][0], a.scale_log2, -base)), p1 = ex2_approx(fmaf(z[n][j][1], a.scale_log2, -base));
-                    sum[n] += p0 + p1;
-                    p[n][j] = bf16x2(p0, p1);
-                }
+                p[n][0] = transposed(bf16x2(z[n][0], z[n][1]));
+                p[n][1] = transposed(bf16x2(z[n][2], z[n][3]));
             }
             {
                 const int v = m * 16 + 2 * t;              // tokens v, v + 1, v + 8, v + 9
@@ -457,16 +462,18 @@ cache_attention_kernel(AttArgs a) {
             use = use + 1 == kStages ? 0 : use + 1;
         }
 
-        // the CTA's warps joined, two groups at a time.  o[n][i][j][e]: element i 32 + 4 g + 2 j + e / 2 of row n 8 + 2 t + e % 2
+        // the CTA's warps joined, two groups at a time
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 1);
-            sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 2);
-            if (t == 0) {
-                join_max[warp * NR + n * 8 + g] = top[n] * a.scale_log2;
-                join_sum[warp * NR + n * 8 + g] = sum[n];
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                for (int off = 4; off < 32; off <<= 1) sum[n][e] += __shfl_xor_sync(0xffffffffu, sum[n][e], off);
+                if (g == 0) {
+                    join_max[warp * NR + n * 8 + 2 * t + e] = base[n][e];
+                    join_sum[warp * NR + n * 8 + 2 * t + e] = sum[n][e];
+                }
             }
-        }
         now = *at_work;
         const bool whole = now.tile == 0 && count == now.blocks;
         float* const part = SHARES && !whole ? a.part + (size_t)(2 * blockIdx.x + (now.tile == 0 ? 1 : 0)) * NR * (D + 2) : nullptr;
@@ -474,7 +481,7 @@ cache_attention_kernel(AttArgs a) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int rl = n * 8 + 2 * t + je, r = row0 + rl;
-            float f[kWarps], high = MINUS_INF, total = 0.f;
+            float f[kWarps], high = kNoLogit, total = 0.f;
 #pragma unroll
             for (int i0 = 0; i0 < G; i0 += 2) {
 #pragma unroll
@@ -494,7 +501,7 @@ cache_attention_kernel(AttArgs a) {
                     for (int w = 0; w < kWarps; ++w) high = fmaxf(high, join_max[w * NR + rl]);
 #pragma unroll
                     for (int w = 0; w < kWarps; ++w) {
-                        f[w] = ex2_approx(join_max[w * NR + rl] - (high == MINUS_INF ? 0.f : high));
+                        f[w] = ex2_approx(join_max[w * NR + rl] - high);
                         total = fmaf(join_sum[w * NR + rl], f[w], total);
                     }
                 }
@@ -503,7 +510,7 @@ cache_attention_kernel(AttArgs a) {
                 for (int w = 0; w < kWarps; ++w)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) v[k] = fmaf(join[((w * 2 + ji) * 8 + 4 * je + k) * 32 + lane], f[w], v[k]);
-                const bool none = high == MINUS_INF && total == 0.f;
+                const bool none = total == 0.f;
                 const int tq = quotient(r, a.R), hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
                 if (r < rows) {
                     if (part) {
@@ -559,14 +566,13 @@ cache_attention_join_kernel(AttArgs a, int NR, int rows, int most) {
     const int n = c1 - c0 + 1;
     const size_t size = (size_t)NR * (D + 2);
     const auto slot = [&](int c) { return a.part + (size_t)(2 * (c0 + c) + (c == 0 ? 1 : 0)) * size; };
-    float high = MINUS_INF;
+    float high = kNoLogit;
     for (int c = threadIdx.x; c < n; c += kJoinThreads) high = fmaxf(high, slot(c)[NR * D + rl]);
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, off));
     if ((threadIdx.x & 31) == 0) weight[threadIdx.x >> 5] = high;
     __syncthreads();
     high = fmaxf(fmaxf(weight[0], weight[1]), fmaxf(weight[2], weight[3]));
-    const float base = high == MINUS_INF ? 0.f : high;
     __syncthreads();
     const int col = threadIdx.x % kQuads, by = threadIdx.x / kQuads;
     float v[4] = {}, sum = 0.f;
@@ -574,7 +580,7 @@ cache_attention_join_kernel(AttArgs a, int NR, int rows, int most) {
         const int m = min(n - c0_, kJoinThreads);
         if ((int)threadIdx.x < m) {
             const float* const p = slot(c0_ + threadIdx.x) + NR * D + rl;
-            const float f = ex2_approx(p[0] - base);
+            const float f = ex2_approx(p[0] - high);
             weight[threadIdx.x] = f;
             sum = fmaf(p[NR], f, sum);
         }
@@ -597,7 +603,7 @@ cache_attention_join_kernel(AttArgs a, int NR, int rows, int most) {
     __syncthreads();
     sum = (weight[0] + weight[1]) + (weight[2] + weight[3]);
     __syncthreads();
-    const bool none = high == MINUS_INF && sum == 0.f;
+    const bool none = sum == 0.f;
     const float inv = none ? 0.f : 1.f / sum;
     for (int e = threadIdx.x; e < D; e += kJoinThreads) {
         float x = red[0][e];
@@ -605,7 +611,7 @@ cache_attention_join_kernel(AttArgs a, int NR, int rows, int most) {
         for (int k = 1; k < kBy; ++k) x += red[k][e];
         out[e] = __float2bfloat16_rn(x * inv);
     }
-    if (lse && threadIdx.x == 0) *lse = none ? MINUS_INF : (base + __log2f(sum)) * kLn2;
+    if (lse && threadIdx.x == 0) *lse = none ? MINUS_INF : (high + __log2f(sum)) * kLn2;
 }
 
 int sm_count() {
