@@ -21,6 +21,7 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kStages = 2;
+constexpr int kWholeBlocks = 24;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 #define MINUS_INF (-__builtin_huge_valf())
 constexpr float kNoLogit = -3.4e38f;                       // below every logit that is a number: nothing seen yet
@@ -46,7 +47,7 @@ struct AttArgs {
     const int32_t* cache_len;
     float* lse;
     int* status;
-    int32_t* before;                                       // shares: blocks in front of each sample, [B + 1]
+    int32_t* before;                                       // shares: blocks in front of each sample, [B + 1], and of the longest
     float* part;                                           // shares: two pieces a CTA, each [8 NT][D + 2]
     int B, Hq, H, Tq, Ncap, causal;
     Divisor R, RT;                                         // query heads of a stored one, tiles of rows
@@ -115,12 +116,12 @@ struct __align__(16) QueryOperand {
     uint4 sums;                                            // (the second half: eight groups)
 };
 template <int G>
-__device__ __forceinline__ void load_queries(QueryOperand<G>* to, const __nv_bfloat16* src, bool there, uint32_t sign, int t) {
+__device__ __forceinline__ void make_operand(QueryOperand<G>* to, const uint4* raw, uint32_t sign, uint32_t keep, int t) {
     float total[G];
 #pragma unroll
     for (int i = 0; i < G; ++i) {
-        uint4 v = there ? __ldg(reinterpret_cast<const uint4*>(src + t * 8 + i * 32)) : make_uint4(0, 0, 0, 0);
-        v = make_uint4(v.x ^ sign, v.y ^ sign, v.z ^ sign, v.w ^ sign);
+        uint4 v = raw[i * 32];
+        v = make_uint4((v.x ^ sign) & keep, (v.y ^ sign) & keep, (v.z ^ sign) & keep, (v.w ^ sign) & keep);
         // elements 0 and 4, 1 and 5, 2 and 6, 3 and 7, as the codes lie
         to->q[i] = make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
         float x = ((bf16lo(v.x) + bf16hi(v.x)) + (bf16lo(v.y) + bf16hi(v.y))) + ((bf16lo(v.z) + bf16hi(v.z)) + (bf16lo(v.w) + bf16hi(v.w)));
@@ -155,9 +156,25 @@ __device__ __forceinline__ int blocks_of(const AttArgs& a, int b) {
     const int len = a.cache_len ? max(0, min(__ldg(a.cache_len + b), a.Ncap)) : a.Ncap;
     return (len + kCacheBlock - 1) / kCacheBlock;
 }
-// CTAs that `total` blocks are shared out to: each has a block for every warp, or there is one CTA.
-__device__ __forceinline__ int sharers(int64_t total, int ctas) {
-    return (int)max((int64_t)1, min((int64_t)ctas, total / kWarps));
+// How `total` blocks are shared out: the first `more` of `ctas` CTAs have `each` + 1 blocks, the others `each`; `whole`: a CTA has
+// the blocks of one segment instead.
+struct Shares {
+    int ctas, each, more;
+    bool whole;
+};
+__device__ __forceinline__ Shares shares_of(int total, int longest, int segs, int most) {
+    Shares s;
+    s.ctas = max(1, min(most, total / kWarps));            // a block for every warp of a CTA, or there is one CTA
+    s.each = total / s.ctas;
+    s.more = total - s.each * s.ctas;
+    // where the longest segment takes hardly longer than a fair share, pieces to join and heads to begin anew cost more
+    s.whole = segs <= most && longest <= s.each + kWholeBlocks;
+    return s;
+}
+__device__ __forceinline__ int first_of(const Shares& s, int cta) { return cta * s.each + min(cta, s.more); }
+__device__ __forceinline__ int holder_of(const Shares& s, int block) {
+    const int front = s.more * (s.each + 1);
+    return block < front ? block / (s.each + 1) : s.more + (block - front) / s.each;
 }
 __device__ __forceinline__ int piece(const Walk& w) { return min(w.blocks - w.tile, w.left); }
 
@@ -172,8 +189,10 @@ cache_attention_kernel(AttArgs a) {
     float* const join_max = join + kWarps * 512;                                            // [warp][NR]
     float* const join_sum = join_max + kWarps * NR;
     QueryOperand<G>* const operand = reinterpret_cast<QueryOperand<G>*>(join_sum + kWarps * NR);      // [NT][lane]
-    Walk* const walks = reinterpret_cast<Walk*>(operand + NT * 32);                                   // [warp][2]
-    int32_t* const before = reinterpret_cast<int32_t*>(walks + kWarps * 2);                           // [B + 1]
+    uint4* const queries = reinterpret_cast<uint4*>(operand + NT * 32);                                // [stage][NT][G][lane]
+    Walk* const walks = reinterpret_cast<Walk*>(queries + kStages * NT * G * 32);                                   // [warp][2]
+    int32_t* const stage_at = reinterpret_cast<int32_t*>(walks + kWarps * 2);                         // of warp 0
+    int32_t* const before = stage_at + 1;                           // [B + 2]
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int segs = a.H * a.RT.d;
     grid_dependency_wait();
@@ -185,9 +204,9 @@ cache_attention_kernel(AttArgs a) {
     Walk* const at_fetch = walks + warp * 2 + 1;
     Walk now;
     if constexpr (SHARES) {
-        // blocks in front of each sample
+        // blocks in front of each sample, and of the longest
         if (warp == 0) {
-            int sum = 0;
+            int sum = 0, longest = 0;
             for (int b0 = 0; b0 < a.B; b0 += 32) {
                 int v = b0 + lane < a.B ? blocks_of(a, b0 + lane) : 0;
                 const int mine = v;
@@ -198,27 +217,40 @@ cache_attention_kernel(AttArgs a) {
                 }
                 if (b0 + lane < a.B) before[b0 + lane] = sum + v - mine;
                 sum += __shfl_sync(0xffffffffu, v, 31);
+                longest = max(longest, mine);
             }
-            if (lane == 0) before[a.B] = sum;
+            longest = __reduce_max_sync(0xffffffffu, longest);
+            if (lane == 0) {
+                before[a.B] = sum;
+                before[a.B + 1] = longest;
+            }
         }
         __syncthreads();
         if (blockIdx.x == 0)
-            for (int i = threadIdx.x; i <= a.B; i += kWarps * 32) a.before[i] = before[i];
-        const int64_t total = (int64_t)before[a.B] * segs;
-        const int ctas = sharers(total, gridDim.x);
-        if (total == 0 || (int)blockIdx.x >= ctas) return;
-        const int64_t from = total * blockIdx.x / ctas, to = total * (blockIdx.x + 1) / ctas;
-        int lo = 0, hi = a.B;                              // the last sample that starts at or before `from` and has blocks
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if ((int64_t)before[mid] * segs <= from) lo = mid; else hi = mid;
+            for (int i = threadIdx.x; i <= a.B + 1; i += kWarps * 32) a.before[i] = before[i];
+        const int total = before[a.B] * segs;
+        const Shares share = shares_of(total, before[a.B + 1], a.B * segs, gridDim.x);
+        if (share.whole) {
+            if ((int)blockIdx.x >= a.B * segs) return;
+            now.b = blockIdx.x / segs;
+            now.seg = blockIdx.x - now.b * segs;
+            now.tile = 0;
+            now.blocks = now.left = before[now.b + 1] - before[now.b];
+        } else {
+            if ((int)blockIdx.x >= share.ctas || total == 0) return;
+            const int from = first_of(share, blockIdx.x);
+            int lo = 0, hi = a.B;                          // the last sample that starts at or before `from`: it has blocks
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) / 2;
+                if (before[mid] * segs <= from) lo = mid; else hi = mid;
+            }
+            now.b = lo;
+            now.blocks = before[lo + 1] - before[lo];
+            const int in = from - before[lo] * segs;
+            now.seg = in / now.blocks;
+            now.tile = in - now.seg * now.blocks;
+            now.left = first_of(share, blockIdx.x + 1) - from;
         }
-        now.b = lo;
-        now.blocks = before[lo + 1] - before[lo];
-        const int64_t in = from - (int64_t)before[lo] * segs;
-        now.seg = (int)(in / now.blocks);
-        now.tile = (int)(in - (int64_t)now.seg * now.blocks);
-        now.left = (int)(to - from);
     } else {
         now.b = blockIdx.x / segs;
         now.seg = blockIdx.x - now.b * segs;
@@ -252,6 +284,7 @@ cache_attention_kernel(AttArgs a) {
     uint8_t* const ring = smem + warp * kStages * L::kBytes;
     const uint32_t ring_at = smem_u32(ring) + lane * 16;
     int fill = 0;
+    bool begins = true;                                    // a piece, whose queries come with its first block
     const auto fetch = [&]() {
         if (SHARES && ahead_left <= 0) {
             Walk w = *at_fetch;
@@ -259,6 +292,7 @@ cache_attention_kernel(AttArgs a) {
                 next(w);
                 ahead_left = piece(w) - warp;
                 ahead_src = first_block(w);
+                begins = true;
             }
             put(at_fetch, w);
         }
@@ -267,6 +301,21 @@ cache_attention_kernel(AttArgs a) {
 #pragma unroll
             for (int i = 0; i < kChunks / 32; ++i)
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + i * 512), "l"(ahead_src + i * 512) : "memory");
+            if (warp == 0 && begins) {
+                begins = false;
+                const int b = at_fetch->b, seg = at_fetch->seg, h = quotient(seg, a.RT), row0 = (seg - h * (int)a.RT.d) * NR;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const int r = row0 + n * 8 + g, tq = quotient(r, a.R), hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
+                    const bool there = r < (int)a.R.d * a.Tq;
+                    const __nv_bfloat16* const src = a.io.q + (there ? b * a.io.qb + hq * a.io.qh + tq * a.io.qt + t * 8 : 0);
+                    const uint32_t to = smem_u32(queries + ((fill * NT + n) * G) * 32 + lane);
+#pragma unroll
+                    for (int i = 0; i < G; ++i)            // (rows behind the last are zeros)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + i * 512), "l"(src + (there ? i * 32 : 0)), "r"(there ? 16 : 0)
+                                     : "memory");
+                }
+            }
             ahead_left -= kWarps;
             ahead_src += kWarps * L::kBytes;
             fill = fill + 1 == kStages ? 0 : fill + 1;
@@ -282,9 +331,15 @@ cache_attention_kernel(AttArgs a) {
         const int b = now.b, h = quotient(now.seg, a.RT), row0 = (now.seg - h * (int)a.RT.d) * NR, rows = (int)a.R.d * a.Tq;
         const int count = piece(now);
         const int len = a.cache_len ? max(0, min(__ldg(a.cache_len + b), a.Ncap)) : a.Ncap;
+        // (they came with the first block of warp 0)
+        if (warp == 0) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+            if (NT > 1 && lane == 0) *stage_at = use;
+        }
+        if constexpr (NT > 1) __syncthreads(); else __syncwarp();
         if (warp < NT) {
-            const int r = row0 + warp * 8 + g, tq = quotient(r, a.R), hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
-            load_queries<G>(operand + warp * 32 + lane, a.io.q + b * a.io.qb + hq * a.io.qh + tq * a.io.qt, r < rows && !a.zero, a.sign, t);
+            const int at = NT > 1 ? *stage_at : use;
+            make_operand<G>(operand + warp * 32 + lane, queries + ((at * NT + warp) * G) * 32 + lane, a.sign, a.zero ? 0u : 0xFFFFFFFFu, t);
         }
         // o[n][i][j][e]: element i 32 + 4 g + 2 j + e / 2 of row n 8 + 2 t + e % 2; base, sum: rows n 8 + 2 t + e, in powers of two
         float o[NT][G][2][4], oc[NT][4], base[NT][2], sum[NT][2];
@@ -549,8 +604,9 @@ cache_attention_join_kernel(AttArgs a, int NR, int rows, int most) {
     const int h = quotient(seg, a.RT), r = (seg - h * (int)a.RT.d) * NR + rl;
     grid_dependency_wait();
     if (r >= (int)a.R.d * a.Tq) return;
-    const int first = a.before[b], blocks = a.before[b + 1] - first;
-    const int64_t total = (int64_t)a.before[a.B] * segs, from = (int64_t)first * segs + (int64_t)seg * blocks;
+    const int first = a.before[b], blocks = a.before[b + 1] - first, total = a.before[a.B] * segs, from = first * segs + seg * blocks;
+    const Shares share = shares_of(total, a.before[a.B + 1], a.B * segs, most);
+    if (share.whole) return;
     const int tq = quotient(r, a.R), hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
     __nv_bfloat16* const out = a.io.out + b * a.io.ob + hq * a.io.oh + tq * a.io.ot;
     float* const lse = a.lse ? a.lse + ((int64_t)b * a.Hq + hq) * a.Tq + tq : nullptr;
@@ -559,9 +615,7 @@ cache_attention_join_kernel(AttArgs a, int NR, int rows, int most) {
         if (lse && threadIdx.x == 0) *lse = MINUS_INF;
         return;
     }
-    const int ctas = sharers(total, most);
-    // CTA c has the blocks from total c / ctas on: the last one that starts at or before a block has it
-    const int c0 = (int)(((from + 1) * ctas - 1) / total), c1 = (int)(((from + blocks) * ctas - 1) / total);
+    const int c0 = holder_of(share, from), c1 = holder_of(share, from + blocks - 1);
     if (c0 == c1) return;                                  // one CTA had it all, and wrote the result
     const int n = c1 - c0 + 1;
     const size_t size = (size_t)NR * (D + 2);
@@ -637,11 +691,7 @@ Plan plan_of(int B, int H, int Ncap, int d, int Tq, int Hq, int sms) {
     const int slots = sms * ctas_per_sm(d, p.NT);
     const int64_t segs = (int64_t)B * H * p.RT, blocks = Ncap / kCacheBlock;
     p.ctas = 0;
-    if (segs < 4 * slots && blocks > 2 * kWarps) {
-        const int64_t most = segs * blocks / kWarps;       // no fewer than a block a warp
-        p.ctas = (int)(most < slots ? most : slots);
-        if (p.ctas <= segs) p.ctas = segs < slots ? 0 : slots;
-    }
+    if (segs < 4 * slots && blocks > kWholeBlocks && segs * blocks < 0x7fffffff) p.ctas = slots;
     return p;
 }
 
@@ -650,10 +700,10 @@ size_t part_bytes(const Plan& p, int d) { return align_up((size_t)2 * p.ctas * 8
 template <int D, int NT>
 int launch(AttArgs a, const Plan& p, cudaStream_t stream) {
     constexpr size_t kSmem = (size_t)kWarps * kStages * CacheBlock<D>::kBytes + kWarps * 2048 + 2 * kWarps * 8 * NT * 4 +
-                             NT * 32 * sizeof(QueryOperand<D / 32>) + kWarps * 2 * sizeof(Walk);
+                             NT * 32 * sizeof(QueryOperand<D / 32>) + kStages * NT * (D / 32) * 512 + kWarps * 2 * sizeof(Walk);
     static DoneOnDevice done[2];
     const bool shares = p.ctas > 0;
-    const size_t smem = kSmem + (shares ? align_up((size_t)(a.B + 1) * 4, 16) : 0);
+    const size_t smem = kSmem + 4 + (shares ? (size_t)(a.B + 2) * 4 : 0);
     const auto kern = shares ? cache_attention_kernel<D, NT, true> : cache_attention_kernel<D, NT, false>;
     int rc = allow_dynamic_smem(kern, kSmem + 16384, done[shares]);
     if (rc != VITCOP_OK) return rc;
@@ -685,7 +735,7 @@ int launch(AttArgs a, const Plan& p, cudaStream_t stream) {
 size_t cache_attention_workspace_bytes(int B, int H, int Ncap, int d, int Tq, int Hq) {
     if (B < 1 || H < 1 || Hq < 1 || Tq < 1) return kStatusBytes;
     const Plan p = plan_of(B, H, Ncap, d, Tq, Hq, sm_count());
-    return kStatusBytes + (p.ctas ? align_up((size_t)(B + 1) * 4, 256) + part_bytes(p, d) : 0);
+    return kStatusBytes + (p.ctas ? align_up((size_t)(B + 2) * 4, 256) + part_bytes(p, d) : 0);
 }
 
 int launch_cache_attention(const CacheQueries& io, const void* cache, int B, int Hq, int H, int Tq, int d, int Ncap,
@@ -699,7 +749,7 @@ int launch_cache_attention(const CacheQueries& io, const void* cache, int B, int
     a.lse = lse;
     a.status = static_cast<int*>(workspace);
     a.before = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + kStatusBytes);
-    a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kStatusBytes + align_up((size_t)(B + 1) * 4, 256));
+    a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kStatusBytes + align_up((size_t)(B + 2) * 4, 256));
     a.B = B; a.Hq = Hq; a.H = H; a.R = divisor(Hq / H); a.Tq = Tq; a.Ncap = Ncap; a.RT = divisor(p.RT); a.causal = causal ? 1 : 0;
     // (a scale of 0 is queries of 0)
     a.zero = scale == 0.f;
