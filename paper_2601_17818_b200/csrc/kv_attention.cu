@@ -47,7 +47,6 @@ struct AttArgs {
     const int32_t* cache_len;
     float* lse;
     int* status;
-    int32_t* before;                                       // shares: blocks in front of each sample, [B + 1], and of the longest
     float* part;                                           // shares: two pieces a CTA, each [8 NT][D + 2]
     int B, Hq, H, Tq, Ncap, causal;
     Divisor R, RT;                                         // query heads of a stored one, tiles of rows
@@ -153,7 +152,7 @@ struct Walk {
     int b, seg, tile, blocks, left;
 };
 __device__ __forceinline__ int blocks_of(const AttArgs& a, int b) {
-    const int len = a.cache_len ? max(0, min(__ldg(a.cache_len + b), a.Ncap)) : a.Ncap;
+    const int len = a.cache_len ? max(0, min(__ldcg(a.cache_len + b), a.Ncap)) : a.Ncap;
     return (len + kCacheBlock - 1) / kCacheBlock;
 }
 // How `total` blocks are shared out: the first `more` of `ctas` CTAs have `each` + 1 blocks, the others `each`; `whole`: a CTA has
@@ -226,8 +225,6 @@ cache_attention_kernel(AttArgs a) {
             }
         }
         __syncthreads();
-        if (blockIdx.x == 0)
-            for (int i = threadIdx.x; i <= a.B + 1; i += kWarps * 32) a.before[i] = before[i];
         const int total = before[a.B] * segs;
         const Shares share = shares_of(total, before[a.B + 1], a.B * segs, gridDim.x);
         if (share.whole) {
@@ -330,7 +327,7 @@ cache_attention_kernel(AttArgs a) {
         now = *at_work;
         const int b = now.b, h = quotient(now.seg, a.RT), row0 = (now.seg - h * (int)a.RT.d) * NR, rows = (int)a.R.d * a.Tq;
         const int count = piece(now);
-        const int len = a.cache_len ? max(0, min(__ldg(a.cache_len + b), a.Ncap)) : a.Ncap;
+        const int len = a.cache_len ? max(0, min(__ldcg(a.cache_len + b), a.Ncap)) : a.Ncap;
         // (they came with the first block of warp 0)
         if (warp == 0) {
             asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
@@ -590,82 +587,105 @@ cache_attention_kernel(AttArgs a) {
     } while (now.left > 0);
 }
 
-// The pieces of a head and tile of rows that several CTAs shared, in their order, one row a CTA.
-constexpr int kJoinThreads = 128;
+// The pieces of a head and tile of rows that several CTAs shared, in their order: a CTA takes 32 elements of a row at a time, 16 groups
+// of 8 threads every 16th piece.  How the blocks were shared out is found out while the kernel in front still runs.
+constexpr int kJoinThreads = 128, kJoinGroups = 16, kJoinAhead = 8;
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads)
-cache_attention_join_kernel(AttArgs a, int NR, int rows, int most) {
-    constexpr int kQuads = D / 4;                          // threads that share a row's elements; kBy of them by piece
-    constexpr int kBy = kJoinThreads / kQuads;
-    __shared__ float red[kBy][D];
-    __shared__ float weight[kJoinThreads];
-    const int segs = a.H * a.RT.d;
-    const int s = blockIdx.x / rows, rl = blockIdx.x - s * rows, b = s / segs, seg = s - b * segs;
-    const int h = quotient(seg, a.RT), r = (seg - h * (int)a.RT.d) * NR + rl;
-    grid_dependency_wait();
-    if (r >= (int)a.R.d * a.Tq) return;
-    const int first = a.before[b], blocks = a.before[b + 1] - first, total = a.before[a.B] * segs, from = first * segs + seg * blocks;
-    const Shares share = shares_of(total, a.before[a.B + 1], a.B * segs, most);
-    if (share.whole) return;
-    const int tq = quotient(r, a.R), hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
-    __nv_bfloat16* const out = a.io.out + b * a.io.ob + hq * a.io.oh + tq * a.io.ot;
-    float* const lse = a.lse ? a.lse + ((int64_t)b * a.Hq + hq) * a.Tq + tq : nullptr;
-    if (blocks == 0) {
-        for (int e = threadIdx.x; e < D; e += kJoinThreads) out[e] = __float2bfloat16_rn(0.f);
-        if (lse && threadIdx.x == 0) *lse = MINUS_INF;
-        return;
+cache_attention_join_kernel(AttArgs a, int NR, Divisor rows, int items, int most) {
+    __shared__ float weight[kJoinThreads], red[kJoinGroups][32], red_max[4], red_sum[4];
+    const int segs = a.H * (int)a.RT.d, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int all = 0, longest = 0;
+    for (int i = lane; i < a.B; i += 32) {
+        const int v = blocks_of(a, i);
+        all += v;
+        longest = max(longest, v);
     }
-    const int c0 = holder_of(share, from), c1 = holder_of(share, from + blocks - 1);
-    if (c0 == c1) return;                                  // one CTA had it all, and wrote the result
-    const int n = c1 - c0 + 1;
-    const size_t size = (size_t)NR * (D + 2);
-    const auto slot = [&](int c) { return a.part + (size_t)(2 * (c0 + c) + (c == 0 ? 1 : 0)) * size; };
-    float high = kNoLogit;
-    for (int c = threadIdx.x; c < n; c += kJoinThreads) high = fmaxf(high, slot(c)[NR * D + rl]);
+    const int total = __reduce_add_sync(0xffffffffu, all) * segs;
+    longest = __reduce_max_sync(0xffffffffu, longest);
+    const Shares share = shares_of(total, longest, a.B * segs, most);
+    if (share.whole) items = 0;
+    bool waited = false;
+    for (int item = blockIdx.x; item < items; item += gridDim.x) {
+        const int chunk = item % (D / 32), sr = item / (D / 32), s = quotient(sr, rows), rl = sr - s * (int)rows.d;
+        const int b = s / segs, seg = s - b * segs, h = quotient(seg, a.RT), r = (seg - h * (int)a.RT.d) * NR + rl;
+        if (r >= (int)a.R.d * a.Tq) continue;
+        int before = 0;
+        for (int i = lane; i < b; i += 32) before += blocks_of(a, i);
+        before = __reduce_add_sync(0xffffffffu, before);
+        const int blocks = blocks_of(a, b), from = before * segs + seg * blocks;
+        const int c0 = blocks > 0 ? holder_of(share, from) : 0, c1 = blocks > 0 ? holder_of(share, from + blocks - 1) : 0;
+        if (blocks > 0 && c0 == c1) continue;                  // one CTA had it all, and wrote the result
+        if (!waited) grid_dependency_wait();
+        waited = true;
+        const int tq = quotient(r, a.R), hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
+        __nv_bfloat16* const out = a.io.out + b * a.io.ob + hq * a.io.oh + tq * a.io.ot + chunk * 32;
+        float* const lse = a.lse && chunk == 0 ? a.lse + ((int64_t)b * a.Hq + hq) * a.Tq + tq : nullptr;
+        if (blocks == 0) {
+            if (tid < 32) out[tid] = __float2bfloat16_rn(0.f);
+            if (lse && tid == 0) *lse = MINUS_INF;
+            continue;
+        }
+        const size_t size = (size_t)NR * (D + 2);
+        const auto slot = [&](int c) { return a.part + (size_t)(2 * (c0 + c) + (c == 0 ? 1 : 0)) * size; };
+        const int n = c1 - c0 + 1, col = tid % 8, by = tid / 8;
+        float v[4] = {}, sum = 0.f, base = kNoLogit;
+        for (int first = 0; first < n; first += kJoinThreads) {
+            const int m = min(n - first, kJoinThreads);
+            float4 x[kJoinAhead];
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, off));
-    if ((threadIdx.x & 31) == 0) weight[threadIdx.x >> 5] = high;
-    __syncthreads();
-    high = fmaxf(fmaxf(weight[0], weight[1]), fmaxf(weight[2], weight[3]));
-    __syncthreads();
-    const int col = threadIdx.x % kQuads, by = threadIdx.x / kQuads;
-    float v[4] = {}, sum = 0.f;
-    for (int c0_ = 0; c0_ < n; c0_ += kJoinThreads) {
-        const int m = min(n - c0_, kJoinThreads);
-        if ((int)threadIdx.x < m) {
-            const float* const p = slot(c0_ + threadIdx.x) + NR * D + rl;
-            const float f = ex2_approx(p[0] - high);
-            weight[threadIdx.x] = f;
-            sum = fmaf(p[NR], f, sum);
+            for (int i = 0; i < kJoinAhead; ++i) {
+                const int c = by + i * kJoinGroups;
+                if (c < m) x[i] = *reinterpret_cast<const float4*>(slot(first + c) + rl * D + chunk * 32 + 4 * col);
+            }
+            float high = kNoLogit, part = 0.f;
+            if (tid < m) {
+                const float* const p = slot(first + tid) + NR * D + rl;
+                high = p[0];
+                part = p[NR];
+            }
+            const float mine = high;
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, off));
+            if (lane == 0) red_max[warp] = high;
+            __syncthreads();
+            const float top = fmaxf(fmaxf(fmaxf(red_max[0], red_max[1]), fmaxf(red_max[2], red_max[3])), base), keep = ex2_approx(base - top);
+            base = top;
+            const float f = tid < m ? ex2_approx(mine - top) : 0.f;
+            weight[tid] = f;
+            sum = fmaf(sum, keep, part * f);
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] *= keep;
+#pragma unroll
+            for (int i = 0; i < kJoinAhead; ++i) {
+                const int c = by + i * kJoinGroups;
+                if (c < m) {
+                    const float w = weight[c];
+                    v[0] = fmaf(x[i].x, w, v[0]);
+                    v[1] = fmaf(x[i].y, w, v[1]);
+                    v[2] = fmaf(x[i].z, w, v[2]);
+                    v[3] = fmaf(x[i].w, w, v[3]);
+                }
+            }
+        }
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+        if (lane == 0) red_sum[warp] = sum;
+        *reinterpret_cast<float4*>(&red[by][4 * col]) = make_float4(v[0], v[1], v[2], v[3]);
+        __syncthreads();
+        if (tid < 32) {
+            sum = (red_sum[0] + red_sum[1]) + (red_sum[2] + red_sum[3]);
+            const bool none = sum == 0.f;
+            float x = red[0][tid];
+#pragma unroll
+            for (int k = 1; k < kJoinGroups; ++k) x += red[k][tid];
+            out[tid] = __float2bfloat16_rn(none ? 0.f : x / sum);
+            if (lse && tid == 0) *lse = none ? MINUS_INF : (base + __log2f(sum)) * kLn2;
         }
         __syncthreads();
-#pragma unroll 8
-        for (int c = by; c < m; c += kBy) {
-            const float4 x = *reinterpret_cast<const float4*>(slot(c0_ + c) + rl * D + 4 * col);
-            const float f = weight[c];
-            v[0] = fmaf(x.x, f, v[0]);
-            v[1] = fmaf(x.y, f, v[1]);
-            v[2] = fmaf(x.z, f, v[2]);
-            v[3] = fmaf(x.w, f, v[3]);
-        }
-        __syncthreads();
     }
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-    if ((threadIdx.x & 31) == 0) weight[threadIdx.x >> 5] = sum;
-    *reinterpret_cast<float4*>(&red[by][4 * col]) = make_float4(v[0], v[1], v[2], v[3]);
-    __syncthreads();
-    sum = (weight[0] + weight[1]) + (weight[2] + weight[3]);
-    __syncthreads();
-    const bool none = sum == 0.f;
-    const float inv = none ? 0.f : 1.f / sum;
-    for (int e = threadIdx.x; e < D; e += kJoinThreads) {
-        float x = red[0][e];
-#pragma unroll
-        for (int k = 1; k < kBy; ++k) x += red[k][e];
-        out[e] = __float2bfloat16_rn(x * inv);
-    }
-    if (lse && threadIdx.x == 0) *lse = none ? MINUS_INF : (high + __log2f(sum)) * kLn2;
+    if (!waited) grid_dependency_wait();                   // (what comes behind takes this kernel's end for that of the one in front)
 }
 
 int sm_count() {
@@ -723,11 +743,13 @@ int launch(AttArgs a, const Plan& p, cudaStream_t stream) {
         if (rc != VITCOP_OK || !shares) return rc;
     }
     const int rows = (int)a.R.d * a.Tq < 8 * NT ? (int)a.R.d * a.Tq : 8 * NT;      // that a tile has at most
-    cfg.gridDim = dim3((unsigned)(a.B * a.H * (int)a.RT.d * rows));
+    const int64_t items = (int64_t)a.B * a.H * a.RT.d * rows * (D / 32);
+    const int wave = sm_count() * 8;
+    cfg.gridDim = dim3((unsigned)(items < wave ? items : wave));
     cfg.blockDim = dim3(kJoinThreads);
     cfg.dynamicSmemBytes = 0;
     KernelTimeScope timed("cache_attention_join_kernel", stream);
-    return record_cuda(cudaLaunchKernelEx(&cfg, cache_attention_join_kernel<D>, a, 8 * NT, rows, p.ctas));
+    return record_cuda(cudaLaunchKernelEx(&cfg, cache_attention_join_kernel<D>, a, 8 * NT, divisor(rows), (int)items, p.ctas));
 }
 
 }  // namespace
@@ -735,7 +757,7 @@ int launch(AttArgs a, const Plan& p, cudaStream_t stream) {
 size_t cache_attention_workspace_bytes(int B, int H, int Ncap, int d, int Tq, int Hq) {
     if (B < 1 || H < 1 || Hq < 1 || Tq < 1) return kStatusBytes;
     const Plan p = plan_of(B, H, Ncap, d, Tq, Hq, sm_count());
-    return kStatusBytes + (p.ctas ? align_up((size_t)(B + 2) * 4, 256) + part_bytes(p, d) : 0);
+    return kStatusBytes + part_bytes(p, d);
 }
 
 int launch_cache_attention(const CacheQueries& io, const void* cache, int B, int Hq, int H, int Tq, int d, int Ncap,
@@ -748,8 +770,7 @@ int launch_cache_attention(const CacheQueries& io, const void* cache, int B, int
     a.cache_len = cache_len;
     a.lse = lse;
     a.status = static_cast<int*>(workspace);
-    a.before = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + kStatusBytes);
-    a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kStatusBytes + align_up((size_t)(B + 2) * 4, 256));
+    a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kStatusBytes);
     a.B = B; a.Hq = Hq; a.H = H; a.R = divisor(Hq / H); a.Tq = Tq; a.Ncap = Ncap; a.RT = divisor(p.RT); a.causal = causal ? 1 : 0;
     // (a scale of 0 is queries of 0)
     a.zero = scale == 0.f;

@@ -70,20 +70,20 @@ __device__ __forceinline__ uint32_t codes_of(const uint4& x, const Group& g) {
 
 // Row r of the sample's new rows: its place in the source, or -1 behind the last.
 __device__ __forceinline__ int source_row(const CacheRows& rows, int b, int r, int N, int& count) {
-    const int L = rows.seq_len ? max(0, min(__ldg(rows.seq_len + b), N)) : N;
+    const int L = rows.seq_len ? max(0, min(__ldcg(rows.seq_len + b), N)) : N;
     if (!rows.keep_idx) {
         count = L;
         return r < L ? r : -1;
     }
-    int nv = rows.vis_len ? __ldg(rows.vis_len + b) : rows.vis_len_uniform;
+    int nv = rows.vis_len ? __ldcg(rows.vis_len + b) : rows.vis_len_uniform;
     nv = max(0, min(nv, L - rows.vis_start));
-    const int nk = max(0, min(min(__ldg(rows.n_keep + b), rows.keep_stride), nv));
+    const int nk = max(0, min(min(__ldcg(rows.n_keep + b), rows.keep_stride), nv));
     count = L - nv + nk;
     if (r >= count) return -1;
     if (r < rows.vis_start) return r;
     if (r >= rows.vis_start + nk) return r - nk + nv;
     // (a corrupt index can never leave the span)
-    return rows.vis_start + max(0, min(__ldg(rows.keep_idx + (int64_t)b * rows.keep_stride + (r - rows.vis_start)), nv - 1));
+    return rows.vis_start + max(0, min(__ldcg(rows.keep_idx + (int64_t)b * rows.keep_stride + (r - rows.vis_start)), nv - 1));
 }
 
 template <int D>
@@ -99,13 +99,13 @@ cache_write_kernel(CacheSource src, CacheRows rows, int H, int N, int R, int tot
     const int bh = on ? p / R : 0, r = on ? p - bh * R : 0, b = bh / H, h = bh - b * H;
     int count = 0;
     const int from = source_row(rows, b, r, N, count);
-    const int64_t start = cache_len ? max(0, __ldg(cache_len + b)) : 0;
+    const int64_t start = cache_len ? max(0, __ldcg(cache_len + b)) : 0;
     if (on && r == 0 && h == 0 && c == 0) new_len[b] = (int32_t)min(start + count, (int64_t)0x7fffffff);
     const int64_t to = start + r;
     const bool write = on && from >= 0 && to < Ncap;
     uint4 k = {}, v = {};
-    if (write && src.K) k = __ldg(reinterpret_cast<const uint4*>(src.K + b * src.kb + h * src.kh + from * src.kn) + c);
-    if (write && src.V) v = __ldg(reinterpret_cast<const uint4*>(src.V + b * src.vb + h * src.vh + from * src.vn) + c);
+    if (write && src.K) k = __ldcg(reinterpret_cast<const uint4*>(src.K + b * src.kb + h * src.kh + from * src.kn) + c);
+    if (write && src.V) v = __ldcg(reinterpret_cast<const uint4*>(src.V + b * src.vb + h * src.vh + from * src.vn) + c);
     const Group gk = group_of(k), gv = group_of(v);        // (all lanes of a warp take part)
     if (!write) return;
     uint8_t* const block = cache + ((int64_t)bh * (Ncap / kCacheBlock) + to / kCacheBlock) * L::kBytes;
@@ -140,7 +140,7 @@ __device__ __forceinline__ uint4 values_of(uint32_t codes, float s, float m) {
     return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
-__device__ __forceinline__ float ld_bf16(const uint8_t* p) { return __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(p)) << 16); }
+__device__ __forceinline__ float ld_bf16(const uint8_t* p) { return __uint_as_float((uint32_t)__ldcg(reinterpret_cast<const uint16_t*>(p)) << 16); }
 
 template <int D>
 __global__ void __launch_bounds__(kRowThreads)
@@ -153,18 +153,18 @@ cache_read_kernel(const uint8_t* cache, int H, int Ncap, const int32_t* cache_le
     const int c = threadIdx.x % T, grp = c / 4, t = c % 4;
     if (p >= total) return;
     const int bh = p / N_out, i = p - bh * N_out, b = bh / H;
-    const int64_t from = (int64_t)(row_begin ? max(0, __ldg(row_begin + b)) : row_begin_uniform) + i;
-    if (from >= (cache_len ? min(__ldg(cache_len + b), Ncap) : Ncap)) return;
+    const int64_t from = (int64_t)(row_begin ? max(0, __ldcg(row_begin + b)) : row_begin_uniform) + i;
+    if (from >= (cache_len ? min(__ldcg(cache_len + b), Ncap) : Ncap)) return;
     const uint8_t* const block = cache + ((int64_t)bh * (Ncap / kCacheBlock) + from / kCacheBlock) * L::kBytes;
     const int row = (int)(from % kCacheBlock);
     if (K_out) {
-        const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(block + L::kKCodes + row * (D / 2) + t * 4 * G + grp * 4));
+        const uint32_t w = __ldcg(reinterpret_cast<const uint32_t*>(block + L::kKCodes + row * (D / 2) + t * 4 * G + grp * 4));
         K_out[(int64_t)p * T + c] = values_of(w, ld_bf16(block + L::kKScale + (row * G + grp) * 2), ld_bf16(block + L::kKCentre + (row * G + grp) * 2));
     }
     if (V_out) {
         const uint8_t* const at = block + L::kVCodes + row * (D / 2) + grp * 2;
-        const uint32_t w = (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(at + (2 * t) * 2 * G)) |
-                           (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(at + (2 * t + 1) * 2 * G)) << 16;
+        const uint32_t w = (uint32_t)__ldcg(reinterpret_cast<const uint16_t*>(at + (2 * t) * 2 * G)) |
+                           (uint32_t)__ldcg(reinterpret_cast<const uint16_t*>(at + (2 * t + 1) * 2 * G)) << 16;
         V_out[(int64_t)p * T + c] = values_of(w, ld_bf16(block + L::kVScale + (row * G + grp) * 2), ld_bf16(block + L::kVCentre + (grp * 32 + row) * 2));
     }
 }
