@@ -70,6 +70,7 @@ class SelectParams(C.Structure):
 
 _lib: Optional[C.CDLL] = None
 _native = None                                   # the extension's function
+_module = None                                   # the extension
 _address: dict = {}                              # entry point -> its handle there
 # (a torch without CUDA has neither; the host-only entry points work there)
 _raw_stream, _device = (getattr(torch._C, name, None) for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
@@ -94,7 +95,7 @@ _select_params = _packer("@iii", SelectParams)
 
 def lib() -> C.CDLL:
     """Loads the shared library (once).  Fails loudly when it has not been built."""
-    global _lib, _native
+    global _lib, _native, _module
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise ImportError(f"{LIB_PATH} is missing: run `python -m paper_2601_17818_b200.build` first")
@@ -152,7 +153,7 @@ def lib() -> C.CDLL:
         loader.exec_module(module)
         for name in NATIVE:
             _address[name] = module.bind(name, C.cast(getattr(L, name), C.c_void_p).value)
-        _native = module.call
+        _native, _module = module.call, module
         _lib = L
     return _lib
 
@@ -335,87 +336,32 @@ def alloc_cache(B: int, H: int, Ncap: int, d: int, device="cuda") -> torch.Tenso
     return torch.empty((B, H, Ncap // 32, 40 * d), dtype=torch.uint8, device=device)
 
 
-def _rows(t, what: str, shape=None):
-    """Data pointer and strides of bf16 rows [B, H, N, d] on the current device, elements of a row side by side; dimensions of
-    extent 1 have no stride."""
-    if t is None:
-        return 0, 0, 0, 0
-    if not t.is_cuda or t.get_device() != _device():
-        raise ValueError(f"{what}: expected a tensor on the current CUDA device")
-    if t.dtype != torch.bfloat16 or t.dim() != 4 or (t.stride(3) != 1 and t.numel() > 0) or (shape is not None and tuple(t.shape) != shape):
-        raise ValueError(f"{what}: expected bf16 [B, H, N, d]{'' if shape is None else ' = ' + str(shape)}, elements of a row side by side")
-    (b, h, n, _), (sb, sh, sn, _) = t.shape, t.stride()
-    return t.data_ptr(), sb if b > 1 else 0, sh if h > 1 else 0, sn if n > 1 else 0
-
-
-def _dense(t, what: str, dtype, shape):
-    """Checks an optional dense tensor on the current device; a dimension of -1 may have any extent."""
-    if t is None:
-        return
-    if not t.is_cuda or t.get_device() != _device():
-        raise ValueError(f"{what}: expected a tensor on the current CUDA device")
-    if t.dtype != dtype or t.dim() != len(shape) or any(n not in (-1, m) for n, m in zip(shape, t.shape)) or not t.is_contiguous():
-        raise ValueError(f"{what}: expected contiguous {dtype} {list(shape)}")
-
-
-def _cache_dims(cache):
-    _dense(cache, "cache", torch.uint8, (-1, -1, -1, -1))
-    B, H, blocks, width = cache.shape
-    if width % 40:
-        raise ValueError("cache: expected uint8 [B, H, Ncap / 32, 40 d]")
-    return B, H, blocks * 32, width // 40
+def _cache_call(name: str, *args) -> None:
+    """The calls of the cache: their tensors are checked (ValueError) and taken apart in the extension."""
+    if _native is None:
+        lib()
+    device = _device()
+    rc = getattr(_module, name)(_raw_stream(device), device, *args)
+    if rc != OK:
+        raise VitcopError(rc, "vitcop_" + name)
 
 
 def vitcop_cache_write(K, V, cache, new_len, cache_len=None, seq_len=None, vis_start: int = 0, vis_len=0, keep_idx=None, n_keep=None):
     """Rows of K and V (bf16 [B,H,N,d], any leading strides) to ``cache`` in 4 bits, from row ``cache_len`` on: all of them, or with
     ``keep_idx`` those that ``vitcop_compact_kv`` keeps.  Returns ``new_len``, the rows that are in the cache then."""
-    B, H, Ncap, d = _cache_dims(cache)
-    ref = K if K is not None else V
-    if ref is None or ref.dim() != 4:
-        raise ValueError("K or V: expected bf16 [B, H, N, d]")
-    N = ref.shape[2]
-    k, kb, kh, kn = _rows(K, "K", (B, H, N, d))
-    v, vb_, vh, vn = _rows(V, "V", (B, H, N, d))
-    for t, what in ((new_len, "new_len"), (cache_len, "cache_len"), (seq_len, "seq_len"), (n_keep, "n_keep")):
-        _dense(t, what, torch.int32, (B,))
-    _dense(keep_idx, "keep_idx", torch.int32, (B, -1))
-    vp, vu = _vis(vis_len)
-    _dense(vp, "vis_len", torch.int32, (B,))
-    _call("vitcop_cache_write", k, v, B, H, N, d, kb, kh, kn, vb_, vh, vn, seq_len, int(vis_start), vp, vu, keep_idx,
-          0 if keep_idx is None else keep_idx.shape[1], n_keep, cache_len, cache, Ncap, new_len)
+    _cache_call("cache_write", K, V, cache, new_len, cache_len, seq_len, vis_start, vis_len, keep_idx, n_keep)
     return new_len
 
 
 def vitcop_cache_read(cache, cache_len, K_out=None, V_out=None, row_begin=0):
     """Rows of ``cache`` from ``row_begin`` (an int, or int32 [B]) on, up to ``cache_len`` (None: all), to bf16 [B,H,N_out,d]."""
-    B, H, Ncap, d = _cache_dims(cache)
-    ref = K_out if K_out is not None else V_out
-    if ref is None or ref.dim() != 4:
-        raise ValueError("K_out or V_out: expected bf16 [B, H, N_out, d]")
-    N_out = ref.shape[2]
-    for t, what in ((K_out, "K_out"), (V_out, "V_out")):
-        _dense(t, what, torch.bfloat16, (B, H, N_out, d))
-    _dense(cache_len, "cache_len", torch.int32, (B,))
-    bp, bu = _vis(row_begin)
-    _dense(bp, "row_begin", torch.int32, (B,))
-    _call("vitcop_cache_read", cache, B, H, Ncap, d, cache_len, bp, bu, K_out, V_out, N_out)
+    _cache_call("cache_read", cache, cache_len, K_out, V_out, row_begin)
     return K_out, V_out
 
 
 def vitcop_cache_attention(q, cache, cache_len, out, workspace, scale: float, causal: bool = True, lse=None):
     """softmax(scale q K^T) V over ``cache``: q, out bf16 [B,Hq,Tq,d] (any leading strides), the last Tq of ``cache_len`` tokens."""
-    B, H, Ncap, d = _cache_dims(cache)
-    if q.dim() != 4:
-        raise ValueError("q: expected bf16 [B, Hq, Tq, d]")
-    Hq, Tq = q.shape[1], q.shape[2]
-    shape = (B, Hq, Tq, d)
-    qp, qb, qh, qt = _rows(q, "q", shape)
-    op, ob, oh, ot = _rows(out, "out", shape)
-    _dense(cache_len, "cache_len", torch.int32, (B,))
-    _dense(lse, "lse", torch.float32, (B, Hq, Tq))
-    _dense(workspace, "workspace", torch.uint8, (-1,))
-    _call("vitcop_cache_attention", qp, cache, B, Hq, H, Tq, d, Ncap, qb, qh, qt, cache_len, int(causal), op, ob, oh, ot, lse, workspace,
-          workspace.numel(), scale=scale)
+    _cache_call("cache_attention", q, cache, cache_len, out, workspace, scale, causal, lse)
     return out
 
 

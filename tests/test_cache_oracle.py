@@ -152,6 +152,7 @@ def test_attention_refuses(L, what, status):
 
 def test_binding_refuses_what_is_not_on_the_device(L, monkeypatch):
     monkeypatch.setattr(vb, "_device", lambda: 0)
+    monkeypatch.setattr(vb, "_raw_stream", lambda device: 0)
     cache = torch.zeros(1, 1, 1, 40 * 64, dtype=torch.uint8)
     x, n = torch.zeros(1, 1, 4, 64, dtype=torch.bfloat16), torch.zeros(1, dtype=torch.int32)
     for call in (lambda: vb.vitcop_cache_write(x, x, cache, n), lambda: vb.vitcop_cache_read(cache, n, x),
