@@ -2,13 +2,17 @@
 //
 // A group of 32 elements (one token, one head) with smallest lo and largest hi is held as s = bf16((hi - lo) / 15),
 // m = bf16(lo + 8 s) and codes c = clamp(round((x - m) / s) + 8, 0, 15), which stand for m + (c - 8) s.  Both directions are
-// bound by memory (4 d bytes of bf16 and 1.25 d bytes of cache per row and head): d / 8 threads take a row, 16 bytes of K and of V each.
+// bound by memory (4 d bytes of bf16 and 1.25 d bytes of cache per row and head).  A warp takes a block of the cache: d / 8 lanes a
+// row, 16 bytes of K and of V each, and the block goes through shared memory, so that the cache sees 16-byte pieces in a row and not
+// the codes' two and four bytes, a scale's two.
+#include "async_copy.cuh"
+#include "f32x2.cuh"
 #include "kv_cache.cuh"
 
 namespace vitcop {
 namespace {
 
-constexpr int kRowThreads = 256;
+constexpr int kCacheWarps = 4;
 
 struct Group {
     float s, m, inv;                                       // bf16 values; inv about 1 / s, 0 where there is nothing to divide
@@ -16,26 +20,29 @@ struct Group {
 };
 
 __device__ __forceinline__ __nv_bfloat162 as_bf162(uint32_t u) { return *reinterpret_cast<__nv_bfloat162*>(&u); }
+__device__ __forceinline__ uint32_t as_u32(__nv_bfloat162 v) { return *reinterpret_cast<uint32_t*>(&v); }
 
 // Scale and centre of the group whose eight elements each of four neighbouring lanes holds.
 __device__ __forceinline__ Group group_of(const uint4& x) {
-    __nv_bfloat162 lo2 = __hmin2_nan(__hmin2_nan(as_bf162(x.x), as_bf162(x.y)), __hmin2_nan(as_bf162(x.z), as_bf162(x.w)));
-    __nv_bfloat162 hi2 = __hmax2_nan(__hmax2_nan(as_bf162(x.x), as_bf162(x.y)), __hmax2_nan(as_bf162(x.z), as_bf162(x.w)));
+    const __nv_bfloat162 lo2 = __hmin2_nan(__hmin2_nan(as_bf162(x.x), as_bf162(x.y)), __hmin2_nan(as_bf162(x.z), as_bf162(x.w)));
+    const __nv_bfloat162 hi2 = __hmax2_nan(__hmax2_nan(as_bf162(x.x), as_bf162(x.y)), __hmax2_nan(as_bf162(x.z), as_bf162(x.w)));
+    // smallest, and the largest with its sign turned: one minimum of both
+    uint32_t both = __byte_perm(as_u32(__hmin2_nan(lo2, as_bf162(__byte_perm(as_u32(lo2), 0u, 0x1032)))),
+                                as_u32(__hmax2_nan(hi2, as_bf162(__byte_perm(as_u32(hi2), 0u, 0x1032)))) ^ 0x80008000u, 0x5410);
 #pragma unroll
-    for (int off = 1; off <= 2; off <<= 1) {
-        lo2 = __hmin2_nan(lo2, __shfl_xor_sync(0xffffffffu, lo2, off));
-        hi2 = __hmax2_nan(hi2, __shfl_xor_sync(0xffffffffu, hi2, off));
-    }
-    const float lo = __bfloat162float(__hmin_nan(lo2.x, lo2.y)), hi = __bfloat162float(__hmax_nan(hi2.x, hi2.y));
+    for (int off = 1; off <= 2; off <<= 1) both = as_u32(__hmin2_nan(as_bf162(both), as_bf162(__shfl_xor_sync(0xffffffffu, both, off))));
+    const float lo = bf16lo(both), hi = -bf16hi(both);
     Group g;
     const float range = hi - lo;                           // NaN or infinite where an element is
     g.bad = !(range < __builtin_huge_valf());
-    // (exact up to the rounding to bf16: hi - lo of bf16 values needs more than 24 bits only where lo or hi is below the other's
-    // last place, and then the quotient is nowhere near the middle of two bf16)
-    g.s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(range, 15.f)));
+    // range / 15 with a product by the reciprocal and what is left of it (Markstein's way); exact up to the rounding to bf16: a quotient
+    // in the middle of two bf16 has a remainder of 0, and hi - lo needs more than 24 bits only where lo or hi is below the
+    // other's last place, far from any middle
+    const float fifteenth = 1.f / 15.f, q = range * fifteenth;
+    g.s = __bfloat162float(__float2bfloat16_rn(fmaf(fmaf(-15.f, q, range), fifteenth, q)));
     if (!(g.s >= 7.888609052210118e-31f)) g.s = 0.f;       // 2^-100: steps near the end of the exponents are none
     g.m = __bfloat162float(__float2bfloat16_rn(fmaf(8.f, g.s, lo)));
-    g.inv = g.s > 0.f ? __frcp_rn(g.s) : 0.f;
+    g.inv = g.s > 0.f ? __fdividef(1.f, g.s) : 0.f;
     if (g.bad) {
         g.s = __int_as_float(0x7fc00000);
         g.m = 0.f;
@@ -44,28 +51,32 @@ __device__ __forceinline__ Group group_of(const uint4& x) {
     return g;
 }
 
-// round((x - m) / s) + 8 in 0 .. 15, ties to even.  The product with the reciprocal is off by a few units in the last place; what is left
-// of x - m (exact: k s has 13 bits) says on which side of a border it really is.
-__device__ __forceinline__ uint32_t code_of(float x, const Group& g) {
-    const float p = x - g.m;
-    float k = rintf(p * g.inv);
-    const float left = fmaf(-k, g.s, p), half = 0.5f * g.s;
-    if (fabsf(left) >= half && g.s > 0.f) {
-        const bool odd = (static_cast<int>(k) & 1) != 0;
-        if (fabsf(left) > half || odd) k += left > 0.f ? 1.f : -1.f;
-    }
-    return static_cast<uint32_t>(static_cast<int>(fminf(fmaxf(k, -8.f), 7.f)) + 8);
-}
-
+// Codes of eight elements.  x - m is exact; its product with the reciprocal is off by a few units in the last place, and what that
+// leaves of x - m, exact too, brings the quotient to the nearest there is (Markstein's way): one that is a whole number and a half comes
+// out as that, and the sum with 1.5 * 2^23 rounds it to the even side.
 __device__ __forceinline__ uint32_t codes_of(const uint4& x, const Group& g) {
+    constexpr float kMagic = 12582912.f;                   // 1.5 * 2^23: a sum with it has the nearest whole number in its last bits
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    uint32_t c = 0;
+    const f32x2 m2 = pack2(-g.m, -g.m), inv2 = pack2(g.inv, g.inv), up = pack2(kMagic, kMagic), s2 = pack2(-g.s, -g.s);
+    float2 n[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        c |= code_of(bf16lo(w[i]), g) << (8 * i);
-        c |= code_of(bf16hi(w[i]), g) << (8 * i + 4);
+        const f32x2 p = add2(pack2(bf16lo(w[i]), bf16hi(w[i])), m2), q = mul2(p, inv2);
+        n[i] = unpack2(add2(fma2(fma2(q, s2, p), inv2, q), up));
     }
-    return g.bad ? 0x88888888u : c;
+    // (only a centre that was rounded by half a step can push the ends out of the codes' range: its last place is 2^-8 of it)
+    if (fabsf(g.m) >= 64.f * g.s) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n[i] = make_float2(fminf(fmaxf(n[i].x, kMagic - 8.f), kMagic + 7.f), fminf(fmaxf(n[i].y, kMagic - 8.f), kMagic + 7.f));
+    }
+    // the numbers carry the bits of 1.5 * 2^23, which add up to a constant; 8 more in each nibble makes the codes
+    constexpr uint32_t kBits = 0x4B400000u;
+    uint32_t codes = 0x88888888u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) codes -= kBits << (4 * i);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) codes += (__float_as_uint(n[i].x) << (8 * i)) + (__float_as_uint(n[i].y) << (8 * i + 4));
+    return g.s > 0.f ? codes : 0x88888888u;
 }
 
 // Row r of the sample's new rows: its place in the source, or -1 behind the last.
@@ -86,101 +97,167 @@ __device__ __forceinline__ int source_row(const CacheRows& rows, int b, int r, i
     return rows.vis_start + max(0, min(__ldcg(rows.keep_idx + (int64_t)b * rows.keep_stride + (r - rows.vis_start)), nv - 1));
 }
 
+// Of a row's bytes in a block (K or V, `half` 0 or 1): those of group grp, and of the eight elements t of it.
 template <int D>
-__global__ void __launch_bounds__(kRowThreads)
-cache_write_kernel(CacheSource src, CacheRows rows, int H, int N, int R, int total, const int32_t* cache_len, uint8_t* cache,
+__device__ __forceinline__ void put_codes(uint8_t* block, int half, int row, int grp, int t, const uint4& x) {
+    using L = CacheBlock<D>;
+    constexpr int G = L::G;
+    const Group g = group_of(x);
+    const uint32_t c = codes_of(x, g);
+    if (half == 0) {
+        *reinterpret_cast<uint32_t*>(block + L::kKCodes + row * (D / 2) + t * 4 * G + grp * 4) = c;
+        if (t < 2) *reinterpret_cast<__nv_bfloat16*>(block + (t ? L::kKCentre : L::kKScale) + (row * G + grp) * 2) = __float2bfloat16_rn(t ? g.m : g.s);
+    } else {
+        uint8_t* const at = block + L::kVCodes + row * (D / 2) + grp * 2 + 4 * t * G;
+        *reinterpret_cast<uint16_t*>(at) = (uint16_t)c;
+        *reinterpret_cast<uint16_t*>(at + 2 * G) = (uint16_t)(c >> 16);
+        if (t < 2)
+            *reinterpret_cast<__nv_bfloat16*>(block + (t ? L::kVCentre + (grp * 32 + row) * 2 : L::kVScale + (row * G + grp) * 2)) =
+                __float2bfloat16_rn(t ? g.m : g.s);
+    }
+}
+
+// Rows first .. last - 1 of a block, K if half is 0, from shared memory to the cache; the other rows' bytes are left alone.
+template <int D>
+__device__ __forceinline__ void flush(const uint8_t* from, uint8_t* to, int half, int first, int last, int lane) {
+    using L = CacheBlock<D>;
+    constexpr int G = L::G;
+    const int base = half ? L::kVCodes : L::kKCodes;
+    if (first == 0 && last == 32) {
+#pragma unroll
+        for (int i = lane; i < 20 * D / 16; i += 32) *reinterpret_cast<uint4*>(to + base + 16 * i) = *reinterpret_cast<const uint4*>(from + base + 16 * i);
+        return;
+    }
+    for (int i = first * (D / 32) + lane; i < last * (D / 32); i += 32)
+        *reinterpret_cast<uint4*>(to + base + 16 * i) = *reinterpret_cast<const uint4*>(from + base + 16 * i);
+    // planes: [32][G], and [G][32] for the centres of V
+    for (int i = first * G + lane; i < last * G; i += 32) {
+        const int scale = base + 16 * D + 2 * i, r = i / G, centre = base + 18 * D + 2 * (half ? (i - r * G) * 32 + r : i);
+        *reinterpret_cast<uint16_t*>(to + scale) = *reinterpret_cast<const uint16_t*>(from + scale);
+        *reinterpret_cast<uint16_t*>(to + centre) = *reinterpret_cast<const uint16_t*>(from + centre);
+    }
+}
+
+__device__ __forceinline__ uint4 ld_row(const __nv_bfloat16* p) {
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kCacheWarps * 32)
+cache_write_kernel(CacheSource src, CacheRows rows, int H, int N, int per_head, int items, const int32_t* cache_len, uint8_t* cache,
                    int Ncap, int32_t* new_len) {
     using L = CacheBlock<D>;
-    constexpr int G = L::G, T = D / 8;
+    constexpr int T = D / 8, U = 32 / T, kAhead = 4;       // lanes of a row, rows of the warp at a time, of which it loads four sets ahead
+    extern __shared__ __align__(128) uint8_t smem[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane % T, mine = lane / T;
+    uint8_t* const image = smem + warp * L::kBytes;
     grid_dependency_wait();
-    const int p = blockIdx.x * (kRowThreads / T) + threadIdx.x / T;
-    const int c = threadIdx.x % T, grp = c / 4, t = c % 4;
-    const bool on = p < total;
-    const int bh = on ? p / R : 0, r = on ? p - bh * R : 0, b = bh / H, h = bh - b * H;
+    const int item = blockIdx.x * kCacheWarps + warp;
+    if (item >= items) return;
+    const int bh = item / per_head, j = item - bh * per_head, b = bh / H, h = bh - b * H;
     int count = 0;
-    const int from = source_row(rows, b, r, N, count);
+    source_row(rows, b, 0, N, count);
     const int64_t start = cache_len ? max(0, __ldcg(cache_len + b)) : 0;
-    if (on && r == 0 && h == 0 && c == 0) new_len[b] = (int32_t)min(start + count, (int64_t)0x7fffffff);
-    const int64_t to = start + r;
-    const bool write = on && from >= 0 && to < Ncap;
-    uint4 k = {}, v = {};
-    if (write && src.K) k = __ldcg(reinterpret_cast<const uint4*>(src.K + b * src.kb + h * src.kh + from * src.kn) + c);
-    if (write && src.V) v = __ldcg(reinterpret_cast<const uint4*>(src.V + b * src.vb + h * src.vh + from * src.vn) + c);
-    const Group gk = group_of(k), gv = group_of(v);        // (all lanes of a warp take part)
-    if (!write) return;
-    uint8_t* const block = cache + ((int64_t)bh * (Ncap / kCacheBlock) + to / kCacheBlock) * L::kBytes;
-    const int row = (int)(to % kCacheBlock);
-    if (src.K) {
-        *reinterpret_cast<uint32_t*>(block + L::kKCodes + row * (D / 2) + t * 4 * G + grp * 4) = codes_of(k, gk);
-        if (t < 2)
-            *reinterpret_cast<__nv_bfloat16*>(block + (t ? L::kKCentre : L::kKScale) + (row * G + grp) * 2) =
-                __float2bfloat16_rn(t ? gk.m : gk.s);
-    }
-    if (src.V) {
-        const uint32_t w = codes_of(v, gv);
-        uint8_t* const at = block + L::kVCodes + row * (D / 2) + grp * 2;
-        *reinterpret_cast<uint16_t*>(at + (2 * t) * 2 * G) = (uint16_t)w;
-        *reinterpret_cast<uint16_t*>(at + (2 * t + 1) * 2 * G) = (uint16_t)(w >> 16);
-        if (t >= 2)
-            *reinterpret_cast<__nv_bfloat16*>(block + (t == 3 ? L::kVCentre + (grp * 32 + row) * 2 : L::kVScale + (row * G + grp) * 2)) =
-                __float2bfloat16_rn(t == 3 ? gv.m : gv.s);
-    }
-}
-
-// Eight values from eight codes.
-__device__ __forceinline__ uint4 values_of(uint32_t codes, float s, float m) {
-    uint32_t o[4];
+    if (j == 0 && h == 0 && lane == 0) new_len[b] = (int32_t)min(start + count, (int64_t)0x7fffffff);
+    const int64_t blk = start / kCacheBlock + j, end = min(start + count, (int64_t)Ncap);
+    if (blk * kCacheBlock >= end) return;
+    const int first = (int)max(start - blk * kCacheBlock, (int64_t)0), last = (int)min(end - blk * kCacheBlock, (int64_t)kCacheBlock);
+    // lane r: where row r of the block comes from
+    int from = -1, unused;
+    if (lane >= first && lane < last) from = source_row(rows, b, (int)(blk * kCacheBlock + lane - start), N, unused);
+    const __nv_bfloat16* const K = src.K ? src.K + b * src.kb + h * src.kh + c * 8 : nullptr;
+    const __nv_bfloat16* const V = src.V ? src.V + b * src.vb + h * src.vh + c * 8 : nullptr;
+    for (int r0 = first / U * U; r0 < last; r0 += kAhead * U) {
+        uint4 k[kAhead], v[kAhead];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float a = fmaf((float)(int)(codes >> (8 * i) & 15u) - 8.f, s, m);
-        const float b = fmaf((float)(int)(codes >> (8 * i + 4) & 15u) - 8.f, s, m);
-        const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-        o[i] = *reinterpret_cast<const uint32_t*>(&v);
+        for (int i = 0; i < kAhead; ++i) {
+            const int64_t row = __shfl_sync(0xffffffffu, from, (r0 + i * U + mine) & 31);
+            const bool there = r0 + i * U + mine < last && row >= 0;
+            k[i] = K && there ? ld_row(K + row * src.kn) : make_uint4(0, 0, 0, 0);
+            v[i] = V && there ? ld_row(V + row * src.vn) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (r0 + i * U >= last) break;                 // (uniform)
+            const int row = r0 + i * U + mine;             // (below 32: its bytes are written to shared memory, whoever owns them)
+            if (K) put_codes<D>(image, 0, row, c / 4, c % 4, k[i]);
+            if (V) put_codes<D>(image, 1, row, c / 4, c % 4, v[i]);
+        }
     }
-    return make_uint4(o[0], o[1], o[2], o[3]);
+    __syncwarp();
+    uint8_t* const block = cache + ((int64_t)bh * (Ncap / kCacheBlock) + blk) * L::kBytes;
+    if (K) flush<D>(image, block, 0, first, last, lane);
+    if (V) flush<D>(image, block, 1, first, last, lane);
 }
 
-__device__ __forceinline__ float ld_bf16(const uint8_t* p) { return __uint_as_float((uint32_t)__ldcg(reinterpret_cast<const uint16_t*>(p)) << 16); }
+// Eight values from eight codes: (128 + c) - 136 = c - 8 is exact in bf16, and so is the product inside the fused sum.
+__device__ __forceinline__ uint4 values_of(uint32_t codes, uint32_t s2, uint32_t m2) {
+    uint32_t x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {                          // elements i and i + 4
+        asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(x[i]) : "r"((codes >> (4 * i) & 0x000F000Fu) | 0x43004300u), "r"(0xC308C308u));
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(x[i]) : "r"(x[i]), "r"(s2), "r"(m2));
+    }
+    return make_uint4(__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[2], x[3], 0x5410), __byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632));
+}
+__device__ __forceinline__ uint32_t twice(const uint8_t* p) { return (uint32_t)*reinterpret_cast<const uint16_t*>(p) * 0x10001u; }
 
 template <int D>
-__global__ void __launch_bounds__(kRowThreads)
+__global__ void __launch_bounds__(kCacheWarps * 32)
 cache_read_kernel(const uint8_t* cache, int H, int Ncap, const int32_t* cache_len, const int32_t* row_begin, int row_begin_uniform,
-                  uint4* K_out, uint4* V_out, int N_out, int total) {
+                  uint4* K_out, uint4* V_out, int N_out, int per_head, int items) {
     using L = CacheBlock<D>;
-    constexpr int G = L::G, T = D / 8;
+    constexpr int G = L::G, T = D / 8, U = 32 / T;
+    extern __shared__ __align__(128) uint8_t smem[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane % T, mine = lane / T, grp = c / 4, t = c % 4;
+    uint8_t* const image = smem + warp * L::kBytes;
     grid_dependency_wait();
-    const int p = blockIdx.x * (kRowThreads / T) + threadIdx.x / T;
-    const int c = threadIdx.x % T, grp = c / 4, t = c % 4;
-    if (p >= total) return;
-    const int bh = p / N_out, i = p - bh * N_out, b = bh / H;
-    const int64_t from = (int64_t)(row_begin ? max(0, __ldcg(row_begin + b)) : row_begin_uniform) + i;
-    if (from >= (cache_len ? min(__ldcg(cache_len + b), Ncap) : Ncap)) return;
-    const uint8_t* const block = cache + ((int64_t)bh * (Ncap / kCacheBlock) + from / kCacheBlock) * L::kBytes;
-    const int row = (int)(from % kCacheBlock);
-    if (K_out) {
-        const uint32_t w = __ldcg(reinterpret_cast<const uint32_t*>(block + L::kKCodes + row * (D / 2) + t * 4 * G + grp * 4));
-        K_out[(int64_t)p * T + c] = values_of(w, ld_bf16(block + L::kKScale + (row * G + grp) * 2), ld_bf16(block + L::kKCentre + (row * G + grp) * 2));
-    }
-    if (V_out) {
-        const uint8_t* const at = block + L::kVCodes + row * (D / 2) + grp * 2;
-        const uint32_t w = (uint32_t)__ldcg(reinterpret_cast<const uint16_t*>(at + (2 * t) * 2 * G)) |
-                           (uint32_t)__ldcg(reinterpret_cast<const uint16_t*>(at + (2 * t + 1) * 2 * G)) << 16;
-        V_out[(int64_t)p * T + c] = values_of(w, ld_bf16(block + L::kVScale + (row * G + grp) * 2), ld_bf16(block + L::kVCentre + (grp * 32 + row) * 2));
+    const int item = blockIdx.x * kCacheWarps + warp;
+    if (item >= items) return;
+    const int bh = item / per_head, j = item - bh * per_head, b = bh / H;
+    const int64_t begin = row_begin ? max(0, __ldcg(row_begin + b)) : row_begin_uniform;
+    const int64_t end = min(begin + N_out, (int64_t)(cache_len ? min(__ldcg(cache_len + b), Ncap) : Ncap)), blk = begin / kCacheBlock + j;
+    if (blk * kCacheBlock >= end) return;
+    const int first = (int)max(begin - blk * kCacheBlock, (int64_t)0), last = (int)min(end - blk * kCacheBlock, (int64_t)kCacheBlock);
+    const uint8_t* const block = cache + ((int64_t)bh * (Ncap / kCacheBlock) + blk) * L::kBytes + (K_out ? 0 : L::kVCodes);
+    const uint32_t dst = smem_u32(image) + (K_out ? 0 : L::kVCodes);
+    const int pieces = (K_out && V_out ? 40 : 20) * D / 16;
+    for (int i = lane; i < pieces; i += 32)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + 16 * i), "l"(block + 16 * i) : "memory");
+    asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+    __syncwarp();
+    const int64_t out = ((int64_t)bh * N_out + (blk * kCacheBlock - begin)) * T + c;
+    for (int r0 = first / U * U; r0 < last; r0 += U) {
+        const int row = r0 + mine;
+        if (row < first || row >= last) continue;
+        if (K_out) {
+            const uint32_t w = *reinterpret_cast<const uint32_t*>(image + L::kKCodes + row * (D / 2) + t * 4 * G + grp * 4);
+            __stcs(K_out + out + row * T, values_of(w, twice(image + L::kKScale + (row * G + grp) * 2), twice(image + L::kKCentre + (row * G + grp) * 2)));
+        }
+        if (V_out) {
+            const uint8_t* const at = image + L::kVCodes + row * (D / 2) + grp * 2 + 4 * t * G;
+            const uint32_t w = (uint32_t)*reinterpret_cast<const uint16_t*>(at) | (uint32_t)*reinterpret_cast<const uint16_t*>(at + 2 * G) << 16;
+            __stcs(V_out + out + row * T, values_of(w, twice(image + L::kVScale + (row * G + grp) * 2), twice(image + L::kVCentre + (grp * 32 + row) * 2)));
+        }
     }
 }
 
-inline cudaLaunchConfig_t row_config(int total, int d, cudaLaunchAttribute* attr, cudaStream_t stream) {
+inline cudaLaunchConfig_t block_config(int items, int d, cudaLaunchAttribute* attr, cudaStream_t stream) {
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
-    const int per_cta = kRowThreads / (d / 8);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((total + per_cta - 1) / per_cta));
-    cfg.blockDim = dim3(kRowThreads);
+    cfg.gridDim = dim3((unsigned)((items + kCacheWarps - 1) / kCacheWarps));
+    cfg.blockDim = dim3(kCacheWarps * 32);
+    cfg.dynamicSmemBytes = (size_t)kCacheWarps * 40 * d;   // (40 KB at most)
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = pdl_allowed(true) ? 1 : 0;
     return cfg;
 }
+// Blocks that `rows` rows from anywhere on may lie in.
+inline int64_t blocks_for(int64_t rows) { return (rows + kCacheBlock - 2) / kCacheBlock + 1; }
 
 }  // namespace
 
@@ -194,28 +271,29 @@ int launch_cache_write(const CacheSource& src, const CacheRows& rows, int B, int
     R = R < Ncap ? R : Ncap;
     if (R < 1) R = 1;
     const int heads = H < 1 ? 1 : H;
-    if ((int64_t)B * heads * R > 0x7fffffff) return VITCOP_ERR_UNSUPPORTED;
-    const int total = (int)((int64_t)B * heads * R);
+    const int64_t per_head = blocks_for(R), items = (int64_t)B * heads * per_head;
+    if (items > 0x7fffffff) return VITCOP_ERR_UNSUPPORTED;
     CacheSource s = src;
     if (H < 1) s.K = s.V = nullptr;
     cudaLaunchAttribute attr[1];
-    const cudaLaunchConfig_t cfg = row_config(total, d, attr, stream);
+    const cudaLaunchConfig_t cfg = block_config((int)items, d, attr, stream);
     KernelTimeScope timed("cache_write_kernel", stream);
     auto kern = d == 64 ? cache_write_kernel<64> : d == 128 ? cache_write_kernel<128> : cache_write_kernel<256>;
-    return record_cuda(cudaLaunchKernelEx(&cfg, kern, s, rows, heads, N, (int)R, total, cache_len, static_cast<uint8_t*>(cache), Ncap, new_len));
+    return record_cuda(cudaLaunchKernelEx(&cfg, kern, s, rows, heads, N, (int)per_head, (int)items, cache_len, static_cast<uint8_t*>(cache),
+                                          Ncap, new_len));
 }
 
 int launch_cache_read(const void* cache, int B, int H, int Ncap, int d, const int32_t* cache_len, const int32_t* row_begin,
                       int row_begin_uniform, void* K_out, void* V_out, int N_out, cudaStream_t stream) {
-    if ((int64_t)B * H * N_out > 0x7fffffff) return VITCOP_ERR_UNSUPPORTED;
-    const int total = B * H * N_out;
-    if (total <= 0) return VITCOP_OK;
+    if (B <= 0 || H <= 0 || N_out <= 0) return VITCOP_OK;
+    const int64_t rows = N_out < Ncap ? N_out : Ncap, per_head = blocks_for(rows), items = (int64_t)B * H * per_head;
+    if (items > 0x7fffffff) return VITCOP_ERR_UNSUPPORTED;
     cudaLaunchAttribute attr[1];
-    const cudaLaunchConfig_t cfg = row_config(total, d, attr, stream);
+    const cudaLaunchConfig_t cfg = block_config((int)items, d, attr, stream);
     KernelTimeScope timed("cache_read_kernel", stream);
     auto kern = d == 64 ? cache_read_kernel<64> : d == 128 ? cache_read_kernel<128> : cache_read_kernel<256>;
     return record_cuda(cudaLaunchKernelEx(&cfg, kern, static_cast<const uint8_t*>(cache), H, Ncap, cache_len, row_begin, row_begin_uniform,
-                                          static_cast<uint4*>(K_out), static_cast<uint4*>(V_out), N_out, total));
+                                          static_cast<uint4*>(K_out), static_cast<uint4*>(V_out), N_out, (int)per_head, (int)items));
 }
 
 }  // namespace vitcop
