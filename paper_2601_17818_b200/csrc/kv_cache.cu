@@ -2,8 +2,7 @@
 //
 // A group of 32 elements (one token, one head) with smallest lo and largest hi is held as s = bf16((hi - lo) / 15),
 // m = bf16(lo + 8 s) and codes c = clamp(round((x - m) / s) + 8, 0, 15), which stand for m + (c - 8) s.  Both directions are
-// bound by memory (4 d bytes of bf16 and 1.25 d bytes of cache per row and head).  A warp takes a block of the cache: d / 8 lanes a
-// row, 16 bytes of K and of V each, and the block goes through shared memory, so that the cache sees 16-byte pieces in a row and not
+// bound by memory (4 d bytes of bf16 and 1.25 d bytes of cache per row and head).  A warp takes a block of the cache, which goes through shared memory, so that the cache sees 16-byte pieces in a row and not
 // the codes' two and four bytes, a scale's two.
 #include "async_copy.cuh"
 #include "f32x2.cuh"
@@ -15,38 +14,41 @@ namespace {
 constexpr int kCacheWarps = 4;
 
 struct Group {
-    float s, m, inv;                                       // bf16 values; inv about 1 / s, 0 where there is nothing to divide
-    bool bad;                                              // an element that is no finite number
+    float s, m;                                            // bf16 values
 };
 
 __device__ __forceinline__ __nv_bfloat162 as_bf162(uint32_t u) { return *reinterpret_cast<__nv_bfloat162*>(&u); }
 __device__ __forceinline__ uint32_t as_u32(__nv_bfloat162 v) { return *reinterpret_cast<uint32_t*>(&v); }
 
-// Scale and centre of the group whose eight elements each of four neighbouring lanes holds.
-__device__ __forceinline__ Group group_of(const uint4& x) {
-    const __nv_bfloat162 lo2 = __hmin2_nan(__hmin2_nan(as_bf162(x.x), as_bf162(x.y)), __hmin2_nan(as_bf162(x.z), as_bf162(x.w)));
-    const __nv_bfloat162 hi2 = __hmax2_nan(__hmax2_nan(as_bf162(x.x), as_bf162(x.y)), __hmax2_nan(as_bf162(x.z), as_bf162(x.w)));
-    // smallest, and the largest with its sign turned: one minimum of both
-    uint32_t both = __byte_perm(as_u32(__hmin2_nan(lo2, as_bf162(__byte_perm(as_u32(lo2), 0u, 0x1032)))),
-                                as_u32(__hmax2_nan(hi2, as_bf162(__byte_perm(as_u32(hi2), 0u, 0x1032)))) ^ 0x80008000u, 0x5410);
+// The nearest bf16 (ties to even), as fp32.
+__device__ __forceinline__ float rounded(float x) { return bf16lo(as_u32(__floats2bfloat162_rn(x, x))); }
+
+// Scale and centre of the group whose sixteen elements each of two neighbouring lanes holds.
+__device__ __forceinline__ Group group_of(const uint4 (&x)[2]) {
+    const uint32_t w[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
+    __nv_bfloat162 lo2 = as_bf162(w[0]), hi2 = lo2;
 #pragma unroll
-    for (int off = 1; off <= 2; off <<= 1) both = as_u32(__hmin2_nan(as_bf162(both), as_bf162(__shfl_xor_sync(0xffffffffu, both, off))));
+    for (int i = 1; i < 8; ++i) {
+        lo2 = __hmin2_nan(lo2, as_bf162(w[i]));
+        hi2 = __hmax2_nan(hi2, as_bf162(w[i]));
+    }
+    // smallest, and the largest with its sign turned: one minimum of both
+    uint32_t both = as_u32(__hmin2_nan(as_bf162(__byte_perm(as_u32(lo2), as_u32(hi2) ^ 0x80008000u, 0x5410)),
+                                       as_bf162(__byte_perm(as_u32(lo2), as_u32(hi2) ^ 0x80008000u, 0x7632))));
+    both = as_u32(__hmin2_nan(as_bf162(both), as_bf162(__shfl_xor_sync(0xffffffffu, both, 1))));
     const float lo = bf16lo(both), hi = -bf16hi(both);
     Group g;
     const float range = hi - lo;                           // NaN or infinite where an element is
-    g.bad = !(range < __builtin_huge_valf());
     // range / 15 with a product by the reciprocal and what is left of it (Markstein's way); exact up to the rounding to bf16: a quotient
     // in the middle of two bf16 has a remainder of 0, and hi - lo needs more than 24 bits only where lo or hi is below the
     // other's last place, far from any middle
     const float fifteenth = 1.f / 15.f, q = range * fifteenth;
-    g.s = __bfloat162float(__float2bfloat16_rn(fmaf(fmaf(-15.f, q, range), fifteenth, q)));
-    if (!(g.s >= 7.888609052210118e-31f)) g.s = 0.f;       // 2^-100: steps near the end of the exponents are none
-    g.m = __bfloat162float(__float2bfloat16_rn(fmaf(8.f, g.s, lo)));
-    g.inv = g.s > 0.f ? __fdividef(1.f, g.s) : 0.f;
-    if (g.bad) {
+    g.s = rounded(fmaf(fmaf(-15.f, q, range), fifteenth, q));
+    if (g.s < 7.888609052210118e-31f) g.s = 0.f;           // 2^-100: steps near the end of the exponents are none
+    g.m = rounded(fmaf(8.f, g.s, lo));
+    if (!(range < __builtin_huge_valf())) {
         g.s = __int_as_float(0x7fc00000);
         g.m = 0.f;
-        g.inv = 0.f;
     }
     return g;
 }
@@ -54,10 +56,10 @@ __device__ __forceinline__ Group group_of(const uint4& x) {
 // Codes of eight elements.  x - m is exact; its product with the reciprocal is off by a few units in the last place, and what that
 // leaves of x - m, exact too, brings the quotient to the nearest there is (Markstein's way): one that is a whole number and a half comes
 // out as that, and the sum with 1.5 * 2^23 rounds it to the even side.
-__device__ __forceinline__ uint32_t codes_of(const uint4& x, const Group& g) {
+__device__ __forceinline__ uint32_t codes_of(const uint4& x, const Group& g, float inv) {
     constexpr float kMagic = 12582912.f;                   // 1.5 * 2^23: a sum with it has the nearest whole number in its last bits
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    const f32x2 m2 = pack2(-g.m, -g.m), inv2 = pack2(g.inv, g.inv), up = pack2(kMagic, kMagic), s2 = pack2(-g.s, -g.s);
+    const f32x2 m2 = pack2(-g.m, -g.m), inv2 = pack2(inv, inv), up = pack2(kMagic, kMagic), s2 = pack2(-g.s, -g.s);
     float2 n[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -76,7 +78,7 @@ __device__ __forceinline__ uint32_t codes_of(const uint4& x, const Group& g) {
     for (int i = 0; i < 8; ++i) codes -= kBits << (4 * i);
 #pragma unroll
     for (int i = 0; i < 4; ++i) codes += (__float_as_uint(n[i].x) << (8 * i)) + (__float_as_uint(n[i].y) << (8 * i + 4));
-    return g.s > 0.f ? codes : 0x88888888u;
+    return g.s > 0.f ? codes : 0x88888888u;                // (no step, or an element that is no number)
 }
 
 // Row r of the sample's new rows: its place in the source, or -1 behind the last.
@@ -97,23 +99,27 @@ __device__ __forceinline__ int source_row(const CacheRows& rows, int b, int r, i
     return rows.vis_start + max(0, min(__ldcg(rows.keep_idx + (int64_t)b * rows.keep_stride + (r - rows.vis_start)), nv - 1));
 }
 
-// Of a row's bytes in a block (K or V, `half` 0 or 1): those of group grp, and of the eight elements t of it.
+// A row's bytes in a block (K or V, `half` 0 or 1): those of sixteen elements, `part` 0 or 1 of group grp.
 template <int D>
-__device__ __forceinline__ void put_codes(uint8_t* block, int half, int row, int grp, int t, const uint4& x) {
+__device__ __forceinline__ void put_codes(uint8_t* block, int half, int row, int grp, int part, const uint4 (&x)[2]) {
     using L = CacheBlock<D>;
     constexpr int G = L::G;
     const Group g = group_of(x);
-    const uint32_t c = codes_of(x, g);
+    const float inv = __fdividef(1.f, g.s);
+    const uint32_t c[2] = {codes_of(x[0], g, inv), codes_of(x[1], g, inv)};
+    const uint16_t plane = (uint16_t)(__float_as_uint(part ? g.m : g.s) >> 16);
     if (half == 0) {
-        *reinterpret_cast<uint32_t*>(block + L::kKCodes + row * (D / 2) + t * 4 * G + grp * 4) = c;
-        if (t < 2) *reinterpret_cast<__nv_bfloat16*>(block + (t ? L::kKCentre : L::kKScale) + (row * G + grp) * 2) = __float2bfloat16_rn(t ? g.m : g.s);
+        uint8_t* const at = block + L::kKCodes + row * (D / 2) + part * 8 * G + grp * 4;
+        *reinterpret_cast<uint32_t*>(at) = c[0];
+        *reinterpret_cast<uint32_t*>(at + 4 * G) = c[1];
+        *reinterpret_cast<uint16_t*>(block + (part ? L::kKCentre : L::kKScale) + (row * G + grp) * 2) = plane;
     } else {
-        uint8_t* const at = block + L::kVCodes + row * (D / 2) + grp * 2 + 4 * t * G;
-        *reinterpret_cast<uint16_t*>(at) = (uint16_t)c;
-        *reinterpret_cast<uint16_t*>(at + 2 * G) = (uint16_t)(c >> 16);
-        if (t < 2)
-            *reinterpret_cast<__nv_bfloat16*>(block + (t ? L::kVCentre + (grp * 32 + row) * 2 : L::kVScale + (row * G + grp) * 2)) =
-                __float2bfloat16_rn(t ? g.m : g.s);
+        uint8_t* const at = block + L::kVCodes + row * (D / 2) + part * 8 * G + grp * 2;
+        *reinterpret_cast<uint16_t*>(at) = (uint16_t)c[0];
+        *reinterpret_cast<uint16_t*>(at + 2 * G) = (uint16_t)(c[0] >> 16);
+        *reinterpret_cast<uint16_t*>(at + 4 * G) = (uint16_t)c[1];
+        *reinterpret_cast<uint16_t*>(at + 6 * G) = (uint16_t)(c[1] >> 16);
+        *reinterpret_cast<uint16_t*>(block + (part ? L::kVCentre + (grp * 32 + row) * 2 : L::kVScale + (row * G + grp) * 2)) = plane;
     }
 }
 
@@ -145,11 +151,11 @@ __device__ __forceinline__ uint4 ld_row(const __nv_bfloat16* p) {
 }
 
 template <int D>
-__global__ void __launch_bounds__(kCacheWarps * 32)
+__global__ void __launch_bounds__(kCacheWarps * 32, 8)
 cache_write_kernel(CacheSource src, CacheRows rows, int H, int N, int per_head, int items, const int32_t* cache_len, uint8_t* cache,
                    int Ncap, int32_t* new_len) {
     using L = CacheBlock<D>;
-    constexpr int T = D / 8, U = 32 / T, kAhead = 4;       // lanes of a row, rows of the warp at a time, of which it loads four sets ahead
+    constexpr int T = D / 16, U = 32 / T, kAhead = 2;      // lanes of a row, rows of the warp at a time, of which it loads two sets ahead
     extern __shared__ __align__(128) uint8_t smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane % T, mine = lane / T;
     uint8_t* const image = smem + warp * L::kBytes;
@@ -167,23 +173,26 @@ cache_write_kernel(CacheSource src, CacheRows rows, int H, int N, int per_head, 
     // lane r: where row r of the block comes from
     int from = -1, unused;
     if (lane >= first && lane < last) from = source_row(rows, b, (int)(blk * kCacheBlock + lane - start), N, unused);
-    const __nv_bfloat16* const K = src.K ? src.K + b * src.kb + h * src.kh + c * 8 : nullptr;
-    const __nv_bfloat16* const V = src.V ? src.V + b * src.vb + h * src.vh + c * 8 : nullptr;
+    const __nv_bfloat16* const K = src.K ? src.K + b * src.kb + h * src.kh + c * 16 : nullptr;
+    const __nv_bfloat16* const V = src.V ? src.V + b * src.vb + h * src.vh + c * 16 : nullptr;
     for (int r0 = first / U * U; r0 < last; r0 += kAhead * U) {
-        uint4 k[kAhead], v[kAhead];
+        uint4 k[kAhead][2], v[kAhead][2];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             const int64_t row = __shfl_sync(0xffffffffu, from, (r0 + i * U + mine) & 31);
             const bool there = r0 + i * U + mine < last && row >= 0;
-            k[i] = K && there ? ld_row(K + row * src.kn) : make_uint4(0, 0, 0, 0);
-            v[i] = V && there ? ld_row(V + row * src.vn) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                k[i][e] = K && there ? ld_row(K + row * src.kn + 8 * e) : make_uint4(0, 0, 0, 0);
+                v[i][e] = V && there ? ld_row(V + row * src.vn + 8 * e) : make_uint4(0, 0, 0, 0);
+            }
         }
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             if (r0 + i * U >= last) break;                 // (uniform)
             const int row = r0 + i * U + mine;             // (below 32: its bytes are written to shared memory, whoever owns them)
-            if (K) put_codes<D>(image, 0, row, c / 4, c % 4, k[i]);
-            if (V) put_codes<D>(image, 1, row, c / 4, c % 4, v[i]);
+            if (K) put_codes<D>(image, 0, row, c / 2, c % 2, k[i]);
+            if (V) put_codes<D>(image, 1, row, c / 2, c % 2, v[i]);
         }
     }
     __syncwarp();
