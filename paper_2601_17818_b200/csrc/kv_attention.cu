@@ -27,7 +27,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNoLogit = -3.4e38f;                       // below every logit that is a number: nothing seen yet
 
 // Resident CTAs an SM, which the registers of the accumulators and the ring's memory leave room for.
-constexpr int ctas_per_sm(int D, int NT) { return D == 256 || NT == 4 ? 2 : D * NT <= 128 ? 4 : 3; }
+constexpr int ctas_per_sm(int D, int NT) { return D == 256 || D * NT > 256 || NT == 4 ? 2 : D * NT <= 128 ? 4 : 3; }
 
 // n / d for 0 <= n < 2^31 by a multiplication: with l = ceil(log2 d), mul = floor(2^(31 + l) / d) + 1 is off by less than 2^l / d parts of
 // 2^(31 + l), which n < 2^31 of them do not add up to a quotient.
@@ -587,14 +587,13 @@ cache_attention_kernel(AttArgs a) {
     } while (now.left > 0);
 }
 
-// The pieces of a head and tile of rows that several CTAs shared, in their order: a CTA takes 32 elements of a row at a time, 16 groups
-// of 8 threads every 16th piece.  How the blocks were shared out is found out while the kernel in front still runs.
-constexpr int kJoinThreads = 128, kJoinGroups = 16, kJoinAhead = 8;
+// The pieces of a head and tile of rows that several CTAs shared, in their order: a warp takes 32 elements of a row at a time, four groups
+// of eight lanes every fourth piece.  How the blocks were shared out is found out while the kernel in front still runs.
+constexpr int kJoinWarps = 4, kJoinAhead = 8;
 template <int D>
-__global__ void __launch_bounds__(kJoinThreads)
+__global__ void __launch_bounds__(kJoinWarps * 32)
 cache_attention_join_kernel(AttArgs a, int NR, Divisor rows, int items, int most) {
-    __shared__ float weight[kJoinThreads], red[kJoinGroups][32], red_max[4], red_sum[4];
-    const int segs = a.H * (int)a.RT.d, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int segs = a.H * (int)a.RT.d, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = lane % 8, by = lane / 8;
     int all = 0, longest = 0;
     for (int i = lane; i < a.B; i += 32) {
         const int v = blocks_of(a, i);
@@ -606,7 +605,7 @@ cache_attention_join_kernel(AttArgs a, int NR, Divisor rows, int items, int most
     const Shares share = shares_of(total, longest, a.B * segs, most);
     if (share.whole) items = 0;
     bool waited = false;
-    for (int item = blockIdx.x; item < items; item += gridDim.x) {
+    for (int item = blockIdx.x * kJoinWarps + warp; item < items; item += gridDim.x * kJoinWarps) {
         const int chunk = item % (D / 32), sr = item / (D / 32), s = quotient(sr, rows), rl = sr - s * (int)rows.d;
         const int b = s / segs, seg = s - b * segs, h = quotient(seg, a.RT), r = (seg - h * (int)a.RT.d) * NR + rl;
         if (r >= (int)a.R.d * a.Tq) continue;
@@ -614,54 +613,37 @@ cache_attention_join_kernel(AttArgs a, int NR, Divisor rows, int items, int most
         for (int i = lane; i < b; i += 32) before += blocks_of(a, i);
         before = __reduce_add_sync(0xffffffffu, before);
         const int blocks = blocks_of(a, b), from = before * segs + seg * blocks;
-        const int c0 = blocks > 0 ? holder_of(share, from) : 0, c1 = blocks > 0 ? holder_of(share, from + blocks - 1) : 0;
-        if (blocks > 0 && c0 == c1) continue;                  // one CTA had it all, and wrote the result
+        const int c0 = blocks > 0 ? holder_of(share, from) : 0, n = blocks > 0 ? holder_of(share, from + blocks - 1) - c0 + 1 : 0;
+        if (n == 1) continue;                              // one CTA had it all, and wrote the result
         if (!waited) grid_dependency_wait();
         waited = true;
-        const int tq = quotient(r, a.R), hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
-        __nv_bfloat16* const out = a.io.out + b * a.io.ob + hq * a.io.oh + tq * a.io.ot + chunk * 32;
-        float* const lse = a.lse && chunk == 0 ? a.lse + ((int64_t)b * a.Hq + hq) * a.Tq + tq : nullptr;
-        if (blocks == 0) {
-            if (tid < 32) out[tid] = __float2bfloat16_rn(0.f);
-            if (lse && tid == 0) *lse = MINUS_INF;
-            continue;
-        }
         const size_t size = (size_t)NR * (D + 2);
         const auto slot = [&](int c) { return a.part + (size_t)(2 * (c0 + c) + (c == 0 ? 1 : 0)) * size; };
-        const int n = c1 - c0 + 1, col = tid % 8, by = tid / 8;
         float v[4] = {}, sum = 0.f, base = kNoLogit;
-        for (int first = 0; first < n; first += kJoinThreads) {
-            const int m = min(n - first, kJoinThreads);
+        for (int first = 0; first < n; first += 32) {
+            const int m = min(n - first, 32);
             float4 x[kJoinAhead];
 #pragma unroll
-            for (int i = 0; i < kJoinAhead; ++i) {
-                const int c = by + i * kJoinGroups;
-                if (c < m) x[i] = *reinterpret_cast<const float4*>(slot(first + c) + rl * D + chunk * 32 + 4 * col);
-            }
-            float high = kNoLogit, part = 0.f;
-            if (tid < m) {
-                const float* const p = slot(first + tid) + NR * D + rl;
-                high = p[0];
+            for (int i = 0; i < kJoinAhead; ++i)
+                if (by + 4 * i < m) x[i] = *reinterpret_cast<const float4*>(slot(first + by + 4 * i) + rl * D + chunk * 32 + 4 * col);
+            float mine = kNoLogit, part = 0.f;
+            if (lane < m) {
+                const float* const p = slot(first + lane) + NR * D + rl;
+                mine = p[0];
                 part = p[NR];
             }
-            const float mine = high;
+            float top = fmaxf(mine, base);
 #pragma unroll
-            for (int off = 16; off > 0; off >>= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, off));
-            if (lane == 0) red_max[warp] = high;
-            __syncthreads();
-            const float top = fmaxf(fmaxf(fmaxf(red_max[0], red_max[1]), fmaxf(red_max[2], red_max[3])), base), keep = ex2_approx(base - top);
+            for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+            const float keep = ex2_approx(base - top), f = lane < m ? ex2_approx(mine - top) : 0.f;
             base = top;
-            const float f = tid < m ? ex2_approx(mine - top) : 0.f;
-            weight[tid] = f;
             sum = fmaf(sum, keep, part * f);
-            __syncthreads();
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] *= keep;
 #pragma unroll
             for (int i = 0; i < kJoinAhead; ++i) {
-                const int c = by + i * kJoinGroups;
-                if (c < m) {
-                    const float w = weight[c];
+                const float w = __shfl_sync(0xffffffffu, f, by + 4 * i);
+                if (by + 4 * i < m) {
                     v[0] = fmaf(x[i].x, w, v[0]);
                     v[1] = fmaf(x[i].y, w, v[1]);
                     v[2] = fmaf(x[i].z, w, v[2]);
@@ -671,19 +653,18 @@ cache_attention_join_kernel(AttArgs a, int NR, Divisor rows, int items, int most
         }
 #pragma unroll
         for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-        if (lane == 0) red_sum[warp] = sum;
-        *reinterpret_cast<float4*>(&red[by][4 * col]) = make_float4(v[0], v[1], v[2], v[3]);
-        __syncthreads();
-        if (tid < 32) {
-            sum = (red_sum[0] + red_sum[1]) + (red_sum[2] + red_sum[3]);
-            const bool none = sum == 0.f;
-            float x = red[0][tid];
 #pragma unroll
-            for (int k = 1; k < kJoinGroups; ++k) x += red[k][tid];
-            out[tid] = __float2bfloat16_rn(none ? 0.f : x / sum);
-            if (lse && tid == 0) *lse = none ? MINUS_INF : (base + __log2f(sum)) * kLn2;
+        for (int e = 0; e < 4; ++e) {
+            v[e] += __shfl_xor_sync(0xffffffffu, v[e], 8);
+            v[e] += __shfl_xor_sync(0xffffffffu, v[e], 16);
         }
-        __syncthreads();
+        const int tq = quotient(r, a.R), hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
+        const bool none = sum == 0.f;                      // (no row seen, an empty sample's among them)
+        const float inv = none ? 0.f : 1.f / sum;
+        if (by == 0)
+            *reinterpret_cast<uint2*>(a.io.out + b * a.io.ob + hq * a.io.oh + tq * a.io.ot + chunk * 32 + 4 * col) =
+                make_uint2(bf16x2(v[0] * inv, v[1] * inv), bf16x2(v[2] * inv, v[3] * inv));
+        if (a.lse && chunk == 0 && lane == 0) a.lse[((int64_t)b * a.Hq + hq) * a.Tq + tq] = none ? MINUS_INF : (base + __log2f(sum)) * kLn2;
     }
     if (!waited) grid_dependency_wait();                   // (what comes behind takes this kernel's end for that of the one in front)
 }
@@ -706,7 +687,7 @@ struct Plan {
 Plan plan_of(int B, int H, int Ncap, int d, int Tq, int Hq, int sms) {
     Plan p;
     const int64_t rows = (int64_t)(Hq / H) * Tq;
-    p.NT = rows <= 8 ? 1 : rows <= 16 || d == 256 ? 2 : 4;
+    p.NT = rows <= 8 ? 1 : rows <= 16 || d == 256 ? 2 : rows <= 24 ? 3 : 4;
     p.RT = (int)((rows + 8 * p.NT - 1) / (8 * p.NT));
     const int slots = sms * ctas_per_sm(d, p.NT);
     const int64_t segs = (int64_t)B * H * p.RT, blocks = Ncap / kCacheBlock;
@@ -744,9 +725,9 @@ int launch(AttArgs a, const Plan& p, cudaStream_t stream) {
     }
     const int rows = (int)a.R.d * a.Tq < 8 * NT ? (int)a.R.d * a.Tq : 8 * NT;      // that a tile has at most
     const int64_t items = (int64_t)a.B * a.H * a.RT.d * rows * (D / 32);
-    const int wave = sm_count() * 8;
-    cfg.gridDim = dim3((unsigned)(items < wave ? items : wave));
-    cfg.blockDim = dim3(kJoinThreads);
+    const int64_t wave = sm_count() * 8, ctas = (items + kJoinWarps - 1) / kJoinWarps;
+    cfg.gridDim = dim3((unsigned)(ctas < wave ? ctas : wave));
+    cfg.blockDim = dim3(kJoinWarps * 32);
     cfg.dynamicSmemBytes = 0;
     KernelTimeScope timed("cache_attention_join_kernel", stream);
     return record_cuda(cudaLaunchKernelEx(&cfg, cache_attention_join_kernel<D>, a, 8 * NT, divisor(rows), (int)items, p.ctas));
@@ -776,8 +757,8 @@ int launch_cache_attention(const CacheQueries& io, const void* cache, int B, int
     a.zero = scale == 0.f;
     a.sign = scale < 0.f ? 0x80008000u : 0u;
     a.scale_log2 = a.zero ? 1.f : (scale < 0.f ? -scale : scale) * kLog2e;
-    if (d == 64) return p.NT == 1 ? launch<64, 1>(a, p, stream) : p.NT == 2 ? launch<64, 2>(a, p, stream) : launch<64, 4>(a, p, stream);
-    if (d == 128) return p.NT == 1 ? launch<128, 1>(a, p, stream) : p.NT == 2 ? launch<128, 2>(a, p, stream) : launch<128, 4>(a, p, stream);
+    if (d == 64) return p.NT == 1 ? launch<64, 1>(a, p, stream) : p.NT == 2 ? launch<64, 2>(a, p, stream) : p.NT == 3 ? launch<64, 3>(a, p, stream) : launch<64, 4>(a, p, stream);
+    if (d == 128) return p.NT == 1 ? launch<128, 1>(a, p, stream) : p.NT == 2 ? launch<128, 2>(a, p, stream) : p.NT == 3 ? launch<128, 3>(a, p, stream) : launch<128, 4>(a, p, stream);
     return p.NT == 1 ? launch<256, 1>(a, p, stream) : launch<256, 2>(a, p, stream);
 }
 
