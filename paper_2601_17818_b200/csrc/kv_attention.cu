@@ -163,7 +163,9 @@ struct Shares {
 };
 __device__ __forceinline__ Shares shares_of(int total, int longest, int segs, int most) {
     Shares s;
-    s.ctas = max(1, min(most, total / kWarps));            // a block for every warp of a CTA, or there is one CTA
+    // as few as take no more rounds of a block a warp than all of them would: fewer pieces, and every warp has work in the last round
+    const int rounds = max(1, (total + most * kWarps - 1) / (most * kWarps));
+    s.ctas = rounds > 2 ? most : max(1, (total + rounds * kWarps - 1) / (rounds * kWarps));
     s.each = total / s.ctas;
     s.more = total - s.each * s.ctas;
     // where the longest segment takes hardly longer than a fair share, pieces to join and heads to begin anew cost more
@@ -692,7 +694,7 @@ Plan plan_of(int B, int H, int Ncap, int d, int Tq, int Hq, int sms) {
     const int slots = sms * ctas_per_sm(d, p.NT);
     const int64_t segs = (int64_t)B * H * p.RT, blocks = Ncap / kCacheBlock;
     p.ctas = 0;
-    if (segs < 4 * slots && blocks > kWholeBlocks && segs * blocks < 0x7fffffff) p.ctas = slots;
+    if (segs < 4 * slots && blocks > kWholeBlocks && segs * blocks < 0x7fff0000) p.ctas = slots;
     return p;
 }
 
