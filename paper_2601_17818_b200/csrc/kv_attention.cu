@@ -8,13 +8,10 @@
 //            centres and as bf16(bf16(p) s) with a group's codes
 // A warp takes every fourth block of 32 tokens of its CTA's piece, with blocks ahead in shared memory (cp.async), and keeps maximum, sum
 // and output of its own; the CTA joins its warps, a second kernel joins the CTAs that shared a head.
-#include <cuda_bf16.h>
-
 #include <type_traits>
 
 #include "async_copy.cuh"
-#include "f32x2.cuh"
-#include "kv_cache.cuh"
+#include "kv_attention.cuh"
 
 namespace vitcop {
 namespace {
@@ -22,38 +19,10 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kStages = 2;
 constexpr int kWholeBlocks = 24;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-#define MINUS_INF (-__builtin_huge_valf())
-constexpr float kNoLogit = -3.4e38f;                       // below every logit that is a number: nothing seen yet
 
 // Resident CTAs an SM, which the registers of the accumulators and the ring's memory leave room for.
 constexpr int ctas_per_sm(int D, int NT) { return D == 256 || D * NT > 256 || NT == 4 ? 2 : D * NT <= 128 ? 4 : 3; }
 
-// n / d for 0 <= n < 2^31 by a multiplication: with l = ceil(log2 d), mul = floor(2^(31 + l) / d) + 1 is off by less than 2^l / d parts of
-// 2^(31 + l), which n < 2^31 of them do not add up to a quotient.
-struct Divisor {
-    uint32_t d, mul, shift;
-};
-Divisor divisor(int d) {
-    int l = 0;
-    while ((1ll << l) < d) ++l;
-    return {(uint32_t)d, d == 1 ? 0u : (uint32_t)((1ull << (31 + l)) / (uint32_t)d + 1), (uint32_t)(l > 0 ? l - 1 : 0)};
-}
-__device__ __forceinline__ int quotient(int n, const Divisor& by) { return by.d == 1 ? n : (int)(__umulhi((uint32_t)n, by.mul) >> by.shift); }
-
-struct AttArgs {
-    CacheQueries io;
-    const uint8_t* cache;
-    const int32_t* cache_len;
-    float* lse;
-    int* status;
-    float* part;                                           // shares: two pieces a CTA, each [8 NT][D + 2]
-    int B, Hq, H, Tq, Ncap, causal;
-    Divisor R, RT;                                         // query heads of a stored one, tiles of rows
-    float scale_log2;                                      // above 0: the sign is the queries'
-    uint32_t sign;                                         // 0x80008000 turns it; scale 0: `zero`
-    bool zero;
-};
 
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -71,20 +40,6 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {   // an 8 x 8 matri
     uint32_t y;
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
-}
-__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ uint32_t code_pair(uint32_t w) {    // 128 + c, twice
-    uint32_t r;
-    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(0x000F000Fu), "r"(0x43004300u));
-    return r;
-}
-__device__ __forceinline__ uint32_t centred(uint32_t pair) {                                              // c - 8, twice
-    uint32_t r;
-    asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(pair), "r"(0xC308C308u));
-    return r;
 }
 __device__ __forceinline__ uint32_t times(uint32_t a, uint32_t b) {
     uint32_t r;
@@ -671,17 +626,6 @@ cache_attention_join_kernel(AttArgs a, int NR, Divisor rows, int items, int most
     if (!waited) grid_dependency_wait();                   // (what comes behind takes this kernel's end for that of the one in front)
 }
 
-int sm_count() {
-    static std::atomic<int> known[kMaxDevices];
-    std::atomic<int>& k = known[current_device()];
-    int v = k.load(std::memory_order_relaxed);
-    if (v == 0) {
-        if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, current_device()) != cudaSuccess || v <= 0) v = 148;
-        k.store(v, std::memory_order_relaxed);
-    }
-    return v;
-}
-
 struct Plan {
     int NT, RT, ctas;                                      // ctas: of the shares; 0: a CTA a head and tile of rows
 };
@@ -744,14 +688,27 @@ int launch(AttArgs a, const Plan& p, cudaStream_t stream) {
 
 }  // namespace
 
+int sm_count() {
+    static std::atomic<int> known[kMaxDevices];
+    std::atomic<int>& k = known[current_device()];
+    int v = k.load(std::memory_order_relaxed);
+    if (v == 0) {
+        if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, current_device()) != cudaSuccess || v <= 0) v = 148;
+        k.store(v, std::memory_order_relaxed);
+    }
+    return v;
+}
+
 size_t cache_attention_workspace_bytes(int B, int H, int Ncap, int d, int Tq, int Hq) {
     if (B < 1 || H < 1 || Hq < 1 || Tq < 1) return kStatusBytes;
+    if (rows_kernel_takes((int64_t)Hq / H * Tq, d)) return rows_workspace_bytes(B, H, Ncap, d, Tq, Hq);
     const Plan p = plan_of(B, H, Ncap, d, Tq, Hq, sm_count());
     return kStatusBytes + part_bytes(p, d);
 }
 
 int launch_cache_attention(const CacheQueries& io, const void* cache, int B, int Hq, int H, int Tq, int d, int Ncap,
                            const int32_t* cache_len, float scale, bool causal, float* lse, void* workspace, cudaStream_t stream) {
+    const bool many = rows_kernel_takes((int64_t)Hq / H * Tq, d);
     const Plan p = plan_of(B, H, Ncap, d, Tq, Hq, sm_count());
     if ((int64_t)B * H * p.RT > 0x7fffffff || (int64_t)Hq / H * Tq > 0x7fffffff - 64) return VITCOP_ERR_UNSUPPORTED;
     AttArgs a;
@@ -766,6 +723,7 @@ int launch_cache_attention(const CacheQueries& io, const void* cache, int B, int
     a.zero = scale == 0.f;
     a.sign = scale < 0.f ? 0x80008000u : 0u;
     a.scale_log2 = a.zero ? 1.f : (scale < 0.f ? -scale : scale) * kLog2e;
+    if (many) return launch_cache_attention_rows(a, d, workspace, stream);
     if (d == 64) return p.NT == 1 ? launch<64, 1>(a, p, stream) : p.NT == 2 ? launch<64, 2>(a, p, stream) : p.NT == 3 ? launch<64, 3>(a, p, stream) : launch<64, 4>(a, p, stream);
     if (d == 128) return p.NT == 1 ? launch<128, 1>(a, p, stream) : p.NT == 2 ? launch<128, 2>(a, p, stream) : p.NT == 3 ? launch<128, 3>(a, p, stream) : launch<128, 4>(a, p, stream);
     return p.NT == 1 ? launch<256, 1>(a, p, stream) : launch<256, 2>(a, p, stream);

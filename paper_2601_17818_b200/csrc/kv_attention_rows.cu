@@ -1,0 +1,557 @@
+// Attention over the cache in 4 bits for many query rows (a question, a chunk of a prompt): 128 rows of a head a CTA, tcgen05.
+//
+// Tokens come in tiles of 64.  Four warps turn a tile into operands: codes of K as the bf16 c - 8, exactly, codes of V as the bf16
+// nearest to the values they stand for, transposed.  With G = d / 32 groups of a row the logits are
+//     z = sum over g of s_g (q_g . (c - 8)_g)  +  sum over g of m_g sum(q_g)
+// G products of their own (q as it is, bf16), whose fp32 sums the scales multiply behind tensor memory, and one more for the centres with
+// sum(q_g) split into three bf16.  Four warps, a thread a row, make the weights of the logits and write them back as
+// operand of the second product, which stays in tensor memory; a row's maximum is moved only when a logit has passed it by 2^8.
+// Every operand is rows of 128 bytes in the 128-byte swizzle.  Waits are bounded: a CTA that gives up reports it, and the join,
+// which always follows, sets the status word.
+#include "gram.cuh"
+#include "kv_attention.cuh"
+#include "tcgen05.cuh"
+
+namespace vitcop {
+namespace {
+
+constexpr int kRows = 128, kTokens = 64;
+constexpr int kSoftmaxThreads = 128, kUnpackThreads = 128, kThreads = kSoftmaxThreads + kUnpackThreads + 32;
+constexpr uint32_t kTmem = 512;
+enum { kRoleUnpack = 1, kRoleMma = 2, kRoleSoftmax = 4 };
+
+template <int D>
+struct RowsSmem {
+    static constexpr int kSubs = D / 64;
+    static constexpr int kQ = 0;                                       // [D / 64][128 rows][128 bytes]
+    static constexpr int kSums = kQ + kSubs * 16384;                   // [128 rows][128 bytes], 32 of which are used
+    static constexpr int kP = kSums + 16384;                           // [128 rows][64 tokens]
+    static constexpr int kStage = kP + 16384;                          // two of them:
+    static constexpr int kK = 0;                                       //   [D / 64][64 tokens][128 bytes]
+    static constexpr int kV = kK + kSubs * 8192;                       //   [D elements][64 tokens]
+    static constexpr int kC = kV + D * 128;                            //   [64 tokens][128 bytes]
+    static constexpr int kS = kC + 8192;                               //   fp32 [G][64 tokens]
+    static constexpr int kStageBytes = kS + 1024;
+    static constexpr int kRaw = kStage + 2 * kStageBytes;              // two tiles as they lie in the cache
+    static constexpr int kRawBytes = 2 * CacheBlock<D>::kBytes;
+    static constexpr int kBars = kRaw + 2 * kRawBytes;
+    static constexpr int kBytes = kBars + 256 + 1024;                  // (and what aligning to 1024 takes)
+};
+
+struct RowsArgs {
+    AttArgs a;
+    uint8_t* reports;                                      // a byte a CTA
+    int splits;
+    unsigned long long wait_ns;
+    int expire_roles;
+    __device__ __forceinline__ unsigned long long limit_of(int role) const { return (expire_roles & role) ? 0ull : wait_ns; }
+};
+
+// Byte of 16-byte piece c of row r.
+__device__ __forceinline__ int at_swizzled(int r, int c) { return r * 128 + ((c ^ (r & 7)) << 4); }
+__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void unpack_bar() { asm volatile("bar.sync 2, 128;" ::: "memory"); }
+__device__ __forceinline__ bool unpack_bar_or(bool pred) {     // the same answer for all of them
+    uint32_t out;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.or.pred q, 2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(out) : "r"((uint32_t)pred) : "memory");
+    return out != 0;
+}
+
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {         // (data behind tmem_wait_ld)
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+}
+template <int N>
+__device__ __forceinline__ void tmem_wait_ld(uint32_t (&r)[N][16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int n = 0; n < N; ++n)                            // (no use of the registers in front of the wait)
+        asm volatile("" : "+r"(r[n][0]), "+r"(r[n][1]), "+r"(r[n][2]), "+r"(r[n][3]), "+r"(r[n][4]), "+r"(r[n][5]), "+r"(r[n][6]), "+r"(r[n][7]),
+                     "+r"(r[n][8]), "+r"(r[n][9]), "+r"(r[n][10]), "+r"(r[n][11]), "+r"(r[n][12]), "+r"(r[n][13]), "+r"(r[n][14]), "+r"(r[n][15]));
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&v)[32]) {
+    const auto u = [&](int i) { return __float_as_uint(v[i]); };
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, "
+        "%20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        ::"r"(taddr), "r"(u(0)), "r"(u(1)), "r"(u(2)), "r"(u(3)), "r"(u(4)), "r"(u(5)), "r"(u(6)), "r"(u(7)), "r"(u(8)), "r"(u(9)), "r"(u(10)),
+        "r"(u(11)), "r"(u(12)), "r"(u(13)), "r"(u(14)), "r"(u(15)), "r"(u(16)), "r"(u(17)), "r"(u(18)), "r"(u(19)), "r"(u(20)), "r"(u(21)),
+        "r"(u(22)), "r"(u(23)), "r"(u(24)), "r"(u(25)), "r"(u(26)), "r"(u(27)), "r"(u(28)), "r"(u(29)), "r"(u(30)), "r"(u(31))
+        : "memory");
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+cache_attention_rows_kernel(RowsArgs k) {
+    using L = CacheBlock<D>;
+    using S = RowsSmem<D>;
+    constexpr int G = L::G;
+    const AttArgs& a = k.a;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    const uint32_t base = smem_u32(smem);
+    const uint32_t bar_full = base + S::kBars, bar_empty = bar_full + 16, bar_s = bar_full + 32, bar_read = bar_full + 40, bar_p = bar_full + 48,
+                   bar_pv = bar_full + 56, bar_drain = bar_full + 64;
+    volatile int* const abort_flag = reinterpret_cast<volatile int*>(smem + S::kBars + 72);
+    uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + S::kBars + 76);
+    int* const first_bad = reinterpret_cast<int*>(smem + S::kBars + 96);        // [G] first token whose values of V are no numbers
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar_full + 8 * i, kUnpackThreads);
+            mbar_init(bar_empty + 8 * i, 1);
+        }
+        mbar_init(bar_s, 1);
+        mbar_init(bar_read, kSoftmaxThreads);
+        mbar_init(bar_p, kSoftmaxThreads);
+        mbar_init(bar_pv, 1);
+        mbar_init(bar_drain, 1);
+        *abort_flag = 0;
+        for (int i = 0; i < G; ++i) first_bad[i] = 0x7fffffff;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 8) tmem_alloc(smem_u32(tmem_slot), kTmem);
+    grid_dependency_wait();
+    grid_dependency_launch_dependents();                   // (the join's CTAs, which wait for this grid to end)
+
+    const int split = blockIdx.x % k.splits, seg = blockIdx.x / k.splits, segs = a.H * (int)a.RT.d, b = seg / segs, hs = seg - b * segs;
+    const int h = quotient(hs, a.RT), row0 = (hs - h * (int)a.RT.d) * kRows, rows = (int)a.R.d * a.Tq;
+    const int len = a.cache_len ? max(0, min(__ldcg(a.cache_len + b), a.Ncap)) : a.Ncap;
+    const int last = min(row0 + kRows, rows) - 1;
+    const int most = a.causal ? max(0, len - a.Tq + quotient(last, a.R) + 1) : len;
+    const int least = a.causal ? max(0, len - a.Tq + quotient(row0, a.R) + 1) : len;
+    const int tiles = (most + kTokens - 1) / kTokens;
+    const int t0 = (int)((int64_t)tiles * split / k.splits), t1 = (int)((int64_t)tiles * (split + 1) / k.splits), n = t1 - t0;
+    const uint8_t* const head = a.cache + ((int64_t)b * a.H + h) * (a.Ncap / kCacheBlock) * L::kBytes;
+
+    // this thread's row as operand
+    const int r = row0 + tid, tq = r < rows ? quotient(r, a.R) : 0, hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
+    int limit = 0;
+    if (tid < kSoftmaxThreads) {
+        limit = r < rows ? (a.causal ? max(0, len - a.Tq + tq + 1) : len) : 0;
+        const bool there = r < rows && !a.zero;
+        const __nv_bfloat16* const src = a.io.q + (r < rows ? b * a.io.qb + hq * a.io.qh + tq * a.io.qt : 0);
+        float total[G];
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            float x = 0.f;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint4 v = there ? __ldcg(reinterpret_cast<const uint4*>(src + i * 32 + c * 8)) : make_uint4(0, 0, 0, 0);
+                v = make_uint4(v.x ^ a.sign, v.y ^ a.sign, v.z ^ a.sign, v.w ^ a.sign);
+                x += ((bf16lo(v.x) + bf16hi(v.x)) + (bf16lo(v.y) + bf16hi(v.y))) + ((bf16lo(v.z) + bf16hi(v.z)) + (bf16lo(v.w) + bf16hi(v.w)));
+                // elements 0 and 4, 1 and 5, 2 and 6, 3 and 7, as the codes lie
+                *reinterpret_cast<uint4*>(smem + S::kQ + (i / 2) * 16384 + at_swizzled(tid, (i & 1) * 4 + c)) =
+                    make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
+            }
+            total[i] = x;
+        }
+        // part p of group i is element p G + i of the product with the centres
+        float part[16] = {};
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            const float first = __bfloat162float(__float2bfloat16_rn(total[i])), second = __bfloat162float(__float2bfloat16_rn(total[i] - first));
+            part[i] = first;
+            part[G + i] = second;
+            part[2 * G + i] = (total[i] - first) - second;
+        }
+        *reinterpret_cast<uint4*>(smem + S::kSums + at_swizzled(tid, 0)) =
+            make_uint4(bf16x2(part[0], part[1]), bf16x2(part[2], part[3]), bf16x2(part[4], part[5]), bf16x2(part[6], part[7]));
+        *reinterpret_cast<uint4*>(smem + S::kSums + at_swizzled(tid, 1)) =
+            make_uint4(bf16x2(part[8], part[9]), bf16x2(part[10], part[11]), bf16x2(part[12], part[13]), bf16x2(part[14], part[15]));
+        fence_async_proxy();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot, tmem_z = tmem, tmem_c = tmem + 4 * kTokens, tmem_o = tmem_c + kTokens;
+
+    if (warp < 4) {
+        // ------------------------------------------------------------------ softmax: a thread a row
+        const unsigned long long lim = k.limit_of(kRoleSoftmax);
+        const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+        float top = kNoLogit, sum = 0.f;                   // in powers of two
+        bool ok = true;
+        for (int i = 0; i < n; ++i) {
+            const int token0 = (t0 + i) * kTokens;
+            const float* const scale = reinterpret_cast<const float*>(smem + S::kStage + (i & 1) * S::kStageBytes + S::kS);
+            ok = __all_sync(0xffffffffu, mbar_wait(bar_s, i & 1, abort_flag, lim));
+            if (!ok) break;
+            tc_fence_after();
+            float z[kTokens];
+#pragma unroll
+            for (int c = 0; c < kTokens / 16; ++c) {
+                uint32_t x[G + 1][16];
+                tmem_ld16(tmem_c + lanes + 16 * c, x[G]);
+#pragma unroll
+                for (int g = 0; g < G; ++g) tmem_ld16(tmem_z + lanes + g * kTokens + 16 * c, x[g]);
+                tmem_wait_ld(x);
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    f32x2 lo = pack2(__uint_as_float(x[G][e]), __uint_as_float(x[G][e + 1])), hi = pack2(__uint_as_float(x[G][e + 2]), __uint_as_float(x[G][e + 3]));
+#pragma unroll
+                    for (int g = 0; g < G; ++g) {
+                        const float4 f = *reinterpret_cast<const float4*>(scale + g * kTokens + 16 * c + e);
+                        lo = fma2(pack2(__uint_as_float(x[g][e]), __uint_as_float(x[g][e + 1])), pack2(f.x, f.y), lo);
+                        hi = fma2(pack2(__uint_as_float(x[g][e + 2]), __uint_as_float(x[g][e + 3])), pack2(f.z, f.w), hi);
+                    }
+                    const float2 u = unpack2(lo), v = unpack2(hi);
+                    z[16 * c + e] = u.x;
+                    z[16 * c + e + 1] = u.y;
+                    z[16 * c + e + 2] = v.x;
+                    z[16 * c + e + 3] = v.y;
+                }
+            }
+            tc_fence_before();
+            mbar_arrive(bar_read);
+            if (token0 + kTokens > least) {
+                const int seen = limit - token0;
+#pragma unroll
+                for (int e = 0; e < kTokens; ++e)
+                    if (e >= seen) z[e] = MINUS_INF;
+            }
+            float high = z[0];
+#pragma unroll
+            for (int e = 1; e < kTokens; ++e) high = fmaxf(high, z[e]);
+            high *= a.scale_log2;
+            if (i > 0) {                                   // the product behind has read the weights, and its sums stand still
+                ok = __all_sync(0xffffffffu, mbar_wait(bar_pv, (i - 1) & 1, abort_flag, lim));
+                if (!ok) break;
+                tc_fence_after();
+            }
+            if (__any_sync(0xffffffffu, high - top > 8.f)) {
+                const float now = fmaxf(top, high), keep = ex2_approx(top - now);
+                top = now;
+                sum *= keep;
+                if (i > 0) {
+#pragma unroll 1
+                    for (int c = 0; c < G; ++c) {
+                        float v[32];
+                        tmem_ld32(tmem_o + lanes + 32 * c, v);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] *= keep;
+                        tmem_st32(tmem_o + lanes + 32 * c, v);
+                    }
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < kTokens / 8; ++c) {
+                uint32_t w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p0 = ex2_approx(fmaf(z[8 * c + 2 * e], a.scale_log2, -top)), p1 = ex2_approx(fmaf(z[8 * c + 2 * e + 1], a.scale_log2, -top));
+                    sum += p0 + p1;
+                    w[e] = bf16x2(p0, p1);
+                }
+                *reinterpret_cast<uint4*>(smem + S::kP + at_swizzled(tid, c)) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            fence_async_proxy();
+            tc_fence_before();
+            mbar_arrive(bar_p);
+        }
+        if (ok && n > 0) {
+            ok = __all_sync(0xffffffffu, mbar_wait(bar_pv, (n - 1) & 1, abort_flag, lim));
+            tc_fence_after();
+        }
+        if (ok) {
+            const bool none = sum == 0.f, alone = k.splits == 1;
+            const float inv = alone ? (none ? 0.f : 1.f / sum) : 1.f;
+            float* const part = a.part + (size_t)blockIdx.x * kRows * (D + 2);
+#pragma unroll 1
+            for (int c = 0; c < G; ++c) {
+                float v[32];
+                if (n > 0) {
+                    tmem_ld32(tmem_o + lanes + 32 * c, v);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] = 0.f;
+                }
+                const bool bad = first_bad[c] < limit;     // a row of V that is no number, and that this query sees
+                // (column 8 i + g of a group is its element 4 g + i)
+                if (r < rows) {
+#pragma unroll
+                    for (int g = 0; g < 8; ++g) {
+                        const float nan = __int_as_float(0x7fc00000);
+                        const float4 o = bad ? make_float4(nan, nan, nan, nan) : make_float4(v[g] * inv, v[8 + g] * inv, v[16 + g] * inv, v[24 + g] * inv);
+                        if (alone)
+                            *reinterpret_cast<uint2*>(a.io.out + b * a.io.ob + hq * a.io.oh + tq * a.io.ot + c * 32 + 4 * g) =
+                                make_uint2(bf16x2(o.x, o.y), bf16x2(o.z, o.w));
+                        else
+                            *reinterpret_cast<float4*>(part + tid * D + c * 32 + 4 * g) = o;
+                    }
+                }
+            }
+            if (r < rows) {
+                if (!alone) {
+                    part[kRows * D + tid] = top;
+                    part[kRows * D + kRows + tid] = sum;
+                } else if (a.lse) {
+                    a.lse[((int64_t)b * a.Hq + hq) * a.Tq + tq] = none ? MINUS_INF : (top + __log2f(sum)) * kLn2;
+                }
+            }
+        }
+    } else if (warp < 8) {
+        // ------------------------------------------------------------------ unpack
+        const unsigned long long lim = k.limit_of(kRoleUnpack);
+        const int u = tid - kSoftmaxThreads, blocks = (len + kCacheBlock - 1) / kCacheBlock;
+        const auto fetch = [&](int i) {                    // (a tile's second block may be behind the last there is)
+            if (i < n) {
+                const int first = (t0 + i) * 2, pieces = min(2, blocks - first) * (L::kBytes / 16);
+                const uint8_t* const src = head + (int64_t)first * L::kBytes;
+                const uint32_t dst = base + S::kRaw + (i & 1) * S::kRawBytes;
+                for (int c = u; c < pieces; c += kUnpackThreads)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + 16 * c), "l"(src + 16 * c) : "memory");
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        fetch(0);
+        fetch(1);
+        bool ok = true;
+        for (int i = 0; i < n; ++i) {
+            if (i >= 2) ok = mbar_wait(bar_empty + 8 * (i & 1), ((i >> 1) - 1) & 1, abort_flag, lim);
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+            if (unpack_bar_or(!ok || *abort_flag)) break;
+            const uint8_t* const raw = smem + S::kRaw + (i & 1) * S::kRawBytes;
+            uint8_t* const stage = smem + S::kStage + (i & 1) * S::kStageBytes;
+            const int token0 = (t0 + i) * kTokens;
+            // K: a thread a quarter of a token's row, twice
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                const int id = u + v * kUnpackThreads, row = id >> 2, t = id & 3;
+                const uint8_t* const block = raw + (row >> 5) * L::kBytes;
+                const int rb = row & 31;
+                uint32_t w[G];
+                if constexpr (G == 4) {
+                    const uint4 x = *reinterpret_cast<const uint4*>(block + L::kKCodes + rb * (D / 2) + t * 16);
+                    w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+                } else {
+                    const uint2 x = *reinterpret_cast<const uint2*>(block + L::kKCodes + rb * (D / 2) + t * 8);
+                    w[0] = x.x; w[1] = x.y;
+                }
+#pragma unroll
+                for (int g = 0; g < G; ++g)
+                    *reinterpret_cast<uint4*>(stage + S::kK + (g / 2) * 8192 + at_swizzled(row, (g & 1) * 4 + t)) =
+                        make_uint4(centred(code_pair(w[g])), centred(code_pair(w[g] >> 4)), centred(code_pair(w[g] >> 8)), centred(code_pair(w[g] >> 12)));
+            }
+            if (u < kTokens) {                             // centres three times over, scales
+                const uint8_t* const block = raw + (u >> 5) * L::kBytes;
+                const int rb = u & 31;
+                uint32_t m[2] = {}, s[2] = {};
+#pragma unroll
+                for (int e = 0; e < G / 2; ++e) {
+                    m[e] = *reinterpret_cast<const uint32_t*>(block + L::kKCentre + rb * 2 * G + 4 * e);
+                    s[e] = *reinterpret_cast<const uint32_t*>(block + L::kKScale + rb * 2 * G + 4 * e);
+                }
+                *reinterpret_cast<uint4*>(stage + S::kC + at_swizzled(u, 0)) = G == 4 ? make_uint4(m[0], m[1], m[0], m[1]) : make_uint4(m[0], m[0], m[0], 0u);
+                *reinterpret_cast<uint4*>(stage + S::kC + at_swizzled(u, 1)) = G == 4 ? make_uint4(m[0], m[1], 0u, 0u) : make_uint4(0u, 0u, 0u, 0u);
+                float* const f = reinterpret_cast<float*>(stage + S::kS) + u;
+#pragma unroll
+                for (int g = 0; g < G; ++g) f[g * kTokens] = g & 1 ? bf16hi(s[g / 2]) : bf16lo(s[g / 2]);
+            }
+            // V: a thread four elements of each group of two tokens, twice
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                const int id = u + v * kUnpackThreads, g8 = id & 7, pair = id >> 3, there = len - token0 - 2 * pair;
+                const uint8_t* const block = raw + (pair >> 4) * L::kBytes;
+                const int rb = 2 * (pair & 15);
+                const uint32_t keep = (there > 0 ? 0x0000FFFFu : 0u) | (there > 1 ? 0xFFFF0000u : 0u);
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    const uint32_t x = (uint32_t)*reinterpret_cast<const uint16_t*>(block + L::kVCodes + rb * (D / 2) + g8 * 2 * G + 2 * g) |
+                                       (uint32_t)*reinterpret_cast<const uint16_t*>(block + L::kVCodes + (rb + 1) * (D / 2) + g8 * 2 * G + 2 * g) << 16;
+                    uint32_t s = (uint32_t)*reinterpret_cast<const uint16_t*>(block + L::kVScale + (rb * G + g) * 2) |
+                                 (uint32_t)*reinterpret_cast<const uint16_t*>(block + L::kVScale + ((rb + 1) * G + g) * 2) << 16;
+                    const uint32_t m = *reinterpret_cast<const uint32_t*>(block + L::kVCentre + (g * 32 + rb) * 2);
+                    // what is no number would reach rows that do not see it: it is a zero here, and those that do see it are told
+                    uint32_t fine = keep;
+                    if ((s & 0x7FFFu) > 0x7F80u) {
+                        fine &= 0xFFFF0000u;
+                        if (there > 0 && g8 == 0) atomicMin(first_bad + g, token0 + 2 * pair);
+                    }
+                    if ((s >> 16 & 0x7FFFu) > 0x7F80u) {
+                        fine &= 0x0000FFFFu;
+                        if (there > 1 && g8 == 0) atomicMin(first_bad + g, token0 + 2 * pair + 1);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        uint32_t y;
+                        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(y) : "r"(centred(code_pair(x >> (4 * e)))), "r"(s), "r"(m));
+                        const int row = g * 32 + 8 * e + g8;
+                        *reinterpret_cast<uint32_t*>(stage + S::kV + at_swizzled(row, pair >> 2) + (pair & 3) * 4) = y & fine;
+                    }
+                }
+            }
+            fence_async_proxy();
+            mbar_arrive(bar_full + 8 * (i & 1));
+            unpack_bar();                                  // (the raw tile has been read)
+            fetch(i + 2);
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    } else if (lane == 0) {
+        // ------------------------------------------------------------------ products
+        const unsigned long long lim = k.limit_of(kRoleMma);
+        constexpr uint32_t idesc_z = umma_idesc_bf16(kRows, kTokens), idesc_o = umma_idesc_bf16(kRows, D);
+        bool ok = true;
+        for (int i = 0; ok && i <= n; ++i) {
+            if (i < n) {
+                ok = mbar_wait(bar_full + 8 * (i & 1), (i >> 1) & 1, abort_flag, lim) && (i == 0 || mbar_wait(bar_read, (i - 1) & 1, abort_flag, lim));
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t stage = base + S::kStage + (i & 1) * S::kStageBytes;
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    const uint64_t dq = umma_desc_k128(base + S::kQ + (g / 2) * 16384) + (uint64_t)((g & 1) * 4);
+                    const uint64_t dk = umma_desc_k128(stage + S::kK + (g / 2) * 8192) + (uint64_t)((g & 1) * 4);
+                    tc_mma_bf16(tmem_z + g * kTokens, dq, dk, idesc_z, 0);
+                    tc_mma_bf16(tmem_z + g * kTokens, dq + 2, dk + 2, idesc_z, 1);
+                }
+                tc_mma_bf16(tmem_c, umma_desc_k128(base + S::kSums), umma_desc_k128(stage + S::kC), idesc_z, 0);
+                tc_commit(bar_s);
+            }
+            if (i > 0) {
+                ok = mbar_wait(bar_p, (i - 1) & 1, abort_flag, lim);
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t dp = umma_desc_k128(base + S::kP), dv = umma_desc_k128(base + S::kStage + ((i - 1) & 1) * S::kStageBytes + S::kV);
+#pragma unroll
+                for (int e = 0; e < kTokens / 16; ++e) tc_mma_bf16(tmem_o, dp + 2 * e, dv + 2 * e, idesc_o, i > 1 || e > 0 ? 1u : 0u);
+                tc_commit(bar_empty + 8 * ((i - 1) & 1));
+                tc_commit(bar_pv);
+            }
+        }
+        tc_commit(bar_drain);                              // (waited for below)
+    }
+    __syncthreads();
+    // Another role may have given up behind the last product: operands and tensor memory stay until all of them have completed.
+    if (tid == kSoftmaxThreads + kUnpackThreads) {
+        mbar_drain(bar_drain, 0);
+        k.reports[blockIdx.x] = *abort_flag ? 1 : 0;
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) {
+        tc_fence_after();
+        tmem_dealloc(tmem, kTmem);
+    }
+}
+
+// The pieces of a row, in their order, a warp a row; and the status word.
+template <int D>
+__global__ void __launch_bounds__(128)
+cache_attention_rows_join_kernel(RowsArgs k, int ctas) {
+    const AttArgs& a = k.a;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rows = (int)a.R.d * a.Tq;
+    constexpr int E = D / 32;                              // elements of a lane: lane E .. lane E + E - 1
+    grid_dependency_wait();
+    if (blockIdx.x == 0 && warp == 0) {
+        bool gave_up = false;
+        for (int c = lane; c < ctas; c += 32) gave_up |= k.reports[c] != 0;
+        gave_up = __any_sync(0xffffffffu, gave_up);
+        if (lane == 0) *a.status = gave_up ? VITCOP_ERR_TIMEOUT : VITCOP_OK;
+    }
+    if (k.splits == 1) return;
+    const int segs = a.H * (int)a.RT.d, items = a.B * segs * kRows;
+    for (int item = blockIdx.x * 4 + warp; item < items; item += gridDim.x * 4) {
+        const int seg = item / kRows, rl = item - seg * kRows, b = seg / segs, hs = seg - b * segs, h = quotient(hs, a.RT);
+        const int r = (hs - h * (int)a.RT.d) * kRows + rl;
+        if (r >= rows) continue;
+        const float* const part = a.part + (size_t)seg * k.splits * kRows * (D + 2);
+        constexpr size_t kSize = (size_t)kRows * (D + 2);
+        float top = kNoLogit, sum = 0.f, v[E] = {};
+        for (int s = 0; s < k.splits; ++s) top = fmaxf(top, part[s * kSize + kRows * D + rl]);
+        for (int s = 0; s < k.splits; ++s) {
+            const float* const p = part + s * kSize;
+            const float f = ex2_approx(p[kRows * D + rl] - top);
+            sum = fmaf(p[kRows * D + kRows + rl], f, sum);
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+                const float2 x = *reinterpret_cast<const float2*>(p + rl * D + lane * E + e);
+                v[e] = fmaf(x.x, f, v[e]);
+                v[e + 1] = fmaf(x.y, f, v[e + 1]);
+            }
+        }
+        const int tq = quotient(r, a.R), hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
+        const bool none = sum == 0.f;
+        const float inv = none ? 0.f : 1.f / sum;
+        uint32_t* const out = reinterpret_cast<uint32_t*>(a.io.out + b * a.io.ob + hq * a.io.oh + tq * a.io.ot + lane * E);
+#pragma unroll
+        for (int e = 0; e < E; e += 2) out[e / 2] = bf16x2(v[e] * inv, v[e + 1] * inv);
+        if (a.lse && lane == 0) a.lse[((int64_t)b * a.Hq + hq) * a.Tq + tq] = none ? MINUS_INF : (top + __log2f(sum)) * kLn2;
+    }
+}
+
+struct RowsPlan {
+    int RT, splits;
+    int64_t ctas;
+};
+RowsPlan plan_of(int B, int H, int Ncap, int Tq, int Hq) {
+    RowsPlan p;
+    const int64_t rows = (int64_t)(Hq / H) * Tq;
+    p.RT = (int)((rows + kRows - 1) / kRows);
+    const int64_t segs = (int64_t)B * H * p.RT, sms = sm_count(), tiles = Ncap / kTokens;
+    int64_t s = segs < sms ? sms / segs : 1;
+    if (s > tiles / 4) s = tiles / 4;                      // four tiles a piece at least
+    p.splits = (int)(s < 1 ? 1 : s > 16 ? 16 : s);
+    p.ctas = segs * p.splits;
+    return p;
+}
+size_t reports_bytes(const RowsPlan& p) { return align_up((size_t)p.ctas, 256); }
+
+template <int D>
+int launch_rows(const RowsArgs& k, const RowsPlan& p, cudaStream_t stream) {
+    static DoneOnDevice done;
+    int rc = allow_dynamic_smem(cache_attention_rows_kernel<D>, RowsSmem<D>::kBytes, done);
+    if (rc != VITCOP_OK) return rc;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)p.ctas);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = RowsSmem<D>::kBytes;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = pdl_allowed(true) ? 1 : 0;
+    {
+        KernelTimeScope timed("cache_attention_rows_kernel", stream);
+        rc = record_cuda(cudaLaunchKernelEx(&cfg, cache_attention_rows_kernel<D>, k));
+        if (rc != VITCOP_OK) return rc;
+    }
+    const int64_t items = p.splits > 1 ? (int64_t)k.a.B * k.a.H * p.RT * kRows : 1, most = sm_count() * 16;
+    cfg.gridDim = dim3((unsigned)((items + 3) / 4 < most ? (items + 3) / 4 : most));
+    cfg.blockDim = dim3(128);
+    cfg.dynamicSmemBytes = 0;
+    KernelTimeScope timed("cache_attention_rows_join_kernel", stream);
+    return record_cuda(cudaLaunchKernelEx(&cfg, cache_attention_rows_join_kernel<D>, k, (int)p.ctas));
+}
+
+}  // namespace
+
+bool rows_kernel_takes(int64_t rows, int d) { return d != 256 && rows >= 64; }
+
+size_t rows_workspace_bytes(int B, int H, int Ncap, int d, int Tq, int Hq) {
+    const RowsPlan p = plan_of(B, H, Ncap, Tq, Hq);
+    return kStatusBytes + reports_bytes(p) + (p.splits > 1 ? align_up((size_t)p.ctas * kRows * (d + 2) * sizeof(float), 256) : 0);
+}
+
+int launch_cache_attention_rows(const AttArgs& args, int d, void* workspace, cudaStream_t stream) {
+    const RowsPlan p = plan_of(args.B, args.H, args.Ncap, args.Tq, args.Hq);
+    if (p.ctas * kRows > 0x7fffffff) return VITCOP_ERR_UNSUPPORTED;
+    RowsArgs k;
+    k.a = args;
+    k.a.RT = divisor(p.RT);
+    k.reports = static_cast<uint8_t*>(workspace) + kStatusBytes;
+    k.a.part = reinterpret_cast<float*>(k.reports + reports_bytes(p));
+    k.splits = p.splits;
+    k.wait_ns = gram_wait_limit_ns();
+    k.expire_roles = pair_expire_roles();
+    return d == 64 ? launch_rows<64>(k, p, stream) : launch_rows<128>(k, p, stream);
+}
+
+}  // namespace vitcop
