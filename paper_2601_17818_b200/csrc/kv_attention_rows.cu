@@ -4,7 +4,7 @@
 // nearest to the values they stand for, transposed.  With G = d / 32 groups of a row the logits are
 //     z = sum over g of s_g (q_g . (c - 8)_g)  +  sum over g of m_g sum(q_g)
 // G products of their own (q as it is, bf16), whose fp32 sums the scales multiply behind tensor memory, and one more for the centres with
-// sum(q_g) split into three bf16.  Four warps, a thread a row, make the weights of the logits and write them back as
+// sum(q_g) split into three bf16.  Eight warps, two threads a row (32 tokens each), make the weights of the logits and write them back as
 // operand of the second product, which stays in tensor memory; a row's maximum is moved only when a logit has passed it by 2^8.
 // Every operand is rows of 128 bytes in the 128-byte swizzle.  Waits are bounded: a CTA that gives up reports it, and the join,
 // which always follows, sets the status word.
@@ -16,7 +16,7 @@ namespace vitcop {
 namespace {
 
 constexpr int kRows = 128, kTokens = 64;
-constexpr int kSoftmaxThreads = 128, kUnpackThreads = 128, kThreads = kSoftmaxThreads + kUnpackThreads + 32;
+constexpr int kSoftmaxThreads = 256, kUnpackThreads = 256, kThreads = kSoftmaxThreads + kUnpackThreads + 32;
 constexpr uint32_t kTmem = 512;
 enum { kRoleUnpack = 1, kRoleMma = 2, kRoleSoftmax = 4 };
 
@@ -35,7 +35,8 @@ struct RowsSmem {
     static constexpr int kRaw = kStage + 2 * kStageBytes;              // two tiles as they lie in the cache
     static constexpr int kRawBytes = 2 * CacheBlock<D>::kBytes;
     static constexpr int kBars = kRaw + 2 * kRawBytes;
-    static constexpr int kBytes = kBars + 256 + 1024;                  // (and what aligning to 1024 takes)
+    static constexpr int kPairs = kBars + 256;                         // fp32 [2][128 rows]: what the two threads of a row tell each other
+    static constexpr int kBytes = kPairs + 1024 + 1024;                  // (and what aligning to 1024 takes)
 };
 
 struct RowsArgs {
@@ -50,29 +51,33 @@ struct RowsArgs {
 // Byte of 16-byte piece c of row r.
 __device__ __forceinline__ int at_swizzled(int r, int c) { return r * 128 + ((c ^ (r & 7)) << 4); }
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void unpack_bar() { asm volatile("bar.sync 2, 128;" ::: "memory"); }
+__device__ __forceinline__ void unpack_bar() { asm volatile("bar.sync 2, 256;" ::: "memory"); }
 __device__ __forceinline__ bool unpack_bar_or(bool pred) {     // the same answer for all of them
     uint32_t out;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.or.pred q, 2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.or.pred q, 2, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
                  : "=r"(out) : "r"((uint32_t)pred) : "memory");
     return out != 0;
 }
 
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {         // (data behind tmem_wait_ld)
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(taddr)
-        : "memory");
-}
 template <int N>
-__device__ __forceinline__ void tmem_wait_ld(uint32_t (&r)[N][16]) {
+__device__ __forceinline__ void words(uint32_t (&w)[N], const uint8_t* p) {
+    if constexpr (N == 4) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p);
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    } else if constexpr (N == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        w[0] = v.x; w[1] = v.y;
+    } else {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
+    }
+}
+
+template <int N>
+__device__ __forceinline__ void tmem_wait_ld(uint32_t (&r)[N][8]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
     for (int n = 0; n < N; ++n)                            // (no use of the registers in front of the wait)
-        asm volatile("" : "+r"(r[n][0]), "+r"(r[n][1]), "+r"(r[n][2]), "+r"(r[n][3]), "+r"(r[n][4]), "+r"(r[n][5]), "+r"(r[n][6]), "+r"(r[n][7]),
-                     "+r"(r[n][8]), "+r"(r[n][9]), "+r"(r[n][10]), "+r"(r[n][11]), "+r"(r[n][12]), "+r"(r[n][13]), "+r"(r[n][14]), "+r"(r[n][15]));
+        asm volatile("" : "+r"(r[n][0]), "+r"(r[n][1]), "+r"(r[n][2]), "+r"(r[n][3]), "+r"(r[n][4]), "+r"(r[n][5]), "+r"(r[n][6]), "+r"(r[n][7]));
 }
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&v)[32]) {
     const auto u = [&](int i) { return __float_as_uint(v[i]); };
@@ -100,6 +105,8 @@ cache_attention_rows_kernel(RowsArgs k) {
                    bar_pv = bar_full + 56, bar_drain = bar_full + 64;
     volatile int* const abort_flag = reinterpret_cast<volatile int*>(smem + S::kBars + 72);
     uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + S::kBars + 76);
+    int* const moved = reinterpret_cast<int*>(smem + S::kBars + 112);           // [3] a row's maximum has to move, tile by tile
+    float* const pairs = reinterpret_cast<float*>(smem + S::kPairs);
     int* const first_bad = reinterpret_cast<int*>(smem + S::kBars + 96);        // [G] first token whose values of V are no numbers
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) {
@@ -113,10 +120,11 @@ cache_attention_rows_kernel(RowsArgs k) {
         mbar_init(bar_pv, 1);
         mbar_init(bar_drain, 1);
         *abort_flag = 0;
+        moved[0] = moved[1] = moved[2] = 0;
         for (int i = 0; i < G; ++i) first_bad[i] = 0x7fffffff;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 8) tmem_alloc(smem_u32(tmem_slot), kTmem);
+    if (warp == kThreads / 32 - 1) tmem_alloc(smem_u32(tmem_slot), kTmem);
     grid_dependency_wait();
     grid_dependency_launch_dependents();                   // (the join's CTAs, which wait for this grid to end)
 
@@ -131,10 +139,10 @@ cache_attention_rows_kernel(RowsArgs k) {
     const uint8_t* const head = a.cache + ((int64_t)b * a.H + h) * (a.Ncap / kCacheBlock) * L::kBytes;
 
     // this thread's row as operand
-    const int r = row0 + tid, tq = r < rows ? quotient(r, a.R) : 0, hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
+    const int rl = tid & (kRows - 1), r = row0 + rl, tq = r < rows ? quotient(r, a.R) : 0, hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
     int limit = 0;
-    if (tid < kSoftmaxThreads) {
-        limit = r < rows ? (a.causal ? max(0, len - a.Tq + tq + 1) : len) : 0;
+    if (tid < kSoftmaxThreads) limit = r < rows ? (a.causal ? max(0, len - a.Tq + tq + 1) : len) : 0;
+    if (tid < kRows) {
         const bool there = r < rows && !a.zero;
         const __nv_bfloat16* const src = a.io.q + (r < rows ? b * a.io.qb + hq * a.io.qh + tq * a.io.qt : 0);
         float total[G];
@@ -172,66 +180,73 @@ cache_attention_rows_kernel(RowsArgs k) {
     tc_fence_after();
     const uint32_t tmem = *tmem_slot, tmem_z = tmem, tmem_c = tmem + 4 * kTokens, tmem_o = tmem_c + kTokens;
 
-    if (warp < 4) {
-        // ------------------------------------------------------------------ softmax: a thread a row
+    if (tid < kSoftmaxThreads) {
+        // ------------------------------------------------------------------ softmax: two threads a row, 32 tokens each
         const unsigned long long lim = k.limit_of(kRoleSoftmax);
-        const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        constexpr int kHalf = kTokens / 2;
+        const int half = warp >> 2;
         float top = kNoLogit, sum = 0.f;                   // in powers of two
         bool ok = true;
         for (int i = 0; i < n; ++i) {
-            const int token0 = (t0 + i) * kTokens;
-            const float* const scale = reinterpret_cast<const float*>(smem + S::kStage + (i & 1) * S::kStageBytes + S::kS);
+            const int token0 = (t0 + i) * kTokens + half * kHalf;
+            const float* const scale = reinterpret_cast<const float*>(smem + S::kStage + (i & 1) * S::kStageBytes + S::kS) + half * kHalf;
             ok = __all_sync(0xffffffffu, mbar_wait(bar_s, i & 1, abort_flag, lim));
-            if (!ok) break;
             tc_fence_after();
-            float z[kTokens];
+            float z[kHalf];
 #pragma unroll
-            for (int c = 0; c < kTokens / 16; ++c) {
-                uint32_t x[G + 1][16];
-                tmem_ld16(tmem_c + lanes + 16 * c, x[G]);
+            for (int c = 0; c < kHalf / 8; ++c) {
+                uint32_t x[G + 1][8];
+                tmem_ld8_issue(tmem_c + lanes + half * kHalf + 8 * c, x[G]);
 #pragma unroll
-                for (int g = 0; g < G; ++g) tmem_ld16(tmem_z + lanes + g * kTokens + 16 * c, x[g]);
+                for (int g = 0; g < G; ++g) tmem_ld8_issue(tmem_z + lanes + g * kTokens + half * kHalf + 8 * c, x[g]);
                 tmem_wait_ld(x);
 #pragma unroll
-                for (int e = 0; e < 16; e += 4) {
+                for (int e = 0; e < 8; e += 4) {
                     f32x2 lo = pack2(__uint_as_float(x[G][e]), __uint_as_float(x[G][e + 1])), hi = pack2(__uint_as_float(x[G][e + 2]), __uint_as_float(x[G][e + 3]));
 #pragma unroll
                     for (int g = 0; g < G; ++g) {
-                        const float4 f = *reinterpret_cast<const float4*>(scale + g * kTokens + 16 * c + e);
+                        const float4 f = *reinterpret_cast<const float4*>(scale + g * kTokens + 8 * c + e);
                         lo = fma2(pack2(__uint_as_float(x[g][e]), __uint_as_float(x[g][e + 1])), pack2(f.x, f.y), lo);
                         hi = fma2(pack2(__uint_as_float(x[g][e + 2]), __uint_as_float(x[g][e + 3])), pack2(f.z, f.w), hi);
                     }
                     const float2 u = unpack2(lo), v = unpack2(hi);
-                    z[16 * c + e] = u.x;
-                    z[16 * c + e + 1] = u.y;
-                    z[16 * c + e + 2] = v.x;
-                    z[16 * c + e + 3] = v.y;
+                    z[8 * c + e] = u.x;
+                    z[8 * c + e + 1] = u.y;
+                    z[8 * c + e + 2] = v.x;
+                    z[8 * c + e + 3] = v.y;
                 }
             }
             tc_fence_before();
             mbar_arrive(bar_read);
-            if (token0 + kTokens > least) {
+            if (token0 + kHalf > least) {
                 const int seen = limit - token0;
 #pragma unroll
-                for (int e = 0; e < kTokens; ++e)
+                for (int e = 0; e < kHalf; ++e)
                     if (e >= seen) z[e] = MINUS_INF;
             }
             float high = z[0];
 #pragma unroll
-            for (int e = 1; e < kTokens; ++e) high = fmaxf(high, z[e]);
+            for (int e = 1; e < kHalf; ++e) high = fmaxf(high, z[e]);
             high *= a.scale_log2;
-            if (i > 0) {                                   // the product behind has read the weights, and its sums stand still
-                ok = __all_sync(0xffffffffu, mbar_wait(bar_pv, (i - 1) & 1, abort_flag, lim));
-                if (!ok) break;
-                tc_fence_after();
+            if (high - top > 8.f) moved[i % 3] = 1;
+            if (tid == 0) moved[(i + 1) % 3] = 0;          // (read last two barriers ago)
+            // the product behind has read the weights, and its sums stand still
+            if (i > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar_pv, (i - 1) & 1, abort_flag, lim)) && ok;
+            tc_fence_after();
+            if (epi_bar_or<kSoftmaxThreads>(!ok)) {
+                ok = false;
+                break;
             }
-            if (__any_sync(0xffffffffu, high - top > 8.f)) {
-                const float now = fmaxf(top, high), keep = ex2_approx(top - now);
+            if (moved[i % 3]) {                            // (the same for all)
+                pairs[half * kRows + rl] = high;
+                epi_bar_sync<kSoftmaxThreads>();
+                const float now = fmaxf(top, fmaxf(high, pairs[(half ^ 1) * kRows + rl])), keep = ex2_approx(top - now);
                 top = now;
                 sum *= keep;
                 if (i > 0) {
 #pragma unroll 1
-                    for (int c = 0; c < G; ++c) {
+                    for (int c = half * (G / 2); c < (half + 1) * (G / 2); ++c) {
                         float v[32];
                         tmem_ld32(tmem_o + lanes + 32 * c, v);
 #pragma unroll
@@ -240,17 +255,19 @@ cache_attention_rows_kernel(RowsArgs k) {
                     }
                 }
             }
+            float more = 0.f;
 #pragma unroll
-            for (int c = 0; c < kTokens / 8; ++c) {
+            for (int c = 0; c < kHalf / 8; ++c) {
                 uint32_t w[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float p0 = ex2_approx(fmaf(z[8 * c + 2 * e], a.scale_log2, -top)), p1 = ex2_approx(fmaf(z[8 * c + 2 * e + 1], a.scale_log2, -top));
-                    sum += p0 + p1;
+                    if (e & 1) more += p0 + p1; else sum += p0 + p1;
                     w[e] = bf16x2(p0, p1);
                 }
-                *reinterpret_cast<uint4*>(smem + S::kP + at_swizzled(tid, c)) = make_uint4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<uint4*>(smem + S::kP + at_swizzled(rl, half * 4 + c)) = make_uint4(w[0], w[1], w[2], w[3]);
             }
+            sum += more;
             fence_async_proxy();
             tc_fence_before();
             mbar_arrive(bar_p);
@@ -259,12 +276,14 @@ cache_attention_rows_kernel(RowsArgs k) {
             ok = __all_sync(0xffffffffu, mbar_wait(bar_pv, (n - 1) & 1, abort_flag, lim));
             tc_fence_after();
         }
-        if (ok) {
+        pairs[half * kRows + rl] = sum;
+        if (!epi_bar_or<kSoftmaxThreads>(!ok)) {
+            sum += pairs[(half ^ 1) * kRows + rl];
             const bool none = sum == 0.f, alone = k.splits == 1;
             const float inv = alone ? (none ? 0.f : 1.f / sum) : 1.f;
             float* const part = a.part + (size_t)blockIdx.x * kRows * (D + 2);
 #pragma unroll 1
-            for (int c = 0; c < G; ++c) {
+            for (int c = half * (G / 2); c < (half + 1) * (G / 2); ++c) {
                 float v[32];
                 if (n > 0) {
                     tmem_ld32(tmem_o + lanes + 32 * c, v);
@@ -283,20 +302,20 @@ cache_attention_rows_kernel(RowsArgs k) {
                             *reinterpret_cast<uint2*>(a.io.out + b * a.io.ob + hq * a.io.oh + tq * a.io.ot + c * 32 + 4 * g) =
                                 make_uint2(bf16x2(o.x, o.y), bf16x2(o.z, o.w));
                         else
-                            *reinterpret_cast<float4*>(part + tid * D + c * 32 + 4 * g) = o;
+                            *reinterpret_cast<float4*>(part + rl * D + c * 32 + 4 * g) = o;
                     }
                 }
             }
-            if (r < rows) {
+            if (r < rows && half == 0) {
                 if (!alone) {
-                    part[kRows * D + tid] = top;
-                    part[kRows * D + kRows + tid] = sum;
+                    part[kRows * D + rl] = top;
+                    part[kRows * D + kRows + rl] = sum;
                 } else if (a.lse) {
                     a.lse[((int64_t)b * a.Hq + hq) * a.Tq + tq] = none ? MINUS_INF : (top + __log2f(sum)) * kLn2;
                 }
             }
         }
-    } else if (warp < 8) {
+    } else if (tid < kSoftmaxThreads + kUnpackThreads) {
         // ------------------------------------------------------------------ unpack
         const unsigned long long lim = k.limit_of(kRoleUnpack);
         const int u = tid - kSoftmaxThreads, blocks = (len + kCacheBlock - 1) / kCacheBlock;
@@ -320,72 +339,58 @@ cache_attention_rows_kernel(RowsArgs k) {
             const uint8_t* const raw = smem + S::kRaw + (i & 1) * S::kRawBytes;
             uint8_t* const stage = smem + S::kStage + (i & 1) * S::kStageBytes;
             const int token0 = (t0 + i) * kTokens;
-            // K: a thread a quarter of a token's row, twice
-#pragma unroll
-            for (int v = 0; v < 2; ++v) {
-                const int id = u + v * kUnpackThreads, row = id >> 2, t = id & 3;
+            {   // K: a thread a quarter of a token's row
+                const int row = u >> 2, t = u & 3, rb = row & 31;
                 const uint8_t* const block = raw + (row >> 5) * L::kBytes;
-                const int rb = row & 31;
                 uint32_t w[G];
-                if constexpr (G == 4) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(block + L::kKCodes + rb * (D / 2) + t * 16);
-                    w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
-                } else {
-                    const uint2 x = *reinterpret_cast<const uint2*>(block + L::kKCodes + rb * (D / 2) + t * 8);
-                    w[0] = x.x; w[1] = x.y;
-                }
+                words<G>(w, block + L::kKCodes + rb * (D / 2) + t * 4 * G);
 #pragma unroll
                 for (int g = 0; g < G; ++g)
                     *reinterpret_cast<uint4*>(stage + S::kK + (g / 2) * 8192 + at_swizzled(row, (g & 1) * 4 + t)) =
                         make_uint4(centred(code_pair(w[g])), centred(code_pair(w[g] >> 4)), centred(code_pair(w[g] >> 8)), centred(code_pair(w[g] >> 12)));
             }
-            if (u < kTokens) {                             // centres three times over, scales
-                const uint8_t* const block = raw + (u >> 5) * L::kBytes;
-                const int rb = u & 31;
-                uint32_t m[2] = {}, s[2] = {};
-#pragma unroll
-                for (int e = 0; e < G / 2; ++e) {
-                    m[e] = *reinterpret_cast<const uint32_t*>(block + L::kKCentre + rb * 2 * G + 4 * e);
-                    s[e] = *reinterpret_cast<const uint32_t*>(block + L::kKScale + rb * 2 * G + 4 * e);
-                }
-                *reinterpret_cast<uint4*>(stage + S::kC + at_swizzled(u, 0)) = G == 4 ? make_uint4(m[0], m[1], m[0], m[1]) : make_uint4(m[0], m[0], m[0], 0u);
-                *reinterpret_cast<uint4*>(stage + S::kC + at_swizzled(u, 1)) = G == 4 ? make_uint4(m[0], m[1], 0u, 0u) : make_uint4(0u, 0u, 0u, 0u);
-                float* const f = reinterpret_cast<float*>(stage + S::kS) + u;
-#pragma unroll
-                for (int g = 0; g < G; ++g) f[g * kTokens] = g & 1 ? bf16hi(s[g / 2]) : bf16lo(s[g / 2]);
-            }
-            // V: a thread four elements of each group of two tokens, twice
-#pragma unroll
-            for (int v = 0; v < 2; ++v) {
-                const int id = u + v * kUnpackThreads, g8 = id & 7, pair = id >> 3, there = len - token0 - 2 * pair;
+            {   // V: a thread four elements of each group of two tokens
+                const int g8 = u & 7, pair = u >> 3, there = len - token0 - 2 * pair, rb = 2 * (pair & 15);
                 const uint8_t* const block = raw + (pair >> 4) * L::kBytes;
-                const int rb = 2 * (pair & 15);
                 const uint32_t keep = (there > 0 ? 0x0000FFFFu : 0u) | (there > 1 ? 0xFFFF0000u : 0u);
+                uint32_t x0[G / 2], x1[G / 2], s[G];       // (scales of two tokens)
+                words<G / 2>(x0, block + L::kVCodes + rb * (D / 2) + g8 * 2 * G);
+                words<G / 2>(x1, block + L::kVCodes + (rb + 1) * (D / 2) + g8 * 2 * G);
+                words<G>(s, block + L::kVScale + rb * 2 * G);
+                uint8_t* const to = stage + S::kV + at_swizzled(g8, pair >> 2) + (pair & 3) * 4;     // (rows 8 apart are 1024 bytes apart)
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
-                    const uint32_t x = (uint32_t)*reinterpret_cast<const uint16_t*>(block + L::kVCodes + rb * (D / 2) + g8 * 2 * G + 2 * g) |
-                                       (uint32_t)*reinterpret_cast<const uint16_t*>(block + L::kVCodes + (rb + 1) * (D / 2) + g8 * 2 * G + 2 * g) << 16;
-                    uint32_t s = (uint32_t)*reinterpret_cast<const uint16_t*>(block + L::kVScale + (rb * G + g) * 2) |
-                                 (uint32_t)*reinterpret_cast<const uint16_t*>(block + L::kVScale + ((rb + 1) * G + g) * 2) << 16;
+                    const uint32_t pick = g & 1 ? 0x7632u : 0x5410u, x = __byte_perm(x0[g / 2], x1[g / 2], pick), f = __byte_perm(s[g / 2], s[(G + g) / 2], pick);
                     const uint32_t m = *reinterpret_cast<const uint32_t*>(block + L::kVCentre + (g * 32 + rb) * 2);
                     // what is no number would reach rows that do not see it: it is a zero here, and those that do see it are told
                     uint32_t fine = keep;
-                    if ((s & 0x7FFFu) > 0x7F80u) {
+                    if ((f & 0x7FFFu) > 0x7F80u) {
                         fine &= 0xFFFF0000u;
                         if (there > 0 && g8 == 0) atomicMin(first_bad + g, token0 + 2 * pair);
                     }
-                    if ((s >> 16 & 0x7FFFu) > 0x7F80u) {
+                    if ((f >> 16 & 0x7FFFu) > 0x7F80u) {
                         fine &= 0x0000FFFFu;
                         if (there > 1 && g8 == 0) atomicMin(first_bad + g, token0 + 2 * pair + 1);
                     }
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         uint32_t y;
-                        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(y) : "r"(centred(code_pair(x >> (4 * e)))), "r"(s), "r"(m));
-                        const int row = g * 32 + 8 * e + g8;
-                        *reinterpret_cast<uint32_t*>(stage + S::kV + at_swizzled(row, pair >> 2) + (pair & 3) * 4) = y & fine;
+                        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(y) : "r"(centred(code_pair(x >> (4 * e)))), "r"(f), "r"(m));
+                        *reinterpret_cast<uint32_t*>(to + (g * 4 + e) * 1024) = y & fine;
                     }
                 }
+            }
+            if (u < kTokens) {                             // centres three times over, scales
+                const uint8_t* const block = raw + (u >> 5) * L::kBytes;
+                const int rb = u & 31;
+                uint32_t m[G / 2], s[G / 2];
+                words<G / 2>(m, block + L::kKCentre + rb * 2 * G);
+                words<G / 2>(s, block + L::kKScale + rb * 2 * G);
+                *reinterpret_cast<uint4*>(stage + S::kC + at_swizzled(u, 0)) = G == 4 ? make_uint4(m[0], m[G / 2 - 1], m[0], m[G / 2 - 1]) : make_uint4(m[0], m[0], m[0], 0u);
+                *reinterpret_cast<uint4*>(stage + S::kC + at_swizzled(u, 1)) = G == 4 ? make_uint4(m[0], m[G / 2 - 1], 0u, 0u) : make_uint4(0u, 0u, 0u, 0u);
+                float* const f = reinterpret_cast<float*>(stage + S::kS) + u;
+#pragma unroll
+                for (int g = 0; g < G; ++g) f[g * kTokens] = g & 1 ? bf16hi(s[g / 2]) : bf16lo(s[g / 2]);
             }
             fence_async_proxy();
             mbar_arrive(bar_full + 8 * (i & 1));
@@ -435,7 +440,7 @@ cache_attention_rows_kernel(RowsArgs k) {
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 8) {
+    if (warp == kThreads / 32 - 1) {
         tc_fence_after();
         tmem_dealloc(tmem, kTmem);
     }
