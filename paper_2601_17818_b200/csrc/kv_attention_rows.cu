@@ -16,7 +16,8 @@ namespace vitcop {
 namespace {
 
 constexpr int kRows = 128, kTokens = 64;
-constexpr int kSoftmaxThreads = 256, kUnpackThreads = 256, kThreads = kSoftmaxThreads + kUnpackThreads + 32;
+constexpr int kSoftmaxThreads = 256, kUnpackThreads = 256, kThreads = kSoftmaxThreads + kUnpackThreads + 64;
+constexpr int kStages = 3;
 constexpr uint32_t kTmem = 512;
 enum { kRoleUnpack = 1, kRoleMma = 2, kRoleSoftmax = 4 };
 
@@ -26,13 +27,13 @@ struct RowsSmem {
     static constexpr int kQ = 0;                                       // [D / 64][128 rows][128 bytes]
     static constexpr int kSums = kQ + kSubs * 16384;                   // [128 rows][128 bytes], 32 of which are used
     static constexpr int kP = kSums + 16384;                           // [128 rows][64 tokens]
-    static constexpr int kStage = kP + 16384;                          // two of them:
+    static constexpr int kStage = kP + 16384;                          // kStages of them:
     static constexpr int kK = 0;                                       //   [D / 64][64 tokens][128 bytes]
     static constexpr int kV = kK + kSubs * 8192;                       //   [D elements][64 tokens]
     static constexpr int kC = kV + D * 128;                            //   [64 tokens][128 bytes]
     static constexpr int kS = kC + 8192;                               //   fp32 [G][64 tokens]
     static constexpr int kStageBytes = kS + 1024;
-    static constexpr int kRaw = kStage + 2 * kStageBytes;              // two tiles as they lie in the cache
+    static constexpr int kRaw = kStage + kStages * kStageBytes;              // two tiles as they lie in the cache
     static constexpr int kRawBytes = 2 * CacheBlock<D>::kBytes;
     static constexpr int kBars = kRaw + 2 * kRawBytes;
     static constexpr int kPairs = kBars + 256;                         // fp32 [2][128 rows]: what the two threads of a row tell each other
@@ -59,6 +60,17 @@ __device__ __forceinline__ bool unpack_bar_or(bool pred) {     // the same answe
     return out != 0;
 }
 
+// As tc_mma_bf16 and tc_commit, called by a warp of which one lane issues.
+__device__ __forceinline__ void mma_elected(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void commit_elected(uint32_t bar) {
+    asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
+                 ::"r"(bar) : "memory");
+}
 template <int N>
 __device__ __forceinline__ void words(uint32_t (&w)[N], const uint8_t* p) {
     if constexpr (N == 4) {
@@ -101,16 +113,16 @@ cache_attention_rows_kernel(RowsArgs k) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const uint32_t base = smem_u32(smem);
-    const uint32_t bar_full = base + S::kBars, bar_empty = bar_full + 16, bar_s = bar_full + 32, bar_read = bar_full + 40, bar_p = bar_full + 48,
-                   bar_pv = bar_full + 56, bar_drain = bar_full + 64;
-    volatile int* const abort_flag = reinterpret_cast<volatile int*>(smem + S::kBars + 72);
-    uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + S::kBars + 76);
-    int* const moved = reinterpret_cast<int*>(smem + S::kBars + 112);           // [3] a row's maximum has to move, tile by tile
+    const uint32_t bar_full = base + S::kBars, bar_empty = bar_full + 8 * kStages, bar_s = bar_empty + 8 * kStages, bar_read = bar_s + 8, bar_p = bar_s + 16,
+                   bar_pv = bar_s + 24, bar_drain = bar_s + 32, bar_q = bar_s + 48;     // (two drains)
+    volatile int* const abort_flag = reinterpret_cast<volatile int*>(smem + S::kBars + 128);
+    uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + S::kBars + 132);
+    int* const moved = reinterpret_cast<int*>(smem + S::kBars + 160);          // [3] a row's maximum has to move, tile by tile
     float* const pairs = reinterpret_cast<float*>(smem + S::kPairs);
-    int* const first_bad = reinterpret_cast<int*>(smem + S::kBars + 96);        // [G] first token whose values of V are no numbers
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int* const first_bad = reinterpret_cast<int*>(smem + S::kBars + 144);       // [G] first token whose values of V are no numbers
+    const int tid = threadIdx.x, warp = tid >> 5;
     if (tid == 0) {
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kStages; ++i) {
             mbar_init(bar_full + 8 * i, kUnpackThreads);
             mbar_init(bar_empty + 8 * i, 1);
         }
@@ -119,12 +131,18 @@ cache_attention_rows_kernel(RowsArgs k) {
         mbar_init(bar_p, kSoftmaxThreads);
         mbar_init(bar_pv, 1);
         mbar_init(bar_drain, 1);
+        mbar_init(bar_drain + 8, 1);
+        mbar_init(bar_q, kRows);
         *abort_flag = 0;
         moved[0] = moved[1] = moved[2] = 0;
         for (int i = 0; i < G; ++i) first_bad[i] = 0x7fffffff;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kThreads / 32 - 1) tmem_alloc(smem_u32(tmem_slot), kTmem);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0), tmem_z = tmem, tmem_c = tmem + 4 * kTokens, tmem_o = tmem_c + kTokens;
     grid_dependency_wait();
     grid_dependency_launch_dependents();                   // (the join's CTAs, which wait for this grid to end)
 
@@ -174,11 +192,8 @@ cache_attention_rows_kernel(RowsArgs k) {
         *reinterpret_cast<uint4*>(smem + S::kSums + at_swizzled(tid, 1)) =
             make_uint4(bf16x2(part[8], part[9]), bf16x2(part[10], part[11]), bf16x2(part[12], part[13]), bf16x2(part[14], part[15]));
         fence_async_proxy();
+        mbar_arrive(bar_q);
     }
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    const uint32_t tmem = *tmem_slot, tmem_z = tmem, tmem_c = tmem + 4 * kTokens, tmem_o = tmem_c + kTokens;
 
     if (tid < kSoftmaxThreads) {
         // ------------------------------------------------------------------ softmax: two threads a row, 32 tokens each
@@ -190,7 +205,7 @@ cache_attention_rows_kernel(RowsArgs k) {
         bool ok = true;
         for (int i = 0; i < n; ++i) {
             const int token0 = (t0 + i) * kTokens + half * kHalf;
-            const float* const scale = reinterpret_cast<const float*>(smem + S::kStage + (i & 1) * S::kStageBytes + S::kS) + half * kHalf;
+            const float* const scale = reinterpret_cast<const float*>(smem + S::kStage + i % kStages * S::kStageBytes + S::kS) + half * kHalf;
             ok = __all_sync(0xffffffffu, mbar_wait(bar_s, i & 1, abort_flag, lim));
             tc_fence_after();
             float z[kHalf];
@@ -282,6 +297,9 @@ cache_attention_rows_kernel(RowsArgs k) {
             const bool none = sum == 0.f, alone = k.splits == 1;
             const float inv = alone ? (none ? 0.f : 1.f / sum) : 1.f;
             float* const part = a.part + (size_t)blockIdx.x * kRows * (D + 2);
+            // (32 rows by 32 elements a warp, turned in shared memory that the tiles have left: 8 lanes then write a row)
+            float* const turn = reinterpret_cast<float*>(smem + S::kStage) + warp * 32 * 36;
+            const int lane = tid & 31;
 #pragma unroll 1
             for (int c = half * (G / 2); c < (half + 1) * (G / 2); ++c) {
                 float v[32];
@@ -292,19 +310,25 @@ cache_attention_rows_kernel(RowsArgs k) {
                     for (int e = 0; e < 32; ++e) v[e] = 0.f;
                 }
                 const bool bad = first_bad[c] < limit;     // a row of V that is no number, and that this query sees
-                // (column 8 i + g of a group is its element 4 g + i)
-                if (r < rows) {
+                const float times = bad ? __int_as_float(0x7fc00000) : inv;
 #pragma unroll
-                    for (int g = 0; g < 8; ++g) {
-                        const float nan = __int_as_float(0x7fc00000);
-                        const float4 o = bad ? make_float4(nan, nan, nan, nan) : make_float4(v[g] * inv, v[8 + g] * inv, v[16 + g] * inv, v[24 + g] * inv);
-                        if (alone)
-                            *reinterpret_cast<uint2*>(a.io.out + b * a.io.ob + hq * a.io.oh + tq * a.io.ot + c * 32 + 4 * g) =
-                                make_uint2(bf16x2(o.x, o.y), bf16x2(o.z, o.w));
-                        else
-                            *reinterpret_cast<float4*>(part + rl * D + c * 32 + 4 * g) = o;
+                for (int g = 0; g < 8; ++g)                // (column 8 i + g of a group is its element 4 g + i)
+                    *reinterpret_cast<float4*>(turn + lane * 36 + 4 * g) = make_float4(v[g] * times, v[8 + g] * times, v[16 + g] * times, v[24 + g] * times);
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int row = (warp & 3) * 32 + 4 * j + (lane >> 3), q = row0 + row;
+                    const float4 o = *reinterpret_cast<const float4*>(turn + (4 * j + (lane >> 3)) * 36 + 4 * (lane & 7));
+                    if (q >= rows) continue;
+                    if (alone) {
+                        const int qt = quotient(q, a.R), qh = h * (int)a.R.d + (q - qt * (int)a.R.d);
+                        *reinterpret_cast<uint2*>(a.io.out + b * a.io.ob + qh * a.io.oh + qt * a.io.ot + c * 32 + 4 * (lane & 7)) =
+                            make_uint2(bf16x2(o.x, o.y), bf16x2(o.z, o.w));
+                    } else {
+                        *reinterpret_cast<float4*>(part + row * D + c * 32 + 4 * (lane & 7)) = o;
                     }
                 }
+                __syncwarp();
             }
             if (r < rows && half == 0) {
                 if (!alone) {
@@ -333,11 +357,11 @@ cache_attention_rows_kernel(RowsArgs k) {
         fetch(1);
         bool ok = true;
         for (int i = 0; i < n; ++i) {
-            if (i >= 2) ok = mbar_wait(bar_empty + 8 * (i & 1), ((i >> 1) - 1) & 1, abort_flag, lim);
+            if (i >= kStages) ok = mbar_wait(bar_empty + 8 * (i % kStages), (i / kStages - 1) & 1, abort_flag, lim);
             asm volatile("cp.async.wait_group 1;" ::: "memory");
             if (unpack_bar_or(!ok || *abort_flag)) break;
             const uint8_t* const raw = smem + S::kRaw + (i & 1) * S::kRawBytes;
-            uint8_t* const stage = smem + S::kStage + (i & 1) * S::kStageBytes;
+            uint8_t* const stage = smem + S::kStage + i % kStages * S::kStageBytes;
             const int token0 = (t0 + i) * kTokens;
             {   // K: a thread a quarter of a token's row
                 const int row = u >> 2, t = u & 3, rb = row & 31;
@@ -393,49 +417,60 @@ cache_attention_rows_kernel(RowsArgs k) {
                 for (int g = 0; g < G; ++g) f[g * kTokens] = g & 1 ? bf16hi(s[g / 2]) : bf16lo(s[g / 2]);
             }
             fence_async_proxy();
-            mbar_arrive(bar_full + 8 * (i & 1));
+            mbar_arrive(bar_full + 8 * (i % kStages));
             unpack_bar();                                  // (the raw tile has been read)
             fetch(i + 2);
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
-    } else if (lane == 0) {
-        // ------------------------------------------------------------------ products
+    } else if (warp == kThreads / 32 - 2) {
+        // ------------------------------------------------------------------ products with the queries
+        // (the whole warp walks, so that the operands' addresses are known to be the same in all lanes; one lane issues)
         const unsigned long long lim = k.limit_of(kRoleMma);
-        constexpr uint32_t idesc_z = umma_idesc_bf16(kRows, kTokens), idesc_o = umma_idesc_bf16(kRows, D);
-        bool ok = true;
-        for (int i = 0; ok && i <= n; ++i) {
-            if (i < n) {
-                ok = mbar_wait(bar_full + 8 * (i & 1), (i >> 1) & 1, abort_flag, lim) && (i == 0 || mbar_wait(bar_read, (i - 1) & 1, abort_flag, lim));
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t stage = base + S::kStage + (i & 1) * S::kStageBytes;
+        constexpr uint32_t idesc = umma_idesc_bf16(kRows, kTokens);
+        int at = 0, phase = 0;
+        const bool there = n > 0 && __all_sync(0xffffffffu, mbar_wait(bar_q, 0, abort_flag, lim));
+        for (int i = 0; there && i < n; ++i) {
+            const bool ok = mbar_wait(bar_full + 8 * at, phase, abort_flag, lim) && (i == 0 || mbar_wait(bar_read, (i - 1) & 1, abort_flag, lim));
+            if (!__all_sync(0xffffffffu, ok)) break;
+            tc_fence_after();
+            const uint32_t stage = base + S::kStage + at * S::kStageBytes;
 #pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    const uint64_t dq = umma_desc_k128(base + S::kQ + (g / 2) * 16384) + (uint64_t)((g & 1) * 4);
-                    const uint64_t dk = umma_desc_k128(stage + S::kK + (g / 2) * 8192) + (uint64_t)((g & 1) * 4);
-                    tc_mma_bf16(tmem_z + g * kTokens, dq, dk, idesc_z, 0);
-                    tc_mma_bf16(tmem_z + g * kTokens, dq + 2, dk + 2, idesc_z, 1);
-                }
-                tc_mma_bf16(tmem_c, umma_desc_k128(base + S::kSums), umma_desc_k128(stage + S::kC), idesc_z, 0);
-                tc_commit(bar_s);
+            for (int g = 0; g < G; ++g) {
+                const uint64_t dq = umma_desc_k128(base + S::kQ + (g / 2) * 16384) + (uint64_t)((g & 1) * 4);
+                const uint64_t dk = umma_desc_k128(stage + S::kK + (g / 2) * 8192) + (uint64_t)((g & 1) * 4);
+                mma_elected(tmem_z + g * kTokens, dq, dk, idesc, 0);
+                mma_elected(tmem_z + g * kTokens, dq + 2, dk + 2, idesc, 1);
             }
-            if (i > 0) {
-                ok = mbar_wait(bar_p, (i - 1) & 1, abort_flag, lim);
-                if (!ok) break;
-                tc_fence_after();
-                const uint64_t dp = umma_desc_k128(base + S::kP), dv = umma_desc_k128(base + S::kStage + ((i - 1) & 1) * S::kStageBytes + S::kV);
-#pragma unroll
-                for (int e = 0; e < kTokens / 16; ++e) tc_mma_bf16(tmem_o, dp + 2 * e, dv + 2 * e, idesc_o, i > 1 || e > 0 ? 1u : 0u);
-                tc_commit(bar_empty + 8 * ((i - 1) & 1));
-                tc_commit(bar_pv);
+            mma_elected(tmem_c, umma_desc_k128(base + S::kSums), umma_desc_k128(stage + S::kC), idesc, 0);
+            commit_elected(bar_s);
+            if (++at == kStages) {
+                at = 0;
+                phase ^= 1;
             }
         }
-        tc_commit(bar_drain);                              // (waited for below)
+        commit_elected(bar_drain);                         // (waited for below)
+    } else {
+        // ------------------------------------------------------------------ products with the weights
+        const unsigned long long lim = k.limit_of(kRoleMma);
+        constexpr uint32_t idesc = umma_idesc_bf16(kRows, D);
+        int at = 0;
+        for (int i = 0; i < n; ++i) {
+            if (!__all_sync(0xffffffffu, mbar_wait(bar_p, i & 1, abort_flag, lim))) break;
+            tc_fence_after();
+            const uint64_t dp = umma_desc_k128(base + S::kP), dv = umma_desc_k128(base + S::kStage + at * S::kStageBytes + S::kV);
+#pragma unroll
+            for (int e = 0; e < kTokens / 16; ++e) mma_elected(tmem_o, dp + 2 * e, dv + 2 * e, idesc, i > 0 || e > 0 ? 1u : 0u);
+            commit_elected(bar_pv);
+            commit_elected(bar_empty + 8 * at);
+            if (++at == kStages) at = 0;
+        }
+        commit_elected(bar_drain + 8);
     }
     __syncthreads();
     // Another role may have given up behind the last product: operands and tensor memory stay until all of them have completed.
     if (tid == kSoftmaxThreads + kUnpackThreads) {
         mbar_drain(bar_drain, 0);
+        mbar_drain(bar_drain + 8, 0);
         k.reports[blockIdx.x] = *abort_flag ? 1 : 0;
     }
     tc_fence_before();
