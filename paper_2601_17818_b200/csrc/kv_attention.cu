@@ -701,14 +701,14 @@ int sm_count() {
 
 size_t cache_attention_workspace_bytes(int B, int H, int Ncap, int d, int Tq, int Hq) {
     if (B < 1 || H < 1 || Hq < 1 || Tq < 1) return kStatusBytes;
-    if (rows_kernel_takes((int64_t)Hq / H * Tq, d)) return rows_workspace_bytes(B, H, Ncap, d, Tq, Hq);
+    if (rows_kernel_takes(B, H, Ncap, (int64_t)Hq / H * Tq, d)) return rows_workspace_bytes(B, H, Ncap, d, Tq, Hq);
     const Plan p = plan_of(B, H, Ncap, d, Tq, Hq, sm_count());
     return kStatusBytes + part_bytes(p, d);
 }
 
 int launch_cache_attention(const CacheQueries& io, const void* cache, int B, int Hq, int H, int Tq, int d, int Ncap,
                            const int32_t* cache_len, float scale, bool causal, float* lse, void* workspace, cudaStream_t stream) {
-    const bool many = rows_kernel_takes((int64_t)Hq / H * Tq, d);
+    const bool many = rows_kernel_takes(B, H, Ncap, (int64_t)Hq / H * Tq, d);
     const Plan p = plan_of(B, H, Ncap, d, Tq, Hq, sm_count());
     if ((int64_t)B * H * p.RT > 0x7fffffff || (int64_t)Hq / H * Tq > 0x7fffffff - 64) return VITCOP_ERR_UNSUPPORTED;
     AttArgs a;

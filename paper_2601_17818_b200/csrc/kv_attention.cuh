@@ -56,7 +56,7 @@ __device__ __forceinline__ uint32_t centred(uint32_t pair) {                    
 #endif
 
 // The kernel for many query rows (tcgen05): 128 rows of a head a CTA.
-bool rows_kernel_takes(int64_t rows, int d);
+bool rows_kernel_takes(int B, int H, int Ncap, int64_t rows, int d);
 size_t rows_workspace_bytes(int B, int H, int Ncap, int d, int Tq, int Hq);
 int launch_cache_attention_rows(const AttArgs& a, int d, void* workspace, cudaStream_t stream);
 

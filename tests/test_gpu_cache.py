@@ -5,7 +5,9 @@ Codes, scales and centres have to be the oracle's.  Values read back are its val
 the value; bf16 of an fp32 that was itself rounded: the same and 2^-23).  Attention:
   logits   fp32 sums of products in which a code stands as up to 271 / 2 + 136 and is brought back to its centre: every product and partial sum
            is off by at most 2^-20 of sum |q| (280 s + |m|) per group, all of them together by DELTA below
-  weights  enter the products in bf16 (2^-8), once with the scale (times code - 8) and once for the centre
+  weights  enter the products in bf16 (2^-8): those of the centres once, those of the codes once more with the scale; or, where
+           there are many query rows, the weights once and the values of V, as they are read back (2^-8).  Either way the part
+           that a row adds is off by at most 2^-8 (2 |code - 8| s + |m|) + 2^-8 (|code - 8| s + |m|), and the products of the two
   out      bf16 (2^-8), and the weights' own error, exp(2 delta) - 1
 """
 import numpy as np
@@ -194,7 +196,7 @@ def _bounds(q, K, V, lens, scale, causal):
     out, lse = oc.attention(q, Kv, Vv, lens, scale, causal)
     tol, ltol = np.zeros(out.shape), np.zeros(lse.shape)
     absq = np.abs(q).reshape(B, Hq, Tq, d // 32, 32).sum(-1)
-    rounded = (HALF * (np.abs(V[2] - 8) * V[0][..., None] + np.abs(V[1])[..., None])).reshape(B, H, N, d)
+    rounded = (HALF * (1 + HALF) * (2 * np.abs(V[2] - 8) * V[0][..., None] + 2 * np.abs(V[1])[..., None])).reshape(B, H, N, d)
     for b in range(B):
         n = int(min(max(lens[b], 0), N))
         for h in range(Hq):
@@ -288,6 +290,63 @@ def test_attention_over_long_and_ragged_caches(B, H, R, Tq, d, lens):
     _poison(cache, lens)
     out, lse = _attend(q, cache, lens, d ** -0.5)
     _check(q, cache, K, V, lens, d ** -0.5, True, out, lse)
+
+
+@pytest.mark.parametrize("B,H,R,Tq,d,Ncap,lens,causal", [
+    (3, 1, 8, 33, 128, 2688, [2688, 31, 0], True),          # pieces of two lengths, a sample that sees nothing, one with more queries than rows
+    (2, 1, 4, 33, 64, 8192, [8100, 65], True), (2, 2, 1, 40, 128, 12800, [129, 12799], False), (1, 1, 7, 19, 128, 16512, [16500], True),
+    (66, 4, 2, 64, 64, 64, [(7 * b) % 65 for b in range(66)], True),   # more heads than SMs: a CTA has all of one
+    (52, 3, 2, 70, 128, 96, [(11 * b) % 97 for b in range(52)], False)])
+def test_many_query_rows(B, H, R, Tq, d, Ncap, lens, causal):
+    q, cache, K, V = _problem(Tq + d, B, H, R, Tq, d, Ncap, lens, spread=1.5)
+    if B < 10:
+        _poison(cache, lens)
+    out, lse = _attend(q, cache, lens, d ** -0.5, causal)
+    _check(q, cache, K, V, lens, d ** -0.5, causal, out, lse)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_many_query_rows_and_rows_that_are_no_numbers(d):
+    """Values that are no numbers reach the queries that see them, in their group, and no others; keys all of those queries' output."""
+    rng = np.random.default_rng(d)
+    n, Tq, R, Ncap = 300, 48, 4, 11008
+    K, V = _bf16(rng, 1, 1, n, d), _bf16(rng, 1, 1, n, d)
+    V[0, 0, 290, 3], V[0, 0, 280, 40] = float("inf"), float("nan")
+    cache, lens = _cache(1, 1, Ncap, d), _i32([0])
+    vb.vitcop_cache_write(K, V, cache, lens)
+    q = _bf16(rng, 1, R, Tq, d)
+    out, lse = _attend(q, cache, [n], d ** -0.5)
+    first = n - Tq                                         # position of the first query
+    for t in range(Tq):
+        bad = [first + t >= 290, first + t >= 280]
+        for g in range(d // 32):
+            part = out[:, :, t, 32 * g:32 * g + 32]
+            assert torch.isnan(part).all() if g < 2 and bad[g] else torch.isfinite(part).all()
+    assert torch.isfinite(lse).all()
+    K[0, 0, 270, 5] = float("nan")
+    vb.vitcop_cache_write(K, _bf16(rng, 1, 1, n, d), cache, lens, cache_len=None)
+    out, lse = _attend(q, cache, [n], d ** -0.5)
+    seen = 270 - first
+    assert torch.isfinite(out[:, :, :seen]).all() and torch.isnan(out[:, :, seen:]).all()
+    assert torch.isfinite(lse[:, :, :seen]).all() and torch.isnan(lse[:, :, seen:]).all()
+
+
+@pytest.mark.parametrize("roles", [1, 2, 4])
+def test_many_query_rows_report_a_wait_that_ran_out(roles):
+    """One role of every CTA gives up at once, with products and copies of the others in flight; the next call is right again."""
+    B, H, R, Tq, d, Ncap = 1, 2, 8, 16, 128, 8192
+    q, cache, K, V = _problem(99, B, H, R, Tq, d, Ncap, [Ncap])
+    ws = vb.alloc_workspace(vb.OP_CACHE_ATTENTION, B=B, H=H, N=Ncap, d=d, Nv=Tq, D=H * R)
+    out = torch.zeros(B, H * R, Tq, d, dtype=torch.bfloat16, device=DEV)
+    try:
+        vb.vitcop_set_wait_limit(0, roles)
+        vb.vitcop_cache_attention(q, cache, _i32([Ncap]), out, ws, d ** -0.5)
+        assert vb.vitcop_poll_status(ws) == vb.ERR_TIMEOUT
+    finally:
+        vb.vitcop_set_wait_limit(0, 0)
+    out, lse = _attend(q, cache, [Ncap], d ** -0.5, ws=ws)
+    again, lse2 = _attend(q, cache, [Ncap], d ** -0.5)
+    assert torch.equal(out, again) and torch.equal(lse, lse2) and torch.isfinite(out).all()
 
 
 def test_attention_without_lengths_lse_or_strides_and_beyond_the_capacity():
