@@ -5,7 +5,8 @@
 //            128 + c (its nibble under the exponent of 128), exactly; per group the token's scale multiplies the product in fp32.
 //            The centres, and the scales times -136, are one more product each, with the groups' sums of q split into three bf16
 //   output   elements times query rows: (128 + c) - 136 = c - 8 is exact too.  The weights enter, transposed, as bf16(p) with the
-//            centres and as bf16(bf16(p) s) with a group's codes
+//            centres and as bf16(bf16(p) s) with a group's codes; what the output is divided by is the sum of the bf16(p) (rows of ones
+//            beside the centres), so that a row that takes nearly all is not off by its weight's rounding
 // A warp takes every fourth block of 32 tokens of its CTA's piece, with blocks ahead in shared memory (cp.async), and keeps maximum, sum
 // and output of its own; the CTA joins its warps, a second kernel joins the CTAs that shared a head.
 #include <type_traits>
@@ -18,6 +19,7 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kStages = 2;
+constexpr uint32_t kOnes = 0x3F803F80u;                    // 1, twice, in bf16
 constexpr int kWholeBlocks = 24;
 
 // Resident CTAs an SM, which the registers of the accumulators and the ring's memory leave room for.
@@ -144,7 +146,8 @@ cache_attention_kernel(AttArgs a) {
     float* const join = reinterpret_cast<float*>(smem + kWarps * kStages * L::kBytes);      // [warp][2 groups][8][lane]
     float* const join_max = join + kWarps * 512;                                            // [warp][NR]
     float* const join_sum = join_max + kWarps * NR;
-    QueryOperand<G>* const operand = reinterpret_cast<QueryOperand<G>*>(join_sum + kWarps * NR);      // [NT][lane]
+    float* const join_weight = join_sum + kWarps * NR;
+    QueryOperand<G>* const operand = reinterpret_cast<QueryOperand<G>*>(join_weight + kWarps * NR);      // [NT][lane]
     uint4* const queries = reinterpret_cast<uint4*>(operand + NT * 32);                                // [stage][NT][G][lane]
     Walk* const walks = reinterpret_cast<Walk*>(queries + kStages * NT * G * 32);                                   // [warp][2]
     int32_t* const stage_at = reinterpret_cast<int32_t*>(walks + kWarps * 2);                         // of warp 0
@@ -428,7 +431,7 @@ cache_attention_kernel(AttArgs a) {
                     c1 &= (there > 8 ? 0x0000FFFFu : 0u) | (there > 9 ? 0xFFFF0000u : 0u);
                 }
 #pragma unroll
-                for (int n = 0; n < NT; ++n) mma(oc[n], c0, 0u, c1, 0u, p[n][0], p[n][1]);
+                for (int n = 0; n < NT; ++n) mma(oc[n], c0, kOnes, c1, kOnes, p[n][0], p[n][1]);
 #pragma unroll
                 for (int i = 0; i < G; ++i) {
                     const uint32_t pick = i & 1 ? 0x7632u : 0x5410u;
@@ -481,16 +484,17 @@ cache_attention_kernel(AttArgs a) {
                 if (g == 0) {
                     join_max[warp * NR + n * 8 + 2 * t + e] = base[n][e];
                     join_sum[warp * NR + n * 8 + 2 * t + e] = sum[n][e];
+                    join_weight[warp * NR + n * 8 + 2 * t + e] = oc[n][2 + e];       // (rows 8 to 15 are all the sum of the weights)
                 }
             }
         now = *at_work;
         const bool whole = now.tile == 0 && count == now.blocks;
-        float* const part = SHARES && !whole ? a.part + (size_t)(2 * blockIdx.x + (now.tile == 0 ? 1 : 0)) * NR * (D + 2) : nullptr;
+        float* const part = SHARES && !whole ? a.part + (size_t)(2 * blockIdx.x + (now.tile == 0 ? 1 : 0)) * NR * (D + 3) : nullptr;
         const int je = warp & 1, ji = warp >> 1;           // this warp's share: group i0 + ji, rows n 8 + 2 t + je
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int rl = n * 8 + 2 * t + je, r = row0 + rl;
-            float f[kWarps], high = kNoLogit, total = 0.f;
+            float f[kWarps], high = kNoLogit, total = 0.f, weight = 0.f;
 #pragma unroll
             for (int i0 = 0; i0 < G; i0 += 2) {
 #pragma unroll
@@ -512,6 +516,7 @@ cache_attention_kernel(AttArgs a) {
                     for (int w = 0; w < kWarps; ++w) {
                         f[w] = ex2_approx(join_max[w * NR + rl] - high);
                         total = fmaf(join_sum[w * NR + rl], f[w], total);
+                        weight = fmaf(join_weight[w * NR + rl], f[w], weight);
                     }
                 }
                 float v[4] = {};
@@ -527,9 +532,10 @@ cache_attention_kernel(AttArgs a) {
                         if (i0 == 0 && ji == 0 && g == 0) {
                             part[NR * D + rl] = high;
                             part[NR * D + NR + rl] = total;
+                            part[NR * D + 2 * NR + rl] = weight;
                         }
                     } else {
-                        const float inv = none ? 0.f : 1.f / total;
+                        const float inv = none ? 0.f : 1.f / weight;
                         *reinterpret_cast<uint2*>(a.io.out + b * a.io.ob + hq * a.io.oh + tq * a.io.ot + (i0 + ji) * 32 + 4 * g) =
                             make_uint2(bf16x2(v[0] * inv, v[1] * inv), bf16x2(v[2] * inv, v[3] * inv));
                         if (i0 == 0 && ji == 0 && g == 0 && a.lse)
@@ -574,20 +580,21 @@ cache_attention_join_kernel(AttArgs a, int NR, Divisor rows, int items, int most
         if (n == 1) continue;                              // one CTA had it all, and wrote the result
         if (!waited) grid_dependency_wait();
         waited = true;
-        const size_t size = (size_t)NR * (D + 2);
+        const size_t size = (size_t)NR * (D + 3);
         const auto slot = [&](int c) { return a.part + (size_t)(2 * (c0 + c) + (c == 0 ? 1 : 0)) * size; };
-        float v[4] = {}, sum = 0.f, base = kNoLogit;
+        float v[4] = {}, sum = 0.f, weight = 0.f, base = kNoLogit;
         for (int first = 0; first < n; first += 32) {
             const int m = min(n - first, 32);
             float4 x[kJoinAhead];
 #pragma unroll
             for (int i = 0; i < kJoinAhead; ++i)
                 if (by + 4 * i < m) x[i] = *reinterpret_cast<const float4*>(slot(first + by + 4 * i) + rl * D + chunk * 32 + 4 * col);
-            float mine = kNoLogit, part = 0.f;
+            float mine = kNoLogit, part = 0.f, mass = 0.f;
             if (lane < m) {
                 const float* const p = slot(first + lane) + NR * D + rl;
                 mine = p[0];
                 part = p[NR];
+                mass = p[2 * NR];
             }
             float top = fmaxf(mine, base);
 #pragma unroll
@@ -595,6 +602,7 @@ cache_attention_join_kernel(AttArgs a, int NR, Divisor rows, int items, int most
             const float keep = ex2_approx(base - top), f = lane < m ? ex2_approx(mine - top) : 0.f;
             base = top;
             sum = fmaf(sum, keep, part * f);
+            weight = fmaf(weight, keep, mass * f);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] *= keep;
 #pragma unroll
@@ -609,7 +617,10 @@ cache_attention_join_kernel(AttArgs a, int NR, Divisor rows, int items, int most
             }
         }
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+        for (int off = 16; off > 0; off >>= 1) {
+            sum += __shfl_xor_sync(0xffffffffu, sum, off);
+            weight += __shfl_xor_sync(0xffffffffu, weight, off);
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             v[e] += __shfl_xor_sync(0xffffffffu, v[e], 8);
@@ -617,7 +628,7 @@ cache_attention_join_kernel(AttArgs a, int NR, Divisor rows, int items, int most
         }
         const int tq = quotient(r, a.R), hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
         const bool none = sum == 0.f;                      // (no row seen, an empty sample's among them)
-        const float inv = none ? 0.f : 1.f / sum;
+        const float inv = none ? 0.f : 1.f / weight;
         if (by == 0)
             *reinterpret_cast<uint2*>(a.io.out + b * a.io.ob + hq * a.io.oh + tq * a.io.ot + chunk * 32 + 4 * col) =
                 make_uint2(bf16x2(v[0] * inv, v[1] * inv), bf16x2(v[2] * inv, v[3] * inv));
@@ -649,11 +660,11 @@ Plan plan_of(int B, int H, int Ncap, int d, int Tq, int Hq, int sms) {
     return p;
 }
 
-size_t part_bytes(const Plan& p, int d) { return align_up((size_t)2 * p.ctas * 8 * p.NT * (d + 2) * sizeof(float), 256); }
+size_t part_bytes(const Plan& p, int d) { return align_up((size_t)2 * p.ctas * 8 * p.NT * (d + 3) * sizeof(float), 256); }
 
 template <int D, int NT>
 int launch(AttArgs a, const Plan& p, cudaStream_t stream) {
-    constexpr size_t kSmem = (size_t)kWarps * kStages * CacheBlock<D>::kBytes + kWarps * 2048 + 2 * kWarps * 8 * NT * 4 +
+    constexpr size_t kSmem = (size_t)kWarps * kStages * CacheBlock<D>::kBytes + kWarps * 2048 + 3 * kWarps * 8 * NT * 4 +
                              NT * 32 * sizeof(QueryOperand<D / 32>) + kStages * NT * (D / 32) * 512 + kWarps * 2 * sizeof(Walk);
     static DoneOnDevice done[2];
     const bool shares = p.ctas > 0;

@@ -30,7 +30,7 @@ struct AttArgs {
     const int32_t* cache_len;
     float* lse;
     int* status;
-    float* part;                                           // shares: two pieces a CTA, each [8 NT][D + 2]
+    float* part;                                           // shares: two pieces a CTA, each [8 NT][D], and maximum, sum and weight [8 NT]
     int B, Hq, H, Tq, Ncap, causal;
     Divisor R, RT;                                         // query heads of a stored one, tiles of rows
     float scale_log2;                                      // above 0: the sign is the queries'

@@ -29,8 +29,8 @@ struct RowsSmem {
     static constexpr int kP = kSums + 16384;                           // [128 rows][64 tokens]
     static constexpr int kStage = kP + 16384;                          // kStages of them:
     static constexpr int kK = 0;                                       //   [D / 64][64 tokens][128 bytes]
-    static constexpr int kV = kK + kSubs * 8192;                       //   [D elements][64 tokens]
-    static constexpr int kC = kV + D * 128;                            //   [64 tokens][128 bytes]
+    static constexpr int kV = kK + kSubs * 8192;                       //   [D elements, and 16 rows: ones and zeros][64 tokens]
+    static constexpr int kC = kV + (D + 16) * 128;                            //   [64 tokens][128 bytes]
     static constexpr int kS = kC + 8192;                               //   fp32 [G][64 tokens]
     static constexpr int kStageBytes = kS + 1024;
     static constexpr int kRaw = kStage + kStages * kStageBytes;              // two tiles as they lie in the cache
@@ -103,6 +103,11 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&v)[32]) 
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
 
+__device__ __forceinline__ void tmem_st1(uint32_t taddr, float v) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "r"(__float_as_uint(v)) : "memory");
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 cache_attention_rows_kernel(RowsArgs k) {
@@ -155,6 +160,12 @@ cache_attention_rows_kernel(RowsArgs k) {
     const int tiles = (most + kTokens - 1) / kTokens;
     const int each = tiles / k.splits, more = tiles - each * k.splits, t0 = split * each + min(split, more), n = each + (split < more ? 1 : 0);
     const uint8_t* const head = a.cache + ((int64_t)b * a.H + h) * (a.Ncap / kCacheBlock) * L::kBytes;
+
+    // the row of ones, whose product is the sum of the weights as they are rounded: what the output is divided by
+    if (tid >= kSoftmaxThreads && tid < kSoftmaxThreads + kUnpackThreads)
+        for (int i = tid - kSoftmaxThreads; i < kStages * 128; i += kUnpackThreads)
+            *reinterpret_cast<uint4*>(smem + S::kStage + (i >> 7) * S::kStageBytes + S::kV + D * 128 + (i & 127) * 16) =
+                (i & 127) < 8 ? make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u) : make_uint4(0, 0, 0, 0);
 
     // this thread's row as operand
     const int rl = tid & (kRows - 1), r = row0 + rl, tq = r < rows ? quotient(r, a.R) : 0, hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
@@ -268,6 +279,12 @@ cache_attention_rows_kernel(RowsArgs k) {
                         for (int e = 0; e < 32; ++e) v[e] *= keep;
                         tmem_st32(tmem_o + lanes + 32 * c, v);
                     }
+                    if (half == 0) {
+                        uint32_t w[1][8];
+                        tmem_ld8_issue(tmem_o + lanes + D, w[0]);
+                        tmem_wait_ld(w);
+                        tmem_st1(tmem_o + lanes + D, __uint_as_float(w[0][0]) * keep);
+                    }
                 }
             }
             float more = 0.f;
@@ -293,8 +310,13 @@ cache_attention_rows_kernel(RowsArgs k) {
             tc_fence_after();
             sum += pairs[(half ^ 1) * kRows + rl];
             const bool none = sum == 0.f, alone = k.splits == 1;
-            const float inv = alone ? (none ? 0.f : 1.f / sum) : 1.f;
-            float* const part = a.part + (size_t)blockIdx.x * kRows * (D + 2);
+            uint32_t weight[1][8] = {};
+            if (n > 0) {
+                tmem_ld8_issue(tmem_o + lanes + D, weight[0]);
+                tmem_wait_ld(weight);
+            }
+            const float inv = alone ? (none ? 0.f : 1.f / __uint_as_float(weight[0][0])) : 1.f;
+            float* const part = a.part + (size_t)blockIdx.x * kRows * (D + 3);
             // (32 rows by 32 elements a warp, turned in shared memory that the tiles have left: 8 lanes then write a row)
             float* const turn = reinterpret_cast<float*>(smem + S::kStage) + warp * 32 * 36;
             const int lane = tid & 31;
@@ -332,6 +354,7 @@ cache_attention_rows_kernel(RowsArgs k) {
                 if (!alone) {
                     part[kRows * D + rl] = top;
                     part[kRows * D + kRows + rl] = sum;
+                    part[kRows * D + 2 * kRows + rl] = __uint_as_float(weight[0][0]);
                 } else if (a.lse) {
                     a.lse[((int64_t)b * a.Hq + hq) * a.Tq + tq] = none ? MINUS_INF : (top + __log2f(sum)) * kLn2;
                 }
@@ -450,7 +473,7 @@ cache_attention_rows_kernel(RowsArgs k) {
     } else {
         // ------------------------------------------------------------------ products with the weights
         const unsigned long long lim = k.limit_of(kRoleMma);
-        constexpr uint32_t idesc = umma_idesc_bf16(kRows, D);
+        constexpr uint32_t idesc = umma_idesc_bf16(kRows, D + 16);
         int at = 0;
         for (int i = 0; i < n; ++i) {
             if (!__all_sync(0xffffffffu, mbar_wait(bar_p, i & 1, abort_flag, lim))) break;
@@ -499,14 +522,15 @@ cache_attention_rows_join_kernel(RowsArgs k, int ctas) {
         const int seg = item / kRows, rl = item - seg * kRows, b = seg / segs, hs = seg - b * segs, h = quotient(hs, a.RT);
         const int r = (hs - h * (int)a.RT.d) * kRows + rl;
         if (r >= rows) continue;
-        const float* const part = a.part + (size_t)seg * k.splits * kRows * (D + 2);
-        constexpr size_t kSize = (size_t)kRows * (D + 2);
-        float top = kNoLogit, sum = 0.f, v[E] = {};
+        const float* const part = a.part + (size_t)seg * k.splits * kRows * (D + 3);
+        constexpr size_t kSize = (size_t)kRows * (D + 3);
+        float top = kNoLogit, sum = 0.f, weight = 0.f, v[E] = {};
         for (int s = 0; s < k.splits; ++s) top = fmaxf(top, part[s * kSize + kRows * D + rl]);
         for (int s = 0; s < k.splits; ++s) {
             const float* const p = part + s * kSize;
             const float f = ex2_approx(p[kRows * D + rl] - top);
             sum = fmaf(p[kRows * D + kRows + rl], f, sum);
+            weight = fmaf(p[kRows * D + 2 * kRows + rl], f, weight);
 #pragma unroll
             for (int e = 0; e < E; e += 2) {
                 const float2 x = *reinterpret_cast<const float2*>(p + rl * D + lane * E + e);
@@ -516,7 +540,7 @@ cache_attention_rows_join_kernel(RowsArgs k, int ctas) {
         }
         const int tq = quotient(r, a.R), hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
         const bool none = sum == 0.f;
-        const float inv = none ? 0.f : 1.f / sum;
+        const float inv = none ? 0.f : 1.f / weight;
         uint32_t* const out = reinterpret_cast<uint32_t*>(a.io.out + b * a.io.ob + hq * a.io.oh + tq * a.io.ot + lane * E);
 #pragma unroll
         for (int e = 0; e < E; e += 2) out[e / 2] = bf16x2(v[e] * inv, v[e + 1] * inv);
@@ -578,7 +602,7 @@ bool rows_kernel_takes(int B, int H, int Ncap, int64_t rows, int d) {
 
 size_t rows_workspace_bytes(int B, int H, int Ncap, int d, int Tq, int Hq) {
     const RowsPlan p = plan_of(B, H, Ncap, Tq, Hq);
-    return kStatusBytes + reports_bytes(p) + (p.splits > 1 ? align_up((size_t)p.ctas * kRows * (d + 2) * sizeof(float), 256) : 0);
+    return kStatusBytes + reports_bytes(p) + (p.splits > 1 ? align_up((size_t)p.ctas * kRows * (d + 3) * sizeof(float), 256) : 0);
 }
 
 int launch_cache_attention_rows(const AttArgs& args, int d, void* workspace, cudaStream_t stream) {
