@@ -1,13 +1,16 @@
 // Attention over the cache in 4 bits for many query rows (a question, a chunk of a prompt): 128 rows of a head a CTA, tcgen05.
 //
-// Tokens come in tiles of 64.  Four warps turn a tile into operands: codes of K as the bf16 c - 8, exactly, codes of V as the bf16
-// nearest to the values they stand for, transposed.  With G = d / 32 groups of a row the logits are
+// Tokens come in tiles of 64.  Eight warps turn a tile into operands: codes of K as the bf16 c - 8, exactly, codes of V as the values
+// they stand for, transposed, in fp16 (three bits more than bf16 has) times a power of two that the largest scale and centre so far allow.  With G = d / 32 groups of a row the logits are
 //     z = sum over g of s_g (q_g . (c - 8)_g)  +  sum over g of m_g sum(q_g)
 // G products of their own (q as it is, bf16), whose fp32 sums the scales multiply behind tensor memory, and one more for the centres with
 // sum(q_g) split into three bf16.  Eight warps, two threads a row (32 tokens each), make the weights of the logits and write them back as
-// operand of the second product, which stays in tensor memory; a row's maximum is moved only when a logit has passed it by 2^8.
+// operand of the second product, which stays in tensor memory; a row's maximum is moved only when a logit has passed it by 2^8.  (Weights in fp16 too,
+// 2^-7 .. 2^15 at the top: the smallest that count are 2^-31 of the largest.)
 // Every operand is rows of 128 bytes in the 128-byte swizzle.  Waits are bounded: a CTA that gives up reports it, and the join,
 // which always follows, sets the status word.
+#include <cuda_fp16.h>
+
 #include "gram.cuh"
 #include "kv_attention.cuh"
 #include "tcgen05.cuh"
@@ -37,7 +40,8 @@ struct RowsSmem {
     static constexpr int kRawBytes = 2 * CacheBlock<D>::kBytes;
     static constexpr int kBars = kRaw + 2 * kRawBytes;
     static constexpr int kPairs = kBars + 256;                         // fp32 [2][128 rows]: what the two threads of a row tell each other
-    static constexpr int kBytes = kPairs + 1024 + 1024;                  // (and what aligning to 1024 takes)
+    static constexpr int kTable = kPairs + 1024;                       // fp16 [2][G][64 tokens]: scales and centres of V, times the power of two
+    static constexpr int kBytes = kTable + 1024 + 1024;                  // (and what aligning to 1024 takes)
 };
 
 struct RowsArgs {
@@ -70,6 +74,10 @@ __device__ __forceinline__ void mma_elected(uint32_t d_tmem, uint64_t a_desc, ui
 __device__ __forceinline__ void commit_elected(uint32_t bar) {
     asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
                  ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
 }
 template <int N>
 __device__ __forceinline__ void words(uint32_t (&w)[N], const uint8_t* p) {
@@ -123,6 +131,8 @@ cache_attention_rows_kernel(RowsArgs k) {
     volatile int* const abort_flag = reinterpret_cast<volatile int*>(smem + S::kBars + 128);
     uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + S::kBars + 132);
     int* const moved = reinterpret_cast<int*>(smem + S::kBars + 160);          // [3] a row's maximum has to move, tile by tile
+    uint32_t* const bounds = reinterpret_cast<uint32_t*>(smem + S::kBars + 192);     // [8] largest value of V that a warp has found possible
+    int* const exponents = reinterpret_cast<int*>(smem + S::kBars + 224);           // [kStages] of that power of two, as a float's bits have it
     float* const pairs = reinterpret_cast<float*>(smem + S::kPairs);
     int* const first_bad = reinterpret_cast<int*>(smem + S::kBars + 144);       // [G] first token whose values of V are no numbers
     const int tid = threadIdx.x, warp = tid >> 5;
@@ -165,7 +175,7 @@ cache_attention_rows_kernel(RowsArgs k) {
     if (tid >= kSoftmaxThreads && tid < kSoftmaxThreads + kUnpackThreads)
         for (int i = tid - kSoftmaxThreads; i < kStages * 128; i += kUnpackThreads)
             *reinterpret_cast<uint4*>(smem + S::kStage + (i >> 7) * S::kStageBytes + S::kV + D * 128 + (i & 127) * 16) =
-                (i & 127) < 8 ? make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u) : make_uint4(0, 0, 0, 0);
+                (i & 127) < 8 ? make_uint4(0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u) : make_uint4(0, 0, 0, 0);
 
     // this thread's row as operand
     const int rl = tid & (kRows - 1), r = row0 + rl, tq = r < rows ? quotient(r, a.R) : 0, hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
@@ -212,7 +222,8 @@ cache_attention_rows_kernel(RowsArgs k) {
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         constexpr int kHalf = kTokens / 2;
         const int half = warp >> 2;
-        float top = kNoLogit, sum = 0.f;                   // in powers of two
+        float top = kNoLogit, sum = 0.f;                   // in powers of two; weights are 2^(logit - top)
+        int exponent = 0;                                  // of V, as the sums have it
         bool ok = true;
         for (int i = 0; i < n; ++i) {
             const int token0 = (t0 + i) * kTokens + half * kHalf;
@@ -255,7 +266,7 @@ cache_attention_rows_kernel(RowsArgs k) {
 #pragma unroll
             for (int e = 1; e < kHalf; ++e) high = fmaxf(high, z[e]);
             high *= a.scale_log2;
-            if (high - top > 8.f) moved[i % 3] = 1;
+            if (high - top > 15.f) moved[i % 3] = 1;
             if (tid == 0) moved[(i + 1) % 3] = 0;          // (read last two barriers ago)
             // the product behind has read the weights, and its sums stand still (one warp asks, the others have the barrier)
             if (i > 0 && warp == 0) ok = mbar_wait(bar_pv, (i - 1) & 1, abort_flag, lim) && ok;
@@ -264,10 +275,12 @@ cache_attention_rows_kernel(RowsArgs k) {
                 break;
             }
             tc_fence_after();
-            if (moved[i % 3]) {                            // (the same for all)
+            const int next = exponents[i % kStages];
+            if (moved[i % 3] || (next != exponent && i > 0)) {         // (the same for all)
                 pairs[half * kRows + rl] = high;
                 epi_bar_sync<kSoftmaxThreads>();
-                const float now = fmaxf(top, fmaxf(high, pairs[(half ^ 1) * kRows + rl])), keep = ex2_approx(top - now);
+                const float now = fmaxf(top, fmaxf(high, pairs[(half ^ 1) * kRows + rl]) - 7.f), keep = ex2_approx(top - now);
+                const float less = keep * __int_as_float(max(0, 127 + exponent - next) << 23);
                 top = now;
                 sum *= keep;
                 if (i > 0) {
@@ -276,7 +289,7 @@ cache_attention_rows_kernel(RowsArgs k) {
                         float v[32];
                         tmem_ld32(tmem_o + lanes + 32 * c, v);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) v[e] *= keep;
+                        for (int e = 0; e < 32; ++e) v[e] *= less;
                         tmem_st32(tmem_o + lanes + 32 * c, v);
                     }
                     if (half == 0) {
@@ -287,6 +300,7 @@ cache_attention_rows_kernel(RowsArgs k) {
                     }
                 }
             }
+            exponent = next;
             float more = 0.f;
 #pragma unroll
             for (int c = 0; c < kHalf / 8; ++c) {
@@ -295,7 +309,7 @@ cache_attention_rows_kernel(RowsArgs k) {
                 for (int e = 0; e < 4; ++e) {
                     const float p0 = ex2_approx(fmaf(z[8 * c + 2 * e], a.scale_log2, -top)), p1 = ex2_approx(fmaf(z[8 * c + 2 * e + 1], a.scale_log2, -top));
                     if (e & 1) more += p0 + p1; else sum += p0 + p1;
-                    w[e] = bf16x2(p0, p1);
+                    w[e] = f16x2(p0, p1);
                 }
                 *reinterpret_cast<uint4*>(smem + S::kP + at_swizzled(rl, half * 4 + c)) = make_uint4(w[0], w[1], w[2], w[3]);
             }
@@ -315,7 +329,7 @@ cache_attention_rows_kernel(RowsArgs k) {
                 tmem_ld8_issue(tmem_o + lanes + D, weight[0]);
                 tmem_wait_ld(weight);
             }
-            const float inv = alone ? (none ? 0.f : 1.f / __uint_as_float(weight[0][0])) : 1.f;
+            const float inv = (alone ? (none ? 0.f : 1.f / __uint_as_float(weight[0][0])) : 1.f) * (n > 0 ? __int_as_float((exponent - 14) << 23) : 1.f);
             float* const part = a.part + (size_t)blockIdx.x * kRows * (D + 3);
             // (32 rows by 32 elements a warp, turned in shared memory that the tiles have left: 8 lanes then write a row)
             float* const turn = reinterpret_cast<float*>(smem + S::kStage) + warp * 32 * 36;
@@ -376,6 +390,8 @@ cache_attention_rows_kernel(RowsArgs k) {
         };
         fetch(0);
         fetch(1);
+        uint16_t* const table = reinterpret_cast<uint16_t*>(smem + S::kTable);
+        int exponent = 16;
         bool ok = true;
         for (int i = 0; i < n; ++i) {
             if (i >= kStages && u < 32) ok = mbar_wait(bar_empty + 8 * (i % kStages), (i / kStages - 1) & 1, abort_flag, lim);
@@ -384,6 +400,25 @@ cache_attention_rows_kernel(RowsArgs k) {
             const uint8_t* const raw = smem + S::kRaw + (i & 1) * S::kRawBytes;
             uint8_t* const stage = smem + S::kStage + i % kStages * S::kStageBytes;
             const int token0 = (t0 + i) * kTokens;
+            // V's scale and centre of a token and group, a thread each, and the largest value that they allow.  What is no number would
+            // reach rows that do not see it: it is a zero here, and those that do see it are told.  So are rows behind the last.
+            float scale = 0.f, centre = 0.f;
+            if (u < kTokens * G) {
+                const int token = u / G, g = u % G, rb = token & 31;
+                const uint8_t* const block = raw + (token >> 5) * L::kBytes;
+                const float f = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(block + L::kVScale + (rb * G + g) * 2) << 16);
+                const float m = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(block + L::kVCentre + (g * 32 + rb) * 2) << 16);
+                if (token0 + token < len) {
+                    if (f == f) {
+                        scale = f;
+                        centre = m;
+                    } else {
+                        atomicMin(first_bad + g, token0 + token);
+                    }
+                }
+            }
+            const uint32_t most_here = __reduce_max_sync(0xffffffffu, __float_as_uint(fmaf(8.f, fabsf(scale), fabsf(centre))));
+            if ((u & 31) == 0) bounds[u >> 5] = most_here;
             {   // K: a thread a quarter of a token's row
                 const int row = u >> 2, t = u & 3, rb = row & 31;
                 const uint8_t* const block = raw + (row >> 5) * L::kBytes;
@@ -393,37 +428,6 @@ cache_attention_rows_kernel(RowsArgs k) {
                 for (int g = 0; g < G; ++g)
                     *reinterpret_cast<uint4*>(stage + S::kK + (g / 2) * 8192 + at_swizzled(row, (g & 1) * 4 + t)) =
                         make_uint4(centred(code_pair(w[g])), centred(code_pair(w[g] >> 4)), centred(code_pair(w[g] >> 8)), centred(code_pair(w[g] >> 12)));
-            }
-            {   // V: a thread four elements of each group of two tokens
-                const int g8 = u & 7, pair = u >> 3, there = len - token0 - 2 * pair, rb = 2 * (pair & 15);
-                const uint8_t* const block = raw + (pair >> 4) * L::kBytes;
-                const uint32_t keep = (there > 0 ? 0x0000FFFFu : 0u) | (there > 1 ? 0xFFFF0000u : 0u);
-                uint32_t x0[G / 2], x1[G / 2], s[G];       // (scales of two tokens)
-                words<G / 2>(x0, block + L::kVCodes + rb * (D / 2) + g8 * 2 * G);
-                words<G / 2>(x1, block + L::kVCodes + (rb + 1) * (D / 2) + g8 * 2 * G);
-                words<G>(s, block + L::kVScale + rb * 2 * G);
-                uint8_t* const to = stage + S::kV + at_swizzled(g8, pair >> 2) + (pair & 3) * 4;     // (rows 8 apart are 1024 bytes apart)
-#pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    const uint32_t pick = g & 1 ? 0x7632u : 0x5410u, x = __byte_perm(x0[g / 2], x1[g / 2], pick), f = __byte_perm(s[g / 2], s[(G + g) / 2], pick);
-                    const uint32_t m = *reinterpret_cast<const uint32_t*>(block + L::kVCentre + (g * 32 + rb) * 2);
-                    // what is no number would reach rows that do not see it: it is a zero here, and those that do see it are told
-                    uint32_t fine = keep;
-                    if ((f & 0x7FFFu) > 0x7F80u) {
-                        fine &= 0xFFFF0000u;
-                        if (there > 0 && g8 == 0) atomicMin(first_bad + g, token0 + 2 * pair);
-                    }
-                    if ((f >> 16 & 0x7FFFu) > 0x7F80u) {
-                        fine &= 0x0000FFFFu;
-                        if (there > 1 && g8 == 0) atomicMin(first_bad + g, token0 + 2 * pair + 1);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        uint32_t y;
-                        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(y) : "r"(centred(code_pair(x >> (4 * e)))), "r"(f), "r"(m));
-                        *reinterpret_cast<uint32_t*>(to + (g * 4 + e) * 1024) = y & fine;
-                    }
-                }
             }
             if (u < kTokens) {                             // centres three times over, scales
                 const uint8_t* const block = raw + (u >> 5) * L::kBytes;
@@ -436,6 +440,39 @@ cache_attention_rows_kernel(RowsArgs k) {
                 float* const f = reinterpret_cast<float*>(stage + S::kS) + u;
 #pragma unroll
                 for (int g = 0; g < G; ++g) f[g * kTokens] = g & 1 ? bf16hi(s[g / 2]) : bf16lo(s[g / 2]);
+            }
+            unpack_bar();
+            uint32_t bound = 0;
+#pragma unroll
+            for (int w = 0; w < kUnpackThreads / 32; ++w) bound = max(bound, bounds[w]);
+            exponent = max(exponent, (int)(bound >> 23));  // (values times 2^(141 - exponent) are below 2^15)
+            const float up = __int_as_float((268 - exponent) << 23);
+            if (u < kTokens * G) {
+                table[(u % G) * kTokens + u / G] = __half_as_ushort(__float2half_rn(scale * up));
+                table[(G + u % G) * kTokens + u / G] = __half_as_ushort(__float2half_rn(centre * up));
+            }
+            if (u == 0) exponents[i % kStages] = exponent;
+            unpack_bar();
+            {   // V: a thread four elements of each group of two tokens
+                const int g8 = u & 7, pair = u >> 3, rb = 2 * (pair & 15);
+                const uint8_t* const block = raw + (pair >> 4) * L::kBytes;
+                uint32_t x0[G / 2], x1[G / 2];
+                words<G / 2>(x0, block + L::kVCodes + rb * (D / 2) + g8 * 2 * G);
+                words<G / 2>(x1, block + L::kVCodes + (rb + 1) * (D / 2) + g8 * 2 * G);
+                uint8_t* const to = stage + S::kV + at_swizzled(g8, pair >> 2) + (pair & 3) * 4;     // (rows 8 apart are 1024 bytes apart)
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    const uint32_t x = __byte_perm(x0[g / 2], x1[g / 2], g & 1 ? 0x7632u : 0x5410u);
+                    const uint32_t f = *reinterpret_cast<const uint32_t*>(table + g * kTokens + 2 * pair), m = *reinterpret_cast<const uint32_t*>(table + (G + g) * kTokens + 2 * pair);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {          // (1024 + c) - 1032 = c - 8
+                        uint32_t y;
+                        asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(y) : "r"(x >> (4 * e)), "r"(0x000F000Fu), "r"(0x64006400u));
+                        asm("add.rn.f16x2 %0, %0, %1;" : "+r"(y) : "r"(0xE408E408u));
+                        asm("fma.rn.f16x2 %0, %0, %1, %2;" : "+r"(y) : "r"(f), "r"(m));
+                        *reinterpret_cast<uint32_t*>(to + (g * 4 + e) * 1024) = y;
+                    }
+                }
             }
             fence_async_proxy();
             mbar_arrive(bar_full + 8 * (i % kStages));
@@ -473,7 +510,7 @@ cache_attention_rows_kernel(RowsArgs k) {
     } else {
         // ------------------------------------------------------------------ products with the weights
         const unsigned long long lim = k.limit_of(kRoleMma);
-        constexpr uint32_t idesc = umma_idesc_bf16(kRows, D + 16);
+        constexpr uint32_t idesc = umma_idesc_bf16(kRows, D + 16) & ~(1u << 7 | 1u << 10);       // (both operands fp16)
         int at = 0;
         for (int i = 0; i < n; ++i) {
             if (!__all_sync(0xffffffffu, mbar_wait(bar_p, i & 1, abort_flag, lim))) break;

@@ -331,6 +331,21 @@ def test_many_query_rows_and_rows_that_are_no_numbers(d):
     assert torch.isfinite(lse[:, :, :seen]).all() and torch.isnan(lse[:, :, seen:]).all()
 
 
+@pytest.mark.parametrize("up", [True, False])
+def test_many_query_rows_over_values_that_grow(up):
+    """Values of V a million times larger, or smaller, at the end than at the beginning."""
+    n, d, R, Tq, Ncap = 700, 128, 8, 24, 10944
+    rng = np.random.default_rng(21)
+    size = np.exp2(np.linspace(-10, 10, n) * (1 if up else -1))[None, None, :, None]
+    K, V = _bf16(rng, 1, 1, n, d), torch.from_numpy((rng.standard_normal((1, 1, n, d)) * size).astype(np.float32)).bfloat16().to(DEV)
+    cache, lens = _cache(1, 1, Ncap, d), _i32([0])
+    vb.vitcop_cache_write(K, V, cache, lens)
+    q = _bf16(rng, 1, R, Tq, d)
+    for length in (n, 65):
+        out, lse = _attend(q, cache, [length], d ** -0.5)
+        _check(q, cache, oc.quantise(_f64(K)), oc.quantise(_f64(V)), [length], d ** -0.5, True, out, lse)
+
+
 @pytest.mark.parametrize("roles", [1, 2, 4])
 def test_many_query_rows_report_a_wait_that_ran_out(roles):
     """One role of every CTA gives up at once, with products and copies of the others in flight; the next call is right again."""
