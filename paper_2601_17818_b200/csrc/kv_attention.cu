@@ -7,7 +7,7 @@
 //   output   elements times query rows: (128 + c) - 136 = c - 8 is exact too.  The weights enter, transposed, as bf16(p) with the
 //            centres and as bf16(bf16(p) s) with a group's codes; what the output is divided by is the sum of the bf16(p) (rows of ones
 //            beside the centres), so that a row that takes nearly all is not off by its weight's rounding
-// A warp takes every fourth block of 32 tokens of its CTA's piece, with blocks ahead in shared memory (cp.async), and keeps maximum, sum
+// A warp takes every fourth (or eighth) block of 32 tokens of its CTA's piece, with blocks ahead in shared memory (cp.async), and keeps maximum, sum
 // and output of its own; the CTA joins its warps, a second kernel joins the CTAs that shared a head.
 #include <type_traits>
 
@@ -136,21 +136,23 @@ __device__ __forceinline__ int holder_of(const Shares& s, int block) {
 }
 __device__ __forceinline__ int piece(const Walk& w) { return min(w.blocks - w.tile, w.left); }
 
-template <int D, int NT, bool SHARES>
-__global__ void __launch_bounds__(kWarps * 32, ctas_per_sm(D, NT))
+// SHARES: the blocks of all heads are shared out to the CTAs; otherwise a CTA has a head and tile of rows.  W: warps of a CTA.
+template <int D, int NT, bool SHARES, int W>
+__global__ void __launch_bounds__(W * 32, ctas_per_sm(D, NT) * kWarps / W > 0 ? ctas_per_sm(D, NT) * kWarps / W : 1)
 cache_attention_kernel(AttArgs a) {
+    static_assert(!SHARES || W == kWarps, "shares are counted in rounds of kWarps blocks");
     using L = CacheBlock<D>;
     constexpr int G = L::G, NR = 8 * NT;
     constexpr int kChunks = L::kBytes / 16;
     extern __shared__ __align__(128) uint8_t smem[];
-    float* const join = reinterpret_cast<float*>(smem + kWarps * kStages * L::kBytes);      // [warp][2 groups][8][lane]
-    float* const join_max = join + kWarps * 512;                                            // [warp][NR]
-    float* const join_sum = join_max + kWarps * NR;
-    float* const join_weight = join_sum + kWarps * NR;
-    QueryOperand<G>* const operand = reinterpret_cast<QueryOperand<G>*>(join_weight + kWarps * NR);      // [NT][lane]
+    float* const join = reinterpret_cast<float*>(smem + W * kStages * L::kBytes);      // [warp][2 groups][8][lane]
+    float* const join_max = join + W * 512;                                            // [warp][NR]
+    float* const join_sum = join_max + W * NR;
+    float* const join_weight = join_sum + W * NR;
+    QueryOperand<G>* const operand = reinterpret_cast<QueryOperand<G>*>(join_weight + W * NR);      // [NT][lane]
     uint4* const queries = reinterpret_cast<uint4*>(operand + NT * 32);                                // [stage][NT][G][lane]
     Walk* const walks = reinterpret_cast<Walk*>(queries + kStages * NT * G * 32);                                   // [warp][2]
-    int32_t* const stage_at = reinterpret_cast<int32_t*>(walks + kWarps * 2);                         // of warp 0
+    int32_t* const stage_at = reinterpret_cast<int32_t*>(walks + W * 2);                         // of warp 0
     int32_t* const before = stage_at + 1;                           // [B + 2]
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int segs = a.H * a.RT.d;
@@ -273,8 +275,8 @@ cache_attention_kernel(AttArgs a) {
                                      : "memory");
                 }
             }
-            ahead_left -= kWarps;
-            ahead_src += kWarps * L::kBytes;
+            ahead_left -= W;
+            ahead_src += W * L::kBytes;
             fill = fill + 1 == kStages ? 0 : fill + 1;
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -459,7 +461,7 @@ cache_attention_kernel(AttArgs a) {
 
         __syncthreads();                                   // (the queries)
         int token0 = (now.tile + warp) * kCacheBlock;
-        for (const int end = (now.tile + count) * kCacheBlock; token0 < end; token0 += kWarps * kCacheBlock) {
+        for (const int end = (now.tile + count) * kCacheBlock; token0 < end; token0 += W * kCacheBlock) {
             const uint8_t* const block = ring + use * L::kBytes;
             asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
             __syncwarp();
@@ -490,11 +492,11 @@ cache_attention_kernel(AttArgs a) {
         now = *at_work;
         const bool whole = now.tile == 0 && count == now.blocks;
         float* const part = SHARES && !whole ? a.part + (size_t)(2 * blockIdx.x + (now.tile == 0 ? 1 : 0)) * NR * (D + 3) : nullptr;
-        const int je = warp & 1, ji = warp >> 1;           // this warp's share: group i0 + ji, rows n 8 + 2 t + je
+        const int je = warp & 1, ji = warp >> 1 & 1;       // this warp's share (of the first four): group i0 + ji, rows n 8 + 2 t + je
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int rl = n * 8 + 2 * t + je, r = row0 + rl;
-            float f[kWarps], high = kNoLogit, total = 0.f, weight = 0.f;
+            float f[W], high = kNoLogit, total = 0.f, weight = 0.f;
 #pragma unroll
             for (int i0 = 0; i0 < G; i0 += 2) {
 #pragma unroll
@@ -511,9 +513,9 @@ cache_attention_kernel(AttArgs a) {
                 __syncthreads();
                 if (i0 == 0) {
 #pragma unroll
-                    for (int w = 0; w < kWarps; ++w) high = fmaxf(high, join_max[w * NR + rl]);
+                    for (int w = 0; w < W; ++w) high = fmaxf(high, join_max[w * NR + rl]);
 #pragma unroll
-                    for (int w = 0; w < kWarps; ++w) {
+                    for (int w = 0; w < W; ++w) {
                         f[w] = ex2_approx(join_max[w * NR + rl] - high);
                         total = fmaf(join_sum[w * NR + rl], f[w], total);
                         weight = fmaf(join_weight[w * NR + rl], f[w], weight);
@@ -521,12 +523,12 @@ cache_attention_kernel(AttArgs a) {
                 }
                 float v[4] = {};
 #pragma unroll
-                for (int w = 0; w < kWarps; ++w)
+                for (int w = 0; w < W; ++w)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) v[k] = fmaf(join[((w * 2 + ji) * 8 + 4 * je + k) * 32 + lane], f[w], v[k]);
                 const bool none = total == 0.f;
                 const int tq = quotient(r, a.R), hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
-                if (r < rows) {
+                if (r < rows && warp < 4) {
                     if (part) {
                         *reinterpret_cast<float4*>(part + rl * D + (i0 + ji) * 32 + 4 * g) = make_float4(v[0], v[1], v[2], v[3]);
                         if (i0 == 0 && ji == 0 && g == 0) {
@@ -639,6 +641,7 @@ cache_attention_join_kernel(AttArgs a, int NR, Divisor rows, int items, int most
 
 struct Plan {
     int NT, RT, ctas;                                      // ctas: of the shares; 0: a CTA a head and tile of rows
+    bool wide;                                             // such CTAs of eight warps
 };
 
 Plan plan_of(int B, int H, int Ncap, int d, int Tq, int Hq, int sms) {
@@ -656,28 +659,34 @@ Plan plan_of(int B, int H, int Ncap, int d, int Tq, int Hq, int sms) {
     const int slots = sms * ctas_per_sm(d, p.NT);
     const int64_t segs = (int64_t)B * H * p.RT, blocks = Ncap / kCacheBlock;
     p.ctas = 0;
+    p.wide = false;
     if (segs < 4 * slots && blocks > kWholeBlocks && segs * blocks < 0x7fff0000) p.ctas = slots;
+    // (an SM for each: 64 heads of 20 rows, 733 tokens 9.2 us with four warps, 7.8 with eight)
+    if (p.ctas == 0 && segs <= sms && blocks > kWarps) p.wide = true;
     return p;
 }
 
 size_t part_bytes(const Plan& p, int d) { return align_up((size_t)2 * p.ctas * 8 * p.NT * (d + 3) * sizeof(float), 256); }
 
+template <int D, int NT, int W>
+constexpr size_t smem_of() {
+    return (size_t)W * kStages * CacheBlock<D>::kBytes + W * 2048 + 3 * W * 8 * NT * 4 + NT * 32 * sizeof(QueryOperand<D / 32>) +
+           kStages * NT * (D / 32) * 512 + W * 2 * sizeof(Walk) + 4;
+}
 template <int D, int NT>
 int launch(AttArgs a, const Plan& p, cudaStream_t stream) {
-    constexpr size_t kSmem = (size_t)kWarps * kStages * CacheBlock<D>::kBytes + kWarps * 2048 + 3 * kWarps * 8 * NT * 4 +
-                             NT * 32 * sizeof(QueryOperand<D / 32>) + kStages * NT * (D / 32) * 512 + kWarps * 2 * sizeof(Walk);
-    static DoneOnDevice done[2];
+    static DoneOnDevice done[3];
     const bool shares = p.ctas > 0;
-    const size_t smem = kSmem + 4 + (shares ? (size_t)(a.B + 2) * 4 : 0);
-    const auto kern = shares ? cache_attention_kernel<D, NT, true> : cache_attention_kernel<D, NT, false>;
-    int rc = allow_dynamic_smem(kern, kSmem + 16384, done[shares]);
+    const size_t smem = shares ? smem_of<D, NT, kWarps>() + (size_t)(a.B + 2) * 4 : p.wide ? smem_of<D, NT, 8>() : smem_of<D, NT, kWarps>();
+    const auto kern = shares ? cache_attention_kernel<D, NT, true, kWarps> : p.wide ? cache_attention_kernel<D, NT, false, 8> : cache_attention_kernel<D, NT, false, kWarps>;
+    int rc = allow_dynamic_smem(kern, (p.wide ? smem_of<D, NT, 8>() : smem_of<D, NT, kWarps>()) + (shares ? 16384 : 0), done[shares ? 1 : p.wide ? 2 : 0]);
     if (rc != VITCOP_OK) return rc;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(shares ? p.ctas : a.B * a.H * p.RT));
-    cfg.blockDim = dim3(kWarps * 32);
+    cfg.blockDim = dim3((p.wide ? 8 : kWarps) * 32);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cfg.attrs = attr;
