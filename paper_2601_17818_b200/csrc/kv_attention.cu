@@ -108,10 +108,8 @@ __device__ __forceinline__ void make_operand(QueryOperand<G>* to, const uint4* r
 struct Walk {
     int b, seg, tile, blocks, left;
 };
-__device__ __forceinline__ int blocks_of(const AttArgs& a, int b) {
-    const int len = a.cache_len ? max(0, min(__ldcg(a.cache_len + b), a.Ncap)) : a.Ncap;
-    return (len + kCacheBlock - 1) / kCacheBlock;
-}
+__device__ __forceinline__ int len_of(const AttArgs& a, int b) { return a.cache_len ? max(0, min(__ldcg(a.cache_len + b), a.Ncap)) : a.Ncap; }
+__device__ __forceinline__ int blocks_of(const AttArgs& a, int b) { return (len_of(a, b) + kCacheBlock - 1) / kCacheBlock; }
 // How `total` blocks are shared out: the first `more` of `ctas` CTAs have `each` + 1 blocks, the others `each`; `whole`: a CTA has
 // the blocks of one segment instead.
 struct Shares {
@@ -153,7 +151,7 @@ cache_attention_kernel(AttArgs a) {
     uint4* const queries = reinterpret_cast<uint4*>(operand + NT * 32);                                // [stage][NT][G][lane]
     Walk* const walks = reinterpret_cast<Walk*>(queries + kStages * NT * G * 32);                                   // [warp][2]
     int32_t* const stage_at = reinterpret_cast<int32_t*>(walks + W * 2);                         // of warp 0
-    int32_t* const before = stage_at + 1;                           // [B + 2]
+    int32_t* const before = stage_at + 1;                           // [B + 2], and the samples' lengths [B]
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int segs = a.H * a.RT.d;
     grid_dependency_wait();
@@ -169,14 +167,18 @@ cache_attention_kernel(AttArgs a) {
         if (warp == 0) {
             int sum = 0, longest = 0;
             for (int b0 = 0; b0 < a.B; b0 += 32) {
-                int v = b0 + lane < a.B ? blocks_of(a, b0 + lane) : 0;
+                const int len = b0 + lane < a.B ? len_of(a, b0 + lane) : 0;
+                int v = (len + kCacheBlock - 1) / kCacheBlock;
                 const int mine = v;
 #pragma unroll
                 for (int off = 1; off < 32; off <<= 1) {
                     const int u = __shfl_up_sync(0xffffffffu, v, off);
                     if (lane >= off) v += u;
                 }
-                if (b0 + lane < a.B) before[b0 + lane] = sum + v - mine;
+                if (b0 + lane < a.B) {
+                    before[b0 + lane] = sum + v - mine;
+                    before[a.B + 2 + b0 + lane] = len;
+                }
                 sum += __shfl_sync(0xffffffffu, v, 31);
                 longest = max(longest, mine);
             }
@@ -289,7 +291,7 @@ cache_attention_kernel(AttArgs a) {
         now = *at_work;
         const int b = now.b, h = quotient(now.seg, a.RT), row0 = (now.seg - h * (int)a.RT.d) * NR, rows = (int)a.R.d * a.Tq;
         const int count = piece(now);
-        const int len = a.cache_len ? max(0, min(__ldcg(a.cache_len + b), a.Ncap)) : a.Ncap;
+        const int len = SHARES ? before[a.B + 2 + b] : len_of(a, b);
         // (they came with the first block of warp 0)
         if (warp == 0) {
             asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
@@ -677,9 +679,9 @@ template <int D, int NT>
 int launch(AttArgs a, const Plan& p, cudaStream_t stream) {
     static DoneOnDevice done[3];
     const bool shares = p.ctas > 0;
-    const size_t smem = shares ? smem_of<D, NT, kWarps>() + (size_t)(a.B + 2) * 4 : p.wide ? smem_of<D, NT, 8>() : smem_of<D, NT, kWarps>();
+    const size_t smem = shares ? smem_of<D, NT, kWarps>() + (size_t)(2 * a.B + 2) * 4 : p.wide ? smem_of<D, NT, 8>() : smem_of<D, NT, kWarps>();
     const auto kern = shares ? cache_attention_kernel<D, NT, true, kWarps> : p.wide ? cache_attention_kernel<D, NT, false, 8> : cache_attention_kernel<D, NT, false, kWarps>;
-    int rc = allow_dynamic_smem(kern, (p.wide ? smem_of<D, NT, 8>() : smem_of<D, NT, kWarps>()) + (shares ? 16384 : 0), done[shares ? 1 : p.wide ? 2 : 0]);
+    int rc = allow_dynamic_smem(kern, (p.wide ? smem_of<D, NT, 8>() : smem_of<D, NT, kWarps>()) + (shares ? 20480 : 0), done[shares ? 1 : p.wide ? 2 : 0]);
     if (rc != VITCOP_OK) return rc;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
