@@ -353,6 +353,7 @@ int vitcop_kproj_knorm(const void* hidden, const void* W_k, int B, int N, int Dh
  *   cache_len   int32 [B] or NULL (= 0): rows that are in the cache already
  *   new_len     int32 [B] out: cache_len[b] + rows of the sample, also where they did not all fit: rows from Ncap on are not
  *               written.  Must not overlap cache_len or another input.
+ * (A pointer to nothing, as an empty cache, no samples, no rows, may be NULL in all three calls.)
  * Errors: INVALID_ARG (NULL cache/new_len, K and V both NULL, negative sizes or strides, span outside the sequence, overlap),
  * UNSUPPORTED (d, Ncap % 32, alignment, more than 2^31 - 1 rows), CUDA. */
 int vitcop_cache_write(const void* K, const void* V, int B, int H, int N, int d,
@@ -380,7 +381,8 @@ int vitcop_cache_read(const void* cache, int B, int H, int Ncap, int d, const in
  *   cache_len  int32 [B] or NULL (= Ncap for every sample)
  *   lse     fp32 [B, Hq, Tq] out, optional: log of the sum of exp(scale * q k) over the rows seen
  *   workspace  vitcop_workspace_bytes(VITCOP_OP_CACHE_ATTENTION, B, H, Ncap, d, Tq, Hq, 0) bytes
- * Errors: INVALID_ARG (NULL q/cache/out, negative sizes or strides, Hq no multiple of H, overlap), UNSUPPORTED (d, Ncap % 32,
+ * Errors: INVALID_ARG (NULL q/cache/out, negative sizes or strides, Hq no multiple of H, a scale that is no number or infinite,
+ * rows of out that share elements, overlap), UNSUPPORTED (d, Ncap % 32,
  * alignment, more than 2^31 - 1 query rows), WORKSPACE, CUDA. */
 int vitcop_cache_attention(const void* q, const void* cache, int B, int Hq, int H, int Tq, int d, int Ncap,
                            int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_t,

@@ -461,7 +461,8 @@ static size_t extent(int B, int H, int N, int d, int64_t sb, int64_t sh, int64_t
     return ((size_t)(B - 1) * (size_t)sb + (size_t)(H - 1) * (size_t)sh + (size_t)(N - 1) * (size_t)sn + (size_t)d) * 2;
 }
 
-static int check_cache(int Ncap, int d, const void* cache) {
+static int check_cache(int B, int H, int Ncap, int d, const void* cache) {
+    if (!cache && cache_bytes(B, H, Ncap, d) > 0) return VITCOP_ERR_INVALID_ARG;
     if ((d != 64 && d != 128 && d != 256) || Ncap % kCacheBlock || !aligned16(cache)) return VITCOP_ERR_UNSUPPORTED;
     return VITCOP_OK;
 }
@@ -470,7 +471,8 @@ int vitcop_cache_write(const void* K, const void* V, int B, int H, int N, int d,
                        int64_t k_stride_n, int64_t v_stride_b, int64_t v_stride_h, int64_t v_stride_n, const int32_t* seq_len,
                        int vis_start, const int32_t* vis_len, int vis_len_uniform, const int32_t* keep_idx, int keep_stride,
                        const int32_t* n_keep, const int32_t* cache_len, void* cache, int Ncap, int32_t* new_len, void* stream) {
-    if ((!K && !V && N > 0) || !cache || !new_len || B < 0 || H < 0 || N < 0 || d < 0 || Ncap < 0) return VITCOP_ERR_INVALID_ARG;
+    if (B < 0 || H < 0 || N < 0 || d < 0 || Ncap < 0) return VITCOP_ERR_INVALID_ARG;
+    if ((!K && !V && extent(B, H, N, d, 0, 0, 0) > 0) || (!new_len && B > 0)) return VITCOP_ERR_INVALID_ARG;
     const int64_t strides[6] = {k_stride_b, k_stride_h, k_stride_n, v_stride_b, v_stride_h, v_stride_n};
     for (int i = 0; i < 6; ++i)
         if (strides[i] < 0) return VITCOP_ERR_INVALID_ARG;
@@ -479,7 +481,7 @@ int vitcop_cache_write(const void* K, const void* V, int B, int H, int N, int d,
         const int rc = check_span(N, vis_start, vis_len, vis_len_uniform, -1);
         if (rc != VITCOP_OK) return rc;
     }
-    const int rc = check_cache(Ncap, d, cache);
+    const int rc = check_cache(B, H, Ncap, d, cache);
     if (rc != VITCOP_OK) return rc;
     for (int i = 0; i < 6; ++i)
         if (strides[i] % 8 && (i < 3 ? K : V)) return VITCOP_ERR_UNSUPPORTED;
@@ -503,9 +505,10 @@ int vitcop_cache_write(const void* K, const void* V, int B, int H, int N, int d,
 
 int vitcop_cache_read(const void* cache, int B, int H, int Ncap, int d, const int32_t* cache_len, const int32_t* row_begin,
                       int row_begin_uniform, void* K_out, void* V_out, int N_out, void* stream) {
-    if (!cache || (!K_out && !V_out && N_out > 0) || B < 0 || H < 0 || Ncap < 0 || d < 0 || N_out < 0) return VITCOP_ERR_INVALID_ARG;
+    if (B < 0 || H < 0 || Ncap < 0 || d < 0 || N_out < 0) return VITCOP_ERR_INVALID_ARG;
+    if (!K_out && !V_out && extent(B, H, N_out, d, 0, 0, 0) > 0) return VITCOP_ERR_INVALID_ARG;
     if (!row_begin && row_begin_uniform < 0) return VITCOP_ERR_INVALID_ARG;
-    const int rc = check_cache(Ncap, d, cache);
+    const int rc = check_cache(B, H, Ncap, d, cache);
     if (rc != VITCOP_OK) return rc;
     if (!aligned16(K_out) || !aligned16(V_out) || B > 65535) return VITCOP_ERR_UNSUPPORTED;
     const size_t cbytes = cache_bytes(B, H, Ncap, d), obytes = (size_t)B * H * N_out * d * 2, lens = (size_t)B * sizeof(int32_t);
@@ -522,18 +525,21 @@ int vitcop_cache_attention(const void* q, const void* cache, int B, int Hq, int 
                            int64_t q_stride_h, int64_t q_stride_t, const int32_t* cache_len, float scale, int causal, void* out,
                            int64_t out_stride_b, int64_t out_stride_h, int64_t out_stride_t, float* lse, void* workspace,
                            size_t workspace_bytes, void* stream) {
-    if (!q || !cache || !out || B < 0 || Hq < 0 || H < 0 || Tq < 0 || d < 0 || Ncap < 0) return VITCOP_ERR_INVALID_ARG;
+    if (B < 0 || Hq < 0 || H < 0 || Tq < 0 || d < 0 || Ncap < 0) return VITCOP_ERR_INVALID_ARG;
+    if ((!q || !out) && extent(B, Hq, Tq, d, 0, 0, 0) > 0) return VITCOP_ERR_INVALID_ARG;
+    if (!(scale - scale == 0.f)) return VITCOP_ERR_INVALID_ARG;            // (NaN, infinite)
     if (H > 0 ? Hq % H != 0 : Hq != 0) return VITCOP_ERR_INVALID_ARG;
     const int64_t strides[6] = {q_stride_b, q_stride_h, q_stride_t, out_stride_b, out_stride_h, out_stride_t};
     for (int i = 0; i < 6; ++i)
         if (strides[i] < 0) return VITCOP_ERR_INVALID_ARG;
-    const int rc = check_cache(Ncap, d, cache);
+    const int rc = check_cache(B, H, Ncap, d, cache);
     if (rc != VITCOP_OK) return rc;
     for (int i = 0; i < 6; ++i)
         if (strides[i] % 8) return VITCOP_ERR_UNSUPPORTED;
     if (!aligned16(q) || !aligned16(out) || B > 65535) return VITCOP_ERR_UNSUPPORTED;
     // (rows of the output that share elements have no value)
-    if ((B > 1 && out_stride_b < d) || (Hq > 1 && out_stride_h < d) || (Tq > 1 && out_stride_t < d)) return VITCOP_ERR_INVALID_ARG;
+    if (extent(B, Hq, Tq, d, 0, 0, 0) > 0 && ((B > 1 && out_stride_b < d) || (Hq > 1 && out_stride_h < d) || (Tq > 1 && out_stride_t < d)))
+        return VITCOP_ERR_INVALID_ARG;
     if ((int64_t)B * Hq * Tq > 0x7fffffff) return VITCOP_ERR_UNSUPPORTED;
     const size_t need = cache_attention_workspace_bytes(B, H, Ncap, d, Tq, Hq);
     const size_t obytes = extent(B, Hq, Tq, d, out_stride_b, out_stride_h, out_stride_t);

@@ -341,10 +341,15 @@ PyObject* cache_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
             PyErr_Clear();
             refuse("scale", "expected a number");
         }
+        const int causal = PyObject_IsTrue(args[8]);
+        if (causal < 0) {
+            PyErr_Clear();
+            refuse("causal", "expected a truth value");
+        }
         float* const lse = dense<float>(args[9], "lse", dev, at::kFloat, {c.B, Hq, Tq});
         return unlocked(bound<decltype(vitcop_cache_attention)>(e), (const void*)qr.data, (const void*)c.data, int32_of(c.B, "B"), int32_of(Hq, "Hq"),
                         int32_of(c.H, "H"), int32_of(Tq, "Tq"), int32_of(c.d, "d"), int32_of(c.Ncap, "Ncap"), qr.stride[0], qr.stride[1],
-                        qr.stride[2], cache_len, static_cast<float>(scale), PyObject_IsTrue(args[8]) == 1 ? 1 : 0, o.data, o.stride[0], o.stride[1],
+                        qr.stride[2], cache_len, static_cast<float>(scale), causal, o.data, o.stride[0], o.stride[1],
                         o.stride[2], lse, workspace, bytes, stream);
     });
 }

@@ -165,3 +165,16 @@ def test_binding_refuses_what_is_not_on_the_device(L, monkeypatch):
     assert vb.alloc_cache(2, 3, 64, 128, device="cpu").shape == (2, 3, 2, 5120)
     with pytest.raises(vb.VitcopError):
         vb.vitcop_workspace_bytes(vb.OP_CACHE_ATTENTION, B=1, H=-1)
+
+
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), float("-inf")])
+def test_attention_refuses_a_scale_that_is_no_number(L, scale):
+    assert L.vitcop_cache_attention(A, C_, 2, 4, 2, 1, 64, 64, 256, 64, 64, NULL, scale, 1, B_, 256, 64, 64, NULL, D_, 1 << 30, NULL) == vb.ERR_INVALID_ARG
+
+
+def test_a_pointer_to_nothing_may_be_null(L):
+    assert _write(L, K=NULL, V=NULL, B=0, cache=NULL, new=NULL) == vb.OK
+    assert _read(L, B=0, cache=NULL, K=NULL, V=NULL) == vb.OK and _read(L, Ncap=0, cache=NULL, K=NULL, V=NULL, N=0) == vb.OK
+    for nothing in (dict(Tq=0), dict(B=0), dict(H=0, Hq=0)):       # (as far as the workspace, which is asked for last)
+        assert _attend(L, q=NULL, out=NULL, ws=NULL, cache=C_, **nothing) == vb.ERR_WORKSPACE
+    assert _attend(L, cache=NULL, Ncap=0, ws=NULL) == vb.ERR_WORKSPACE

@@ -541,3 +541,22 @@ def test_what_the_binding_refuses():
     for call in (lambda: vb.vitcop_cache_write(x, x, cache, n, cache_len=n), lambda: vb.vitcop_cache_attention(x, cache, n, x, ws, 1.0)):
         with pytest.raises(vb.VitcopError):
             call()
+
+
+def test_no_rows_no_samples_no_capacity():
+    x = torch.zeros(2, 4, 3, 64, dtype=torch.bfloat16, device=DEV)
+    empty, n, to = vb.alloc_cache(2, 2, 0, 64), _i32([5, 0]), _i32([9, 9])
+    vb.vitcop_cache_write(x[:, :2], x[:, :2], empty, to, cache_len=n)      # (nothing fits)
+    assert to.tolist() == [8, 3]
+    vb.vitcop_cache_read(empty, n, torch.zeros(2, 2, 3, 64, dtype=torch.bfloat16, device=DEV))
+    out, lse = _attend(x, empty, [5, 0], 1.0)
+    assert torch.all(out == 0) and torch.all(torch.isneginf(lse))
+    cache, _ = _cache(2, 2, 64, 64), _attend(x[:, :, :0], empty, [5, 0], 1.0)
+    assert _attend(x[:, :, :0], cache, [5, 0], 1.0)[0].shape == (2, 4, 0, 64)
+    none, no_len = vb.alloc_cache(0, 2, 64, 64), _i32([])
+    vb.vitcop_cache_write(x[:0, :2], x[:0, :2], none, no_len)
+    vb.vitcop_cache_read(none, no_len, x[:0, :2])
+    _attend(x[:0], none, [], 1.0)
+    with pytest.raises(ValueError):
+        vb.vitcop_cache_attention(x, cache, n, torch.zeros_like(x), vb.alloc_workspace(vb.OP_CACHE_ATTENTION, B=2, H=2, N=64, d=64, Nv=3, D=4),
+                                  1.0, causal=n)
