@@ -21,6 +21,9 @@ constexpr int kWarps = 4;
 constexpr int kStages = 2;
 constexpr uint32_t kOnes = 0x3F803F80u;                    // 1, twice, in bf16
 constexpr int kWholeBlocks = 24;
+// Weights are 2^(logit - base) with a base that starts this far above the maximum: they stay below 2^-16, so that sums of weights times
+// values of V hold wherever those values lie in fp32's range, and the smallest that count are still 2^-100 of the largest.
+constexpr float kHeadroom = 24.f;
 
 // Resident CTAs an SM, which the registers of the accumulators and the ring's memory leave room for.
 constexpr int ctas_per_sm(int D, int NT) { return D == 256 || D * NT > 256 || NT == 4 ? 2 : D * NT <= 128 ? 4 : 3; }
@@ -392,12 +395,12 @@ cache_attention_kernel(AttArgs a) {
                 }
                 // (the sums stay relative to an older maximum until a logit has passed it by 2^8)
                 float high[2] = {fmaxf(z[n][0], z[n][2]), fmaxf(z[n][1], z[n][3])};
-                if (__any_sync(0xffffffffu, fmaf(high[0], a.scale_log2, -base[n][0]) > 8.f || fmaf(high[1], a.scale_log2, -base[n][1]) > 8.f)) {
+                if (__any_sync(0xffffffffu, fmaf(high[0], a.scale_log2, -base[n][0]) > 8.f - kHeadroom || fmaf(high[1], a.scale_log2, -base[n][1]) > 8.f - kHeadroom)) {
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
 #pragma unroll
                         for (int off = 4; off < 32; off <<= 1) high[e] = fmaxf(high[e], __shfl_xor_sync(0xffffffffu, high[e], off));
-                        const float top = fmaxf(base[n][e], high[e] * a.scale_log2), keep = ex2_approx(base[n][e] - top);
+                        const float top = fmaxf(base[n][e], fmaf(high[e], a.scale_log2, kHeadroom)), keep = ex2_approx(base[n][e] - top);
                         base[n][e] = top;
                         sum[n][e] *= keep;
 #pragma unroll

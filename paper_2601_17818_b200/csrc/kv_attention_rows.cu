@@ -20,7 +20,7 @@ namespace {
 
 constexpr int kRows = 128, kTokens = 64;
 constexpr int kSoftmaxThreads = 256, kUnpackThreads = 256, kThreads = kSoftmaxThreads + kUnpackThreads + 64;
-constexpr int kStages = 3;
+constexpr int kStages = 3, kMostSplits = 16;
 constexpr uint32_t kTmem = 512;
 enum { kRoleUnpack = 1, kRoleMma = 2, kRoleSoftmax = 4 };
 
@@ -329,7 +329,7 @@ cache_attention_rows_kernel(RowsArgs k) {
                 tmem_ld8_issue(tmem_o + lanes + D, weight[0]);
                 tmem_wait_ld(weight);
             }
-            const float inv = (alone ? (none ? 0.f : 1.f / __uint_as_float(weight[0][0])) : 1.f) * (n > 0 ? __int_as_float((exponent - 14) << 23) : 1.f);
+            const float inv = none ? 0.f : __int_as_float((exponent - 14) << 23) / __uint_as_float(weight[0][0]);
             float* const part = a.part + (size_t)blockIdx.x * kRows * (D + 3);
             // (32 rows by 32 elements a warp, turned in shared memory that the tiles have left: 8 lanes then write a row)
             float* const turn = reinterpret_cast<float*>(smem + S::kStage) + warp * 32 * 36;
@@ -561,26 +561,39 @@ cache_attention_rows_join_kernel(RowsArgs k, int ctas) {
         if (r >= rows) continue;
         const float* const part = a.part + (size_t)seg * k.splits * kRows * (D + 3);
         constexpr size_t kSize = (size_t)kRows * (D + 3);
-        float top = kNoLogit, sum = 0.f, weight = 0.f, v[E] = {};
-        for (int s = 0; s < k.splits; ++s) top = fmaxf(top, part[s * kSize + kRows * D + rl]);
+        // (lane s: piece s; each piece is a mean of its own, which counts with its share of the weights)
+        static_assert(kMostSplits <= 32);
+        const float* const mine = part + lane * kSize + kRows * D + rl;
+        const bool there = lane < k.splits;
+        const float piece = there ? mine[0] : kNoLogit;
+        float top = piece, sum = there ? mine[kRows] : 0.f, weight = there ? mine[2 * kRows] : 0.f;
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+        const float f = ex2_approx(piece - top);
+        sum *= f;
+        weight *= f;
+        float share = weight;
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) {
+            sum += __shfl_xor_sync(0xffffffffu, sum, off);
+            weight += __shfl_xor_sync(0xffffffffu, weight, off);
+        }
+        const bool none = sum == 0.f;
+        share = none ? 0.f : share / weight;
+        float v[E] = {};
         for (int s = 0; s < k.splits; ++s) {
-            const float* const p = part + s * kSize;
-            const float f = ex2_approx(p[kRows * D + rl] - top);
-            sum = fmaf(p[kRows * D + kRows + rl], f, sum);
-            weight = fmaf(p[kRows * D + 2 * kRows + rl], f, weight);
+            const float w = __shfl_sync(0xffffffffu, share, s);
 #pragma unroll
             for (int e = 0; e < E; e += 2) {
-                const float2 x = *reinterpret_cast<const float2*>(p + rl * D + lane * E + e);
-                v[e] = fmaf(x.x, f, v[e]);
-                v[e + 1] = fmaf(x.y, f, v[e + 1]);
+                const float2 x = *reinterpret_cast<const float2*>(part + s * kSize + rl * D + lane * E + e);
+                v[e] = fmaf(x.x, w, v[e]);
+                v[e + 1] = fmaf(x.y, w, v[e + 1]);
             }
         }
         const int tq = quotient(r, a.R), hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
-        const bool none = sum == 0.f;
-        const float inv = none ? 0.f : 1.f / weight;
         uint32_t* const out = reinterpret_cast<uint32_t*>(a.io.out + b * a.io.ob + hq * a.io.oh + tq * a.io.ot + lane * E);
 #pragma unroll
-        for (int e = 0; e < E; e += 2) out[e / 2] = bf16x2(v[e] * inv, v[e + 1] * inv);
+        for (int e = 0; e < E; e += 2) out[e / 2] = bf16x2(v[e], v[e + 1]);
         if (a.lse && lane == 0) a.lse[((int64_t)b * a.Hq + hq) * a.Tq + tq] = none ? MINUS_INF : (top + __log2f(sum)) * kLn2;
     }
 }
@@ -596,7 +609,7 @@ RowsPlan plan_of(int B, int H, int Ncap, int Tq, int Hq) {
     const int64_t segs = (int64_t)B * H * p.RT, sms = sm_count(), tiles = Ncap / kTokens;
     int64_t s = segs < sms ? sms / segs : 1;
     if (s > tiles / 4) s = tiles / 4;                      // four tiles a piece at least
-    p.splits = (int)(s < 1 ? 1 : s > 16 ? 16 : s);
+    p.splits = (int)(s < 1 ? 1 : s > kMostSplits ? kMostSplits : s);
     p.ctas = segs * p.splits;
     return p;
 }

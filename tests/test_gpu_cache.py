@@ -560,3 +560,16 @@ def test_no_rows_no_samples_no_capacity():
     with pytest.raises(ValueError):
         vb.vitcop_cache_attention(x, cache, n, torch.zeros_like(x), vb.alloc_workspace(vb.OP_CACHE_ATTENTION, B=2, H=2, N=64, d=64, Nv=3, D=4),
                                   1.0, causal=n)
+
+
+@pytest.mark.parametrize("B,H,R,Tq,d,Ncap,n", [(1, 2, 4, 1, 64, 64, 50), (1, 2, 7, 2, 128, 2048, 1999), (70, 2, 1, 1, 256, 128, 128),
+                                               (1, 1, 4, 48, 128, 11008, 1500), (40, 4, 2, 20, 64, 352, 300)])
+def test_values_near_the_end_of_the_range(B, H, R, Tq, d, Ncap, n):
+    """Values of which a handful add up to more than fp32 holds; their mean is one of them."""
+    rng = np.random.default_rng(n)
+    K, V = _bf16(rng, B, H, n, d), torch.from_numpy((2e38 + 3e36 * rng.standard_normal((B, H, n, d))).astype(np.float32)).bfloat16().to(DEV)
+    cache, lens = _cache(B, H, Ncap, d), _i32([0] * B)
+    vb.vitcop_cache_write(K, V, cache, lens)
+    q = _bf16(rng, B, H * R, Tq, d)
+    out, lse = _attend(q, cache, [n] * B, d ** -0.5)
+    _check(q, cache, oc.quantise(_f64(K)), oc.quantise(_f64(V)), [n] * B, d ** -0.5, True, out, lse)
