@@ -381,6 +381,9 @@ int vitcop_cache_read(const void* cache, int B, int H, int Ncap, int d, const in
  *   cache_len  int32 [B] or NULL (= Ncap for every sample)
  *   lse     fp32 [B, Hq, Tq] out, optional: log of the sum of exp(scale * q k) over the rows seen
  *   workspace  vitcop_workspace_bytes(VITCOP_OP_CACHE_ATTENTION, B, H, Ncap, d, Tq, Hq, 0) bytes
+ * Many query rows (more than 32 of a stored head, d 64 or 128, long enough a cache) run through a kernel whose waits are bounded
+ * (vitcop_set_wait_limit): the status word is TIMEOUT, and out unspecified, where one ran out.  It holds the values of V as the
+ * largest of a head allow; where some are 2^24 times smaller, the rows concerned are done anew, some 100 times slower.
  * Errors: INVALID_ARG (NULL q/cache/out, negative sizes or strides, Hq no multiple of H, a scale that is no number or infinite,
  * rows of out that share elements, overlap), UNSUPPORTED (d, Ncap % 32,
  * alignment, more than 2^31 - 1 query rows), WORKSPACE, CUDA. */

@@ -23,6 +23,10 @@ constexpr int kSoftmaxThreads = 256, kUnpackThreads = 256, kThreads = kSoftmaxTh
 constexpr int kStages = 3, kMostSplits = 16;
 constexpr uint32_t kTmem = 512;
 enum { kRoleUnpack = 1, kRoleMma = 2, kRoleSoftmax = 4 };
+// What a CTA reports.  Far apart: in units of the largest value of V so far, which its power of two goes by, those of some token and group
+// (of 32 elements) are too small for fp16, although they may be all that a row or a column has.  The join does its rows anew, in fp32.
+enum { kGaveUp = 1, kFarApart = 2 };
+constexpr int kApart = 24;                                 // powers of two: fp16 has 2^-12 of a group's largest value, or more, left there
 
 template <int D>
 struct RowsSmem {
@@ -134,6 +138,7 @@ cache_attention_rows_kernel(RowsArgs k) {
     uint32_t* const bounds = reinterpret_cast<uint32_t*>(smem + S::kBars + 192);     // [8] largest value of V that a warp has found possible
     int* const exponents = reinterpret_cast<int*>(smem + S::kBars + 224);           // [kStages] of that power of two, as a float's bits have it
     float* const pairs = reinterpret_cast<float*>(smem + S::kPairs);
+    volatile int* const far_apart = reinterpret_cast<volatile int*>(smem + S::kBars + 240);
     int* const first_bad = reinterpret_cast<int*>(smem + S::kBars + 144);       // [G] first token whose values of V are no numbers
     const int tid = threadIdx.x, warp = tid >> 5;
     if (tid == 0) {
@@ -148,7 +153,7 @@ cache_attention_rows_kernel(RowsArgs k) {
         mbar_init(bar_drain, 1);
         mbar_init(bar_drain + 8, 1);
         mbar_init(bar_q, kRows);
-        *abort_flag = 0;
+        *abort_flag = *far_apart = 0;
         moved[0] = moved[1] = moved[2] = 0;
         for (int i = 0; i < G; ++i) first_bad[i] = 0x7fffffff;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -391,7 +396,7 @@ cache_attention_rows_kernel(RowsArgs k) {
         fetch(0);
         fetch(1);
         uint16_t* const table = reinterpret_cast<uint16_t*>(smem + S::kTable);
-        int exponent = 16;
+        int exponent = 16, least_exponent = 255;           // (of the values that this thread has seen, zeros apart)
         bool ok = true;
         for (int i = 0; i < n; ++i) {
             if (i >= kStages && u < 32) ok = mbar_wait(bar_empty + 8 * (i % kStages), (i / kStages - 1) & 1, abort_flag, lim);
@@ -417,7 +422,8 @@ cache_attention_rows_kernel(RowsArgs k) {
                     }
                 }
             }
-            const uint32_t most_here = __reduce_max_sync(0xffffffffu, __float_as_uint(fmaf(8.f, fabsf(scale), fabsf(centre))));
+            const uint32_t here = __float_as_uint(fmaf(8.f, fabsf(scale), fabsf(centre))), most_here = __reduce_max_sync(0xffffffffu, here);
+            if (here) least_exponent = min(least_exponent, (int)(here >> 23));
             if ((u & 31) == 0) bounds[u >> 5] = most_here;
             {   // K: a thread a quarter of a token's row
                 const int row = u >> 2, t = u & 3, rb = row & 31;
@@ -480,6 +486,7 @@ cache_attention_rows_kernel(RowsArgs k) {
             fetch(i + 2);
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
+        if (least_exponent + kApart < exponent) *far_apart = 1;
     } else if (warp == kThreads / 32 - 2) {
         // ------------------------------------------------------------------ products with the queries
         // (the whole warp walks, so that the operands' addresses are known to be the same in all lanes; one lane issues)
@@ -529,7 +536,7 @@ cache_attention_rows_kernel(RowsArgs k) {
     if (tid == kSoftmaxThreads + kUnpackThreads) {
         mbar_drain(bar_drain, 0);
         mbar_drain(bar_drain + 8, 0);
-        k.reports[blockIdx.x] = *abort_flag ? 1 : 0;
+        k.reports[blockIdx.x] = (*abort_flag ? kGaveUp : 0) | (*far_apart ? kFarApart : 0);
     }
     tc_fence_before();
     __syncthreads();
@@ -539,22 +546,106 @@ cache_attention_rows_kernel(RowsArgs k) {
     }
 }
 
-// The pieces of a row, in their order, a warp a row; and the status word.
+// Row r of head h of sample b by one warp, from the cache, in fp32: a lane has a token of a block for its logit, and element `lane` of every
+// group for the output.  (512 rows of 32 heads, 4000 tokens: 10.8 ms, 0.1 where fp16 holds the values.)
+template <int D>
+__device__ __noinline__ void row_anew(const AttArgs& a, int b, int h, int r, float* q) {
+    using L = CacheBlock<D>;
+    constexpr int G = L::G;
+    constexpr float kHeadroom = 24.f;                      // (weights below 2^-24: sums with values at the end of the range hold)
+    const int lane = threadIdx.x & 31, tq = quotient(r, a.R), hq = h * (int)a.R.d + (r - tq * (int)a.R.d);
+    const int len = a.cache_len ? max(0, min(__ldcg(a.cache_len + b), a.Ncap)) : a.Ncap, limit = a.causal ? max(0, len - a.Tq + tq + 1) : len;
+    const __nv_bfloat16* const src = a.io.q + b * a.io.qb + hq * a.io.qh + tq * a.io.qt;
+    float total[G];
+    __syncwarp();
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        const float x = a.zero ? 0.f : a.sign ? -__bfloat162float(src[g * 32 + lane]) : __bfloat162float(src[g * 32 + lane]);
+        q[g * 32 + lane] = total[g] = x;
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) total[g] += __shfl_xor_sync(0xffffffffu, total[g], off);
+    }
+    __syncwarp();
+    const auto bf16_at = [](const uint8_t* p) { return __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(p)) << 16); };
+    const uint8_t* block = a.cache + ((int64_t)b * a.H + h) * (a.Ncap / kCacheBlock) * L::kBytes;
+    float top = kNoLogit, sum = 0.f, v[G] = {};
+    for (int token0 = 0; token0 < limit; token0 += kCacheBlock, block += L::kBytes) {
+        const int seen = min(limit - token0, kCacheBlock);
+        float z = MINUS_INF;
+        if (lane < seen) {
+            z = 0.f;
+#pragma unroll 1
+            for (int g = 0; g < G; ++g) {
+                float dot = 0.f;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(block + L::kKCodes + lane * (D / 2) + t * 4 * G + g * 4));
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) dot = fmaf((float)((int)(w >> (4 * e) & 15) - 8), q[g * 32 + 8 * t + e], dot);
+                }
+                z = fmaf(bf16_at(block + L::kKScale + (lane * G + g) * 2), dot, z);
+                float group = total[0];
+#pragma unroll
+                for (int i = 1; i < G; ++i)
+                    if (i == g) group = total[i];
+                z = fmaf(bf16_at(block + L::kKCentre + (lane * G + g) * 2), group, z);
+            }
+        }
+        float high = z;
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, off));
+        const float now = fmaxf(top, fmaf(high, a.scale_log2, kHeadroom)), keep = ex2_approx(top - now), p = ex2_approx(fmaf(z, a.scale_log2, -now));
+        top = now;
+        sum = fmaf(sum, keep, p);
+#pragma unroll
+        for (int g = 0; g < G; ++g) v[g] *= keep;
+#pragma unroll 4
+        for (int i = 0; i < seen; ++i) {
+            const float w = __shfl_sync(0xffffffffu, p, i);
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const uint32_t c = __ldg(reinterpret_cast<const uint16_t*>(block + L::kVCodes + i * (D / 2) + (lane / 4) * 2 * G + g * 2)) >> (4 * (lane % 4)) & 15;
+                v[g] = fmaf(w, fmaf((float)((int)c - 8), bf16_at(block + L::kVScale + (i * G + g) * 2), bf16_at(block + L::kVCentre + (g * 32 + i) * 2)), v[g]);
+            }
+        }
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+    const bool none = sum == 0.f;
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+        a.io.out[b * a.io.ob + hq * a.io.oh + tq * a.io.ot + g * 32 + lane] = __float2bfloat16_rn(none ? 0.f : v[g] / sum);
+    if (a.lse && lane == 0) a.lse[((int64_t)b * a.Hq + hq) * a.Tq + tq] = none ? MINUS_INF : (top + __log2f(sum)) * kLn2;
+}
+
+// The pieces of a row, in their order, a warp a row; rows that are to be done anew; and the status word.
+constexpr int kQuarter = kRows / 4;
 template <int D>
 __global__ void __launch_bounds__(128)
-cache_attention_rows_join_kernel(RowsArgs k, int ctas) {
+cache_attention_rows_join_kernel(const __grid_constant__ RowsArgs k, int ctas) {
+    __shared__ float queries[4][D];
     const AttArgs& a = k.a;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rows = (int)a.R.d * a.Tq;
     constexpr int E = D / 32;                              // elements of a lane: lane E .. lane E + E - 1
     grid_dependency_wait();
     if (blockIdx.x == 0 && warp == 0) {
         bool gave_up = false;
-        for (int c = lane; c < ctas; c += 32) gave_up |= k.reports[c] != 0;
+        for (int c = lane; c < ctas; c += 32) gave_up |= (k.reports[c] & kGaveUp) != 0;
         gave_up = __any_sync(0xffffffffu, gave_up);
         if (lane == 0) *a.status = gave_up ? VITCOP_ERR_TIMEOUT : VITCOP_OK;
     }
-    if (k.splits == 1) return;
     const int segs = a.H * (int)a.RT.d, items = a.B * segs * kRows;
+    if (k.splits == 1) {                                   // a CTA 32 rows, of those that it has to look at
+        for (int item = blockIdx.x; item < items / kQuarter; item += gridDim.x) {
+            const int seg = item / 4, b = seg / segs, hs = seg - b * segs, h = quotient(hs, a.RT);
+            if (!(k.reports[seg] & kFarApart)) continue;
+            for (int i = warp; i < kQuarter; i += 4) {
+                const int r = (hs - h * (int)a.RT.d) * kRows + (item % 4) * kQuarter + i;
+                if (r < rows) row_anew<D>(a, b, h, r, queries[warp]);
+            }
+        }
+        return;
+    }
     for (int item = blockIdx.x * 4 + warp; item < items; item += gridDim.x * 4) {
         const int seg = item / kRows, rl = item - seg * kRows, b = seg / segs, hs = seg - b * segs, h = quotient(hs, a.RT);
         const int r = (hs - h * (int)a.RT.d) * kRows + rl;
@@ -565,8 +656,13 @@ cache_attention_rows_join_kernel(RowsArgs k, int ctas) {
         static_assert(kMostSplits <= 32);
         const float* const mine = part + lane * kSize + kRows * D + rl;
         const bool there = lane < k.splits;
+        const uint8_t report = there ? k.reports[seg * k.splits + lane] : 0;
         const float piece = there ? mine[0] : kNoLogit;
         float top = piece, sum = there ? mine[kRows] : 0.f, weight = there ? mine[2 * kRows] : 0.f;
+        if (__any_sync(0xffffffffu, report & kFarApart)) {
+            row_anew<D>(a, b, h, r, queries[warp]);
+            continue;
+        }
 #pragma unroll
         for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
         const float f = ex2_approx(piece - top);
@@ -635,8 +731,8 @@ int launch_rows(const RowsArgs& k, const RowsPlan& p, cudaStream_t stream) {
         rc = record_cuda(cudaLaunchKernelEx(&cfg, cache_attention_rows_kernel<D>, k));
         if (rc != VITCOP_OK) return rc;
     }
-    const int64_t items = p.splits > 1 ? (int64_t)k.a.B * k.a.H * p.RT * kRows : 1, most = sm_count() * 16;
-    cfg.gridDim = dim3((unsigned)((items + 3) / 4 < most ? (items + 3) / 4 : most));
+    const int64_t segs = (int64_t)k.a.B * k.a.H * p.RT, want = segs * (p.splits > 1 ? kRows / 4 : kRows / kQuarter), most = sm_count() * (p.splits > 1 ? 16 : 4);
+    cfg.gridDim = dim3((unsigned)(want < most ? want : most));
     cfg.blockDim = dim3(128);
     cfg.dynamicSmemBytes = 0;
     KernelTimeScope timed("cache_attention_rows_join_kernel", stream);

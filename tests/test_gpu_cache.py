@@ -573,3 +573,18 @@ def test_values_near_the_end_of_the_range(B, H, R, Tq, d, Ncap, n):
     q = _bf16(rng, B, H * R, Tq, d)
     out, lse = _attend(q, cache, [n] * B, d ** -0.5)
     _check(q, cache, oc.quantise(_f64(K)), oc.quantise(_f64(V)), [n] * B, d ** -0.5, True, out, lse)
+
+
+@pytest.mark.parametrize("B,H,R,Tq,d,Ncap,n", [(1, 1, 4, 48, 128, 11008, 1500), (1, 2, 7, 48, 64, 2048, 300), (40, 4, 2, 20, 128, 352, 300), (40, 4, 2, 20, 64, 352, 300)])
+def test_many_query_rows_and_values_of_other_sizes(B, H, R, Tq, d, Ncap, n):
+    """Values at the end of the range that some of the queries do not see, and groups far apart in size, are everybody's own."""
+    rng = np.random.default_rng(n + d)
+    K, V = _bf16(rng, B, H, n, d), _bf16(rng, B, H, n, d)
+    V[0, 0, n - 5, :32] = 3.38e38
+    V[0, 0, n - 15] *= 2.0 ** 100
+    V[B - 1, H - 1, :, 32:64] *= 2.0 ** -40
+    cache, lens = _cache(B, H, Ncap, d), _i32([0] * B)
+    vb.vitcop_cache_write(K, V, cache, lens)
+    q = _bf16(rng, B, H * R, Tq, d)
+    out, lse = _attend(q, cache, [n] * B, d ** -0.5)
+    _check(q, cache, oc.quantise(_f64(K)), oc.quantise(_f64(V)), [n] * B, d ** -0.5, True, out, lse)
