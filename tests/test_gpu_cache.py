@@ -588,3 +588,33 @@ def test_many_query_rows_and_values_of_other_sizes(B, H, R, Tq, d, Ncap, n):
     q = _bf16(rng, B, H * R, Tq, d)
     out, lse = _attend(q, cache, [n] * B, d ** -0.5)
     _check(q, cache, oc.quantise(_f64(K)), oc.quantise(_f64(V)), [n] * B, d ** -0.5, True, out, lse)
+
+
+@pytest.mark.parametrize("B,H,R,Tq,d,Ncap", [(3, 8, 7, 1, 128, 2048), (2, 4, 4, 40, 128, 4096), (1, 2, 4, 1, 64, 512), (80, 2, 2, 20, 64, 320)])
+def test_two_streams_at_once_and_replays_with_other_lengths(B, H, R, Tq, d, Ncap):
+    """Calls on two streams, each with its workspace, at the same time; a captured call takes the lengths that it finds when it runs."""
+    lens = [Ncap - 37 * b % 300 for b in range(B)]
+    q, cache, _, _ = _problem(B + d, B, H, R, Tq, d, Ncap, lens)
+    shared = q[:, :1, :1].expand(B, H * R, Tq, d)          # (one row for all of a sample's queries)
+    n = _i32(lens)
+    ws = [vb.alloc_workspace(vb.OP_CACHE_ATTENTION, B=B, H=H, N=Ncap, d=d, Nv=Tq, D=H * R) for _ in range(3)]
+    outs = [torch.empty_like(q, memory_format=torch.contiguous_format) for _ in range(3)]
+    want = [_attend(x, cache, ln, 0.1, strided=False)[0] for x, ln in ((q, lens), (shared, lens), (q, [x // 2 for x in lens]))]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s, x, o, w in zip(streams, (q, shared), outs, ws):
+            with torch.cuda.stream(s):
+                vb.vitcop_cache_attention(x, cache, n, o, w, 0.1)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+    assert all(vb.vitcop_poll_status(w) == vb.OK for w in ws[:2])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        vb.vitcop_cache_attention(q, cache, n, outs[2], ws[2], 0.1)
+    for ln, w in ((lens, want[0]), ([x // 2 for x in lens], want[2]), ([0] * B, torch.zeros_like(want[0]))):
+        n.copy_(_i32(ln))
+        outs[2].fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[2], w) and vb.vitcop_poll_status(ws[2]) == vb.OK
