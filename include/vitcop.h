@@ -80,14 +80,16 @@ int vitcop_poll_status(const void* workspace, void* stream, int* device_status);
 
 /* ---------------------------------------------------------------- diagnostic: bounded device waits
  * The paper has no counterpart.  Kernels whose CTAs wait for one another or for asynchronous copies (the Gram
- * sweeps of the redundancy filter) bound every wait; when a wait runs out, the CTA abandons its work, lets its
+ * sweeps of the redundancy filter, the attention of many query rows over the cache) bound every wait; when a
+ * wait runs out, the CTA abandons its work, lets its
  * copies and tensor-core operations in flight finish, frees its tensor memory and records VITCOP_ERR_TIMEOUT in
  * the status word (read it with vitcop_poll_status; the call's outputs are then undefined, the workspace and the
  * library remain usable).  This call sets the limit for launches made after it, process-wide:
  *   limit_ns      time after which a wait gives up; 0 restores the default of 2 s
  *   expire_roles  for failure-handling tests: waits of the named roles give up at once, whatever their state
  *                 (1 load warp, 2 tensor-core issue warp, 4 epilogue warps; 8, 16, 32 the same in the kernels that run
- *                 on pairs of multiprocessors alone: density sweep, key projection; 0 = none)
+ *                 on pairs of multiprocessors alone: density sweep, key projection; and in the attention of many query
+ *                 rows over the cache; 0 = none)
  * Always returns VITCOP_OK. */
 int vitcop_set_wait_limit(unsigned long long limit_ns, int expire_roles);
 
