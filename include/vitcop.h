@@ -356,7 +356,7 @@ int vitcop_kproj_knorm(const void* hidden, const void* W_k, int B, int N, int Dh
  *   new_len     int32 [B] out: cache_len[b] + rows of the sample, also where they did not all fit: rows from Ncap on are not
  *               written.  Must not overlap cache_len or another input.
  * (A pointer to nothing, as an empty cache, no samples, no rows, may be NULL in all three calls.)
- * Errors: INVALID_ARG (NULL cache/new_len, K and V both NULL, negative sizes or strides, span outside the sequence, overlap),
+ * Errors: INVALID_ARG (NULL cache/new_len, K and V both NULL, negative sizes or strides, d 0, span outside the sequence, overlap),
  * UNSUPPORTED (d, Ncap % 32, alignment, more than 2^31 - 1 rows), CUDA. */
 int vitcop_cache_write(const void* K, const void* V, int B, int H, int N, int d,
                        int64_t k_stride_b, int64_t k_stride_h, int64_t k_stride_n,
@@ -386,7 +386,7 @@ int vitcop_cache_read(const void* cache, int B, int H, int Ncap, int d, const in
  * Many query rows (more than 32 of a stored head, d 64 or 128, long enough a cache) run through a kernel whose waits are bounded
  * (vitcop_set_wait_limit): the status word is TIMEOUT, and out unspecified, where one ran out.  It holds the values of V as the
  * largest of a head allow; where some are 2^24 times smaller, the rows concerned are done anew, some 100 times slower.
- * Errors: INVALID_ARG (NULL q/cache/out, negative sizes or strides, Hq no multiple of H, a scale that is no number or infinite,
+ * Errors: INVALID_ARG (NULL q/cache/out, negative sizes or strides, d 0, Hq no multiple of H, a scale that is no number or infinite,
  * rows of out that share elements, overlap), UNSUPPORTED (d, Ncap % 32,
  * alignment, more than 2^31 - 1 query rows), WORKSPACE, CUDA. */
 int vitcop_cache_attention(const void* q, const void* cache, int B, int Hq, int H, int Tq, int d, int Ncap,

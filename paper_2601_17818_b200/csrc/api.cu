@@ -471,7 +471,7 @@ int vitcop_cache_write(const void* K, const void* V, int B, int H, int N, int d,
                        int64_t k_stride_n, int64_t v_stride_b, int64_t v_stride_h, int64_t v_stride_n, const int32_t* seq_len,
                        int vis_start, const int32_t* vis_len, int vis_len_uniform, const int32_t* keep_idx, int keep_stride,
                        const int32_t* n_keep, const int32_t* cache_len, void* cache, int Ncap, int32_t* new_len, void* stream) {
-    if (B < 0 || H < 0 || N < 0 || d < 0 || Ncap < 0) return VITCOP_ERR_INVALID_ARG;
+    if (B < 0 || H < 0 || N < 0 || d <= 0 || Ncap < 0) return VITCOP_ERR_INVALID_ARG;
     if ((!K && !V && extent(B, H, N, d, 0, 0, 0) > 0) || (!new_len && B > 0)) return VITCOP_ERR_INVALID_ARG;
     const int64_t strides[6] = {k_stride_b, k_stride_h, k_stride_n, v_stride_b, v_stride_h, v_stride_n};
     for (int i = 0; i < 6; ++i)
@@ -505,7 +505,7 @@ int vitcop_cache_write(const void* K, const void* V, int B, int H, int N, int d,
 
 int vitcop_cache_read(const void* cache, int B, int H, int Ncap, int d, const int32_t* cache_len, const int32_t* row_begin,
                       int row_begin_uniform, void* K_out, void* V_out, int N_out, void* stream) {
-    if (B < 0 || H < 0 || Ncap < 0 || d < 0 || N_out < 0) return VITCOP_ERR_INVALID_ARG;
+    if (B < 0 || H < 0 || Ncap < 0 || d <= 0 || N_out < 0) return VITCOP_ERR_INVALID_ARG;
     if (!K_out && !V_out && extent(B, H, N_out, d, 0, 0, 0) > 0) return VITCOP_ERR_INVALID_ARG;
     if (!row_begin && row_begin_uniform < 0) return VITCOP_ERR_INVALID_ARG;
     const int rc = check_cache(B, H, Ncap, d, cache);
@@ -525,7 +525,7 @@ int vitcop_cache_attention(const void* q, const void* cache, int B, int Hq, int 
                            int64_t q_stride_h, int64_t q_stride_t, const int32_t* cache_len, float scale, int causal, void* out,
                            int64_t out_stride_b, int64_t out_stride_h, int64_t out_stride_t, float* lse, void* workspace,
                            size_t workspace_bytes, void* stream) {
-    if (B < 0 || Hq < 0 || H < 0 || Tq < 0 || d < 0 || Ncap < 0) return VITCOP_ERR_INVALID_ARG;
+    if (B < 0 || Hq < 0 || H < 0 || Tq < 0 || d <= 0 || Ncap < 0) return VITCOP_ERR_INVALID_ARG;
     if ((!q || !out) && extent(B, Hq, Tq, d, 0, 0, 0) > 0) return VITCOP_ERR_INVALID_ARG;
     if (!(scale - scale == 0.f)) return VITCOP_ERR_INVALID_ARG;            // (NaN, infinite)
     if (H > 0 ? Hq % H != 0 : Hq != 0) return VITCOP_ERR_INVALID_ARG;
