@@ -336,32 +336,38 @@ def alloc_cache(B: int, H: int, Ncap: int, d: int, device="cuda") -> torch.Tenso
     return torch.empty((B, H, Ncap // 32, 40 * d), dtype=torch.uint8, device=device)
 
 
-def _cache_call(name: str, *args) -> None:
-    """The calls of the cache: their tensors are checked (ValueError) and taken apart in the extension."""
-    if _native is None:
-        lib()
-    device = _device()
-    rc = getattr(_module, name)(_raw_stream(device), device, *args)
-    if rc != OK:
-        raise VitcopError(rc, "vitcop_" + name)
-
-
+# (the calls of the cache: their tensors are checked (ValueError) and taken apart in the extension)
 def vitcop_cache_write(K, V, cache, new_len, cache_len=None, seq_len=None, vis_start: int = 0, vis_len=0, keep_idx=None, n_keep=None):
     """Rows of K and V (bf16 [B,H,N,d], any leading strides) to ``cache`` in 4 bits, from row ``cache_len`` on: all of them, or with
     ``keep_idx`` those that ``vitcop_compact_kv`` keeps.  Returns ``new_len``, the rows that are in the cache then."""
-    _cache_call("cache_write", K, V, cache, new_len, cache_len, seq_len, vis_start, vis_len, keep_idx, n_keep)
+    if _module is None:
+        lib()
+    device = _device()
+    rc = _module.cache_write(_raw_stream(device), device, K, V, cache, new_len, cache_len, seq_len, vis_start, vis_len, keep_idx, n_keep)
+    if rc:
+        raise VitcopError(rc, "vitcop_cache_write")
     return new_len
 
 
 def vitcop_cache_read(cache, cache_len, K_out=None, V_out=None, row_begin=0):
     """Rows of ``cache`` from ``row_begin`` (an int, or int32 [B]) on, up to ``cache_len`` (None: all), to bf16 [B,H,N_out,d]."""
-    _cache_call("cache_read", cache, cache_len, K_out, V_out, row_begin)
+    if _module is None:
+        lib()
+    device = _device()
+    rc = _module.cache_read(_raw_stream(device), device, cache, cache_len, K_out, V_out, row_begin)
+    if rc:
+        raise VitcopError(rc, "vitcop_cache_read")
     return K_out, V_out
 
 
 def vitcop_cache_attention(q, cache, cache_len, out, workspace, scale: float, causal: bool = True, lse=None):
     """softmax(scale q K^T) V over ``cache``: q, out bf16 [B,Hq,Tq,d] (any leading strides), the last Tq of ``cache_len`` tokens."""
-    _cache_call("cache_attention", q, cache, cache_len, out, workspace, scale, causal, lse)
+    if _module is None:
+        lib()
+    device = _device()
+    rc = _module.cache_attention(_raw_stream(device), device, q, cache, cache_len, out, workspace, scale, causal, lse)
+    if rc:
+        raise VitcopError(rc, "vitcop_cache_attention")
     return out
 
 

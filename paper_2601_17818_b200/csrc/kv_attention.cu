@@ -111,7 +111,7 @@ __device__ __forceinline__ void make_operand(QueryOperand<G>* to, const uint4* r
 
 // Where a CTA is in its share of the work: block `tile` of segment `seg` (head and tile of rows) of sample b, `left` blocks to go.
 struct Walk {
-    int b, seg, tile, blocks, left;
+    int b, seg, tile, blocks, left, len;                   // (len: of a CTA without a share)
 };
 __device__ __forceinline__ int len_of(const AttArgs& a, int b) { return a.cache_len ? max(0, min(__ldcg(a.cache_len + b), a.Ncap)) : a.Ncap; }
 __device__ __forceinline__ int blocks_of(const AttArgs& a, int b) { return (len_of(a, b) + kCacheBlock - 1) / kCacheBlock; }
@@ -221,8 +221,8 @@ cache_attention_kernel(AttArgs a) {
         now.b = blockIdx.x / segs;
         now.seg = blockIdx.x - now.b * segs;
         now.tile = 0;
-        now.blocks = blocks_of(a, now.b);
-        now.left = now.blocks;
+        now.len = len_of(a, now.b);
+        now.blocks = now.left = a.Ncap / kCacheBlock;      // (as long as the length is on its way)
     }
     const auto next = [&](Walk& w) {                       // to the piece behind
         w.left -= piece(w);
@@ -243,7 +243,7 @@ cache_attention_kernel(AttArgs a) {
     const auto first_block = [&](const Walk& w) {
         return a.cache + (((int64_t)w.b * a.H + quotient(w.seg, a.RT)) * (a.Ncap / kCacheBlock) + w.tile + warp) * L::kBytes + lane * 16;
     };
-    put(at_work, now);
+    if constexpr (SHARES) put(at_work, now);
     put(at_fetch, now);
     int ahead_left = piece(now) - warp;                    // blocks of the piece from this warp's next on
     const uint8_t* ahead_src = first_block(now);
@@ -290,13 +290,18 @@ cache_attention_kernel(AttArgs a) {
     };
 #pragma unroll
     for (int i = 0; i < kStages; ++i) fetch();
+    if constexpr (!SHARES) {                               // the first blocks have not waited for it
+        now.blocks = now.left = (now.len + kCacheBlock - 1) / kCacheBlock;
+        ahead_left += now.blocks - a.Ncap / kCacheBlock;
+        put(at_work, now);
+    }
     int use = 0;
 
     do {
         now = *at_work;
         const int b = now.b, h = quotient(now.seg, a.RT), row0 = (now.seg - h * (int)a.RT.d) * NR, rows = (int)a.R.d * a.Tq;
         const int count = piece(now);
-        const int len = SHARES ? before[a.B + 2 + b] : len_of(a, b);
+        const int len = SHARES ? before[a.B + 2 + b] : now.len;
         // (they came with the first block of warp 0)
         if (warp == 0) {
             asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
@@ -557,6 +562,7 @@ cache_attention_kernel(AttArgs a) {
         next(now);
         put(at_work, now);
     } while (now.left > 0);
+    if constexpr (!SHARES) asm volatile("cp.async.wait_all;" ::: "memory");      // (blocks behind the last)
 }
 
 // The pieces of a head and tile of rows that several CTAs shared, in their order: a warp takes 32 elements of a row at a time, four groups
