@@ -23,7 +23,7 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kStages = 2;
 constexpr uint32_t kOnes = 0x3F803F80u;                    // 1, twice, in bf16
-constexpr int kWholeBlocks = 24;                           // what pieces of heads cost, in blocks of a CTA
+constexpr int kWholeBlocks = 24;                           // what pieces of heads cost at least, in blocks of a CTA
 // Weights are 2^(logit - base) with a base that starts this far above the maximum: they stay below 2^-16, so that sums of weights times
 // values of V hold wherever those values lie in fp32's range, and the smallest that count are still 2^-100 of the largest.
 constexpr float kHeadroom = 24.f;
@@ -673,9 +673,24 @@ Plan plan_of(int B, int H, int Ncap, int d, int Tq, int Hq, int sms) {
     const int64_t segs = (int64_t)B * H * p.RT, blocks = Ncap / kCacheBlock;
     p.ctas = 0;
     p.wide = false;
-    if (segs < 4 * slots && blocks > kWholeBlocks && segs * blocks < 0x7fff0000) p.ctas = slots;
-    // (an SM for each: 64 heads of 20 rows, 733 tokens 9.2 us with four warps, 7.8 with eight)
-    if (p.ctas == 0 && segs <= sms && blocks > kWarps) p.wide = true;
+    // Blocks are shared out where that costs less (pieces, their join, the lengths in front) than what CTAs with a head each leave idle: SMs
+    // that have fewer heads, or shorter ones (taken for 5/8 of the capacity).  (Up to four rounds of heads: what launch() has room for.)
+    const bool one = segs <= sms, two = !one && segs <= 2 * sms && d * p.NT <= 128;
+    bool whole = blocks <= kWholeBlocks || segs >= 4 * slots || segs * blocks >= 0x7fff0000;
+    if (!whole && blocks <= 128 && (one || two)) {
+        // A head has an SM, or half of one, and eight warps.  128 heads, 1500 tokens: 13.1 us, shared out 17.2; 128 of 20 rows of 64,
+        // up to 1500: 13.1 and 20.5; 288 heads, 1000 tokens: 17.1 and 22.2; but 8 heads, 1000: 9.4 and 7.3, and 160, 1500: 20.3 and 20.7.
+        whole = one ? blocks * (27 * sms - 25 * segs) <= 675 * sms : blocks * (2 * sms - segs) <= 40 * sms;
+        p.wide = whole;
+    }
+    // (four warps a head, all heads at once, or some behind others: 512 heads, up to 777 tokens 15.8 us, shared out 17.1, up to 4000 66.6
+    // and 57.3; 384 of 20 rows of 64, up to 3000 43.5 and 56.1; 1024, up to 1000 33.2 and 39.6, up to 4000 109 and 103; 512 of 16 rows,
+    // up to 1000 28.3 and 58.5)
+    if (!whole && !one)
+        whole = segs <= slots ? 8 * blocks * slots <= 8 * (8 + 16 * p.NT) * slots + 5 * blocks * segs : blocks * slots <= (40 + 20 * p.NT) * segs;
+    // (a short head that has an SM to itself: 64 of 20 rows, 733 tokens 9.2 us with four warps, 7.8 with eight)
+    if (blocks <= kWholeBlocks) p.wide = one && blocks > kWarps;
+    if (!whole) p.ctas = slots;
     return p;
 }
 
