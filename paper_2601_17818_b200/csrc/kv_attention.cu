@@ -29,7 +29,7 @@ constexpr int kWholeBlocks = 24;                           // what pieces of hea
 constexpr float kHeadroom = 24.f;
 
 // Resident CTAs an SM, which the registers of the accumulators and the ring's memory leave room for.
-constexpr int ctas_per_sm(int D, int NT) { return D == 256 || D * NT > 256 || NT == 4 ? 2 : D * NT <= 128 ? 4 : 3; }
+constexpr int ctas_per_sm(int D, int NT) { return D == 256 || D * NT > 256 ? 2 : D * NT <= 128 ? 4 : 3; }
 
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -660,14 +660,18 @@ struct Plan {
 Plan plan_of(int B, int H, int Ncap, int d, int Tq, int Hq, int sms) {
     Plan p;
     const int64_t rows = (int64_t)(Hq / H) * Tq;
-    p.NT = rows <= 8 ? 1 : rows <= 16 || d == 256 ? 2 : rows <= 24 ? 3 : 4;
-    // short caches and few heads: tiles as narrow as leave an SM for each (20 rows of 64 heads, 733 tokens: 9.0 us in tiles of 16, 11.4 of 24)
-    if (Ncap <= 1024)
-        for (int n = 1; n < p.NT; ++n)
-            if ((int64_t)B * H * ((rows + 8 * n - 1) / (8 * n)) <= sms) {
-                p.NT = n;
-                break;
-            }
+    // (tiles of 32 rows leave an SM eight warps: 32 rows of 16 heads, 16000 tokens 40.9 us, in tiles of 16 36.7)
+    p.NT = rows <= 8 ? 1 : rows > 16 && rows <= 24 && d != 256 ? 3 : 2;
+    // Few heads, and not too much to read for each tile again: tiles as narrow as leave an SM for each.  20 rows of 64 heads, 733 tokens: 9.0 us in
+    // tiles of 16, 11.4 of 24; 64 rows of 16 heads, 1000 tokens: 9.5 in tiles of 8, 16.9 of 32; 20 rows of 8, 8000: 14.8 and 19.0 of 24; but
+    // 20 rows of 32, 4000: 24.2 in tiles of 8, 23.3 of 24.
+    for (int n = 1; n < p.NT; ++n) {
+        const int64_t tiles = (int64_t)B * H * ((rows + 8 * n - 1) / (8 * n));
+        if (tiles <= sms && tiles * (Ncap / kCacheBlock) <= 6400) {
+            p.NT = n;
+            break;
+        }
+    }
     p.RT = (int)((rows + 8 * p.NT - 1) / (8 * p.NT));
     const int slots = sms * ctas_per_sm(d, p.NT);
     const int64_t segs = (int64_t)B * H * p.RT, blocks = Ncap / kCacheBlock;
@@ -772,8 +776,8 @@ int launch_cache_attention(const CacheQueries& io, const void* cache, int B, int
     a.sign = scale < 0.f ? 0x80008000u : 0u;
     a.scale_log2 = a.zero ? 1.f : (scale < 0.f ? -scale : scale) * kLog2e;
     if (many) return launch_cache_attention_rows(a, d, workspace, stream);
-    if (d == 64) return p.NT == 1 ? launch<64, 1>(a, p, stream) : p.NT == 2 ? launch<64, 2>(a, p, stream) : p.NT == 3 ? launch<64, 3>(a, p, stream) : launch<64, 4>(a, p, stream);
-    if (d == 128) return p.NT == 1 ? launch<128, 1>(a, p, stream) : p.NT == 2 ? launch<128, 2>(a, p, stream) : p.NT == 3 ? launch<128, 3>(a, p, stream) : launch<128, 4>(a, p, stream);
+    if (d == 64) return p.NT == 1 ? launch<64, 1>(a, p, stream) : p.NT == 2 ? launch<64, 2>(a, p, stream) : launch<64, 3>(a, p, stream);
+    if (d == 128) return p.NT == 1 ? launch<128, 1>(a, p, stream) : p.NT == 2 ? launch<128, 2>(a, p, stream) : launch<128, 3>(a, p, stream);
     return p.NT == 1 ? launch<256, 1>(a, p, stream) : launch<256, 2>(a, p, stream);
 }
 

@@ -744,9 +744,11 @@ int launch_rows(const RowsArgs& k, const RowsPlan& p, cudaStream_t stream) {
 
 }  // namespace
 
-// (64 rows of 8 heads, 600 tokens: 17 us here, 8 in tiles of 32 rows; of 16 heads, 3000 tokens: 21 and 28; 512 of 32, 4000: 106 and 226)
+// Where its start (10 us of a CTA) pays, and half a tile of rows is not empty.  64 rows of 32 heads, 1800 tokens: 23.3 us here, 18.0 in tiles of
+// 16; of 128 heads of 64, 300 tokens: 14.0 and 10.7; 68 rows of the same: 13.9 and 18.7; 64 of 16, 4000: 23.1 and 26.8; 448 of 8, 1500: 22.3
+// and 25.7; 512 of 32, 4000: 104 and some 220.
 bool rows_kernel_takes(int B, int H, int Ncap, int64_t rows, int d) {
-    return d != 256 && rows > 32 && (double)B * H * rows * Ncap >= 2e6;
+    return d != 256 && rows > 32 && (double)B * H * rows * Ncap >= (rows <= 64 ? 6e6 : 2e6);
 }
 
 size_t rows_workspace_bytes(int B, int H, int Ncap, int d, int Tq, int Hq) {

@@ -618,3 +618,34 @@ def test_two_streams_at_once_and_replays_with_other_lengths(B, H, R, Tq, d, Ncap
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(outs[2], w) and vb.vitcop_poll_status(ws[2]) == vb.OK
+
+
+@pytest.mark.parametrize("B,H,R,Tq,d,Ncap,lens,causal", [(4, 4, 1, 60, 64, 6304, [6300, 0, 31, 4097], True), (2, 6, 2, 32, 128, 8192, [8192, 100], False)])
+def test_half_a_tile_of_query_rows(B, H, R, Tq, d, Ncap, lens, causal):
+    q, cache, K, V = _problem(Tq + d, B, H, R, Tq, d, Ncap, lens, spread=1.5)
+    _poison(cache, lens)
+    out, lse = _attend(q, cache, lens, d ** -0.5, causal)
+    _check(q, cache, K, V, lens, d ** -0.5, causal, out, lse)
+
+
+@pytest.mark.parametrize("B,H,R,Tq,d,Ncap", [
+    (2, 64, 1, 1, 128, 1536), (5, 32, 1, 1, 64, 1024), (9, 32, 1, 1, 128, 896), (16, 32, 1, 1, 64, 800), (11, 64, 1, 1, 128, 896), (1, 8, 1, 1, 128, 1024),
+    (3, 32, 4, 4, 128, 1280), (8, 32, 4, 4, 64, 1024), (12, 32, 4, 5, 64, 864), (2, 4, 8, 5, 128, 1056), (3, 64, 4, 2, 256, 832), (2, 4, 8, 4, 64, 4096)])
+def test_however_heads_are_given_to_ctas(B, H, R, Tq, d, Ncap):
+    """A CTA a head (of four warps or of eight, all at once or not), or blocks shared out: lengths from none to all."""
+    rng = np.random.default_rng(B * H + Tq)
+    K, V = _bf16(rng, 1, H, Ncap, d).expand(B, H, Ncap, d), _bf16(rng, 1, H, Ncap, d).expand(B, H, Ncap, d)
+    cache, n = _cache(B, H, Ncap, d), _i32([0] * B)
+    lens = [0, Ncap, 33, Ncap - 1, 1, 257, Ncap // 2, 5, 700, 130, 64, 31, 500, 96, Ncap, 3][:B]
+    vb.vitcop_cache_write(K, V, cache, n, seq_len=_i32(lens))
+    q = _bf16(rng, B, H * R, Tq, d)
+    out, lse = _attend(q, cache, lens, d ** -0.5)
+    heads = sorted({0, 1, H // 2, H - 1})                  # (the oracle looks at some of them)
+    rows = [h * R + i for h in heads for i in range(R)]
+    held = [tuple(np.repeat(x, B, 0) for x in oc.quantise(_f64(t[:1, heads]))) for t in (K, V)]
+    _check(q[:, rows], cache, *held, lens, d ** -0.5, True, out[:, rows], lse[:, rows])
+    for h in range(H):                                     # and the others against it: the cache is the same for all calls
+        if h % 7 == 3:
+            one, _ = _attend(q[:, h * R:(h + 1) * R], cache[:, h:h + 1].contiguous(), lens, d ** -0.5)
+            # (each is off by at most HALF (|out| + 2 |code - 8| s + 2 |m|), and values reach 5)
+            assert (one.float() - out[:, h * R:(h + 1) * R].float()).abs().max() <= 2 * HALF * 3 * 5
