@@ -681,9 +681,10 @@ Plan plan_of(int B, int H, int Ncap, int d, int Tq, int Hq, int sms) {
     // that have fewer heads, or shorter ones (taken for 5/8 of the capacity).  (Up to four rounds of heads: what launch() has room for.)
     const bool one = segs <= sms, two = !one && segs <= 2 * sms && d * p.NT <= 128;
     bool whole = blocks <= kWholeBlocks || segs >= 4 * slots || segs * blocks >= 0x7fff0000;
-    if (!whole && blocks <= 128 && (one || two)) {
+    if (!whole && ((one && blocks <= 128) || (two && blocks <= 64))) {
         // A head has an SM, or half of one, and eight warps.  128 heads, 1500 tokens: 13.1 us, shared out 17.2; 128 of 20 rows of 64,
-        // up to 1500: 13.1 and 20.5; 288 heads, 1000 tokens: 17.1 and 22.2; but 8 heads, 1000: 9.4 and 7.3, and 160, 1500: 20.3 and 20.7.
+        // up to 1500: 13.1 and 20.5; 288 heads, 1000 tokens: 17.1 and 22.2; but 8 heads, 1000: 9.4 and 7.3, and 160, 1500: 20.3 and 20.7,
+        // 256, up to 2944 (six draws of the lengths): 29.3 and 28.5.
         whole = one ? blocks * (27 * sms - 25 * segs) <= 675 * sms : blocks * (2 * sms - segs) <= 40 * sms;
         p.wide = whole;
     }
