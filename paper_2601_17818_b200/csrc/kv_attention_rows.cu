@@ -46,8 +46,11 @@ struct RowsSmem {
     static constexpr int kRaw = kStage + kStages * kStageBytes;              // two tiles as they lie in the cache
     static constexpr int kRawBytes = 2 * CacheBlock<D>::kBytes;
     static constexpr int kBars = kRaw + 2 * kRawBytes;
-    static constexpr int kPairs = kBars + 256;                         // fp32 [2][128 rows]: what the two threads of a row tell each other
-    static constexpr int kTable = kPairs + 1024;                       // fp16 [2][G][64 tokens]: scales and centres of V, times the power of two
+    // What the two threads of a row tell each other, fp32 [2][128 rows] each: maxima, tile by tile, and the sums at the end.  (Arrays of their
+    // own: nothing holds a thread up between its partner's last maximum and its own sum.)
+    static constexpr int kPairs = kBars + 256;
+    static constexpr int kEnds = kPairs + 1024;
+    static constexpr int kTable = kEnds + 1024;                       // fp16 [2][G][64 tokens]: scales and centres of V, times the power of two
     static constexpr int kBytes = kTable + 1024 + 1024;                  // (and what aligning to 1024 takes)
 };
 
@@ -141,6 +144,7 @@ cache_attention_rows_kernel(RowsArgs k) {
     uint32_t* const bounds = reinterpret_cast<uint32_t*>(smem + S::kBars + 192);     // [8] largest value of V that a warp has found possible
     int* const exponents = reinterpret_cast<int*>(smem + S::kBars + 224);           // [kStages] of that power of two, as a float's bits have it
     float* const pairs = reinterpret_cast<float*>(smem + S::kPairs);
+    float* const ends = reinterpret_cast<float*>(smem + S::kEnds);
     volatile int* const far_apart = reinterpret_cast<volatile int*>(smem + S::kBars + 240);
     int* const first_bad = reinterpret_cast<int*>(smem + S::kBars + 144);       // [G] first token whose values of V are no numbers
     const int tid = threadIdx.x, warp = tid >> 5;
@@ -327,10 +331,10 @@ cache_attention_rows_kernel(RowsArgs k) {
             mbar_arrive(bar_p);
         }
         if (ok && n > 0 && warp == 0) ok = mbar_wait(bar_pv, (n - 1) & 1, abort_flag, lim);
-        pairs[half * kRows + rl] = sum;
+        ends[half * kRows + rl] = sum;
         if (!epi_bar_or<kSoftmaxThreads>(!ok)) {
             tc_fence_after();
-            sum += pairs[(half ^ 1) * kRows + rl];
+            sum += ends[(half ^ 1) * kRows + rl];
             const bool none = sum == 0.f, alone = k.splits == 1;
             uint32_t weight[1][8] = {};
             if (n > 0) {

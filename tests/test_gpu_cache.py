@@ -649,3 +649,16 @@ def test_however_heads_are_given_to_ctas(B, H, R, Tq, d, Ncap):
             one, _ = _attend(q[:, h * R:(h + 1) * R], cache[:, h:h + 1].contiguous(), lens, d ** -0.5)
             # (each is off by at most HALF (|out| + 2 |code - 8| s + 2 |m|), and values reach 5)
             assert (one.float() - out[:, h * R:(h + 1) * R].float()).abs().max() <= 2 * HALF * 3 * 5
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_many_query_rows_of_one_tile(d):
+    """CTAs that have one tile of tokens, whose maximum always moves; logits far enough from 0 that another's would show."""
+    B, H, R, Tq, Ncap = 66, 4, 2, 64, 256
+    lens = [[64, 33, 1, 40, 63][b % 5] for b in range(B)]
+    q, cache, K, V = _problem(d + 7, B, H, R, Tq, d, Ncap, lens, spread=3.0)
+    out, lse = _attend(q, cache, lens, d ** -0.5, False)
+    _check(q, cache, K, V, lens, d ** -0.5, False, out, lse)
+    for _ in range(30):
+        again, lse2 = _attend(q, cache, lens, d ** -0.5, False)
+        assert torch.equal(again, out) and torch.equal(lse2, lse)
