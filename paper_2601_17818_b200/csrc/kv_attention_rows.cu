@@ -165,6 +165,12 @@ cache_attention_rows_kernel(RowsArgs k) {
         for (int i = 0; i < G; ++i) first_bad[i] = 0x7fffffff;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    // the row of ones, whose product is the sum of the weights as they are rounded: what the output is divided by.  (In front of
+    // the barrier: where there is no tile, the output goes through the same bytes with no other in between.)
+    if (tid >= kSoftmaxThreads && tid < kSoftmaxThreads + kUnpackThreads)
+        for (int i = tid - kSoftmaxThreads; i < kStages * 128; i += kUnpackThreads)
+            *reinterpret_cast<uint4*>(smem + S::kStage + (i >> 7) * S::kStageBytes + S::kV + D * 128 + (i & 127) * 16) =
+                (i & 127) < 8 ? make_uint4(0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u) : make_uint4(0, 0, 0, 0);
     if (warp == kThreads / 32 - 1) tmem_alloc(smem_u32(tmem_slot), kTmem);
     tc_fence_before();
     __syncthreads();
@@ -182,12 +188,6 @@ cache_attention_rows_kernel(RowsArgs k) {
     const int tiles = (most + kTokens - 1) / kTokens;
     const int each = tiles / k.splits, more = tiles - each * k.splits, t0 = split * each + min(split, more), n = each + (split < more ? 1 : 0);
     const uint8_t* const head = a.cache + ((int64_t)b * a.H + h) * (a.Ncap / kCacheBlock) * L::kBytes;
-
-    // the row of ones, whose product is the sum of the weights as they are rounded: what the output is divided by
-    if (tid >= kSoftmaxThreads && tid < kSoftmaxThreads + kUnpackThreads)
-        for (int i = tid - kSoftmaxThreads; i < kStages * 128; i += kUnpackThreads)
-            *reinterpret_cast<uint4*>(smem + S::kStage + (i >> 7) * S::kStageBytes + S::kV + D * 128 + (i & 127) * 16) =
-                (i & 127) < 8 ? make_uint4(0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u) : make_uint4(0, 0, 0, 0);
 
     // this thread's row as operand
     const int rl = tid & (kRows - 1), r = row0 + rl, tq = r < rows ? quotient(r, a.R) : 0, hq = h * (int)a.R.d + (r - tq * (int)a.R.d);

@@ -662,3 +662,17 @@ def test_many_query_rows_of_one_tile(d):
     for _ in range(30):
         again, lse2 = _attend(q, cache, lens, d ** -0.5, False)
         assert torch.equal(again, out) and torch.equal(lse2, lse)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,H,Ncap", [(66, 4, 256), (2, 4, 4096)])
+def test_many_query_rows_and_samples_without_a_tile(d, B, H, Ncap):
+    """CTAs that see no token (all of a head, or a piece of one) write zeros."""
+    R, Tq = 2, 64
+    lens = [[0, 64, 0, 5][b % 4] for b in range(B)]
+    q, cache, K, V = _problem(d + 8, B, H, R, Tq, d, Ncap, lens)
+    for _ in range(30):
+        out, lse = _attend(q, cache, lens, d ** -0.5, False)
+        for b in range(0, B, 2):
+            assert torch.all(out[b] == 0) and torch.all(torch.isneginf(lse[b]))
+    _check(q, cache, K, V, lens, d ** -0.5, False, out, lse)

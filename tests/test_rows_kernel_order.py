@@ -29,3 +29,9 @@ def test_a_rows_two_sums_do_not_take_the_place_of_its_maxima(kernel):
     with open(os.path.join(CSRC, "kv_attention_rows.cu")) as fh:
         at = dict(re.findall(r"static constexpr int (kPairs|kEnds|kTable) = (\w+ \+ \d+);", fh.read()))
     assert at == {"kPairs": "kBars + 256", "kEnds": "kPairs + 1024", "kTable": "kEnds + 1024"}      # (2 * 128 * 4 bytes each)
+
+
+def test_the_row_of_ones_is_written_in_front_of_the_first_barrier(kernel):
+    """A CTA without a tile turns its output in the bytes of the first stage, where the ones are, and meets no barrier on the way."""
+    ones, barrier, turn = kernel.index("0x3C003C00u"), kernel.index("__syncthreads();"), kernel.index("float* const turn")
+    assert ones < barrier < turn
