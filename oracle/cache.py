@@ -24,6 +24,10 @@ def quantise(x):
         s = round_bf16((hi - lo) / 15)
         s = np.where(s < 2.0 ** -100, 0.0, s)
         m = round_bf16(lo + 8 * s)
+        # (fp64 loses an element below 2^-53 of the centre, and with it the side of a border it is on.  The centre is a border, or 2^-10
+        # of a step and more away from one, and at most 8.5 steps from 0: an element of 2^-40 of it is on the same side)
+        least = np.ldexp(np.abs(m[..., None]), -40)
+        x = np.where(x == 0, 0.0, np.copysign(np.maximum(np.abs(x), least), x))
         q = np.rint((x - m[..., None]) / np.where(s > 0, s, 1.0)[..., None])
         code = np.where(s[..., None] > 0, np.clip(q, -8, 7), 0.0) + 8
     s, m = np.where(bad, np.nan, s), np.where(bad, 0.0, m)

@@ -178,3 +178,17 @@ def test_a_pointer_to_nothing_may_be_null(L):
     for nothing in (dict(Tq=0), dict(B=0), dict(H=0, Hq=0)):       # (as far as the workspace, which is asked for last)
         assert _attend(L, q=NULL, out=NULL, ws=NULL, cache=C_, **nothing) == vb.ERR_WORKSPACE
     assert _attend(L, cache=NULL, Ncap=0, ws=NULL) == vb.ERR_WORKSPACE
+
+
+def test_codes_by_exact_fractions():
+    """Elements of any size beside their centre, down to the last bf16 there is: the nearest code, computed with fractions."""
+    from fractions import Fraction
+    rng = np.random.default_rng(6)
+    for trial in range(200):
+        x = oc.round_bf16(rng.standard_normal(32) * np.exp2(-rng.integers(0, 130, 32).astype(np.float64)))
+        x[:2] = [(-0.9375, 0.9375), (-15.0, 15.0), (-0.8125, 1.0625), (oc.round_bf16(rng.standard_normal()) - 2, 2.5)][trial % 4]
+        x = oc.round_bf16(x)
+        s, m, code = oc.quantise(x)
+        for e in range(32):
+            q = (Fraction(float(x[e])) - Fraction(float(m[0]))) / Fraction(float(s[0]))
+            assert code[0, e] == min(max(round(q), -8), 7) + 8         # (Python's: halves to even)

@@ -676,3 +676,22 @@ def test_many_query_rows_and_samples_without_a_tile(d, B, H, Ncap):
         for b in range(0, B, 2):
             assert torch.all(out[b] == 0) and torch.all(torch.isneginf(lse[b]))
     _check(q, cache, K, V, lens, d ** -0.5, False, out, lse)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_elements_far_below_the_centre_fall_to_their_side_of_a_border(d):
+    """Where the centre is a whole number of steps and a half away from 0, an element's sign decides, however small it is; 0 itself is a tie."""
+    rng = np.random.default_rng(d)
+    N = 64
+    x = rng.choice([1.0, -1.0, 0.0], (1, 2, N, d)) * np.exp2(-rng.integers(17, 118, (1, 2, N, d)).astype(np.float64))
+    group = x.reshape(-1, 32)
+    ends = rng.integers(0, 4, len(group))
+    lo, hi = np.array([-0.9375, -0.8125, -1.0, -15.0])[ends], np.array([0.9375, 1.0625, 0.875, 15.0])[ends]
+    group[np.arange(len(group)), rng.integers(0, 16, len(group))] = lo
+    group[np.arange(len(group)), rng.integers(16, 32, len(group))] = hi
+    s, m, _ = oc.quantise(x)
+    assert (2 * m / s % 2 == 1).mean() > 0.6               # (three of the four pairs of ends; the other has its centre at 0)
+    x = torch.from_numpy(x.astype(np.float32)).bfloat16().to(DEV)
+    cache, n = _cache(1, 2, N, d), _i32([0])
+    vb.vitcop_cache_write(x, x, cache, n)
+    _same_rows(cache, 0, list(range(N)), _f64(x)[0], _f64(x)[0])
