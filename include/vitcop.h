@@ -387,8 +387,8 @@ int vitcop_cache_read(const void* cache, int B, int H, int Ncap, int d, const in
  * (vitcop_set_wait_limit): the status word is TIMEOUT, and out unspecified, where one ran out.  It holds the values of V as the
  * largest of a head allow; where some are 2^24 times smaller, the rows concerned are done anew, some 100 times slower.
  * Errors: INVALID_ARG (NULL q/cache/out, negative sizes or strides, d 0, Hq no multiple of H, a scale that is no number or infinite,
- * rows of out that share elements, overlap), UNSUPPORTED (d, Ncap % 32,
- * alignment, more than 2^31 - 1 query rows), WORKSPACE, CUDA. */
+ * rows of out that share elements (or lie interleaved: in the order of strides, each dimension has to step over what those below it reach),
+ * overlap), UNSUPPORTED (d, Ncap % 32, alignment, more than 2^31 - 1 query rows), WORKSPACE, CUDA. */
 int vitcop_cache_attention(const void* q, const void* cache, int B, int Hq, int H, int Tq, int d, int Ncap,
                            int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_t,
                            const int32_t* cache_len, float scale, int causal,

@@ -1,4 +1,5 @@
 // Public C ABI of libvitcop: argument validation, workspace carving and dispatch to the launchers.
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <cstdint>
@@ -461,6 +462,22 @@ static size_t extent(int B, int H, int N, int d, int64_t sb, int64_t sh, int64_t
     return ((size_t)(B - 1) * (size_t)sb + (size_t)(H - 1) * (size_t)sh + (size_t)(N - 1) * (size_t)sn + (size_t)d) * 2;
 }
 
+// Whether rows of such a tensor share elements: in the order of their strides, each dimension has to step over what those before it reach.
+static bool rows_share(int B, int H, int N, int d, int64_t sb, int64_t sh, int64_t sn) {
+    struct Dim {
+        int64_t n, stride;
+    } dims[3] = {{B, sb}, {H, sh}, {N, sn}};
+    std::sort(dims, dims + 3, [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
+    int64_t reach = d;
+    for (const Dim& dim : dims) {
+        if (dim.n <= 1) continue;
+        if (dim.stride < reach) return true;
+        int64_t span;
+        if (__builtin_mul_overflow(dim.n - 1, dim.stride, &span) || __builtin_add_overflow(reach, span, &reach)) return true;
+    }
+    return false;
+}
+
 static int check_cache(int B, int H, int Ncap, int d, const void* cache) {
     if (!cache && cache_bytes(B, H, Ncap, d) > 0) return VITCOP_ERR_INVALID_ARG;
     if ((d != 64 && d != 128 && d != 256) || Ncap % kCacheBlock || !aligned16(cache)) return VITCOP_ERR_UNSUPPORTED;
@@ -538,8 +555,7 @@ int vitcop_cache_attention(const void* q, const void* cache, int B, int Hq, int 
         if (strides[i] % 8) return VITCOP_ERR_UNSUPPORTED;
     if (!aligned16(q) || !aligned16(out) || B > 65535) return VITCOP_ERR_UNSUPPORTED;
     // (rows of the output that share elements have no value)
-    if (extent(B, Hq, Tq, d, 0, 0, 0) > 0 && ((B > 1 && out_stride_b < d) || (Hq > 1 && out_stride_h < d) || (Tq > 1 && out_stride_t < d)))
-        return VITCOP_ERR_INVALID_ARG;
+    if (extent(B, Hq, Tq, d, 0, 0, 0) > 0 && rows_share(B, Hq, Tq, d, out_stride_b, out_stride_h, out_stride_t)) return VITCOP_ERR_INVALID_ARG;
     if ((int64_t)B * Hq * Tq > 0x7fffffff) return VITCOP_ERR_UNSUPPORTED;
     const size_t need = cache_attention_workspace_bytes(B, H, Ncap, d, Tq, Hq);
     const size_t obytes = extent(B, Hq, Tq, d, out_stride_b, out_stride_h, out_stride_t);

@@ -192,3 +192,14 @@ def test_codes_by_exact_fractions():
         for e in range(32):
             q = (Fraction(float(x[e])) - Fraction(float(m[0]))) / Fraction(float(s[0]))
             assert code[0, e] == min(max(round(q), -8), 7) + 8         # (Python's: halves to even)
+
+
+@pytest.mark.parametrize("B,Hq,Tq,strides,shared", [
+    (2, 4, 2, (256, 64, 64), True), (2, 4, 2, (512, 64, 64), True), (2, 4, 2, (64, 128, 512), False), (2, 4, 2, (448, 64, 256), True),
+    (2, 4, 2, (0, 128, 64), True), (2, 1, 2, (64, 0, 64), True), (1, 4, 2, (0, 128, 120), True), (2, 4, 2, (1 << 62, 1 << 62, 64), True),
+    (2, 4, 2, (512, 128, 64), False), (2, 4, 2, (512, 64, 256), False), (2, 4, 2, (64, 256, 128), False), (1, 1, 1, (0, 0, 0), False),
+    (1, 4, 2, (0, 64, 256), False), (2, 1, 2, (128, 0, 64), False), (2, 4, 2, (1024, 72, 328), False)])
+def test_attention_refuses_rows_of_the_output_that_share_elements(L, B, Hq, Tq, strides, shared):
+    """Together too: head 1 of the first query, and the first head of query 1.  (What passes is asked for its workspace next.)"""
+    status = _attend(L, B=B, Hq=Hq, H=min(Hq, 2), Tq=Tq, qs=(512, 128, 64), os=strides, ws=NULL)
+    assert status == (vb.ERR_INVALID_ARG if shared else vb.ERR_WORKSPACE)
