@@ -384,8 +384,9 @@ int vitcop_cache_read(const void* cache, int B, int H, int Ncap, int d, const in
  *   lse     fp32 [B, Hq, Tq] out, optional: log of the sum of exp(scale * q k) over the rows seen
  *   workspace  vitcop_workspace_bytes(VITCOP_OP_CACHE_ATTENTION, B, H, Ncap, d, Tq, Hq, 0) bytes
  * Many query rows (more than 32 of a stored head, d 64 or 128, long enough a cache) run through a kernel whose waits are bounded
- * (vitcop_set_wait_limit): the status word is TIMEOUT, and out unspecified, where one ran out.  It holds the values of V as the
- * largest of a head allow; where some are 2^24 times smaller, the rows concerned are done anew, some 100 times slower.
+ * (vitcop_set_wait_limit): the status word is TIMEOUT, and out unspecified, where one ran out.  It holds weights and values of V in fp16, as the
+ * largest of a head allow.  A row whose output that may put off by 2^-8 of the largest in a group of 32 elements (it looks at little but tokens
+ * whose values are 2^20 times and more below others', or the group is some 2^25 times below another) is done anew in fp32, some 200 times slower.
  * Errors: INVALID_ARG (NULL q/cache/out, negative sizes or strides, d 0, Hq no multiple of H, a scale that is no number or infinite,
  * rows of out that share elements (or lie interleaved: in the order of strides, each dimension has to step over what those below it reach),
  * overlap), UNSUPPORTED (d, Ncap % 32, alignment, more than 2^31 - 1 query rows), WORKSPACE, CUDA. */

@@ -26,10 +26,15 @@ constexpr int kSoftmaxThreads = 256, kUnpackThreads = 256, kThreads = kSoftmaxTh
 constexpr int kStages = 3, kMostSplits = 16;
 constexpr uint32_t kTmem = 512;
 enum { kRoleUnpack = 1, kRoleMma = 2, kRoleSoftmax = 4 };
-// What a CTA reports.  Far apart: in units of the largest value of V so far, which its power of two goes by, those of some token and group
-// (of 32 elements) are too small for fp16, although they may be all that a row or a column has.  The join does its rows anew, in fp32.
-enum { kGaveUp = 1, kFarApart = 2 };
-constexpr int kApart = 24;                                 // powers of two: fp16 has 2^-12 of a group's largest value, or more, left there
+// What a CTA reports: whether a wait ran out, and a bit for each of its rows that fp16 does not hold, which the join does anew in fp32.
+// Weights are off by 2^-25 at most where they are small, and values of V (in the units that their power of two makes: the largest is below 2^15)
+// by 2^-25, so that a row's sum over the N tokens of the CTA is off by N 2^-25 V + W 2^-25 in a group of 32 elements whose largest value is
+// V, with W the sum of the row's weights, 2^7 at least.  A row is reported where that is more than 2^-8 of the largest of the group's 32
+// sums: it looks at little but tokens with far smaller values than others have, or the whole group is some 2^-25 of another.
+struct Report {
+    uint32_t gave_up, rows[kRows / 32];
+};
+constexpr float kLostOf = 0x1p-17f;                        // 2^-25 over 2^-8
 
 template <int D>
 struct RowsSmem {
@@ -51,12 +56,13 @@ struct RowsSmem {
     static constexpr int kPairs = kBars + 256;
     static constexpr int kEnds = kPairs + 1024;
     static constexpr int kTable = kEnds + 1024;                       // fp16 [2][G][64 tokens]: scales and centres of V, times the power of two
-    static constexpr int kBytes = kTable + 1024 + 1024;                  // (and what aligning to 1024 takes)
+    static constexpr int kAnew = kTable + 1024;                        // [2][4] rows to be done anew, as the two halves of the softmax warps find
+    static constexpr int kBytes = kAnew + 32 + 1024;                     // (and what aligning to 1024 takes)
 };
 
 struct RowsArgs {
     AttArgs a;
-    uint8_t* reports;                                      // a byte a CTA
+    Report* reports;                                       // one a CTA
     int splits;
     unsigned long long wait_ns;
     int expire_roles;
@@ -145,7 +151,8 @@ cache_attention_rows_kernel(RowsArgs k) {
     int* const exponents = reinterpret_cast<int*>(smem + S::kBars + 224);           // [kStages] of that power of two, as a float's bits have it
     float* const pairs = reinterpret_cast<float*>(smem + S::kPairs);
     float* const ends = reinterpret_cast<float*>(smem + S::kEnds);
-    volatile int* const far_apart = reinterpret_cast<volatile int*>(smem + S::kBars + 240);
+    uint32_t* const greatest = reinterpret_cast<uint32_t*>(smem + S::kBars + 176);   // [G] largest value of V that a group has, as a float's bits
+    uint32_t* const anew = reinterpret_cast<uint32_t*>(smem + S::kAnew);
     int* const first_bad = reinterpret_cast<int*>(smem + S::kBars + 144);       // [G] first token whose values of V are no numbers
     const int tid = threadIdx.x, warp = tid >> 5;
     if (tid == 0) {
@@ -160,9 +167,13 @@ cache_attention_rows_kernel(RowsArgs k) {
         mbar_init(bar_drain, 1);
         mbar_init(bar_drain + 8, 1);
         mbar_init(bar_q, kRows);
-        *abort_flag = *far_apart = 0;
+        *abort_flag = 0;
         moved[0] = moved[1] = moved[2] = 0;
-        for (int i = 0; i < G; ++i) first_bad[i] = 0x7fffffff;
+        for (int i = 0; i < G; ++i) {
+            first_bad[i] = 0x7fffffff;
+            greatest[i] = 0;
+        }
+        for (int i = 0; i < 8; ++i) anew[i] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     // the row of ones, whose product is the sum of the weights as they are rounded: what the output is divided by.  (In front of
@@ -341,7 +352,9 @@ cache_attention_rows_kernel(RowsArgs k) {
                 tmem_ld8_issue(tmem_o + lanes + D, weight[0]);
                 tmem_wait_ld(weight);
             }
-            const float inv = none ? 0.f : __int_as_float((exponent - 14) << 23) / __uint_as_float(weight[0][0]);
+            const float total = __uint_as_float(weight[0][0]), inv = none ? 0.f : __int_as_float((exponent - 14) << 23) / total;
+            const float lost_weights = (float)(n * kTokens) * kLostOf * __int_as_float((268 - exponent) << 23), lost_values = total * kLostOf;
+            bool redo = false;
             float* const part = a.part + (size_t)blockIdx.x * kRows * (D + 3);
             // (32 rows by 32 elements a warp, turned in shared memory that the tiles have left: 8 lanes then write a row)
             float* const turn = reinterpret_cast<float*>(smem + S::kStage) + warp * 32 * 36;
@@ -355,6 +368,12 @@ cache_attention_rows_kernel(RowsArgs k) {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[e] = 0.f;
                 }
+                // (all of a group may be 0, and the sums then are)
+                const float most_value = __uint_as_float(greatest[c]);
+                float largest = 0.f;
+#pragma unroll
+                for (int e = 0; e < 32; ++e) largest = fmaxf(largest, fabsf(v[e]));
+                redo |= most_value > 0.f && largest < fmaf(most_value, lost_weights, lost_values);
                 const bool bad = first_bad[c] < limit;     // a row of V that is no number, and that this query sees
                 const float times = bad ? __int_as_float(0x7fc00000) : inv;
 #pragma unroll
@@ -376,6 +395,8 @@ cache_attention_rows_kernel(RowsArgs k) {
                 }
                 __syncwarp();
             }
+            const uint32_t which = __ballot_sync(0xffffffffu, redo && r < rows && !none);
+            if (lane == 0) anew[warp] = which;
             if (r < rows && half == 0) {
                 if (!alone) {
                     part[kRows * D + rl] = top;
@@ -403,7 +424,8 @@ cache_attention_rows_kernel(RowsArgs k) {
         fetch(0);
         fetch(1);
         uint16_t* const table = reinterpret_cast<uint16_t*>(smem + S::kTable);
-        int exponent = 16, least_exponent = 255;           // (of the values that this thread has seen, zeros apart)
+        int exponent = 16;
+        uint32_t mine = 0;                                 // largest value of V in this thread's group, in its tokens
         bool ok = true;
         for (int i = 0; i < n; ++i) {
             if (i >= kStages && u < 32) ok = mbar_wait(bar_empty + 8 * (i % kStages), (i / kStages - 1) & 1, abort_flag, lim);
@@ -413,14 +435,14 @@ cache_attention_rows_kernel(RowsArgs k) {
             uint8_t* const stage = smem + S::kStage + i % kStages * S::kStageBytes;
             const int token0 = (t0 + i) * kTokens;
             // V's scale and centre of a token and group, a thread each, and the largest value that they allow.  What is no number would
-            // reach rows that do not see it: it is a zero here, and those that do see it are told.  So are rows behind the last.
+            // reach rows that do not see it: it is a zero here, and those that do see it are told.  So are tokens that no row sees.
             float scale = 0.f, centre = 0.f;
             if (u < kTokens * G) {
                 const int token = u / G, g = u % G, rb = token & 31;
                 const uint8_t* const block = raw + (token >> 5) * L::kBytes;
                 const float f = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(block + L::kVScale + (rb * G + g) * 2) << 16);
                 const float m = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(block + L::kVCentre + (g * 32 + rb) * 2) << 16);
-                if (token0 + token < len) {
+                if (token0 + token < most) {
                     if (f == f) {
                         scale = f;
                         centre = m;
@@ -430,7 +452,7 @@ cache_attention_rows_kernel(RowsArgs k) {
                 }
             }
             const uint32_t here = __float_as_uint(fmaf(8.f, fabsf(scale), fabsf(centre))), most_here = __reduce_max_sync(0xffffffffu, here);
-            if (here) least_exponent = min(least_exponent, (int)(here >> 23));
+            mine = max(mine, here);
             if ((u & 31) == 0) bounds[u >> 5] = most_here;
             {   // K: a thread a quarter of a token's row
                 const int row = u >> 2, t = u & 3, rb = row & 31;
@@ -487,13 +509,17 @@ cache_attention_rows_kernel(RowsArgs k) {
                     }
                 }
             }
+            if (i == n - 1) {                              // (thread u has group u % G in all tiles; where G = 2 half of them have none)
+#pragma unroll
+                for (int off = G; off < 32; off <<= 1) mine = max(mine, __shfl_xor_sync(0xffffffffu, mine, off));
+                if ((u & 31) < G) atomicMax(greatest + (u & 31), mine);
+            }
             fence_async_proxy();
             mbar_arrive(bar_full + 8 * (i % kStages));
             unpack_bar();                                  // (the raw tile has been read)
             fetch(i + 2);
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
-        if (least_exponent + kApart < exponent) *far_apart = 1;
     } else if (warp == kThreads / 32 - 2) {
         // ------------------------------------------------------------------ products with the queries
         // (the whole warp walks, so that the operands' addresses are known to be the same in all lanes; one lane issues)
@@ -543,7 +569,10 @@ cache_attention_rows_kernel(RowsArgs k) {
     if (tid == kSoftmaxThreads + kUnpackThreads) {
         mbar_drain(bar_drain, 0);
         mbar_drain(bar_drain + 8, 0);
-        k.reports[blockIdx.x] = (*abort_flag ? kGaveUp : 0) | (*far_apart ? kFarApart : 0);
+        Report& report = k.reports[blockIdx.x];
+        report.gave_up = *abort_flag != 0;
+#pragma unroll
+        for (int i = 0; i < kRows / 32; ++i) report.rows[i] = anew[i] | anew[kRows / 32 + i];
     }
     tc_fence_before();
     __syncthreads();
@@ -554,7 +583,7 @@ cache_attention_rows_kernel(RowsArgs k) {
 }
 
 // Row r of head h of sample b by one warp, from the cache, in fp32: a lane has a token of a block for its logit, and element `lane` of every
-// group for the output.  (512 rows of 32 heads, 4000 tokens: 10.8 ms, 0.1 where fp16 holds the values.)
+// group for the output.  (All 512 rows of 32 heads, 4000 tokens: 19.7 ms, 0.11 where fp16 holds them.)
 template <int D>
 __device__ __noinline__ void row_anew(const AttArgs& a, int b, int h, int r, float* q) {
     using L = CacheBlock<D>;
@@ -637,19 +666,17 @@ cache_attention_rows_join_kernel(const __grid_constant__ RowsArgs k, int ctas) {
     grid_dependency_wait();
     if (blockIdx.x == 0 && warp == 0) {
         bool gave_up = false;
-        for (int c = lane; c < ctas; c += 32) gave_up |= (k.reports[c] & kGaveUp) != 0;
+        for (int c = lane; c < ctas; c += 32) gave_up |= k.reports[c].gave_up != 0;
         gave_up = __any_sync(0xffffffffu, gave_up);
         if (lane == 0) *a.status = gave_up ? VITCOP_ERR_TIMEOUT : VITCOP_OK;
     }
     const int segs = a.H * (int)a.RT.d, items = a.B * segs * kRows;
-    if (k.splits == 1) {                                   // a CTA 32 rows, of those that it has to look at
+    if (k.splits == 1) {                                   // a CTA 32 rows at a time
         for (int item = blockIdx.x; item < items / kQuarter; item += gridDim.x) {
             const int seg = item / 4, b = seg / segs, hs = seg - b * segs, h = quotient(hs, a.RT);
-            if (!(k.reports[seg] & kFarApart)) continue;
-            for (int i = warp; i < kQuarter; i += 4) {
-                const int r = (hs - h * (int)a.RT.d) * kRows + (item % 4) * kQuarter + i;
-                if (r < rows) row_anew<D>(a, b, h, r, queries[warp]);
-            }
+            const uint32_t todo = k.reports[seg].rows[item % 4];
+            for (int i = warp; i < kQuarter; i += 4)
+                if (todo >> i & 1) row_anew<D>(a, b, h, (hs - h * (int)a.RT.d) * kRows + (item % 4) * kQuarter + i, queries[warp]);
         }
         return;
     }
@@ -663,10 +690,10 @@ cache_attention_rows_join_kernel(const __grid_constant__ RowsArgs k, int ctas) {
         static_assert(kMostSplits <= 32);
         const float* const mine = part + lane * kSize + kRows * D + rl;
         const bool there = lane < k.splits;
-        const uint8_t report = there ? k.reports[seg * k.splits + lane] : 0;
+        const bool redo = there && (k.reports[seg * k.splits + lane].rows[rl / 32] >> (rl % 32) & 1);
         const float piece = there ? mine[0] : kNoLogit;
         float top = piece, sum = there ? mine[kRows] : 0.f, weight = there ? mine[2 * kRows] : 0.f;
-        if (__any_sync(0xffffffffu, report & kFarApart)) {
+        if (__any_sync(0xffffffffu, redo)) {
             row_anew<D>(a, b, h, r, queries[warp]);
             continue;
         }
@@ -716,7 +743,7 @@ RowsPlan plan_of(int B, int H, int Ncap, int Tq, int Hq) {
     p.ctas = segs * p.splits;
     return p;
 }
-size_t reports_bytes(const RowsPlan& p) { return align_up((size_t)p.ctas, 256); }
+size_t reports_bytes(const RowsPlan& p) { return align_up((size_t)p.ctas * sizeof(Report), 256); }
 
 template <int D>
 int launch_rows(const RowsArgs& k, const RowsPlan& p, cudaStream_t stream) {
@@ -766,8 +793,8 @@ int launch_cache_attention_rows(const AttArgs& args, int d, void* workspace, cud
     RowsArgs k;
     k.a = args;
     k.a.RT = divisor(p.RT);
-    k.reports = static_cast<uint8_t*>(workspace) + kStatusBytes;
-    k.a.part = reinterpret_cast<float*>(k.reports + reports_bytes(p));
+    k.reports = reinterpret_cast<Report*>(static_cast<char*>(workspace) + kStatusBytes);
+    k.a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kStatusBytes + reports_bytes(p));
     k.splits = p.splits;
     k.wait_ns = gram_wait_limit_ns();
     k.expire_roles = pair_expire_roles();

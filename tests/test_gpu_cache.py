@@ -695,3 +695,42 @@ def test_elements_far_below_the_centre_fall_to_their_side_of_a_border(d):
     cache, n = _cache(1, 2, N, d), _i32([0])
     vb.vitcop_cache_write(x, x, cache, n)
     _same_rows(cache, 0, list(range(N)), _f64(x)[0], _f64(x)[0])
+
+
+@pytest.mark.parametrize("B,H,R,Tq,d,Ncap,n", [(1, 1, 4, 48, 128, 11008, 1500), (1, 2, 7, 48, 64, 4096, 300), (40, 4, 4, 20, 128, 352, 300)])
+def test_a_token_of_next_to_no_value_costs_other_rows_nothing(B, H, R, Tq, d, Ncap, n):
+    """Padding or a sink whose values are 2^-45 of the others': rows that look elsewhere are not done anew in fp32 (they are the bits that they
+    are with zeros there), those that look at nothing else are right."""
+    rng = np.random.default_rng(n + d)
+    K, V = _bf16(rng, B, H, n, d), _bf16(rng, B, H, n, d)
+    q = _bf16(rng, B, H * R, Tq, d)
+    K[:, :, 2] = 4.0                                       # the token that the odd queries look at
+    q[:, :, 1::2] = (0.3 * q[:, :, 1::2].float() + 3.0).bfloat16()
+    cache, lens = _cache(B, H, Ncap, d), _i32([0] * B)
+    V[:, :, 2] = 0.0
+    vb.vitcop_cache_write(K, V, cache, lens)
+    zeros, _ = _attend(q, cache, [n] * B, d ** -0.5)
+    V[:, :, 2] = _bf16(rng, B, H, d, spread=2.0 ** -45)
+    vb.vitcop_cache_write(K, V, cache, lens)
+    out, lse = _attend(q, cache, [n] * B, d ** -0.5)
+    _check(q, cache, oc.quantise(_f64(K)), oc.quantise(_f64(V)), [n] * B, d ** -0.5, True, out, lse)
+    assert torch.equal(out[:, :, ::2], zeros[:, :, ::2])
+
+
+def test_many_small_weights_on_large_values():
+    """A thousand tokens of 2^-33 of a row's weight each, with values 2^20 times those of the token that it looks at: a tenth of its output."""
+    B, H, n, d, R, Tq, Ncap = 37, 4, 1000, 128, 4, 48, 1024       # (more tiles of rows than SMs: a CTA has all tokens)
+    K = torch.zeros(B, H, n, d, dtype=torch.bfloat16, device=DEV)
+    V = torch.full((B, H, n, d), 2.0 ** 20, dtype=torch.bfloat16, device=DEV)
+    K[:, :, 7], V[:, :, 7] = 1.015625, 1.0
+    cache, lens = _cache(B, H, Ncap, d), _i32([0] * B)
+    vb.vitcop_cache_write(K, V, cache, lens)
+    q = torch.full((B, H * R, Tq, d), 2.0, dtype=torch.bfloat16, device=DEV)
+    out, lse = _attend(q, cache, [n] * B, d ** -0.5, causal=False)
+    z = 2 * 1.015625 * d ** 0.5
+    w = (n - 1) * np.exp(-z)
+    want = (1 + w * 2.0 ** 20) / (1 + w)
+    assert want > 1.1
+    # (all of the sums are exact but for the weights: 2^-8 each at most, and the rounding of the output)
+    assert (out.double() - want).abs().max() <= want * (2 * HALF + HALF ** 2)
+    assert (lse.double() - z - np.log1p(w)).abs().max() <= 2.0 ** -20 * (1 + z)
