@@ -734,3 +734,114 @@ def test_many_small_weights_on_large_values():
     # (all of the sums are exact but for the weights: 2^-8 each at most, and the rounding of the output)
     assert (out.double() - want).abs().max() <= want * (2 * HALF + HALF ** 2)
     assert (lse.double() - z - np.log1p(w)).abs().max() <= 2.0 ** -20 * (1 + z)
+
+
+@pytest.mark.parametrize("B,H,R,Tq,d,Ncap,lens", [
+    (1, 32, 1, 1, 128, 16512, [256]), (4, 32, 1, 1, 128, 16512, [1500, 33, 0, 700]), (3, 2, 4, 5, 256, 8192, [40, 500, 1]),
+    (1, 4, 7, 64, 128, 16512, [300]), (2, 2, 4, 40, 64, 16512, [1, 129]), (40, 4, 1, 1, 64, 4096, [3 * b for b in range(40)])])
+def test_short_sequences_in_long_caches(B, H, R, Tq, d, Ncap, lens):
+    """A cache has room for the longest conversation; what is in it may be a hundredth of that."""
+    n = max(lens)
+    rng = np.random.default_rng(B + Ncap)
+    K, V = _bf16(rng, B, H, n, d), _bf16(rng, B, H, n, d)
+    cache, to = _cache(B, H, Ncap, d), _i32([0] * B)
+    vb.vitcop_cache_write(K, V, cache, to, seq_len=_i32(lens))
+    q = _bf16(rng, B, H * R, Tq, d, spread=1.5)
+    out, lse = _attend(q, cache, lens, d ** -0.5)
+    _check(q, cache, oc.quantise(_f64(K)), oc.quantise(_f64(V)), lens, d ** -0.5, True, out, lse)
+
+
+@pytest.mark.parametrize("B,H,R,Tq,d,Ncap", [(16, 32, 1, 1, 64, 800), (2, 64, 1, 1, 128, 1536), (12, 32, 4, 2, 64, 864), (2, 4, 8, 5, 128, 1056), (1, 8, 4, 3, 64, 4096)])
+def test_every_head_however_heads_are_given_to_ctas(B, H, R, Tq, d, Ncap):
+    """All heads against fp64, outputs and sums: a piece of a head that is lost or counted twice shows in lse."""
+    rng = np.random.default_rng(B * H + Tq + 1)
+    K, V = _bf16(rng, 1, H, Ncap, d), _bf16(rng, 1, H, Ncap, d)
+    cache, n = _cache(B, H, Ncap, d), _i32([0] * B)
+    lens = [Ncap, 0, Ncap - 1, 33, 257, Ncap // 2, 1, 700, 5, 130, 64, 31, 500, 96, Ncap, 3][:B]
+    vb.vitcop_cache_write(K.expand(B, H, Ncap, d), V.expand(B, H, Ncap, d), cache, n, seq_len=_i32(lens))
+    q = _bf16(rng, B, H * R, Tq, d)
+    out, lse = _attend(q, cache, lens, d ** -0.5)
+    k, v = oc.quantise(_f64(K)), oc.quantise(_f64(V))
+    for b in range(B):
+        _check(q[b:b + 1], cache, k, v, lens[b:b + 1], d ** -0.5, True, out[b:b + 1], lse[b:b + 1])
+
+
+@pytest.mark.parametrize("B,H,R,Tq,d,Ncap,lens", [(1, 2, 8, 48, 128, 5440, [5400]), (2, 1, 7, 24, 64, 8192, [777, 8100]), (40, 4, 4, 20, 128, 352, [(37 * b) % 353 for b in range(40)])])
+def test_many_query_rows_hold_eleven_bits(B, H, R, Tq, d, Ncap, lens):
+    """Weights and values of V in fp16: each off by 2^-11 at most, and the sum of the weights, which the output is divided by, too."""
+    q, cache, K, V = _problem(Tq + d + 1, B, H, R, Tq, d, Ncap, lens)
+    out, lse = _attend(q, cache, lens, d ** -0.5)
+    qq, Kv, Vv = _f64(q), oc.values(*K), oc.values(*V)
+    absq = np.abs(qq).reshape(B, H * R, Tq, d // 32, 32).sum(-1)
+    for b in range(0, B, max(1, B // 4)):
+        w, _ = oc.attention(qq[b:b + 1], Kv[b:b + 1], Vv[b:b + 1], lens[b:b + 1], d ** -0.5, True)
+        size, _ = oc.attention(qq[b:b + 1], Kv[b:b + 1], np.abs(Vv[b:b + 1]), lens[b:b + 1], d ** -0.5, True)
+        reach = (280 * K[0][b] + np.abs(K[1][b])).max(1)[:, None, None]                  # [H, 1, 1, G]
+        delta = d ** -0.5 * 2.0 ** -20 * (absq[b].reshape(H, R, Tq, -1) * reach).sum(-1).reshape(1, H * R, Tq, 1)
+        off = np.expm1(2 * delta) + 2.0 ** -17
+        eleven = 2.0 ** -11 * (1 + 2.0 ** -10)
+        tol = HALF * np.abs(w) + (1 + HALF) * ((2 * eleven + off) * size + eleven * np.abs(w)) + 1e-30
+        worst = (np.abs(_f64(out)[b:b + 1] - w) / tol).max()
+        assert worst <= 1, worst
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("B,H,R,Tq,Ncap,n", [(1, 2, 4, 3, 128, 100), (1, 2, 1, 1, 4096, 3000), (1, 1, 8, 40, 8192, 300)])
+def test_a_query_that_is_no_number_is_its_own(B, H, R, Tq, Ncap, n, d):
+    """NaN and infinities in a query: all of its output is NaN, and no other's changes; one that sees nothing stays at zero."""
+    rng = np.random.default_rng(n + d)
+    K, V = _bf16(rng, B, H, n, d), _bf16(rng, B, H, n, d)
+    cache, lens = _cache(B, H, Ncap, d), _i32([0] * B)
+    vb.vitcop_cache_write(K, V, cache, lens)
+    q = _bf16(rng, B, H * R, Tq, d)
+    out, lse = _attend(q, cache, [n], d ** -0.5)
+    bad = torch.zeros(B, H * R, Tq, dtype=torch.bool, device=DEV)
+    p = q.clone()
+    for i, what in enumerate((float("nan"), float("inf"), float("-inf"))):
+        at = (0, (i * R) % (H * R) + min(i, R - 1) if R > 1 else i % (H * R), (i * 7) % Tq)
+        p[at][5 + 20 * i], bad[at] = what, True
+    out2, lse2 = _attend(p, cache, [n], d ** -0.5)
+    assert torch.isnan(out2[bad]).all() and torch.isnan(lse2[bad]).all()
+    assert torch.equal(out2[~bad], out[~bad]) and torch.equal(lse2[~bad], lse[~bad])
+    out3, lse3 = _attend(p, cache, [0], d ** -0.5)
+    assert torch.all(out3 == 0) and torch.all(torch.isneginf(lse3))
+
+
+@pytest.mark.parametrize("B,H,R,Tq,d,Ncap,n", [(1, 2, 4, 3, 128, 128, 100), (1, 2, 1, 1, 256, 4096, 3000), (1, 1, 8, 40, 64, 8192, 300)])
+def test_logits_beyond_the_range_are_their_rows_own(B, H, R, Tq, d, Ncap, n):
+    """Products that pass what fp32 holds: NaN where a logit is infinite upwards, and nothing in other rows."""
+    rng = np.random.default_rng(n + d)
+    K, V = _bf16(rng, B, H, n, d, spread=0.1, offset=1.0), _bf16(rng, B, H, n, d)
+    cache, lens = _cache(B, H, Ncap, d), _i32([0] * B)
+    vb.vitcop_cache_write(K, V, cache, lens)
+    q = _bf16(rng, B, H * R, Tq, d)
+    out, lse = _attend(q, cache, [n], d ** -0.5)
+    p = q.clone()
+    p[:, 0, Tq - 1] = 3e38
+    out2, lse2 = _attend(p, cache, [n], d ** -0.5)
+    assert torch.isnan(out2[:, 0, Tq - 1]).all()
+    rest = torch.ones(B, H * R, Tq, dtype=torch.bool, device=DEV)
+    rest[:, 0, Tq - 1] = False
+    assert torch.equal(out2[rest], out[rest]) and torch.equal(lse2[rest], lse[rest])
+
+
+@pytest.mark.parametrize("R,Tq,Ncap,n", [(1, 4, 96, 60), (8, 4, 96, 60), (4, 40, 4096, 700), (1, 2, 8192, 5000)])
+def test_wide_heads_and_rows_that_are_no_numbers(R, Tq, Ncap, n):
+    """d = 256: a row of V that is no number reaches the queries that see it, in its group; a key all of their output."""
+    rng, d = np.random.default_rng(n), 256
+    K, V = _bf16(rng, 1, 1, n, d), _bf16(rng, 1, 1, n, d)
+    q = _bf16(rng, 1, R, Tq, d)
+    cache, lens = _cache(1, 1, Ncap, d), _i32([0])
+    V[0, 0, n - 1, 200], V[0, 0, n - 2, 7] = float("inf"), float("nan")
+    vb.vitcop_cache_write(K, V, cache, lens)
+    out, lse = _attend(q, cache, [n], d ** -0.5)
+    assert torch.isfinite(lse).all()
+    nan = torch.isnan(out)
+    for t in range(Tq):
+        for g in range(8):
+            sees = (g == 6 and t >= Tq - 1) or (g == 0 and t >= Tq - 2)
+            assert nan[:, :, t, 32 * g:32 * g + 32].all() if sees else not nan[:, :, t, 32 * g:32 * g + 32].any()
+    K[0, 0, n - 2, 99] = float("-inf")
+    vb.vitcop_cache_write(K, _bf16(rng, 1, 1, n, d), cache, lens)
+    out, lse = _attend(q, cache, [n], d ** -0.5)
+    assert torch.isfinite(out[:, :, :Tq - 2]).all() and torch.isnan(out[:, :, max(0, Tq - 2):]).all() and torch.isnan(lse[:, :, max(0, Tq - 2):]).all()
