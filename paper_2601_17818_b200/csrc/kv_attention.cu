@@ -77,12 +77,12 @@ struct __align__(16) QueryOperand {
     uint4 sums;                                            // (the second half: eight groups)
 };
 template <int G>
-__device__ __forceinline__ void make_operand(QueryOperand<G>* to, const uint4* raw, uint32_t sign, uint32_t keep, int t) {
+__device__ __forceinline__ void make_operand(QueryOperand<G>* to, const uint4* raw, uint32_t sign, int t) {
     float total[G];
 #pragma unroll
     for (int i = 0; i < G; ++i) {
         uint4 v = raw[i * 32];
-        v = make_uint4((v.x ^ sign) & keep, (v.y ^ sign) & keep, (v.z ^ sign) & keep, (v.w ^ sign) & keep);
+        v = make_uint4(v.x ^ sign, v.y ^ sign, v.z ^ sign, v.w ^ sign);
         // elements 0 and 4, 1 and 5, 2 and 6, 3 and 7, as the codes lie
         to->q[i] = make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
         float x = ((bf16lo(v.x) + bf16hi(v.x)) + (bf16lo(v.y) + bf16hi(v.y))) + ((bf16lo(v.z) + bf16hi(v.z)) + (bf16lo(v.w) + bf16hi(v.w)));
@@ -310,7 +310,7 @@ cache_attention_kernel(AttArgs a) {
         if constexpr (NT > 1) __syncthreads(); else __syncwarp();
         if (warp < NT) {
             const int at = NT > 1 ? *stage_at : use;
-            make_operand<G>(operand + warp * 32 + lane, queries + ((at * NT + warp) * G) * 32 + lane, a.sign, a.zero ? 0u : 0xFFFFFFFFu, t);
+            make_operand<G>(operand + warp * 32 + lane, queries + ((at * NT + warp) * G) * 32 + lane, a.sign, t);
         }
         // o[n][i][j][e]: element i 32 + 4 g + 2 j + e / 2 of row n 8 + 2 t + e % 2; base, sum: rows n 8 + 2 t + e, in powers of two
         float o[NT][G][2][4], oc[NT][4], base[NT][2], sum[NT][2];
@@ -772,10 +772,9 @@ int launch_cache_attention(const CacheQueries& io, const void* cache, int B, int
     a.status = static_cast<int*>(workspace);
     a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kStatusBytes);
     a.B = B; a.Hq = Hq; a.H = H; a.R = divisor(Hq / H); a.Tq = Tq; a.Ncap = Ncap; a.RT = divisor(p.RT); a.causal = causal ? 1 : 0;
-    // (a scale of 0 is queries of 0)
-    a.zero = scale == 0.f;
     a.sign = scale < 0.f ? 0x80008000u : 0u;
-    a.scale_log2 = a.zero ? 1.f : (scale < 0.f ? -scale : scale) * kLog2e;
+    // (0 would make NaN of the -inf of tokens that are not seen; the smallest number above it leaves no logit of fp32 more than 2^-21)
+    a.scale_log2 = fmaxf(fabsf(scale) * kLog2e, 0x1p-149f);
     if (many) return launch_cache_attention_rows(a, d, workspace, stream);
     if (d == 64) return p.NT == 1 ? launch<64, 1>(a, p, stream) : p.NT == 2 ? launch<64, 2>(a, p, stream) : launch<64, 3>(a, p, stream);
     if (d == 128) return p.NT == 1 ? launch<128, 1>(a, p, stream) : p.NT == 2 ? launch<128, 2>(a, p, stream) : launch<128, 3>(a, p, stream);

@@ -34,8 +34,7 @@ struct AttArgs {
     int B, Hq, H, Tq, Ncap, causal;
     Divisor R, RT;                                         // query heads of a stored one, tiles of rows
     float scale_log2;                                      // above 0: the sign is the queries'
-    uint32_t sign;                                         // 0x80008000 turns it; scale 0: `zero`
-    bool zero;
+    uint32_t sign;                                         // 0x80008000 turns it
 };
 
 #ifdef __CUDACC__

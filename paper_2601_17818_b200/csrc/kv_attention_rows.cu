@@ -205,8 +205,8 @@ cache_attention_rows_kernel(RowsArgs k) {
     int limit = 0;
     if (tid < kSoftmaxThreads) limit = r < rows ? (a.causal ? max(0, len - a.Tq + tq + 1) : len) : 0;
     if (tid < kRows) {
-        const bool there = r < rows && !a.zero;
-        const __nv_bfloat16* const src = a.io.q + (r < rows ? b * a.io.qb + hq * a.io.qh + tq * a.io.qt : 0);
+        const bool there = r < rows;
+        const __nv_bfloat16* const src = a.io.q + (there ? b * a.io.qb + hq * a.io.qh + tq * a.io.qt : 0);
         float total[G];
 #pragma unroll
         for (int i = 0; i < G; ++i) {
@@ -596,7 +596,7 @@ __device__ __noinline__ void row_anew(const AttArgs& a, int b, int h, int r, flo
     __syncwarp();
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-        const float x = a.zero ? 0.f : a.sign ? -__bfloat162float(src[g * 32 + lane]) : __bfloat162float(src[g * 32 + lane]);
+        const float x = a.sign ? -__bfloat162float(src[g * 32 + lane]) : __bfloat162float(src[g * 32 + lane]);
         q[g * 32 + lane] = total[g] = x;
 #pragma unroll
         for (int off = 16; off > 0; off >>= 1) total[g] += __shfl_xor_sync(0xffffffffu, total[g], off);

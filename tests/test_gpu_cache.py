@@ -845,3 +845,19 @@ def test_wide_heads_and_rows_that_are_no_numbers(R, Tq, Ncap, n):
     vb.vitcop_cache_write(K, _bf16(rng, 1, 1, n, d), cache, lens)
     out, lse = _attend(q, cache, [n], d ** -0.5)
     assert torch.isfinite(out[:, :, :Tq - 2]).all() and torch.isnan(out[:, :, max(0, Tq - 2):]).all() and torch.isnan(lse[:, :, max(0, Tq - 2):]).all()
+
+
+@pytest.mark.parametrize("B,H,R,Tq,d,Ncap,n", [(1, 2, 4, 3, 128, 128, 100), (1, 1, 8, 40, 64, 8192, 300)])
+def test_a_scale_of_zero_is_a_product(B, H, R, Tq, d, Ncap, n):
+    """Zero times a query that is no number is no number either."""
+    rng = np.random.default_rng(n + d + 1)
+    K, V = _bf16(rng, B, H, n, d), _bf16(rng, B, H, n, d)
+    cache, lens = _cache(B, H, Ncap, d), _i32([0] * B)
+    vb.vitcop_cache_write(K, V, cache, lens)
+    q = _bf16(rng, B, H * R, Tq, d)
+    q[0, 1, 2, 5], q[0, H * R - 1, 0, 0] = float("nan"), float("inf")
+    out, lse = _attend(q, cache, [n], 0.0, causal=False)
+    bad = torch.zeros(B, H * R, Tq, dtype=torch.bool, device=DEV)
+    bad[0, 1, 2] = bad[0, H * R - 1, 0] = True
+    assert torch.isnan(out[bad]).all() and torch.isnan(lse[bad]).all() and torch.isfinite(out[~bad]).all()
+    assert (lse[~bad] - np.log(n)).abs().max() <= 2.0 ** -20 * 8
