@@ -387,7 +387,7 @@ int vitcop_cache_read(const void* cache, int B, int H, int Ncap, int d, const in
  * (vitcop_set_wait_limit): the status word is TIMEOUT, and out unspecified, where one ran out.  It holds weights and values of V in fp16, as the
  * largest of a head allow.  A row whose output that may put off by 2^-8 of the largest in a group of 32 elements (it looks at little but tokens
  * whose values are 2^20 times and more below others', or the group is some 2^25 times below another) is done anew in fp32, some 200 times slower.
- * Errors: INVALID_ARG (NULL q/cache/out, negative sizes or strides, d 0, Hq no multiple of H, a scale that is no number or infinite,
+ * Errors: INVALID_ARG (NULL q/cache/out, negative sizes or strides, d 0, Hq no multiple of H, a scale that is no number or beyond 2^127,
  * rows of out that share elements (or lie interleaved: in the order of strides, each dimension has to step over what those below it reach),
  * overlap), UNSUPPORTED (d, Ncap % 32, alignment, more than 2^31 - 1 query rows), WORKSPACE, CUDA. */
 int vitcop_cache_attention(const void* q, const void* cache, int B, int Hq, int H, int Tq, int d, int Ncap,

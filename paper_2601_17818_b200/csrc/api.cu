@@ -544,7 +544,7 @@ int vitcop_cache_attention(const void* q, const void* cache, int B, int Hq, int 
                            size_t workspace_bytes, void* stream) {
     if (B < 0 || Hq < 0 || H < 0 || Tq < 0 || d <= 0 || Ncap < 0) return VITCOP_ERR_INVALID_ARG;
     if ((!q || !out) && extent(B, Hq, Tq, d, 0, 0, 0) > 0) return VITCOP_ERR_INVALID_ARG;
-    if (!(scale - scale == 0.f)) return VITCOP_ERR_INVALID_ARG;            // (NaN, infinite)
+    if (!(std::fabs(scale) <= 0x1p127f)) return VITCOP_ERR_INVALID_ARG;    // (NaN, infinite, or so in powers of two)
     if (H > 0 ? Hq % H != 0 : Hq != 0) return VITCOP_ERR_INVALID_ARG;
     const int64_t strides[6] = {q_stride_b, q_stride_h, q_stride_t, out_stride_b, out_stride_h, out_stride_t};
     for (int i = 0; i < 6; ++i)

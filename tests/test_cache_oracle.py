@@ -203,3 +203,9 @@ def test_attention_refuses_rows_of_the_output_that_share_elements(L, B, Hq, Tq, 
     """Together too: head 1 of the first query, and the first head of query 1.  (What passes is asked for its workspace next.)"""
     status = _attend(L, B=B, Hq=Hq, H=min(Hq, 2), Tq=Tq, qs=(512, 128, 64), os=strides, ws=NULL)
     assert status == (vb.ERR_INVALID_ARG if shared else vb.ERR_WORKSPACE)
+
+
+@pytest.mark.parametrize("scale,status", [(2.5e38, vb.ERR_INVALID_ARG), (-3.4e38, vb.ERR_INVALID_ARG), (2.0 ** 127, vb.ERR_WORKSPACE), (-1e38, vb.ERR_WORKSPACE),
+                                          (1e-45, vb.ERR_WORKSPACE)])
+def test_attention_refuses_a_scale_that_is_infinite_in_powers_of_two(L, scale, status):
+    assert L.vitcop_cache_attention(A, C_, 2, 4, 2, 1, 64, 64, 256, 64, 64, NULL, scale, 1, B_, 256, 64, 64, NULL, NULL, 0, NULL) == status
