@@ -676,25 +676,21 @@ Plan plan_of(int B, int H, int Ncap, int d, int Tq, int Hq, int sms) {
     const int slots = sms * ctas_per_sm(d, p.NT);
     const int64_t segs = (int64_t)B * H * p.RT, blocks = Ncap / kCacheBlock;
     p.ctas = 0;
-    p.wide = false;
-    // Blocks are shared out where that costs less (pieces, their join, the lengths in front) than what CTAs with a head each leave idle: SMs
-    // that have fewer heads, or shorter ones (taken for 5/8 of the capacity).  (Up to four rounds of heads: what launch() has room for.)
+    // The lengths are on the device; the plan takes all samples for as long as the cache has room, so that it is the same for every call of a
+    // sequence that grows.  Blocks are shared out where that costs less (pieces, their join, the lengths in front) than what CTAs with a head
+    // each leave idle, which is the SMs that have one head fewer than others.  Heads of 128, one query, all as long as the cache: 160 heads of
+    // 2048 tokens 24.5 us and 23.0 shared out, of 4096 43.0 and 32.8; 288 of 4096 44.5 and 49.3; 384 of 1536 27.7 and 35.6, of 6144 92 and 85; 512 of
+    // 4096 80.5 and 83.0; 2048 of 4096 256 and 281.  The other way round for few heads: 8 of 1056 10.0 and 9.2, 64 of 1536 12.1 and 11.9, 128 of
+    // 4096 27.5 and 29.1.  Batches of which most samples are far shorter are better off with a CTA a head (512, a quarter of 4096 on
+    // average, up to all: 35.2 us and 61.6), those between a quarter and all the other way (60.9 and 56.0).
+    // (Up to four rounds of heads: what launch() has room for.)
     const bool one = segs <= sms, two = !one && segs <= 2 * sms && d * p.NT <= 128;
     bool whole = blocks <= kWholeBlocks || segs >= 4 * slots || segs * blocks >= 0x7fff0000;
-    if (!whole && ((one && blocks <= 128) || (two && blocks <= 64))) {
-        // A head has an SM, or half of one, and eight warps.  128 heads, 1500 tokens: 13.1 us, shared out 17.2; 128 of 20 rows of 64,
-        // up to 1500: 13.1 and 20.5; 288 heads, 1000 tokens: 17.1 and 22.2; but 8 heads, 1000: 9.4 and 7.3, and 160, 1500: 20.3 and 20.7,
-        // 256, up to 2944 (six draws of the lengths): 29.3 and 28.5.
-        whole = one ? blocks * (27 * sms - 25 * segs) <= 675 * sms : blocks * (2 * sms - segs) <= 40 * sms;
-        p.wide = whole;
-    }
-    // (four warps a head, all heads at once, or some behind others: 512 heads, up to 777 tokens 15.8 us, shared out 17.1, up to 4000 66.6
-    // and 57.3; 384 of 20 rows of 64, up to 3000 43.5 and 56.1; 1024, up to 1000 33.2 and 39.6, up to 4000 109 and 103; 512 of 16 rows,
-    // up to 1000 28.3 and 58.5)
-    if (!whole && !one)
-        whole = segs <= slots ? 8 * blocks * slots <= 8 * (8 + 16 * p.NT) * slots + 5 * blocks * segs : blocks * slots <= (40 + 20 * p.NT) * segs;
-    // (a short head that has an SM to itself: 64 of 20 rows, 733 tokens 9.2 us with four warps, 7.8 with eight)
-    if (blocks <= kWholeBlocks) p.wide = one && blocks > kWarps;
+    if (!whole && one) whole = blocks <= 128 && blocks * (27 * sms - 25 * segs) <= 675 * sms;
+    if (!whole && !one) whole = blocks * ((segs + sms - 1) / sms * sms - segs) <= (40 + 30 * p.NT) * sms;
+    // Eight warps where a head has an SM, or half of one.  64 heads of 512 tokens: 7.1 us with four, 6.5 with eight, of 2048 19.5 and 14.9; 160 of
+    // 640 10.1 and 10.4, of 800 12.4 and 12.2, of 2048 26.0 and 24.5; 288 of 640 10.6 and 11.0, of 1536 21.4 and 21.4, of 4096 47.9 and 44.5.
+    p.wide = whole && (one ? blocks > kWarps : two && blocks > kWholeBlocks);
     if (!whole) p.ctas = slots;
     return p;
 }

@@ -861,3 +861,18 @@ def test_a_scale_of_zero_is_a_product(B, H, R, Tq, d, Ncap, n):
     bad[0, 1, 2] = bad[0, H * R - 1, 0] = True
     assert torch.isnan(out[bad]).all() and torch.isnan(lse[bad]).all() and torch.isfinite(out[~bad]).all()
     assert (lse[~bad] - np.log(n)).abs().max() <= 2.0 ** -20 * 8
+
+
+@pytest.mark.parametrize("R,Tq,d,Ncap", [(1, 1, 128, 3008), (4, 4, 64, 4000), (4, 5, 128, 4800), (1, 1, 256, 3008)])
+def test_more_heads_than_sms_and_blocks_shared_out(R, Tq, d, Ncap):
+    """160 heads of long caches: blocks of all heads shared out, samples from empty to full."""
+    B, H, rng = 5, 32, np.random.default_rng(Ncap + d)
+    K, V = _bf16(rng, 1, H, Ncap, d), _bf16(rng, 1, H, Ncap, d)
+    cache, n = _cache(B, H, Ncap, d), _i32([0] * B)
+    lens = [Ncap, 0, 1000, 33, Ncap - 1]
+    vb.vitcop_cache_write(K.expand(B, H, Ncap, d), V.expand(B, H, Ncap, d), cache, n, seq_len=_i32(lens))
+    q = _bf16(rng, B, H * R, Tq, d)
+    out, lse = _attend(q, cache, lens, d ** -0.5)
+    k, v = oc.quantise(_f64(K)), oc.quantise(_f64(V))
+    for b in range(B):
+        _check(q[b:b + 1], cache, k, v, lens[b:b + 1], d ** -0.5, True, out[b:b + 1], lse[b:b + 1])
