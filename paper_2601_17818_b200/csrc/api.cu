@@ -188,6 +188,12 @@ int vitcop_kernel_timing_end(vitcop_kernel_time* out, int capacity, int* count) 
     return rc;
 }
 
+// More query rows than the attention over the cache counts (their product may pass 64 bits).
+static bool too_many_queries(int B, int Hq, int Tq) {
+    const int64_t rows = (int64_t)Hq * Tq;
+    return rows > 0 && B > 0x7fffffff / rows;
+}
+
 int vitcop_workspace_bytes(int op, int B, int H, int N, int d, int Nv, int D, int Dh, size_t* bytes) {
     (void)Dh;
     if (!bytes || B < 0 || Nv < 0 || D < 0) return VITCOP_ERR_INVALID_ARG;
@@ -215,6 +221,7 @@ int vitcop_workspace_bytes(int op, int B, int H, int N, int d, int Nv, int D, in
             return VITCOP_OK;
         case VITCOP_OP_CACHE_ATTENTION:
             if (H < 0 || N < 0 || d < 0) return VITCOP_ERR_INVALID_ARG;
+            if (too_many_queries(B, D, Nv)) return VITCOP_ERR_UNSUPPORTED;
             *bytes = cache_attention_workspace_bytes(B, H, N, d, Nv, D);
             return VITCOP_OK;
         default: return VITCOP_ERR_INVALID_ARG;
@@ -556,7 +563,7 @@ int vitcop_cache_attention(const void* q, const void* cache, int B, int Hq, int 
     if (!aligned16(q) || !aligned16(out) || B > 65535) return VITCOP_ERR_UNSUPPORTED;
     // (rows of the output that share elements have no value)
     if (extent(B, Hq, Tq, d, 0, 0, 0) > 0 && rows_share(B, Hq, Tq, d, out_stride_b, out_stride_h, out_stride_t)) return VITCOP_ERR_INVALID_ARG;
-    if ((int64_t)B * Hq * Tq > 0x7fffffff) return VITCOP_ERR_UNSUPPORTED;
+    if (too_many_queries(B, Hq, Tq)) return VITCOP_ERR_UNSUPPORTED;
     const size_t need = cache_attention_workspace_bytes(B, H, Ncap, d, Tq, Hq);
     const size_t obytes = extent(B, Hq, Tq, d, out_stride_b, out_stride_h, out_stride_t);
     const size_t rows = (size_t)B * Hq * Tq * sizeof(float), lens = (size_t)B * sizeof(int32_t);

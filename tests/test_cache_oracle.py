@@ -1,5 +1,7 @@
 """The K/V cache in 4 bits without a GPU: the oracle held to closed forms and to bounds, and what the entry points refuse."""
 import ctypes as C
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -7,7 +9,7 @@ import torch
 
 from oracle import cache as oc
 from paper_2601_17818_b200 import binding as vb
-from paper_2601_17818_b200.build import build_library
+from paper_2601_17818_b200.build import ROOT, build_library
 
 
 @pytest.fixture(scope="module")
@@ -209,3 +211,14 @@ def test_attention_refuses_rows_of_the_output_that_share_elements(L, B, Hq, Tq, 
                                           (1e-45, vb.ERR_WORKSPACE)])
 def test_attention_refuses_a_scale_that_is_infinite_in_powers_of_two(L, scale, status):
     assert L.vitcop_cache_attention(A, C_, 2, 4, 2, 1, 64, 64, 256, 64, 64, NULL, scale, 1, B_, 256, 64, 64, NULL, NULL, 0, NULL) == status
+
+
+@pytest.mark.parametrize("B,Hq,H,Tq,status", [(1, 1 << 30, 1, 1 << 30, vb.ERR_UNSUPPORTED), (4, 1 << 30, 1, 1 << 30, vb.ERR_UNSUPPORTED),
+                                              (1 << 30, 1 << 30, 1 << 30, 16, vb.ERR_UNSUPPORTED), (2, 1 << 15, 1 << 15, 1 << 15, vb.ERR_UNSUPPORTED),
+                                              (1, 1 << 15, 1, (1 << 16) - 1, vb.OK), (1, 0, 1, 1 << 30, vb.OK), (1, 4, 8, 1 << 28, vb.OK)])
+def test_workspace_of_more_query_rows_than_are_counted(L, B, Hq, H, Tq, status):
+    """In a process of its own: a product that loses its upper bits ended it with a division by zero."""
+    code = (f"import ctypes as C\nfrom paper_2601_17818_b200 import binding as vb\nn = C.c_size_t(0)\n"
+            f"print(vb.lib().vitcop_workspace_bytes(vb.OP_CACHE_ATTENTION, {B}, {H}, 64, 64, {Tq}, {Hq}, 0, C.byref(n)))")
+    run = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=ROOT)
+    assert run.returncode == 0 and int(run.stdout) == status, run.stderr
