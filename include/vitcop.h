@@ -357,7 +357,7 @@ int vitcop_kproj_knorm(const void* hidden, const void* W_k, int B, int N, int Dh
  *               written.  Must not overlap cache_len or another input.
  * (A pointer to nothing, as an empty cache, no samples, no rows, may be NULL in all three calls.)
  * Errors: INVALID_ARG (NULL cache/new_len, K and V both NULL, negative sizes or strides, d 0, span outside the sequence, overlap),
- * UNSUPPORTED (d, Ncap % 32, alignment, more than 2^31 - 1 rows), CUDA. */
+ * UNSUPPORTED (d, Ncap % 32, alignment, B above 65535, more than 2^31 - 1 rows), CUDA. */
 int vitcop_cache_write(const void* K, const void* V, int B, int H, int N, int d,
                        int64_t k_stride_b, int64_t k_stride_h, int64_t k_stride_n,
                        int64_t v_stride_b, int64_t v_stride_h, int64_t v_stride_n,
@@ -378,6 +378,8 @@ int vitcop_cache_read(const void* cache, int B, int H, int Ncap, int d, const in
  * Query head hq reads stored head hq / (Hq / H).  The Tq queries of a sample are the last Tq of its cache_len[b] tokens
  * (their own K and V are in the cache already): with causal != 0 query t sees the first cache_len[b] - Tq + t + 1 rows, without it
  * all cache_len[b].  A query that sees no row (an empty sample, more queries than rows) gets out = 0 and lse = -inf.
+ * (A logit is made of terms of up to 280 s |q| and |m q|, whose sums have to stay in the fp32 range; an infinite or undefined one makes its
+ * query's output NaN and leaves the others'.)
  *   q, out  bf16 [B, Hq, Tq, d], element (b,h,t,e) at q + b*q_stride_b + h*q_stride_h + t*q_stride_t + e (strides in elements,
  *           multiples of 8, not negative); out must not overlap q or the cache
  *   cache_len  int32 [B] or NULL (= Ncap for every sample)
@@ -389,7 +391,8 @@ int vitcop_cache_read(const void* cache, int B, int H, int Ncap, int d, const in
  * whose values are 2^20 times and more below others', or the group is some 2^25 times below another) is done anew in fp32, some 200 times slower.
  * Errors: INVALID_ARG (NULL q/cache/out, negative sizes or strides, d 0, Hq no multiple of H, a scale that is no number or beyond 2^127,
  * rows of out that share elements (or lie interleaved: in the order of strides, each dimension has to step over what those below it reach),
- * overlap), UNSUPPORTED (d, Ncap % 32, alignment, more than 2^31 - 1 query rows), WORKSPACE, CUDA. */
+ * overlap), UNSUPPORTED (d, Ncap % 32, alignment, B above 65535, more than 2^31 - 1 query rows, which vitcop_workspace_bytes answers too),
+ * WORKSPACE, CUDA. */
 int vitcop_cache_attention(const void* q, const void* cache, int B, int Hq, int H, int Tq, int d, int Ncap,
                            int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_t,
                            const int32_t* cache_len, float scale, int causal,

@@ -7,11 +7,16 @@
 //   output   elements times query rows: (128 + c) - 136 = c - 8 is exact too.  The weights enter, transposed, as bf16(p) with the
 //            centres and as bf16(bf16(p) s) with a group's codes; what the output is divided by is the sum of the bf16(p) (rows of ones
 //            beside the centres), so that a row that takes nearly all is not off by its weight's rounding
+// What is rounded, and why: the matrix instructions take operands of 16 bits.  Weights are bf16, which holds 2^-100 of a row's largest as it
+// holds the largest; fp16 (three bits more) would need a power of two for every row and group.  Weight times scale is the operand in
+// place of the scaled code, which would cost a product for each of a block's elements instead of one for each of its groups.  Together they add 0.001 to the
+// 0.0016 that the output's own rounding to bf16 is off by (root mean square against 64 bits: 0.0018 to 0.0020).  128 + c in place of c costs the
+// logits' fp32 sums some five bits, and saves an instruction for every two codes of K.
 // A warp takes every fourth (or eighth) block of 32 tokens of its CTA's piece, with blocks ahead in shared memory (cp.async), and keeps
 // maximum, sum and output of its own; the CTA joins its warps, a second kernel joins the CTAs that shared a head.
 // Bound by instructions: 680 a block (d = 128, eight rows or fewer), most of them what turns four bits into operands, which the ALU pipe
-// takes every second cycle.  16 x 32 heads of 128, one query each: 2048 tokens 46 us, 3.6 TB/s of cache (the copy rate is 6.5), 4096
-// tokens 4.0 TB/s; issue slots 58 %, ALU 55 %, tensor pipe 26 %.  256 tokens of 32 heads: 4.9 us, of which the launch is more than half.
+// takes every second cycle.  16 x 32 heads of 128, one query each: 2048 tokens 44 us, 3.8 TB/s of cache (the copy rate is 6.5), 4096
+// tokens 4.2 TB/s; issue slots 58 %, ALU 57 %, tensor pipe 26 %.  256 tokens of 32 heads: 4.9 us, of which the launch is more than half.
 #include <type_traits>
 
 #include "async_copy.cuh"
