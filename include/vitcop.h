@@ -55,6 +55,7 @@ extern "C" {
 #define VITCOP_OP_COLLAB_STEP 8   /* vitcop_collaborative_step */
 #define VITCOP_OP_KPROJ       9   /* vitcop_kproj_knorm: B, H, N, d */
 #define VITCOP_OP_CACHE_ATTENTION 10  /* vitcop_cache_attention: B, H = stored heads, N = Ncap, d, Nv = Tq, D = Hq */
+#define VITCOP_OP_ATTENTION   11  /* vitcop_window_attention, vitcop_tree_attention: B, H = stored heads, N, d, Nv = Tq, D = Hq */
 
 /* Human-readable name of a status code (static storage, never NULL). */
 const char* vitcop_status_string(int status);
@@ -398,6 +399,69 @@ int vitcop_cache_attention(const void* q, const void* cache, int B, int Hq, int 
                            const int32_t* cache_len, float scale, int causal,
                            void* out, int64_t out_stride_b, int64_t out_stride_h, int64_t out_stride_t, float* lse,
                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------- rotary positions with several axes
+ * The paper has no counterpart.  Visual tokens stand on a grid: their positions have a time, a height and a width, and a token that a
+ * pruning step keeps has those that it had.  This call turns the rows of q and k by them, as vitcop_kproj_knorm does with one position a token:
+ *     theta = position[axis[e]][b][token] * inv_freq[e]      (a, b) = (x[e], x[e + n_freq]) -> (a cos theta - b sin theta, b cos theta + a sin theta)
+ * for e < n_freq; elements from 2 n_freq on are copied.  inverse != 0 turns back, which is also the gradient: dq and dk in, those of the
+ * rows in front of the turn out.  Angles are taken in 64 bits, sines, cosines and products in fp32; one rounding.
+ *   q, k       bf16 [B, Hq, N, d], [B, Hk, N, d], element (b,h,t,e) at q + b*q_stride_b + h*q_stride_h + t*q_stride_t + e (strides in
+ *              elements, multiples of 8, not negative); either may be NULL together with its output
+ *   position   int32 [axes, B, n_pos]
+ *   token      int32 [B, N] or NULL (= row): the token whose position a row takes, as kept_pos of the compaction; above n_pos - 1 counts as that;
+ *              a row whose token is negative is left as it was
+ *   seq_len    int32 [B] or NULL (= N for every sample): rows from there on are left as they were
+ *   inv_freq   fp64 [n_freq], axis int32 [n_freq] (values in [0, axes), others count as the nearest)
+ *   q_out, k_out  as q and k, strides of their own.  In place (same pointer and strides as the input) is fine; otherwise outputs must
+ *              not share elements with inputs or one another.  (Two tensors may lie in one another's gaps, as q, k and v of one projection do,
+ *              where the strides of their tokens are the same and those of their samples multiples of it.)
+ * Errors: INVALID_ARG (negative sizes or strides, d 0, axes < 1, q and k both NULL, NULL position/inv_freq/axis, n_pos < N without token, overlap, rows of an
+ * output that share elements), UNSUPPORTED (d % 8, n_freq % 8, 2 n_freq > d, n_freq > 256, alignment, B above 65535, more than 2^31 - 1 rows), CUDA. */
+int vitcop_rotary_axes(const void* q, const void* k, int B, int Hq, int Hk, int N, int d,
+                       int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_t,
+                       int64_t k_stride_b, int64_t k_stride_h, int64_t k_stride_t,
+                       const int32_t* position, int axes, int n_pos, const int32_t* token, const int32_t* seq_len,
+                       const double* inv_freq, const int32_t* axis, int n_freq, int inverse,
+                       void* q_out, int64_t qo_stride_b, int64_t qo_stride_h, int64_t qo_stride_t,
+                       void* k_out, int64_t ko_stride_b, int64_t ko_stride_h, int64_t ko_stride_t, void* stream);
+
+/* ---------------------------------------------------------------- attention over K and V in bf16
+ * The paper has no counterpart.  out = softmax(scale * q K^T) V over the rows of K and V that a query sees, for the sequences that a pruning
+ * step leaves: prompts, chunks of them, the tokens of a step.  Logits, maximum, sum and output are held in fp32, weights enter their
+ * product in bf16.  Query head hq reads stored head hq / (Hq / H).  Query t of sample b, t < query_len[b], belongs to row
+ * p = cache_len[b] - query_len[b] + t of K and V (its own, which is there already).  Outputs of queries from query_len[b] on are left as they were.
+ *   vitcop_window_attention  sees the rows j <= p with j < n_sink (first tokens that stay visible) or j > p - window
+ *   vitcop_tree_attention    sees all rows j < cache_len[b] - query_len[b], and row cache_len[b] - query_len[b] + i (drafted token i < query_len[b])
+ *                            where bit i of tree[b][t] is set: t itself and its ancestors, for a tree
+ * A query that sees no row, or stands in front of row 0, gets out = 0 and lse = -inf.  A logit of +inf or NaN makes its query's output NaN, one of -inf counts
+ * as a row not seen.  What stands in rows that a query does not see, NaN and infinities too, does not reach it.
+ *   q, out   bf16 [B, Hq, Tq, d], element (b,h,t,e) at q + b*q_stride_b + h*q_stride_h + t*q_stride_t + e (strides in elements,
+ *            multiples of 8, not negative); out must not overlap anything else
+ *   K, V     bf16 [B, H, N, d], strides likewise
+ *   cache_len  int32 [B] or NULL (= N): rows of K and V (negative counts as 0, above N as N)
+ *   query_len  int32 [B] or NULL (= Tq): queries (negative counts as 0, above Tq as Tq).  With both lengths those of a padded batch, query t stands at row t
+ *   tree     int64 [B, Tq]
+ *   lse      fp32 [B, Hq, Tq] out, optional: log of the sum of exp(scale * q k) over the rows seen
+ *   workspace  vitcop_workspace_bytes(VITCOP_OP_ATTENTION, B, H, N, d, Tq, Hq, 0) bytes
+ * (A pointer to nothing, as no rows or no queries, may be NULL.)
+ * Errors: INVALID_ARG (NULL q/K/V/tree/out, negative sizes, strides, window or n_sink, d 0, Hq no multiple of H, a scale that is no number or beyond
+ * 2^127, rows of out that share elements, overlap), UNSUPPORTED (d not 64, 128 or 256, Tq > 64 with a tree, alignment, B above 65535, more than 2^31 - 1
+ * query rows), WORKSPACE, CUDA. */
+int vitcop_window_attention(const void* q, const void* K, const void* V, int B, int Hq, int H, int Tq, int d, int N,
+                            int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_t,
+                            int64_t k_stride_b, int64_t k_stride_h, int64_t k_stride_n,
+                            int64_t v_stride_b, int64_t v_stride_h, int64_t v_stride_n,
+                            const int32_t* cache_len, const int32_t* query_len, int window, int n_sink, float scale,
+                            void* out, int64_t out_stride_b, int64_t out_stride_h, int64_t out_stride_t, float* lse,
+                            void* workspace, size_t workspace_bytes, void* stream);
+int vitcop_tree_attention(const void* q, const void* K, const void* V, int B, int Hq, int H, int Tq, int d, int N,
+                          int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_t,
+                          int64_t k_stride_b, int64_t k_stride_h, int64_t k_stride_n,
+                          int64_t v_stride_b, int64_t v_stride_h, int64_t v_stride_n,
+                          const int32_t* cache_len, const int32_t* query_len, const int64_t* tree, float scale,
+                          void* out, int64_t out_stride_b, int64_t out_stride_h, int64_t out_stride_t, float* lse,
+                          void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------- schedule and cost model (host arithmetic)
  * Algorithm 1 prunes to floor(m * pi) tokens per stage (pi relative to the ORIGINAL m visual tokens); Appendix E

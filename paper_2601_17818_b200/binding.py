@@ -25,7 +25,7 @@ LIB_PATH = os.path.join(_PKG, "libvitcop.so")
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_BUDGET, ERR_CUDA, ERR_TIMEOUT = range(7)
 (OP_FILTER, OP_KNORM, OP_SELECT, OP_COMPACT, OP_PRUNE_STEP, OP_SIMILARITY, OP_SALIENCY, OP_MERGE, OP_COLLAB_STEP,
- OP_KPROJ, OP_CACHE_ATTENTION) = range(11)
+ OP_KPROJ, OP_CACHE_ATTENTION, OP_ATTENTION) = range(12)
 MAX_VISUAL_TOKENS = 16384
 
 EXPORTS = [
@@ -36,13 +36,15 @@ EXPORTS = [
     "vitcop_flops_layer", "vitcop_visual_tokens_at_layer", "vitcop_flops_total", "vitcop_cr_int",
     "vitcop_collaborative_step", "vitcop_set_wait_limit", "vitcop_kproj_knorm",
     "vitcop_cache_write", "vitcop_cache_read", "vitcop_cache_attention",
+    "vitcop_rotary_axes", "vitcop_window_attention", "vitcop_tree_attention",
 ]
 
-# the calls of a pruning step and of the cache behind it, which go through the extension
+# the calls of a pruning step and of the attention behind it, which go through the extension
 NATIVE = [
     "vitcop_redundancy_filter", "vitcop_similarity_rows", "vitcop_knorm_score", "vitcop_select", "vitcop_compact_kv",
     "vitcop_prune_step", "vitcop_prune_step_static", "vitcop_merge_clusters", "vitcop_cls_saliency",
     "vitcop_collaborative_step", "vitcop_kproj_knorm", "vitcop_cache_write", "vitcop_cache_read", "vitcop_cache_attention",
+    "vitcop_rotary_axes", "vitcop_window_attention", "vitcop_tree_attention",
 ]
 
 
@@ -141,6 +143,11 @@ def lib() -> C.CDLL:
         L.vitcop_cache_read.argtypes = [vp, i32, i32, i32, i32, vp, vp, i32, vp, vp, i32, vp]
         L.vitcop_cache_attention.argtypes = [vp, vp, i32, i32, i32, i32, i32, i32, i64, i64, i64, vp, C.c_float, i32, vp, i64, i64, i64,
                                              vp, vp, sz, vp]
+        L.vitcop_rotary_axes.argtypes = [vp, vp, i32, i32, i32, i32, i32, i64, i64, i64, i64, i64, i64, vp, i32, i32, vp, vp, vp, vp, i32, i32,
+                                         vp, i64, i64, i64, vp, i64, i64, i64, vp]
+        rows = [vp, vp, vp, i32, i32, i32, i32, i32, i32] + [i64] * 9 + [vp, vp]
+        L.vitcop_window_attention.argtypes = rows + [i32, i32, C.c_float, vp, i64, i64, i64, vp, vp, sz, vp]
+        L.vitcop_tree_attention.argtypes = rows + [vp, C.c_float, vp, i64, i64, i64, vp, vp, sz, vp]
         L.vitcop_kernel_timing_begin.argtypes = []
         L.vitcop_kernel_timing_end.argtypes = [C.POINTER(KernelTime), i32, C.POINTER(C.c_int)]
         for name in EXPORTS:
@@ -336,7 +343,7 @@ def alloc_cache(B: int, H: int, Ncap: int, d: int, device="cuda") -> torch.Tenso
     return torch.empty((B, H, Ncap // 32, 40 * d), dtype=torch.uint8, device=device)
 
 
-# (the calls of the cache: their tensors are checked (ValueError) and taken apart in the extension)
+# (the calls of the cache and those behind it: their tensors are checked (ValueError) and taken apart in the extension)
 def vitcop_cache_write(K, V, cache, new_len, cache_len=None, seq_len=None, vis_start: int = 0, vis_len=0, keep_idx=None, n_keep=None):
     """Rows of K and V (bf16 [B,H,N,d], any leading strides) to ``cache`` in 4 bits, from row ``cache_len`` on: all of them, or with
     ``keep_idx`` those that ``vitcop_compact_kv`` keeps.  Returns ``new_len``, the rows that are in the cache then."""
@@ -368,6 +375,43 @@ def vitcop_cache_attention(q, cache, cache_len, out, workspace, scale: float, ca
     rc = _module.cache_attention(_raw_stream(device), device, q, cache, cache_len, out, workspace, scale, causal, lse)
     if rc:
         raise VitcopError(rc, "vitcop_cache_attention")
+    return out
+
+
+def vitcop_rotary_axes(q, k, position, inv_freq, axis, q_out, k_out, token=None, seq_len=None, inverse: bool = False):
+    """q and k (bf16 [B,H,N,d], any leading strides; either may be None) turned by ``position`` (int32 [axes,B,n_pos]): frequency e (``inv_freq``
+    fp64, ``axis`` int32) turns elements e and e + F.  ``token``: whose position a row takes (``kept_pos``; negative: the row stays as
+    it is).  In place where an output is its input."""
+    if _module is None:
+        lib()
+    device = _device()
+    rc = _module.rotary_axes(_raw_stream(device), device, q, k, position, inv_freq, axis, q_out, k_out, token, seq_len, inverse)
+    if rc:
+        raise VitcopError(rc, "vitcop_rotary_axes")
+    return q_out, k_out
+
+
+def vitcop_window_attention(q, K, V, cache_len, out, workspace, scale: float, window: int, n_sink: int = 0, query_len=None, lse=None):
+    """softmax(scale q K^T) V over bf16 rows [B,H,N,d]: a query at row p sees ``n_sink`` first rows and the last ``window`` up to its own.  q, out
+    bf16 [B,Hq,Tq,d] (any leading strides), the last ``query_len`` (None: Tq) of ``cache_len`` (None: N) rows."""
+    if _module is None:
+        lib()
+    device = _device()
+    rc = _module.window_attention(_raw_stream(device), device, q, K, V, cache_len, out, workspace, scale, window, n_sink, query_len, lse)
+    if rc:
+        raise VitcopError(rc, "vitcop_window_attention")
+    return out
+
+
+def vitcop_tree_attention(q, K, V, cache_len, tree, out, workspace, scale: float, query_len=None, lse=None):
+    """As ``vitcop_window_attention`` for at most 64 drafted tokens: query t sees all rows in front of theirs, and drafted row i where bit i
+    of ``tree`` (int64 [B,Tq]) is set in word t."""
+    if _module is None:
+        lib()
+    device = _device()
+    rc = _module.tree_attention(_raw_stream(device), device, q, K, V, cache_len, tree, out, workspace, scale, query_len, lse)
+    if rc:
+        raise VitcopError(rc, "vitcop_tree_attention")
     return out
 
 

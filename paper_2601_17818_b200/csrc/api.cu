@@ -7,9 +7,11 @@
 #include <mutex>
 #include <vector>
 
+#include "attention.cuh"
 #include "gram.cuh"
 #include "internal.cuh"
 #include "kv_cache.cuh"
+#include "rotary.cuh"
 
 namespace vitcop {
 
@@ -223,6 +225,11 @@ int vitcop_workspace_bytes(int op, int B, int H, int N, int d, int Nv, int D, in
             if (H < 0 || N < 0 || d < 0) return VITCOP_ERR_INVALID_ARG;
             if (too_many_queries(B, D, Nv)) return VITCOP_ERR_UNSUPPORTED;
             *bytes = cache_attention_workspace_bytes(B, H, N, d, Nv, D);
+            return VITCOP_OK;
+        case VITCOP_OP_ATTENTION:
+            if (H < 0 || N < 0 || d < 0) return VITCOP_ERR_INVALID_ARG;
+            if (too_many_queries(B, D, Nv)) return VITCOP_ERR_UNSUPPORTED;
+            *bytes = attention_workspace_bytes(B, H, N, d, Nv, D);
             return VITCOP_OK;
         default: return VITCOP_ERR_INVALID_ARG;
     }
@@ -580,6 +587,166 @@ int vitcop_cache_attention(const void* q, const void* cache, int B, int Hq, int 
     const CacheQueries io = {static_cast<const __nv_bfloat16*>(q), static_cast<__nv_bfloat16*>(out), q_stride_b, q_stride_h, q_stride_t,
                              out_stride_b, out_stride_h, out_stride_t};
     return launch_cache_attention(io, cache, B, Hq, H, Tq, d, Ncap, cache_len, scale, causal != 0, lse, workspace, s);
+}
+
+// Whether two such tensors may share elements.  Not where they lie apart, nor where one lies in the gaps of the other: tokens (or samples) step alike, and
+// what a token (a sample) reaches over has places of its own inside that step.
+struct Rows4 {
+    const void* data;
+    int H;
+    int64_t sb, sh, sn;
+    size_t bytes;                                          // reached over
+};
+static bool rows_meet(const Rows4& x, const Rows4& y, int B, int N, int d) {
+    if (!overlaps(x.data, x.bytes, y.data, y.bytes)) return false;
+    const int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(y.data) - reinterpret_cast<uintptr_t>(x.data)) / 2;
+    const auto in_gaps = [&](int64_t step, int64_t reach_x, int64_t reach_y) {
+        const int64_t at = (apart % step + step) % step;
+        return at >= reach_x && at + reach_y <= step;
+    };
+    const int64_t token_x = (x.H - 1) * x.sh + d, token_y = (y.H - 1) * y.sh + d;
+    if (N > 1 && x.sn == y.sn && x.sn > 0 && (B <= 1 || (x.sb % x.sn == 0 && y.sb % y.sn == 0)) && in_gaps(x.sn, token_x, token_y)) return false;
+    return !(B > 1 && x.sb == y.sb && x.sb > 0 && in_gaps(x.sb, token_x + (N - 1) * x.sn, token_y + (N - 1) * y.sn));
+}
+
+int vitcop_rotary_axes(const void* q, const void* k, int B, int Hq, int Hk, int N, int d, int64_t q_stride_b, int64_t q_stride_h,
+                       int64_t q_stride_t, int64_t k_stride_b, int64_t k_stride_h, int64_t k_stride_t, const int32_t* position, int axes,
+                       int n_pos, const int32_t* token, const int32_t* seq_len, const double* inv_freq, const int32_t* axis, int n_freq,
+                       int inverse, void* q_out, int64_t qo_stride_b, int64_t qo_stride_h, int64_t qo_stride_t, void* k_out,
+                       int64_t ko_stride_b, int64_t ko_stride_h, int64_t ko_stride_t, void* stream) {
+    if (B < 0 || Hq < 0 || Hk < 0 || N < 0 || d <= 0 || axes < 1 || n_pos < 0 || n_freq < 0) return VITCOP_ERR_INVALID_ARG;
+    if ((!q && !k) || (q == nullptr) != (q_out == nullptr) || (k == nullptr) != (k_out == nullptr)) return VITCOP_ERR_INVALID_ARG;
+    const int64_t strides[12] = {q_stride_b, q_stride_h, q_stride_t, qo_stride_b, qo_stride_h, qo_stride_t,
+                                 k_stride_b, k_stride_h, k_stride_t, ko_stride_b, ko_stride_h, ko_stride_t};
+    for (int i = 0; i < 12; ++i)
+        if (strides[i] < 0) return VITCOP_ERR_INVALID_ARG;
+    if (n_freq > 0 && (!inv_freq || !axis)) return VITCOP_ERR_INVALID_ARG;
+    if (B > 0 && N > 0 && ((n_freq > 0 && (!position || n_pos == 0)) || (!token && n_pos < N))) return VITCOP_ERR_INVALID_ARG;
+    if (d % 8 || n_freq % 8 || 2 * (int64_t)n_freq > d || n_freq > kMostFrequencies) return VITCOP_ERR_UNSUPPORTED;
+    for (int i = 0; i < 12; ++i)
+        if (strides[i] % 8 && (i < 6 ? q : k)) return VITCOP_ERR_UNSUPPORTED;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || !aligned8(inv_freq) || B > 65535) return VITCOP_ERR_UNSUPPORTED;
+    if (!q) Hq = 0;
+    if (!k) Hk = 0;
+    if (N > 0 && (int64_t)B * N > 0x7fffffff / std::max<int64_t>(1, (int64_t)Hq + Hk)) return VITCOP_ERR_UNSUPPORTED;
+    if (B == 0 || N == 0 || Hq + Hk == 0) return VITCOP_OK;
+    const Rows4 rows[4] = {{q, Hq, q_stride_b, q_stride_h, q_stride_t, extent(B, Hq, N, d, q_stride_b, q_stride_h, q_stride_t)},
+                           {k, Hk, k_stride_b, k_stride_h, k_stride_t, extent(B, Hk, N, d, k_stride_b, k_stride_h, k_stride_t)},
+                           {q_out, Hq, qo_stride_b, qo_stride_h, qo_stride_t, extent(B, Hq, N, d, qo_stride_b, qo_stride_h, qo_stride_t)},
+                           {k_out, Hk, ko_stride_b, ko_stride_h, ko_stride_t, extent(B, Hk, N, d, ko_stride_b, ko_stride_h, ko_stride_t)}};
+    const size_t n = sizeof(int32_t), lens = (size_t)B * n;
+    const void* small[] = {position, token, seq_len, inv_freq, axis};
+    const size_t bytes[] = {(size_t)axes * B * n_pos * n, token ? lens * N : 0, lens, (size_t)n_freq * sizeof(double), (size_t)n_freq * n};
+    for (int o = 2; o < 4; ++o) {
+        const Rows4& out = rows[o];
+        if (out.bytes == 0) continue;
+        if (rows_share(B, out.H, N, d, out.sb, out.sh, out.sn)) return VITCOP_ERR_INVALID_ARG;
+        for (int i = 0; i < 5; ++i)
+            if (overlaps(small[i], bytes[i], out.data, out.bytes)) return VITCOP_ERR_INVALID_ARG;
+        for (int i = 0; i < 4; ++i) {
+            const Rows4& x = rows[i];
+            const bool in_place = i == o - 2 && x.data == out.data && x.sb == out.sb && x.sh == out.sh && x.sn == out.sn;
+            if (i != o && x.bytes > 0 && !in_place && rows_meet(x, out, B, N, d)) return VITCOP_ERR_INVALID_ARG;
+        }
+    }
+    RotaryArgs a = {};
+    a.q = static_cast<const __nv_bfloat16*>(q);
+    a.k = static_cast<const __nv_bfloat16*>(k);
+    a.q_out = static_cast<__nv_bfloat16*>(q_out);
+    a.k_out = static_cast<__nv_bfloat16*>(k_out);
+    for (int i = 0; i < 3; ++i) {
+        a.qs[i] = strides[i];
+        a.qo[i] = strides[3 + i];
+        a.ks[i] = strides[6 + i];
+        a.ko[i] = strides[9 + i];
+    }
+    a.position = position;
+    a.token = token;
+    a.seq_len = seq_len;
+    a.axis = axis;
+    a.inv_freq = inv_freq;
+    a.B = B;
+    a.Hq = Hq;
+    a.Hk = Hk;
+    a.N = N;
+    a.d = d;
+    a.axes = axes;
+    a.n_pos = n_pos;
+    a.F = n_freq;
+    a.inverse = inverse != 0;
+    return launch_rotary_axes(a, static_cast<cudaStream_t>(stream));
+}
+
+// What the two calls of the attention over bf16 rows have in common.
+struct AttentionCall {
+    const void *q, *K, *V;
+    int B, Hq, H, Tq, d, N;
+    int64_t at[12];                                        // strides of q, K, V, out
+    const int32_t *cache_len, *query_len;
+    const int64_t* tree;
+    int window, n_sink;
+    float scale;
+    void* out;
+    float* lse;
+    void* workspace;
+    size_t workspace_bytes;
+};
+static int run_attention(const AttentionCall& c, bool is_tree, void* stream) {
+    if (c.B < 0 || c.Hq < 0 || c.H < 0 || c.Tq < 0 || c.d <= 0 || c.N < 0 || c.window < 0 || c.n_sink < 0) return VITCOP_ERR_INVALID_ARG;
+    const size_t queries = extent(c.B, c.Hq, c.Tq, c.d, 0, 0, 0);
+    if ((!c.q || !c.out || (is_tree && !c.tree)) && queries > 0) return VITCOP_ERR_INVALID_ARG;
+    if ((!c.K || !c.V) && queries > 0 && c.N > 0) return VITCOP_ERR_INVALID_ARG;
+    if (!(std::fabs(c.scale) <= 0x1p127f)) return VITCOP_ERR_INVALID_ARG;  // (NaN, infinite, or so in powers of two)
+    if (c.H > 0 ? c.Hq % c.H != 0 : c.Hq != 0) return VITCOP_ERR_INVALID_ARG;
+    for (int64_t s : c.at)
+        if (s < 0) return VITCOP_ERR_INVALID_ARG;
+    if ((c.d != 64 && c.d != 128 && c.d != 256) || c.B > 65535 || (is_tree && c.Tq > 64)) return VITCOP_ERR_UNSUPPORTED;
+    for (int64_t s : c.at)
+        if (s % 8) return VITCOP_ERR_UNSUPPORTED;
+    if (!aligned16(c.q) || !aligned16(c.K) || !aligned16(c.V) || !aligned16(c.out) || !aligned8(c.tree)) return VITCOP_ERR_UNSUPPORTED;
+    // (rows of the output that share elements have no value)
+    if (queries > 0 && rows_share(c.B, c.Hq, c.Tq, c.d, c.at[9], c.at[10], c.at[11])) return VITCOP_ERR_INVALID_ARG;
+    if (too_many_queries(c.B, c.Hq, c.Tq)) return VITCOP_ERR_UNSUPPORTED;
+    const size_t need = attention_workspace_bytes(c.B, c.H, c.N, c.d, c.Tq, c.Hq), lens = (size_t)c.B * sizeof(int32_t);
+    const size_t obytes = extent(c.B, c.Hq, c.Tq, c.d, c.at[9], c.at[10], c.at[11]), rows = (size_t)c.B * c.Hq * c.Tq * sizeof(float);
+    const void* ins[] = {c.q, c.K, c.V, c.cache_len, c.query_len, c.tree};
+    const size_t insz[] = {extent(c.B, c.Hq, c.Tq, c.d, c.at[0], c.at[1], c.at[2]), extent(c.B, c.H, c.N, c.d, c.at[3], c.at[4], c.at[5]),
+                           extent(c.B, c.H, c.N, c.d, c.at[6], c.at[7], c.at[8]), lens, lens, (size_t)c.B * c.Tq * sizeof(int64_t)};
+    for (int i = 0; i < 6; ++i)
+        if (overlaps(ins[i], insz[i], c.out, obytes) || overlaps(ins[i], insz[i], c.lse, rows) || overlaps(ins[i], insz[i], c.workspace, need))
+            return VITCOP_ERR_INVALID_ARG;
+    if (overlaps(c.out, obytes, c.lse, rows) || overlaps(c.out, obytes, c.workspace, need) || overlaps(c.lse, rows, c.workspace, need))
+        return VITCOP_ERR_INVALID_ARG;
+    if (!c.workspace || c.workspace_bytes < need || !aligned256(c.workspace)) return VITCOP_ERR_WORKSPACE;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (queries == 0) return reset_status(c.workspace, s);
+    const auto bf16 = [](const void* p) { return static_cast<const __nv_bfloat16*>(p); };
+    const SeqRows io = {bf16(c.q), bf16(c.K), bf16(c.V), static_cast<__nv_bfloat16*>(c.out), {c.at[0], c.at[1], c.at[2]},
+                        {c.at[3], c.at[4], c.at[5]}, {c.at[6], c.at[7], c.at[8]}, {c.at[9], c.at[10], c.at[11]}};
+    return launch_attention(io, c.B, c.Hq, c.H, c.Tq, c.d, c.N, c.cache_len, c.query_len, is_tree ? c.tree : nullptr, c.window, c.n_sink, c.scale,
+                            c.lse, c.workspace, s);
+}
+
+int vitcop_window_attention(const void* q, const void* K, const void* V, int B, int Hq, int H, int Tq, int d, int N, int64_t q_stride_b,
+                            int64_t q_stride_h, int64_t q_stride_t, int64_t k_stride_b, int64_t k_stride_h, int64_t k_stride_n,
+                            int64_t v_stride_b, int64_t v_stride_h, int64_t v_stride_n, const int32_t* cache_len, const int32_t* query_len,
+                            int window, int n_sink, float scale, void* out, int64_t out_stride_b, int64_t out_stride_h, int64_t out_stride_t,
+                            float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    return run_attention({q, K, V, B, Hq, H, Tq, d, N,
+                          {q_stride_b, q_stride_h, q_stride_t, k_stride_b, k_stride_h, k_stride_n, v_stride_b, v_stride_h, v_stride_n, out_stride_b,
+                           out_stride_h, out_stride_t},
+                          cache_len, query_len, nullptr, window, n_sink, scale, out, lse, workspace, workspace_bytes}, false, stream);
+}
+
+int vitcop_tree_attention(const void* q, const void* K, const void* V, int B, int Hq, int H, int Tq, int d, int N, int64_t q_stride_b,
+                          int64_t q_stride_h, int64_t q_stride_t, int64_t k_stride_b, int64_t k_stride_h, int64_t k_stride_n,
+                          int64_t v_stride_b, int64_t v_stride_h, int64_t v_stride_n, const int32_t* cache_len, const int32_t* query_len,
+                          const int64_t* tree, float scale, void* out, int64_t out_stride_b, int64_t out_stride_h, int64_t out_stride_t, float* lse,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+    return run_attention({q, K, V, B, Hq, H, Tq, d, N,
+                          {q_stride_b, q_stride_h, q_stride_t, k_stride_b, k_stride_h, k_stride_n, v_stride_b, v_stride_h, v_stride_n, out_stride_b,
+                           out_stride_h, out_stride_t},
+                          cache_len, query_len, tree, 0, 0, scale, out, lse, workspace, workspace_bytes}, true, stream);
 }
 
 int vitcop_prune_step_static(const void* hidden, const void* K, const void* V, int B, int H, int N, int d, int Dh,

@@ -1,0 +1,459 @@
+// Attention over K and V in bf16, with a window and first tokens that stay visible or with a tree of drafted tokens: the kernel for few query
+// rows (a token, a few drafted ones), and which kernel a call takes.
+//
+// The rows of a stored head are all its query heads' (i = t R + r), 16 or 32 of them a CTA.  m16n8k16 twice: logits z = q k of 16 tokens, whose
+// accumulators are, as they lie, the weights' operand of the second product.  A warp has tokens of its own, 16 at a time, which it fetches
+// three blocks ahead of their use, with a running maximum, sum and output of its own; a row's maximum is moved only when a logit has passed it
+// by 2^8.  Up to eight CTAs of a cluster share a head's tokens; warps are joined in shared memory, CTAs in that of the cluster, so that
+// there is one launch and nothing in global memory between.
+// Rows of V that are no numbers must not reach queries that do not see them, and 0 times NaN does: a block that is not seen by all rows is looked
+// through, and one that holds any is added token by token.
+// Weights enter the second product in bf16, and the output is divided by the sum of the weights as they were rounded, which takes the
+// roundings' common part out.
+// Bound by HBM where the tokens are many, by latency otherwise.
+#include "attention.cuh"
+
+#include <algorithm>
+#include <cmath>
+
+#include "async_copy.cuh"
+
+namespace vitcop {
+namespace {
+
+constexpr int kWarps = 4, kBlock = 16, kStages = 3;
+constexpr float kMayPass = 8.f;
+
+template <int D, int MT>
+struct FewSmem {
+    static constexpr int kRows = 16 * MT;
+    static constexpr int kHalf = kBlock * D * 2;                       // a block's K, or V
+    static constexpr int kWarp = kStages * 2 * kHalf;                  // and, behind the blocks, the warp's output [rows][D + 8]
+    static constexpr int kPitch = D + 8;
+    static constexpr int kQ = kWarps * kWarp;                          // [rows][D]
+    static constexpr int kEnds = kQ + kRows * D * 2;                   // [kWarps + 1][3][rows]: maximum, sum, sum of rounded weights
+    static constexpr int kBytes = kEnds + (kWarps + 1) * 3 * kRows * 4;
+    static_assert(kRows * kPitch * 4 <= kWarp);
+};
+
+// Byte of 16-byte piece c of row r of D elements: eight rows' pieces of one column lie in all banks.
+template <int D>
+__device__ __forceinline__ uint32_t piece_at(int r, int c) { return (uint32_t)(r * (2 * D) + ((c ^ (r & 7)) << 4)); }
+
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// 16 bytes to shared memory, zeros where `there` is false (and nothing is read).
+__device__ __forceinline__ void fetch16(uint32_t dst, const void* src, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ float4 cluster_ld4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float2 cluster_ld2(uint32_t addr) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float cluster_ld(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+// Parts of a row, each with maximum, sum and sum of rounded weights (of the lane, where it has one), brought to one maximum: returns what this
+// lane's part counts by.
+__device__ __forceinline__ float joined(float& top, float& sum, float& weight) {
+    const float mine = top;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    const float f = ex2_approx(mine - top);
+    sum *= f;
+    weight *= f;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+        sum += __shfl_xor_sync(0xffffffffu, sum, off);
+        weight += __shfl_xor_sync(0xffffffffu, weight, off);
+    }
+    return f;
+}
+
+struct FewArgs {
+    SeqArgs a;
+    Divisor tiles, heads;                                  // tiles of rows of a head, heads of a sample
+    int ctas;                                              // of a cluster
+};
+
+template <int D, int MT, bool TREE>
+__global__ void __launch_bounds__(kWarps * 32)
+attention_few_kernel(const __grid_constant__ FewArgs k) {
+    using S = FewSmem<D, MT>;
+    constexpr int kRows = S::kRows, kPieces = D / 8, NT = D / 8, E = D / 32;
+    const SeqArgs& a = k.a;
+    extern __shared__ __align__(128) uint8_t smem[];
+    const uint32_t base = smem_u32(smem);
+    float* const ends = reinterpret_cast<float*>(smem + S::kEnds);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    grid_dependency_wait();
+    grid_dependency_launch_dependents();
+    if (blockIdx.x == 0 && tid == 0) *a.status = VITCOP_OK;
+
+    const int rank = blockIdx.x & (k.ctas - 1), seg = blockIdx.x / k.ctas;
+    const int bh = quotient(seg, k.tiles), row0 = (seg - bh * (int)k.tiles.d) * kRows, b = quotient(bh, k.heads), h = bh - b * (int)k.heads.d;
+    const int R = (int)a.R.d;
+    const Sample s = sample_of(a, b);
+    const int rows = min(kRows, R * s.queries - row0);     // of this CTA
+    if (rows <= 0) return;                                 // (its whole cluster)
+    const Span span = span_of<TREE>(a, s, quotient(row0, a.R), quotient(row0 + rows - 1, a.R));
+    const int blocks_a = (span.a + kBlock - 1) / kBlock, blocks = blocks_a + (span.b1 - span.b0 + kBlock - 1) / kBlock;
+    // this CTA's blocks, and of those every fourth to a warp
+    const int each = blocks / k.ctas, more = blocks - each * k.ctas, first = rank * each + min(rank, more), last = first + each + (rank < more ? 1 : 0);
+    const __nv_bfloat16* const Kh = a.io.K + b * a.io.k_at[0] + h * a.io.k_at[1];
+    const __nv_bfloat16* const Vh = a.io.V + b * a.io.v_at[0] + h * a.io.v_at[1];
+    const auto begin_of = [&](int i) { return i < blocks_a ? i * kBlock : span.b0 + (i - blocks_a) * kBlock; };
+    const auto end_of = [&](int i) { return i < blocks_a ? min(span.a, (i + 1) * kBlock) : min(span.b1, span.b0 + (i - blocks_a + 1) * kBlock); };
+    const uint32_t mine = base + warp * S::kWarp;
+    const auto fetch = [&](int i, int stage) {
+        if (i < last) {
+            const int j0 = begin_of(i), j1 = end_of(i);
+            const uint32_t to = mine + stage * 2 * S::kHalf;
+#pragma unroll
+            for (int n = 0; n < kBlock * kPieces / 32; ++n) {
+                const int r = (n * 32 + lane) / kPieces, c = lane % kPieces, j = j0 + r;
+                const bool there = j < j1;
+                const int64_t row = there ? j : j0;
+                fetch16(to + piece_at<D>(r, c), Kh + row * a.io.k_at[2] + c * 8, there);
+                fetch16(to + S::kHalf + piece_at<D>(r, c), Vh + row * a.io.v_at[2] + c * 8, there);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int st = 0; st < kStages - 1; ++st) fetch(first + warp + st * kWarps, st);
+
+    // queries to shared memory
+    for (int i = tid; i < kRows * kPieces; i += kWarps * 32) {
+        const int r = i / kPieces, c = i - r * kPieces;
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (r < rows) {
+            const int t = quotient(row0 + r, a.R), hq = h * R + (row0 + r - t * R);
+            x = __ldcg(reinterpret_cast<const uint4*>(a.io.q + b * a.io.q_at[0] + hq * a.io.q_at[1] + t * a.io.q_at[2] + c * 8));
+            x = make_uint4(x.x ^ a.sign, x.y ^ a.sign, x.z ^ a.sign, x.w ^ a.sign);
+        }
+        *reinterpret_cast<uint4*>(smem + S::kQ + piece_at<D>(r, c)) = x;
+    }
+    // what the four rows of this thread see (a row behind the last sees nothing)
+    const auto row_seen = [&](int r) { return Seen<TREE>(a, s, b, r < rows ? quotient(row0 + r, a.R) : s.queries); };
+    Seen<TREE> seen[2 * MT] = {row_seen(lane / 4), row_seen(lane / 4 + 8)};
+    if constexpr (MT == 2) {
+        seen[2] = row_seen(lane / 4 + 16);
+        seen[3] = row_seen(lane / 4 + 24);
+    }
+    __syncthreads();
+    uint32_t q[MT][D / 16][4];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) ldsm4(q[m][e], base + S::kQ + piece_at<D>(m * 16 + (lane & 15), 2 * e + (lane >> 4)));
+
+    float o[MT][NT][4] = {}, top[2 * MT], sum[2 * MT] = {}, weight[2 * MT] = {};
+#pragma unroll
+    for (int i = 0; i < 2 * MT; ++i) top[i] = kNoLogit;
+    int stage = 0;
+#pragma unroll 1
+    for (int i = first + warp; i < last; i += kWarps) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+        __syncwarp();
+        fetch(i + (kStages - 1) * kWarps, stage == 0 ? kStages - 1 : stage - 1);       // (where the last block was, which all lanes are done with)
+        const uint32_t kb = mine + stage * 2 * S::kHalf, vb = kb + S::kHalf;
+        stage = stage == kStages - 1 ? 0 : stage + 1;
+        float z[MT][2][4] = {};
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) {
+            uint32_t x[4];
+            ldsm4(x, kb + piece_at<D>((lane >> 4) * 8 + (lane & 7), 2 * e + ((lane >> 3) & 1)));
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                mma(z[m][0], q[m][e], x[0], x[1]);
+                mma(z[m][1], q[m][e], x[2], x[3]);
+            }
+        }
+        const int j0 = begin_of(i), j1 = end_of(i);
+        const bool all = j1 - j0 == kBlock && span.full(j0, j1);
+        if (!all) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int j = j0 + n * 8 + (lane & 3) * 2 + (e & 1);
+                        if (!(j < j1 && seen[2 * m + (e >> 1)](j))) z[m][n][e] = MINUS_INF;
+                    }
+        }
+        bool passed = false;
+        float high[2 * MT];
+#pragma unroll
+        for (int r = 0; r < 2 * MT; ++r) {
+            const float(&zm)[2][4] = z[r / 2];
+            const int e = (r & 1) * 2;
+            float x = fmaxf(fmaxf(zm[0][e], zm[0][e + 1]), fmaxf(zm[1][e], zm[1][e + 1]));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+            high[r] = x * a.scale_log2;                    // (0 times an infinite logit: no number, and none in the output)
+            passed |= high[r] - top[r] > kMayPass;
+        }
+        if (__any_sync(0xffffffffu, passed)) {
+#pragma unroll
+            for (int r = 0; r < 2 * MT; ++r) {
+                const float now = fmaxf(top[r], high[r]), keep = ex2_approx(top[r] - now);
+                top[r] = now;
+                sum[r] *= keep;
+                weight[r] *= keep;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    o[r / 2][n][(r & 1) * 2] *= keep;
+                    o[r / 2][n][(r & 1) * 2 + 1] *= keep;
+                }
+            }
+        }
+        uint32_t p[MT][4];
+#pragma unroll
+        for (int r = 0; r < 2 * MT; ++r)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const float* const x = &z[r / 2][n][(r & 1) * 2];
+                const float p0 = ex2_approx(fmaf(x[0], a.scale_log2, -top[r])), p1 = ex2_approx(fmaf(x[1], a.scale_log2, -top[r]));
+                sum[r] += p0 + p1;
+                const uint32_t w = bf16x2(p0, p1);
+                weight[r] += bf16lo(w) + bf16hi(w);
+                p[r / 2][2 * n + (r & 1)] = w;
+            }
+        bool odd = false;
+        if (!all) {
+            uint32_t any = 0;
+#pragma unroll
+            for (int n = 0; n < kBlock * kPieces / 32; ++n) {
+                uint32_t x[4];
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(vb + 16 * (n * 32 + lane)) : "memory");
+#pragma unroll
+                for (int e = 0; e < 4; ++e) any |= (x[e] & 0x7F807F80u) + 0x00800080u;         // (an exponent of ones carries into the sign's place)
+            }
+            odd = __any_sync(0xffffffffu, (any & 0x80008000u) != 0);
+        }
+        if (!odd) {
+#pragma unroll
+            for (int e = 0; e < NT / 2; ++e) {
+                uint32_t x[4];
+                ldsm4_t(x, vb + piece_at<D>(((lane >> 3) & 1) * 8 + (lane & 7), 2 * e + (lane >> 4)));
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    mma(o[m][2 * e], p[m], x[0], x[1]);
+                    mma(o[m][2 * e + 1], p[m], x[2], x[3]);
+                }
+            }
+        } else {
+#pragma unroll 1
+            for (int t = 0; t < j1 - j0; ++t) {
+#pragma unroll
+                for (int r = 0; r < 2 * MT; ++r) {
+                    const uint32_t w0 = p[r / 2][r & 1], w1 = p[r / 2][2 + (r & 1)];
+                    const uint32_t w = __shfl_sync(0xffffffffu, t < 8 ? w0 : w1, (lane & ~3) | ((t & 7) >> 1));
+                    if (!seen[r](j0 + t)) continue;
+                    const float f = t & 1 ? bf16hi(w) : bf16lo(w);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        uint32_t v;
+                        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(vb + piece_at<D>(t, n) + (lane & 3) * 4) : "memory");
+                        o[r / 2][n][(r & 1) * 2] = fmaf(f, bf16lo(v), o[r / 2][n][(r & 1) * 2]);
+                        o[r / 2][n][(r & 1) * 2 + 1] = fmaf(f, bf16hi(v), o[r / 2][n][(r & 1) * 2 + 1]);
+                    }
+                }
+            }
+        }
+    }
+    // ---------------------------------------------------------------------- the warps' parts
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncwarp();
+    float* const part = reinterpret_cast<float*>(smem + warp * S::kWarp);
+#pragma unroll
+    for (int r = 0; r < 2 * MT; ++r) {
+#pragma unroll
+        for (int off = 1; off < 4; off <<= 1) {
+            sum[r] += __shfl_xor_sync(0xffffffffu, sum[r], off);
+            weight[r] += __shfl_xor_sync(0xffffffffu, weight[r], off);
+        }
+        const int row = r * 8 + lane / 4;
+        if ((lane & 3) == 0) {
+            ends[(warp * 3 + 0) * kRows + row] = top[r];
+            ends[(warp * 3 + 1) * kRows + row] = sum[r];
+            ends[(warp * 3 + 2) * kRows + row] = weight[r];
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+            *reinterpret_cast<float2*>(part + row * S::kPitch + n * 8 + (lane & 3) * 2) = make_float2(o[r / 2][n][(r & 1) * 2], o[r / 2][n][(r & 1) * 2 + 1]);
+    }
+    __syncthreads();
+    float* const all_ends = ends + kWarps * 3 * kRows;
+    const bool alone = k.ctas == 1;
+    // a warp a row, E elements a lane
+    const auto finish = [&](int row, const float (&v)[E], float t, float su, float we) {
+        const int i = row0 + row, tq = quotient(i, a.R), hq = h * R + (i - tq * R);
+        const bool none = su == 0.f;                       // (nothing seen)
+        const float inv = none ? 0.f : 1.f / we;
+        uint32_t* const to = reinterpret_cast<uint32_t*>(a.io.out + b * a.io.out_at[0] + hq * a.io.out_at[1] + tq * a.io.out_at[2] + lane * E);
+        if constexpr (E == 2) *to = bf16x2(v[0] * inv, v[1] * inv);
+        else
+#pragma unroll
+            for (int e = 0; e < E; e += 4) *reinterpret_cast<uint2*>(to + e / 2) = make_uint2(bf16x2(v[e] * inv, v[e + 1] * inv), bf16x2(v[e + 2] * inv, v[e + 3] * inv));
+        if (a.lse && lane == 0) a.lse[((int64_t)b * a.Hq + hq) * a.Tq + tq] = none ? MINUS_INF : (t + log2f(su)) * kLn2;
+    };
+    for (int row = warp; row < rows; row += kWarps) {
+        const bool there = lane < kWarps;
+        float t = there ? ends[(lane * 3 + 0) * kRows + row] : kNoLogit, su = there ? ends[(lane * 3 + 1) * kRows + row] : 0.f,
+              we = there ? ends[(lane * 3 + 2) * kRows + row] : 0.f;
+        const float f = joined(t, su, we);
+        float v[E] = {};
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            const float fw = __shfl_sync(0xffffffffu, f, w);
+            const float* const from = reinterpret_cast<const float*>(smem + w * S::kWarp) + row * S::kPitch + lane * E;
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+                const float2 x = *reinterpret_cast<const float2*>(from + e);
+                v[e] = fmaf(x.x, fw, v[e]);
+                v[e + 1] = fmaf(x.y, fw, v[e + 1]);
+            }
+        }
+        if (alone) {
+            finish(row, v, t, su, we);
+        } else {                                           // (in the place of the first warp's, whose elements this lane has read)
+            float* const to = reinterpret_cast<float*>(smem) + row * S::kPitch + lane * E;
+#pragma unroll
+            for (int e = 0; e < E; e += 2) *reinterpret_cast<float2*>(to + e) = make_float2(v[e], v[e + 1]);
+            if (lane == 0) {
+                all_ends[row] = t;
+                all_ends[kRows + row] = su;
+                all_ends[2 * kRows + row] = we;
+            }
+        }
+    }
+    if (alone) return;
+    // ---------------------------------------------------------------------- the cluster's parts: rows in turn to its CTAs
+    cluster_sync_all();
+    for (int row = rank + k.ctas * warp; row < rows; row += k.ctas * kWarps) {
+        const bool there = lane < k.ctas;
+        const uint32_t at = cluster_map(smem_u32(all_ends + row), there ? lane : 0);
+        float t = there ? cluster_ld(at) : kNoLogit, su = there ? cluster_ld(at + kRows * 4) : 0.f, we = there ? cluster_ld(at + kRows * 8) : 0.f;
+        const float f = joined(t, su, we);
+        float v[E] = {};
+        const uint32_t mine_at = base + (row * S::kPitch + lane * E) * 4;
+        for (int c = 0; c < k.ctas; ++c) {
+            const float fc = __shfl_sync(0xffffffffu, f, c);
+            const uint32_t from = cluster_map(mine_at, c);
+            if constexpr (E == 2) {
+                const float2 x = cluster_ld2(from);
+                v[0] = fmaf(x.x, fc, v[0]);
+                v[1] = fmaf(x.y, fc, v[1]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; e += 4) {
+                    const float4 x = cluster_ld4(from + 4 * e);
+                    v[e] = fmaf(x.x, fc, v[e]);
+                    v[e + 1] = fmaf(x.y, fc, v[e + 1]);
+                    v[e + 2] = fmaf(x.z, fc, v[e + 2]);
+                    v[e + 3] = fmaf(x.w, fc, v[e + 3]);
+                }
+            }
+        }
+        finish(row, v, t, su, we);
+    }
+    cluster_sync_all();                                    // (the others may still be reading what this CTA has)
+}
+
+template <int D, int MT, bool TREE>
+int launch_few(FewArgs k, int64_t segs, cudaStream_t stream) {
+    using S = FewSmem<D, MT>;
+    static DoneOnDevice done;
+    const int rc = allow_dynamic_smem(attention_few_kernel<D, MT, TREE>, S::kBytes, done);
+    if (rc != VITCOP_OK) return rc;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)k.ctas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(segs * k.ctas));
+    cfg.blockDim = dim3(kWarps * 32);
+    cfg.dynamicSmemBytes = S::kBytes;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = pdl_allowed(true) ? 2 : 1;
+    KernelTimeScope timed("attention_few_kernel", stream);
+    return record_cuda(cudaLaunchKernelEx(&cfg, attention_few_kernel<D, MT, TREE>, k));
+}
+
+template <int D, int MT>
+int launch_few(const FewArgs& k, int64_t segs, cudaStream_t stream) {
+    return k.a.tree ? launch_few<D, MT, true>(k, segs, stream) : launch_few<D, MT, false>(k, segs, stream);
+}
+
+int launch_attention_few(const SeqArgs& a, int d, cudaStream_t stream) {
+    const int64_t rows = (int64_t)a.R.d * a.Tq;
+    const int tile = rows > 16 && d != 256 ? 32 : 16;
+    FewArgs k;
+    k.a = a;
+    const int64_t tiles = (rows + tile - 1) / tile, segs = tiles * a.B * a.H;
+    if (segs * 8 > 0x7fffffff) return VITCOP_ERR_UNSUPPORTED;
+    k.tiles = divisor((int)tiles);
+    k.heads = divisor(a.H);
+    // tokens that a tile's rows may see, four blocks of which are a CTA's at a time
+    int64_t span = a.N;
+    if (!a.tree) span = std::min<int64_t>(span, (int64_t)a.n_sink + a.window + tile / (int)a.R.d + 1);
+    const int64_t rounds = (span + kWarps * kBlock - 1) / (kWarps * kBlock);
+    k.ctas = 1;
+    while (k.ctas < 8 && segs * k.ctas * 2 <= 2 * sm_count() && k.ctas * 2 <= rounds) k.ctas *= 2;
+    switch (d) {
+        case 64: return tile == 32 ? launch_few<64, 2>(k, segs, stream) : launch_few<64, 1>(k, segs, stream);
+        case 128: return tile == 32 ? launch_few<128, 2>(k, segs, stream) : launch_few<128, 1>(k, segs, stream);
+        default: return launch_few<256, 1>(k, segs, stream);
+    }
+}
+
+}  // namespace
+
+size_t attention_workspace_bytes(int, int, int, int, int, int) { return kStatusBytes; }
+
+int launch_attention(const SeqRows& io, int B, int Hq, int H, int Tq, int d, int N, const int32_t* cache_len, const int32_t* query_len,
+                     const int64_t* tree, int window, int n_sink, float scale, float* lse, void* workspace, cudaStream_t stream) {
+    SeqArgs a;
+    a.io = io;
+    a.cache_len = cache_len;
+    a.query_len = query_len;
+    a.tree = tree;
+    a.lse = lse;
+    a.status = static_cast<int*>(workspace);
+    a.B = B;
+    a.Hq = Hq;
+    a.H = H;
+    a.Tq = Tq;
+    a.N = N;
+    a.window = window;
+    a.n_sink = n_sink;
+    a.R = divisor(Hq / H);
+    a.scale_log2 = std::fmax(std::fabs(scale) * kLog2e, 0x1p-149f);    // (0 times the -inf of a hidden row would be no number)
+    a.sign = std::signbit(scale) ? 0x80008000u : 0u;
+    return launch_attention_few(a, d, stream);
+}
+
+}  // namespace vitcop

@@ -9,6 +9,9 @@
 //   cache_write(stream, device, K, V, cache, new_len, cache_len, seq_len, vis_start, vis_len, keep_idx, n_keep) -> int
 //   cache_read(stream, device, cache, cache_len, K_out, V_out, row_begin) -> int
 //   cache_attention(stream, device, q, cache, cache_len, out, workspace, scale, causal, lse) -> int
+//   rotary_axes(stream, device, q, k, position, inv_freq, axis, q_out, k_out, token, seq_len, inverse) -> int
+//   window_attention(stream, device, q, K, V, cache_len, out, workspace, scale, window, n_sink, query_len, lse) -> int
+//   tree_attention(stream, device, q, K, V, cache_len, tree, out, workspace, scale, query_len, lse) -> int
 //     check types, shapes and devices of their tensors (ValueError), take sizes and strides from them, and call the entry point of
 //     that name.  (The same checks written in Python took 8 us of a decoding step's call, its kernel 5.)
 // Every entry point is called through its own type (taken from the header), each word converted to the parameter's type, so
@@ -75,7 +78,8 @@ Entry entries[] = {
     ENTRY(vitcop_knorm_score), ENTRY(vitcop_select), ENTRY(vitcop_compact_kv), ENTRY(vitcop_prune_step),
     ENTRY(vitcop_prune_step_static), ENTRY(vitcop_collaborative_step), ENTRY(vitcop_merge_clusters),
     ENTRY(vitcop_cls_saliency), ENTRY(vitcop_kproj_knorm), ENTRY(vitcop_redundancy_filter), ENTRY(vitcop_similarity_rows),
-    ENTRY(vitcop_cache_write), ENTRY(vitcop_cache_read), ENTRY(vitcop_cache_attention)};
+    ENTRY(vitcop_cache_write), ENTRY(vitcop_cache_read), ENTRY(vitcop_cache_attention), ENTRY(vitcop_rotary_axes),
+    ENTRY(vitcop_window_attention), ENTRY(vitcop_tree_attention)};
 constexpr int kEntries = sizeof(entries) / sizeof(entries[0]);
 
 bool to_word(PyObject* o, int64_t& v) {
@@ -162,7 +166,7 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n) {
     return PyLong_FromLong(rc);
 }
 
-// ---- the calls of the cache in 4 bits
+// ---- the calls of the cache in 4 bits, of rotary positions and of the attention over bf16 rows
 struct Refused : std::invalid_argument {
     using std::invalid_argument::invalid_argument;
 };
@@ -202,7 +206,7 @@ Rows rows_of(const at::Tensor* t, const char* what, int64_t device, int64_t B, i
     on_device(*t, what, device);
     if (t->scalar_type() != at::kBFloat16 || t->dim() != 4 || t->size(0) != B || t->size(1) != H || t->size(2) != N || t->size(3) != d ||
         (t->numel() > 0 && t->stride(3) != 1))
-        refuse(what, "expected bf16 [B, H, N, d] that fits the cache, elements of a row side by side");
+        refuse(what, "expected bf16 [B, H, N, d] that fits the other tensors, elements of a row side by side");
     r.data = t->data_ptr();
     if (t->numel() > 0)
         for (int i = 0; i < 3; ++i) r.stride[i] = t->size(i) > 1 ? t->stride(i) : 0;
@@ -242,6 +246,23 @@ PerSample per_sample(PyObject* o, const char* what, int64_t device, int64_t B) {
     if (THPVariable_Check(o)) p.each = dense<int32_t>(o, what, device, at::kInt, {B});
     else p.all = int32_of(integer(o, what), what);
     return p;
+}
+
+double number(PyObject* o, const char* what) {
+    const double v = PyFloat_AsDouble(o);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        refuse(what, "expected a number");
+    }
+    return v;
+}
+bool truth(PyObject* o, const char* what) {
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) {
+        PyErr_Clear();
+        refuse(what, "expected a truth value");
+    }
+    return v != 0;
 }
 
 int entry(const char* name) {
@@ -336,21 +357,101 @@ PyObject* cache_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const int32_t* const cache_len = dense<int32_t>(args[4], "cache_len", dev, at::kInt, {c.B});
         void* const workspace = dense<void>(args[6], "workspace", dev, at::kByte, {-1});
         const size_t bytes = workspace ? (size_t)THPVariable_Unpack(args[6]).numel() : 0;
-        const double scale = PyFloat_AsDouble(args[7]);
-        if (PyErr_Occurred()) {
-            PyErr_Clear();
-            refuse("scale", "expected a number");
-        }
-        const int causal = PyObject_IsTrue(args[8]);
-        if (causal < 0) {
-            PyErr_Clear();
-            refuse("causal", "expected a truth value");
-        }
+        const double scale = number(args[7], "scale");
+        const int causal = truth(args[8], "causal");
         float* const lse = dense<float>(args[9], "lse", dev, at::kFloat, {c.B, Hq, Tq});
         return unlocked(bound<decltype(vitcop_cache_attention)>(e), (const void*)qr.data, (const void*)c.data, int32_of(c.B, "B"), int32_of(Hq, "Hq"),
                         int32_of(c.H, "H"), int32_of(Tq, "Tq"), int32_of(c.d, "d"), int32_of(c.Ncap, "Ncap"), qr.stride[0], qr.stride[1],
                         qr.stride[2], cache_len, static_cast<float>(scale), causal, o.data, o.stride[0], o.stride[1],
                         o.stride[2], lse, workspace, bytes, stream);
+    });
+}
+
+PyObject* rotary_axes(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    static const int e = entry("vitcop_rotary_axes");
+    return guarded(n, 12, "rotary_axes", [&]() -> int {
+        void* const stream = reinterpret_cast<void*>(static_cast<uintptr_t>(integer(args[0], "stream")));
+        const int64_t dev = integer(args[1], "device");
+        const at::Tensor *const q = tensor_or_none(args[2], "q"), *const k = tensor_or_none(args[3], "k"), *const any = q ? q : k;
+        if (!any || any->dim() != 4 || (q && q->dim() != 4) || (k && k->dim() != 4)) refuse("q, k", "expected bf16 [B, H, N, d]");
+        const int64_t B = any->size(0), N = any->size(2), d = any->size(3), Hq = q ? q->size(1) : 0, Hk = k ? k->size(1) : 0;
+        const Rows qr = rows_of(q, "q", dev, B, Hq, N, d), kr = rows_of(k, "k", dev, B, Hk, N, d);
+        const Rows qo = rows_of(tensor_or_none(args[7], "q_out"), "q_out", dev, B, Hq, N, d), ko = rows_of(tensor_or_none(args[8], "k_out"), "k_out", dev, B, Hk, N, d);
+        const int32_t* const position = dense<int32_t>(args[4], "position", dev, at::kInt, {-1, B, -1});
+        if (!position && args[4] == Py_None) refuse("position", "expected a tensor");
+        const at::Tensor& p = THPVariable_Unpack(args[4]);
+        const double* const inv_freq = dense<double>(args[5], "inv_freq", dev, at::kDouble, {-1});
+        if (args[5] == Py_None) refuse("inv_freq", "expected a tensor");
+        const int64_t F = THPVariable_Unpack(args[5]).size(0);
+        const int32_t* const axis = dense<int32_t>(args[6], "axis", dev, at::kInt, {F});
+        const int32_t* const token = dense<int32_t>(args[9], "token", dev, at::kInt, {B, N});
+        const int32_t* const seq_len = dense<int32_t>(args[10], "seq_len", dev, at::kInt, {B});
+        return unlocked(bound<decltype(vitcop_rotary_axes)>(e), (const void*)qr.data, (const void*)kr.data, int32_of(B, "B"), int32_of(Hq, "Hq"), int32_of(Hk, "Hk"),
+                        int32_of(N, "N"), int32_of(d, "d"), qr.stride[0], qr.stride[1], qr.stride[2], kr.stride[0], kr.stride[1], kr.stride[2], position,
+                        int32_of(p.size(0), "position"), int32_of(p.size(2), "position"), token, seq_len, inv_freq, axis, int32_of(F, "inv_freq"),
+                        (int)truth(args[11], "inverse"), qo.data, qo.stride[0], qo.stride[1], qo.stride[2], ko.data, ko.stride[0], ko.stride[1], ko.stride[2], stream);
+    });
+}
+
+// Tensors of the attention over bf16 rows, args from q on; the rest of the arguments is the callers'.
+struct Attention {
+    int64_t B, Hq, H, Tq, d, N;
+    Rows q, K, V, out;
+    const int32_t *cache_len, *query_len;
+    void* workspace;
+    size_t bytes;
+    float* lse;
+};
+Attention attention_of(int64_t dev, PyObject* q_, PyObject* K_, PyObject* V_, PyObject* len, PyObject* out_, PyObject* workspace, PyObject* query_len, PyObject* lse) {
+    const at::Tensor *const q = tensor_or_none(q_, "q"), *const K = tensor_or_none(K_, "K"), *const V = tensor_or_none(V_, "V"), *const out = tensor_or_none(out_, "out");
+    if (!q || q->dim() != 4) refuse("q", "expected bf16 [B, Hq, Tq, d]");
+    if (!K || K->dim() != 4 || !V) refuse("K, V", "expected bf16 [B, H, N, d]");
+    if (!out) refuse("out", "expected a tensor");
+    Attention a;
+    a.B = q->size(0);
+    a.Hq = q->size(1);
+    a.Tq = q->size(2);
+    a.d = q->size(3);
+    a.H = K->size(1);
+    a.N = K->size(2);
+    a.q = rows_of(q, "q", dev, a.B, a.Hq, a.Tq, a.d);
+    a.K = rows_of(K, "K", dev, a.B, a.H, a.N, a.d);
+    a.V = rows_of(V, "V", dev, a.B, a.H, a.N, a.d);
+    a.out = rows_of(out, "out", dev, a.B, a.Hq, a.Tq, a.d);
+    a.cache_len = dense<int32_t>(len, "cache_len", dev, at::kInt, {a.B});
+    a.query_len = dense<int32_t>(query_len, "query_len", dev, at::kInt, {a.B});
+    a.workspace = dense<void>(workspace, "workspace", dev, at::kByte, {-1});
+    a.bytes = a.workspace ? (size_t)THPVariable_Unpack(workspace).numel() : 0;
+    a.lse = dense<float>(lse, "lse", dev, at::kFloat, {a.B, a.Hq, a.Tq});
+    return a;
+}
+
+PyObject* window_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    static const int e = entry("vitcop_window_attention");
+    return guarded(n, 13, "window_attention", [&]() -> int {
+        void* const stream = reinterpret_cast<void*>(static_cast<uintptr_t>(integer(args[0], "stream")));
+        const Attention a = attention_of(integer(args[1], "device"), args[2], args[3], args[4], args[5], args[6], args[7], args[11], args[12]);
+        const float scale = static_cast<float>(number(args[8], "scale"));
+        const int window = int32_of(integer(args[9], "window"), "window"), n_sink = int32_of(integer(args[10], "n_sink"), "n_sink");
+        return unlocked(bound<decltype(vitcop_window_attention)>(e), (const void*)a.q.data, (const void*)a.K.data, (const void*)a.V.data, int32_of(a.B, "B"),
+                        int32_of(a.Hq, "Hq"), int32_of(a.H, "H"), int32_of(a.Tq, "Tq"), int32_of(a.d, "d"), int32_of(a.N, "N"), a.q.stride[0], a.q.stride[1],
+                        a.q.stride[2], a.K.stride[0], a.K.stride[1], a.K.stride[2], a.V.stride[0], a.V.stride[1], a.V.stride[2], a.cache_len, a.query_len, window,
+                        n_sink, scale, a.out.data, a.out.stride[0], a.out.stride[1], a.out.stride[2], a.lse, a.workspace, a.bytes, stream);
+    });
+}
+
+PyObject* tree_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    static const int e = entry("vitcop_tree_attention");
+    return guarded(n, 12, "tree_attention", [&]() -> int {
+        void* const stream = reinterpret_cast<void*>(static_cast<uintptr_t>(integer(args[0], "stream")));
+        const int64_t dev = integer(args[1], "device");
+        const Attention a = attention_of(dev, args[2], args[3], args[4], args[5], args[7], args[8], args[10], args[11]);
+        const int64_t* const tree = dense<int64_t>(args[6], "tree", dev, at::kLong, {a.B, a.Tq});
+        const float scale = static_cast<float>(number(args[9], "scale"));
+        return unlocked(bound<decltype(vitcop_tree_attention)>(e), (const void*)a.q.data, (const void*)a.K.data, (const void*)a.V.data, int32_of(a.B, "B"),
+                        int32_of(a.Hq, "Hq"), int32_of(a.H, "H"), int32_of(a.Tq, "Tq"), int32_of(a.d, "d"), int32_of(a.N, "N"), a.q.stride[0], a.q.stride[1],
+                        a.q.stride[2], a.K.stride[0], a.K.stride[1], a.K.stride[2], a.V.stride[0], a.V.stride[1], a.V.stride[2], a.cache_len, a.query_len, tree,
+                        scale, a.out.data, a.out.stride[0], a.out.stride[1], a.out.stride[2], a.lse, a.workspace, a.bytes, stream);
     });
 }
 
@@ -360,6 +461,9 @@ PyMethodDef methods[] = {
     {"cache_write", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_write)), METH_FASTCALL, "vitcop_cache_write"},
     {"cache_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_read)), METH_FASTCALL, "vitcop_cache_read"},
     {"cache_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_attention)), METH_FASTCALL, "vitcop_cache_attention"},
+    {"rotary_axes", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rotary_axes)), METH_FASTCALL, "vitcop_rotary_axes"},
+    {"window_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(window_attention)), METH_FASTCALL, "vitcop_window_attention"},
+    {"tree_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(tree_attention)), METH_FASTCALL, "vitcop_tree_attention"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", "Calls the entry points of the C ABI.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
