@@ -81,7 +81,7 @@ int vitcop_poll_status(const void* workspace, void* stream, int* device_status);
 
 /* ---------------------------------------------------------------- diagnostic: bounded device waits
  * The paper has no counterpart.  Kernels whose CTAs wait for one another or for asynchronous copies (the Gram
- * sweeps of the redundancy filter, the attention of many query rows over the cache) bound every wait; when a
+ * sweeps of the redundancy filter, the attentions of many query rows) bound every wait; when a
  * wait runs out, the CTA abandons its work, lets its
  * copies and tensor-core operations in flight finish, frees its tensor memory and records VITCOP_ERR_TIMEOUT in
  * the status word (read it with vitcop_poll_status; the call's outputs are then undefined, the workspace and the
@@ -89,8 +89,8 @@ int vitcop_poll_status(const void* workspace, void* stream, int* device_status);
  *   limit_ns      time after which a wait gives up; 0 restores the default of 2 s
  *   expire_roles  for failure-handling tests: waits of the named roles give up at once, whatever their state
  *                 (1 load warp, 2 tensor-core issue warp, 4 epilogue warps; 8, 16, 32 the same in the kernels that run
- *                 on pairs of multiprocessors alone: density sweep, key projection; and in the attention of many query
- *                 rows over the cache; 0 = none)
+ *                 on pairs of multiprocessors alone: density sweep, key projection; and in the attentions of many query
+ *                 rows; 0 = none)
  * Always returns VITCOP_OK. */
 int vitcop_set_wait_limit(unsigned long long limit_ns, int expire_roles);
 
@@ -443,7 +443,9 @@ int vitcop_rotary_axes(const void* q, const void* k, int B, int Hq, int Hk, int 
  *   query_len  int32 [B] or NULL (= Tq): queries (negative counts as 0, above Tq as Tq).  With both lengths those of a padded batch, query t stands at row t
  *   tree     int64 [B, Tq]
  *   lse      fp32 [B, Hq, Tq] out, optional: log of the sum of exp(scale * q k) over the rows seen
- *   workspace  vitcop_workspace_bytes(VITCOP_OP_ATTENTION, B, H, N, d, Tq, Hq, 0) bytes
+ *   workspace  vitcop_workspace_bytes(VITCOP_OP_ATTENTION, B, H, N, d, Tq, Hq, 0) bytes: a status word
+ * Many query rows (more than 32 of a stored head, d 64 or 128) run through a kernel whose waits are bounded (vitcop_set_wait_limit): the status word is
+ * TIMEOUT, and out unspecified, where one ran out.
  * (A pointer to nothing, as no rows or no queries, may be NULL.)
  * Errors: INVALID_ARG (NULL q/K/V/tree/out, negative sizes, strides, window or n_sink, d 0, Hq no multiple of H, a scale that is no number or beyond
  * 2^127, rows of out that share elements, overlap), UNSUPPORTED (d not 64, 128 or 256, Tq > 64 with a tree, alignment, B above 65535, more than 2^31 - 1

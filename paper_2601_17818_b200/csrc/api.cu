@@ -243,6 +243,15 @@ int vitcop_poll_status(const void* workspace, void* stream, int* device_status) 
     if (rc != VITCOP_OK) return rc;
     rc = record_cuda(cudaStreamSynchronize(s));
     if (rc != VITCOP_OK) return rc;
+    if ((v & ~(kStatusInReports - 1)) == kStatusInReports) {
+        uint8_t reports[kMaxReports];
+        const int n = std::min(v & (kStatusInReports - 1), kMaxReports);
+        rc = record_cuda(cudaMemcpyAsync(reports, static_cast<const char*>(workspace) + kReportsAt, n, cudaMemcpyDeviceToHost, s));
+        if (rc != VITCOP_OK) return rc;
+        rc = record_cuda(cudaStreamSynchronize(s));
+        if (rc != VITCOP_OK) return rc;
+        v = std::any_of(reports, reports + n, [](uint8_t r) { return r != 0; }) ? VITCOP_ERR_TIMEOUT : VITCOP_OK;
+    }
     *device_status = v;
     return VITCOP_OK;
 }

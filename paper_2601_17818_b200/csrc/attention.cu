@@ -453,6 +453,10 @@ int launch_attention(const SeqRows& io, int B, int Hq, int H, int Tq, int d, int
     a.R = divisor(Hq / H);
     a.scale_log2 = std::fmax(std::fabs(scale) * kLog2e, 0x1p-149f);    // (0 times the -inf of a hidden row would be no number)
     a.sign = std::signbit(scale) ? 0x80008000u : 0u;
+    if (tiles_kernel_takes(a, d)) {
+        const int rc = launch_attention_tiles(a, d, stream);
+        if (rc != VITCOP_ERR_UNSUPPORTED) return rc;
+    }
     return launch_attention_few(a, d, stream);
 }
 

@@ -1,4 +1,4 @@
-// What the kernels of the attention over bf16 rows share (attention.cu).
+// What the kernels of the attention over bf16 rows share (attention.cu, attention_tiles.cu).
 #pragma once
 
 #include <cuda_bf16.h>
@@ -108,6 +108,9 @@ __device__ __forceinline__ Span span_of(const SeqArgs& a, const Sample& s, int t
 
 int launch_attention(const SeqRows& io, int B, int Hq, int H, int Tq, int d, int N, const int32_t* cache_len, const int32_t* query_len,
                      const int64_t* tree, int window, int n_sink, float scale, float* lse, void* workspace, cudaStream_t stream);
+// The kernel for many query rows (tcgen05).
+bool tiles_kernel_takes(const SeqArgs& a, int d);
+int launch_attention_tiles(const SeqArgs& a, int d, cudaStream_t stream);
 size_t attention_workspace_bytes(int B, int H, int N, int d, int Tq, int Hq);
 
 }  // namespace vitcop

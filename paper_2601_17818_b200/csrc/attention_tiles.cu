@@ -1,0 +1,804 @@
+// Attention over K and V in bf16 for many query rows (prompts, questions, large trees): tcgen05, two tiles of 128 query rows a CTA.
+//
+// A tile's rows are as many tokens as 128 / R query heads of a stored one allow (row t R + r), brought by one tensor copy; the two tiles of an item
+// read the same blocks of 128 tokens.  Blocks end where the last row's window (or the sinks) ends, so that nothing behind a sequence is read;
+// what a first block reaches back beyond its segment, or the sequence, is masked.  Of a block that a tile sees in part only the 32-token
+// columns that it sees are worked on.
+//   warps 0-3, 4-7  softmax of a tile, a thread a row: logits from tensor memory, weights back to where the logits were, as the operand of
+//                   the second product; a row's maximum is moved, and its sums with it, only when a logit has passed it by 2^8
+//   warp 8          tensor copies: queries, then K and V of a block in turn through a ring
+//   warp 9          products: PV(A), QK(A), PV(B), QK(B): while one tile's softmax runs, the other's products do
+//   warps 10, 11    rows of V that are no numbers must not reach rows that do not see them, and 0 times NaN does: blocks that are masked are looked
+//                   through, such rows taken out and added again at the end for those who see them
+// A CTA takes items in turn, the next item's first products under the last one's output.  Where items are fewer than SMs, a cluster of up to eight CTAs
+// shares an item's blocks and joins its parts in shared memory.
+#include "attention.cuh"
+
+#include <algorithm>
+
+#include "gram.cuh"
+#include "tcgen05.cuh"
+
+namespace vitcop {
+namespace {
+
+constexpr int kTile = 128, kBlock = 128;
+constexpr int kSoftmaxThreads = 256, kThreads = kSoftmaxThreads + 128;
+constexpr int kMasked = 16;                                // blocks of an item that a tile sees in part: at most two at either edge of a tile's
+                                                           // window, two where its segments begin, two where the sinks end
+constexpr float kMayPass = 8.f;
+enum { kRoleLoad = 1, kRoleMma = 2, kRoleSoftmax = 4 };
+
+struct Item {
+    int there, b, h, t0, len, queries, k0, k1;
+};
+
+template <int D>
+struct TilesSmem {
+    static constexpr int kSubs = D / 64;                               // operands are [D / 64][128 rows][128 bytes]
+    static constexpr int kOperand = kSubs * 16384;
+    static constexpr int kSlots = D == 128 ? 5 : 10;
+    static constexpr int kQ = 0;
+    static constexpr int kRing = 2 * kOperand;
+    static constexpr int kBars = kRing + kSlots * kOperand;
+    static constexpr int kItems = kBars + 400;                         // two of them
+    static constexpr int kBad = kItems + 2 * (int)sizeof(Item);        // [2][kMasked][4] words: rows of V that were taken out
+    static constexpr int kBytes = kBars + 2048 + 1024;                 // (and what aligning to 1024 takes)
+    static_assert(kBad + 2 * kMasked * 16 + 16 <= kBars + 2048);
+    // parts of a cluster, where the operands were: [256 rows][D + 4] and [3][256]
+    static constexpr int kPitch = D + 4;
+    static constexpr int kPartEnds = 256 * kPitch * 4;
+    static_assert(kPartEnds + 2 * 256 * 4 <= kBars);
+};
+
+struct TilesArgs {
+    SeqArgs a;
+    Divisor heads;                                         // heads of a sample
+    int items, per_head, tokens, ctas;                     // items, and those of a head; tokens of a tile; CTAs of a cluster
+    bool wide;                                             // rows of the output lie at multiples of 32 bytes
+    int q_b, k_h, k_b, v_h, v_b;                           // 0 where all samples, or heads, are one, else 1
+    unsigned long long wait_ns;
+    int expire_roles;
+    __device__ __forceinline__ unsigned long long limit_of(int role) const { return (expire_roles & role) ? 0ull : wait_ns; }
+};
+
+__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// Called by a warp of which one lane issues.
+__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void commit_one(uint32_t bar) {
+    asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
+                 ::"r"(bar) : "memory");
+}
+// Operand whose 64-element rows (128 bytes, swizzled) run along the product's N: 8 of them (steps of its K) are 1024 bytes, the next 64 of N 16384 further.
+__device__ __forceinline__ uint64_t umma_desc_mn128(uint32_t smem_addr) {
+    return umma_desc_k128(smem_addr) | (uint64_t)(16384u >> 4) << 16;
+}
+__device__ __forceinline__ void tmem_ld32_issue(uint32_t taddr, uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void pin32(uint32_t (&r)[32]) {   // (no use of the registers in front of the wait)
+#pragma unroll
+    for (int i = 0; i < 32; i += 8)
+        asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7]));
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// The blocks of an item: first those of the sinks, then those of the window (or of the whole sequence), both counted from their end.
+struct Blocks {
+    Span v;
+    int na, n;
+    __device__ __forceinline__ int end(int k) const { return k < na ? v.a - (na - 1 - k) * kBlock : v.b1 - (n - 1 - k) * kBlock; }
+    __device__ __forceinline__ int begin_of_segment(int k) const { return k < na ? 0 : v.b0; }
+};
+template <bool TREE>
+__device__ __forceinline__ Blocks blocks_of(const SeqArgs& a, const Sample& s, int t0, int t1) {
+    Blocks x;
+    x.v = span_of<TREE>(a, s, t0, t1);
+    x.na = (x.v.a + kBlock - 1) / kBlock;
+    x.n = x.na + (x.v.b1 - x.v.b0 + kBlock - 1) / kBlock;
+    return x;
+}
+// Columns [lo, hi) of block k that a tile works on, multiples of 32 (none: lo = hi), and whether all its rows see all of them.
+struct Columns {
+    int lo, hi;
+    bool all;
+};
+__device__ __forceinline__ Columns columns_of(const Blocks& x, int k, const Span& tile) {
+    const int end = x.end(k), start = end - kBlock, segment = x.begin_of_segment(k), from = max(start, segment);
+    const bool front = from < tile.a, window = from < tile.b1 && end > tile.b0;
+    Columns c = {0, 0, true};
+    if (!front && !window) return c;
+    const int lo = front ? from : max(from, tile.b0), hi = window ? min(end, tile.b1) : min(end, tile.a);
+    c.lo = (lo - start) & ~31;
+    c.hi = (hi - start + 31) & ~31;
+    c.all = start + c.lo >= segment && tile.full(start + c.lo, start + c.hi);
+    return c;
+}
+
+// Bits c of a word: a <= c < b.
+__device__ __forceinline__ uint32_t below(int x) { return x <= 0 ? 0u : x >= 32 ? 0xffffffffu : (1u << x) - 1u; }
+__device__ __forceinline__ uint32_t bits_of(const Seen<false>& s, int j0) { return below(s.front - j0) | (below(s.p + 1 - j0) & ~below(s.lo - j0)); }
+__device__ __forceinline__ uint32_t bits_of(const Seen<true>& s, int j0) {
+    const int i = j0 - s.base;                             // drafted token of bit 0
+    const uint32_t drafted = i <= -32 || i >= 64 ? 0u : i < 0 ? (uint32_t)(s.bits << -i) : (uint32_t)(s.bits >> i);
+    return below(s.front - j0) | (drafted & below(s.len - j0) & ~below(-j0));
+}
+
+// What tokens whose V was taken out add to a row: in fp32, from where they lie.
+template <int D, bool TREE>
+__device__ __noinline__ void add_taken_out(const TilesArgs& k, const Blocks& x, const Span* spans, int k0, int k1, const uint32_t* bad, const Seen<TREE>& seen,
+                                           const __nv_bfloat16* q, const __nv_bfloat16* Kh, const __nv_bfloat16* Vh, float top, int part, float (&v)[32]) {
+    int n = 0;
+    for (int i = k0; i < k1; ++i) {
+        const Columns ca = columns_of(x, i, spans[0]), cb = columns_of(x, i, spans[1]);
+        if (ca.all && cb.all) continue;
+        const int start = x.end(i) - kBlock, from = max(start, x.begin_of_segment(i));
+        for (int w = 0; w < 4; ++w) {
+            for (uint32_t left = bad[n * 4 + w]; left; left &= left - 1) {
+                const int j = start + w * 32 + __ffs(left) - 1;
+                if (j < from || !seen(j)) continue;
+                float z = 0.f;
+                for (int e = 0; e < D; ++e) z = fmaf(__bfloat162float(q[e]), __bfloat162float(Kh[j * k.a.io.k_at[2] + e]), z);
+                z = k.a.sign ? -z : z;
+                const float p = ex2_approx(fmaf(z, k.a.scale_log2, -top));
+#pragma unroll
+                for (int e = 0; e < 32; ++e) v[e] = fmaf(p, __bfloat162float(Vh[j * k.a.io.v_at[2] + part * 32 + e]), v[e]);
+            }
+        }
+        ++n;
+    }
+}
+
+template <int D, bool TREE>
+__global__ void __launch_bounds__(kThreads, 1)
+attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                       const __grid_constant__ TilesArgs k) {
+    using S = TilesSmem<D>;
+    constexpr int kSlots = S::kSlots, kSubs = S::kSubs;
+    const SeqArgs& a = k.a;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    const uint32_t base = smem_u32(smem);
+    const uint32_t bar_full = base + S::kBars, bar_empty = bar_full + 8 * kSlots, bar_q = bar_empty + 8 * kSlots, bar_q_free = bar_q + 16, bar_s = bar_q_free + 8,
+                   bar_p = bar_s + 16, bar_o = bar_p + 16, bar_o_free = bar_o + 16, bar_item = bar_o_free + 16, bar_done = bar_item + 16,
+                   bar_drain = bar_done + 16, bar_checked = bar_drain + 8;
+    volatile int* const abort_flag = reinterpret_cast<volatile int*>(smem + S::kBars + 376);
+    uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + S::kBars + 380);
+    volatile int* const any_bad = reinterpret_cast<volatile int*>(smem + S::kBars + 384);           // [2 items][2 warps]
+    volatile Item* const items = reinterpret_cast<volatile Item*>(smem + S::kItems);
+    uint32_t* const bad = reinterpret_cast<uint32_t*>(smem + S::kBad);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        for (int i = 0; i < kSlots; ++i) {
+            mbar_init(bar_full + 8 * i, 1);
+            mbar_init(bar_empty + 8 * i, 3);               // the products' end, and both warps that look through V
+            mbar_init(bar_checked + 8 * i, 64);
+        }
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(bar_q + 8 * x, 1);
+            mbar_init(bar_s + 8 * x, 1);
+            mbar_init(bar_p + 8 * x, kTile);
+            mbar_init(bar_o + 8 * x, 1);
+            mbar_init(bar_o_free + 8 * x, kTile);
+            mbar_init(bar_item + 8 * x, 1);
+            mbar_init(bar_done + 8 * x, kSoftmaxThreads / 32 + 3);
+        }
+        mbar_init(bar_q_free, 1);
+        mbar_init(bar_drain, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 9) tmem_alloc(smem_u32(tmem_slot), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
+    grid_dependency_wait();
+    grid_dependency_launch_dependents();
+    // S(A), S(B): 128 columns each, whose first 64 take the weights; O(A), O(B): D columns each
+    const auto tmem_s = [&](int x) { return tmem + x * kBlock; };
+    const auto tmem_o = [&](int x) { return tmem + 2 * kBlock + x * D; };
+    const int rank = blockIdx.x & (k.ctas - 1);
+    uint32_t issued = 0, fetched = 0;                      // operands and items whose copies the load lane has started
+    const int R = (int)a.R.d, tokens = k.tokens;
+    const auto spans_of = [&](const Sample& s, int t0, Span (&v)[2]) {
+        v[0] = span_of<TREE>(a, s, t0, t0 + tokens - 1);
+        v[1] = span_of<TREE>(a, s, t0 + tokens, t0 + 2 * tokens - 1);
+    };
+    const auto sample_in = [&](const Item& it) {
+        const Sample s = {it.len, it.queries, it.len - it.queries};
+        return s;
+    };
+    // item n of this CTA, as the load warp leaves it
+    const auto item_at = [&](int n, unsigned long long lim, Item& it) {
+        if (!__all_sync(0xffffffffu, mbar_wait(bar_item + 8 * (n & 1), (n >> 1) & 1, abort_flag, lim))) return false;
+        volatile Item& from = items[n & 1];
+        it.there = from.there;
+        it.b = from.b;
+        it.h = from.h;
+        it.t0 = from.t0;
+        it.len = from.len;
+        it.queries = from.queries;
+        it.k0 = from.k0;
+        it.k1 = from.k1;
+        return it.there != 0;
+    };
+
+    if (warp < 8) {
+        // ------------------------------------------------------------------ softmax
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        const unsigned long long lim = k.limit_of(kRoleSoftmax);
+        const int x = warp >> 2, row = tid & (kTile - 1), tl = quotient(row, a.R), r = row - tl * R;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_at = tmem_s(x) + lanes, o_at = tmem_o(x) + lanes;
+        uint32_t phase_s = 0, phase_o = 0, phase_other = 0;
+        const f32x2 scale2 = pack2(a.scale_log2, a.scale_log2);
+        Item it;
+        bool ok = true;
+        for (int n = 0; ok && item_at(n, lim, it); ++n) {
+            const Sample s = sample_in(it);
+            const Blocks blocks = blocks_of<TREE>(a, s, it.t0, it.t0 + 2 * tokens - 1);
+            Span spans[2];
+            spans_of(s, it.t0, spans);
+            const int t = it.t0 + x * tokens + tl;
+            const bool there = tl < tokens && t < s.queries;
+            const Seen<TREE> seen(a, s, it.b, there ? t : s.queries);
+            float top = kNoLogit;                          // in powers of two; weights are 2^(logit - top)
+            f32x2 sum0 = pack2(0.f, 0.f), sum1 = sum0;
+            int count = 0;
+            for (int i = it.k0; i < it.k1; ++i) {
+                const Columns c = columns_of(blocks, i, spans[x]);
+                if (c.lo == c.hi) continue;
+                ok = __all_sync(0xffffffffu, mbar_wait(bar_s + 8 * x, phase_s, abort_flag, lim));
+                if (!ok) break;
+                phase_s ^= 1;
+                tc_fence_after();
+                uint32_t z[4][32];
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    if (w * 32 >= c.lo && w * 32 < c.hi) tmem_ld32_issue(s_at + w * 32, z[w]);
+                tmem_ld_wait();
+                float high = MINUS_INF;
+                const int start = blocks.end(i) - kBlock, segment = blocks.begin_of_segment(i);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    if (w * 32 >= c.lo && w * 32 < c.hi) {
+                        pin32(z[w]);
+                        if (!c.all) {
+                            const uint32_t keep = bits_of(seen, start + w * 32) & ~below(segment - start - w * 32);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) z[w][e] = keep >> e & 1 ? z[w][e] : 0xff800000u;
+                        }
+                        float h0 = MINUS_INF, h1 = MINUS_INF;
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4) {
+                            h0 = fmaxf(h0, fmaxf(__uint_as_float(z[w][e]), __uint_as_float(z[w][e + 1])));
+                            h1 = fmaxf(h1, fmaxf(__uint_as_float(z[w][e + 2]), __uint_as_float(z[w][e + 3])));
+                        }
+                        high = fmaxf(high, fmaxf(h0, h1));
+                    }
+                }
+                high *= a.scale_log2;
+                if (__any_sync(0xffffffffu, high - top > kMayPass)) {
+                    const float now = fmaxf(top, high), keep = ex2_approx(top - now);
+                    top = now;
+                    const f32x2 keep2 = pack2(keep, keep);
+                    sum0 = mul2(sum0, keep2);
+                    sum1 = mul2(sum1, keep2);
+                    if (count > 0) {                       // (the products so far have ended: the logits' came behind them)
+#pragma unroll 1
+                        for (int e = 0; e < D; e += 16) {
+                            uint32_t o[16];
+                            asm volatile(
+                                "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+                                "tcgen05.wait::ld.sync.aligned;"
+                                : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3]), "=r"(o[4]), "=r"(o[5]), "=r"(o[6]), "=r"(o[7]), "=r"(o[8]), "=r"(o[9]),
+                                  "=r"(o[10]), "=r"(o[11]), "=r"(o[12]), "=r"(o[13]), "=r"(o[14]), "=r"(o[15])
+                                : "r"(o_at + e)
+                                : "memory");
+#pragma unroll
+                            for (int u = 0; u < 16; ++u) o[u] = __float_as_uint(__uint_as_float(o[u]) * keep);
+                            tmem_st16(o_at + e, o);
+                        }
+                    }
+                }
+                ++count;
+                const f32x2 top2 = pack2(-top, -top);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    if (w * 32 >= c.lo && w * 32 < c.hi) {
+                        uint32_t p[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const float2 y = unpack2(fma2(pack2(__uint_as_float(z[w][2 * e]), __uint_as_float(z[w][2 * e + 1])), scale2, top2));
+                            const float p0 = ex2_approx(y.x), p1 = ex2_approx(y.y);
+                            if (e & 1) sum1 = add2(sum1, pack2(p0, p1));
+                            else sum0 = add2(sum0, pack2(p0, p1));
+                            p[e] = bf16x2(p0, p1);
+                        }
+                        tmem_st16(s_at + w * 16, p);
+                    }
+                }
+                tmem_st_wait();
+                tc_fence_before();
+                mbar_arrive(bar_p + 8 * x);
+            }
+            if (!ok) break;
+            // ---- the output
+            const float2 sa = unpack2(sum0), sb = unpack2(sum1);
+            const float sum = (sa.x + sa.y) + (sb.x + sb.y);
+            if (count > 0) {
+                ok = __all_sync(0xffffffffu, mbar_wait(bar_o + 8 * x, phase_o, abort_flag, lim));
+                if (!ok) break;
+                phase_o ^= 1;
+                tc_fence_after();
+            }
+            const bool none = sum == 0.f, alone = k.ctas == 1;
+            const float inv = none ? 0.f : 1.f / sum;
+            const int hq = it.h * R + r;
+            const __nv_bfloat16* const q = a.io.q + it.b * a.io.q_at[0] + hq * a.io.q_at[1] + t * a.io.q_at[2];
+            __nv_bfloat16* const out = a.io.out + it.b * a.io.out_at[0] + hq * a.io.out_at[1] + t * a.io.out_at[2];
+            const bool odd = (any_bad[(n & 1) * 2] | any_bad[(n & 1) * 2 + 1]) != 0;
+            float* const part = reinterpret_cast<float*>(smem) + (x * kTile + row) * S::kPitch;
+            if (!alone) {
+                // parts go where operands were: the other tile's products have to have ended too
+                bool other = false;
+                for (int i = it.k0; i < it.k1; ++i) {
+                    const Columns c = columns_of(blocks, i, spans[x ^ 1]);
+                    other |= c.lo != c.hi;
+                }
+                if (other) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(bar_o + 8 * (x ^ 1), phase_other, abort_flag, lim));
+                    if (!ok) break;
+                    phase_other ^= 1;
+                }
+                reinterpret_cast<float*>(smem + S::kPartEnds)[x * kTile + row] = top;
+                reinterpret_cast<float*>(smem + S::kPartEnds)[kSoftmaxThreads + x * kTile + row] = sum;
+            } else if (a.lse && there) {
+                a.lse[((int64_t)it.b * a.Hq + hq) * a.Tq + t] = none ? MINUS_INF : (top + log2f(sum)) * kLn2;
+            }
+#pragma unroll 1
+            for (int e = 0; e < D; e += 32) {
+                float v[32];
+                __syncwarp();
+                if (count > 0) {
+                    tmem_ld32(o_at + e, v);
+                } else {
+#pragma unroll
+                    for (int u = 0; u < 32; ++u) v[u] = 0.f;
+                }
+                if (odd && there) {
+                    const Span both[2] = {spans[0], spans[1]};
+                    const Blocks all = blocks;
+                    const Seen<TREE> sees = seen;
+                    float extra[32] = {};
+                    add_taken_out<D, TREE>(k, all, both, it.k0, it.k1, bad + (n & 1) * kMasked * 4, sees, q,
+                                           a.io.K + it.b * a.io.k_at[0] + it.h * a.io.k_at[1], a.io.V + it.b * a.io.v_at[0] + it.h * a.io.v_at[1], top, e / 32, extra);
+#pragma unroll
+                    for (int u = 0; u < 32; ++u) v[u] += extra[u];
+                }
+                if (!alone) {
+#pragma unroll
+                    for (int u = 0; u < 32; u += 4) *reinterpret_cast<float4*>(part + e + u) = make_float4(v[u], v[u + 1], v[u + 2], v[u + 3]);
+                } else if (there) {
+                    uint32_t p[16];
+#pragma unroll
+                    for (int u = 0; u < 16; ++u) p[u] = none ? 0u : bf16x2(v[2 * u] * inv, v[2 * u + 1] * inv);
+                    if (k.wide) {
+#pragma unroll
+                        for (int u = 0; u < 16; u += 8)
+                            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + e + 2 * u), "r"(p[u]), "r"(p[u + 1]), "r"(p[u + 2]),
+                                         "r"(p[u + 3]), "r"(p[u + 4]), "r"(p[u + 5]), "r"(p[u + 6]), "r"(p[u + 7]) : "memory");
+                    } else {
+#pragma unroll
+                        for (int u = 0; u < 16; u += 4) *reinterpret_cast<uint4*>(out + e + 2 * u) = make_uint4(p[u], p[u + 1], p[u + 2], p[u + 3]);
+                    }
+                }
+            }
+            __syncwarp();
+            if (count > 0) {
+                tc_fence_before();
+                mbar_arrive(bar_o_free + 8 * x);
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_done + 8 * (n & 1));
+        }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        if (warp == 8) {
+            // -------------------------------------------------------------- tensor copies
+            if (lane == 0) {
+                const unsigned long long lim = k.limit_of(kRoleLoad);
+                uint32_t slot = 0, phase = 0;
+                int n = 0;
+                bool ok = true;
+                const auto fetch = [&](const CUtensorMap* map, int row, int h, int b) {   // an operand to the ring
+                    if (!mbar_wait(bar_empty + 8 * slot, phase ^ 1, abort_flag, lim)) return false;
+                    mbar_expect_tx(bar_full + 8 * slot, S::kOperand);
+#pragma unroll
+                    for (int i = 0; i < kSubs; ++i) tma_load_4d(base + S::kRing + slot * S::kOperand + i * 16384, map, bar_full + 8 * slot, i * 64, row, h, b);
+                    ++issued;
+                    if (++slot == (uint32_t)kSlots) {
+                        slot = 0;
+                        phase ^= 1;
+                    }
+                    return true;
+                };
+                const auto publish = [&](const Item& it) {
+                    if (n >= 2 && !mbar_wait(bar_done + 8 * (n & 1), ((n >> 1) - 1) & 1, abort_flag, lim)) return false;
+                    volatile Item& to = items[n & 1];
+                    to.there = it.there;
+                    to.b = it.b;
+                    to.h = it.h;
+                    to.t0 = it.t0;
+                    to.len = it.len;
+                    to.queries = it.queries;
+                    to.k0 = it.k0;
+                    to.k1 = it.k1;
+                    mbar_arrive(bar_item + 8 * (n & 1));
+                    return true;
+                };
+                // the last tokens first: in front of a full window they are the ones with the most to look at
+                for (int i = blockIdx.x / k.ctas; ok && i < k.items; i += gridDim.x / k.ctas) {
+                    const int bhs = a.B * a.H, tile = i / bhs, bh = i - tile * bhs, b = quotient(bh, k.heads), h = bh - b * a.H;
+                    const int t0 = (k.per_head - 1 - tile) * 2 * tokens;
+                    const Sample s = sample_of(a, b);
+                    if (t0 >= s.queries) continue;
+                    const Blocks blocks = blocks_of<TREE>(a, s, t0, t0 + 2 * tokens - 1);
+                    const int each = blocks.n / k.ctas, more = blocks.n - each * k.ctas;
+                    Item it = {1, b, h, t0, s.len, s.queries, rank * each + min(rank, more), 0};
+                    it.k1 = it.k0 + each + (rank < more ? 1 : 0);
+                    ok = publish(it) && (n == 0 || mbar_wait(bar_q_free, (n - 1) & 1, abort_flag, lim));
+                    if (!ok) break;
+                    for (int x = 0; x < 2; ++x) {
+                        mbar_expect_tx(bar_q + 8 * x, tokens * R * 128 * kSubs);
+#pragma unroll
+                        for (int e = 0; e < kSubs; ++e)
+                            tma_load_4d(base + S::kQ + x * S::kOperand + e * 16384, &map_q, bar_q + 8 * x, e * 64, h * R, t0 + x * tokens, b * k.q_b);
+                    }
+                    ++n;
+                    for (int j = it.k0; ok && j < it.k1; ++j) {
+                        const int row = blocks.end(j) - kBlock;
+                        ok = fetch(&map_k, row, h * k.k_h, b * k.k_b) && fetch(&map_v, row, h * k.v_h, b * k.v_b);
+                    }
+                }
+                if (ok) {
+                    const Item end = {};
+                    ok = publish(end);
+                }
+                fetched = n;
+            }
+            __syncwarp();
+        } else if (warp == 9) {
+            // -------------------------------------------------------------- products
+            const unsigned long long lim = k.limit_of(kRoleMma);
+            const uint32_t idesc_s = umma_idesc_bf16(kTile, 0) | (a.sign ? 1u << 13 : 0u), idesc_o = umma_idesc_bf16(kTile, D) | 1u << 16;
+            uint32_t slot = 0, phase = 0, phase_p[2] = {0, 0}, phase_checked = 0, outputs[2] = {0, 0};
+            const auto waited = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, lim)); };
+            const auto next = [&]() {
+                if (++slot == (uint32_t)kSlots) {
+                    slot = 0;
+                    phase ^= 1;
+                }
+            };
+            Item it;
+            bool ok = true;
+            for (int n = 0; ok && item_at(n, lim, it); ++n) {
+                const Sample s = sample_in(it);
+                const Blocks blocks = blocks_of<TREE>(a, s, it.t0, it.t0 + 2 * tokens - 1);
+                Span spans[2];
+                spans_of(s, it.t0, spans);
+                ok = waited(bar_q, n & 1) && waited(bar_q + 8, n & 1);
+                bool begun[2] = {false, false};
+                Columns before[2] = {{0, 0, true}, {0, 0, true}};
+                for (int i = it.k0; ok && i <= it.k1; ++i) {
+                    // block i - 1's second product, block i's first
+                    const bool second = i > it.k0, first = i < it.k1;
+                    Columns now[2] = {{0, 0, true}, {0, 0, true}};
+                    if (first)
+                        for (int x = 0; x < 2; ++x) now[x] = columns_of(blocks, i, spans[x]);
+                    uint32_t v_slot = 0;
+                    if (second) {
+                        ok = waited(bar_full + 8 * slot, phase);
+                        if (ok && !(before[0].all && before[1].all)) {
+                            ok = waited(bar_checked + 8 * slot, phase_checked >> slot & 1);
+                            phase_checked ^= 1u << slot;
+                        }
+                        v_slot = slot;
+                        next();
+                    }
+                    if (ok && first) ok = waited(bar_full + 8 * slot, phase);
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        if (second && before[x].lo != before[x].hi) {
+                            ok = waited(bar_p + 8 * x, phase_p[x]);
+                            phase_p[x] ^= 1;
+                            if (ok && !begun[x] && outputs[x] > 0) ok = waited(bar_o_free + 8 * x, (outputs[x] - 1) & 1);
+                            if (!ok) break;
+                            tc_fence_after();
+                            const uint64_t dv = umma_desc_mn128(base + S::kRing + v_slot * S::kOperand);
+                            for (int e = before[x].lo / 16; e < before[x].hi / 16; ++e) {
+                                mma_ts(tmem_o(x), tmem_s(x) + 8 * e, dv + (uint64_t)(e * 128), idesc_o, begun[x] ? 1u : 0u);
+                                begun[x] = true;
+                            }
+                            if (!first) commit_one(bar_o + 8 * x);
+                        }
+                        if (second && x == 1) commit_one(bar_empty + 8 * v_slot);
+                        if (first && now[x].lo != now[x].hi) {
+                            const uint32_t idesc = idesc_s | (uint32_t)((now[x].hi - now[x].lo) >> 3) << 17;
+                            const uint32_t ring = base + S::kRing + slot * S::kOperand + now[x].lo * 128;
+#pragma unroll
+                            for (int e = 0; e < D / 16; ++e)
+                                mma_ss(tmem_s(x) + now[x].lo, umma_desc_k128(base + S::kQ + x * S::kOperand + (e / 4) * 16384) + (uint64_t)((e % 4) * 2),
+                                       umma_desc_k128(ring + (e / 4) * 16384) + (uint64_t)((e % 4) * 2), idesc, e > 0 ? 1u : 0u);
+                            commit_one(bar_s + 8 * x);
+                        }
+                    }
+                    if (!ok) break;
+                    if (first) {
+                        commit_one(bar_empty + 8 * slot);
+                        next();
+                    }
+                    if (i == it.k1 - 1 || it.k0 == it.k1) commit_one(bar_q_free);
+                    // an output whose last block was not the item's last
+                    if (!first)
+                        for (int x = 0; x < 2; ++x)
+                            if (begun[x] && before[x].lo == before[x].hi) commit_one(bar_o + 8 * x);
+                    before[0] = now[0];
+                    before[1] = now[1];
+                }
+                for (int x = 0; x < 2; ++x) outputs[x] += begun[x] ? 1 : 0;
+                __syncwarp();
+                if (ok && lane == 0) mbar_arrive(bar_done + 8 * (n & 1));
+            }
+            commit_one(bar_drain);                         // (waited for below)
+        } else {
+            // -------------------------------------------------------------- rows of V that are no numbers
+            const unsigned long long lim = k.limit_of(kRoleLoad);
+            const int u = tid - kSoftmaxThreads - 64;
+            uint32_t slot = 0, phase = 0;
+            Item it;
+            bool ok = true;
+            // (every operand of the ring is waited for in its turn: by parity alone a later round could not be told from an earlier one)
+            const auto arrived = [&]() { return __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * slot, phase, abort_flag, lim)); };
+            const auto leave = [&]() {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_empty + 8 * slot);
+                if (++slot == (uint32_t)kSlots) {
+                    slot = 0;
+                    phase ^= 1;
+                }
+            };
+            for (int n = 0; ok && item_at(n, lim, it); ++n) {
+                const Sample s = sample_in(it);
+                const Blocks blocks = blocks_of<TREE>(a, s, it.t0, it.t0 + 2 * tokens - 1);
+                Span spans[2];
+                spans_of(s, it.t0, spans);
+                uint32_t* const words = bad + (n & 1) * kMasked * 4;
+                int masked = 0;
+                volatile int& odd_here = any_bad[(n & 1) * 2 + warp - 10];
+                if (lane == 0) odd_here = 0;
+                for (int i = it.k0; i < it.k1; ++i) {
+                    ok = arrived();
+                    if (!ok) break;
+                    leave();
+                    ok = arrived();
+                    if (!ok) break;
+                    if (!(columns_of(blocks, i, spans[0]).all && columns_of(blocks, i, spans[1]).all)) {
+                        ok = masked < kMasked;
+                        if (!ok) break;
+                        uint8_t* const v = smem + S::kRing + slot * S::kOperand;
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            const int r = half * 64 + u;
+                            uint32_t any = 0;
+#pragma unroll
+                            for (int e = 0; e < kSubs * 8; ++e) {      // (pieces in another order in each lane: eight lie in all banks)
+                                const uint4 y = *reinterpret_cast<const uint4*>(v + (e / 8) * 16384 + r * 128 + ((e + lane) & 7) * 16);
+                                any |= ((y.x & 0x7F807F80u) + 0x00800080u) | ((y.y & 0x7F807F80u) + 0x00800080u) | ((y.z & 0x7F807F80u) + 0x00800080u) |
+                                       ((y.w & 0x7F807F80u) + 0x00800080u);
+                            }
+                            const bool odd = (any & 0x80008000u) != 0;
+                            if (odd)
+                                for (int e = 0; e < kSubs * 8; ++e) *reinterpret_cast<uint4*>(v + (e / 8) * 16384 + r * 128 + (e & 7) * 16) = make_uint4(0, 0, 0, 0);
+                            const uint32_t found = __ballot_sync(0xffffffffu, odd);
+                            if (lane == 0) {
+                                words[masked * 4 + half * 2 + u / 32] = found;
+                                if (found) odd_here = 1;
+                            }
+                        }
+                        ++masked;
+                        fence_async_proxy();
+                        mbar_arrive(bar_checked + 8 * slot);
+                    }
+                    leave();
+                }
+                __syncwarp();
+                if (ok && lane == 0) mbar_arrive(bar_done + 8 * (n & 1));
+            }
+        }
+    }
+    __syncthreads();
+    // Another role may have given up behind the last product: operands and tensor memory stay until all of them have completed.
+    // The same goes for copies in flight.
+    if (warp == 8 && lane == 0 && *abort_flag) {
+        for (uint32_t i = 0; i < (uint32_t)kSlots && i < issued; ++i) {
+            const uint32_t at = issued - 1 - i;
+            mbar_drain(bar_full + 8 * (at % kSlots), (at / kSlots) & 1);
+        }
+        for (int x = 0; fetched > 0 && x < 2; ++x) mbar_drain(bar_q + 8 * x, (fetched - 1) & 1);
+    }
+    if (tid == 0) {
+        mbar_drain(bar_drain, 0);
+        if (blockIdx.x == 0) *a.status = kStatusInReports | (int)gridDim.x;
+        report_gave_up(a.status, *abort_flag != 0);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 9) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+    if (k.ctas == 1) return;
+    // ---------------------------------------------------------------------- the cluster's parts: rows in turn to its CTAs
+    cluster_sync_all();
+    const int tile = (blockIdx.x / k.ctas) / (a.B * a.H), bh = (blockIdx.x / k.ctas) - tile * a.B * a.H, b = quotient(bh, k.heads), h = bh - b * a.H;
+    const int t0 = (k.per_head - 1 - tile) * 2 * tokens;
+    const Sample s = sample_of(a, b);
+    if (warp < 8 && t0 < s.queries) {
+        constexpr int E = D / 32;
+        const float* const ends = reinterpret_cast<const float*>(smem + S::kPartEnds);
+        for (int row = rank + k.ctas * warp; row < 2 * kTile; row += k.ctas * 8) {
+            const int x = row / kTile, rl = row - x * kTile, tl = quotient(rl, a.R), t = t0 + x * tokens + tl, hq = h * R + (rl - tl * R);
+            if (tl >= tokens || t >= s.queries) continue;
+            const bool there = lane < k.ctas;
+            const uint32_t at = cluster_map(smem_u32(ends + row), there ? lane : 0);
+            float top = kNoLogit, sum = 0.f;
+            if (there) {
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(top) : "r"(at) : "memory");
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(sum) : "r"(at + kSoftmaxThreads * 4) : "memory");
+            }
+            const float mine = top;
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+            const float f = ex2_approx(mine - top);
+            sum *= f;
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+            float v[E] = {};
+            for (int c = 0; c < k.ctas; ++c) {
+                const float fc = __shfl_sync(0xffffffffu, f, c);
+                const uint32_t from = cluster_map(base + (row * S::kPitch + lane * E) * 4, c);
+#pragma unroll
+                for (int e = 0; e < E; e += 2) {
+                    float v0, v1;
+                    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v0), "=f"(v1) : "r"(from + 4 * e) : "memory");
+                    v[e] = fmaf(v0, fc, v[e]);
+                    v[e + 1] = fmaf(v1, fc, v[e + 1]);
+                }
+            }
+            const bool none = sum == 0.f;
+            const float inv = none ? 0.f : 1.f / sum;
+            uint32_t* const out = reinterpret_cast<uint32_t*>(a.io.out + b * a.io.out_at[0] + hq * a.io.out_at[1] + t * a.io.out_at[2] + lane * E);
+#pragma unroll
+            for (int e = 0; e < E; e += 2) out[e / 2] = none ? 0u : bf16x2(v[e] * inv, v[e + 1] * inv);
+            if (a.lse && lane == 0) a.lse[((int64_t)b * a.Hq + hq) * a.Tq + t] = none ? MINUS_INF : (top + log2f(sum)) * kLn2;
+        }
+    }
+    cluster_sync_all();                                    // (the others may still be reading what this CTA has)
+}
+
+// Rows of 64 elements as operands: a map over (d, n1, n2, n3) with boxes of (64, box1, box2, 1).  A dimension of one has no stride to speak of.
+struct Dim {
+    int64_t n, stride;
+};
+bool rows_map(CUtensorMap* map, const void* data, int d, Dim x1, Dim x2, Dim x3, int box1, int box2) {
+    const Dim dims[3] = {x1, x2, x3};
+    uint64_t n[4] = {(uint64_t)d}, bytes[3];
+    for (int i = 0; i < 3; ++i) {
+        n[i + 1] = (uint64_t)dims[i].n;
+        bytes[i] = (uint64_t)(dims[i].n == 1 ? d : dims[i].stride) * 2;
+    }
+    const uint32_t box[4] = {64, (uint32_t)box1, (uint32_t)box2, 1};
+    return make_bf16_map_4d(map, data, n, bytes, box);
+}
+
+template <int D, bool TREE>
+int launch_tiles(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const TilesArgs& k, int grid, cudaStream_t stream) {
+    static DoneOnDevice done;
+    const int rc = allow_dynamic_smem(attention_tiles_kernel<D, TREE>, TilesSmem<D>::kBytes, done);
+    if (rc != VITCOP_OK) return rc;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)k.ctas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = TilesSmem<D>::kBytes;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = pdl_allowed(true) ? 2 : 1;
+    KernelTimeScope timed("attention_tiles_kernel", stream);
+    return record_cuda(cudaLaunchKernelEx(&cfg, attention_tiles_kernel<D, TREE>, mq, mk, mv, k));
+}
+
+}  // namespace
+
+// Where a call has a kernel of this kind.  Everything it refuses goes to the other kernel.
+bool tiles_kernel_takes(const SeqArgs& a, int d) {
+    const int64_t rows = (int64_t)a.R.d * a.Tq;
+    return d != 256 && a.R.d <= 64 && rows > 32 && a.N > 0;
+}
+
+// ERR_UNSUPPORTED where rows lie so that tensor copies cannot fetch them.
+int launch_attention_tiles(const SeqArgs& a, int d, cudaStream_t stream) {
+    TilesArgs k;
+    k.a = a;
+    const SeqRows& io = a.io;
+    const int R = (int)a.R.d;
+    k.tokens = kTile / R;
+    k.per_head = (a.Tq + 2 * k.tokens - 1) / (2 * k.tokens);
+    const int64_t items = (int64_t)a.B * a.H * k.per_head;
+    if (items > 0x7fffffff / 8) return VITCOP_ERR_UNSUPPORTED;
+    k.items = (int)items;
+    k.heads = divisor(a.H);
+    const auto step = [](int n, int64_t stride) { return n > 1 && stride == 0 ? 0 : 1; };
+    k.q_b = step(a.B, io.q_at[0]);
+    k.k_b = step(a.B, io.k_at[0]);
+    k.k_h = step(a.H, io.k_at[1]);
+    k.v_b = step(a.B, io.v_at[0]);
+    k.v_h = step(a.H, io.v_at[1]);
+    if (!step(a.Hq, io.q_at[1]) || !step(a.Tq, io.q_at[2]) || !step(a.N, io.k_at[2]) || !step(a.N, io.v_at[2])) return VITCOP_ERR_UNSUPPORTED;
+    CUtensorMap mq, mk, mv;
+    if (!rows_map(&mq, io.q, d, {a.Hq, io.q_at[1]}, {a.Tq, io.q_at[2]}, {k.q_b ? a.B : 1, io.q_at[0]}, R, k.tokens) ||
+        !rows_map(&mk, io.K, d, {a.N, io.k_at[2]}, {k.k_h ? a.H : 1, io.k_at[1]}, {k.k_b ? a.B : 1, io.k_at[0]}, kBlock, 1) ||
+        !rows_map(&mv, io.V, d, {a.N, io.v_at[2]}, {k.v_h ? a.H : 1, io.v_at[1]}, {k.v_b ? a.B : 1, io.v_at[0]}, kBlock, 1))
+        return VITCOP_ERR_UNSUPPORTED;
+    k.wide = reinterpret_cast<uintptr_t>(io.out) % 32 == 0 && io.out_at[0] % 16 == 0 && io.out_at[1] % 16 == 0 && io.out_at[2] % 16 == 0;
+    k.wait_ns = gram_wait_limit_ns();
+    k.expire_roles = pair_expire_roles();
+    // blocks that an item may have
+    int64_t span = a.N;
+    if (!a.tree) span = std::min<int64_t>(span, (int64_t)a.n_sink + a.window + 2 * k.tokens);
+    const int64_t blocks = (span + kBlock - 1) / kBlock;
+    const int sms = std::min(sm_count(), kMaxReports);
+    k.ctas = 1;
+    while (k.ctas < 8 && items * k.ctas * 2 <= sms && k.ctas * 2 <= blocks) k.ctas *= 2;
+    const int grid = (int)(k.ctas > 1 ? items * k.ctas : std::min<int64_t>(items, sms));
+    if (d == 64) return a.tree ? launch_tiles<64, true>(mq, mk, mv, k, grid, stream) : launch_tiles<64, false>(mq, mk, mv, k, grid, stream);
+    return a.tree ? launch_tiles<128, true>(mq, mk, mv, k, grid, stream) : launch_tiles<128, false>(mq, mk, mv, k, grid, stream);
+}
+
+}  // namespace vitcop

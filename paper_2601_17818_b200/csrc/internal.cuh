@@ -16,6 +16,8 @@ constexpr size_t kStatusBytes = 256;
 // the others.  Its CTAs report in a byte each whether they gave up, and a later kernel of the call sets the word.  (A memset
 // in front of the first kernel is 1.2 us of its own and another 1.5 until the kernel behind it starts.)
 constexpr int kReportsAt = 64, kMaxReports = (int)kStatusBytes - kReportsAt;
+// (Where a call is one kernel, the word itself says that the first n reports hold the answer: kStatusInReports | n.)
+constexpr int kStatusInReports = 1 << 30;
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 

@@ -172,4 +172,8 @@ bool make_rowmajor_bf16_map(CUtensorMap* map, const void* base, int batches, int
 // sequence or the heads reads as zero.
 bool make_keys_map(CUtensorMap* map, const void* K, int B, int H, int N, int d, int box_tokens, int box_heads);
 
+// 4-D tensor map with the 128-byte swizzle over bf16 elements, strides (of the last three dimensions) in bytes (host; gram.cu).  What lies outside reads
+// as zero.
+bool make_bf16_map_4d(CUtensorMap* map, const void* base, const uint64_t (&dims)[4], const uint64_t (&strides)[3], const uint32_t (&box)[4]);
+
 }  // namespace vitcop

@@ -345,6 +345,78 @@ def test_rows_beyond_32_bits(Tq):
     torch.cuda.empty_cache()
 
 
+def _check_long(q, K, V, lens, counts, scale, out, lse, window=NO_WINDOW, n_sink=0, tree=None):
+    """As _check, by torch in fp64 on the GPU, a head at a time: for long sequences that are all numbers."""
+    B, Hq, Tq, d = q.shape
+    R = Hq // K.shape[1]
+    for b in range(B):
+        n, m = min(max(lens[b], 0), K.shape[2]), min(max(counts[b], 0), Tq)
+        j, p = torch.arange(n, device=DEV)[None], n - m + torch.arange(m, device=DEV)[:, None]
+        if tree is None:
+            seen = (j <= p) & ((j < n_sink) | (j + window > p))
+        else:
+            seen = (j < n - m) | ((tree[b, :m, None] >> (j - (n - m)).clamp(0, 63)) & 1 == 1)
+        seen &= p >= 0
+        for h in range(Hq):
+            qd, k, v = q[b, h, :m].double(), K[b, h // R, :n].double(), V[b, h // R, :n].double()
+            z = (qd @ k.T * scale).masked_fill(~seen, -np.inf)
+            wlse = torch.logsumexp(z, -1)
+            w = torch.exp(z - wlse[:, None]).nan_to_num(0.0)
+            want, size = w @ v, w @ v.abs()
+            delta = 2.0 ** -22 * (d / 16 + 2) * abs(scale) * (qd.abs() @ k.abs().T).masked_fill(~seen, 0).amax(-1, keepdim=True)
+            tol = HALF * (1 + HALF) * (size + 2 * want.abs()) + (torch.exp(2 * delta) - 1) * (size + want.abs())
+            assert ((out[b, h, :m].double() - want).abs() <= tol).all()
+            empty = torch.isneginf(wlse)
+            assert torch.isneginf(lse[b, h, :m][empty]).all()
+            off = (lse[b, h, :m].double() - wlse).abs()[~empty]
+            assert (off <= (delta[:, 0] + 2.0 ** -20 * (1 + wlse.abs()))[~empty]).all()
+        assert (out[b, :, m:] == 9.0).all() and (lse[b, :, m:] == 9.0).all()
+
+
+@pytest.mark.parametrize("B,H,R,N,d,window,n_sink", [(1, 1, 7, 2990, 128, 700, 64), (2, 2, 2, 1501, 64, 900, 0), (3, 8, 8, 901, 128, 200, 16), (1, 2, 1, 5000, 128, NO_WINDOW, 0),
+                                                     (1, 1, 7, 3333, 64, 2000, 130), (5, 16, 1, 1290, 64, 300, 4), (1, 1, 64, 600, 128, 333, 3), (1, 1, 65, 90, 128, 33, 3)])
+def test_long_prompts(B, H, R, N, d, window, n_sink):
+    """Many blocks an item, many items a CTA."""
+    rng, q, K, V = _case(N, B, H, R, N, d, N)
+    lens = [N, 3 * N // 4, N // 5, N - 1, 1][:B]
+    out, lse = _run(q, K, V, lens, d ** -0.5, window, n_sink, counts=lens)
+    _check_long(q, K, V, lens, lens, d ** -0.5, out, lse, window, n_sink)
+    out, lse = _run(q[:, :, :N // 3], K, V, lens, d ** -0.5, window, n_sink)   # a chunk of a prompt, longer than some sequences
+    _check_long(q[:, :, :N // 3], K, V, lens, [N // 3] * B, d ** -0.5, out, lse, window, n_sink)
+
+
+@pytest.mark.parametrize("B,H,R,Tq,N,d", [(8, 4, 7, 60, 4672, 128), (1, 2, 8, 64, 16000, 64), (3, 32, 1, 64, 1111, 128), (2, 1, 7, 5, 9000, 128), (1, 4, 7, 1, 16512, 128)])
+def test_long_caches_and_large_trees(B, H, R, Tq, N, d):
+    rng, q, K, V = _case(N, B, H, R, Tq, d, N)
+    lens = [N, N - 1, Tq + 7, N // 2, N // 3, 77, N - 64, N // 4][:B]
+    tree = torch.from_numpy(_tree(rng, B, Tq)).to(DEV)
+    out, lse = _run(q, K, V, lens, d ** -0.5, tree=tree.cpu().numpy())
+    _check_long(q, K, V, lens, [Tq] * B, d ** -0.5, out, lse, tree=tree)
+    for window, n_sink in ((N // 2, 64), (130, 0)):
+        out, lse = _run(q, K, V, lens, d ** -0.5, window, n_sink)
+        _check_long(q, K, V, lens, [Tq] * B, d ** -0.5, out, lse, window, n_sink)
+
+
+@pytest.mark.parametrize("roles", [1, 2, 4])
+@pytest.mark.parametrize("B,N,Tq", [(1, 3000, 300), (16, 900, 900)])
+def test_a_wait_that_ran_out_is_reported(roles, B, N, Tq):
+    """One role of every CTA gives up at once, with copies and products of the others in flight (CTAs of a cluster on one item; CTAs with items in
+    turn); the next call is right again."""
+    H, R, d = 2, 4, 128
+    rng, q, K, V = _case(15, B, H, R, Tq, d, N)
+    ws, out = vb.alloc_workspace(vb.OP_ATTENTION, B=B, H=H, N=N, d=d, Nv=Tq, D=H * R), torch.zeros_like(q)
+    try:
+        vb.vitcop_set_wait_limit(0, roles)
+        vb.vitcop_window_attention(q, K, V, None, out, ws, d ** -0.5, 500, 4)
+        assert vb.vitcop_poll_status(ws) == vb.ERR_TIMEOUT
+    finally:
+        vb.vitcop_set_wait_limit(0, 0)
+    out, lse = _run(q, K, V, None, d ** -0.5, 500, 4, workspace=ws)
+    again, lse2 = _run(q, K, V, None, d ** -0.5, 500, 4)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+    _check_long(q[:1], K[:1], V[:1], [N], [Tq], d ** -0.5, out, lse, 500, 4)
+
+
 def test_no_rows_and_nothing_to_do():
     rng, q, K, V = _case(10, 2, 2, 2, 3, 64, 40)
     out, lse = _run(q, K[:, :, :0], V[:, :, :0], None, 0.1)
