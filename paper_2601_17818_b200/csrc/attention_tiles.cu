@@ -5,11 +5,12 @@
 // what a first block reaches back beyond its segment, or the sequence, is masked.  Of a block that a tile sees in part only the 32-token
 // columns that it sees are worked on.
 //   warps 0-3, 4-7  softmax of a tile, a thread a row: logits from tensor memory, weights back to where the logits were, as the operand of
-//                   the second product; a row's maximum is moved, and its sums with it, only when a logit has passed it by 2^8
-//   warp 8          tensor copies: queries, then K and V of a block in turn through a ring
+//                   the second product.  Weights are made with the row's maximum so far while the block's own is looked for; only when a logit
+//                   has passed it by 2^8 is it moved, the sums so far with it, and the weights are made anew
+//   warp 8          tensor copies: queries, then K and V of a block in turn through a ring.  Rows of V that are no numbers must not reach rows that do
+//                   not see them, and 0 times NaN does: blocks that are masked are looked through, such rows taken out and added again at the end
+//                   for those who see them
 //   warp 9          products: PV(A), QK(A), PV(B), QK(B): while one tile's softmax runs, the other's products do
-//   warps 10, 11    rows of V that are no numbers must not reach rows that do not see them, and 0 times NaN does: blocks that are masked are looked
-//                   through, such rows taken out and added again at the end for those who see them
 // A CTA takes items in turn, the next item's first products under the last one's output.  Where items are fewer than SMs, a cluster of up to eight CTAs
 // shares an item's blocks and joins its parts in shared memory.
 #include "attention.cuh"
@@ -23,15 +24,16 @@ namespace vitcop {
 namespace {
 
 constexpr int kTile = 128, kBlock = 128;
-constexpr int kSoftmaxThreads = 256, kThreads = kSoftmaxThreads + 128;
-constexpr int kMasked = 16;                                // blocks of an item that a tile sees in part: at most two at either edge of a tile's
-                                                           // window, two where its segments begin, two where the sinks end
+constexpr int kSoftmaxThreads = 256, kLoadWarp = kSoftmaxThreads / 32, kMmaWarp = kLoadWarp + 1;
+// Two warps have nothing to do: registers change hands by four warps, and a row's 128 logits want more than the 168 a thread that the block is launched
+// with.  (Next to 227 KB of shared memory there is no cache to spill to.)
+constexpr int kThreads = kSoftmaxThreads + 128, kSoftmaxRegs = 208, kOtherRegs = 88;
+static_assert(kSoftmaxThreads * kSoftmaxRegs + 128 * kOtherRegs == kThreads * 168, "registers that are asked for and not there are waited for, for ever");
+constexpr int kMasked = 14;                                // blocks of an item that a tile sees in part: of either tile at most two at the end of its
+                                                           // window, two where it begins, two where the sinks end; and the first
 constexpr float kMayPass = 8.f;
+constexpr int kItemBytes = 128;
 enum { kRoleLoad = 1, kRoleMma = 2, kRoleSoftmax = 4 };
-
-struct Item {
-    int there, b, h, t0, len, queries, k0, k1;
-};
 
 template <int D>
 struct TilesSmem {
@@ -41,10 +43,11 @@ struct TilesSmem {
     static constexpr int kQ = 0;
     static constexpr int kRing = 2 * kOperand;
     static constexpr int kBars = kRing + kSlots * kOperand;
-    static constexpr int kItems = kBars + 400;                         // two of them
-    static constexpr int kBad = kItems + 2 * (int)sizeof(Item);        // [2][kMasked][4] words: rows of V that were taken out
-    static constexpr int kBytes = kBars + 2048 + 1024;                 // (and what aligning to 1024 takes)
-    static_assert(kBad + 2 * kMasked * 16 + 16 <= kBars + 2048);
+    static constexpr int kFlags = kBars + 24 * kSlots + 144;        // behind the barriers
+    static constexpr int kItems = (kFlags + 24 + 15) / 16 * 16;                        // two of them
+    static constexpr int kBad = kItems + 2 * kItemBytes;        // [2][kMasked][4] words: rows of V that were taken out
+    static constexpr int kBytes = kBad + 2 * kMasked * 16;
+    static_assert(kBytes <= 232448);
     // parts of a cluster, where the operands were: [256 rows][D + 4] and [3][256]
     static constexpr int kPitch = D + 4;
     static constexpr int kPartEnds = 256 * kPitch * 4;
@@ -62,23 +65,45 @@ struct TilesArgs {
     __device__ __forceinline__ unsigned long long limit_of(int role) const { return (expire_roles & role) ? 0ull : wait_ns; }
 };
 
+// As mbar_wait, for a warp.  One lane asks, the others step along: a barrier asked by 32 lanes of 16 warps holds up all else that goes through shared
+// memory's pipe, and where one lane loops apart from the others the first access to tensor memory behind it takes 600 cycles.
+__device__ __forceinline__ bool asked(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, 0, 0;\n\tsetp.eq.u32 q, %3, 0;\n\t"
+        "@q mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity), "r"(threadIdx.x & 31)
+        : "memory");
+    return __any_sync(0xffffffffu, done != 0);
+}
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned long long limit_ns) {
+    unsigned long long t0 = 0ull;
+    bool in_time = limit_ns != 0ull;
+    for (uint32_t it = 1; in_time; ++it) {
+        if (asked(bar, parity)) return true;
+        if ((it & 63u) == 0u) {                            // (reading the clock takes longer than most waits)
+            const unsigned long long now = __shfl_sync(0xffffffffu, global_ns(), 0);
+            if (t0 == 0ull) t0 = now;
+            in_time = !__any_sync(0xffffffffu, *abort_flag != 0) && now - t0 <= limit_ns;
+        }
+    }
+    *abort_flag = 1;
+    return false;
+}
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-// Called by a warp of which one lane issues.
-__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
-        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-        : "memory");
+// One lane of a warp, the same each time.
+__device__ __forceinline__ bool elected() {
+    uint32_t e;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+    return e != 0;
 }
-__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+// As tc_mma_bf16, the first operand in tensor memory.
+__device__ __forceinline__ void tc_mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
-        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem), "r"(a_tmem),
+        "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
-}
-__device__ __forceinline__ void commit_one(uint32_t bar) {
-    asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
-                 ::"r"(bar) : "memory");
 }
 // Operand whose 64-element rows (128 bytes, swizzled) run along the product's N: 8 of them (steps of its K) are 1024 bytes, the next 64 of N 16384 further.
 __device__ __forceinline__ uint64_t umma_desc_mn128(uint32_t smem_addr) {
@@ -107,6 +132,15 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
         "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
         "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&o)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3]), "=r"(o[4]), "=r"(o[5]), "=r"(o[6]), "=r"(o[7]), "=r"(o[8]), "=r"(o[9]), "=r"(o[10]),
+          "=r"(o[11]), "=r"(o[12]), "=r"(o[13]), "=r"(o[14]), "=r"(o[15])
+        : "r"(taddr)
         : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -143,7 +177,40 @@ __device__ __forceinline__ Columns columns_of(const Blocks& x, int k, const Span
     return c;
 }
 
-// Bits c of a word: a <= c < b.
+// Blocks first .. end - 1 of a window (a whole sequence), which all rows of a tile see all of: what most blocks are.
+struct Whole {
+    int first, end;
+};
+template <bool TREE>
+__device__ __forceinline__ Whole whole_of(const Blocks& x, const Span& tile) {
+    const int lo = TREE ? 0 : max(tile.all_lo, x.v.b0), hi = TREE ? tile.all_front : tile.all_hi;
+    // block i ends at b1 - (n - 1 - i) 128: not behind hi, and begins not in front of lo
+    const int behind = max(0, x.v.b1 - hi), room = x.v.b1 - lo - kBlock;
+    Whole w = {x.n, x.n};
+    if (hi > 0 && room >= 0) {
+        w.end = x.n - (behind + kBlock - 1) / kBlock;
+        w.first = max(x.na, x.n - 1 - room / kBlock);
+    }
+    return w;
+}
+
+// What a CTA works on next: two tiles of a head, as the load warp leaves it.
+struct Tile {
+    Span span;
+    Whole whole;
+    __device__ __forceinline__ Columns columns(const Blocks& x, int k) const {
+        const Columns c = {0, kBlock, true};
+        return k >= whole.first && k < whole.end ? c : columns_of(x, k, span);
+    }
+};
+struct Item {
+    int there, b, h, t0, len, queries, k0, k1;
+    Blocks blocks;
+    Tile tiles[2];
+};
+static_assert(sizeof(Item) == kItemBytes);
+
+// Bits below x of a word.
 __device__ __forceinline__ uint32_t below(int x) { return x <= 0 ? 0u : x >= 32 ? 0xffffffffu : (1u << x) - 1u; }
 __device__ __forceinline__ uint32_t bits_of(const Seen<false>& s, int j0) { return below(s.front - j0) | (below(s.p + 1 - j0) & ~below(s.lo - j0)); }
 __device__ __forceinline__ uint32_t bits_of(const Seen<true>& s, int j0) {
@@ -152,25 +219,25 @@ __device__ __forceinline__ uint32_t bits_of(const Seen<true>& s, int j0) {
     return below(s.front - j0) | (drafted & below(s.len - j0) & ~below(-j0));
 }
 
-// What tokens whose V was taken out add to a row: in fp32, from where they lie.
+// What tokens whose V was taken out add to a row, elements `from` .. `from` + 31: in fp32, from where they lie.
 template <int D, bool TREE>
-__device__ __noinline__ void add_taken_out(const TilesArgs& k, const Blocks& x, const Span* spans, int k0, int k1, const uint32_t* bad, const Seen<TREE>& seen,
-                                           const __nv_bfloat16* q, const __nv_bfloat16* Kh, const __nv_bfloat16* Vh, float top, int part, float (&v)[32]) {
+__device__ __noinline__ void add_taken_out(const SeqArgs& a, const Item& it, const Seen<TREE>& seen, const uint32_t* bad, int hq, int t, int from, float top, float (&v)[32]) {
+    const __nv_bfloat16* const q = a.io.q + it.b * a.io.q_at[0] + hq * a.io.q_at[1] + t * a.io.q_at[2];
+    const __nv_bfloat16* const K = a.io.K + it.b * a.io.k_at[0] + it.h * a.io.k_at[1];
+    const __nv_bfloat16* const V = a.io.V + it.b * a.io.v_at[0] + it.h * a.io.v_at[1] + from;
     int n = 0;
-    for (int i = k0; i < k1; ++i) {
-        const Columns ca = columns_of(x, i, spans[0]), cb = columns_of(x, i, spans[1]);
-        if (ca.all && cb.all) continue;
-        const int start = x.end(i) - kBlock, from = max(start, x.begin_of_segment(i));
+    for (int i = it.k0; i < it.k1; ++i) {
+        if (it.tiles[0].columns(it.blocks, i).all && it.tiles[1].columns(it.blocks, i).all) continue;
+        const int start = it.blocks.end(i) - kBlock, segment = it.blocks.begin_of_segment(i);
         for (int w = 0; w < 4; ++w) {
             for (uint32_t left = bad[n * 4 + w]; left; left &= left - 1) {
-                const int j = start + w * 32 + __ffs(left) - 1;
-                if (j < from || !seen(j)) continue;
+                const int64_t j = start + w * 32 + __ffs(left) - 1;
+                if (j < segment || !seen((int)j)) continue;
                 float z = 0.f;
-                for (int e = 0; e < D; ++e) z = fmaf(__bfloat162float(q[e]), __bfloat162float(Kh[j * k.a.io.k_at[2] + e]), z);
-                z = k.a.sign ? -z : z;
-                const float p = ex2_approx(fmaf(z, k.a.scale_log2, -top));
+                for (int e = 0; e < D; ++e) z = fmaf(__bfloat162float(q[e]), __bfloat162float(K[j * a.io.k_at[2] + e]), z);
+                const float p = ex2_approx(fmaf(a.sign ? -z : z, a.scale_log2, -top));
 #pragma unroll
-                for (int e = 0; e < 32; ++e) v[e] = fmaf(p, __bfloat162float(Vh[j * k.a.io.v_at[2] + part * 32 + e]), v[e]);
+                for (int e = 0; e < 32; ++e) v[e] = fmaf(p, __bfloat162float(V[j * a.io.v_at[2] + e]), v[e]);
             }
         }
         ++n;
@@ -184,39 +251,38 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     using S = TilesSmem<D>;
     constexpr int kSlots = S::kSlots, kSubs = S::kSubs;
     const SeqArgs& a = k.a;
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t base = smem_u32(smem);
     const uint32_t bar_full = base + S::kBars, bar_empty = bar_full + 8 * kSlots, bar_q = bar_empty + 8 * kSlots, bar_q_free = bar_q + 16, bar_s = bar_q_free + 8,
                    bar_p = bar_s + 16, bar_o = bar_p + 16, bar_o_free = bar_o + 16, bar_item = bar_o_free + 16, bar_done = bar_item + 16,
-                   bar_drain = bar_done + 16, bar_checked = bar_drain + 8;
-    volatile int* const abort_flag = reinterpret_cast<volatile int*>(smem + S::kBars + 376);
-    uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + S::kBars + 380);
-    volatile int* const any_bad = reinterpret_cast<volatile int*>(smem + S::kBars + 384);           // [2 items][2 warps]
-    volatile Item* const items = reinterpret_cast<volatile Item*>(smem + S::kItems);
+                   bar_drain = bar_done + 16, bar_p2 = bar_drain + 8, bar_checked = bar_p2 + 16;
+    volatile int* const abort_flag = reinterpret_cast<volatile int*>(smem + S::kFlags);
+    uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + S::kFlags + 4);
+    volatile int* const any_bad = reinterpret_cast<volatile int*>(smem + S::kFlags + 8);           // [2 items]
     uint32_t* const bad = reinterpret_cast<uint32_t*>(smem + S::kBad);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
         for (int i = 0; i < kSlots; ++i) {
             mbar_init(bar_full + 8 * i, 1);
-            mbar_init(bar_empty + 8 * i, 3);               // the products' end, and both warps that look through V
-            mbar_init(bar_checked + 8 * i, 64);
+            mbar_init(bar_empty + 8 * i, 1);
+            mbar_init(bar_checked + 8 * i, 1);
         }
         for (int x = 0; x < 2; ++x) {
             mbar_init(bar_q + 8 * x, 1);
             mbar_init(bar_s + 8 * x, 1);
-            mbar_init(bar_p + 8 * x, kTile);
+            mbar_init(bar_p + 8 * x, 4);
+            mbar_init(bar_p2 + 8 * x, 4);
             mbar_init(bar_o + 8 * x, 1);
-            mbar_init(bar_o_free + 8 * x, kTile);
+            mbar_init(bar_o_free + 8 * x, 4);
             mbar_init(bar_item + 8 * x, 1);
-            mbar_init(bar_done + 8 * x, kSoftmaxThreads / 32 + 3);
+            mbar_init(bar_done + 8 * x, kSoftmaxThreads / 32 + 1);
         }
         mbar_init(bar_q_free, 1);
         mbar_init(bar_drain, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 9) tmem_alloc(smem_u32(tmem_slot), 512);
+    if (warp == kMmaWarp) tmem_alloc(smem_u32(tmem_slot), 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -229,188 +295,175 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     const int rank = blockIdx.x & (k.ctas - 1);
     uint32_t issued = 0, fetched = 0;                      // operands and items whose copies the load lane has started
     const int R = (int)a.R.d, tokens = k.tokens;
-    const auto spans_of = [&](const Sample& s, int t0, Span (&v)[2]) {
-        v[0] = span_of<TREE>(a, s, t0, t0 + tokens - 1);
-        v[1] = span_of<TREE>(a, s, t0 + tokens, t0 + 2 * tokens - 1);
-    };
     const auto sample_in = [&](const Item& it) {
         const Sample s = {it.len, it.queries, it.len - it.queries};
         return s;
     };
-    // item n of this CTA, as the load warp leaves it
-    const auto item_at = [&](int n, unsigned long long lim, Item& it) {
-        if (!__all_sync(0xffffffffu, mbar_wait(bar_item + 8 * (n & 1), (n >> 1) & 1, abort_flag, lim))) return false;
-        volatile Item& from = items[n & 1];
-        it.there = from.there;
-        it.b = from.b;
-        it.h = from.h;
-        it.t0 = from.t0;
-        it.len = from.len;
-        it.queries = from.queries;
-        it.k0 = from.k0;
-        it.k1 = from.k1;
-        return it.there != 0;
+    // whether there is an item n for this CTA
+    const Item* const items = reinterpret_cast<const Item*>(smem + S::kItems);
+    const auto item_there = [&](int n, unsigned long long lim) {
+        return warp_wait(bar_item + 8 * (n & 1), (n >> 1) & 1, abort_flag, lim) && items[n & 1].there != 0;
     };
 
-    if (warp < 8) {
+    if (warp < kLoadWarp) {
         // ------------------------------------------------------------------ softmax
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-        const unsigned long long lim = k.limit_of(kRoleSoftmax);
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         const int x = warp >> 2, row = tid & (kTile - 1), tl = quotient(row, a.R), r = row - tl * R;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_at = tmem_s(x) + lanes, o_at = tmem_o(x) + lanes;
-        uint32_t phase_s = 0, phase_o = 0, phase_other = 0;
+        uint32_t phase_s = 0, phase_o = 0;
         const f32x2 scale2 = pack2(a.scale_log2, a.scale_log2);
-        Item it;
         bool ok = true;
-        for (int n = 0; ok && item_at(n, lim, it); ++n) {
-            const Sample s = sample_in(it);
-            const Blocks blocks = blocks_of<TREE>(a, s, it.t0, it.t0 + 2 * tokens - 1);
-            Span spans[2];
-            spans_of(s, it.t0, spans);
-            const int t = it.t0 + x * tokens + tl;
-            const bool there = tl < tokens && t < s.queries;
-            const Seen<TREE> seen(a, s, it.b, there ? t : s.queries);
+        const auto waited = [&](uint32_t bar, uint32_t parity) { return warp_wait(bar, parity, abort_flag, k.limit_of(kRoleSoftmax)); };
+        const auto tell = [&](uint32_t bar) {              // what this warp has written to tensor memory is there
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar);
+        };
+        for (int n = 0; ok && item_there(n, k.limit_of(kRoleSoftmax)); ++n) {
+            const Item& it = items[n & 1];
+            // (made anew where it is wanted, in the blocks that are masked)
+            const auto seen_by_row = [&]() {
+                const int t = it.t0 + x * tokens + tl;
+                return Seen<TREE>(a, sample_in(it), it.b, tl < tokens && t < it.queries ? t : it.queries);
+            };
             float top = kNoLogit;                          // in powers of two; weights are 2^(logit - top)
-            f32x2 sum0 = pack2(0.f, 0.f), sum1 = sum0;
+            f32x2 sum = pack2(0.f, 0.f);
             int count = 0;
-            for (int i = it.k0; i < it.k1; ++i) {
-                const Columns c = columns_of(blocks, i, spans[x]);
+            const Whole whole = it.tiles[x].whole;
+            const int k1 = it.k1;
+            for (int i = it.k0; i < k1; ++i) {
+                Columns c = {0, kBlock, true};
+                if (!(i >= whole.first && i < whole.end)) c = columns_of(it.blocks, i, it.tiles[x].span);
                 if (c.lo == c.hi) continue;
-                ok = __all_sync(0xffffffffu, mbar_wait(bar_s + 8 * x, phase_s, abort_flag, lim));
+                ok = waited(bar_s + 8 * x, phase_s);
                 if (!ok) break;
                 phase_s ^= 1;
                 tc_fence_after();
                 uint32_t z[4][32];
 #pragma unroll
-                for (int w = 0; w < 4; ++w)
-                    if (w * 32 >= c.lo && w * 32 < c.hi) tmem_ld32_issue(s_at + w * 32, z[w]);
+                for (int w = 0; w < 4; ++w) tmem_ld32_issue(s_at + w * 32, z[w]);      // (columns that were not worked on are anything)
                 tmem_ld_wait();
-                float high = MINUS_INF;
-                const int start = blocks.end(i) - kBlock, segment = blocks.begin_of_segment(i);
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    if (w * 32 >= c.lo && w * 32 < c.hi) {
-                        pin32(z[w]);
-                        if (!c.all) {
-                            const uint32_t keep = bits_of(seen, start + w * 32) & ~below(segment - start - w * 32);
+                for (int w = 0; w < 4; ++w) pin32(z[w]);
+                if (!c.all || c.hi - c.lo < kBlock) {
+                    const Seen<TREE> seen = seen_by_row();
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) z[w][e] = keep >> e & 1 ? z[w][e] : 0xff800000u;
-                        }
-                        float h0 = MINUS_INF, h1 = MINUS_INF;
+                    for (int w = 0; w < 4; ++w) {
+                        const int j0 = it.blocks.end(i) - kBlock + w * 32;
+                        const uint32_t keep = w * 32 >= c.lo && w * 32 < c.hi ? bits_of(seen, j0) & ~below(it.blocks.begin_of_segment(i) - j0) : 0u;
 #pragma unroll
-                        for (int e = 0; e < 32; e += 4) {
-                            h0 = fmaxf(h0, fmaxf(__uint_as_float(z[w][e]), __uint_as_float(z[w][e + 1])));
-                            h1 = fmaxf(h1, fmaxf(__uint_as_float(z[w][e + 2]), __uint_as_float(z[w][e + 3])));
-                        }
-                        high = fmaxf(high, fmaxf(h0, h1));
+                        for (int e = 0; e < 32; ++e) z[w][e] = keep >> e & 1 ? z[w][e] : 0xff800000u;
                     }
                 }
-                high *= a.scale_log2;
+                f32x2 more = pack2(0.f, 0.f), more2 = more;
+                const auto weights = [&](int w) {          // of 32 columns
+                    const f32x2 top2 = pack2(-top, -top);
+                    uint32_t p[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float2 y = unpack2(fma2(pack2(__uint_as_float(z[w][2 * e]), __uint_as_float(z[w][2 * e + 1])), scale2, top2));
+                        const float p0 = ex2_approx(y.x), p1 = ex2_approx(y.y);
+                        if (e & 1) more2 = add2(more2, pack2(p0, p1));
+                        else more = add2(more, pack2(p0, p1));
+                        p[e] = bf16x2(p0, p1);
+                    }
+                    tmem_st16(s_at + w * 16, p);
+                };
+                float h[4] = {MINUS_INF, MINUS_INF, MINUS_INF, MINUS_INF};
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    weights(w);
+#pragma unroll
+                    for (int v = 2 * w; v < 2 * w + 2; ++v)
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) h[e / 2 & 3] = fmaxf(h[e / 2 & 3], fmaxf(__uint_as_float(z[v][e]), __uint_as_float(z[v][e + 1])));
+                }
+                const float high = fmaxf(fmaxf(h[0], h[1]), fmaxf(h[2], h[3])) * a.scale_log2;
                 if (__any_sync(0xffffffffu, high - top > kMayPass)) {
                     const float now = fmaxf(top, high), keep = ex2_approx(top - now);
                     top = now;
-                    const f32x2 keep2 = pack2(keep, keep);
-                    sum0 = mul2(sum0, keep2);
-                    sum1 = mul2(sum1, keep2);
+                    sum = mul2(sum, pack2(keep, keep));
                     if (count > 0) {                       // (the products so far have ended: the logits' came behind them)
 #pragma unroll 1
                         for (int e = 0; e < D; e += 16) {
                             uint32_t o[16];
-                            asm volatile(
-                                "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
-                                "tcgen05.wait::ld.sync.aligned;"
-                                : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3]), "=r"(o[4]), "=r"(o[5]), "=r"(o[6]), "=r"(o[7]), "=r"(o[8]), "=r"(o[9]),
-                                  "=r"(o[10]), "=r"(o[11]), "=r"(o[12]), "=r"(o[13]), "=r"(o[14]), "=r"(o[15])
-                                : "r"(o_at + e)
-                                : "memory");
+                            tmem_ld16(o_at + e, o);
 #pragma unroll
                             for (int u = 0; u < 16; ++u) o[u] = __float_as_uint(__uint_as_float(o[u]) * keep);
                             tmem_st16(o_at + e, o);
                         }
                     }
+                    more = more2 = pack2(0.f, 0.f);
+                    weights(0);
+                    weights(1);
                 }
                 ++count;
-                const f32x2 top2 = pack2(-top, -top);
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    if (w * 32 >= c.lo && w * 32 < c.hi) {
-                        uint32_t p[16];
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const float2 y = unpack2(fma2(pack2(__uint_as_float(z[w][2 * e]), __uint_as_float(z[w][2 * e + 1])), scale2, top2));
-                            const float p0 = ex2_approx(y.x), p1 = ex2_approx(y.y);
-                            if (e & 1) sum1 = add2(sum1, pack2(p0, p1));
-                            else sum0 = add2(sum0, pack2(p0, p1));
-                            p[e] = bf16x2(p0, p1);
-                        }
-                        tmem_st16(s_at + w * 16, p);
-                    }
-                }
                 tmem_st_wait();
-                tc_fence_before();
-                mbar_arrive(bar_p + 8 * x);
+                tell(bar_p + 8 * x);
+                weights(2);
+                weights(3);
+                sum = add2(sum, add2(more, more2));
+                tmem_st_wait();
+                tell(bar_p2 + 8 * x);
             }
             if (!ok) break;
             // ---- the output
-            const float2 sa = unpack2(sum0), sb = unpack2(sum1);
-            const float sum = (sa.x + sa.y) + (sb.x + sb.y);
+            const float2 both = unpack2(sum);
+            const float total = both.x + both.y;
             if (count > 0) {
-                ok = __all_sync(0xffffffffu, mbar_wait(bar_o + 8 * x, phase_o, abort_flag, lim));
+                ok = waited(bar_o + 8 * x, phase_o);
                 if (!ok) break;
                 phase_o ^= 1;
                 tc_fence_after();
             }
-            const bool none = sum == 0.f, alone = k.ctas == 1;
-            const float inv = none ? 0.f : 1.f / sum;
-            const int hq = it.h * R + r;
-            const __nv_bfloat16* const q = a.io.q + it.b * a.io.q_at[0] + hq * a.io.q_at[1] + t * a.io.q_at[2];
+            const bool none = total == 0.f, alone = k.ctas == 1;
+            const float inv = none ? 0.f : 1.f / total;
+            const int hq = it.h * R + r, t = it.t0 + x * tokens + tl;
+            const bool there = tl < tokens && t < it.queries;
             __nv_bfloat16* const out = a.io.out + it.b * a.io.out_at[0] + hq * a.io.out_at[1] + t * a.io.out_at[2];
-            const bool odd = (any_bad[(n & 1) * 2] | any_bad[(n & 1) * 2 + 1]) != 0;
+            const bool odd = any_bad[n & 1] != 0;
             float* const part = reinterpret_cast<float*>(smem) + (x * kTile + row) * S::kPitch;
             if (!alone) {
                 // parts go where operands were: the other tile's products have to have ended too
                 bool other = false;
                 for (int i = it.k0; i < it.k1; ++i) {
-                    const Columns c = columns_of(blocks, i, spans[x ^ 1]);
+                    const Columns c = it.tiles[x ^ 1].columns(it.blocks, i);
                     other |= c.lo != c.hi;
                 }
-                if (other) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(bar_o + 8 * (x ^ 1), phase_other, abort_flag, lim));
-                    if (!ok) break;
-                    phase_other ^= 1;
-                }
+                // (one item a CTA: its first output)
+                ok = !other || waited(bar_o + 8 * (x ^ 1), 0);
+                if (!ok) break;
                 reinterpret_cast<float*>(smem + S::kPartEnds)[x * kTile + row] = top;
-                reinterpret_cast<float*>(smem + S::kPartEnds)[kSoftmaxThreads + x * kTile + row] = sum;
+                reinterpret_cast<float*>(smem + S::kPartEnds)[2 * kTile + x * kTile + row] = total;
             } else if (a.lse && there) {
-                a.lse[((int64_t)it.b * a.Hq + hq) * a.Tq + t] = none ? MINUS_INF : (top + log2f(sum)) * kLn2;
+                a.lse[((int64_t)it.b * a.Hq + hq) * a.Tq + t] = none ? MINUS_INF : (top + log2f(total)) * kLn2;
             }
 #pragma unroll 1
             for (int e = 0; e < D; e += 32) {
-                float v[32];
+                uint32_t o[32];
                 __syncwarp();
                 if (count > 0) {
-                    tmem_ld32(o_at + e, v);
+                    tmem_ld32_issue(o_at + e, o);
+                    tmem_ld_wait();
+                    pin32(o);
                 } else {
 #pragma unroll
-                    for (int u = 0; u < 32; ++u) v[u] = 0.f;
+                    for (int u = 0; u < 32; ++u) o[u] = 0;
                 }
                 if (odd && there) {
-                    const Span both[2] = {spans[0], spans[1]};
-                    const Blocks all = blocks;
-                    const Seen<TREE> sees = seen;
+                    const Seen<TREE> sees = seen_by_row();
                     float extra[32] = {};
-                    add_taken_out<D, TREE>(k, all, both, it.k0, it.k1, bad + (n & 1) * kMasked * 4, sees, q,
-                                           a.io.K + it.b * a.io.k_at[0] + it.h * a.io.k_at[1], a.io.V + it.b * a.io.v_at[0] + it.h * a.io.v_at[1], top, e / 32, extra);
+                    add_taken_out<D, TREE>(a, it, sees, bad + (n & 1) * kMasked * 4, hq, t, e, top, extra);
 #pragma unroll
-                    for (int u = 0; u < 32; ++u) v[u] += extra[u];
+                    for (int u = 0; u < 32; ++u) o[u] = __float_as_uint(__uint_as_float(o[u]) + extra[u]);
                 }
                 if (!alone) {
 #pragma unroll
-                    for (int u = 0; u < 32; u += 4) *reinterpret_cast<float4*>(part + e + u) = make_float4(v[u], v[u + 1], v[u + 2], v[u + 3]);
+                    for (int u = 0; u < 32; u += 4) *reinterpret_cast<uint4*>(part + e + u) = make_uint4(o[u], o[u + 1], o[u + 2], o[u + 3]);
                 } else if (there) {
                     uint32_t p[16];
 #pragma unroll
-                    for (int u = 0; u < 16; ++u) p[u] = none ? 0u : bf16x2(v[2 * u] * inv, v[2 * u + 1] * inv);
+                    for (int u = 0; u < 16; ++u) p[u] = none ? 0u : bf16x2(__uint_as_float(o[2 * u]) * inv, __uint_as_float(o[2 * u + 1]) * inv);
                     if (k.wide) {
 #pragma unroll
                         for (int u = 0; u < 16; u += 8)
@@ -422,235 +475,234 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     }
                 }
             }
-            __syncwarp();
-            if (count > 0) {
-                tc_fence_before();
-                mbar_arrive(bar_o_free + 8 * x);
-            }
+            if (count > 0) tell(bar_o_free + 8 * x);
             __syncwarp();
             if (lane == 0) mbar_arrive(bar_done + 8 * (n & 1));
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-        if (warp == 8) {
-            // -------------------------------------------------------------- tensor copies
-            if (lane == 0) {
-                const unsigned long long lim = k.limit_of(kRoleLoad);
-                uint32_t slot = 0, phase = 0;
-                int n = 0;
-                bool ok = true;
-                const auto fetch = [&](const CUtensorMap* map, int row, int h, int b) {   // an operand to the ring
-                    if (!mbar_wait(bar_empty + 8 * slot, phase ^ 1, abort_flag, lim)) return false;
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if (warp == kLoadWarp) {
+            // ------------------------------------------------------------------ tensor copies
+            const auto waited = [&](uint32_t bar, uint32_t parity) { return warp_wait(bar, parity, abort_flag, k.limit_of(kRoleLoad)); };
+            uint32_t slot = 0, phase = 0;
+            int n = 0;
+            bool ok = true;
+            const auto fetch = [&](const CUtensorMap* map, int row, int h, int b) {        // an operand to the ring
+                if (!waited(bar_empty + 8 * slot, phase ^ 1)) return false;
+                if (lane == 0) {
                     mbar_expect_tx(bar_full + 8 * slot, S::kOperand);
 #pragma unroll
                     for (int i = 0; i < kSubs; ++i) tma_load_4d(base + S::kRing + slot * S::kOperand + i * 16384, map, bar_full + 8 * slot, i * 64, row, h, b);
-                    ++issued;
-                    if (++slot == (uint32_t)kSlots) {
-                        slot = 0;
-                        phase ^= 1;
+                }
+                ++issued;
+                if (++slot == (uint32_t)kSlots) {
+                    slot = 0;
+                    phase ^= 1;
+                }
+                return true;
+            };
+            // the rows of V in a slot that are no numbers become zeros; a lane has rows lane, lane + 32, ..
+            const auto take_out = [&](uint32_t at, uint32_t parity, uint32_t* words) {
+                if (!waited(bar_full + 8 * at, parity)) return false;
+                uint8_t* const v = smem + S::kRing + at * S::kOperand;
+                uint32_t found_any = 0;
+#pragma unroll 1
+                for (int w = 0; w < 4; ++w) {
+                    uint8_t* const row = v + (w * 32 + lane) * 128;
+                    uint32_t any = 0;
+#pragma unroll
+                    for (int e = 0; e < kSubs * 8; ++e) {      // (pieces in another order in each lane: eight lie in all banks)
+                        const uint4 y = *reinterpret_cast<const uint4*>(row + (e / 8) * 16384 + ((e + lane) & 7) * 16);
+                        any |= ((y.x & 0x7F807F80u) + 0x00800080u) | ((y.y & 0x7F807F80u) + 0x00800080u) | ((y.z & 0x7F807F80u) + 0x00800080u) |
+                               ((y.w & 0x7F807F80u) + 0x00800080u);
                     }
-                    return true;
-                };
-                const auto publish = [&](const Item& it) {
-                    if (n >= 2 && !mbar_wait(bar_done + 8 * (n & 1), ((n >> 1) - 1) & 1, abort_flag, lim)) return false;
-                    volatile Item& to = items[n & 1];
-                    to.there = it.there;
-                    to.b = it.b;
-                    to.h = it.h;
-                    to.t0 = it.t0;
-                    to.len = it.len;
-                    to.queries = it.queries;
-                    to.k0 = it.k0;
-                    to.k1 = it.k1;
+                    const bool odd = (any & 0x80008000u) != 0; // (an exponent of ones carries into the sign's place)
+                    if (odd)
+                        for (int e = 0; e < kSubs * 8; ++e) *reinterpret_cast<uint4*>(row + (e / 8) * 16384 + (e & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    const uint32_t found = __ballot_sync(0xffffffffu, odd);
+                    if (lane == 0) words[w] = found;
+                    found_any |= found;
+                }
+                if (lane == 0 && found_any) any_bad[n & 1] = 1;
+                fence_async_proxy();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_checked + 8 * at);
+                return true;
+            };
+            const auto publish = [&](const Item& it) {
+                if (n >= 2 && !waited(bar_done + 8 * (n & 1), ((n >> 1) - 1) & 1)) return false;
+                if (lane == 0) {
+                    *reinterpret_cast<Item*>(smem + S::kItems + (n & 1) * kItemBytes) = it;
+                    any_bad[n & 1] = 0;
                     mbar_arrive(bar_item + 8 * (n & 1));
-                    return true;
-                };
-                // the last tokens first: in front of a full window they are the ones with the most to look at
-                for (int i = blockIdx.x / k.ctas; ok && i < k.items; i += gridDim.x / k.ctas) {
-                    const int bhs = a.B * a.H, tile = i / bhs, bh = i - tile * bhs, b = quotient(bh, k.heads), h = bh - b * a.H;
-                    const int t0 = (k.per_head - 1 - tile) * 2 * tokens;
-                    const Sample s = sample_of(a, b);
-                    if (t0 >= s.queries) continue;
-                    const Blocks blocks = blocks_of<TREE>(a, s, t0, t0 + 2 * tokens - 1);
-                    const int each = blocks.n / k.ctas, more = blocks.n - each * k.ctas;
-                    Item it = {1, b, h, t0, s.len, s.queries, rank * each + min(rank, more), 0};
-                    it.k1 = it.k0 + each + (rank < more ? 1 : 0);
-                    ok = publish(it) && (n == 0 || mbar_wait(bar_q_free, (n - 1) & 1, abort_flag, lim));
-                    if (!ok) break;
+                }
+                __syncwarp();
+                return true;
+            };
+            // the last tokens first: in front of a full window they are the ones with the most to look at
+            for (int i = blockIdx.x / k.ctas; ok && i < k.items; i += gridDim.x / k.ctas) {
+                const int bhs = a.B * a.H, tile = i / bhs, bh = i - tile * bhs, b = quotient(bh, k.heads), h = bh - b * a.H;
+                const int t0 = (k.per_head - 1 - tile) * 2 * tokens;
+                const Sample s = sample_of(a, b);
+                if (t0 >= s.queries) continue;
+                Item it;
+                it.there = 1;
+                it.b = b;
+                it.h = h;
+                it.t0 = t0;
+                it.len = s.len;
+                it.queries = s.queries;
+                it.blocks = blocks_of<TREE>(a, s, t0, t0 + 2 * tokens - 1);
+                for (int x = 0; x < 2; ++x) {
+                    it.tiles[x].span = span_of<TREE>(a, s, t0 + x * tokens, t0 + (x + 1) * tokens - 1);
+                    it.tiles[x].whole = whole_of<TREE>(it.blocks, it.tiles[x].span);
+                }
+                const int each = it.blocks.n / k.ctas, more = it.blocks.n - each * k.ctas;
+                it.k0 = rank * each + min(rank, more);
+                it.k1 = it.k0 + each + (rank < more ? 1 : 0);
+                ok = publish(it) && (n == 0 || waited(bar_q_free, (n - 1) & 1));
+                if (!ok) break;
+                if (lane == 0)
                     for (int x = 0; x < 2; ++x) {
                         mbar_expect_tx(bar_q + 8 * x, tokens * R * 128 * kSubs);
 #pragma unroll
                         for (int e = 0; e < kSubs; ++e)
                             tma_load_4d(base + S::kQ + x * S::kOperand + e * 16384, &map_q, bar_q + 8 * x, e * 64, h * R, t0 + x * tokens, b * k.q_b);
                     }
-                    ++n;
-                    for (int j = it.k0; ok && j < it.k1; ++j) {
-                        const int row = blocks.end(j) - kBlock;
-                        ok = fetch(&map_k, row, h * k.k_h, b * k.k_b) && fetch(&map_v, row, h * k.v_h, b * k.v_b);
-                    }
-                }
-                if (ok) {
-                    const Item end = {};
-                    ok = publish(end);
-                }
-                fetched = n;
-            }
-            __syncwarp();
-        } else if (warp == 9) {
-            // -------------------------------------------------------------- products
-            const unsigned long long lim = k.limit_of(kRoleMma);
-            const uint32_t idesc_s = umma_idesc_bf16(kTile, 0) | (a.sign ? 1u << 13 : 0u), idesc_o = umma_idesc_bf16(kTile, D) | 1u << 16;
-            uint32_t slot = 0, phase = 0, phase_p[2] = {0, 0}, phase_checked = 0, outputs[2] = {0, 0};
-            const auto waited = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, lim)); };
-            const auto next = [&]() {
-                if (++slot == (uint32_t)kSlots) {
-                    slot = 0;
-                    phase ^= 1;
-                }
-            };
-            Item it;
-            bool ok = true;
-            for (int n = 0; ok && item_at(n, lim, it); ++n) {
-                const Sample s = sample_in(it);
-                const Blocks blocks = blocks_of<TREE>(a, s, it.t0, it.t0 + 2 * tokens - 1);
-                Span spans[2];
-                spans_of(s, it.t0, spans);
-                ok = waited(bar_q, n & 1) && waited(bar_q + 8, n & 1);
-                bool begun[2] = {false, false};
-                Columns before[2] = {{0, 0, true}, {0, 0, true}};
-                for (int i = it.k0; ok && i <= it.k1; ++i) {
-                    // block i - 1's second product, block i's first
-                    const bool second = i > it.k0, first = i < it.k1;
-                    Columns now[2] = {{0, 0, true}, {0, 0, true}};
-                    if (first)
-                        for (int x = 0; x < 2; ++x) now[x] = columns_of(blocks, i, spans[x]);
-                    uint32_t v_slot = 0;
-                    if (second) {
-                        ok = waited(bar_full + 8 * slot, phase);
-                        if (ok && !(before[0].all && before[1].all)) {
-                            ok = waited(bar_checked + 8 * slot, phase_checked >> slot & 1);
-                            phase_checked ^= 1u << slot;
-                        }
+                ++fetched;
+                int masked = 0;
+                uint32_t v_slot = 0, v_phase = 0;
+                for (int j = it.k0; ok && j <= it.k1; ++j) {
+                    const uint32_t before = v_slot, before_phase = v_phase;
+                    if (j < it.k1) {
+                        const int row = it.blocks.end(j) - kBlock;
+                        ok = fetch(&map_k, row, h * k.k_h, b * k.k_b);
                         v_slot = slot;
-                        next();
+                        v_phase = phase;
+                        ok = ok && fetch(&map_v, row, h * k.v_h, b * k.v_b);
                     }
-                    if (ok && first) ok = waited(bar_full + 8 * slot, phase);
-                    if (!ok) break;
-                    tc_fence_after();
+                    // the block before, whose V is there by now or soon
+                    if (ok && j > it.k0 && !(it.tiles[0].columns(it.blocks, j - 1).all && it.tiles[1].columns(it.blocks, j - 1).all)) {
+                        ok = masked < kMasked && take_out(before, before_phase, bad + ((n & 1) * kMasked + masked) * 4);
+                        ++masked;
+                    }
+                }
+                ++n;
+            }
+            if (ok) {
+                Item end;
+                end.there = 0;
+                publish(end);
+            }
+        } else if (warp == kMmaWarp) {
+            // -------------------------------------------------------------- products
+            // (one lane all the way: what it spends between two products the tensor cores may spend waiting)
+            if (elected()) {
+                const unsigned long long lim = k.limit_of(kRoleMma);
+                const uint32_t idesc_s = umma_idesc_bf16(kTile, 0) | (a.sign ? 1u << 13 : 0u), idesc_o = umma_idesc_bf16(kTile, D) | 1u << 16;
+                uint32_t slot = 0, phase = 0, phase_p[2] = {0, 0}, phase_checked = 0, outputs[2] = {0, 0};
+                const auto waited = [&](uint32_t bar, uint32_t parity) { return mbar_wait(bar, parity, abort_flag, lim); };
+                // S(x) = Q(x) K^T over columns c; O(x) += P(x) V over tokens c
+                const auto first_product = [&](int x, uint32_t ring, const Columns& c) {
+                    const uint64_t dq = umma_desc_k128(base + S::kQ + x * S::kOperand), dk = umma_desc_k128(ring + c.lo * 128);
+                    const uint32_t d = tmem_s(x) + c.lo, idesc = idesc_s | (uint32_t)((c.hi - c.lo) >> 3) << 17;
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        if (second && before[x].lo != before[x].hi) {
-                            ok = waited(bar_p + 8 * x, phase_p[x]);
-                            phase_p[x] ^= 1;
-                            if (ok && !begun[x] && outputs[x] > 0) ok = waited(bar_o_free + 8 * x, (outputs[x] - 1) & 1);
+                    for (int e = 0; e < D / 16; ++e) tc_mma_bf16(d, dq + (uint64_t)((e / 4) * 1024 + (e % 4) * 2), dk + (uint64_t)((e / 4) * 1024 + (e % 4) * 2), idesc, e > 0 ? 1u : 0u);
+                    tc_commit(bar_s + 8 * x);
+                };
+                const auto second_product = [&](int x, uint32_t ring, int lo, int hi, bool begun) {
+                    const uint64_t dv = umma_desc_mn128(ring);
+                    if (hi - lo == kBlock / 2) {
+#pragma unroll
+                        for (int e = 0; e < kBlock / 32; ++e) tc_mma_bf16_ts(tmem_o(x), tmem_s(x) + lo / 2 + 8 * e, dv + (uint64_t)(lo * 8 + e * 128), idesc_o, begun || e > 0 ? 1u : 0u);
+                    } else {
+#pragma unroll 1
+                        for (int e = lo / 16; e < hi / 16; ++e, begun = true) tc_mma_bf16_ts(tmem_o(x), tmem_s(x) + 8 * e, dv + (uint64_t)(e * 128), idesc_o, begun ? 1u : 0u);
+                    }
+                };
+                bool ok = true;
+                for (int n = 0; ok; ++n) {
+                    ok = waited(bar_item + 8 * (n & 1), (n >> 1) & 1);
+                    const Item& it = items[n & 1];
+                    if (!ok || !it.there) break;
+                    const int k0 = it.k0, k1 = it.k1;
+                    const Whole whole[2] = {it.tiles[0].whole, it.tiles[1].whole};
+                    ok = waited(bar_q, n & 1) && waited(bar_q + 8, n & 1);
+                    bool begun[2] = {false, false};
+                    Columns before[2] = {{0, 0, true}, {0, 0, true}};
+#pragma unroll 1
+                    for (int i = k0; ok && i <= k1; ++i) {
+                        // block i - 1's second product, block i's first
+                        const bool second = i > k0, first = i < k1;
+                        uint32_t v_slot = slot;
+                        if (second) {
+                            ok = waited(bar_full + 8 * slot, phase);
+                            if (ok && !(before[0].all && before[1].all)) {
+                                ok = waited(bar_checked + 8 * slot, phase_checked >> slot & 1);
+                                phase_checked ^= 1u << slot;
+                            }
+                            if (++slot == (uint32_t)kSlots) {
+                                slot = 0;
+                                phase ^= 1;
+                            }
+                        }
+                        Columns now[2] = {{0, 0, true}, {0, 0, true}};
+                        if (first) {
+                            ok = ok && waited(bar_full + 8 * slot, phase);
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) {
+                                now[x].hi = kBlock;
+                                if (i < whole[x].first || i >= whole[x].end) now[x] = columns_of(it.blocks, i, it.tiles[x].span);
+                            }
+                        }
+                        const uint32_t v_ring = base + S::kRing + v_slot * S::kOperand, k_ring = base + S::kRing + slot * S::kOperand;
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const bool adds = second && before[x].lo != before[x].hi;
+                            if (ok && adds) {
+                                ok = waited(bar_p + 8 * x, phase_p[x]);
+                                if (ok && !begun[x] && outputs[x] > 0) ok = waited(bar_o_free + 8 * x, (outputs[x] - 1) & 1);
+                            }
                             if (!ok) break;
                             tc_fence_after();
-                            const uint64_t dv = umma_desc_mn128(base + S::kRing + v_slot * S::kOperand);
-                            for (int e = before[x].lo / 16; e < before[x].hi / 16; ++e) {
-                                mma_ts(tmem_o(x), tmem_s(x) + 8 * e, dv + (uint64_t)(e * 128), idesc_o, begun[x] ? 1u : 0u);
+                            if (adds) {
+                                second_product(x, v_ring, before[x].lo, min(before[x].hi, kBlock / 2), begun[x]);
+                                begun[x] |= before[x].lo < kBlock / 2;
+                                ok = waited(bar_p2 + 8 * x, phase_p[x]);
+                                if (!ok) break;
+                                phase_p[x] ^= 1;
+                                tc_fence_after();
+                                second_product(x, v_ring, max(before[x].lo, kBlock / 2), before[x].hi, begun[x]);
                                 begun[x] = true;
                             }
-                            if (!first) commit_one(bar_o + 8 * x);
+                            if (!first && begun[x]) tc_commit(bar_o + 8 * x);
+                            if (second && x == 1) tc_commit(bar_empty + 8 * v_slot);
+                            if (now[x].lo != now[x].hi) first_product(x, k_ring, now[x]);
+                            before[x] = now[x];
                         }
-                        if (second && x == 1) commit_one(bar_empty + 8 * v_slot);
-                        if (first && now[x].lo != now[x].hi) {
-                            const uint32_t idesc = idesc_s | (uint32_t)((now[x].hi - now[x].lo) >> 3) << 17;
-                            const uint32_t ring = base + S::kRing + slot * S::kOperand + now[x].lo * 128;
-#pragma unroll
-                            for (int e = 0; e < D / 16; ++e)
-                                mma_ss(tmem_s(x) + now[x].lo, umma_desc_k128(base + S::kQ + x * S::kOperand + (e / 4) * 16384) + (uint64_t)((e % 4) * 2),
-                                       umma_desc_k128(ring + (e / 4) * 16384) + (uint64_t)((e % 4) * 2), idesc, e > 0 ? 1u : 0u);
-                            commit_one(bar_s + 8 * x);
-                        }
-                    }
-                    if (!ok) break;
-                    if (first) {
-                        commit_one(bar_empty + 8 * slot);
-                        next();
-                    }
-                    if (i == it.k1 - 1 || it.k0 == it.k1) commit_one(bar_q_free);
-                    // an output whose last block was not the item's last
-                    if (!first)
-                        for (int x = 0; x < 2; ++x)
-                            if (begun[x] && before[x].lo == before[x].hi) commit_one(bar_o + 8 * x);
-                    before[0] = now[0];
-                    before[1] = now[1];
-                }
-                for (int x = 0; x < 2; ++x) outputs[x] += begun[x] ? 1 : 0;
-                __syncwarp();
-                if (ok && lane == 0) mbar_arrive(bar_done + 8 * (n & 1));
-            }
-            commit_one(bar_drain);                         // (waited for below)
-        } else {
-            // -------------------------------------------------------------- rows of V that are no numbers
-            const unsigned long long lim = k.limit_of(kRoleLoad);
-            const int u = tid - kSoftmaxThreads - 64;
-            uint32_t slot = 0, phase = 0;
-            Item it;
-            bool ok = true;
-            // (every operand of the ring is waited for in its turn: by parity alone a later round could not be told from an earlier one)
-            const auto arrived = [&]() { return __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * slot, phase, abort_flag, lim)); };
-            const auto leave = [&]() {
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar_empty + 8 * slot);
-                if (++slot == (uint32_t)kSlots) {
-                    slot = 0;
-                    phase ^= 1;
-                }
-            };
-            for (int n = 0; ok && item_at(n, lim, it); ++n) {
-                const Sample s = sample_in(it);
-                const Blocks blocks = blocks_of<TREE>(a, s, it.t0, it.t0 + 2 * tokens - 1);
-                Span spans[2];
-                spans_of(s, it.t0, spans);
-                uint32_t* const words = bad + (n & 1) * kMasked * 4;
-                int masked = 0;
-                volatile int& odd_here = any_bad[(n & 1) * 2 + warp - 10];
-                if (lane == 0) odd_here = 0;
-                for (int i = it.k0; i < it.k1; ++i) {
-                    ok = arrived();
-                    if (!ok) break;
-                    leave();
-                    ok = arrived();
-                    if (!ok) break;
-                    if (!(columns_of(blocks, i, spans[0]).all && columns_of(blocks, i, spans[1]).all)) {
-                        ok = masked < kMasked;
                         if (!ok) break;
-                        uint8_t* const v = smem + S::kRing + slot * S::kOperand;
-#pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            const int r = half * 64 + u;
-                            uint32_t any = 0;
-#pragma unroll
-                            for (int e = 0; e < kSubs * 8; ++e) {      // (pieces in another order in each lane: eight lie in all banks)
-                                const uint4 y = *reinterpret_cast<const uint4*>(v + (e / 8) * 16384 + r * 128 + ((e + lane) & 7) * 16);
-                                any |= ((y.x & 0x7F807F80u) + 0x00800080u) | ((y.y & 0x7F807F80u) + 0x00800080u) | ((y.z & 0x7F807F80u) + 0x00800080u) |
-                                       ((y.w & 0x7F807F80u) + 0x00800080u);
-                            }
-                            const bool odd = (any & 0x80008000u) != 0;
-                            if (odd)
-                                for (int e = 0; e < kSubs * 8; ++e) *reinterpret_cast<uint4*>(v + (e / 8) * 16384 + r * 128 + (e & 7) * 16) = make_uint4(0, 0, 0, 0);
-                            const uint32_t found = __ballot_sync(0xffffffffu, odd);
-                            if (lane == 0) {
-                                words[masked * 4 + half * 2 + u / 32] = found;
-                                if (found) odd_here = 1;
+                        if (first) {
+                            tc_commit(bar_empty + 8 * slot);
+                            if (++slot == (uint32_t)kSlots) {
+                                slot = 0;
+                                phase ^= 1;
                             }
                         }
-                        ++masked;
-                        fence_async_proxy();
-                        mbar_arrive(bar_checked + 8 * slot);
+                        if (i == k1 - 1 || k0 == k1) tc_commit(bar_q_free);
                     }
-                    leave();
+                    outputs[0] += begun[0] ? 1 : 0;
+                    outputs[1] += begun[1] ? 1 : 0;
+                    if (ok) mbar_arrive(bar_done + 8 * (n & 1));
                 }
-                __syncwarp();
-                if (ok && lane == 0) mbar_arrive(bar_done + 8 * (n & 1));
+                tc_commit(bar_drain);                      // (waited for below)
             }
+            __syncwarp();
         }
     }
     __syncthreads();
     // Another role may have given up behind the last product: operands and tensor memory stay until all of them have completed.
     // The same goes for copies in flight.
-    if (warp == 8 && lane == 0 && *abort_flag) {
+    if (warp == kLoadWarp && lane == 0 && *abort_flag) {
         for (uint32_t i = 0; i < (uint32_t)kSlots && i < issued; ++i) {
             const uint32_t at = issued - 1 - i;
             mbar_drain(bar_full + 8 * (at % kSlots), (at / kSlots) & 1);
@@ -664,7 +716,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 9) {
+    if (warp == kMmaWarp) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
@@ -674,10 +726,10 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     const int tile = (blockIdx.x / k.ctas) / (a.B * a.H), bh = (blockIdx.x / k.ctas) - tile * a.B * a.H, b = quotient(bh, k.heads), h = bh - b * a.H;
     const int t0 = (k.per_head - 1 - tile) * 2 * tokens;
     const Sample s = sample_of(a, b);
-    if (warp < 8 && t0 < s.queries) {
+    if (warp < kLoadWarp && t0 < s.queries) {
         constexpr int E = D / 32;
         const float* const ends = reinterpret_cast<const float*>(smem + S::kPartEnds);
-        for (int row = rank + k.ctas * warp; row < 2 * kTile; row += k.ctas * 8) {
+        for (int row = rank + k.ctas * warp; row < 2 * kTile; row += k.ctas * kLoadWarp) {
             const int x = row / kTile, rl = row - x * kTile, tl = quotient(rl, a.R), t = t0 + x * tokens + tl, hq = h * R + (rl - tl * R);
             if (tl >= tokens || t >= s.queries) continue;
             const bool there = lane < k.ctas;
@@ -685,7 +737,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             float top = kNoLogit, sum = 0.f;
             if (there) {
                 asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(top) : "r"(at) : "memory");
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(sum) : "r"(at + kSoftmaxThreads * 4) : "memory");
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(sum) : "r"(at + 2 * kTile * 4) : "memory");
             }
             const float mine = top;
 #pragma unroll
