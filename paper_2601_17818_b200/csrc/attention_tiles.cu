@@ -560,7 +560,13 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 const int each = it.blocks.n / k.ctas, more = it.blocks.n - each * k.ctas;
                 it.k0 = rank * each + min(rank, more);
                 it.k1 = it.k0 + each + (rank < more ? 1 : 0);
-                ok = publish(it) && (n == 0 || waited(bar_q_free, (n - 1) & 1));
+                ok = publish(it);
+                if (!ok) break;
+                if (it.k0 == it.k1) {                      // (no copies: nothing would wait for them before their places are used for something else)
+                    ++n;
+                    continue;
+                }
+                ok = fetched == 0 || waited(bar_q_free, (fetched - 1) & 1);
                 if (!ok) break;
                 if (lane == 0)
                     for (int x = 0; x < 2; ++x) {
@@ -600,7 +606,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             if (elected()) {
                 const unsigned long long lim = k.limit_of(kRoleMma);
                 const uint32_t idesc_s = umma_idesc_bf16(kTile, 0) | (a.sign ? 1u << 13 : 0u), idesc_o = umma_idesc_bf16(kTile, D) | 1u << 16;
-                uint32_t slot = 0, phase = 0, phase_p[2] = {0, 0}, phase_checked = 0, outputs[2] = {0, 0};
+                uint32_t slot = 0, phase = 0, phase_q = 0, phase_p[2] = {0, 0}, phase_checked = 0, outputs[2] = {0, 0};
                 const auto waited = [&](uint32_t bar, uint32_t parity) { return mbar_wait(bar, parity, abort_flag, lim); };
                 // S(x) = Q(x) K^T over columns c; O(x) += P(x) V over tokens c
                 const auto first_product = [&](int x, uint32_t ring, const Columns& c) {
@@ -627,7 +633,12 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     if (!ok || !it.there) break;
                     const int k0 = it.k0, k1 = it.k1;
                     const Whole whole[2] = {it.tiles[0].whole, it.tiles[1].whole};
-                    ok = waited(bar_q, n & 1) && waited(bar_q + 8, n & 1);
+                    if (k0 == k1) {
+                        mbar_arrive(bar_done + 8 * (n & 1));
+                        continue;
+                    }
+                    ok = waited(bar_q, phase_q) && waited(bar_q + 8, phase_q);
+                    phase_q ^= 1;
                     bool begun[2] = {false, false};
                     Columns before[2] = {{0, 0, true}, {0, 0, true}};
 #pragma unroll 1
@@ -688,7 +699,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                                 phase ^= 1;
                             }
                         }
-                        if (i == k1 - 1 || k0 == k1) tc_commit(bar_q_free);
+                        if (i == k1 - 1) tc_commit(bar_q_free);
                     }
                     outputs[0] += begun[0] ? 1 : 0;
                     outputs[1] += begun[1] ? 1 : 0;
