@@ -21,7 +21,7 @@
 namespace vitcop {
 namespace {
 
-constexpr int kWarps = 4, kBlock = 16, kStages = 3;
+constexpr int kWarps = 4, kBlock = 16, kStages = 3, kMostParts = 8;
 constexpr float kMayPass = 8.f;
 
 template <int D, int MT>
@@ -32,7 +32,7 @@ struct FewSmem {
     static constexpr int kPitch = D + 8;
     static constexpr int kQ = kWarps * kWarp;                          // [rows][D]
     static constexpr int kEnds = kQ + kRows * D * 2;                   // [kWarps + 1][3][rows]: maximum, sum, sum of rounded weights
-    static constexpr int kBytes = kEnds + (kWarps + 1) * 3 * kRows * 4;
+    static constexpr int kBytes = kEnds + ((kWarps + 1) * 3 + kMostParts) * kRows * 4;     // and [rows][parts]: what they count by
     static_assert(kRows * kPitch * 4 <= kWarp);
 };
 
@@ -54,39 +54,6 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
 __device__ __forceinline__ void fetch16(uint32_t dst, const void* src, bool there) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
-__device__ __forceinline__ float4 cluster_ld4(uint32_t addr) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ float2 cluster_ld2(uint32_t addr) {
-    float2 v;
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ float cluster_ld(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
-}
-
-// Parts of a row, each with maximum, sum and sum of rounded weights (of the lane, where it has one), brought to one maximum: returns what this
-// lane's part counts by.
-__device__ __forceinline__ float joined(float& top, float& sum, float& weight) {
-    const float mine = top;
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-    const float f = ex2_approx(mine - top);
-    sum *= f;
-    weight *= f;
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-        sum += __shfl_xor_sync(0xffffffffu, sum, off);
-        weight += __shfl_xor_sync(0xffffffffu, weight, off);
-    }
-    return f;
-}
-
 struct FewArgs {
     SeqArgs a;
     Divisor tiles, heads;                                  // tiles of rows of a head, heads of a sample
@@ -97,7 +64,7 @@ template <int D, int MT, bool TREE>
 __global__ void __launch_bounds__(kWarps * 32)
 attention_few_kernel(const __grid_constant__ FewArgs k) {
     using S = FewSmem<D, MT>;
-    constexpr int kRows = S::kRows, kPieces = D / 8, NT = D / 8, E = D / 32;
+    constexpr int kRows = S::kRows, kPieces = D / 8, NT = D / 8;
     const SeqArgs& a = k.a;
     extern __shared__ __align__(128) uint8_t smem[];
     const uint32_t base = smem_u32(smem);
@@ -303,79 +270,104 @@ attention_few_kernel(const __grid_constant__ FewArgs k) {
             *reinterpret_cast<float2*>(part + row * S::kPitch + n * 8 + (lane & 3) * 2) = make_float2(o[r / 2][n][(r & 1) * 2], o[r / 2][n][(r & 1) * 2 + 1]);
     }
     __syncthreads();
-    float* const all_ends = ends + kWarps * 3 * kRows;
+    // What each part of a row counts by, a thread a row; then the sums, a thread four elements.  At first of the warps' parts, which a CTA by itself writes out
+    // and others leave in the place of the first; then of the CTAs', rows in turn to each.
     const bool alone = k.ctas == 1;
-    // a warp a row, E elements a lane
-    const auto finish = [&](int row, const float (&v)[E], float t, float su, float we) {
-        const int i = row0 + row, tq = quotient(i, a.R), hq = h * R + (i - tq * R);
-        const bool none = su == 0.f;                       // (nothing seen)
-        const float inv = none ? 0.f : 1.f / we;
-        uint32_t* const to = reinterpret_cast<uint32_t*>(a.io.out + b * a.io.out_at[0] + hq * a.io.out_at[1] + tq * a.io.out_at[2] + lane * E);
-        if constexpr (E == 2) *to = bf16x2(v[0] * inv, v[1] * inv);
-        else
-#pragma unroll
-            for (int e = 0; e < E; e += 4) *reinterpret_cast<uint2*>(to + e / 2) = make_uint2(bf16x2(v[e] * inv, v[e + 1] * inv), bf16x2(v[e + 2] * inv, v[e + 3] * inv));
-        if (a.lse && lane == 0) a.lse[((int64_t)b * a.Hq + hq) * a.Tq + tq] = none ? MINUS_INF : (t + log2f(su)) * kLn2;
+    const auto query_of = [&](int row, int& tq, int& hq) {
+        const int i = row0 + row;
+        tq = quotient(i, a.R);
+        hq = h * R + (i - tq * R);
     };
-    for (int row = warp; row < rows; row += kWarps) {
-        const bool there = lane < kWarps;
-        float t = there ? ends[(lane * 3 + 0) * kRows + row] : kNoLogit, su = there ? ends[(lane * 3 + 1) * kRows + row] : 0.f,
-              we = there ? ends[(lane * 3 + 2) * kRows + row] : 0.f;
-        const float f = joined(t, su, we);
-        float v[E] = {};
+    const auto counted = [&](float (&tops)[kMostParts], const float (&sums)[kMostParts], const float (&weights)[kMostParts], float& t, float& su, float& we) {
+        t = kNoLogit;
+        su = we = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            const float fw = __shfl_sync(0xffffffffu, f, w);
-            const float* const from = reinterpret_cast<const float*>(smem + w * S::kWarp) + row * S::kPitch + lane * E;
+        for (int i = 0; i < kMostParts; ++i) t = fmaxf(t, tops[i]);
 #pragma unroll
-            for (int e = 0; e < E; e += 2) {
-                const float2 x = *reinterpret_cast<const float2*>(from + e);
-                v[e] = fmaf(x.x, fw, v[e]);
-                v[e + 1] = fmaf(x.y, fw, v[e + 1]);
-            }
+        for (int i = 0; i < kMostParts; ++i) {
+            tops[i] = ex2_approx(tops[i] - t);
+            su = fmaf(sums[i], tops[i], su);
+            we = fmaf(weights[i], tops[i], we);
         }
-        if (alone) {
-            finish(row, v, t, su, we);
-        } else {                                           // (in the place of the first warp's, whose elements this lane has read)
-            float* const to = reinterpret_cast<float*>(smem) + row * S::kPitch + lane * E;
+    };
+    const auto whole = [&](int row, float t, float su) {
+        int tq, hq;
+        query_of(row, tq, hq);
+        if (a.lse) a.lse[((int64_t)b * a.Hq + hq) * a.Tq + tq] = su == 0.f ? MINUS_INF : (t + log2f(su)) * kLn2;
+    };
+    const auto write = [&](int row, int e, const float4& v) {
+        int tq, hq;
+        query_of(row, tq, hq);
+        *reinterpret_cast<uint2*>(a.io.out + b * a.io.out_at[0] + hq * a.io.out_at[1] + tq * a.io.out_at[2] + e) = make_uint2(bf16x2(v.x, v.y), bf16x2(v.z, v.w));
+    };
+    const auto add = [](float4& v, const float4& x, float f) {
+        v.x = fmaf(x.x, f, v.x);
+        v.y = fmaf(x.y, f, v.y);
+        v.z = fmaf(x.z, f, v.z);
+        v.w = fmaf(x.w, f, v.w);
+    };
+    float* const all_ends = ends + kWarps * 3 * kRows;     // [3][rows] of the CTA
+    float* const counts = all_ends + 3 * kRows;            // [rows][parts]
+    if (tid < rows) {
+        float tops[kMostParts], sums[kMostParts], weights[kMostParts], t, su, we;
 #pragma unroll
-            for (int e = 0; e < E; e += 2) *reinterpret_cast<float2*>(to + e) = make_float2(v[e], v[e + 1]);
-            if (lane == 0) {
-                all_ends[row] = t;
-                all_ends[kRows + row] = su;
-                all_ends[2 * kRows + row] = we;
-            }
+        for (int w = 0; w < kMostParts; ++w) {
+            tops[w] = w < kWarps ? ends[(w * 3 + 0) * kRows + tid] : kNoLogit;
+            sums[w] = w < kWarps ? ends[(w * 3 + 1) * kRows + tid] : 0.f;
+            weights[w] = w < kWarps ? ends[(w * 3 + 2) * kRows + tid] : 0.f;
+        }
+        counted(tops, sums, weights, t, su, we);
+        const float inv = !alone ? 1.f : su == 0.f ? 0.f : 1.f / we;     // (0: nothing seen)
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) counts[tid * kWarps + w] = tops[w] * inv;
+        if (alone) {
+            whole(tid, t, su);
+        } else {
+            all_ends[tid] = t;
+            all_ends[kRows + tid] = su;
+            all_ends[2 * kRows + tid] = we;
         }
     }
-    if (alone) return;
-    // ---------------------------------------------------------------------- the cluster's parts: rows in turn to its CTAs
-    cluster_sync_all();
-    for (int row = rank + k.ctas * warp; row < rows; row += k.ctas * kWarps) {
-        const bool there = lane < k.ctas;
-        const uint32_t at = cluster_map(smem_u32(all_ends + row), there ? lane : 0);
-        float t = there ? cluster_ld(at) : kNoLogit, su = there ? cluster_ld(at + kRows * 4) : 0.f, we = there ? cluster_ld(at + kRows * 8) : 0.f;
-        const float f = joined(t, su, we);
-        float v[E] = {};
-        const uint32_t mine_at = base + (row * S::kPitch + lane * E) * 4;
-        for (int c = 0; c < k.ctas; ++c) {
-            const float fc = __shfl_sync(0xffffffffu, f, c);
-            const uint32_t from = cluster_map(mine_at, c);
-            if constexpr (E == 2) {
-                const float2 x = cluster_ld2(from);
-                v[0] = fmaf(x.x, fc, v[0]);
-                v[1] = fmaf(x.y, fc, v[1]);
-            } else {
+    __syncthreads();
+#pragma unroll 2
+    for (int i = tid; i < rows * (D / 4); i += kWarps * 32) {
+        const int row = i / (D / 4), e = i % (D / 4) * 4;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                for (int e = 0; e < E; e += 4) {
-                    const float4 x = cluster_ld4(from + 4 * e);
-                    v[e] = fmaf(x.x, fc, v[e]);
-                    v[e + 1] = fmaf(x.y, fc, v[e + 1]);
-                    v[e + 2] = fmaf(x.z, fc, v[e + 2]);
-                    v[e + 3] = fmaf(x.w, fc, v[e + 3]);
-                }
-            }
+        for (int w = 0; w < kWarps; ++w) add(v, *reinterpret_cast<const float4*>(smem + w * S::kWarp + (row * S::kPitch + e) * 4), counts[row * kWarps + w]);
+        if (alone) write(row, e, v);
+        else *reinterpret_cast<float4*>(smem + (row * S::kPitch + e) * 4) = v;     // (this thread has read what was there)
+    }
+    if (alone) return;
+    cluster_sync_all();
+    const int mine_rows = (rows - rank + k.ctas - 1) / k.ctas;
+    if (tid < mine_rows) {
+        const int row = rank + k.ctas * tid;
+        const uint32_t at = smem_u32(all_ends + row);
+        float tops[kMostParts], sums[kMostParts], weights[kMostParts], t, su, we;
+#pragma unroll
+        for (int c = 0; c < kMostParts; ++c) {
+            const uint32_t from = cluster_map(at, c < k.ctas ? c : rank);
+            tops[c] = c < k.ctas ? cluster_ld(from) : kNoLogit;
+            sums[c] = c < k.ctas ? cluster_ld(from + kRows * 4) : 0.f;
+            weights[c] = c < k.ctas ? cluster_ld(from + kRows * 8) : 0.f;
         }
-        finish(row, v, t, su, we);
+        counted(tops, sums, weights, t, su, we);
+        const float inv = su == 0.f ? 0.f : 1.f / we;
+#pragma unroll
+        for (int c = 0; c < kMostParts; ++c)
+            if (c < k.ctas) counts[tid * k.ctas + c] = tops[c] * inv;
+        whole(row, t, su);
+    }
+    __syncthreads();
+    for (int i = tid; i < mine_rows * (D / 4); i += kWarps * 32) {
+        const int j = i / (D / 4), e = i % (D / 4) * 4, row = rank + k.ctas * j;
+        const uint32_t at = base + (row * S::kPitch + e) * 4;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int c = 0; c < kMostParts; ++c)
+            if (c < k.ctas) add(v, cluster_ld4(cluster_map(at, c)), counts[j * k.ctas + c]);
+        write(row, e, v);
     }
     cluster_sync_all();                                    // (the others may still be reading what this CTA has)
 }
@@ -422,7 +414,7 @@ int launch_attention_few(const SeqArgs& a, int d, cudaStream_t stream) {
     if (!a.tree) span = std::min<int64_t>(span, (int64_t)a.n_sink + a.window + tile / (int)a.R.d + 1);
     const int64_t rounds = (span + kWarps * kBlock - 1) / (kWarps * kBlock);
     k.ctas = 1;
-    while (k.ctas < 8 && segs * k.ctas * 2 <= 2 * sm_count() && k.ctas * 2 <= rounds) k.ctas *= 2;
+    while (k.ctas < kMostParts && segs * k.ctas * 2 <= 2 * sm_count() && k.ctas * 2 <= rounds) k.ctas *= 2;
     switch (d) {
         case 64: return tile == 32 ? launch_few<64, 2>(k, segs, stream) : launch_few<64, 1>(k, segs, stream);
         case 128: return tile == 32 ? launch_few<128, 2>(k, segs, stream) : launch_few<128, 1>(k, segs, stream);

@@ -26,6 +26,18 @@ struct SeqArgs {
 };
 
 #ifdef __CUDACC__
+// Of the shared memory of a cluster's CTA.
+__device__ __forceinline__ float4 cluster_ld4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float cluster_ld(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+
 // Sample b: its rows of K and V, its queries, and the row in front of the first query's own.
 struct Sample {
     int len, queries, base;

@@ -32,7 +32,7 @@ static_assert(kSoftmaxThreads * kSoftmaxRegs + 128 * kOtherRegs == kThreads * 16
 constexpr int kMasked = 14;                                // blocks of an item that a tile sees in part: of either tile at most two at the end of its
                                                            // window, two where it begins, two where the sinks end; and the first
 constexpr float kMayPass = 8.f;
-constexpr int kItemBytes = 128;
+constexpr int kItemBytes = 128, kMostCtas = 8;
 enum { kRoleLoad = 1, kRoleMma = 2, kRoleSoftmax = 4 };
 
 template <int D>
@@ -48,10 +48,11 @@ struct TilesSmem {
     static constexpr int kBad = kItems + 2 * kItemBytes;        // [2][kMasked][4] words: rows of V that were taken out
     static constexpr int kBytes = kBad + 2 * kMasked * 16;
     static_assert(kBytes <= 232448);
-    // parts of a cluster, where the operands were: [256 rows][D + 4] and [3][256]
+    // parts of a cluster, where the operands were: [256 rows][D + 4], and their maxima and sums, [2][256]
     static constexpr int kPitch = D + 4;
     static constexpr int kPartEnds = 256 * kPitch * 4;
-    static_assert(kPartEnds + 2 * 256 * 4 <= kBars);
+    static constexpr int kPartCounts = kPartEnds + 2 * 256 * 4;        // [256]
+    static_assert(kPartCounts + 256 * 4 <= kBars);
 };
 
 struct TilesArgs {
@@ -91,6 +92,7 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
     *abort_flag = 1;
     return false;
 }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory"); }
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 // One lane of a warp, the same each time.
 __device__ __forceinline__ bool elected() {
@@ -282,6 +284,11 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (tid == kSoftmaxThreads) {
+        prefetch_map(&map_q);
+        prefetch_map(&map_k);
+        prefetch_map(&map_v);
+    }
     if (warp == kMmaWarp) tmem_alloc(smem_u32(tmem_slot), 512);
     tc_fence_before();
     __syncthreads();
@@ -372,14 +379,14 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 float h[4] = {MINUS_INF, MINUS_INF, MINUS_INF, MINUS_INF};
 #pragma unroll
                 for (int w = 0; w < 2; ++w) {
-                    weights(w);
+                    if (count > 0) weights(w);             // (there is no maximum before the first block)
 #pragma unroll
                     for (int v = 2 * w; v < 2 * w + 2; ++v)
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) h[e / 2 & 3] = fmaxf(h[e / 2 & 3], fmaxf(__uint_as_float(z[v][e]), __uint_as_float(z[v][e + 1])));
                 }
                 const float high = fmaxf(fmaxf(h[0], h[1]), fmaxf(h[2], h[3])) * a.scale_log2;
-                if (__any_sync(0xffffffffu, high - top > kMayPass)) {
+                if (count == 0 || __any_sync(0xffffffffu, high - top > kMayPass)) {
                     const float now = fmaxf(top, high), keep = ex2_approx(top - now);
                     top = now;
                     sum = mul2(sum, pack2(keep, keep));
@@ -737,44 +744,60 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     const int tile = (blockIdx.x / k.ctas) / (a.B * a.H), bh = (blockIdx.x / k.ctas) - tile * a.B * a.H, b = quotient(bh, k.heads), h = bh - b * a.H;
     const int t0 = (k.per_head - 1 - tile) * 2 * tokens;
     const Sample s = sample_of(a, b);
-    if (warp < kLoadWarp && t0 < s.queries) {
-        constexpr int E = D / 32;
+    if (t0 < s.queries) {
+        // what each part of a row counts by, a thread a row; then the sums, a thread four elements
+        const int mine = 2 * kTile / k.ctas;
         const float* const ends = reinterpret_cast<const float*>(smem + S::kPartEnds);
-        for (int row = rank + k.ctas * warp; row < 2 * kTile; row += k.ctas * kLoadWarp) {
-            const int x = row / kTile, rl = row - x * kTile, tl = quotient(rl, a.R), t = t0 + x * tokens + tl, hq = h * R + (rl - tl * R);
-            if (tl >= tokens || t >= s.queries) continue;
-            const bool there = lane < k.ctas;
-            const uint32_t at = cluster_map(smem_u32(ends + row), there ? lane : 0);
-            float top = kNoLogit, sum = 0.f;
-            if (there) {
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(top) : "r"(at) : "memory");
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(sum) : "r"(at + 2 * kTile * 4) : "memory");
+        float* const counts = reinterpret_cast<float*>(smem + S::kPartCounts);         // [rows][CTAs]
+        const auto query_of = [&](int row, int& t, int& hq) {
+            const int y = row / kTile, rl = row - y * kTile, tl = quotient(rl, a.R);
+            t = t0 + y * tokens + tl;
+            hq = h * R + (rl - tl * R);
+            return tl < tokens && t < s.queries;
+        };
+        if (tid < mine) {
+            const int row = rank + k.ctas * tid;
+            const uint32_t at = smem_u32(ends + row);
+            float tops[kMostCtas], sums[kMostCtas], top = kNoLogit, total = 0.f;
+#pragma unroll
+            for (int c = 0; c < kMostCtas; ++c) {
+                tops[c] = c < k.ctas ? cluster_ld(cluster_map(at, c)) : kNoLogit;
+                sums[c] = c < k.ctas ? cluster_ld(cluster_map(at, c) + 2 * kTile * 4) : 0.f;
             }
-            const float mine = top;
 #pragma unroll
-            for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-            const float f = ex2_approx(mine - top);
-            sum *= f;
+            for (int c = 0; c < kMostCtas; ++c) top = fmaxf(top, tops[c]);
 #pragma unroll
-            for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-            float v[E] = {};
-            for (int c = 0; c < k.ctas; ++c) {
-                const float fc = __shfl_sync(0xffffffffu, f, c);
-                const uint32_t from = cluster_map(base + (row * S::kPitch + lane * E) * 4, c);
-#pragma unroll
-                for (int e = 0; e < E; e += 2) {
-                    float v0, v1;
-                    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v0), "=f"(v1) : "r"(from + 4 * e) : "memory");
-                    v[e] = fmaf(v0, fc, v[e]);
-                    v[e + 1] = fmaf(v1, fc, v[e + 1]);
-                }
+            for (int c = 0; c < kMostCtas; ++c) {
+                tops[c] = ex2_approx(tops[c] - top);
+                total = fmaf(sums[c], tops[c], total);
             }
-            const bool none = sum == 0.f;
-            const float inv = none ? 0.f : 1.f / sum;
-            uint32_t* const out = reinterpret_cast<uint32_t*>(a.io.out + b * a.io.out_at[0] + hq * a.io.out_at[1] + t * a.io.out_at[2] + lane * E);
+            const bool none = total == 0.f;
+            const float inv = none ? 0.f : 1.f / total;
 #pragma unroll
-            for (int e = 0; e < E; e += 2) out[e / 2] = none ? 0u : bf16x2(v[e] * inv, v[e + 1] * inv);
-            if (a.lse && lane == 0) a.lse[((int64_t)b * a.Hq + hq) * a.Tq + t] = none ? MINUS_INF : (top + log2f(sum)) * kLn2;
+            for (int c = 0; c < kMostCtas; ++c)
+                if (c < k.ctas) counts[tid * k.ctas + c] = tops[c] * inv;
+            int t, hq;
+            if (query_of(row, t, hq) && a.lse) a.lse[((int64_t)b * a.Hq + hq) * a.Tq + t] = none ? MINUS_INF : (top + log2f(total)) * kLn2;
+        }
+        __syncthreads();
+#pragma unroll 2
+        for (int i = tid; i < mine * (D / 4); i += kThreads) {
+            const int j = i / (D / 4), e = i % (D / 4) * 4, row = rank + k.ctas * j;
+            int t, hq;
+            if (!query_of(row, t, hq)) continue;
+            const uint32_t at = base + (row * S::kPitch + e) * 4;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int c = 0; c < kMostCtas; ++c) {
+                if (c >= k.ctas) break;
+                const float4 y = cluster_ld4(cluster_map(at, c));
+                const float f = counts[j * k.ctas + c];
+                v.x = fmaf(y.x, f, v.x);
+                v.y = fmaf(y.y, f, v.y);
+                v.z = fmaf(y.z, f, v.z);
+                v.w = fmaf(y.w, f, v.w);
+            }
+            *reinterpret_cast<uint2*>(a.io.out + b * a.io.out_at[0] + hq * a.io.out_at[1] + t * a.io.out_at[2] + e) = make_uint2(bf16x2(v.x, v.y), bf16x2(v.z, v.w));
         }
     }
     cluster_sync_all();                                    // (the others may still be reading what this CTA has)
@@ -858,7 +881,7 @@ int launch_attention_tiles(const SeqArgs& a, int d, cudaStream_t stream) {
     const int64_t blocks = (span + kBlock - 1) / kBlock;
     const int sms = std::min(sm_count(), kMaxReports);
     k.ctas = 1;
-    while (k.ctas < 8 && items * k.ctas * 2 <= sms && k.ctas * 2 <= blocks) k.ctas *= 2;
+    while (k.ctas < kMostCtas && items * k.ctas * 2 <= sms && k.ctas * 2 <= blocks) k.ctas *= 2;
     const int grid = (int)(k.ctas > 1 ? items * k.ctas : std::min<int64_t>(items, sms));
     if (d == 64) return a.tree ? launch_tiles<64, true>(mq, mk, mv, k, grid, stream) : launch_tiles<64, false>(mq, mk, mv, k, grid, stream);
     return a.tree ? launch_tiles<128, true>(mq, mk, mv, k, grid, stream) : launch_tiles<128, false>(mq, mk, mv, k, grid, stream);
