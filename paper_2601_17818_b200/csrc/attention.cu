@@ -89,17 +89,24 @@ attention_few_kernel(const __grid_constant__ FewArgs k) {
     const auto begin_of = [&](int i) { return i < blocks_a ? i * kBlock : span.b0 + (i - blocks_a) * kBlock; };
     const auto end_of = [&](int i) { return i < blocks_a ? min(span.a, (i + 1) * kBlock) : min(span.b1, span.b0 + (i - blocks_a + 1) * kBlock); };
     const uint32_t mine = base + warp * S::kWarp;
+    // (a lane has 16 bytes of every kStep-th row of a block)
+    constexpr int kStep = 32 / (kPieces < 32 ? kPieces : 32), kRowsALane = kBlock / kStep;
+    const int my_row = lane / kPieces, my_piece = lane % kPieces;
+    const __nv_bfloat16* const Kl = Kh + my_row * a.io.k_at[2] + my_piece * 8;
+    const __nv_bfloat16* const Vl = Vh + my_row * a.io.v_at[2] + my_piece * 8;
+    const int64_t k_step = kStep * a.io.k_at[2], v_step = kStep * a.io.v_at[2];
     const auto fetch = [&](int i, int stage) {
         if (i < last) {
-            const int j0 = begin_of(i), j1 = end_of(i);
+            const int j0 = begin_of(i), there = end_of(i) - j0;
             const uint32_t to = mine + stage * 2 * S::kHalf;
+            const __nv_bfloat16 *pk = Kl + j0 * a.io.k_at[2], *pv = Vl + j0 * a.io.v_at[2];
 #pragma unroll
-            for (int n = 0; n < kBlock * kPieces / 32; ++n) {
-                const int r = (n * 32 + lane) / kPieces, c = lane % kPieces, j = j0 + r;
-                const bool there = j < j1;
-                const int64_t row = there ? j : j0;
-                fetch16(to + piece_at<D>(r, c), Kh + row * a.io.k_at[2] + c * 8, there);
-                fetch16(to + S::kHalf + piece_at<D>(r, c), Vh + row * a.io.v_at[2] + c * 8, there);
+            for (int n = 0; n < kRowsALane; ++n) {         // (nothing is read of rows behind the last)
+                const int r = n * kStep + my_row;
+                fetch16(to + piece_at<D>(r, my_piece), pk, r < there);
+                fetch16(to + S::kHalf + piece_at<D>(r, my_piece), pv, r < there);
+                pk += k_step;
+                pv += v_step;
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -108,15 +115,16 @@ attention_few_kernel(const __grid_constant__ FewArgs k) {
     for (int st = 0; st < kStages - 1; ++st) fetch(first + warp + st * kWarps, st);
 
     // queries to shared memory
-    for (int i = tid; i < kRows * kPieces; i += kWarps * 32) {
-        const int r = i / kPieces, c = i - r * kPieces;
-        uint4 x = make_uint4(0, 0, 0, 0);
+    constexpr int kQueryPieces = kRows * kPieces / (kWarps * 32);
+    uint4 query[kQueryPieces];
+#pragma unroll
+    for (int n = 0; n < kQueryPieces; ++n) {
+        const int i = n * kWarps * 32 + tid, r = i / kPieces, c = i % kPieces;
+        query[n] = make_uint4(0, 0, 0, 0);
         if (r < rows) {
             const int t = quotient(row0 + r, a.R), hq = h * R + (row0 + r - t * R);
-            x = __ldcg(reinterpret_cast<const uint4*>(a.io.q + b * a.io.q_at[0] + hq * a.io.q_at[1] + t * a.io.q_at[2] + c * 8));
-            x = make_uint4(x.x ^ a.sign, x.y ^ a.sign, x.z ^ a.sign, x.w ^ a.sign);
+            query[n] = __ldcg(reinterpret_cast<const uint4*>(a.io.q + b * a.io.q_at[0] + hq * a.io.q_at[1] + t * a.io.q_at[2] + c * 8));
         }
-        *reinterpret_cast<uint4*>(smem + S::kQ + piece_at<D>(r, c)) = x;
     }
     // what the four rows of this thread see (a row behind the last sees nothing)
     const auto row_seen = [&](int r) { return Seen<TREE>(a, s, b, r < rows ? quotient(row0 + r, a.R) : s.queries); };
@@ -124,6 +132,12 @@ attention_few_kernel(const __grid_constant__ FewArgs k) {
     if constexpr (MT == 2) {
         seen[2] = row_seen(lane / 4 + 16);
         seen[3] = row_seen(lane / 4 + 24);
+    }
+#pragma unroll
+    for (int n = 0; n < kQueryPieces; ++n) {
+        const int i = n * kWarps * 32 + tid;
+        const uint4 x = query[n];
+        *reinterpret_cast<uint4*>(smem + S::kQ + piece_at<D>(i / kPieces, i % kPieces)) = make_uint4(x.x ^ a.sign, x.y ^ a.sign, x.z ^ a.sign, x.w ^ a.sign);
     }
     __syncthreads();
     uint32_t q[MT][D / 16][4];
@@ -414,7 +428,8 @@ int launch_attention_few(const SeqArgs& a, int d, cudaStream_t stream) {
     if (!a.tree) span = std::min<int64_t>(span, (int64_t)a.n_sink + a.window + tile / (int)a.R.d + 1);
     const int64_t rounds = (span + kWarps * kBlock - 1) / (kWarps * kBlock);
     k.ctas = 1;
-    while (k.ctas < kMostParts && segs * k.ctas * 2 <= 2 * sm_count() && k.ctas * 2 <= rounds) k.ctas *= 2;
+    // (joining CTAs costs as much as a round of their blocks, of many rows two)
+    while (k.ctas < kMostParts && segs * k.ctas * 2 <= 2 * sm_count() && k.ctas * 2 * (tile / 16) <= rounds) k.ctas *= 2;
     switch (d) {
         case 64: return tile == 32 ? launch_few<64, 2>(k, segs, stream) : launch_few<64, 1>(k, segs, stream);
         case 128: return tile == 32 ? launch_few<128, 2>(k, segs, stream) : launch_few<128, 1>(k, segs, stream);
