@@ -7,6 +7,10 @@
 
 namespace vitcop {
 
+// Weights are 2^(logit - top), top this much above the largest logit there was when it was set (in powers of two): it stays until a logit passes it, which few
+// do, and no weight is above 1, so that sums with values near the end of fp32's range hold.
+constexpr float kHeadroom = 24.f;
+
 // Queries, keys, values, output: bf16, strides of samples, heads, tokens in elements.
 struct SeqRows {
     const __nv_bfloat16 *q, *K, *V;

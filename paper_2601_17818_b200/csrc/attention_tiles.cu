@@ -5,8 +5,8 @@
 // what a first block reaches back beyond its segment, or the sequence, is masked.  Of a block that a tile sees in part only the 32-token
 // columns that it sees are worked on.
 //   warps 0-3, 4-7  softmax of a tile, a thread a row: logits from tensor memory, weights back to where the logits were, as the operand of
-//                   the second product.  Weights are made with the row's maximum so far while the block's own is looked for; only when a logit
-//                   has passed it by 2^8 is it moved, the sums so far with it, and the weights are made anew
+//                   the second product.  Weights are made by the maximum so far while the block's own is looked for; only when a logit has passed
+//                   it by 2^24 is it moved, the sums so far with it, and the weights are made anew
 //   warp 8          tensor copies: queries, then K and V of a block in turn through a ring.  Rows of V that are no numbers must not reach rows that do
 //                   not see them, and 0 times NaN does: blocks that are masked are looked through, such rows taken out and added again at the end
 //                   for those who see them
@@ -31,7 +31,6 @@ constexpr int kThreads = kSoftmaxThreads + 128, kSoftmaxRegs = 208, kOtherRegs =
 static_assert(kSoftmaxThreads * kSoftmaxRegs + 128 * kOtherRegs == kThreads * 168, "registers that are asked for and not there are waited for, for ever");
 constexpr int kMasked = 14;                                // blocks of an item that a tile sees in part: of either tile at most two at the end of its
                                                            // window, two where it begins, two where the sinks end; and the first
-constexpr float kMayPass = 8.f;
 constexpr int kItemBytes = 128, kMostCtas = 8;
 enum { kRoleLoad = 1, kRoleMma = 2, kRoleSoftmax = 4 };
 
@@ -136,6 +135,15 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
         "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, "
+        "%20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+        "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&o)[16]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
@@ -212,8 +220,12 @@ struct Item {
 };
 static_assert(sizeof(Item) == kItemBytes);
 
-// Bits below x of a word.
-__device__ __forceinline__ uint32_t below(int x) { return x <= 0 ? 0u : x >= 32 ? 0xffffffffu : (1u << x) - 1u; }
+// Bits below x of a word (a shift by 32 and more leaves none).
+__device__ __forceinline__ uint32_t below(int x) {
+    uint32_t from;
+    asm("shl.b32 %0, %1, %2;" : "=r"(from) : "r"(0xffffffffu), "r"(max(x, 0)));
+    return ~from;
+}
 __device__ __forceinline__ uint32_t bits_of(const Seen<false>& s, int j0) { return below(s.front - j0) | (below(s.p + 1 - j0) & ~below(s.lo - j0)); }
 __device__ __forceinline__ uint32_t bits_of(const Seen<true>& s, int j0) {
     const int i = j0 - s.base;                             // drafted token of bit 0
@@ -333,7 +345,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 const int t = it.t0 + x * tokens + tl;
                 return Seen<TREE>(a, sample_in(it), it.b, tl < tokens && t < it.queries ? t : it.queries);
             };
-            float top = kNoLogit;                          // in powers of two; weights are 2^(logit - top)
+            float top = kNoLogit;                          // in powers of two: weights are 2^(logit - top), 1 at most
             f32x2 sum = pack2(0.f, 0.f);
             int count = 0;
             const Whole whole = it.tiles[x].whole;
@@ -346,22 +358,35 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 if (!ok) break;
                 phase_s ^= 1;
                 tc_fence_after();
+                // Logits of rows that are not seen become -inf where they lie, 32 columns at a time and only those in which some row of the warp has
+                // one: a loop, for what is unrolled over a row's registers and seldom run is fetched anew each time.
+                if (!c.all || c.hi - c.lo < kBlock) {
+                    const Seen<TREE> seen = seen_by_row();
+                    const int start = it.blocks.end(i) - kBlock, segment = it.blocks.begin_of_segment(i);
+                    uint32_t keep[4];
+#pragma unroll
+                    for (int w = 0; w < 4; ++w)            // (columns that were not worked on are anything)
+                        keep[w] = w * 32 >= c.lo && w * 32 < c.hi ? bits_of(seen, start + w * 32) & ~below(segment - start - w * 32) : 0u;
+#pragma unroll 1
+                    for (int w = 0; w < 4; ++w) {
+                        const uint32_t mine = w == 0 ? keep[0] : w == 1 ? keep[1] : w == 2 ? keep[2] : keep[3];
+                        if (__all_sync(0xffffffffu, mine == 0xffffffffu)) continue;
+                        uint32_t y[32];
+                        tmem_ld32_issue(s_at + w * 32, y);
+                        tmem_ld_wait();
+                        pin32(y);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) y[e] = mine >> e & 1 ? y[e] : 0xff800000u;
+                        tmem_st32(s_at + w * 32, y);
+                    }
+                    tmem_st_wait();
+                }
                 uint32_t z[4][32];
 #pragma unroll
-                for (int w = 0; w < 4; ++w) tmem_ld32_issue(s_at + w * 32, z[w]);      // (columns that were not worked on are anything)
+                for (int w = 0; w < 4; ++w) tmem_ld32_issue(s_at + w * 32, z[w]);
                 tmem_ld_wait();
 #pragma unroll
                 for (int w = 0; w < 4; ++w) pin32(z[w]);
-                if (!c.all || c.hi - c.lo < kBlock) {
-                    const Seen<TREE> seen = seen_by_row();
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const int j0 = it.blocks.end(i) - kBlock + w * 32;
-                        const uint32_t keep = w * 32 >= c.lo && w * 32 < c.hi ? bits_of(seen, j0) & ~below(it.blocks.begin_of_segment(i) - j0) : 0u;
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) z[w][e] = keep >> e & 1 ? z[w][e] : 0xff800000u;
-                    }
-                }
                 f32x2 more = pack2(0.f, 0.f), more2 = more;
                 const auto weights = [&](int w) {          // of 32 columns
                     const f32x2 top2 = pack2(-top, -top);
@@ -386,8 +411,8 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                         for (int e = 0; e < 32; e += 2) h[e / 2 & 3] = fmaxf(h[e / 2 & 3], fmaxf(__uint_as_float(z[v][e]), __uint_as_float(z[v][e + 1])));
                 }
                 const float high = fmaxf(fmaxf(h[0], h[1]), fmaxf(h[2], h[3])) * a.scale_log2;
-                if (count == 0 || __any_sync(0xffffffffu, high - top > kMayPass)) {
-                    const float now = fmaxf(top, high), keep = ex2_approx(top - now);
+                if (count == 0 || __any_sync(0xffffffffu, high > top)) {
+                    const float now = high > top ? high + kHeadroom : top, keep = ex2_approx(top - now);
                     top = now;
                     sum = mul2(sum, pack2(keep, keep));
                     if (count > 0) {                       // (the products so far have ended: the logits' came behind them)
