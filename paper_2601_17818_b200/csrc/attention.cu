@@ -413,22 +413,51 @@ int launch_few(const FewArgs& k, int64_t segs, cudaStream_t stream) {
     return k.a.tree ? launch_few<D, MT, true>(k, segs, stream) : launch_few<D, MT, false>(k, segs, stream);
 }
 
-int launch_attention_few(const SeqArgs& a, int d, cudaStream_t stream) {
+// How a call is shared out, and about how many us that takes: a CTA begins and ends (with a cluster's join), and in between fetches and works on four
+// blocks of 16 tokens at a time.  Two CTAs fit an SM (one of 256-wide heads); clusters of eight are not all there at once beyond 128 CTAs.
+// Measured (in a graph; estimate in brackets), clusters of 1 / 2 / 4 / 8: 64 rows of 32 heads of 128, 355 tokens 13.1 / 10.9 / 10.8 / 18.4 us (12.6 / 10.6
+// / 11.4 / 24), 4195 tokens 78.6 / 44.1 / 31.1 / 41.1 (78 / 43 / 31 / 44); 7 rows of 64 heads, 4160 tokens 52.6 / 30.4 / 24.9 / 29.6 (52 / 28 / 21 / 29);
+// 256 rows of 32 heads of 64, 592 tokens 10.8 / 17.6 / 27.7 / 51.0 (11 / 16 / 26 / 60).
+struct FewPlan {
+    int tile, ctas;
+    int64_t tiles, segs;
+    double us;
+};
+FewPlan few_plan(const SeqArgs& a, int d) {
+    FewPlan p;
     const int64_t rows = (int64_t)a.R.d * a.Tq;
-    const int tile = rows > 16 && d != 256 ? 32 : 16;
+    p.tile = rows > 16 && d != 256 ? 32 : 16;
+    p.tiles = (rows + p.tile - 1) / p.tile;
+    p.segs = p.tiles * a.B * a.H;
+    // tokens that a tile's rows may see
+    int64_t span = a.N;
+    if (!a.tree) span = std::min<int64_t>(span, (int64_t)a.n_sink + a.window + p.tile / (int)a.R.d + 1);
+    const double rounds = (double)span / (kWarps * kBlock), begin = d == 64 ? 4.0 : p.tile == 32 ? 6.5 : 3.5;
+    const double round = d == 64 ? 0.62 : d == 128 && p.tile == 16 ? 0.75 : d == 128 ? 1.1 : 1.5;
+    const double sms = sm_count();
+    p.us = 1e30;
+    p.ctas = 1;
+    for (int c = 1; c <= kMostParts; c *= 2) {
+        const double n = (double)p.segs * c, slots = c == 8 ? 128 : d == 256 ? sms : 2 * sms;
+        const double join = c == 1 ? 0.0 : c == 2 ? 1.0 : c == 4 ? 3.0 : 8.0;
+        const double us = std::ceil(n / slots) * (begin + round * (n > sms ? 1.2 : 1.0) * rounds / c) + join * (p.tile == 32 ? 1.0 : 0.25);
+        if (us < p.us) {
+            p.us = us;
+            p.ctas = c;
+        }
+    }
+    return p;
+}
+
+int launch_attention_few(const SeqArgs& a, int d, const FewPlan& p, cudaStream_t stream) {
     FewArgs k;
     k.a = a;
-    const int64_t tiles = (rows + tile - 1) / tile, segs = tiles * a.B * a.H;
-    if (segs * 8 > 0x7fffffff) return VITCOP_ERR_UNSUPPORTED;
-    k.tiles = divisor((int)tiles);
+    k.ctas = p.ctas;
+    const int tile = p.tile;
+    const int64_t segs = p.segs;
+    if (segs * kMostParts > 0x7fffffff) return VITCOP_ERR_UNSUPPORTED;
+    k.tiles = divisor((int)p.tiles);
     k.heads = divisor(a.H);
-    // tokens that a tile's rows may see, four blocks of which are a CTA's at a time
-    int64_t span = a.N;
-    if (!a.tree) span = std::min<int64_t>(span, (int64_t)a.n_sink + a.window + tile / (int)a.R.d + 1);
-    const int64_t rounds = (span + kWarps * kBlock - 1) / (kWarps * kBlock);
-    k.ctas = 1;
-    // (joining CTAs costs as much as a round of their blocks, of many rows two)
-    while (k.ctas < kMostParts && segs * k.ctas * 2 <= 2 * sm_count() && k.ctas * 2 * (tile / 16) <= rounds) k.ctas *= 2;
     switch (d) {
         case 64: return tile == 32 ? launch_few<64, 2>(k, segs, stream) : launch_few<64, 1>(k, segs, stream);
         case 128: return tile == 32 ? launch_few<128, 2>(k, segs, stream) : launch_few<128, 1>(k, segs, stream);
@@ -459,11 +488,12 @@ int launch_attention(const SeqRows& io, int B, int Hq, int H, int Tq, int d, int
     a.R = divisor(Hq / H);
     a.scale_log2 = std::fmax(std::fabs(scale) * kLog2e, 0x1p-149f);    // (0 times the -inf of a hidden row would be no number)
     a.sign = std::signbit(scale) ? 0x80008000u : 0u;
-    if (tiles_kernel_takes(a, d)) {
+    const FewPlan few = few_plan(a, d);
+    if (tiles_kernel_us(a, d) < few.us) {
         const int rc = launch_attention_tiles(a, d, stream);
         if (rc != VITCOP_ERR_UNSUPPORTED) return rc;
     }
-    return launch_attention_few(a, d, stream);
+    return launch_attention_few(a, d, few, stream);
 }
 
 }  // namespace vitcop

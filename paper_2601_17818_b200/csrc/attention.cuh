@@ -125,7 +125,7 @@ __device__ __forceinline__ Span span_of(const SeqArgs& a, const Sample& s, int t
 int launch_attention(const SeqRows& io, int B, int Hq, int H, int Tq, int d, int N, const int32_t* cache_len, const int32_t* query_len,
                      const int64_t* tree, int window, int n_sink, float scale, float* lse, void* workspace, cudaStream_t stream);
 // The kernel for many query rows (tcgen05).
-bool tiles_kernel_takes(const SeqArgs& a, int d);
+double tiles_kernel_us(const SeqArgs& a, int d);           // about how long it takes; without end for what it does not do
 int launch_attention_tiles(const SeqArgs& a, int d, cudaStream_t stream);
 size_t attention_workspace_bytes(int B, int H, int N, int d, int Tq, int Hq);
 

@@ -16,6 +16,7 @@
 #include "attention.cuh"
 
 #include <algorithm>
+#include <cmath>
 
 #include "gram.cuh"
 #include "tcgen05.cuh"
@@ -867,11 +868,34 @@ int launch_tiles(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap
 
 }  // namespace
 
-// Where a call has a kernel of this kind.  Everything it refuses goes to the other kernel.
-bool tiles_kernel_takes(const SeqArgs& a, int d) {
-    const int64_t rows = (int64_t)a.R.d * a.Tq;
-    return d != 256 && a.R.d <= 64 && rows > 32 && a.N > 0;
+// How a call is shared out, and about how many us that takes: items have a beginning and an end of 5 (a kernel's first 11), a block of two tiles 1.9 and of one
+// 1.6; a cluster's join 3.  Measured (estimate in brackets), in clusters of four and by the other kernel at its best: 64 rows of 32 heads of 128, 355 tokens
+// 13.5 and 10.8 us (16), 1059 tokens 19.0 and 15.0 (18), 4195 tokens 29.4 and 31.1 (28); 256 rows, 1315 tokens 22.1 and 31.4 (20).  Items in turn: 512 of
+// 256 rows, 547 tokens 70.7 and 197 (58).
+struct TilesPlan {
+    int tokens, per_head, ctas;
+    int64_t items;
+    double us;
+};
+static TilesPlan tiles_plan(const SeqArgs& a, int d) {
+    TilesPlan p = {0, 0, 1, 0, 1e30};
+    const int R = (int)a.R.d;
+    if (d == 256 || R > kTile / 2 || a.N == 0) return p;
+    p.tokens = kTile / R;
+    p.per_head = (a.Tq + 2 * p.tokens - 1) / (2 * p.tokens);
+    p.items = (int64_t)a.B * a.H * p.per_head;
+    if (p.items > 0x7fffffff / kMostCtas) return p;
+    // tokens that an item's rows may see
+    int64_t span = a.N;
+    if (!a.tree) span = std::min<int64_t>(span, (int64_t)a.n_sink + a.window + std::min(a.Tq, 2 * p.tokens));
+    const int64_t blocks = (span + kBlock - 1) / kBlock;
+    const int sms = std::min(sm_count(), kMaxReports);
+    while (p.ctas < kMostCtas && p.items * p.ctas * 2 <= sms && p.ctas * 2 <= blocks) p.ctas *= 2;
+    const double block = a.Tq > p.tokens ? 1.9 : 1.6;
+    p.us = p.items <= sms ? 11 + block * blocks / p.ctas + (p.ctas > 1 ? 3 : 0) : 6 + std::ceil((double)p.items / sms) * (5 + block * blocks);
+    return p;
 }
+double tiles_kernel_us(const SeqArgs& a, int d) { return tiles_plan(a, d).us; }
 
 // ERR_UNSUPPORTED where rows lie so that tensor copies cannot fetch them.
 int launch_attention_tiles(const SeqArgs& a, int d, cudaStream_t stream) {
@@ -879,11 +903,11 @@ int launch_attention_tiles(const SeqArgs& a, int d, cudaStream_t stream) {
     k.a = a;
     const SeqRows& io = a.io;
     const int R = (int)a.R.d;
-    k.tokens = kTile / R;
-    k.per_head = (a.Tq + 2 * k.tokens - 1) / (2 * k.tokens);
-    const int64_t items = (int64_t)a.B * a.H * k.per_head;
-    if (items > 0x7fffffff / 8) return VITCOP_ERR_UNSUPPORTED;
-    k.items = (int)items;
+    const TilesPlan plan = tiles_plan(a, d);
+    k.tokens = plan.tokens;
+    k.per_head = plan.per_head;
+    k.items = (int)plan.items;
+    k.ctas = plan.ctas;
     k.heads = divisor(a.H);
     const auto step = [](int n, int64_t stride) { return n > 1 && stride == 0 ? 0 : 1; };
     k.q_b = step(a.B, io.q_at[0]);
@@ -900,14 +924,7 @@ int launch_attention_tiles(const SeqArgs& a, int d, cudaStream_t stream) {
     k.wide = reinterpret_cast<uintptr_t>(io.out) % 32 == 0 && io.out_at[0] % 16 == 0 && io.out_at[1] % 16 == 0 && io.out_at[2] % 16 == 0;
     k.wait_ns = gram_wait_limit_ns();
     k.expire_roles = pair_expire_roles();
-    // blocks that an item may have
-    int64_t span = a.N;
-    if (!a.tree) span = std::min<int64_t>(span, (int64_t)a.n_sink + a.window + 2 * k.tokens);
-    const int64_t blocks = (span + kBlock - 1) / kBlock;
-    const int sms = std::min(sm_count(), kMaxReports);
-    k.ctas = 1;
-    while (k.ctas < kMostCtas && items * k.ctas * 2 <= sms && k.ctas * 2 <= blocks) k.ctas *= 2;
-    const int grid = (int)(k.ctas > 1 ? items * k.ctas : std::min<int64_t>(items, sms));
+    const int sms = std::min(sm_count(), kMaxReports), grid = (int)(k.ctas > 1 ? plan.items * k.ctas : std::min<int64_t>(plan.items, sms));
     if (d == 64) return a.tree ? launch_tiles<64, true>(mq, mk, mv, k, grid, stream) : launch_tiles<64, false>(mq, mk, mv, k, grid, stream);
     return a.tree ? launch_tiles<128, true>(mq, mk, mv, k, grid, stream) : launch_tiles<128, false>(mq, mk, mv, k, grid, stream);
 }

@@ -398,8 +398,8 @@ def test_long_caches_and_large_trees(B, H, R, Tq, N, d):
 
 
 @pytest.mark.parametrize("roles", [1, 2, 4])
-@pytest.mark.parametrize("B,N,Tq", [(1, 3000, 300), (16, 900, 900)])
-def test_a_wait_that_ran_out_is_reported(roles, B, N, Tq):
+@pytest.mark.parametrize("B,N,Tq,window", [(1, 3000, 300, 2500), (16, 900, 900, 500)])
+def test_a_wait_that_ran_out_is_reported(roles, B, N, Tq, window):
     """One role of every CTA gives up at once, with copies and products of the others in flight (CTAs of a cluster on one item; CTAs with items in
     turn); the next call is right again."""
     H, R, d = 2, 4, 128
@@ -407,14 +407,14 @@ def test_a_wait_that_ran_out_is_reported(roles, B, N, Tq):
     ws, out = vb.alloc_workspace(vb.OP_ATTENTION, B=B, H=H, N=N, d=d, Nv=Tq, D=H * R), torch.zeros_like(q)
     try:
         vb.vitcop_set_wait_limit(0, roles)
-        vb.vitcop_window_attention(q, K, V, None, out, ws, d ** -0.5, 500, 4)
+        vb.vitcop_window_attention(q, K, V, None, out, ws, d ** -0.5, window, 4)
         assert vb.vitcop_poll_status(ws) == vb.ERR_TIMEOUT
     finally:
         vb.vitcop_set_wait_limit(0, 0)
-    out, lse = _run(q, K, V, None, d ** -0.5, 500, 4, workspace=ws)
-    again, lse2 = _run(q, K, V, None, d ** -0.5, 500, 4)
+    out, lse = _run(q, K, V, None, d ** -0.5, window, 4, workspace=ws)
+    again, lse2 = _run(q, K, V, None, d ** -0.5, window, 4)
     assert torch.equal(out, again) and torch.equal(lse, lse2)
-    _check_long(q[:1], K[:1], V[:1], [N], [Tq], d ** -0.5, out, lse, 500, 4)
+    _check_long(q[:1], K[:1], V[:1], [N], [Tq], d ** -0.5, out, lse, window, 4)
 
 
 def test_no_rows_and_nothing_to_do():
