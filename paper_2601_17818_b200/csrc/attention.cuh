@@ -110,7 +110,7 @@ __device__ __forceinline__ Span span_of(const SeqArgs& a, const Sample& s, int t
     }
     const int p0 = s.base + t0, p1 = s.base + t1;
     v.b1 = p1 + 1;
-    v.b0 = max(0, p0 - a.window + 1);
+    v.b0 = max(0, max(p0, 0) - a.window + 1);              // (queries in front of the first row see nothing; a window may be 2^31 - 1)
     v.a = min(a.n_sink, v.b1);
     if (v.b0 <= v.a) v.a = v.b0 = 0;
     if (p0 >= 0) {

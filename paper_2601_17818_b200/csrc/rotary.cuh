@@ -3,7 +3,7 @@
 
 #include <cuda_bf16.h>
 
-#include "internal.cuh"
+#include "kv_attention.cuh"
 
 namespace vitcop {
 
@@ -14,7 +14,8 @@ struct RotaryArgs {
     const int32_t *position, *token, *seq_len, *axis;
     const double* inv_freq;
     int B, Hq, Hk, N, d, axes, n_pos, F, inverse;
-    int tokens, heads;                                     // of a CTA (the launcher's)
+    int tokens;                                            // of a CTA (this and the next are the launcher's)
+    Divisor heads, pieces;                                 // of a token, of a row
 };
 constexpr int kMostFrequencies = 256;                      // of a row
 int launch_rotary_axes(RotaryArgs args, cudaStream_t stream);

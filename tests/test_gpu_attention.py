@@ -346,7 +346,7 @@ def test_rows_beyond_32_bits(Tq):
 
 
 def _check_long(q, K, V, lens, counts, scale, out, lse, window=NO_WINDOW, n_sink=0, tree=None):
-    """As _check, by torch in fp64 on the GPU, a head at a time: for long sequences that are all numbers."""
+    """As _check, by torch in fp64 on the GPU, a head at a time.  Rows of V that are no numbers count with those who see them alone."""
     B, Hq, Tq, d = q.shape
     R = Hq // K.shape[1]
     for b in range(B):
@@ -359,18 +359,145 @@ def _check_long(q, K, V, lens, counts, scale, out, lse, window=NO_WINDOW, n_sink
         seen &= p >= 0
         for h in range(Hq):
             qd, k, v = q[b, h, :m].double(), K[b, h // R, :n].double(), V[b, h // R, :n].double()
-            z = (qd @ k.T * scale).masked_fill(~seen, -np.inf)
+            z = torch.where(seen, qd @ k.T * scale, -np.inf)
             wlse = torch.logsumexp(z, -1)
-            w = torch.exp(z - wlse[:, None]).nan_to_num(0.0)
-            want, size = w @ v, w @ v.abs()
-            delta = 2.0 ** -22 * (d / 16 + 2) * abs(scale) * (qd.abs() @ k.abs().T).masked_fill(~seen, 0).amax(-1, keepdim=True)
-            tol = HALF * (1 + HALF) * (size + 2 * want.abs()) + (torch.exp(2 * delta) - 1) * (size + want.abs())
-            assert ((out[b, h, :m].double() - want).abs() <= tol).all()
+            w = torch.exp(z - wlse[:, None])
             empty = torch.isneginf(wlse)
-            assert torch.isneginf(lse[b, h, :m][empty]).all()
-            off = (lse[b, h, :m].double() - wlse).abs()[~empty]
-            assert (off <= (delta[:, 0] + 2.0 ** -20 * (1 + wlse.abs()))[~empty]).all()
+            w[empty] = 0
+            odd = (seen.double() @ (~torch.isfinite(v)).double() > 0) | torch.isnan(wlse)[:, None]
+            v = v.nan_to_num(0.0, 0.0, 0.0)
+            want, size = w @ v, w @ v.abs()
+            delta = 2.0 ** -22 * (d / 16 + 2) * abs(scale) * torch.where(seen, qd.abs() @ k.abs().T, 0).amax(-1, keepdim=True) if n else torch.zeros(m, 1, device=DEV)
+            tol = HALF * (1 + HALF) * (size + 2 * want.abs()) + (torch.exp(2 * delta) - 1) * (size + want.abs()) + 1e-37
+            got = out[b, h, :m].double()
+            assert (((got - want).abs() <= tol) | odd).all()
+            assert (~torch.isfinite(got) == odd).all()
+            assert (got[empty] == 0).all() and torch.isneginf(lse[b, h, :m][empty]).all()
+            off, fine = (lse[b, h, :m].double() - wlse).abs(), ~empty & ~torch.isnan(wlse)
+            assert (off <= delta[:, 0] + 2.0 ** -20 * (1 + wlse.abs()))[fine].all()
+            assert torch.isnan(lse[b, h, :m][torch.isnan(wlse)]).all()
         assert (out[b, :, m:] == 9.0).all() and (lse[b, :, m:] == 9.0).all()
+
+
+def _kernels_of(*args, **kw):
+    """(out, lse, names of the kernels that a call has launched)"""
+    vb.vitcop_kernel_timing_begin()
+    try:
+        out, lse = _run(*args, **kw)
+    finally:
+        names = set(vb.vitcop_kernel_timing_end())
+    return out, lse, names
+
+
+MANY = {"attention_tiles_kernel"}
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,H,R,Tq,N,window,n_sink", [(16, 32, 1, 256, 300, 1, 0), (16, 32, 1, 256, 290, 0, 3), (16, 32, 1, 200, 301, 0, 0), (12, 32, 1, 260, 259, 40, 1000),
+                                                      (2, 8, 4, 300, 2300, 1700, 35), (3, 4, 7, 129, 1999, 1024, 0), (4, 8, 5, 515, 1500, 333, 130), (4, 4, 64, 50, 1500, 900, 9),
+                                                      (9, 32, 1, 131, 140, NO_WINDOW, 0)])
+def test_many_rows_windows_and_sinks(d, B, H, R, Tq, N, window, n_sink):
+    rng, q, K, V = _case(N + d, B, H, R, Tq, d, N)
+    lens = ([N, max(0, N - 13), Tq // 2, 0, 1, Tq, Tq - 1] * 3)[:B]            # (more queries than rows, no rows)
+    out, lse, names = _kernels_of(q, K, V, lens, d ** -0.5, window, n_sink)
+    assert names == MANY
+    _check_long(q, K, V, lens, [Tq] * B, d ** -0.5, out, lse, window, n_sink)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("B,H,R,N,window,n_sink", [(5, 16, 2, 700, 256, 35), (6, 8, 7, 400, 100, 5), (3, 4, 4, 1100, NO_WINDOW, 0)])
+def test_many_rows_padded_behind_with_anything(bad, B, H, R, N, window, n_sink):
+    d = 128
+    rng, q, K, V = _case(N, B, H, R, N, d, N)
+    lens = [N, N - 17, N // 2, 1, 0, N // 3][:B]
+    for b in range(B):
+        K[b, :, lens[b]:], V[b, :, lens[b]:], q[b, :, lens[b]:] = bad, bad, float("nan")
+    out, lse, names = _kernels_of(q, K, V, lens, d ** -0.5, window, n_sink, counts=lens)
+    assert names == MANY
+    _check_long(q, K, V, lens, lens, d ** -0.5, out, lse, window, n_sink)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,H,R,Tq,N,window,n_sink", [(2, 8, 4, 300, 1500, 700, 40), (16, 32, 1, 256, 400, 90, 5)])
+def test_many_rows_and_values_that_are_no_numbers(bad, d, B, H, R, Tq, N, window, n_sink):
+    """A single element, whole rows, at the edges of windows and sinks, one after the other."""
+    rng, q, K, V = _case(d, B, H, R, Tq, d, N)
+    at = sorted({0, 4, n_sink - 1, n_sink, N - Tq - window, N - Tq - window + 1, N - Tq - window + 60, N - Tq, N - Tq + 77, N - 130, N - 129, N - 2})
+    V[:, :, at] = bad
+    V[1, 0, N - 140, 7] = bad
+    out, lse, names = _kernels_of(q, K, V, None, d ** -0.5, window, n_sink)
+    assert names == MANY
+    _check_long(q, K, V, [N] * B, [Tq] * B, d ** -0.5, out, lse, window, n_sink)
+
+
+def test_many_rows_and_keys_that_are_no_numbers():
+    B, H, R, Tq, d, N, window, n_sink = 2, 8, 4, 300, 128, 1500, 700, 40
+    rng, q, K, V = _case(3, B, H, R, Tq, d, N)
+    K[0, :, [3, N - 200, N - 1]] = float("nan")
+    K[1, 2, N - 900, 5] = float("inf")
+    q[1, 9, 17, 3] = float("nan")
+    out, lse, names = _kernels_of(q, K, V, None, d ** -0.5, window, n_sink)
+    assert names == MANY
+    j, p = torch.arange(N, device=DEV)[None], N - Tq + torch.arange(Tq, device=DEV)[:, None]
+    seen = (j <= p) & ((j < n_sink) | (j + window > p))
+    hit = seen[:, [3, N - 200, N - 1]].any(1)
+    assert torch.isnan(out[0, :, hit]).all() and torch.isfinite(out[0, :, ~hit]).all()
+    assert torch.isnan(out[1, 9, 17]).all()
+    clean = K.nan_to_num(0.0, 0.0, 0.0)
+    want, _ = _run(q.nan_to_num(0.0), clean, V, None, d ** -0.5, window, n_sink)
+    same = [h for h in range(H * R) if h // R != 2 and h != 9]
+    assert torch.equal(out[1, same], want[1, same])
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3, 60.0])
+def test_many_rows_scales_and_values_near_the_end(scale):
+    B, H, R, Tq, d, N = 2, 8, 4, 260, 64, 1400
+    rng, q, K, V = _case(6, B, H, R, Tq, d, N)
+    V[0] *= 2.0 ** 125 / V[0].abs().max()
+    out, lse, names = _kernels_of(q, K, V, [N, N - 70], scale, 1000, 3)
+    assert names == MANY
+    _check_long(q, K, V, [N, N - 70], [Tq] * B, scale, out, lse, 1000, 3)
+
+
+def test_many_rows_strides_and_shared_tensors():
+    """One stored head for all samples, or heads; queries and output apart, the latter at odd multiples of 16 bytes; a row for all tokens, which the other
+    kernel takes."""
+    rng = np.random.default_rng(8)
+    B, H, R, d, N, Tq = 3, 4, 4, 128, 1500, 270
+    V = _bf16(rng, B, N, H, d).transpose(1, 2)
+    q = _bf16(rng, B, H * R, Tq, 2 * d)[..., d:]
+    wide = torch.full((B, H * R, Tq, 2 * d + 8), 9.0, dtype=torch.bfloat16, device=DEV)
+    lens = [N, N - 1, 1000]
+    for one in (_bf16(rng, 1, H, N, d).expand(B, H, N, d), _bf16(rng, 1, 1, N, d).expand(B, H, N, d), _bf16(rng, B, 1, N, d).expand(B, H, N, d)):
+        for k, v in ((one, V), (V, one)):
+            wide.fill_(9.0)
+            out, lse, names = _kernels_of(q, k, v, lens, 0.1, 900, 7, out=wide[..., 8:d + 8])
+            assert names == MANY
+            _check_long(q, k, v, lens, [Tq] * B, 0.1, out, lse, 900, 7)
+            assert (wide[..., :8] == 9.0).all() and (wide[..., d + 8:] == 9.0).all()
+    one = _bf16(rng, B, H, 1, d).expand(B, H, N, d)
+    out, lse, names = _kernels_of(q, one, V, lens, 0.1, 900, 7)
+    assert names == {"attention_few_kernel"}
+    _check_long(q, one, V, lens, [Tq] * B, 0.1, out, lse, 900, 7)
+    shared = _bf16(rng, 1, H * R, Tq, d).expand(B, H * R, Tq, d)
+    out, lse, names = _kernels_of(shared, V, V, lens, 0.1, 900, 7)
+    assert names == MANY
+    _check_long(shared, V, V, lens, [Tq] * B, 0.1, out, lse, 900, 7)
+
+
+@pytest.mark.parametrize("bad", [0.0, float("nan")])
+@pytest.mark.parametrize("B,H,R,Tq,N,d", [(8, 4, 7, 60, 3000, 128), (8, 8, 8, 64, 2500, 64), (16, 32, 1, 64, 1300, 128)])
+def test_many_rows_of_trees(bad, B, H, R, Tq, N, d):
+    rng, q, K, V = _case(N, B, H, R, Tq, d, N)
+    lens = ([N, N - 1, Tq, Tq - 3, 5, 0, N - 64, N // 2] * 2)[:B]
+    tree = torch.from_numpy(_tree(rng, B, Tq)).to(DEV)
+    tree[0, 0] = -1
+    for b in range(B):
+        V[b, :, max(0, lens[b] - Tq + 2):lens[b]:5] += bad
+    out, lse, names = _kernels_of(q, K, V, lens, d ** -0.5, tree=tree.cpu().numpy())
+    assert names == MANY
+    _check_long(q, K, V, lens, [Tq] * B, d ** -0.5, out, lse, tree=tree)
 
 
 @pytest.mark.parametrize("B,H,R,N,d,window,n_sink", [(1, 1, 7, 2990, 128, 700, 64), (2, 2, 2, 1501, 64, 900, 0), (3, 8, 8, 901, 128, 200, 16), (1, 2, 1, 5000, 128, NO_WINDOW, 0),
