@@ -416,8 +416,9 @@ int vitcop_cache_attention(const void* q, const void* cache, int B, int Hq, int 
  *   q_out, k_out  as q and k, strides of their own.  In place (same pointer and strides as the input) is fine; otherwise outputs must
  *              not share elements with inputs or one another.  (Two tensors may lie in one another's gaps, as q, k and v of one projection do,
  *              where the strides of their tokens are the same and those of their samples multiples of it.)
- * Errors: INVALID_ARG (negative sizes or strides, d 0, axes < 1, q and k both NULL, NULL position/inv_freq/axis, n_pos < N without token, overlap, rows of an
- * output that share elements), UNSUPPORTED (d % 8, n_freq % 8, 2 n_freq > d, n_freq > 256, alignment, B above 65535, more than 2^31 - 1 rows), CUDA. */
+ * Errors: INVALID_ARG (negative sizes or strides, d 0, axes < 1, q and k both NULL, NULL position/inv_freq/axis, n_pos 0 or without token < N, overlap, rows of an
+ * output that share elements), UNSUPPORTED (d % 8, d > 4096, n_freq % 8, 2 n_freq > d, n_freq > 256, alignment, B above 65535, Hq or Hk above 32767, more than
+ * 2^31 - 2^16 rows of all heads), CUDA. */
 int vitcop_rotary_axes(const void* q, const void* k, int B, int Hq, int Hk, int N, int d,
                        int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_t,
                        int64_t k_stride_b, int64_t k_stride_h, int64_t k_stride_t,
@@ -444,12 +445,12 @@ int vitcop_rotary_axes(const void* q, const void* k, int B, int Hq, int Hk, int 
  *   tree     int64 [B, Tq]
  *   lse      fp32 [B, Hq, Tq] out, optional: log of the sum of exp(scale * q k) over the rows seen
  *   workspace  vitcop_workspace_bytes(VITCOP_OP_ATTENTION, B, H, N, d, Tq, Hq, 0) bytes: a status word
- * Many query rows (more than 32 of a stored head, d 64 or 128) run through a kernel whose waits are bounded (vitcop_set_wait_limit): the status word is
+ * Many query rows (d 64 or 128, where that is the faster way) run through a kernel whose waits are bounded (vitcop_set_wait_limit): the status word is
  * TIMEOUT, and out unspecified, where one ran out.
  * (A pointer to nothing, as no rows or no queries, may be NULL.)
  * Errors: INVALID_ARG (NULL q/K/V/tree/out, negative sizes, strides, window or n_sink, d 0, Hq no multiple of H, a scale that is no number or beyond
- * 2^127, rows of out that share elements, overlap), UNSUPPORTED (d not 64, 128 or 256, Tq > 64 with a tree, alignment, B above 65535, more than 2^31 - 1
- * query rows), WORKSPACE, CUDA. */
+ * 2^127, rows of out that share elements, overlap), UNSUPPORTED (d not 64, 128 or 256, Tq > 64 with a tree, alignment, B above 65535, N above 2^31 - 2^16, more
+ * than 2^31 - 1 query rows), WORKSPACE, CUDA. */
 int vitcop_window_attention(const void* q, const void* K, const void* V, int B, int Hq, int H, int Tq, int d, int N,
                             int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_t,
                             int64_t k_stride_b, int64_t k_stride_h, int64_t k_stride_n,

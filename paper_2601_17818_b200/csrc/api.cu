@@ -630,14 +630,14 @@ int vitcop_rotary_axes(const void* q, const void* k, int B, int Hq, int Hk, int 
     for (int i = 0; i < 12; ++i)
         if (strides[i] < 0) return VITCOP_ERR_INVALID_ARG;
     if (n_freq > 0 && (!inv_freq || !axis)) return VITCOP_ERR_INVALID_ARG;
-    if (B > 0 && N > 0 && ((n_freq > 0 && (!position || n_pos == 0)) || (!token && n_pos < N))) return VITCOP_ERR_INVALID_ARG;
-    if (d % 8 || n_freq % 8 || 2 * (int64_t)n_freq > d || n_freq > kMostFrequencies) return VITCOP_ERR_UNSUPPORTED;
+    if (B > 0 && N > 0 && (n_pos == 0 || (n_freq > 0 && !position) || (!token && n_pos < N))) return VITCOP_ERR_INVALID_ARG;
+    if (d % 8 || d > 4096 || n_freq % 8 || 2 * (int64_t)n_freq > d || n_freq > kMostFrequencies || Hq > 32767 || Hk > 32767) return VITCOP_ERR_UNSUPPORTED;
     for (int i = 0; i < 12; ++i)
         if (strides[i] % 8 && (i < 6 ? q : k)) return VITCOP_ERR_UNSUPPORTED;
     if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || !aligned8(inv_freq) || B > 65535) return VITCOP_ERR_UNSUPPORTED;
     if (!q) Hq = 0;
     if (!k) Hk = 0;
-    if (N > 0 && (int64_t)B * N > 0x7fffffff / std::max<int64_t>(1, (int64_t)Hq + Hk)) return VITCOP_ERR_UNSUPPORTED;
+    if (N > 0 && (int64_t)B * N > 0x7fff0000 / std::max<int64_t>(1, (int64_t)Hq + Hk)) return VITCOP_ERR_UNSUPPORTED;
     if (B == 0 || N == 0 || Hq + Hk == 0) return VITCOP_OK;
     const Rows4 rows[4] = {{q, Hq, q_stride_b, q_stride_h, q_stride_t, extent(B, Hq, N, d, q_stride_b, q_stride_h, q_stride_t)},
                            {k, Hk, k_stride_b, k_stride_h, k_stride_t, extent(B, Hk, N, d, k_stride_b, k_stride_h, k_stride_t)},
@@ -709,7 +709,7 @@ static int run_attention(const AttentionCall& c, bool is_tree, void* stream) {
     if (c.H > 0 ? c.Hq % c.H != 0 : c.Hq != 0) return VITCOP_ERR_INVALID_ARG;
     for (int64_t s : c.at)
         if (s < 0) return VITCOP_ERR_INVALID_ARG;
-    if ((c.d != 64 && c.d != 128 && c.d != 256) || c.B > 65535 || (is_tree && c.Tq > 64)) return VITCOP_ERR_UNSUPPORTED;
+    if ((c.d != 64 && c.d != 128 && c.d != 256) || c.B > 65535 || c.N > 0x7fff0000 || (is_tree && c.Tq > 64)) return VITCOP_ERR_UNSUPPORTED;
     for (int64_t s : c.at)
         if (s % 8) return VITCOP_ERR_UNSUPPORTED;
     if (!aligned16(c.q) || !aligned16(c.K) || !aligned16(c.V) || !aligned16(c.out) || !aligned8(c.tree)) return VITCOP_ERR_UNSUPPORTED;

@@ -76,6 +76,18 @@ attention_few_kernel(const __grid_constant__ FewArgs k) {
     const int rank = blockIdx.x & (k.ctas - 1), seg = blockIdx.x / k.ctas;
     const int bh = quotient(seg, k.tiles), row0 = (seg - bh * (int)k.tiles.d) * kRows, b = quotient(bh, k.heads), h = bh - b * (int)k.heads.d;
     const int R = (int)a.R.d;
+    // queries, on their way before the lengths are known (rows that the sample does not have are stored nowhere)
+    constexpr int kQueryPieces = kRows * kPieces / (kWarps * 32);
+    uint4 query[kQueryPieces];
+#pragma unroll
+    for (int n = 0; n < kQueryPieces; ++n) {
+        const int i = n * kWarps * 32 + tid, r = i / kPieces, c = i % kPieces;
+        query[n] = make_uint4(0, 0, 0, 0);
+        if (row0 + r < R * a.Tq) {
+            const int t = quotient(row0 + r, a.R), hq = h * R + (row0 + r - t * R);
+            query[n] = __ldcg(reinterpret_cast<const uint4*>(a.io.q + b * a.io.q_at[0] + hq * a.io.q_at[1] + t * a.io.q_at[2] + c * 8));
+        }
+    }
     const Sample s = sample_of(a, b);
     const int rows = min(kRows, R * s.queries - row0);     // of this CTA
     if (rows <= 0) return;                                 // (its whole cluster)
@@ -113,18 +125,6 @@ attention_few_kernel(const __grid_constant__ FewArgs k) {
 #pragma unroll
     for (int st = 0; st < kStages - 1; ++st) fetch(first + warp + st * kWarps, st);
 
-    // queries to shared memory
-    constexpr int kQueryPieces = kRows * kPieces / (kWarps * 32);
-    uint4 query[kQueryPieces];
-#pragma unroll
-    for (int n = 0; n < kQueryPieces; ++n) {
-        const int i = n * kWarps * 32 + tid, r = i / kPieces, c = i % kPieces;
-        query[n] = make_uint4(0, 0, 0, 0);
-        if (r < rows) {
-            const int t = quotient(row0 + r, a.R), hq = h * R + (row0 + r - t * R);
-            query[n] = __ldcg(reinterpret_cast<const uint4*>(a.io.q + b * a.io.q_at[0] + hq * a.io.q_at[1] + t * a.io.q_at[2] + c * 8));
-        }
-    }
     // what the four rows of this thread see (a row behind the last sees nothing)
     const auto row_seen = [&](int r) { return Seen<TREE>(a, s, b, r < rows ? quotient(row0 + r, a.R) : s.queries); };
     Seen<TREE> seen[2 * MT] = {row_seen(lane / 4), row_seen(lane / 4 + 8)};
@@ -455,7 +455,7 @@ int launch_attention_few(const SeqArgs& a, int d, const FewPlan& p, cudaStream_t
     k.ctas = p.ctas;
     const int tile = p.tile;
     const int64_t segs = p.segs;
-    if (segs * kMostParts > 0x7fffffff) return VITCOP_ERR_UNSUPPORTED;
+    if (segs * k.ctas > 0x7fffffff) return VITCOP_ERR_UNSUPPORTED;
     k.tiles = divisor((int)p.tiles);
     k.heads = divisor(a.H);
     switch (d) {

@@ -1,5 +1,6 @@
 """Rotary positions and attention over bf16 rows without a GPU: the oracle held to closed forms, and what the entry points refuse."""
 import ctypes as C
+import os
 
 import numpy as np
 import pytest
@@ -121,7 +122,7 @@ def test_attention_refuses(L, is_tree):
     assert status(lse=OUT) == inv and status(ws=OUT) == inv and status(lse=WS) == inv
     assert status(out=C.c_void_p((112 << 20) - 256)) == inv                                            # lengths in the output
     assert status(ws=NULL) == vb.ERR_WORKSPACE and status(bytes=8) == vb.ERR_WORKSPACE and status(ws=C.c_void_p((96 << 20) + 16)) == vb.ERR_WORKSPACE
-    assert status(B=65536) == uns and status(Tq=2 ** 30, os=(2 ** 50, 2 ** 40, 128)) == uns
+    assert status(B=65536) == uns and status(Tq=2 ** 30, os=(2 ** 50, 2 ** 40, 128)) == uns and status(N=2 ** 31 - 1, ks=(0, 0, 0), vs=(0, 0, 0)) == uns
     if is_tree:
         assert status(tree=NULL) == inv and status(tree=C.c_void_p((120 << 20) + 4)) == uns and status(Tq=65) == uns
         assert status(tree=OUT) == inv
@@ -153,6 +154,8 @@ def test_rotary_refuses(L):
         assert status(**{name: -1}) == inv, name
     assert status(axes=0) == inv and status(d=0) == inv and status(n_pos=15) == inv and status(token=C.c_void_p(115 << 20), n_pos=0) == inv
     assert status(d=100) == uns and status(F=4) == uns and status(F=72) == uns and status(d=1024, F=264, qs=(0, 0, 0), ks=(0, 0, 0)) == uns
+    assert status(d=4104, F=8) == uns and status(Hq=32768) == uns and status(Hk=40000) == uns and status(N=2 ** 31 - 1, token=C.c_void_p(115 << 20)) == uns
+    assert status(token=C.c_void_p(115 << 20), n_pos=0, F=0) == inv
     assert status(B=65536) == uns and status(inv_freq=C.c_void_p((113 << 20) + 4)) == uns
     for name in ("qs", "ks", "qo", "ko"):
         for i in range(3):
@@ -195,3 +198,20 @@ def test_the_binding_refuses_other_tensors(L):
     for name in ("window_attention", "tree_attention", "rotary_axes"):
         with pytest.raises(TypeError):
             getattr(vb._module, name)(0, 0)
+
+
+def test_registers_that_change_hands_are_there():
+    """The kernel for many query rows gives registers of some warps to others: the compiler's number a thread is the one that the exchange counts on (asked for and
+    not there, they would be waited for without end), and its loop over blocks has no cache to spill to."""
+    import re
+    import subprocess
+    from paper_2601_17818_b200 import build
+    r = subprocess.run([build._nvcc(), *build.NVCC_FLAGS, "-Xptxas", "-v", "-cubin", os.path.join(build.CSRC, "attention_tiles.cu"), "-o", os.devnull],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    used = re.findall(r"Compiling entry function '\S*attention_tiles_kernel\S*'.*?Used (\d+) registers", r.stderr, re.S)
+    with open(os.path.join(build.CSRC, "attention_tiles.cu")) as fh:
+        source = fh.read()
+    softmax, other = (int(re.search(rf"{name} = (\d+)", source).group(1)) for name in ("kSoftmaxRegs", "kOtherRegs"))
+    threads = int(re.search(r"kSoftmaxThreads = (\d+)", source).group(1))
+    assert len(used) == 4 and set(used) == {str((threads * softmax + 128 * other) // (threads + 128))}
