@@ -111,6 +111,12 @@ __device__ __forceinline__ void tc_mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem,
 __device__ __forceinline__ uint64_t umma_desc_mn128(uint32_t smem_addr) {
     return umma_desc_k128(smem_addr) | (uint64_t)(16384u >> 4) << 16;
 }
+// A descriptor, its address (in 16 bytes) further on; what is not the address stays in the same register.
+__device__ __forceinline__ uint64_t further(uint64_t desc, uint32_t by) {
+    uint64_t d;
+    asm("{\n\t.reg .b32 lo, hi;\n\tmov.b64 {lo, hi}, %1;\n\tadd.u32 lo, lo, %2;\n\tmov.b64 %0, {lo, hi};\n\t}" : "=l"(d) : "l"(desc), "r"(by));
+    return d;
+}
 __device__ __forceinline__ void tmem_ld32_issue(uint32_t taddr, uint32_t (&r)[32]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
@@ -294,7 +300,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         }
         mbar_init(bar_q_free, 1);
         mbar_init(bar_drain, 1);
-        *abort_flag = 0;
+        *abort_flag = (base & 1023u) != 0;                 // (operands lie at multiples of 1024, or nothing is done)
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (tid == kSoftmaxThreads) {
@@ -622,7 +628,8 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     }
                     // the block before, whose V is there by now or soon
                     if (ok && j > it.k0 && !(it.tiles[0].columns(it.blocks, j - 1).all && it.tiles[1].columns(it.blocks, j - 1).all)) {
-                        ok = masked < kMasked && take_out(before, before_phase, bad + ((n & 1) * kMasked + masked) * 4);
+                        if (masked >= kMasked) *abort_flag = 1;
+                    ok = masked < kMasked && take_out(before, before_phase, bad + ((n & 1) * kMasked + masked) * 4);
                         ++masked;
                     }
                 }
@@ -646,17 +653,17 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     const uint64_t dq = umma_desc_k128(base + S::kQ + x * S::kOperand), dk = umma_desc_k128(ring + c.lo * 128);
                     const uint32_t d = tmem_s(x) + c.lo, idesc = idesc_s | (uint32_t)((c.hi - c.lo) >> 3) << 17;
 #pragma unroll
-                    for (int e = 0; e < D / 16; ++e) tc_mma_bf16(d, dq + (uint64_t)((e / 4) * 1024 + (e % 4) * 2), dk + (uint64_t)((e / 4) * 1024 + (e % 4) * 2), idesc, e > 0 ? 1u : 0u);
+                    for (int e = 0; e < D / 16; ++e) tc_mma_bf16(d, further(dq, (e / 4) * 1024 + (e % 4) * 2), further(dk, (e / 4) * 1024 + (e % 4) * 2), idesc, e > 0 ? 1u : 0u);
                     tc_commit(bar_s + 8 * x);
                 };
                 const auto second_product = [&](int x, uint32_t ring, int lo, int hi, bool begun) {
                     const uint64_t dv = umma_desc_mn128(ring);
                     if (hi - lo == kBlock / 2) {
 #pragma unroll
-                        for (int e = 0; e < kBlock / 32; ++e) tc_mma_bf16_ts(tmem_o(x), tmem_s(x) + lo / 2 + 8 * e, dv + (uint64_t)(lo * 8 + e * 128), idesc_o, begun || e > 0 ? 1u : 0u);
+                        for (int e = 0; e < kBlock / 32; ++e) tc_mma_bf16_ts(tmem_o(x), tmem_s(x) + lo / 2 + 8 * e, further(dv, lo * 8 + e * 128), idesc_o, begun || e > 0 ? 1u : 0u);
                     } else {
 #pragma unroll 1
-                        for (int e = lo / 16; e < hi / 16; ++e, begun = true) tc_mma_bf16_ts(tmem_o(x), tmem_s(x) + 8 * e, dv + (uint64_t)(e * 128), idesc_o, begun ? 1u : 0u);
+                        for (int e = lo / 16; e < hi / 16; ++e, begun = true) tc_mma_bf16_ts(tmem_o(x), tmem_s(x) + 8 * e, further(dv, e * 128), idesc_o, begun ? 1u : 0u);
                     }
                 };
                 bool ok = true;
