@@ -13,6 +13,11 @@
 //   warp 9          products: PV(A), QK(A), PV(B), QK(B): while one tile's softmax runs, the other's products do
 // A CTA takes items in turn, the next item's first products under the last one's output.  Where items are fewer than SMs, a cluster of up to eight CTAs
 // shares an item's blocks and joins its parts in shared memory.
+// Bound by the chain of a tile, logits to weights to products, which one other tile does not fill, and tensor memory holds no third: some 3300 cycles for a
+// block of two tiles, of which the tensor cores work 2048 and the units of exponentials as many.  16512 tokens x 28 heads of 128, window 4096: 860-920 us
+// (0.94-1.0 PFLOP/s, at the power limit); 2 x 4672, window 1024: 178; 8 x up to 704 x 32 heads, window 256: 77, where items' beginnings and ends count.
+// Weights enter the second product in bf16, the output is divided by the sum of the unrounded ones: 0.0019-0.0023 of the output's size from 64 bits.  (By
+// that of the rounded ones: 0.0018, 11 % more time.)
 #include "attention.cuh"
 
 #include <algorithm>
