@@ -8,7 +8,7 @@
 namespace vitcop {
 
 // Weights are 2^(logit - top), top this much above the largest logit there was when it was set (in powers of two): it stays until a logit passes it, which few
-// do, and no weight is above 1, so that sums with values near the end of fp32's range hold.
+// do, and no weight is above 1.  (Values of V below 2^-100 or so lose bits for it.)
 constexpr float kHeadroom = 24.f;
 
 // Queries, keys, values, output: bf16, strides of samples, heads, tokens in elements.

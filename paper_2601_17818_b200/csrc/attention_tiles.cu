@@ -530,7 +530,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             const auto waited = [&](uint32_t bar, uint32_t parity) { return warp_wait(bar, parity, abort_flag, k.limit_of(kRoleLoad)); };
             uint32_t slot = 0, phase = 0;
             int n = 0;
-            bool ok = true;
+            bool ok = *abort_flag == 0;                    // (operands that lie nowhere are not fetched)
             const auto fetch = [&](const CUtensorMap* map, int row, int h, int b) {        // an operand to the ring
                 if (!waited(bar_empty + 8 * slot, phase ^ 1)) return false;
                 if (lane == 0) {
@@ -634,7 +634,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     // the block before, whose V is there by now or soon
                     if (ok && j > it.k0 && !(it.tiles[0].columns(it.blocks, j - 1).all && it.tiles[1].columns(it.blocks, j - 1).all)) {
                         if (masked >= kMasked) *abort_flag = 1;
-                    ok = masked < kMasked && take_out(before, before_phase, bad + ((n & 1) * kMasked + masked) * 4);
+                        ok = masked < kMasked && take_out(before, before_phase, bad + ((n & 1) * kMasked + masked) * 4);
                         ++masked;
                     }
                 }
