@@ -417,6 +417,20 @@ def test_many_rows_padded_behind_with_anything(bad, B, H, R, N, window, n_sink):
     _check_long(q, K, V, lens, lens, d ** -0.5, out, lse, window, n_sink)
 
 
+@pytest.mark.parametrize("B,H,R,N", [(31, 8, 2, 600), (32, 16, 1, 550), (33, 16, 1, 550), (40, 3, 7, 300)])
+def test_many_rows_every_sample_its_own_number(B, H, R, N):
+    """Also none at all, in samples in front, behind and between."""
+    d = 64
+    rng, q, K, V = _case(B, B, H, R, N, d, N)
+    counts = rng.integers(0, N + 1, B)
+    counts[[0, 3, 4, B - 1]], counts[5] = [0, -2, 0, 0], N + 7
+    lens = np.minimum(N, np.clip(counts, 0, N) + rng.integers(0, 90, B)).tolist()
+    counts = counts.tolist()
+    out, lse, names = _kernels_of(q, K, V, lens, d ** -0.5, 130, 9, counts=counts)
+    assert names == MANY
+    _check_long(q, K, V, lens, counts, d ** -0.5, out, lse, 130, 9)
+
+
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("B,H,R,Tq,N,window,n_sink", [(2, 8, 4, 300, 1500, 700, 40), (16, 32, 1, 256, 400, 90, 5)])
