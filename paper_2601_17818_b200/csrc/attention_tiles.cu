@@ -87,7 +87,10 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
     unsigned long long t0 = 0ull;
     bool in_time = limit_ns != 0ull;
     for (uint32_t it = 1; in_time; ++it) {
-        if (asked(bar, parity)) return true;
+        if (asked(bar, parity)) {
+            __syncwarp();                                  // (a vote orders no memory: what the barrier stands for is there for the lane that asked)
+            return true;
+        }
         if ((it & 63u) == 0u) {                            // (reading the clock takes longer than most waits)
             const unsigned long long now = __shfl_sync(0xffffffffu, global_ns(), 0);
             if (t0 == 0ull) t0 = now;
