@@ -29,3 +29,10 @@ def test_all_lanes_see_what_the_lane_that_asks_a_barrier_sees():
     assert len(re.findall(r"return true", wait)) == 1
     assert re.search(r"if \(asked\(bar, parity\)\) \{\s*__syncwarp\(\);\s*return true;", wait)
     assert '"memory"' in _body(code, "bool asked(") and code.count("asked(") == 2              # (nothing else asks that way)
+
+
+def test_nothing_is_read_as_constant_beside_a_kernel_that_may_write_it():
+    """The kernels are launched while the one in front is still running: what it writes is not constant for as long as they run, as reads through the read-only cache
+    ask for."""
+    for name in ("rotary.cu", "attention.cu", "attention_tiles.cu", "attention.cuh"):
+        assert not re.search(r"__ldg\(|ld\.global\.nc|__restrict__", _code(name)), name
