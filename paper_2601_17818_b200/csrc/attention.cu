@@ -285,7 +285,8 @@ attention_few_kernel(const __grid_constant__ FewArgs k) {
     }
     __syncthreads();
     // What each part of a row counts by, a thread a row; then the sums, a thread four elements.  At first of the warps' parts, which a CTA by itself writes out
-    // and others leave in the place of the first; then of the CTAs', rows in turn to each.
+    // and others leave in the place of the first; then of the CTAs', rows in turn to each.  Where nothing weighs anything in a whole row (it sees nothing, or
+    // logits of -inf alone) its first count is kNothing: the output is 0 by selection, for parts may hold 0 times a value that is no number.
     const bool alone = k.ctas == 1;
     const auto query_of = [&](int row, int& tq, int& hq) {
         const int i = row0 + row;
@@ -331,9 +332,9 @@ attention_few_kernel(const __grid_constant__ FewArgs k) {
             weights[w] = w < kWarps ? ends[(w * 3 + 2) * kRows + tid] : 0.f;
         }
         counted(tops, sums, weights, t, su, we);
-        const float inv = !alone ? 1.f : su == 0.f ? 0.f : 1.f / we;     // (0: nothing seen)
+        const float inv = alone ? 1.f / we : 1.f;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) counts[tid * kWarps + w] = tops[w] * inv;
+        for (int w = 0; w < kWarps; ++w) counts[tid * kWarps + w] = alone && su == 0.f ? kNothing : tops[w] * inv;
         if (alone) {
             whole(tid, t, su);
         } else {
@@ -349,7 +350,7 @@ attention_few_kernel(const __grid_constant__ FewArgs k) {
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) add(v, *reinterpret_cast<const float4*>(smem + w * S::kWarp + (row * S::kPitch + e) * 4), counts[row * kWarps + w]);
-        if (alone) write(row, e, v);
+        if (alone) write(row, e, counts[row * kWarps] == kNothing ? make_float4(0.f, 0.f, 0.f, 0.f) : v);
         else *reinterpret_cast<float4*>(smem + (row * S::kPitch + e) * 4) = v;     // (this thread has read what was there)
     }
     if (alone) return;
@@ -367,10 +368,10 @@ attention_few_kernel(const __grid_constant__ FewArgs k) {
             weights[c] = c < k.ctas ? cluster_ld(from + kRows * 8) : 0.f;
         }
         counted(tops, sums, weights, t, su, we);
-        const float inv = su == 0.f ? 0.f : 1.f / we;
+        const float inv = 1.f / we;
 #pragma unroll
         for (int c = 0; c < kMostParts; ++c)
-            if (c < k.ctas) counts[tid * k.ctas + c] = tops[c] * inv;
+            if (c < k.ctas) counts[tid * k.ctas + c] = su == 0.f ? kNothing : tops[c] * inv;
         whole(row, t, su);
     }
     __syncthreads();
@@ -381,7 +382,7 @@ attention_few_kernel(const __grid_constant__ FewArgs k) {
 #pragma unroll
         for (int c = 0; c < kMostParts; ++c)
             if (c < k.ctas) add(v, cluster_ld4(cluster_map(at, c)), counts[j * k.ctas + c]);
-        write(row, e, v);
+        write(row, e, counts[j * k.ctas] == kNothing ? make_float4(0.f, 0.f, 0.f, 0.f) : v);
     }
     cluster_sync_all();                                    // (the others may still be reading what this CTA has)
 }

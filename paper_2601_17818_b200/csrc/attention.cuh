@@ -11,6 +11,8 @@ namespace vitcop {
 // do, and no weight is above 1.  (Values of V below 2^-100 or so lose bits for it.)
 constexpr float kHeadroom = 24.f;
 
+constexpr float kNothing = -1.f;                           // in place of what a part of a row counts by, where no part weighs anything
+
 // Queries, keys, values, output: bf16, strides of samples, heads, tokens in elements.
 struct SeqRows {
     const __nv_bfloat16 *q, *K, *V;

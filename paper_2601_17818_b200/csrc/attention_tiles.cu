@@ -815,7 +815,8 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     const int t0 = (k.per_head - 1 - tile) * 2 * tokens;
     const Sample s = sample_of(a, b);
     if (t0 < s.queries) {
-        // what each part of a row counts by, a thread a row; then the sums, a thread four elements
+        // what each part of a row counts by (kNothing: none weighs anything, the output is 0 whatever the parts are), a thread a row; then the sums, a thread
+        // four elements
         const int mine = 2 * kTile / k.ctas;
         const float* const ends = reinterpret_cast<const float*>(smem + S::kPartEnds);
         float* const counts = reinterpret_cast<float*>(smem + S::kPartCounts);         // [rows][CTAs]
@@ -842,10 +843,10 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 total = fmaf(sums[c], tops[c], total);
             }
             const bool none = total == 0.f;
-            const float inv = none ? 0.f : 1.f / total;
+            const float inv = 1.f / total;
 #pragma unroll
             for (int c = 0; c < kMostCtas; ++c)
-                if (c < k.ctas) counts[tid * k.ctas + c] = tops[c] * inv;
+                if (c < k.ctas) counts[tid * k.ctas + c] = none ? kNothing : tops[c] * inv;
             int t, hq;
             if (query_of(row, t, hq) && a.lse) a.lse[((int64_t)b * a.Hq + hq) * a.Tq + t] = none ? MINUS_INF : (top + log2f(total)) * kLn2;
         }
@@ -867,6 +868,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 v.z = fmaf(y.z, f, v.z);
                 v.w = fmaf(y.w, f, v.w);
             }
+            if (counts[j * k.ctas] == kNothing) v = make_float4(0.f, 0.f, 0.f, 0.f);
             *reinterpret_cast<uint2*>(a.io.out + b * a.io.out_at[0] + hq * a.io.out_at[1] + t * a.io.out_at[2] + e) = make_uint2(bf16x2(v.x, v.y), bf16x2(v.z, v.w));
         }
     }

@@ -1,0 +1,71 @@
+"""Rotary positions and attention over bf16 rows where little is left to weigh, near the ends of fp32, over sizes on which the division of work turns, and beside the
+other calls (``-m gpu``).  Tolerances as in test_gpu_attention.py, where they are derived; what is added to them is derived here beside its use.
+
+Which path a call takes is asserted by its kernel's name and, of the kernel for many rows, by the number of CTAs that it has left in its status word.
+"""
+import numpy as np
+import pytest
+import torch
+
+from paper_2601_17818_b200 import binding as vb
+from test_gpu_attention import DEV, HALF, MANY, NO_WINDOW, _bf16, _case, _check_long, _f64, _i32, _kernels_of, _run
+
+pytestmark = pytest.mark.gpu
+FEW = {"attention_few_kernel"}
+# B, H, R, Tq, N, kernel: a CTA a head, a cluster a head; items in turn, a cluster an item
+PATHS = [(2, 100, 1, 1, 64, FEW), (2, 2, 2, 3, 600, FEW), (2, 8, 4, 300, 1500, MANY), (2, 1, 4, 300, 3000, MANY)]
+PATHS = [(d, *path) for path in PATHS for d in (64, 128, 256) if d < 256 or path[-1] is FEW]
+NAN, INF = float("nan"), float("inf")
+
+
+def _plain(q, K, V, seen, scale):
+    """(out, lse, tolerances of both) in fp64 by torch: of a causal call whose rows ``seen`` (bool [B, H, N]) weigh something, K and V finite there."""
+    R, Tq, N, d = q.shape[1] // K.shape[1], q.shape[2], K.shape[2], q.shape[3]
+    rows = lambda x: torch.where(seen[..., None], x, 0).double().repeat_interleave(R, 1)
+    see = seen.repeat_interleave(R, 1)[:, :, None] & (torch.arange(N, device=DEV) <= N - Tq + torch.arange(Tq, device=DEV)[:, None])
+    qd, k, v = q.double(), rows(K), rows(V)
+    z = torch.where(see, qd @ k.mT * scale, -np.inf)
+    lse = torch.logsumexp(z, -1)
+    w = torch.exp(z - lse[..., None])
+    w = torch.where(torch.isneginf(lse)[..., None], 0, w)
+    want, size = w @ v, w @ v.abs()
+    delta = 2.0 ** -22 * (d / 16 + 2) * abs(scale) * torch.where(see, qd.abs() @ k.abs().mT, 0).amax(-1, keepdim=True)
+    return want, lse, HALF * (1 + HALF) * (size + 2 * want.abs()) + (torch.exp(2 * delta) - 1) * (size + want.abs()), delta[..., 0] + 2.0 ** -20 * (1 + lse.abs())
+
+
+@pytest.mark.parametrize("d,B,H,R,Tq,N,kernel", PATHS)
+def test_nothing_weighed_beside_values_that_are_no_numbers(d, B, H, R, Tq, N, kernel):
+    """Logits of -inf alone: out = 0 and lse = -inf, whatever V holds and however a row's parts are joined.  (Where others weigh something, 0 times what is no number
+    is none.)"""
+    rng, q, K, V = _case(N + d, B, H, R, Tq, d, N)
+    q[..., 0] = 1.0
+    K[0, ..., 0] = -INF
+    V[0, :, ::7], V[0, :, 1::9], V[0, :, N - 2] = NAN, INF, -INF
+    K[1, :, ::3, 0] = -INF
+    V[1, :, 3, 5], V[1, :, N // 2 // 3 * 3, 9] = NAN, -INF
+    out, lse, names = _kernels_of(q, K, V, None, d ** -0.5)
+    assert names == kernel
+    assert (out[0] == 0).all() and torch.isneginf(lse[0]).all()
+    assert torch.isnan(out[1][..., [5, 9]]).all()
+    seen = torch.arange(N, device=DEV).expand(B, H, N) % 3 != 0
+    want, wlse, tol, lse_tol = _plain(q, K, V, seen, d ** -0.5)
+    rest = [e for e in range(d) if e not in (5, 9)]
+    assert ((out[1].double() - want[1]).abs() <= tol[1])[..., rest].all()
+    assert ((lse[1].double() - wlse[1]).abs() <= lse_tol[1]).all()
+
+
+@pytest.mark.parametrize("bad", [INF, -INF])
+@pytest.mark.parametrize("d,B,H,R,Tq,N,kernel", PATHS)
+def test_infinite_keys_of_rows_that_are_seen(bad, d, B, H, R, Tq, N, kernel):
+    """One infinite element: its logit is +inf, and the output no number, or -inf, and the row weighs nothing, as its query's element has the same sign or the other."""
+    rng, q, K, V = _case(N + d + 1, B, H, R, Tq, d, N)
+    at = torch.zeros(N, dtype=torch.bool, device=DEV)
+    at[[1, N // 3, N // 2, N - Tq]] = True                 # (all of them seen by all queries)
+    K[:, :, at, 2] = bad
+    q[..., 2] = torch.where(torch.rand(q.shape[:-1], device=DEV) < 0.5, 1.0, -1.0).bfloat16()
+    out, lse, names = _kernels_of(q, K, V, None, d ** -0.5)
+    assert names == kernel
+    want, wlse, tol, lse_tol = _plain(q, K, V, ~at.expand(B, H, N), d ** -0.5)
+    nan = q[..., 2].float() * bad > 0
+    assert nan.any() and torch.isnan(out[nan]).all() and torch.isnan(lse[nan]).all()
+    assert ((out.double() - want).abs() <= tol)[~nan].all() and ((lse.double() - wlse).abs() <= lse_tol)[~nan].all()
