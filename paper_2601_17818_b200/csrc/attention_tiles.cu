@@ -912,10 +912,20 @@ int launch_tiles(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap
     return record_cuda(cudaLaunchKernelEx(&cfg, attention_tiles_kernel<D, TREE>, mq, mk, mv, k));
 }
 
+// Clusters of this size that run at a time, an SM a CTA (all kernels of this file alike): not SMs / ctas, for a cluster stays inside a group of SMs.
+int clusters_that_run(int ctas) {
+    static KnownOnDevice known[3];
+    static DoneOnDevice done;
+    constexpr int kBytes = TilesSmem<128>::kBytes;
+    const auto allow = [] { return allow_dynamic_smem(attention_tiles_kernel<128, false>, kBytes, done); };
+    return clusters_at_once(attention_tiles_kernel<128, false>, ctas, kThreads, kBytes, allow, known[ctas == 2 ? 0 : ctas == 4 ? 1 : 2]);
+}
+
 }  // namespace
 
 // How a call is shared out, and about how many us that takes: items have a beginning and an end of 5 (a kernel's first 11), a block of two tiles 1.9 and of one
-// 1.6; a cluster's join 3.  Measured (estimate in brackets), in clusters of four and by the other kernel at its best: 64 rows of 32 heads of 128, 355 tokens
+// 1.6; a cluster's join 3.  Clusters that do not all run at once take twice as long: 16 to 18 items of 1500 rows 35.5 us in eights, 20.9 in fours; 34 to 37 39.2 in fours,
+// 26.7 in pairs (this B200 runs 15 clusters of eight and 33 of four).  Measured (estimate in brackets), in clusters of four and by the other kernel at its best: 64 rows of 32 heads of 128, 355 tokens
 // 13.5 and 10.8 us (16), 1059 tokens 19.0 and 15.0 (18), 4195 tokens 29.4 and 31.1 (28); 256 rows, 1315 tokens 22.1 and 31.4 (20).  Items in turn: 512 of
 // 256 rows, 547 tokens 70.7 and 197 (58).
 struct TilesPlan {
@@ -936,7 +946,7 @@ static TilesPlan tiles_plan(const SeqArgs& a, int d) {
     if (!a.tree) span = std::min<int64_t>(span, (int64_t)a.n_sink + a.window + std::min(a.Tq, 2 * p.tokens));
     const int64_t blocks = (span + kBlock - 1) / kBlock;
     const int sms = std::min(sm_count(), kMaxReports);
-    while (p.ctas < kMostCtas && p.items * p.ctas * 2 <= sms && p.ctas * 2 <= blocks) p.ctas *= 2;
+    while (p.ctas < kMostCtas && p.items * p.ctas * 2 <= sms && p.ctas * 2 <= blocks && p.items <= clusters_that_run(p.ctas * 2)) p.ctas *= 2;
     const double block = a.Tq > p.tokens ? 1.9 : 1.6;
     p.us = p.items <= sms ? 11 + block * blocks / p.ctas + (p.ctas > 1 ? 3 : 0) : 6 + std::ceil((double)p.items / sms) * (5 + block * blocks);
     return p;

@@ -69,3 +69,30 @@ def test_infinite_keys_of_rows_that_are_seen(bad, d, B, H, R, Tq, N, kernel):
     nan = q[..., 2].float() * bad > 0
     assert nan.any() and torch.isnan(out[nan]).all() and torch.isnan(lse[nan]).all()
     assert ((out.double() - want).abs() <= tol)[~nan].all() and ((lse.double() - wlse).abs() <= lse_tol)[~nan].all()
+
+
+def _us(B, H, R, Tq, d, N):
+    rng, q, K, V = _case(N, B, H, R, Tq, d, N)
+    out, ws = torch.empty_like(q), vb.alloc_workspace(vb.OP_ATTENTION, B=B, H=H, N=N, d=d, Nv=Tq, D=H * R)
+    graph, times = torch.cuda.CUDAGraph(), []
+    vb.vitcop_window_attention(q, K, V, None, out, ws, d ** -0.5, NO_WINDOW)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        for _ in range(20):
+            vb.vitcop_window_attention(q, K, V, None, out, ws, d ** -0.5, NO_WINDOW)
+    for _ in range(8):
+        begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        begin.record()
+        graph.replay()
+        end.record()
+        torch.cuda.synchronize()
+        times.append(begin.elapsed_time(end) * 50)
+    return min(times)
+
+
+@pytest.mark.parametrize("heads", [(15, 16), (16, 17), (17, 18), (18, 19), (33, 34), (36, 37), (37, 38)])
+def test_a_head_more_does_not_bring_clusters_that_wait_for_others(heads):
+    """An item a head, a cluster an item: one that does not run beside the others begins when they end, and the call takes twice as long (smaller clusters, and the half of a
+    step of them: a head more may cost half as much again)."""
+    fewer, more = (_us(1, h, 1, 256, 128, 1500) for h in heads)
+    assert max(fewer, more) <= 1.5 * min(fewer, more)
