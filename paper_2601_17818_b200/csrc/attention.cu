@@ -415,11 +415,24 @@ int launch_few(const FewArgs& k, int64_t segs, cudaStream_t stream) {
     return k.a.tree ? launch_few<D, MT, true>(k, segs, stream) : launch_few<D, MT, false>(k, segs, stream);
 }
 
+// Clusters of c = 1 << log CTAs that run at a time (with either mask): not SMs / c, for a cluster stays inside a group of SMs.  (Where it cannot be told: one CTA an SM.)
+template <int D, int MT>
+int clusters_that_run(int log) {
+    static KnownOnDevice known[4];
+    static DoneOnDevice done;
+    constexpr int kBytes = FewSmem<D, MT>::kBytes;
+    const auto allow = [] { return allow_dynamic_smem(attention_few_kernel<D, MT, false>, kBytes, done); };
+    const int n = clusters_at_once(attention_few_kernel<D, MT, false>, 1 << log, kWarps * 32, kBytes, allow, known[log]);
+    return n > 0 ? n : std::max(1, sm_count() >> log);
+}
+
 // How a call is shared out, and about how many us that takes: a CTA begins and ends (with a cluster's join), and in between fetches and works on four
-// blocks of 16 tokens at a time.  Two CTAs fit an SM (one of 256-wide heads); clusters of eight are not all there at once beyond 128 CTAs.
-// Measured (in a graph; estimate in brackets), clusters of 1 / 2 / 4 / 8: 64 rows of 32 heads of 128, 355 tokens 13.1 / 10.9 / 10.8 / 18.4 us (12.6 / 10.6
-// / 11.4 / 24), 4195 tokens 78.6 / 44.1 / 31.1 / 41.1 (78 / 43 / 31 / 44); 7 rows of 64 heads, 4160 tokens 52.6 / 30.4 / 24.9 / 29.6 (52 / 28 / 21 / 29);
-// 256 rows of 32 heads of 64, 592 tokens 10.8 / 17.6 / 27.7 / 51.0 (11 / 16 / 26 / 60).
+// blocks of 16 tokens at a time, a fifth longer for each further CTA that its SM has; clusters that do not run at once come in rounds.
+// Measured (in a graph; estimate in brackets), clusters of 1 / 2 / 4 / 8, over 4160 tokens: rows of 16 heads of 64 29.3 / 17.4 / 10.9 / 8.0 us (29 / 16 / 9.9 / 7.8), of 128 56.3 /
+// 31.2 / 18.0 / 11.9 (52 / 28 / 16 / 12), of 256 75.4 / 41.2 / 23.4 / 27.6 (75 / 40 / 22 / 27: 15 clusters of eight run at once); of 24 heads of 128 56.4 / 31.2 / 18.0 / 12.9
+// (52 / 28 / 16 / 13); of 34 heads of 256 75.7 / 41.5 / 46.5 / 43.2 (75 / 40 / 44 / 39: 33 clusters of four).  32 rows of 16 heads of 64 41.6 / 24.6 / 15.1 / 11.4 (44 / 25 / 16 / 12),
+// of 128 74.7 / 42.4 / 25.1 / 17.8 (78 / 43 / 26 / 18).  25 rows of 32 heads of 128, 640 tokens: 10.7 in fours, 11.3 in eights (11.0 and 11.3).  64 rows of 32 heads of 128,
+// 355 tokens 13.1 / 10.9 / 10.8 / 18.4 (13 / 11 / 10 / 18); 7 rows of 64 heads, 4160 tokens 52.6 / 30.4 / 24.9 / 29.6 (52 / 28 / 19 / 24).
 struct FewPlan {
     int tile, ctas;
     int64_t tiles, segs;
@@ -434,18 +447,20 @@ FewPlan few_plan(const SeqArgs& a, int d) {
     // tokens that a tile's rows may see
     int64_t span = a.N;
     if (!a.tree) span = std::min<int64_t>(span, (int64_t)a.n_sink + a.window + p.tile / (int)a.R.d + 1);
-    const double rounds = (double)span / (kWarps * kBlock), begin = d == 64 ? 4.0 : p.tile == 32 ? 6.5 : 3.5;
-    const double round = d == 64 ? 0.62 : d == 128 && p.tile == 16 ? 0.75 : d == 128 ? 1.1 : 1.5;
-    const double sms = sm_count();
+    const bool wide = p.tile == 32;
+    const double rounds = (double)span / (kWarps * kBlock), begin = d == 64 ? (wide ? 4.0 : 2.5) : wide ? 6.5 : 3.5;
+    const double round = d == 64 ? (wide ? 0.62 : 0.41) : d == 128 && !wide ? 0.75 : 1.1;
+    const double sms = sm_count(), joins[2][4] = {{0.0, 0.25, 0.75, 2.0}, {0.0, 1.0, 1.5, 3.0}};
     p.us = 1e30;
     p.ctas = 1;
-    for (int c = 1; c <= kMostParts; c *= 2) {
-        const double n = (double)p.segs * c, slots = c == 8 ? 128 : d == 256 ? sms : 2 * sms;
-        const double join = c == 1 ? 0.0 : c == 2 ? 1.0 : c == 4 ? 3.0 : 8.0;
-        const double us = std::ceil(n / slots) * (begin + round * (n > sms ? 1.2 : 1.0) * rounds / c) + join * (p.tile == 32 ? 1.0 : 0.25);
+    for (int log = 0; 1 << log <= kMostParts; ++log) {
+        const int at_once = d == 256 ? clusters_that_run<256, 1>(log) : d == 128 ? (wide ? clusters_that_run<128, 2>(log) : clusters_that_run<128, 1>(log))
+                                                                                   : wide ? clusters_that_run<64, 2>(log) : clusters_that_run<64, 1>(log);
+        const double an_sm = std::ceil((double)(std::min<int64_t>(p.segs, at_once) << log) / sms);
+        const double us = std::ceil((double)p.segs / at_once) * (begin + round * (0.8 + 0.2 * an_sm) * rounds / (1 << log)) + joins[wide][log];
         if (us < p.us) {
             p.us = us;
-            p.ctas = c;
+            p.ctas = 1 << log;
         }
     }
     return p;

@@ -96,3 +96,9 @@ def test_a_head_more_does_not_bring_clusters_that_wait_for_others(heads):
     step of them: a head more may cost half as much again)."""
     fewer, more = (_us(1, h, 1, 256, 128, 1500) for h in heads)
     assert max(fewer, more) <= 1.5 * min(fewer, more)
+
+
+@pytest.mark.parametrize("d,fewer,more", [(256, 16, 24), (256, 34, 64), (128, 24, 34), (64, 24, 64)])
+def test_a_token_over_fewer_heads_takes_no_longer(d, fewer, more):
+    """The same of the kernel for few rows (4 % for the clock)."""
+    assert _us(1, fewer, 1, 1, d, 4160) <= 1.04 * _us(1, more, 1, 1, d, 4160)
