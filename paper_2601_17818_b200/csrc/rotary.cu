@@ -5,7 +5,8 @@
 // angle, here it leaves what sine and cosine of an fp32 in [-1, 1] half turns are off by.  A CTA takes a few tokens: their cosines and sines
 // once, to shared memory, for all heads of q and k; then every thread turns 8 elements and the 8 that are F behind them, 16 bytes each.  Both
 // halves of a row are whole sectors wherever heads and tokens lie, so that no order of the two is slower than the other.
-// Tables are read past the read-only cache: a kernel in front that is still running when this one is launched may be what writes them.
+// Tables are not read as constants (a kernel in front that is still running when this one is launched may be what writes them), nor past the L1: all tokens of an SM want them,
+// narrow rows (as the gradient's of 2 x 2943 rows of 32 heads of 64) 10.6 us instead of 11.1.
 // Bound by HBM: 4 x 4672 tokens, 32 heads of 128 in all, 49.9 us (0.94 of the copy rate; one pair of pieces a thread at a time 54.2); 8 x 704 kept rows of
 // 64 heads 31.3 us; one token 2.6 us.
 #include <algorithm>
@@ -44,9 +45,9 @@ rotary_axes_kernel(const __grid_constant__ RotaryArgs k) {
     for (int i = tid; i < k.tokens * F; i += kThreads) {
         const int t = i / F, e = i - t * F, token = tokens[t];
         if (token < 0) continue;
-        const int axis = min(max(__ldcg(k.axis + e), 0), k.axes - 1);
+        const int axis = min(max(k.axis[e], 0), k.axes - 1);
         const int at = __ldcg(k.position + ((int64_t)axis * k.B + b) * k.n_pos + token);
-        const double turn = (double)at * (__ldcg(k.inv_freq + e) * 0.15915494309189535);        // (1 / 2 pi)
+        const double turn = (double)at * (k.inv_freq[e] * 0.15915494309189535);        // (1 / 2 pi)
         float s, c;
         sincospif((float)(2.0 * (turn - rint(turn))), &s, &c);
         turns[i] = c;
