@@ -430,7 +430,8 @@ int vitcop_rotary_axes(const void* q, const void* k, int B, int Hq, int Hk, int 
 /* ---------------------------------------------------------------- attention over K and V in bf16
  * The paper has no counterpart.  out = softmax(scale * q K^T) V over the rows of K and V that a query sees, for the sequences that a pruning
  * step leaves: prompts, chunks of them, the tokens of a step.  Logits, maximum, sum and output are held in fp32, weights enter their
- * product in bf16.  Query head hq reads stored head hq / (Hq / H).  Query t of sample b, t < query_len[b], belongs to row
+ * product in bf16.  Sums of V do not pass V's own size, so that they are finite where V is; over up to 2^r rows out is off by up to 2^(2 r - 123) besides, which
+ * counts where V is below 2^-90 or so.  Query head hq reads stored head hq / (Hq / H).  Query t of sample b, t < query_len[b], belongs to row
  * p = cache_len[b] - query_len[b] + t of K and V (its own, which is there already).  Outputs of queries from query_len[b] on are left as they were.
  *   vitcop_window_attention  sees the rows j <= p with j < n_sink (first tokens that stay visible) or j > p - window
  *   vitcop_tree_attention    sees all rows j < cache_len[b] - query_len[b], and row cache_len[b] - query_len[b] + i (drafted token i < query_len[b])

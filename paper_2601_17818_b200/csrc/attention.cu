@@ -3,8 +3,8 @@
 //
 // The rows of a stored head are all its query heads' (i = t R + r), 16 or 32 of them a CTA.  m16n8k16 twice: logits z = q k of 16 tokens, whose
 // accumulators are, as they lie, the weights' operand of the second product.  A warp has tokens of its own, 16 at a time, which it fetches
-// three blocks ahead of their use, with a running maximum, sum and output of its own; a row's maximum is moved only when a logit has passed it
-// by 2^24.  Up to eight CTAs of a cluster share a head's tokens; warps are joined in shared memory, CTAs in that of the cluster, so that
+// three blocks ahead of their use, with a running maximum, sum and output of its own; a row's maximum is set high above the logits and moved only when one comes
+// near it.  Up to eight CTAs of a cluster share a head's tokens; warps are joined in shared memory, CTAs in that of the cluster, so that
 // there is one launch and nothing in global memory between.
 // Rows of V that are no numbers must not reach queries that do not see them, and 0 times NaN does: a block that is not seen by all rows is looked
 // through, and one that holds any is added token by token.
@@ -191,12 +191,12 @@ attention_few_kernel(const __grid_constant__ FewArgs k) {
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
             high[r] = x * a.scale_log2;                    // (0 times an infinite logit: no number, and none in the output)
-            passed |= high[r] > top[r];
+            passed |= high[r] > top[r] - a.room;
         }
         if (__any_sync(0xffffffffu, passed)) {
 #pragma unroll
             for (int r = 0; r < 2 * MT; ++r) {
-                const float now = high[r] > top[r] ? high[r] + kHeadroom : top[r], keep = ex2_approx(top[r] - now);
+                const float now = high[r] > top[r] - a.room ? high[r] + a.headroom : top[r], keep = ex2_approx(top[r] - now);
                 top[r] = now;
                 sum[r] *= keep;
                 weight[r] *= keep;
@@ -502,6 +502,11 @@ int launch_attention(const SeqRows& io, int B, int Hq, int H, int Tq, int d, int
     a.N = N;
     a.window = window;
     a.n_sink = n_sink;
+    const int64_t rows = std::max<int64_t>(1, tree ? N : std::min<int64_t>(N, (int64_t)window + n_sink));
+    int room = 1;
+    while (rows >> room) ++room;
+    a.room = (float)room;
+    a.headroom = (float)(room + kSlack);
     a.R = divisor(Hq / H);
     a.scale_log2 = std::fmax(std::fabs(scale) * kLog2e, 0x1p-149f);    // (0 times the -inf of a hidden row would be no number)
     a.sign = std::signbit(scale) ? 0x80008000u : 0u;

@@ -7,9 +7,11 @@
 
 namespace vitcop {
 
-// Weights are 2^(logit - top), top this much above the largest logit there was when it was set (in powers of two): it stays until a logit passes it, which few
-// do, and no weight is above 1.  (Values of V below 2^-100 or so lose bits for it.)
-constexpr float kHeadroom = 24.f;
+// Weights are 2^(logit - top), top `headroom` above the largest logit there was when it was set (in powers of two): it stays until a logit comes within `room` of it.
+// 2^room is more than the rows that a query may see, so that weights add up to no more than 1 and no sum is larger than V is.  Between the two lie kSlack powers of two, which few
+// logits cross (with 11 of them left: 7 % more time for prompts).  The largest weight may be 2^-headroom: a product with V is off by 2^-149 then, r rows of them by
+// r 2^(headroom - 149) of the output, which counts where V is below 2^-90 or so.
+constexpr int kSlack = 24;
 
 constexpr float kNothing = -1.f;                           // in place of what a part of a row counts by, where no part weighs anything
 
@@ -27,6 +29,7 @@ struct SeqArgs {
     int* status;
     int B, Hq, H, Tq, N, window, n_sink;
     Divisor R;                                             // query heads of a stored one
+    float room, headroom;
     float scale_log2;                                      // not below 0: the sign is the queries'
     uint32_t sign;                                         // 0x80008000 turns it
 };

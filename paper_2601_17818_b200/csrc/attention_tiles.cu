@@ -5,8 +5,8 @@
 // what a first block reaches back beyond its segment, or the sequence, is masked.  Of a block that a tile sees in part only the 32-token
 // columns that it sees are worked on.
 //   warps 0-3, 4-7  softmax of a tile, a thread a row: logits from tensor memory, weights back to where the logits were, as the operand of
-//                   the second product.  Weights are made by the maximum so far while the block's own is looked for; only when a logit has passed
-//                   it by 2^24 is it moved, the sums so far with it, and the weights are made anew
+//                   the second product.  Weights are made by the maximum so far, set high above the logits, while the block's own is looked for; only when a
+//                   logit comes near it is it moved, the sums so far with it, and the weights are made anew
 //   warp 8          tensor copies: queries, then K and V of a block in turn through a ring.  Rows of V that are no numbers must not reach rows that do
 //                   not see them, and 0 times NaN does: blocks that are masked are looked through, such rows taken out and added again at the end
 //                   for those who see them
@@ -426,8 +426,8 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                         for (int e = 0; e < 32; e += 2) h[e / 2 & 3] = fmaxf(h[e / 2 & 3], fmaxf(__uint_as_float(z[v][e]), __uint_as_float(z[v][e + 1])));
                 }
                 const float high = fmaxf(fmaxf(h[0], h[1]), fmaxf(h[2], h[3])) * a.scale_log2;
-                if (count == 0 || __any_sync(0xffffffffu, high > top)) {
-                    const float now = high > top ? high + kHeadroom : top, keep = ex2_approx(top - now);
+                if (count == 0 || __any_sync(0xffffffffu, high > top - a.room)) {
+                    const float now = high > top - a.room ? high + a.headroom : top, keep = ex2_approx(top - now);
                     top = now;
                     sum = mul2(sum, pack2(keep, keep));
                     if (count > 0) {                       // (the products so far have ended: the logits' came behind them)

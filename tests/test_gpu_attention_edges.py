@@ -102,3 +102,36 @@ def test_a_head_more_does_not_bring_clusters_that_wait_for_others(heads):
 def test_a_token_over_fewer_heads_takes_no_longer(d, fewer, more):
     """The same of the kernel for few rows (4 % for the clock)."""
     assert _us(1, fewer, 1, 1, d, 4160) <= 1.04 * _us(1, more, 1, 1, d, 4160)
+
+
+# (the same paths, with rows enough for a maximum that moves late)
+LATE = [(2, 100, 1, 1, 400, FEW), (2, 2, 2, 3, 600, FEW), (2, 8, 4, 300, 1500, MANY), (2, 1, 4, 300, 3000, MANY)]
+LATE = [(d, *path) for path in LATE for d in (64, 128, 256) if d < 256 or path[-1] is FEW]
+
+
+@pytest.mark.parametrize("rise", [10.0, 16.25, 16.5, 30.0])
+@pytest.mark.parametrize("d,B,H,R,Tq,N,kernel", LATE)
+def test_large_values_under_a_maximum_that_rises_late(rise, d, B, H, R, Tq, N, kernel):
+    """Logits of 0, then of ``rise`` (14 to 43 powers of two): the mean of rows of 2^127 is 2^127, however many of them weigh as much as one can."""
+    rng, q, K, V = _case(3, B, H, R, Tq, d, N)
+    q[..., 0], K[..., 0] = 1.0, rise
+    q[..., 1:], K[:, :, :200, 0] = 0.0, 0.0
+    V[:] = 2.0 ** 127
+    V[1, ..., ::2] *= -1
+    out, lse, names = _kernels_of(q, K, V, None, 1.0)
+    assert names == kernel
+    want, wlse, tol, lse_tol = _plain(q, K, V, torch.ones(B, H, N, dtype=torch.bool, device=DEV), 1.0)
+    assert ((out.double() - want).abs() <= tol).all() and ((lse.double() - wlse).abs() <= lse_tol).all()
+
+
+@pytest.mark.parametrize("power", [-80, -95])
+@pytest.mark.parametrize("d,B,H,R,Tq,N,kernel", LATE)
+def test_small_values_keep_their_digits(power, d, B, H, R, Tq, N, kernel):
+    """The largest weight may be 2^-(24 + b), b the bits of N, and a product with V, or a sum of them, is off by 2^-149 besides its own rounding: N 2^(b - 125) of the output
+    each."""
+    rng, q, K, V = _case(5, B, H, R, Tq, d, N)
+    V *= 2.0 ** power
+    out, lse, names = _kernels_of(q, K, V, None, d ** -0.5)
+    assert names == kernel
+    want, wlse, tol, lse_tol = _plain(q, K, V, torch.ones(B, H, N, dtype=torch.bool, device=DEV), d ** -0.5)
+    assert ((out.double() - want).abs() <= tol + N * 2.0 ** (N.bit_length() - 124)).all() and ((lse.double() - wlse).abs() <= lse_tol).all()
