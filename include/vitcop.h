@@ -416,7 +416,7 @@ int vitcop_cache_attention(const void* q, const void* cache, int B, int Hq, int 
  *   q_out, k_out  as q and k, strides of their own.  In place (same pointer and strides as the input) is fine; otherwise outputs must
  *              not share elements with inputs or one another.  (Two tensors may lie in one another's gaps, as q, k and v of one projection do,
  *              where the strides of their tokens are the same and those of their samples multiples of it.)
- * Errors: INVALID_ARG (negative sizes or strides, d 0, axes < 1, q and k both NULL, NULL position/inv_freq/axis, n_pos 0 or without token < N, overlap, rows of an
+ * Errors: INVALID_ARG (negative sizes or strides, d 0, axes < 1, q and k both NULL where there are rows, NULL position/inv_freq/axis, n_pos 0 or without token < N, overlap, rows of an
  * output that share elements), UNSUPPORTED (d % 8, d > 4096, n_freq % 8, 2 n_freq > d, n_freq > 256, alignment, B above 65535, Hq or Hk above 32767, more than
  * 2^31 - 2^16 rows of all heads), CUDA. */
 int vitcop_rotary_axes(const void* q, const void* k, int B, int Hq, int Hk, int N, int d,

@@ -624,7 +624,9 @@ int vitcop_rotary_axes(const void* q, const void* k, int B, int Hq, int Hk, int 
                        int inverse, void* q_out, int64_t qo_stride_b, int64_t qo_stride_h, int64_t qo_stride_t, void* k_out,
                        int64_t ko_stride_b, int64_t ko_stride_h, int64_t ko_stride_t, void* stream) {
     if (B < 0 || Hq < 0 || Hk < 0 || N < 0 || d <= 0 || axes < 1 || n_pos < 0 || n_freq < 0) return VITCOP_ERR_INVALID_ARG;
-    if ((!q && !k) || (q == nullptr) != (q_out == nullptr) || (k == nullptr) != (k_out == nullptr)) return VITCOP_ERR_INVALID_ARG;
+    // (tensors of no elements have no address)
+    const bool any = B > 0 && N > 0 && (int64_t)Hq + Hk > 0;
+    if ((!q && !k && any) || (q == nullptr) != (q_out == nullptr) || (k == nullptr) != (k_out == nullptr)) return VITCOP_ERR_INVALID_ARG;
     const int64_t strides[12] = {q_stride_b, q_stride_h, q_stride_t, qo_stride_b, qo_stride_h, qo_stride_t,
                                  k_stride_b, k_stride_h, k_stride_t, ko_stride_b, ko_stride_h, ko_stride_t};
     for (int i = 0; i < 12; ++i)

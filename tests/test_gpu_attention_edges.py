@@ -135,3 +135,13 @@ def test_small_values_keep_their_digits(power, d, B, H, R, Tq, N, kernel):
     assert names == kernel
     want, wlse, tol, lse_tol = _plain(q, K, V, torch.ones(B, H, N, dtype=torch.bool, device=DEV), d ** -0.5)
     assert ((out.double() - want).abs() <= tol + N * 2.0 ** (N.bit_length() - 124)).all() and ((lse.double() - wlse).abs() <= lse_tol).all()
+
+
+@pytest.mark.parametrize("B,Hq,Hk,N", [(0, 4, 2, 8), (2, 4, 2, 0), (2, 0, 2, 8), (2, 4, 0, 8), (2, 0, 0, 8)])
+def test_turning_tensors_of_no_elements(B, Hq, Hk, N):
+    rng = np.random.default_rng(1)
+    q, k = _bf16(rng, B, Hq, N, 64), _bf16(rng, B, Hk, N, 64)
+    qo, ko = torch.zeros_like(q), torch.zeros_like(k)
+    args = torch.zeros(1, B, N, dtype=torch.int32, device=DEV), torch.ones(32, dtype=torch.float64, device=DEV), torch.zeros(32, dtype=torch.int32, device=DEV)
+    vb.vitcop_rotary_axes(q, k, *args, qo, ko)
+    assert torch.equal(q, qo) and torch.equal(k, ko)      # (position 0 turns nothing)
