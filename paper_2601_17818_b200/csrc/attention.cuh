@@ -74,7 +74,7 @@ struct Seen<false> {
         if (t >= s.queries || s.base + t < 0) return;
         p = s.base + t;
         front = min(a.n_sink, p + 1);
-        lo = p - a.window + 1;                             // (p >= 0 and window <= 2^31 - 1: no overflow)
+        lo = max(0, p - a.window + 1);                     // (not below 0: places of rows are subtracted from it)
     }
     __device__ __forceinline__ bool operator()(int j) const { return j < front || (j >= lo && j <= p); }
 };

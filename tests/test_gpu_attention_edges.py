@@ -145,3 +145,13 @@ def test_turning_tensors_of_no_elements(B, Hq, Hk, N):
     args = torch.zeros(1, B, N, dtype=torch.int32, device=DEV), torch.ones(32, dtype=torch.float64, device=DEV), torch.zeros(32, dtype=torch.int32, device=DEV)
     vb.vitcop_rotary_axes(q, k, *args, qo, ko)
     assert torch.equal(q, qo) and torch.equal(k, ko)      # (position 0 turns nothing)
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 2, 2 ** 31 - 200, 2 ** 30])
+@pytest.mark.parametrize("B,H,R,Tq,N", [(16, 16, 1, 300, 300), (1, 2, 2, 5, 90)])
+def test_windows_near_the_end_of_32_bits(window, B, H, R, Tq, N):
+    """All of them are no window at all."""
+    rng, q, K, V = _case(2, B, H, R, Tq, 64, N)
+    out, lse, names = _kernels_of(q, K, V, None, 0.125, window, 0)
+    assert names == (MANY if Tq > 5 else FEW)
+    _check_long(q, K, V, [N] * B, [Tq] * B, 0.125, out, lse, window, 0)
