@@ -90,3 +90,16 @@ int main() {
     assert r.returncode == 0, r.stderr
     r = subprocess.run([program], capture_output=True, text=True, timeout=60)
     assert r.returncode == 0 and r.stdout.strip() == "0", (r.returncode, r.stdout)
+
+
+def test_hardly_anything_is_spilled():
+    """The kernel for many rows has no cache beside its shared memory: a reload takes some 600 cycles.  What the compiler says: a few words that are set once, in front of the
+    loops (more of them, or of the kernel for few rows, would be a row's)."""
+    import subprocess
+    from paper_2601_17818_b200 import build
+    for name, kernels, most in (("attention_tiles.cu", 4, 32), ("attention.cu", 10, 20)):
+        r = subprocess.run([build._nvcc(), *build.NVCC_FLAGS, "-Xptxas", "-v", "-cubin", os.path.join(build.CSRC, name), "-o", os.devnull], capture_output=True, text=True)
+        assert r.returncode == 0, r.stderr
+        said = re.findall(r"Compiling entry function '\S*attention_(?:few|tiles)_kernel\S*'.*?(\d+) bytes spill stores, (\d+) bytes spill loads", r.stderr, re.S)
+        assert len(said) == kernels
+        assert all(int(stores) <= most and int(loads) <= most for stores, loads in said), said

@@ -155,3 +155,96 @@ def test_windows_near_the_end_of_32_bits(window, B, H, R, Tq, N):
     out, lse, names = _kernels_of(q, K, V, None, 0.125, window, 0)
     assert names == (MANY if Tq > 5 else FEW)
     _check_long(q, K, V, [N] * B, [Tq] * B, 0.125, out, lse, window, 0)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_one_axis_is_the_table_of_the_key_projection(d):
+    """Keys turned by their projection, and keys projected and then turned.  The latter are rounded in front of the turn as well: half a place of |a| + |b|, next to the half
+    place of either result; the table is rounded to fp32, and so are the products (2^-20 of |a| + |b|)."""
+    B, N, Dh, H, F = 2, 75, 128, 3, d // 2
+    rng = np.random.default_rng(d)
+    hidden, W = _bf16(rng, B, N, Dh), _bf16(rng, H * d, Dh, spread=Dh ** -0.5)
+    position, f = rng.integers(0, 4000, (B, N)), 10000.0 ** (-np.arange(F) / F)
+    table = np.arange(4000)[:, None] * f
+    cos, sin = (torch.tensor(g(table), dtype=torch.float32, device=DEV) for g in (np.cos, np.sin))
+    ws = vb.alloc_workspace(vb.OP_KPROJ, B=B, H=H, N=N, d=d)
+    K, turned, of_axes = (torch.zeros(B, H, N, d, dtype=torch.bfloat16, device=DEV) for _ in range(3))
+    vb.vitcop_kproj_knorm(hidden, W, H, d, K, ws)
+    vb.vitcop_kproj_knorm(hidden, W, H, d, turned, ws, rope_cos=cos, rope_sin=sin, position_ids=_i32(position))
+    vb.vitcop_rotary_axes(None, K, _i32(position[None]), torch.tensor(f, dtype=torch.float64, device=DEV), _i32(np.zeros(F)), None, of_axes)
+    size = (K[..., :F].double().abs() + K[..., F:].double().abs()).repeat(1, 1, 1, 2)
+    tol = (HALF * (1 + HALF) + 2.0 ** -20) * size + HALF * (turned.double().abs() + of_axes.double().abs())
+    assert ((turned.double() - of_axes.double()).abs() <= tol).all()
+    assert not torch.equal(turned, K)
+
+
+def _turn(seed, B=2, Hq=4, Hk=2, N=90, d=64, F=32):
+    rng = np.random.default_rng(seed)
+    q, k, position = _bf16(rng, B, N, Hq, d).transpose(1, 2), _bf16(rng, B, Hk, N, d), _i32(rng.integers(0, 9000, (3, B, N)))
+    return q, k, position, torch.tensor(10000.0 ** (-np.arange(F) / F), dtype=torch.float64, device=DEV), _i32(np.arange(F) * 3 // F)
+
+
+def test_turning_on_two_streams_and_in_a_graph():
+    """Two streams at once; a captured turn, and the one back beside it, replayed on other rows and positions."""
+    cases = [_turn(s) for s in (1, 2)]
+    want = [vb.vitcop_rotary_axes(*c, *(torch.zeros_like(x) for x in c[:2])) for c in cases]
+    outs = [tuple(torch.zeros_like(x) for x in c[:2]) for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for c, o, s in zip(cases, outs, streams):
+            with torch.cuda.stream(s):
+                vb.vitcop_rotary_axes(*c, *o)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for o, w in zip(outs, want) for x, y in zip(o, w))
+    held, out, back = [x.clone() for x in cases[0]], [torch.zeros_like(x) for x in cases[0][:2]], [torch.zeros_like(x) for x in cases[0][:2]]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        vb.vitcop_rotary_axes(*held, *out)
+        vb.vitcop_rotary_axes(*out, *held[2:], *back, inverse=True)
+    for c, w in ((cases[1], want[1]), (cases[0], want[0])):
+        for x, y in zip(held, c):
+            x.copy_(y)
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y, z, b in zip(out, w, c[:2], back):
+            assert torch.equal(x, y)
+            # (two roundings of half a place, of the size of either element of a pair)
+            size = (z[..., :32].double().abs() + z[..., 32:].double().abs()).repeat(1, 1, 1, 2)
+            assert ((b.double() - z.double()).abs() <= 2 * HALF * size + 2.0 ** -20 * size).all()
+
+
+def test_tables_that_the_kernel_in_front_writes():
+    """Positions and frequencies of a turn come from the kernel right in front of it, which the turn may be launched beside; nothing waits between the calls."""
+    q, k, position, f, axis = _turn(3)
+    zeros = [torch.zeros_like(x) for x in (q, k)]
+    tables = [(position * n % 7000, f * (1 + n / 8), (axis + n) % 3) for n in range(1, 9)]
+    want = [[x.clone() for x in vb.vitcop_rotary_axes(q, k, *t, *zeros)] for t in tables]
+    held, outs = [x.clone() for x in tables[0]], [[torch.zeros_like(x) for x in (q, k)] for _ in tables]
+    torch.cuda.synchronize()
+    for t, o in zip(tables, outs):
+        for x, y in zip(held, t):
+            x.copy_(y)
+        vb.vitcop_rotary_axes(q, k, *held, *o)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for o, w in zip(outs, want) for x, y in zip(o, w))
+
+
+@pytest.mark.parametrize("Tq", [3, 300])
+def test_two_graphs_that_share_a_workspace(Tq):
+    """Replayed in turn on one stream, each in either order."""
+    B, H, R, d, N = 2, 2, 4, 128, 900
+    ws = vb.alloc_workspace(vb.OP_ATTENTION, B=B, H=H, N=N, d=d, Nv=Tq, D=H * R)
+    cases = [_case(s, B, H, R, Tq, d, N)[1:] for s in (1, 2)]
+    want = [_run(*c, None, 0.1, 500, 4)[0] for c in cases]
+    outs, graphs = [torch.zeros_like(c[0]) for c in cases], [torch.cuda.CUDAGraph() for _ in cases]
+    for c, o, g in zip(cases, outs, graphs):
+        with torch.cuda.graph(g):
+            vb.vitcop_window_attention(*c, None, o, ws, 0.1, 500, 4)
+    for order in ((0, 1), (1, 0), (0, 0, 1)):
+        for o in outs:
+            o.zero_()
+        for i in order:
+            graphs[i].replay()
+        assert vb.vitcop_poll_status(ws) == vb.OK
+        assert all(torch.equal(o, w) for o, w in zip(outs, want))
