@@ -3,15 +3,16 @@
 //
 // The rows of a stored head are all its query heads' (i = t R + r), 16 or 32 of them a CTA.  m16n8k16 twice: logits z = q k of 16 tokens, whose
 // accumulators are, as they lie, the weights' operand of the second product.  A warp has tokens of its own, 16 at a time, which it fetches
-// three blocks ahead of their use, with a running maximum, sum and output of its own; a row's maximum is set high above the logits and moved only when one comes
+// two blocks ahead of the one it works on, with a running maximum, sum and output of its own; a row's maximum is set high above the logits and moved only when one comes
 // near it.  Up to eight CTAs of a cluster share a head's tokens; warps are joined in shared memory, CTAs in that of the cluster, so that
 // there is one launch and nothing in global memory between.
 // Rows of V that are no numbers must not reach queries that do not see them, and 0 times NaN does: a block that is not seen by all rows is looked
 // through, and one that holds any is added token by token.
 // Weights enter the second product in bf16, and the output is divided by the sum of the weights as they were rounded, which takes the
 // roundings' common part out.
-// Bound by HBM where the tokens are many: 7 rows of 64 heads of 128, up to 4160 tokens each, in 25 us (0.84 of the copy rate).  By latency otherwise: a row of
-// 32 heads, 291 tokens, 5.5 us; 25 rows, 640 tokens, 10.7; 256 rows of 32 narrow heads, some 590 tokens, 10.6 (issue slots 35 % busy).
+// Bound by HBM where the tokens are many: 7 rows of 64 heads of 128, 4160 tokens each, in 25 us (0.83 of the copy rate; 64 heads more take 20 us more,
+// the copy rate, so that 5 or 6 are launch, first blocks and joins).  By latency otherwise: a row of
+// 32 heads, 291 tokens, 5.6 us; 25 rows, 640 tokens, 10.7; 256 rows of 32 narrow heads, some 590 tokens, 10.7 (issue slots 35 % busy).
 #include "attention.cuh"
 
 #include <algorithm>

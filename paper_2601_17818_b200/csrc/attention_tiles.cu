@@ -14,8 +14,8 @@
 // A CTA takes items in turn, the next item's first products under the last one's output.  Where items are fewer than SMs, a cluster of up to eight CTAs
 // shares an item's blocks and joins its parts in shared memory.
 // Bound by the chain of a tile, logits to weights to products, which one other tile does not fill, and tensor memory holds no third: some 3300 cycles for a
-// block of two tiles, of which the tensor cores work 2048 and the units of exponentials as many.  16512 tokens x 28 heads of 128, window 4096: 860-920 us
-// (0.94-1.0 PFLOP/s, at the power limit); 2 x 4672, window 1024: 181; 8 x up to 704 x 32 heads, window 256: 71, where items' beginnings and ends count.
+// block of two tiles, of which the tensor cores work 2048 and the units of exponentials as many.  16512 tokens x 28 heads of 128, window 4096: 870-930 us
+// (0.93-1.0 PFLOP/s, at the power limit), without a window 1902 (1.03); 2 x 4672, window 1024: 183; 8 x up to 704 x 32 heads, window 256: 71, where items' beginnings and ends count.
 // Weights enter the second product in bf16, the output is divided by the sum of the unrounded ones: 0.0019-0.0023 of the output's size from 64 bits.  (By
 // that of the rounded ones: 0.0018, 11 % more time.)
 #include "attention.cuh"
@@ -927,7 +927,9 @@ int clusters_that_run(int ctas) {
 // 1.6; a cluster's join 3.  Clusters that do not all run at once take twice as long: 16 to 18 items of 1500 rows 35.5 us in eights, 20.9 in fours; 34 to 37 39.2 in fours,
 // 26.7 in pairs (this B200 runs 15 clusters of eight and 33 of four).  Measured (estimate in brackets), in clusters of four and by the other kernel at its best: 64 rows of 32 heads of 128, 355 tokens
 // 13.5 and 10.8 us (16), 1059 tokens 19.0 and 15.0 (18), 4195 tokens 29.4 and 31.1 (28); 256 rows, 1315 tokens 22.1 and 31.4 (20).  Items in turn: 512 of
-// 256 rows, 547 tokens 70.7 and 197 (58).
+// 256 rows, 547 tokens 70.7 and 197 (58); 256 of 256 rows, 547 tokens 35.2 and 104.7 (35), of heads of 64 30.1 and 60.1 (35).  Heads of 64 are 0 to 17 % faster than heads of 128, and no
+// choice between the kernels hung on it: 64 rows of 64 heads, 4195 tokens 35.4 and 30.0 (40), 32 heads, 1500 tokens 17.2 and 21.2 (20), 300 rows of 32, 2000 tokens 25.9 and 47.4 (29).
+// 64 tokens x 28 heads over 16512 rows, clusters of eight: 51 and 91 (45).
 struct TilesPlan {
     int tokens, per_head, ctas;
     int64_t items;

@@ -4,11 +4,13 @@
 // a rotation).  Angles are taken in 64 bits, as turns of which the whole ones are dropped: a position of 20000 leaves fp32 three digits of its
 // angle, here it leaves what sine and cosine of an fp32 in [-1, 1] half turns are off by.  A CTA takes a few tokens: their cosines and sines
 // once, to shared memory, for all heads of q and k; then every thread turns 8 elements and the 8 that are F behind them, 16 bytes each.  Both
-// halves of a row are whole sectors wherever heads and tokens lie, so that no order of the two is slower than the other.
+// halves of a row are whole sectors wherever heads and tokens lie, as long as they are multiples of 32 bytes (8 frequencies, or a stride at an odd multiple of 16 bytes,
+// take twice the sectors), so that no order of the two is slower than the other.
 // Tables are not read as constants (a kernel in front that is still running when this one is launched may be what writes them), nor past the L1: all tokens of an SM want them,
 // narrow rows (as the gradient's of 2 x 2943 rows of 32 heads of 64) 10.6 us instead of 11.1.
-// Bound by HBM: 4 x 4672 tokens, 32 heads of 128 in all, 49.9 us (0.94 of the copy rate; one pair of pieces a thread at a time 54.2); 8 x 704 kept rows of
-// 64 heads 31.3 us; one token 2.6 us.
+// Bound by HBM: 4 x 4672 tokens, 32 heads of 128 in all, 49.7 us (0.94 of the copy rate; one pair of pieces a thread at a time 54.2); 8 x 704 kept rows of
+// 64 heads 31.2 us (0.90); one token 2.6 us.  Not by it where rows are few or narrow: 2 x 2943 rows of 32 heads of 64, half turned, 10.6 us (0.70), whose CTAs wait for token,
+// position and angles, one after the other, before their first row and then have two rounds of rows.
 #include <algorithm>
 
 #include <cuda_bf16.h>

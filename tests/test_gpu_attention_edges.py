@@ -100,8 +100,8 @@ def test_a_head_more_does_not_bring_clusters_that_wait_for_others(heads):
 
 @pytest.mark.parametrize("d,fewer,more", [(256, 16, 24), (256, 34, 64), (128, 24, 34), (64, 24, 64)])
 def test_a_token_over_fewer_heads_takes_no_longer(d, fewer, more):
-    """The same of the kernel for few rows (4 % for the clock)."""
-    assert _us(1, fewer, 1, 1, d, 4160) <= 1.04 * _us(1, more, 1, 1, d, 4160)
+    """The same of the kernel for few rows (8 % for the clock)."""
+    assert _us(1, fewer, 1, 1, d, 4160) <= 1.08 * _us(1, more, 1, 1, d, 4160)
 
 
 # (the same paths, with rows enough for a maximum that moves late)
