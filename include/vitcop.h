@@ -437,7 +437,8 @@ int vitcop_rotary_axes(const void* q, const void* k, int B, int Hq, int Hk, int 
  *   vitcop_tree_attention    sees all rows j < cache_len[b] - query_len[b], and row cache_len[b] - query_len[b] + i (drafted token i < query_len[b])
  *                            where bit i of tree[b][t] is set: t itself and its ancestors, for a tree
  * A query that sees no row, or stands in front of row 0, gets out = 0 and lse = -inf.  A logit of +inf or NaN makes its query's output NaN, one of -inf weighs
- * 0: out = 0 and lse = -inf where there is no other, whatever V holds there; else 0 times a value of V that is no number is none.  What stands in rows that a query does not see, NaN and infinities too, does not reach it.
+ * 0: out = 0 and lse = -inf where there is no other, whatever V holds there; else 0 times a value of V that is no number is none.  What stands in rows that a
+ * query does not see, NaN and infinities too, does not reach it.
  *   q, out   bf16 [B, Hq, Tq, d], element (b,h,t,e) at q + b*q_stride_b + h*q_stride_h + t*q_stride_t + e (strides in elements,
  *            multiples of 8, not negative); out must not overlap anything else
  *   K, V     bf16 [B, H, N, d], strides likewise
